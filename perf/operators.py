@@ -376,9 +376,9 @@ def _plain_select(st):
     k = min(K, c["V"])
     top, tok = top[..., :k], tok[..., :k]
     m = torch.where(torch.isfinite(top[..., :1]), top[..., :1], 0.0).to(F64)
-    lse = m + torch.log(torch.exp(x.to(F64) - m).sum(-1, keepdim=True))
+    log_sum = torch.log(torch.exp(x.to(F64) - m).sum(-1, keepdim=True))
     score = st["scores"].to(F64)[..., None]
-    total = score + (top.to(F64) - lse)
+    total = score + ((top.to(F64) - m) - log_sum)
     valid = torch.isfinite(top)
     first = torch.arange(k, device=x.device) == 0
     total = torch.where(done[..., None], score, total)
@@ -533,12 +533,12 @@ def exact(c, seed):
             if not len(ids):
                 continue
             x = logits[w][ids]
-            log_sum = float(np.max(x)) + math.log(float(np.sum(np.exp(x - np.max(x)))))
+            log_sum = math.log(float(np.sum(np.exp(x - np.max(x)))))
             enough = np.partition(x, -K)[-K] if len(x) > K else -np.inf
             near = np.flatnonzero(x >= enough)
             near = near[np.lexsort((ids[near], -x[near]))][:K]
             for r, i in enumerate(near):
-                total = score + (float(x[i]) - log_sum)
+                total = score + ((float(x[i]) - float(np.max(x))) - log_sum)
                 found.append((-total * float(max(n + 1, 1)) ** -c["alpha"], w, r, int(ids[i]), total, n + 1))
         for k, (_, w, _, token, total, n) in enumerate(sorted(found)[:K]):
             out["parents"][b, k], out["tokens"][b, k], out["out_scores"][b, k] = b * W + w, token, total
