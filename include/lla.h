@@ -24,6 +24,13 @@
  *                        per-head LLA with a decoupled rotary branch (one rotary key per token)
  *   lla_dense_*          the uncompressed loop-t KV decode in the same kernel style (the
  *                        "teacher" column of Table absorbed_latency, App. J), for comparison
+ *   lla_pages_fork, lla_pages_extend, lla_pages_free, lla_pages_compact
+ *                        sequences that share pages of any of these caches: forked and reordered,
+ *                        grown (copying a shared last page before it is written), freed, moved
+ *                        to the front of the pools
+ *   lla_beam_select, lla_beam_search
+ *                        the best continuations of the beams over the vocabulary, and the beam
+ *                        search loop over the calls above
  *
  * Attention reads the latents directly (App. J, "Absorbed attention"): the score is bilinear,
  * q . (W_up,t c) = (W_up,t^T q) . c, and the value path satisfies
@@ -84,6 +91,8 @@ typedef enum { LLA_BF16 = 0, LLA_F32 = 1 } lla_dtype;
 #define LLA_DEVERR_EMPTY_PASS2 0x4u /* pass 2 with an empty sequence (nothing to attend to) */
 #define LLA_DEVERR_TIMEOUT 0x8u     /* a bounded wait expired */
 #define LLA_DEVERR_SLOT 0x10u       /* an encode slot outside the pool */
+#define LLA_DEVERR_SEQUENCE 0x20u   /* a parent or a sequence number outside the batch */
+#define LLA_DEVERR_PAGES 0x40u      /* fewer free blocks than lla_pages_extend needs */
 
 /* Every wait of a kernel on its own pipeline (an mbarrier phase) gives up after this much global
  * time, sets LLA_DEVERR_TIMEOUT and lets the launch finish with undefined outputs. */
@@ -475,6 +484,191 @@ lla_status lla_dense_decode_attn(const lla_geometry *g, const lla_cache *cache,
                                  const void *q, const void *cur_k, const void *cur_v,
                                  lla_dtype io_dtype, void *out, void *workspace,
                                  size_t workspace_bytes, void *stream);
+
+/*
+ * Sequences that share pages.  A block belongs to every sequence whose block-table row holds it, and
+ * ref_count says to how many; a block of count 0 is free, and nothing else says so: there is no free
+ * list, and a new page is always the free block of the lowest number.  So block ids do not depend on
+ * the order in which threads run, and the pool stays packed towards its front.  Sequence s holds
+ * block_table[s][0 .. ceil(context_lens[s] / 64)); what its row has behind that is not read and, except
+ * for the pages it gets, not written.  All layers of a model share one lla_pages, as they share a table.
+ * The paper has no counterpart: its caches are fabricated (Sec. 7); this is what a serving program
+ * (parallel samples, beam search, shared prompts) needs around the calls above.
+ *
+ * With every count and length zero (cudaMemset) all blocks are free and all sequences empty.
+ */
+#define LLA_MAX_BLOCKS (1 << 24)
+#define LLA_MAX_POOLS 128
+
+typedef struct {
+    int32_t *ref_count;         /* device [num_blocks], 16-byte aligned */
+    int64_t num_blocks;         /* 1..LLA_MAX_BLOCKS (LLA_ERR_UNSUPPORTED beyond) */
+    int32_t *block_table;       /* device [S][max_blocks_per_seq] */
+    int32_t max_blocks_per_seq; /* 1..LLA_MAX_BLOCKS (LLA_ERR_UNSUPPORTED beyond) */
+    int32_t *context_lens;      /* device [S] */
+    int32_t S;                  /* sequences, 0..LLA_MAX_BATCH */
+} lla_pages;
+
+/* What the page calls copy: one pool of num_blocks blocks (lla_pages), of any cache of this library.
+ * A block is `pages` pages, each a K-plane of 64 rows of k_row_bytes (in granules of 16 bytes if
+ * k_row_bytes % 16 == 0, else 4) and a row-major V-plane of 64 rows of v_row_bytes.  Filled by
+ * lla_cache_pool, lla_cache_2d_pool or lla_rope_pool. */
+typedef struct {
+    void *base;          /* device, 16-byte aligned */
+    int32_t pages;       /* 1..4096 */
+    int32_t k_row_bytes; /* 4..8192, a multiple of 4 */
+    int32_t v_row_bytes; /* 0..8192, a multiple of 4 */
+} lla_pool;
+
+/* The pool of a per-head cache (lla_cache.pool), of an LLA-2D cache, and of rotary planes.  Host only. */
+lla_status lla_cache_pool(const lla_geometry *g, void *pool, lla_pool *out);
+lla_status lla_cache_2d_pool(const lla_geometry *g, void *pool, lla_pool *out);
+lla_status lla_rope_pool(int32_t d_rope, void *rope_pool, lla_pool *out);
+
+/*
+ * Fork and reorder: sequence s of `to` becomes a copy of sequence parents[s] of `from`, sharing all of
+ * its pages, or an empty one where parents[s] is -1.  A parent may be named any number of times; the
+ * pages of one that is not named lose its reference, and are free if it was the last.  This is the
+ * reordering of states after lla_beam_select, the parallel samples of a prompt, and the removal of
+ * ended sequences from a batch, in one call.
+ *   from, to   two views of the same ref_count and num_blocks, with different block_table and
+ *              context_lens arrays (LLA_ERR_INVALID_ARG where they overlap); `from` holds nothing
+ *              after the call, although its arrays are left as they are: its next use is as a `to`
+ *   parents    device [to->S] int32; one outside [-1, from->S) sets LLA_DEVERR_SEQUENCE and counts as -1
+ * A parent of more pages than to->max_blocks_per_seq sets LLA_DEVERR_CONTEXT, and its children are empty.
+ */
+lla_status lla_pages_fork(const lla_pages *from, const lla_pages *to, const int32_t *parents,
+                          void *stream);
+
+/* Workspace bytes lla_pages_extend needs for S sequences.  Host only. */
+lla_status lla_pages_extend_workspace_size(int32_t S, size_t *bytes);
+
+/*
+ * Growth: context_lens[s] += n_s, with a page for every new token, and their slots.  A last page that
+ * is not full and that another sequence holds too is copied before it is written: the sequence gets a
+ * block of its own with the page's context_lens[s] % 64 rows in every pool (the block's other rows are
+ * left as they are).  Where all holders of such a page grow in the call, the lowest of them keeps it.
+ *   pools, L      host array of the L pools (0..LLA_MAX_POOLS) whose rows are copied: every layer's, and
+ *                 its rotary planes where it has them; each has pages->num_blocks blocks
+ *   slot_mapping  device [N] int64, written: the slot of each new token as the encodes take it, or -1
+ *                 (a token to skip) for a sequence that does not grow
+ *   cu_new        device [S + 1] int32 prefix sums of n_s (packed, as cu_seqlens), or NULL: every n_s is
+ *                 N / S (then N must be a multiple of S).  Slots behind cu_new[S] are -1
+ *   skip          device [S] uint8 or NULL: a sequence with a value other than 0 does not grow
+ *   lens_before   device [S] int32 or NULL, written: the lengths before the call (what pass 1 of a decode
+ *                 attends to)
+ *   free_blocks   device int32 or NULL, written: the free blocks that remain
+ * All or nothing: with too few free blocks for the whole call LLA_DEVERR_PAGES is set, no length, table or
+ * count changes, and every slot is -1.  A sequence whose length or growth is out of range
+ * (LLA_DEVERR_CONTEXT) or whose last page is no block (LLA_DEVERR_BLOCK_ID) does not grow.
+ * Two kernels on the stream.  The workspace (device, 16-byte aligned) needs no initialisation; calls that
+ * share it must be ordered.
+ */
+lla_status lla_pages_extend(const lla_pages *pages, const lla_pool *pools, int32_t L,
+                            int64_t *slot_mapping, int32_t N, const int32_t *cu_new,
+                            const uint8_t *skip, int32_t *lens_before, int32_t *free_blocks,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Frees the pages of n sequences (0..LLA_MAX_BATCH): their blocks lose a reference, their lengths become 0.
+ *   seqs  device [n] int32 sequence numbers; a negative one is skipped, one >= S sets LLA_DEVERR_SEQUENCE,
+ *         and one that is named twice is freed once
+ */
+lla_status lla_pages_free(const lla_pages *pages, const int32_t *seqs, int32_t n, void *stream);
+
+/* Workspace bytes lla_pages_compact needs for num_blocks blocks.  Host only. */
+lla_status lla_pages_compact_workspace_size(int64_t num_blocks, size_t *bytes);
+
+/*
+ * Compaction: afterwards the R blocks in use are the blocks 0..R-1, so that the rest of every pool can be
+ * given to something else.  Only blocks from R on move (the k-th of them to the k-th free block below R,
+ * whole, in every pool), and the tables of `pages` and ref_count follow.
+ *   pages  holds every table of the ledger; a table that it does not hold is renamed with `remap`
+ *   remap  device [num_blocks] int32, written: the new number of every block, -1 for a free one
+ *   live   device int32, written: R
+ * Two kernels on the stream; the workspace as for lla_pages_extend.
+ */
+lla_status lla_pages_compact(const lla_pages *pages, const lla_pool *pools, int32_t L, int32_t *remap,
+                             int32_t *live, void *workspace, size_t workspace_bytes, void *stream);
+
+#define LLA_MAX_BEAMS 32
+#define LLA_MAX_VOCAB (1 << 24)
+
+/* Workspace bytes lla_beam_select needs.  Host only. */
+lla_status lla_beam_select_workspace_size(int32_t B, int32_t W, int32_t V, int32_t K,
+                                          lla_dtype logits_dtype, size_t *bytes);
+
+/*
+ * Beam search's selection: for each of B sequences the K best continuations of its W beams over a
+ * vocabulary of V tokens.  Token v continues beam w of score s_w at
+ *   s = s_w + z_v - log sum_u exp z_u
+ * over the beam's finite logits z (a logit that is infinite or NaN masks its token).  Continuations are
+ * ranked by s n^-length_penalty, n the hypothesis' tokens after the step; s and the ranking are computed in 64 bits
+ * (from a sum of exponentials held in more than 32).  Within a beam the order is that of the logits; ties
+ * go to the lower beam, within a beam to the lower token.  A beam whose score is not finite has no
+ * continuation; a finished one has one: itself, with token eos, at its score and length.
+ *   logits        device [B][W] rows of V, row_stride elements apart (>= V), logits_dtype; element-aligned
+ *   scores        device [B][W] fp32: the beams' sums of log probabilities
+ *   finished      device [B][W] uint8 or NULL (none is): beams that ended
+ *   lengths       device [B][W] int32 or NULL: tokens of each hypothesis so far; NULL (then length_penalty
+ *                 must be 0 and out_lengths NULL)
+ *   eos           the token that ends a hypothesis, or -1
+ *   length_penalty  -16..16; 0 ranks by s
+ *   parents       device [B][K] int32, written: b W + w, the beam that each continues (lla_pages_fork's
+ *                 parents when K = W), best first; -1 where there are fewer than K
+ *   tokens        device [B][K] int32, written (-1 where parents is)
+ *   out_scores    device [B][K] fp32, written: s, rounded once (-inf where parents is -1)
+ *   out_finished  device [B][K] uint8 or NULL, written: 1 where the token is eos or parents is -1, else 0
+ *   out_lengths   device [B][K] int32 or NULL, written (0 where parents is -1)
+ * W, K <= LLA_MAX_BEAMS, B W <= LLA_MAX_BATCH, V <= LLA_MAX_VOCAB.  No output may overlap an input.  Two
+ * kernels on the stream; the workspace as for lla_pages_extend.
+ */
+lla_status lla_beam_select(int32_t B, int32_t W, int32_t V, int32_t K, const void *logits,
+                           int64_t row_stride, lla_dtype logits_dtype, const float *scores,
+                           const uint8_t *finished, const int32_t *lengths, int32_t eos,
+                           float length_penalty, int32_t *parents, int32_t *tokens, float *out_scores,
+                           uint8_t *out_finished, int32_t *out_lengths, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
+/*
+ * Callback of lla_beam_search, called on the calling host thread: enqueues the model's step `step` on
+ * `stream` and sets *logits (and *row_stride, preset to V) to the B W rows of its logits.  The beams' new
+ * tokens are `tokens`; pass 1 of the decode attends to lens_before[s] cached tokens of pages->block_table,
+ * the encode takes `slots`, and after it pages->context_lens[s] tokens are cached.  Returns LLA_OK, or
+ * another status to stop the search (lla_beam_search then returns it).
+ */
+typedef lla_status (*lla_step_fn)(int32_t step, const lla_pages *pages, const int32_t *lens_before,
+                                  const int32_t *tokens, const int64_t *slots, const void **logits,
+                                  int64_t *row_stride, void *stream, void *user);
+
+/* Workspace bytes lla_beam_search needs.  Host only. */
+lla_status lla_beam_search_workspace_size(int32_t B, int32_t W, int32_t V, lla_dtype logits_dtype,
+                                          size_t *bytes);
+
+/*
+ * Beam search of B sequences with W beams each over `steps` steps: host orchestration of this library's
+ * kernels on `stream`.  Step i is lla_pages_extend by one token (finished beams do not grow), the caller's
+ * model, lla_beam_select with K = W, lla_pages_fork by its parents.
+ *   pages_a, pages_b  two page sets as lla_pages_fork takes them, S = B W; sequence b W + w is beam w of
+ *                     sequence b.  Step i runs on pages_a where i is even, on pages_b where it is odd;
+ *                     before the call pages_a holds the prompts without their last token (a fork of every
+ *                     prompt into its W beams), after it pages_(steps even ? a : b) holds the beams
+ *   tokens, scores, finished, lengths
+ *                     device [steps + 1][B][W] (int32, fp32, uint8, int32): slab i is the input of step
+ *                     i, slab i + 1 its selection.  The caller fills slab 0: the prompts' last tokens,
+ *                     score 0 for one beam of a sequence and -inf for the others, zeros
+ *   parents           device [steps][B][W] int32, written: the beam of slab i that each of slab i + 1
+ *                     continues; a hypothesis is read by walking back from its beam in the last slab
+ *   pools, L          as lla_pages_extend
+ * The error behaviour of each step is that of its call; the first non-OK status is returned (the work
+ * enqueued before it stays enqueued).  The workspace as for lla_pages_extend.
+ */
+lla_status lla_beam_search(const lla_pages *pages_a, const lla_pages *pages_b, const lla_pool *pools,
+                           int32_t L, int32_t B, int32_t W, int32_t V, lla_dtype logits_dtype,
+                           int32_t steps, int32_t eos, float length_penalty, int32_t *tokens,
+                           float *scores, uint8_t *finished, int32_t *lengths, int32_t *parents,
+                           lla_step_fn step, void *user, void *workspace, size_t workspace_bytes,
+                           void *stream);
 
 /*
  * Reads the sticky device error word of the current device after synchronising `stream`.

@@ -589,6 +589,171 @@ lla_status lla_prefill_attn_rope(const lla_geometry *g, const lla_codec *codec,
                                workspace_bytes, static_cast<cudaStream_t>(stream));
 }
 
+namespace {
+
+lla_status check_pages(const lla_pages *p) {
+    if (!p || p->num_blocks < 1 || p->max_blocks_per_seq < 1 || p->S < 0 || p->S > LLA_MAX_BATCH) return LLA_ERR_INVALID_ARG;
+    if (p->num_blocks > LLA_MAX_BLOCKS || p->max_blocks_per_seq > LLA_MAX_BLOCKS) return LLA_ERR_UNSUPPORTED;
+    if (!p->ref_count || !aligned(p->ref_count, 16)) return LLA_ERR_INVALID_ARG;
+    if (p->S > 0 && (!p->block_table || !p->context_lens)) return LLA_ERR_INVALID_ARG;
+    return LLA_OK;
+}
+
+lla_status check_pools(const lla_pool *pools, int32_t L) {
+    if (L < 0 || (L > 0 && !pools)) return LLA_ERR_INVALID_ARG;
+    if (L > LLA_MAX_POOLS) return LLA_ERR_UNSUPPORTED;
+    for (int32_t l = 0; l < L; ++l) {
+        const lla_pool &p = pools[l];
+        if (!p.base || !aligned(p.base, 16) || p.pages < 1 || p.pages > 4096) return LLA_ERR_INVALID_ARG;
+        if (p.k_row_bytes < 4 || p.k_row_bytes > 8192 || p.k_row_bytes % 4 != 0) return LLA_ERR_INVALID_ARG;
+        if (p.v_row_bytes < 0 || p.v_row_bytes > 8192 || p.v_row_bytes % 4 != 0) return LLA_ERR_INVALID_ARG;
+    }
+    return LLA_OK;
+}
+
+bool overlap(const void *a, size_t na, const void *b, size_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return na > 0 && nb > 0 && x < y + nb && y < x + na;
+}
+
+lla_status pool_of_geometry(const lla_geometry *g, int max_rank, int pages, void *pool, lla_pool *out) {
+    const lla_status st = check_geometry(g, max_rank);
+    if (st != LLA_OK) return st;
+    if (!pool || !aligned(pool, 16) || !out) return LLA_ERR_INVALID_ARG;
+    *out = lla_pool{pool, pages, g->r_k * elem_size(g->storage), g->r_v * elem_size(g->storage)};
+    return LLA_OK;
+}
+
+}  // namespace
+
+lla_status lla_cache_pool(const lla_geometry *g, void *pool, lla_pool *out) {
+    return pool_of_geometry(g, kMaxRank, g ? g->H : 0, pool, out);
+}
+
+lla_status lla_cache_2d_pool(const lla_geometry *g, void *pool, lla_pool *out) {
+    return pool_of_geometry(g, kMaxRank2D, 1, pool, out);
+}
+
+lla_status lla_rope_pool(int32_t d_rope, void *rope_pool, lla_pool *out) {
+    size_t bytes = 0;
+    const lla_status st = lla_rope_plane_bytes(d_rope, &bytes);
+    if (st != LLA_OK) return st;
+    if (!rope_pool || !aligned(rope_pool, 16) || !out) return LLA_ERR_INVALID_ARG;
+    *out = lla_pool{rope_pool, 1, d_rope * 2, 0};
+    return LLA_OK;
+}
+
+lla_status lla_pages_fork(const lla_pages *from, const lla_pages *to, const int32_t *parents, void *stream) {
+    lla_status st = check_pages(from);
+    if (st != LLA_OK) return st;
+    if ((st = check_pages(to)) != LLA_OK) return st;
+    if (from->ref_count != to->ref_count || from->num_blocks != to->num_blocks) return LLA_ERR_INVALID_ARG;
+    if (to->S > 0 && !parents) return LLA_ERR_INVALID_ARG;
+    const size_t ft = static_cast<size_t>(from->S) * from->max_blocks_per_seq * 4, fl = static_cast<size_t>(from->S) * 4;
+    const size_t tt = static_cast<size_t>(to->S) * to->max_blocks_per_seq * 4, tl = static_cast<size_t>(to->S) * 4;
+    if (overlap(from->block_table, ft, to->block_table, tt) || overlap(from->context_lens, fl, to->context_lens, tl) ||
+        overlap(parents, tl, to->block_table, tt) || overlap(parents, tl, to->context_lens, tl))
+        return LLA_ERR_INVALID_ARG;
+    if (from->S + to->S == 0) return LLA_OK;
+    return launch_pages_fork(*from, *to, parents, static_cast<cudaStream_t>(stream));
+}
+
+lla_status lla_pages_extend_workspace_size(int32_t S, size_t *bytes) {
+    if (!bytes || S < 0 || S > LLA_MAX_BATCH) return LLA_ERR_INVALID_ARG;
+    *bytes = pages_extend_workspace_bytes();
+    return LLA_OK;
+}
+
+lla_status lla_pages_extend(const lla_pages *pages, const lla_pool *pools, int32_t L, int64_t *slot_mapping, int32_t N,
+                            const int32_t *cu_new, const uint8_t *skip, int32_t *lens_before, int32_t *free_blocks,
+                            void *workspace, size_t workspace_bytes, void *stream) {
+    lla_status st = check_pages(pages);
+    if (st != LLA_OK) return st;
+    if ((st = check_pools(pools, L)) != LLA_OK) return st;
+    if (N < 0 || (N > 0 && !slot_mapping)) return LLA_ERR_INVALID_ARG;
+    if (!cu_new && (pages->S == 0 ? N != 0 : N % pages->S != 0)) return LLA_ERR_INVALID_ARG;
+    // with no sequence there is no token, and cu_new is one zero: every slot of a padded mapping is a token to skip
+    if (pages->S == 0) {
+        if (N > 0 && cudaMemsetAsync(slot_mapping, 0xff, static_cast<size_t>(N) * 8, static_cast<cudaStream_t>(stream)) != cudaSuccess)
+            return LLA_ERR_CUDA;
+        if (!free_blocks) return LLA_OK;
+    }
+    if (!workspace || !aligned(workspace, 16)) return LLA_ERR_INVALID_ARG;
+    if (workspace_bytes < pages_extend_workspace_bytes()) return LLA_ERR_WORKSPACE;
+    return launch_pages_extend(*pages, pools, L, slot_mapping, pages->S == 0 ? 0 : N, cu_new, skip, lens_before, free_blocks,
+                               workspace, static_cast<cudaStream_t>(stream));
+}
+
+lla_status lla_pages_free(const lla_pages *pages, const int32_t *seqs, int32_t n, void *stream) {
+    const lla_status st = check_pages(pages);
+    if (st != LLA_OK) return st;
+    if (n < 0 || n > LLA_MAX_BATCH || (n > 0 && !seqs)) return LLA_ERR_INVALID_ARG;
+    if (n == 0) return LLA_OK;
+    return launch_pages_free(*pages, seqs, n, static_cast<cudaStream_t>(stream));
+}
+
+lla_status lla_pages_compact_workspace_size(int64_t num_blocks, size_t *bytes) {
+    if (!bytes || num_blocks < 1) return LLA_ERR_INVALID_ARG;
+    if (num_blocks > LLA_MAX_BLOCKS) return LLA_ERR_UNSUPPORTED;
+    *bytes = pages_compact_workspace_bytes(num_blocks);
+    return LLA_OK;
+}
+
+lla_status lla_pages_compact(const lla_pages *pages, const lla_pool *pools, int32_t L, int32_t *remap, int32_t *live,
+                             void *workspace, size_t workspace_bytes, void *stream) {
+    lla_status st = check_pages(pages);
+    if (st != LLA_OK) return st;
+    if ((st = check_pools(pools, L)) != LLA_OK) return st;
+    if (!remap || !live || !workspace || !aligned(workspace, 16)) return LLA_ERR_INVALID_ARG;
+    if (workspace_bytes < pages_compact_workspace_bytes(pages->num_blocks)) return LLA_ERR_WORKSPACE;
+    return launch_pages_compact(*pages, pools, L, remap, live, workspace, static_cast<cudaStream_t>(stream));
+}
+
+namespace {
+
+lla_status check_beams(int32_t B, int32_t W, int32_t V, int32_t K, lla_dtype dtype) {
+    if (B < 0 || W < 1 || V < 1 || K < 1 || !valid_dtype(dtype)) return LLA_ERR_INVALID_ARG;
+    if (W > LLA_MAX_BEAMS || K > LLA_MAX_BEAMS || V > LLA_MAX_VOCAB) return LLA_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(B) * W > LLA_MAX_BATCH) return LLA_ERR_INVALID_ARG;
+    return LLA_OK;
+}
+
+}  // namespace
+
+lla_status lla_beam_select_workspace_size(int32_t B, int32_t W, int32_t V, int32_t K, lla_dtype logits_dtype, size_t *bytes) {
+    const lla_status st = check_beams(B, W, V, K, logits_dtype);
+    if (st != LLA_OK) return st;
+    if (!bytes) return LLA_ERR_INVALID_ARG;
+    *bytes = beam_select_workspace_bytes(B, W, V, K, logits_dtype == LLA_BF16);
+    return LLA_OK;
+}
+
+lla_status lla_beam_select(int32_t B, int32_t W, int32_t V, int32_t K, const void *logits, int64_t row_stride,
+                           lla_dtype logits_dtype, const float *scores, const uint8_t *finished, const int32_t *lengths,
+                           int32_t eos, float length_penalty, int32_t *parents, int32_t *tokens, float *out_scores,
+                           uint8_t *out_finished, int32_t *out_lengths, void *workspace, size_t workspace_bytes,
+                           void *stream) {
+    const lla_status st = check_beams(B, W, V, K, logits_dtype);
+    if (st != LLA_OK) return st;
+    if (row_stride < V || row_stride > (int64_t(1) << 40) || eos < -1 || eos >= V) return LLA_ERR_INVALID_ARG;
+    if (!(length_penalty >= -16.f && length_penalty <= 16.f)) return LLA_ERR_INVALID_ARG;
+    if (!lengths && (length_penalty != 0.f || out_lengths)) return LLA_ERR_INVALID_ARG;
+    if (B == 0) return LLA_OK;
+    if (!logits || !aligned(logits, elem_size(logits_dtype)) || !scores || !parents || !tokens || !out_scores)
+        return LLA_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 16)) return LLA_ERR_INVALID_ARG;
+    if (workspace_bytes < beam_select_workspace_bytes(B, W, V, K, logits_dtype == LLA_BF16)) return LLA_ERR_WORKSPACE;
+    BeamSelectArgs a = {};
+    a.B = B; a.W = W; a.V = V; a.K = K; a.bf16 = logits_dtype == LLA_BF16;
+    a.logits = logits; a.row_stride = row_stride;
+    a.scores = scores; a.finished = finished; a.lengths = lengths;
+    a.eos = eos; a.length_penalty = length_penalty;
+    a.parents = parents; a.tokens = tokens; a.out_scores = out_scores;
+    a.out_finished = out_finished; a.out_lengths = out_lengths;
+    a.workspace = workspace;
+    return launch_beam_select(a, static_cast<cudaStream_t>(stream));
+}
+
 lla_status lla_get_device_error(void *stream, uint32_t *word) {
     if (!word) return LLA_ERR_INVALID_ARG;
     lla_status st = LLA_OK;

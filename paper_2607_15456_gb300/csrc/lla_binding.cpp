@@ -14,6 +14,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -30,6 +31,7 @@ struct Names {
     PyObject *T, *H, *d, *r_k, *r_v, *storage, *scale;
     PyObject *codec[6];
     PyObject *pool, *num_blocks, *block_table, *max_blocks;
+    PyObject *ref_count, *context_lens, *address, *count, *blocks, *device;
 } names;
 
 struct Unusual {};  // thrown to leave for the Python path
@@ -317,11 +319,152 @@ PyObject *prefill_attn_rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// The page and beam calls: tensors of one type and shape on the current device.
+const at::Tensor &typed(PyObject *o, at::ScalarType type) {
+    const at::Tensor &t = tensor(o);
+    if (t.scalar_type() != type || t.get_device() != c10::cuda::current_device()) throw Unusual();
+    return t;
+}
+template <typename P>
+P *typed_ptr(PyObject *o, at::ScalarType type, int64_t n) {  // n elements in one dimension, or None
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = typed(o, type);
+    if (t.dim() != 1 || t.size(0) != n) throw Unusual();
+    return static_cast<P *>(t.data_ptr());
+}
+template <typename P>
+P *typed_ptr(PyObject *o, at::ScalarType type, int64_t n0, int64_t n1) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = typed(o, type);
+    if (t.dim() != 2 || t.size(0) != n0 || t.size(1) != n1) throw Unusual();
+    return static_cast<P *>(t.data_ptr());
+}
+const at::Tensor &scratch(PyObject *o) {
+    const at::Tensor &t = tensor(o);
+    if (t.get_device() != c10::cuda::current_device()) throw Unusual();
+    return t;
+}
+int32_t size32(int64_t n) {
+    if (n > std::numeric_limits<int32_t>::max()) throw Unusual();
+    return static_cast<int32_t>(n);
+}
+lla_pages pages(PyObject *o) {
+    const Ref rc(PyObject_GetAttr(o, names.ref_count)), bt(PyObject_GetAttr(o, names.block_table)),
+        cl(PyObject_GetAttr(o, names.context_lens));
+    const at::Tensor &r = typed(rc.o, at::kInt), &t = typed(bt.o, at::kInt);
+    if (r.dim() != 1 || t.dim() != 2) throw Unusual();
+    lla_pages p;
+    p.ref_count = static_cast<int32_t *>(r.data_ptr());
+    p.num_blocks = r.size(0);
+    p.block_table = static_cast<int32_t *>(t.data_ptr());
+    p.max_blocks_per_seq = size32(t.size(1));
+    p.S = size32(t.size(0));
+    p.context_lens = typed_ptr<int32_t>(cl.o, at::kInt, p.S);
+    return p;
+}
+struct PoolArray {
+    const lla_pool *p;
+    int32_t L;
+};
+PoolArray pools(PyObject *o, const lla_pages &p) {  // lla.Pools, whose array lives as long as it does
+    const Ref ad(PyObject_GetAttr(o, names.address)), n(PyObject_GetAttr(o, names.count)),
+        bl(PyObject_GetAttr(o, names.blocks)), dv(PyObject_GetAttr(o, names.device));
+    PoolArray a = {reinterpret_cast<const lla_pool *>(static_cast<intptr_t>(integer(ad.o))), integer32(n.o)};
+    if (integer(bl.o) < p.num_blocks || (a.L > 0 && integer32(dv.o) != c10::cuda::current_device())) throw Unusual();
+    return a;
+}
+
+PyObject *pages_fork(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 4, [&] {
+        const lla_pages from = pages(a[0]), to = pages(a[1]);
+        const auto *parents = typed_ptr<int32_t>(a[2], at::kInt, to.S);
+        void *st = stream_of(a[3]);
+        NoGil nogil;
+        return lla_pages_fork(&from, &to, parents, st);
+    });
+}
+
+PyObject *pages_extend(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 9, [&] {
+        const lla_pages p = pages(a[0]);
+        const PoolArray ps = pools(a[1], p);
+        const at::Tensor &slots = typed(a[2], at::kLong), &ws = scratch(a[3]);
+        const int32_t N = size32(slots.numel());
+        auto *sp = static_cast<int64_t *>(slots.data_ptr());
+        const auto *cu = typed_ptr<int32_t>(a[4], at::kInt, p.S + 1);
+        const auto *skip = typed_ptr<uint8_t>(a[5], at::kByte, p.S);
+        auto *before = typed_ptr<int32_t>(a[6], at::kInt, p.S), *free_blocks = typed_ptr<int32_t>(a[7], at::kInt, 1);
+        void *w = ws.data_ptr();
+        const size_t wb = nbytes(ws);
+        void *st = stream_of(a[8]);
+        NoGil nogil;
+        return lla_pages_extend(&p, ps.p, ps.L, sp, N, cu, skip, before, free_blocks, w, wb, st);
+    });
+}
+
+PyObject *pages_free(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 3, [&] {
+        const lla_pages p = pages(a[0]);
+        const at::Tensor &seqs = typed(a[1], at::kInt);
+        const int32_t count = size32(seqs.numel());
+        const auto *sp = static_cast<const int32_t *>(seqs.data_ptr());
+        void *st = stream_of(a[2]);
+        NoGil nogil;
+        return lla_pages_free(&p, sp, count, st);
+    });
+}
+
+PyObject *pages_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 6, [&] {
+        const lla_pages p = pages(a[0]);
+        const PoolArray ps = pools(a[1], p);
+        auto *remap = typed_ptr<int32_t>(a[2], at::kInt, p.num_blocks), *live = typed_ptr<int32_t>(a[3], at::kInt, 1);
+        const at::Tensor &ws = scratch(a[4]);
+        void *w = ws.data_ptr();
+        const size_t wb = nbytes(ws);
+        void *st = stream_of(a[5]);
+        NoGil nogil;
+        return lla_pages_compact(&p, ps.p, ps.L, remap, live, w, wb, st);
+    });
+}
+
+PyObject *beam_select(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 13, [&] {
+        if (!THPVariable_CheckExact(a[0])) throw Unusual();
+        const at::Tensor &z = THPVariable_Unpack(a[0]);  // rows may be padded
+        if (!z.defined() || !z.is_cuda() || z.get_device() != c10::cuda::current_device() || z.dim() != 3) throw Unusual();
+        const int64_t B = z.size(0), W = z.size(1), V = z.size(2);
+        const int64_t rows = W > 1 ? z.stride(1) : B > 1 ? z.stride(0) : V;
+        if ((V > 1 && z.stride(2) != 1) || (B > 1 && W > 1 && z.stride(0) != W * rows)) throw Unusual();
+        const at::Tensor &par = typed(a[2], at::kInt), &ws = scratch(a[5]);
+        if (par.dim() != 2 || par.size(0) != B) throw Unusual();
+        const int64_t K = par.size(1);
+        const int32_t b = size32(B), w = size32(W), v = size32(V), k = size32(K);
+        const auto *scores = typed_ptr<float>(a[1], at::kFloat, B, W);
+        auto *parents = static_cast<int32_t *>(par.data_ptr()), *tokens = typed_ptr<int32_t>(a[3], at::kInt, B, K);
+        auto *out_scores = typed_ptr<float>(a[4], at::kFloat, B, K);
+        const auto *finished = typed_ptr<uint8_t>(a[6], at::kByte, B, W);
+        const auto *lengths = typed_ptr<int32_t>(a[7], at::kInt, B, W);
+        auto *out_finished = typed_ptr<uint8_t>(a[8], at::kByte, B, K);
+        auto *out_lengths = typed_ptr<int32_t>(a[9], at::kInt, B, K);
+        const int32_t eos = integer32(a[10]);
+        const float alpha = static_cast<float>(real(a[11]));
+        const lla_dtype zd = dtype(z);
+        void *zp = z.data_ptr(), *wp = ws.data_ptr();
+        const size_t wb = nbytes(ws);
+        void *st = stream_of(a[12]);
+        NoGil nogil;
+        return lla_beam_select(b, w, v, k, zp, rows, zd, scores, finished, lengths, eos, alpha, parents, tokens, out_scores,
+                               out_finished, out_lengths, wp, wb, st);
+    });
+}
+
 #define LLA_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     LLA_METHOD(decode_attn), LLA_METHOD(decode_attn_2d), LLA_METHOD(decode_attn_loops), LLA_METHOD(decode_attn_rope),
     LLA_METHOD(decode_attn_decoupled), LLA_METHOD(encode), LLA_METHOD(encode_2d), LLA_METHOD(encode_layers),
-    LLA_METHOD(prefill_attn), LLA_METHOD(prefill_attn_rope), {nullptr, nullptr, 0, nullptr}};
+    LLA_METHOD(prefill_attn), LLA_METHOD(prefill_attn_rope), LLA_METHOD(pages_fork), LLA_METHOD(pages_extend),
+    LLA_METHOD(pages_free), LLA_METHOD(pages_compact), LLA_METHOD(beam_select), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lla_native", "Native marshalling of the calls of lla.py.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
@@ -332,6 +475,7 @@ PyMODINIT_FUNC PyInit__lla_native() {
     auto s = [](const char *t) { return PyUnicode_InternFromString(t); };
     names = Names{s("T"), s("H"), s("d"), s("r_k"), s("r_v"), s("storage"), s("scale"),
                   {s("w_down_k"), s("w_down_v"), s("w_up_k"), s("w_up_v"), s("mu_k"), s("mu_v")},
-                  s("pool"), s("num_blocks"), s("block_table"), s("max_blocks_per_seq")};
+                  s("pool"), s("num_blocks"), s("block_table"), s("max_blocks_per_seq"),
+                  s("ref_count"), s("context_lens"), s("address"), s("count"), s("blocks"), s("device")};
     return PyModule_Create(&module);
 }

@@ -140,6 +140,35 @@ lla_status launch_rope_key_store(int d_rope, double base, int pairing, void *rop
                                  const void *k, int x_bf16, const int32_t *positions, const int64_t *slots,
                                  int N, cudaStream_t stream);
 
+// Sequences that share pages (lla_pages.cu): launches behind the checks of lla_abi.cu (no empty batch).
+lla_status launch_pages_fork(const lla_pages &from, const lla_pages &to, const int32_t *parents, cudaStream_t stream);
+lla_status launch_pages_free(const lla_pages &p, const int32_t *seqs, int n, cudaStream_t stream);
+size_t pages_extend_workspace_bytes();
+lla_status launch_pages_extend(const lla_pages &p, const lla_pool *pools, int L, int64_t *slots, int N, const int32_t *cu_new,
+                               const uint8_t *skip, int32_t *lens_before, int32_t *free_blocks, void *workspace,
+                               cudaStream_t stream);
+size_t pages_compact_workspace_bytes(int64_t num_blocks);
+lla_status launch_pages_compact(const lla_pages &p, const lla_pool *pools, int L, int32_t *remap, int32_t *live, void *workspace,
+                                cudaStream_t stream);
+// The selection of the next beams (lla_beam.cu).
+struct BeamSelectArgs {
+    int B, W, V, K, bf16;
+    const void *logits;
+    int64_t row_stride;
+    const float *scores;
+    const uint8_t *finished;
+    const int32_t *lengths;
+    int eos;
+    float length_penalty;
+    int32_t *parents, *tokens;
+    float *out_scores;
+    uint8_t *out_finished;
+    int32_t *out_lengths;
+    void *workspace;
+};
+size_t beam_select_workspace_bytes(int B, int W, int V, int K, bool bf16);
+lla_status launch_beam_select(const BeamSelectArgs &a, cudaStream_t stream);
+
 int num_sms();  // SM count of the current device (cached), 0 on failure
 
 // Per-device flags of a one-time kernel set-up.  Host threads that race on a first call both

@@ -1,0 +1,712 @@
+// lla_pages.cu -- sequences that share pages of the paged caches: fork, growth, freeing and compaction
+// (lla_pages_*).  The ledger is ref_count alone: block b is free where ref_count[b] is 0, and a new page is
+// always the free block of the lowest number.  So every result is a function of the inputs, whatever order
+// threads run in: counts are integer sums, block ids are ranks from prefix sums.
+//
+// What bounds these calls is latency (a table row of the headline batch is 200 bytes, the ledger of a
+// 280 GB pool of 24 layers 90 KB) until pages are copied; the copies are bound by HBM.
+#include <cooperative_groups.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "lla_device.cuh"
+#include "lla_internal.h"
+#include "lla_units.cuh"
+
+namespace lla {
+namespace {
+
+namespace cg = cooperative_groups;
+
+// Pages that hold `len` tokens (0 <= len <= 64 * LLA_MAX_BLOCKS).
+__device__ __forceinline__ int pages_of(int len) {
+    return static_cast<int>((static_cast<unsigned>(len) + kBlockTokens - 1) / kBlockTokens);
+}
+
+// A sequence's length if its table row can hold it, else -1.
+__device__ __forceinline__ int checked_len(int len, int max_blocks) {
+    return len >= 0 && len <= static_cast<int64_t>(max_blocks) * kBlockTokens ? len : -1;
+}
+
+// ------------------------------------------------------------------------------------------------ fork
+
+constexpr int kForkThreads = 128;
+constexpr int kForkSpan = 1024;  // table entries of a CTA
+
+struct ForkArgs {
+    int32_t *ref;
+    int nb;
+    const int32_t *from_table, *from_lens;
+    int from_max, from_S;
+    int32_t *to_table, *to_lens;
+    int to_max, to_S;
+    const int32_t *parents;
+    unsigned *err;
+};
+
+// Rows 0 .. to_S-1 of the grid copy a child's table; rows to_S .. to_S+from_S-1 change the counts of a parent's
+// pages by its children - 1, once for all of its children, and not at all for the usual parent of one child.
+__global__ void __launch_bounds__(kForkThreads) fork_kernel(const ForkArgs a) {
+    pdl_wait();
+    pdl_trigger();
+    const int tid = threadIdx.x;
+    unsigned bad = 0;
+    if (static_cast<int>(blockIdx.x) < a.to_S) {
+        const int s = blockIdx.x;
+        const int p = a.parents[s];
+        int len = 0;
+        if (p < -1 || p >= a.from_S) {
+            bad = LLA_DEVERR_SEQUENCE;
+        } else if (p >= 0) {
+            len = checked_len(a.from_lens[p], a.from_max);
+            if (len < 0 || pages_of(len) > a.to_max) {
+                bad = LLA_DEVERR_CONTEXT;
+                len = 0;
+            }
+        }
+        const int n = pages_of(len);
+        const int32_t *src = a.from_table + static_cast<int64_t>(p < 0 ? 0 : p) * a.from_max;
+        int32_t *dst = a.to_table + static_cast<int64_t>(s) * a.to_max;
+        for (int lo = blockIdx.y * kForkSpan; lo < n; lo += gridDim.y * kForkSpan) {
+            const int hi = min(n, lo + kForkSpan);
+            int v[kForkSpan / kForkThreads];
+#pragma unroll
+            for (int j = 0; j < kForkSpan / kForkThreads; ++j)
+                if (lo + tid + j * kForkThreads < hi) v[j] = src[lo + tid + j * kForkThreads];
+#pragma unroll
+            for (int j = 0; j < kForkSpan / kForkThreads; ++j)
+                if (lo + tid + j * kForkThreads < hi) dst[lo + tid + j * kForkThreads] = v[j];
+        }
+        if (blockIdx.y == 0 && tid == 0) {
+            a.to_lens[s] = len;
+            if (bad) atomicOr(a.err, bad);
+        }
+        return;
+    }
+    const int p = blockIdx.x - a.to_S;
+    const int n = pages_of(max(0, checked_len(a.from_lens[p], a.from_max)));
+    if (static_cast<int>(blockIdx.y) * kForkSpan >= n) return;
+    int change = -1;
+    if (n <= a.to_max)
+        for (int i = 0; i < a.to_S; i += kForkThreads)
+            change += __syncthreads_count(i + tid < a.to_S && a.parents[i + tid] == p);
+    const int32_t *row = a.from_table + static_cast<int64_t>(p) * a.from_max;
+    for (int lo = blockIdx.y * kForkSpan + tid; lo < n; lo += gridDim.y * kForkSpan) {
+        const int hi = min(n, lo - tid + kForkSpan);
+#pragma unroll 4
+        for (int i = lo; i < hi; i += kForkThreads) {
+            const int b = row[i];
+            if (b < 0 || b >= a.nb)
+                bad = LLA_DEVERR_BLOCK_ID;
+            else if (change)
+                atomicAdd(a.ref + b, change);
+        }
+    }
+    if (bad) atomicOr(a.err, bad);
+}
+
+// ------------------------------------------------------------------------------------------------ free
+
+constexpr int kFreeThreads = 256;
+
+// One CTA per listed sequence.  The exchange of the length makes a second mention of a sequence find it empty.
+__global__ void __launch_bounds__(kFreeThreads)
+free_kernel(int32_t *ref, int nb, const int32_t *table, int max_blocks, int32_t *lens, int S, const int32_t *seqs,
+            unsigned *err) {
+    __shared__ int held;
+    pdl_wait();
+    pdl_trigger();
+    const int s = seqs[blockIdx.x];
+    if (s < 0) return;
+    if (s >= S) {
+        if (threadIdx.x == 0) atomicOr(err, LLA_DEVERR_SEQUENCE);
+        return;
+    }
+    if (threadIdx.x == 0) {
+        const int len = checked_len(atomicExch(lens + s, 0), max_blocks);
+        if (len < 0) atomicOr(err, LLA_DEVERR_CONTEXT);
+        held = pages_of(max(0, len));
+    }
+    __syncthreads();
+    const int n = held;
+    const int32_t *row = table + static_cast<int64_t>(s) * max_blocks;
+    bool bad = false;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += kFreeThreads) {
+        const int b = row[i];
+        if (b < 0 || b >= nb)
+            bad = true;
+        else
+            atomicSub(ref + b, 1);
+    }
+    if (bad) atomicOr(err, LLA_DEVERR_BLOCK_ID);
+}
+
+// ------------------------------------------------------------------------------- prefix sums of a cluster
+
+constexpr int kPlanThreads = 1024;  // a sequence each, too
+static_assert(kPlanThreads == LLA_MAX_BATCH, "thread s plans sequence s");
+
+// Exclusive prefix sum over a CTA's threads and the CTA's total.  `part` has 33 entries; a barrier on both sides.
+template <typename T>
+__device__ __forceinline__ T block_scan(T v, T *part, T &total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    T inc = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const T u = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += u;
+    }
+    __syncthreads();  // part is free
+    if (lane == 31) part[warp] = inc;
+    __syncthreads();
+    if (warp == 0) {
+        T w = part[lane];
+        T winc = w;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const T u = __shfl_up_sync(0xffffffffu, winc, o);
+            if (lane >= o) winc += u;
+        }
+        part[lane] = winc - w;
+        if (lane == 31) part[32] = winc;
+    }
+    __syncthreads();
+    total = part[32];
+    return part[warp] + inc - v;
+}
+
+// The ledger entries [begin, end) of a thread of the cluster: consecutive entries to consecutive threads, a
+// multiple of four each, so that they are read in 16-byte words.
+struct Segment {
+    int begin, end;
+};
+__device__ __forceinline__ Segment my_segment(int nb, int rank, int ctas) {
+    const int threads = ctas * kPlanThreads;
+    const int per = ((nb + threads - 1) / threads + 3) & ~3;
+    const int64_t b = static_cast<int64_t>(rank * kPlanThreads + threadIdx.x) * per;
+    Segment s;
+    s.begin = static_cast<int>(b < nb ? b : nb);
+    s.end = static_cast<int>(b + per < nb ? b + per : nb);
+    return s;
+}
+// f(id, count) for the entries of a segment, in order.
+template <typename F>
+__device__ __forceinline__ void for_ledger(const int32_t *ref, Segment s, F f) {
+    int i = s.begin;
+    for (; i + 4 <= s.end; i += 4) {
+        const int4 v = *reinterpret_cast<const int4 *>(ref + i);
+        f(i, v.x);
+        f(i + 1, v.y);
+        f(i + 2, v.z);
+        f(i + 3, v.w);
+    }
+    for (; i < s.end; ++i) f(i, ref[i]);
+}
+
+// Sums `mine` over the CTAs of the cluster: what the CTAs before this one have, and all.  A cluster barrier lies in
+// it: what any CTA did before the call is done after it.  Every CTA must have started (a barrier of the cluster
+// before), since its shared memory is written.
+struct ClusterSums {
+    int before, all;
+};
+__device__ __forceinline__ ClusterSums cluster_sums(int mine, int *totals /* shared, 16 */) {
+    cg::cluster_group cl = cg::this_cluster();
+    const int rank = static_cast<int>(cl.block_rank()), n = static_cast<int>(cl.num_blocks());
+    if (threadIdx.x < static_cast<unsigned>(n)) cl.map_shared_rank(totals, threadIdx.x)[rank] = mine;
+    cl.sync();
+    ClusterSums s = {0, 0};
+    for (int r = 0; r < n; ++r) {
+        if (r < rank) s.before += totals[r];
+        s.all += totals[r];
+    }
+    return s;
+}
+
+// ---------------------------------------------------------------------------------------------- extend
+
+struct ExtendCopy {  // one page to copy: `rows` rows of block src to block dst
+    int src, dst, rows, unused;
+};
+// The workspace: what the plan tells the kernel behind it.
+struct ExtendPlan {
+    int copies, unused[3];
+    ExtendCopy copy[LLA_MAX_BATCH];
+    int grow[LLA_MAX_BATCH];    // tokens that sequence s gets
+    int before[LLA_MAX_BATCH];  // its length before the call
+};
+
+struct ExtendArgs {
+    int32_t *ref;
+    int nb;
+    int32_t *table;
+    int max_blocks;
+    int32_t *lens;
+    int S;
+    const int32_t *cu_new;
+    int N, per;
+    const uint8_t *skip;
+    int32_t *lens_before, *free_blocks;
+    ExtendPlan *plan;
+    unsigned *err;
+};
+
+// The plan of a growth, by one cluster.  Thread s of every CTA works out sequence s (the CTAs do the same sums: it
+// is less than passing them on), all threads count the free blocks of their part of the ledger, and after the
+// cluster's exchange of counts each free block whose rank is below the need knows its sequence by a binary search.
+// Everything that is read and later changed (lengths, counts, last pages) is read before that exchange.
+__global__ void __launch_bounds__(kPlanThreads) extend_plan_kernel(const ExtendArgs a) {
+    constexpr int kSlots = 2 * LLA_MAX_BATCH;
+    __shared__ int key[kSlots], growers[kSlots], lowest[kSlots];
+    __shared__ int first[LLA_MAX_BATCH];  // blocks that sequences before s take
+    __shared__ int old_pages[LLA_MAX_BATCH], copy_of[LLA_MAX_BATCH];
+    __shared__ unsigned long long part64[33];
+    __shared__ int part[33], totals[16];
+    cg::cluster_group cl = cg::this_cluster();
+    const int tid = threadIdx.x, rank = static_cast<int>(cl.block_rank()), ctas = static_cast<int>(cl.num_blocks());
+    for (int i = tid; i < kSlots; i += kPlanThreads) {
+        key[i] = -1;
+        growers[i] = 0;
+        lowest[i] = kSlots;
+    }
+    cl.sync();  // every CTA has started
+    pdl_wait();
+    pdl_trigger();
+    // sequence tid: its growth, and whether others hold its last page
+    int len = 0, n = 0, tail = -1, holders = 0;
+    unsigned bad = 0;
+    if (tid < a.S) {
+        len = a.lens[tid];
+        int64_t asked = a.per;
+        bool in_range = true;
+        if (a.cu_new) {
+            const int64_t c0 = a.cu_new[tid], c1 = a.cu_new[tid + 1];
+            asked = c1 - c0;
+            in_range = c0 >= 0 && asked >= 0 && c1 <= a.N;
+        }
+        if (a.skip && a.skip[tid]) asked = 0;
+        if (!in_range || checked_len(len, a.max_blocks) < 0 ||
+            len + asked > static_cast<int64_t>(a.max_blocks) * kBlockTokens) {
+            bad = LLA_DEVERR_CONTEXT;
+            asked = 0;
+        }
+        n = static_cast<int>(asked);
+        if (n > 0 && len % kBlockTokens) {
+            tail = a.table[static_cast<int64_t>(tid) * a.max_blocks + len / kBlockTokens];
+            if (tail < 0 || tail >= a.nb) {
+                bad = LLA_DEVERR_BLOCK_ID;
+                n = 0;
+            } else {
+                holders = a.ref[tail];
+            }
+        }
+    }
+    if (bad && rank == 0) atomicOr(a.err, bad);
+    __syncthreads();
+    int slot = 0;
+    const bool shared_tail = n > 0 && holders > 1;
+    if (shared_tail) {  // the growing holders of a page meet in a hash table: their number and the lowest of them
+        slot = (static_cast<unsigned>(tail) * 2654435769u) >> 21;  // golden-ratio hashing to 2048 slots
+        for (;;) {
+            const int was = atomicCAS(&key[slot], -1, tail);
+            if (was == -1 || was == tail) break;
+            slot = (slot + 1) % kSlots;
+        }
+        atomicAdd(&growers[slot], 1);
+        atomicMin(&lowest[slot], tid);
+    }
+    __syncthreads();
+    const int copy = shared_tail && !(growers[slot] >= holders && lowest[slot] == tid);
+    const int rows = len % kBlockTokens;
+    unsigned long long need = 0, all = 0;
+    if (n > 0) need = static_cast<unsigned long long>(pages_of(len + n) - pages_of(len) + copy);
+    // copies in the high bits: at most 2^10, and at most 2^10 * 2^24 blocks in the low ones
+    const unsigned long long at = block_scan<unsigned long long>(need | static_cast<unsigned long long>(copy) << 40, part64, all);
+    const unsigned long long low40 = (1ull << 40) - 1;
+    const int64_t wanted = static_cast<int64_t>(all & low40);
+    // a need beyond the ledger is not granted, so that what is used of `first` is below 2^24
+    const int copy_index = static_cast<int>(at >> 40);
+    first[tid] = static_cast<int>(min(static_cast<unsigned long long>(LLA_MAX_BLOCKS) * 2, at & low40));
+    old_pages[tid] = n > 0 ? pages_of(len) : 0;
+    copy_of[tid] = copy ? copy_index : -1;
+    // free blocks of my part of the ledger (none needed and none asked for: no need to look)
+    const Segment seg = my_segment(a.nb, rank, ctas);
+    int mine = 0, cta_free = 0;
+    if (wanted > 0 || a.free_blocks)
+        for_ledger(a.ref, seg, [&](int, int count) { mine += count == 0; });
+    const int before_me = block_scan<int>(mine, part, cta_free);
+    const ClusterSums free = cluster_sums(cta_free, totals);
+    const bool granted = wanted <= free.all || wanted == 0;
+    if (rank == 0) {
+        if (tid < a.S) {
+            if (a.lens_before) a.lens_before[tid] = len;
+            a.plan->grow[tid] = granted ? n : 0;
+            a.plan->before[tid] = len;
+            if (granted && n > 0) a.lens[tid] = len + n;
+            if (granted && copy) {
+                ExtendCopy *c = &a.plan->copy[copy_index];
+                c->src = tail;
+                c->rows = rows;
+                atomicSub(a.ref + tail, 1);
+            }
+        }
+        if (tid == 0) {
+            a.plan->copies = granted ? static_cast<int>(all >> 40) : 0;
+            if (a.free_blocks) *a.free_blocks = free.all - (granted ? static_cast<int>(wanted) : 0);
+            if (!granted) atomicOr(a.err, LLA_DEVERR_PAGES);
+        }
+    }
+    if (!granted || wanted == 0) return;
+    // the k-th free block: to sequence s = the last with first[s] <= k
+    int k = free.before + before_me;
+    if (k >= wanted) return;
+    for_ledger(a.ref, seg, [&](int id, int count) {
+        if (count != 0) return;
+        if (k < wanted) {
+            int lo = 0, hi = a.S - 1;  // first[lo] <= k
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (first[mid] <= k) lo = mid;
+                else hi = mid - 1;
+            }
+            const int i = k - first[lo], c = copy_of[lo];
+            // the copied last page comes first, then the fresh ones
+            a.table[static_cast<int64_t>(lo) * a.max_blocks + old_pages[lo] + i - (c >= 0)] = id;
+            if (c >= 0 && i == 0) a.plan->copy[c].dst = id;
+            a.ref[id] = 1;
+        }
+        ++k;
+    });
+}
+
+// Up to LLA_MAX_POOLS pools; first[l] is the number of pages that a block has in the pools before l.
+struct PoolSet {
+    lla_pool p[LLA_MAX_POOLS];
+    int first[LLA_MAX_POOLS + 1];
+    int L;
+};
+
+__device__ __forceinline__ int pool_of(const PoolSet &ps, int unit) {
+    int lo = 0, hi = ps.L - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (ps.first[mid] <= unit) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+constexpr int kCopyThreads = 256;
+
+// Words of T that a warp moves, kAhead loads in flight per lane: n words, word w at byte offset at(w) of both sides.
+template <typename T, int kAhead, typename F>
+__device__ __forceinline__ void warp_copy(char *dst, const char *src, int n, F at) {
+    const int lane = threadIdx.x & 31;
+    for (int w0 = lane; w0 < n; w0 += 32 * kAhead) {
+        T v[kAhead];
+        int off[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (w0 + 32 * j < n) {
+                off[j] = at(w0 + 32 * j);
+                v[j] = *reinterpret_cast<const T *>(src + off[j]);
+            }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (w0 + 32 * j < n) *reinterpret_cast<T *>(dst + off[j]) = v[j];
+    }
+}
+
+// Behind the plan: the rows of copied pages in every pool, a warp per (copy, page), and the slots of the new tokens.
+// Of a page only the rows that hold tokens are read and written: the first `rows` of each K granule, and a prefix of
+// the V-plane.
+__global__ void __launch_bounds__(kCopyThreads, 4)
+extend_finish_kernel(const ExtendArgs a, const __grid_constant__ PoolSet ps, int64_t *slots) {
+    pdl_wait();
+    pdl_trigger();
+    const ExtendPlan *plan = a.plan;
+    const int per_copy = ps.first[ps.L];
+    const int64_t units = static_cast<int64_t>(plan->copies) * per_copy;
+    const int warps = gridDim.x * (kCopyThreads / 32);
+    for (int64_t u = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); u < units; u += warps) {
+        const int c = static_cast<int>(u / per_copy), in_copy = static_cast<int>(u - static_cast<int64_t>(c) * per_copy);
+        const int l = pool_of(ps, in_copy), page = in_copy - ps.first[l];
+        const int kb = ps.p[l].k_row_bytes, vb = ps.p[l].v_row_bytes, rows = plan->copy[c].rows;
+        const int64_t page_bytes = static_cast<int64_t>(kBlockTokens) * (kb + vb);
+        char *base = static_cast<char *>(ps.p[l].base) + page * page_bytes;
+        const char *src = base + plan->copy[c].src * (page_bytes * ps.p[l].pages);
+        char *dst = base + plan->copy[c].dst * (page_bytes * ps.p[l].pages);
+        // word w of the K-plane is row w % rows of granule w / rows: (w + 1/2) / rows is at least 1/126 away from a
+        // whole number and at most 2048, where two roundings of fp32 are off by less than 2^-11
+        const float inv = 1.f / static_cast<float>(rows);
+        if (kb % 16 == 0)
+            warp_copy<uint4, 8>(dst, src, kb / 16 * rows, [&](int w) {
+                const int g = static_cast<int>((static_cast<float>(w) + 0.5f) * inv);
+                return (g * kBlockTokens + (w - g * rows)) * 16;
+            });
+        else
+            warp_copy<uint32_t, 8>(dst, src, kb / 4 * rows, [&](int w) {
+                const int g = static_cast<int>((static_cast<float>(w) + 0.5f) * inv);
+                return (g * kBlockTokens + (w - g * rows)) * 4;
+            });
+        const int v0 = kBlockTokens * kb, words = vb * rows / 16, rest = vb * rows % 16 / 4;
+        warp_copy<uint4, 8>(dst, src, words, [&](int w) { return v0 + w * 16; });
+        warp_copy<uint32_t, 1>(dst, src, rest, [&](int w) { return v0 + words * 16 + w * 4; });
+    }
+    const int threads = gridDim.x * kCopyThreads;
+    for (int i = blockIdx.x * kCopyThreads + threadIdx.x; i < a.N; i += threads) {
+        int s, j;
+        if (a.cu_new) {
+            int lo = 0, hi = a.S - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (a.cu_new[mid] <= i) lo = mid;
+                else hi = mid - 1;
+            }
+            s = lo;
+            j = a.cu_new[s] <= i && i < a.cu_new[s + 1] ? i - a.cu_new[s] : INT32_MAX;
+        } else {
+            s = i / a.per;
+            j = i - s * a.per;
+        }
+        int64_t slot = -1;
+        if (j < plan->grow[s]) {
+            const int pos = plan->before[s] + j;
+            const int b = a.table[static_cast<int64_t>(s) * a.max_blocks + pos / kBlockTokens];
+            slot = static_cast<int64_t>(b) * kBlockTokens + pos % kBlockTokens;
+        }
+        slots[i] = slot;
+    }
+}
+
+// --------------------------------------------------------------------------------------------- compact
+
+// The workspace: counts, then holes [nb / 2] (free blocks below R in order) and movers [nb / 2] (blocks in use
+// from R on in order): as many of the one as of the other.
+struct CompactPlan {
+    int moves, live_below, unused[2];
+};
+struct CompactArgs {
+    int32_t *ref;
+    int nb;
+    int32_t *table;
+    int max_blocks;
+    const int32_t *lens;
+    int S;
+    int32_t *remap, *live;
+    CompactPlan *plan;
+    int32_t *holes, *movers;
+    unsigned *err;
+};
+
+__global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const CompactArgs a) {
+    __shared__ int part[33], totals[16];
+    cg::cluster_group cl = cg::this_cluster();
+    const int tid = threadIdx.x, rank = static_cast<int>(cl.block_rank()), ctas = static_cast<int>(cl.num_blocks());
+    cl.sync();  // every CTA has started
+    pdl_wait();
+    pdl_trigger();
+    const Segment seg = my_segment(a.nb, rank, ctas);
+    int mine = 0, cta_live = 0;
+    for_ledger(a.ref, seg, [&](int, int count) { mine += count != 0; });
+    const int before_me = block_scan<int>(mine, part, cta_live);
+    const ClusterSums live = cluster_sums(cta_live, totals);
+    const int R = live.all, my_rank = live.before + before_me;
+    // blocks in use below R, known to the one thread whose entries hold R (nobody where all are in use)
+    if (R == a.nb) {
+        if (rank == 0 && tid == 0) a.plan->live_below = R;
+    } else if (seg.begin <= R && R < seg.end) {
+        int lr = my_rank;
+        for_ledger(a.ref, seg, [&](int id, int count) { lr += id < R && count != 0; });
+        a.plan->live_below = lr;
+    }
+    cl.sync();
+    const int below = *static_cast<volatile int *>(&a.plan->live_below);
+    int lr = my_rank;
+    for_ledger(a.ref, seg, [&](int id, int count) {
+        if (count != 0) {
+            if (id < R) a.remap[id] = id;
+            else a.movers[lr - below] = id;
+            ++lr;
+        } else {
+            a.remap[id] = -1;
+            if (id < R) a.holes[id - lr] = id;
+        }
+    });
+    cl.sync();
+    const int moves = R - below;
+    for (int k = rank * kPlanThreads + tid; k < moves; k += ctas * kPlanThreads) {
+        const int from = a.movers[k], to = a.holes[k];
+        a.remap[from] = to;
+        a.ref[to] = a.ref[from];
+        a.ref[from] = 0;
+    }
+    if (rank == 0 && tid == 0) {
+        a.plan->moves = moves;
+        *a.live = R;
+    }
+}
+
+constexpr int kMoveBytes = kCopyThreads * 16 * 4;  // of a block, moved at once by a CTA
+
+// Up to LLA_MAX_POOLS pools; first[l] is the number of kMoveBytes chunks that a block has in the pools before l.
+struct BlockSet {
+    char *base[LLA_MAX_POOLS];
+    int64_t bytes[LLA_MAX_POOLS];
+    int first[LLA_MAX_POOLS + 1];
+    int L;
+};
+
+// Behind the plan: whole blocks from movers to holes (no hole is a mover, so the order does not matter), and the tables.
+__global__ void __launch_bounds__(kCopyThreads) compact_move_kernel(const CompactArgs a, const __grid_constant__ BlockSet bs) {
+    pdl_wait();
+    pdl_trigger();
+    const int tid = threadIdx.x;
+    bool bad_len = false, bad_id = false;
+    for (int s = blockIdx.x; s < a.S; s += gridDim.x) {
+        const int len = checked_len(a.lens[s], a.max_blocks);
+        bad_len |= len < 0;
+        const int n = pages_of(max(0, len));
+        int32_t *row = a.table + static_cast<int64_t>(s) * a.max_blocks;
+        for (int i = tid; i < n; i += kCopyThreads) {
+            const int b = row[i];
+            const int to = b >= 0 && b < a.nb ? a.remap[b] : -1;
+            if (to < 0) bad_id = true;  // no block, or a free one: left as it is
+            else if (to != b) row[i] = to;
+        }
+    }
+    if (bad_len) atomicOr(a.err, LLA_DEVERR_CONTEXT);
+    if (bad_id) atomicOr(a.err, LLA_DEVERR_BLOCK_ID);
+    const int per_block = bs.first[bs.L];
+    const int64_t units = static_cast<int64_t>(a.plan->moves) * per_block;
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const int k = static_cast<int>(u / per_block), in_block = static_cast<int>(u - static_cast<int64_t>(k) * per_block);
+        int lo = 0, hi = bs.L - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (bs.first[mid] <= in_block) lo = mid;
+            else hi = mid - 1;
+        }
+        const int64_t bytes = bs.bytes[lo], off = static_cast<int64_t>(in_block - bs.first[lo]) * kMoveBytes;
+        const char *src = bs.base[lo] + a.movers[k] * bytes + off;
+        char *dst = bs.base[lo] + a.holes[k] * bytes + off;
+        const int n = static_cast<int>(bytes - off < kMoveBytes ? bytes - off : kMoveBytes);
+        uint4 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if ((tid + j * kCopyThreads) * 16 < n) v[j] = __ldcs(reinterpret_cast<const uint4 *>(src) + tid + j * kCopyThreads);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if ((tid + j * kCopyThreads) * 16 < n) __stcs(reinterpret_cast<uint4 *>(dst) + tid + j * kCopyThreads, v[j]);
+    }
+}
+
+// ------------------------------------------------------------------------------------------- launches
+
+// CTAs of a plan's cluster.
+int plan_ctas(int64_t num_blocks) { return num_blocks > 16384 ? 8 : 1; }
+
+template <typename A>
+lla_status launch_plan(void (*kern)(A), int ctas, const A &a, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(kPlanThreads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kern, a) == cudaSuccess ? LLA_OK : LLA_ERR_CUDA;
+}
+
+}  // namespace
+
+lla_status launch_pages_fork(const lla_pages &from, const lla_pages &to, const int32_t *parents, cudaStream_t stream) {
+    lla_status st;
+    ForkArgs a = {};
+    a.ref = from.ref_count; a.nb = static_cast<int>(from.num_blocks);
+    a.from_table = from.block_table; a.from_lens = from.context_lens;
+    a.from_max = from.max_blocks_per_seq; a.from_S = from.S;
+    a.to_table = to.block_table; a.to_lens = to.context_lens;
+    a.to_max = to.max_blocks_per_seq; a.to_S = to.S;
+    a.parents = parents;
+    a.err = device_error_word(&st);
+    if (!a.err) return st;
+    const int most = from.max_blocks_per_seq;
+    const int spans = (most + kForkSpan - 1) / kForkSpan;
+    return launch_ex(fork_kernel, dim3(to.S + from.S, spans < 32 ? spans : 32), kForkThreads, 0, stream, a);
+}
+
+lla_status launch_pages_free(const lla_pages &p, const int32_t *seqs, int n, cudaStream_t stream) {
+    lla_status st;
+    unsigned *err = device_error_word(&st);
+    if (!err) return st;
+    return launch_ex(free_kernel, dim3(n), kFreeThreads, 0, stream, p.ref_count, static_cast<int>(p.num_blocks),
+                     static_cast<const int32_t *>(p.block_table), p.max_blocks_per_seq, p.context_lens, p.S, seqs, err);
+}
+
+size_t pages_extend_workspace_bytes() { return sizeof(ExtendPlan); }
+
+lla_status launch_pages_extend(const lla_pages &p, const lla_pool *pools, int L, int64_t *slots, int N, const int32_t *cu_new,
+                               const uint8_t *skip, int32_t *lens_before, int32_t *free_blocks, void *workspace,
+                               cudaStream_t stream) {
+    lla_status st;
+    ExtendArgs a = {};
+    a.ref = p.ref_count; a.nb = static_cast<int>(p.num_blocks);
+    a.table = p.block_table; a.max_blocks = p.max_blocks_per_seq; a.lens = p.context_lens; a.S = p.S;
+    a.cu_new = cu_new; a.N = N; a.per = cu_new || p.S == 0 ? 0 : N / p.S;
+    a.skip = skip; a.lens_before = lens_before; a.free_blocks = free_blocks;
+    a.plan = static_cast<ExtendPlan *>(workspace);
+    a.err = device_error_word(&st);
+    if (!a.err) return st;
+    PoolSet ps = {};
+    ps.L = L;
+    for (int l = 0; l < L; ++l) {
+        ps.p[l] = pools[l];
+        ps.first[l + 1] = ps.first[l] + pools[l].pages;
+    }
+    if ((st = launch_plan(extend_plan_kernel, plan_ctas(p.num_blocks), a, stream)) != LLA_OK) return st;
+    const int sms = num_sms();
+    if (sms <= 0) return LLA_ERR_CUDA;
+    // every CTA resident at once; no more than there can be work for
+    const int64_t work = static_cast<int64_t>(p.S) * ps.first[L] * 32 + N;
+    const int64_t ctas = (work + kCopyThreads - 1) / kCopyThreads;
+    return launch_ex(extend_finish_kernel, dim3(static_cast<unsigned>(ctas < sms * 4 ? (ctas > 0 ? ctas : 1) : sms * 4)),
+                     kCopyThreads, 0, stream, a, ps, slots);
+}
+
+size_t pages_compact_workspace_bytes(int64_t num_blocks) {
+    return sizeof(CompactPlan) + 2 * static_cast<size_t>(num_blocks / 2 + 1) * sizeof(int32_t);
+}
+
+lla_status launch_pages_compact(const lla_pages &p, const lla_pool *pools, int L, int32_t *remap, int32_t *live, void *workspace,
+                                cudaStream_t stream) {
+    lla_status st;
+    CompactArgs a = {};
+    a.ref = p.ref_count; a.nb = static_cast<int>(p.num_blocks);
+    a.table = p.block_table; a.max_blocks = p.max_blocks_per_seq; a.lens = p.context_lens; a.S = p.S;
+    a.remap = remap; a.live = live;
+    a.plan = static_cast<CompactPlan *>(workspace);
+    a.holes = reinterpret_cast<int32_t *>(a.plan + 1);
+    a.movers = a.holes + a.nb / 2 + 1;
+    a.err = device_error_word(&st);
+    if (!a.err) return st;
+    BlockSet bs = {};
+    bs.L = L;
+    for (int l = 0; l < L; ++l) {
+        bs.base[l] = static_cast<char *>(pools[l].base);
+        bs.bytes[l] = static_cast<int64_t>(kBlockTokens) * (pools[l].k_row_bytes + pools[l].v_row_bytes) * pools[l].pages;
+        const int64_t chunks = (bs.bytes[l] + kMoveBytes - 1) / kMoveBytes;
+        bs.first[l + 1] = bs.first[l] + static_cast<int>(chunks);  // at most 128 pools of 2^18 chunks
+    }
+    if ((st = launch_plan(compact_plan_kernel, plan_ctas(p.num_blocks), a, stream)) != LLA_OK) return st;
+    const int sms = num_sms();
+    if (sms <= 0) return LLA_ERR_CUDA;
+    return launch_ex(compact_move_kernel, dim3(sms * 8), kCopyThreads, 0, stream, a, bs);
+}
+
+}  // namespace lla

@@ -31,6 +31,9 @@ LLA_DEVERR_CONTEXT = 0x2
 LLA_DEVERR_EMPTY_PASS2 = 0x4
 LLA_DEVERR_TIMEOUT = 0x8
 LLA_DEVERR_SLOT = 0x10
+LLA_DEVERR_SEQUENCE = 0x20
+LLA_DEVERR_PAGES = 0x40
+LLA_MAX_BEAMS = 32
 
 _STATUS = {0: "LLA_OK", 1: "LLA_ERR_INVALID_ARG", 2: "LLA_ERR_UNSUPPORTED", 3: "LLA_ERR_CUDA",
            4: "LLA_ERR_TIMEOUT", 5: "LLA_ERR_DEVICE_CHECK", 6: "LLA_ERR_WORKSPACE"}
@@ -62,12 +65,27 @@ class lla_cache(ctypes.Structure):
                 ("block_table", ctypes.c_void_p), ("max_blocks_per_seq", ctypes.c_int32)]
 
 
-# lla_capture_fn and lla_query_fn of include/lla.h
+class lla_pages(ctypes.Structure):
+    _fields_ = [("ref_count", ctypes.c_void_p), ("num_blocks", ctypes.c_int64),
+                ("block_table", ctypes.c_void_p), ("max_blocks_per_seq", ctypes.c_int32),
+                ("context_lens", ctypes.c_void_p), ("S", ctypes.c_int32)]
+
+
+class lla_pool(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("pages", ctypes.c_int32),
+                ("k_row_bytes", ctypes.c_int32), ("v_row_bytes", ctypes.c_int32)]
+
+
+# lla_capture_fn, lla_query_fn and lla_step_fn of include/lla.h
 CAPTURE_FN = ctypes.CFUNCTYPE(ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_void_p),
                               ctypes.POINTER(ctypes.c_void_p), ctypes.c_void_p, ctypes.c_void_p)
 QUERY_FN = ctypes.CFUNCTYPE(ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                             ctypes.POINTER(ctypes.c_void_p), ctypes.POINTER(ctypes.c_void_p),
                             ctypes.c_void_p, ctypes.c_void_p)
+
+STEP_FN = ctypes.CFUNCTYPE(ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(lla_pages), ctypes.c_void_p,
+                           ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(ctypes.c_void_p),
+                           ctypes.POINTER(ctypes.c_int64), ctypes.c_void_p, ctypes.c_void_p)
 
 _lib = None
 _native_module = None
@@ -139,6 +157,21 @@ def library() -> ctypes.CDLL:
             "lla_clear_device_error": (I32, [P]),
             "lla_prefill_two_pass": (I32, [P, I32, P, P, I32, P, I32, P, I32, I32, I32, P, CAPTURE_FN,
                                            QUERY_FN, P, P, SZ, P]),
+            "lla_cache_pool": (I32, [P, P, P]),
+            "lla_cache_2d_pool": (I32, [P, P, P]),
+            "lla_rope_pool": (I32, [I32, P, P]),
+            "lla_pages_fork": (I32, [P, P, P, P]),
+            "lla_pages_extend_workspace_size": (I32, [I32, P]),
+            "lla_pages_extend": (I32, [P, P, I32, P, I32, P, P, P, P, P, SZ, P]),
+            "lla_pages_free": (I32, [P, P, I32, P]),
+            "lla_pages_compact_workspace_size": (I32, [I64, P]),
+            "lla_pages_compact": (I32, [P, P, I32, P, P, P, SZ, P]),
+            "lla_beam_select_workspace_size": (I32, [I32, I32, I32, I32, I32, P]),
+            "lla_beam_select": (I32, [I32, I32, I32, I32, P, I64, I32, P, P, P, I32, ctypes.c_float, P, P, P,
+                                      P, P, P, SZ, P]),
+            "lla_beam_search_workspace_size": (I32, [I32, I32, I32, I32, P]),
+            "lla_beam_search": (I32, [P, P, P, I32, I32, I32, I32, I32, I32, I32, ctypes.c_float, P, P, P, P,
+                                      P, STEP_FN, P, P, SZ, P]),
             "lla_set_wait_limit_ns": (I32, [ctypes.c_uint64]),
             "lla_get_wait_limit_ns": (ctypes.c_uint64, []),
         }
@@ -585,6 +618,273 @@ def lla_dense_decode_attn(geom: Geometry, cache: Cache, context_lens: torch.Tens
         ctypes.byref(g), ctypes.byref(ch), _ptr(context_lens), q.shape[0], max_ctx, _ptr(q),
         _ptr(cur_k), _ptr(cur_v), _dtype_code(q), _ptr(out), _ptr(workspace),
         workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def _typed(t: Optional[torch.Tensor], dtype, name: str, shape=None):
+    """The address of a contiguous tensor of `dtype` (and `shape`) on the current device, or None."""
+    if t is None:
+        return None
+    p = _ptr(t)
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, which is not the current device")
+    return p
+
+
+def _scratch(t: torch.Tensor):
+    """Address and bytes of a workspace on the current device."""
+    p = _ptr(t)
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"the workspace is on {t.device}, which is not the current device")
+    return p, t.numel() * t.element_size()
+
+
+@dataclass
+class Pages:
+    """Sequences that share the blocks of a pool: ref_count [num_blocks] int32 (sequences that hold
+    each block; 0: free), block_table [S][max_blocks] int32, context_lens [S] int32.  All zero: every block is
+    free, every sequence empty.  Page sets over one pool share the ref_count tensor."""
+    ref_count: torch.Tensor
+    block_table: torch.Tensor
+    context_lens: torch.Tensor
+
+    def c(self) -> lla_pages:
+        if self.ref_count.dim() != 1 or self.block_table.dim() != 2:
+            raise ValueError("ref_count is [num_blocks], block_table [S][max_blocks]")
+        S, mb = self.block_table.shape
+        return lla_pages(_typed(self.ref_count, torch.int32, "ref_count"), self.ref_count.shape[0],
+                         _typed(self.block_table, torch.int32, "block_table"), mb,
+                         _typed(self.context_lens, torch.int32, "context_lens", (S,)), S)
+
+
+@dataclass
+class Pool:
+    """One pool that page calls copy in, as lla_cache_pool, lla_cache_2d_pool or lla_rope_pool describe it."""
+    base: torch.Tensor
+    pages: int
+    k_row_bytes: int
+    v_row_bytes: int
+
+    def c(self) -> lla_pool:
+        return lla_pool(_ptr(self.base), self.pages, self.k_row_bytes, self.v_row_bytes)
+
+
+class Pools:
+    """The pools that a page call copies in (every layer's, and its rotary planes), marshalled once."""
+
+    def __init__(self, pools=()):
+        self.pools = tuple(pools)
+        self.count = len(self.pools)
+        self.array = (lla_pool * max(1, self.count))(*[p.c() for p in self.pools])
+        self.address = ctypes.addressof(self.array)
+        # blocks that every one of them has room for
+        self.blocks = min((p.base.numel() * p.base.element_size() //
+                           (LLA_BLOCK_TOKENS * p.pages * (p.k_row_bytes + p.v_row_bytes)) for p in self.pools),
+                          default=1 << 62)
+        self.device = self.pools[0].base.device.index if self.pools else -1
+        if any(p.base.device.index != self.device for p in self.pools):
+            raise ValueError("pools of one call must be on one device")
+
+    def check(self, pages: Pages) -> None:
+        if self.blocks < pages.ref_count.shape[0]:
+            raise ValueError(f"a pool has {self.blocks} blocks, ref_count {pages.ref_count.shape[0]}")
+        if self.count and self.device != torch.cuda.current_device():
+            raise ValueError("the pools are not on the current device")
+
+
+def _pool(fn: str, first, pool: torch.Tensor) -> Pool:
+    out = lla_pool()
+    _check(fn, getattr(library(), fn)(first, _ptr(pool), ctypes.byref(out)))
+    return Pool(pool, out.pages, out.k_row_bytes, out.v_row_bytes)
+
+
+def lla_cache_pool(geom: Geometry, pool: torch.Tensor) -> Pool:
+    return _pool("lla_cache_pool", ctypes.byref(geom.c()), pool)
+
+
+def lla_cache_2d_pool(geom: Geometry, pool: torch.Tensor) -> Pool:
+    return _pool("lla_cache_2d_pool", ctypes.byref(geom.c()), pool)
+
+
+def lla_rope_pool(d_rope: int, rope_pool: torch.Tensor) -> Pool:
+    return _pool("lla_rope_pool", d_rope, rope_pool)
+
+
+def lla_pages_fork(src: Pages, dst: Pages, parents: torch.Tensor, stream=None) -> None:
+    """dst's sequence s becomes a copy of src's sequence parents[s] ([S] int32; -1: empty) on the same pages;
+    src holds nothing afterwards."""
+    if _done("lla_pages_fork", _native().pages_fork(src, dst, parents, _handle(stream))):
+        return
+    a, b = src.c(), dst.c()
+    _check("lla_pages_fork", library().lla_pages_fork(
+        ctypes.byref(a), ctypes.byref(b), _typed(parents, torch.int32, "parents", (b.S,)), _stream(stream)))
+
+
+def lla_pages_extend_workspace_size(S: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check("lla_pages_extend_workspace_size",
+           library().lla_pages_extend_workspace_size(S, ctypes.byref(out)))
+    return out.value
+
+
+def lla_pages_extend(pages: Pages, pools: Pools, slot_mapping: torch.Tensor, workspace: torch.Tensor,
+                     cu_new: Optional[torch.Tensor] = None, skip: Optional[torch.Tensor] = None,
+                     lens_before: Optional[torch.Tensor] = None, free_blocks: Optional[torch.Tensor] = None,
+                     stream=None) -> None:
+    """Sequence s grows by cu_new[s + 1] - cu_new[s] tokens (cu_new [S + 1] int32), or each by
+    slot_mapping.numel() / S; slot_mapping [N] int64 is written.  skip [S] uint8 (or bool): sequences that do not
+    grow.  lens_before [S] int32, free_blocks [1] int32: written where given."""
+    if _done("lla_pages_extend", _native().pages_extend(
+            pages, pools, slot_mapping, workspace, cu_new, skip, lens_before, free_blocks, _handle(stream))):
+        return
+    p = pages.c()
+    pools.check(pages)
+    if skip is not None and skip.dtype == torch.bool:
+        skip = skip.view(torch.uint8)
+    _check("lla_pages_extend", library().lla_pages_extend(
+        ctypes.byref(p), pools.address, pools.count, _typed(slot_mapping, torch.int64, "slot_mapping"),
+        slot_mapping.numel(), _typed(cu_new, torch.int32, "cu_new", (p.S + 1,)),
+        _typed(skip, torch.uint8, "skip", (p.S,)), _typed(lens_before, torch.int32, "lens_before", (p.S,)),
+        _typed(free_blocks, torch.int32, "free_blocks", (1,)), *_scratch(workspace), _stream(stream)))
+
+
+def lla_pages_free(pages: Pages, seqs: torch.Tensor, stream=None) -> None:
+    """Frees the pages of the sequences seqs [n] int32 (negative: skipped)."""
+    if _done("lla_pages_free", _native().pages_free(pages, seqs, _handle(stream))):
+        return
+    p = pages.c()
+    _check("lla_pages_free", library().lla_pages_free(
+        ctypes.byref(p), _typed(seqs, torch.int32, "seqs"), seqs.numel(), _stream(stream)))
+
+
+def lla_pages_compact_workspace_size(num_blocks: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check("lla_pages_compact_workspace_size",
+           library().lla_pages_compact_workspace_size(num_blocks, ctypes.byref(out)))
+    return out.value
+
+
+def lla_pages_compact(pages: Pages, pools: Pools, remap: torch.Tensor, live: torch.Tensor,
+                      workspace: torch.Tensor, stream=None) -> None:
+    """Moves the blocks in use to the front of every pool.  remap [num_blocks] int32 (new number of each block, -1
+    where free) and live [1] int32 (blocks in use) are written."""
+    if _done("lla_pages_compact", _native().pages_compact(pages, pools, remap, live, workspace, _handle(stream))):
+        return
+    p = pages.c()
+    pools.check(pages)
+    _check("lla_pages_compact", library().lla_pages_compact(
+        ctypes.byref(p), pools.address, pools.count, _typed(remap, torch.int32, "remap", (p.num_blocks,)),
+        _typed(live, torch.int32, "live", (1,)), *_scratch(workspace), _stream(stream)))
+
+
+def lla_beam_select_workspace_size(B: int, W: int, V: int, K: int, dtype=torch.bfloat16) -> int:
+    out = ctypes.c_size_t(0)
+    _check("lla_beam_select_workspace_size", library().lla_beam_select_workspace_size(
+        B, W, V, K, LLA_BF16 if dtype == torch.bfloat16 else LLA_F32, ctypes.byref(out)))
+    return out.value
+
+
+def _logit_rows(logits: torch.Tensor) -> int:
+    """The distance of the rows of logits [B][W][V], whose last dimension is dense (rows may be padded)."""
+    if logits.dim() != 3 or logits.stride(2) != 1 and logits.shape[2] > 1:
+        raise ValueError("logits are [B][W][V] with a dense last dimension")
+    B, W, V = logits.shape
+    rows = logits.stride(1) if W > 1 else logits.stride(0) if B > 1 else V
+    if B > 1 and W > 1 and logits.stride(0) != W * rows:
+        raise ValueError("the rows of logits must lie at one distance")
+    if not logits.is_cuda:
+        raise ValueError("tensors passed to liblla must be CUDA tensors")
+    if logits.device.index != torch.cuda.current_device():
+        raise ValueError(f"logits are on {logits.device}, which is not the current device")
+    return rows
+
+
+def lla_beam_select(logits: torch.Tensor, scores: torch.Tensor, parents: torch.Tensor, tokens: torch.Tensor,
+                    out_scores: torch.Tensor, workspace: torch.Tensor, finished: Optional[torch.Tensor] = None,
+                    lengths: Optional[torch.Tensor] = None, out_finished: Optional[torch.Tensor] = None,
+                    out_lengths: Optional[torch.Tensor] = None, eos: int = -1, length_penalty: float = 0.0,
+                    stream=None) -> None:
+    """The best K = parents.shape[1] continuations of the beams: logits [B][W][V] (bf16 or fp32; rows may be
+    padded), scores [B][W] fp32, finished [B][W] uint8, lengths [B][W] int32; parents, tokens [B][K] int32,
+    out_scores [B][K] fp32, out_finished [B][K] uint8 and out_lengths [B][K] int32 are written."""
+    if _done("lla_beam_select", _native().beam_select(
+            logits, scores, parents, tokens, out_scores, workspace, finished, lengths, out_finished, out_lengths, eos,
+            length_penalty, _handle(stream))):
+        return
+    rows = _logit_rows(logits)
+    B, W, V = logits.shape
+    if parents.dim() != 2:
+        raise ValueError("parents are [B][K]")
+    K = parents.shape[1]
+    _check("lla_beam_select", library().lla_beam_select(
+        B, W, V, K, logits.data_ptr(), rows, _dtype_code(logits), _typed(scores, torch.float32, "scores", (B, W)),
+        _typed(finished, torch.uint8, "finished", (B, W)), _typed(lengths, torch.int32, "lengths", (B, W)), eos,
+        length_penalty, _typed(parents, torch.int32, "parents", (B, K)), _typed(tokens, torch.int32, "tokens", (B, K)),
+        _typed(out_scores, torch.float32, "out_scores", (B, K)),
+        _typed(out_finished, torch.uint8, "out_finished", (B, K)),
+        _typed(out_lengths, torch.int32, "out_lengths", (B, K)), *_scratch(workspace), _stream(stream)))
+
+
+def lla_beam_search_workspace_size(B: int, W: int, V: int, dtype=torch.bfloat16) -> int:
+    out = ctypes.c_size_t(0)
+    _check("lla_beam_search_workspace_size", library().lla_beam_search_workspace_size(
+        B, W, V, LLA_BF16 if dtype == torch.bfloat16 else LLA_F32, ctypes.byref(out)))
+    return out.value
+
+
+def lla_beam_search(pages_a: Pages, pages_b: Pages, pools: Pools, V: int, step, tokens: torch.Tensor,
+                    scores: torch.Tensor, finished: torch.Tensor, lengths: torch.Tensor, parents: torch.Tensor,
+                    workspace: torch.Tensor, dtype=torch.bfloat16, eos: int = -1, length_penalty: float = 0.0,
+                    stream=None) -> None:
+    """Beam search over parents.shape[0] steps: tokens, scores, finished, lengths [steps + 1][B][W] (slab 0 filled
+    by the caller), parents [steps][B][W].  step(i, pages, lens_before, tokens, slots) runs the model for step i
+    and returns its logits [B][W][V] of `dtype` (kept alive until the call returns): pages is pages_a or pages_b,
+    lens_before [B W] int32, tokens [B][W] int32, slots [B W] int64."""
+    if parents.dim() != 3:
+        raise ValueError("parents are [steps][B][W]")
+    steps, B, W = parents.shape
+    slabs = (steps + 1, B, W)
+    a, b = pages_a.c(), pages_b.c()
+    pools.check(pages_a)
+    pools.check(pages_b)
+    base, nbytes = _scratch(workspace)
+    flat = workspace.view(-1).view(torch.uint8)
+    keep, errors = [], []
+
+    def _view(address, dtype_, size):
+        return flat[address - base:address - base + size].view(dtype_)
+
+    def _step(i, _pages, before, _tokens, slots, logits, row_stride, _stream_, _user):
+        try:
+            n = B * W
+            z = step(i, pages_b if i % 2 else pages_a, _view(before, torch.int32, 4 * n), tokens[i],
+                     _view(slots, torch.int64, 8 * n))
+            if z.dtype != dtype or tuple(z.shape) != (B, W, V):
+                raise ValueError(f"step must return {dtype} logits of shape {(B, W, V)}, not {z.dtype} {tuple(z.shape)}")
+            row_stride[0] = _logit_rows(z)
+            logits[0] = z.data_ptr()
+            keep.append(z)
+            return 0
+        except Exception as e:  # reported after the C call returns
+            errors.append(e)
+            return 1
+
+    if dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"unsupported dtype {dtype}")
+    cb = STEP_FN(_step)
+    st = library().lla_beam_search(
+        ctypes.byref(a), ctypes.byref(b), pools.address, pools.count, B, W, V,
+        LLA_BF16 if dtype == torch.bfloat16 else LLA_F32, steps, eos, length_penalty,
+        _typed(tokens, torch.int32, "tokens", slabs), _typed(scores, torch.float32, "scores", slabs),
+        _typed(finished, torch.uint8, "finished", slabs), _typed(lengths, torch.int32, "lengths", slabs),
+        _typed(parents, torch.int32, "parents"), cb, None, base,
+        nbytes, _stream(stream))
+    if errors:
+        raise errors[0]
+    _check("lla_beam_search", st)
 
 
 def lla_get_device_error(stream=None) -> int:
