@@ -34,17 +34,19 @@ namespace {
 constexpr int kScanThreads = 256;
 constexpr int kWords = 4;                             // 16-byte words of a thread and tile
 constexpr int kTileWords = kScanThreads * kWords;     // 16 KB a tile
-constexpr int kFew = 64;                              // threads of a tile that may bring candidates
-constexpr int kCap = 4096;                            // candidates that a CTA holds
+constexpr int kStages = 2;                            // tiles in shared memory
+constexpr int kScanCtas = 4;                          // of an SM
+constexpr int kFew = 40;                              // threads of a tile that may bring candidates
+constexpr int kCap = 2304;                            // candidates that a CTA holds
 constexpr int kMaxShares = 32;                        // shares of a row: a warp merges them
 constexpr int kListLen = LLA_MAX_BEAMS;               // a list is a warp's lanes
 constexpr float kRise = 60.f;                         // a logit this far over m moves m (e^60 2^24 is finite)
 
 typedef unsigned long long u64;
 
-// The sum and its offset of a share: S = (hi + lo), in units of exp(m).
+// The sum of a share, hi + lo, and the base of its terms (Base; c = -inf: no finite logit).
 struct Share {
-    float m, hi, lo, unused;
+    float c, hi, lo, wide;
 };
 
 // Numbers in order as unsigned integers: a < b as floats (no NaN) exactly if key(a) < key(b); -0 is made 0 before.
@@ -84,9 +86,9 @@ __device__ __forceinline__ u64 add2(u64 a, u64 b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-__device__ __forceinline__ u64 mul2(u64 a, u64 b) {
+__device__ __forceinline__ u64 fma2(u64 a, u64 b, u64 c) {
     u64 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
 
@@ -195,30 +197,30 @@ struct Row {
         }
         return make_uint4(r[0], r[1], r[2], r[3]);
     }
-    __device__ __forceinline__ uint4 whole(int w) const {
-        uint4 v;
-        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                     : "l"(base + static_cast<int64_t>(w) * 16));
-        return v;
-    }
-    __device__ __forceinline__ void load(uint4 (&v)[kWords], int tile) const {
-        const int w0 = tile * kTileWords + threadIdx.x;
-        const int64_t lo = static_cast<int64_t>(tile) * kTileWords * kPer, hi = lo + kTileWords * kPer;
-        if (lo >= skip && hi <= static_cast<int64_t>(skip) + V) {  // the same for the whole CTA
-#pragma unroll
-            for (int j = 0; j < kWords; ++j) v[j] = whole(w0 + j * kScanThreads);
-        } else {
-#pragma unroll
-            for (int j = 0; j < kWords; ++j) {
-                const int64_t i = static_cast<int64_t>(w0 + j * kScanThreads) * kPer;
-                if (i >= skip && i + kPer <= static_cast<int64_t>(skip) + V) v[j] = whole(w0 + j * kScanThreads);
-                else v[j] = edge(w0 + j * kScanThreads);
-            }
+    // The tiles [first_whole, end_whole) consist of whole words.
+    __device__ __forceinline__ int first_whole() const { return skip ? 1 : 0; }
+    __device__ __forceinline__ int end_whole() const { return (skip + V) / (kPer * kTileWords); }
+    // A thread's words of a tile (word j * kScanThreads + thread of it) into its place in shared memory, word by word;
+    // no group of copies is committed.
+    __device__ __forceinline__ void copy(uint4 (*slot)[kScanThreads], int tile) const {
+#pragma unroll 1
+        for (int j = 0; j < kWords; ++j) {
+            const int w = tile * kTileWords + j * kScanThreads + threadIdx.x;
+            const int64_t i = static_cast<int64_t>(w) * kPer;
+            if (i >= skip && i + kPer <= static_cast<int64_t>(skip) + V)
+                cp_async16(&slot[j][threadIdx.x], base + static_cast<int64_t>(w) * 16);
+            else
+                slot[j][threadIdx.x] = edge(w);
         }
     }
-    __device__ __forceinline__ int token(int tile, int j, int e) const {
-        return (tile * kTileWords + j * kScanThreads + static_cast<int>(threadIdx.x)) * kPer + e - skip;
+    // The token of logit e of a thread's word j, and a thread's logit i (word i / kPer) from shared memory.
+    __device__ __forceinline__ int token(int tile, int j, int e, int thread) const {
+        return (tile * kTileWords + j * kScanThreads + thread) * kPer + e - skip;
+    }
+    __device__ __forceinline__ float staged(const uint4 (*slot)[kScanThreads], int thread, int i) const {
+        const uint4 *w = &slot[i / kPer][thread];
+        if (BF16) return bf_to_f(reinterpret_cast<const uint16_t *>(w)[i % kPer]);
+        return reinterpret_cast<const float *>(w)[i % kPer];
     }
 };
 
@@ -253,64 +255,74 @@ __device__ __forceinline__ float tile_max(const uint4 (&v)[kWords]) {
     }
 }
 
-// Infinite and NaN logits become -inf.
-template <bool BF16>
-__device__ __forceinline__ void mask_infinite(uint4 (&v)[kWords]) {
-#pragma unroll
-    for (int j = 0; j < kWords; ++j) {
-        uint32_t *u = reinterpret_cast<uint32_t *>(&v[j]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (BF16) {
-                if ((u[i] & 0x7f80u) == 0x7f80u) u[i] = (u[i] & 0xffff0000u) | 0xff80u;
-                if ((u[i] & 0x7f800000u) == 0x7f800000u) u[i] = (u[i] & 0xffffu) | 0xff800000u;
-            } else if ((u[i] & 0x7f800000u) == 0x7f800000u) {
-                u[i] = 0xff800000u;
-            }
-        }
+// What a thread's terms are scaled by.  Terms are 2^(z kLog2e - c) with a whole number c, so that a change of c is exact
+// and a term takes one multiply-add; where the largest logit is beyond +-65536 (a row masked whole by the lowest
+// number, say) they are 2^((z - c) kLog2e) (`wide`).
+constexpr float kLog2e = 1.44269504f;
+struct Base {
+    float c;
+    bool wide;
+    __device__ __forceinline__ void set(float top) {
+        wide = !(fabsf(top) <= 65536.f);
+        c = wide ? top : rintf(top * kLog2e);
     }
+    __device__ __forceinline__ float at() const { return wide ? c : c * (1.f / kLog2e); }  // as a logit, nearly
+};
+// The factor of a sum that goes from one base to another.
+__device__ __forceinline__ float rebase(const Base &from, const Base &to) {
+    if (!from.wide && !to.wide) return ex2(from.c - to.c);
+    return ex2((from.at() - to.at()) * kLog2e);
 }
 
-// sum 2^((z - m) log2 e) over a thread's logits of a tile: a tree of pairs.
+// The sum of a thread's terms of a tile, not wide: a tree of pairs.
 template <bool BF16>
-__device__ __forceinline__ float tile_sum(const uint4 (&v)[kWords], float m) {
-    const u64 minus = pack2(-m, -m), l2e = pack2(1.44269504f, 1.44269504f);
+__device__ __forceinline__ float tile_sum(const uint4 (&v)[kWords], float c) {
+    const u64 minus = pack2(-c, -c), l2e = pack2(kLog2e, kLog2e);
     u64 s[kWords];
 #pragma unroll
     for (int j = 0; j < kWords; ++j) {
         u64 t[BF16 ? 4 : 2];
 #pragma unroll
         for (int i = 0; i < (BF16 ? 4 : 2); ++i) {
-            const u64 x = mul2(add2(pack2(logit<BF16>(v[j], 2 * i), logit<BF16>(v[j], 2 * i + 1)), minus), l2e);
-            const float2 f = unpack2(x);
+            const float2 f = unpack2(fma2(pack2(logit<BF16>(v[j], 2 * i), logit<BF16>(v[j], 2 * i + 1)), l2e, minus));
             t[i] = pack2(ex2(f.x), ex2(f.y));
         }
         s[j] = BF16 ? add2(add2(t[0], t[1]), add2(t[BF16 ? 2 : 0], t[BF16 ? 3 : 1])) : add2(t[0], t[1]);
     }
-    const float2 f = unpack2(add2(add2(s[0], s[1]), add2(s[2], s[3])));
+#pragma unroll
+    for (int n = kWords / 2; n > 0; n /= 2)
+#pragma unroll
+        for (int j = 0; j < n; ++j) s[j] = add2(s[j], s[j + n]);
+    const float2 f = unpack2(s[0]);
     return f.x + f.y;
 }
 
 // Shared state of a scanning CTA.
 struct Scan {
+    uint4 ring[kStages][kWords][kScanThreads];  // a thread reads the words that it copied itself
     u64 buf[kCap];
     u64 tops[kScanThreads / 32][kListLen];
+    uint32_t most[kScanThreads / 32], least[kScanThreads / 32];
     float maxima[kScanThreads / 32], his[kScanThreads / 32], los[kScanThreads / 32];
-    int count;  // candidates in buf
+    Base base;
+    int count;  // candidates in buf (over kCap: some were dropped)
 };
 
-// The best 32 of the CTA's candidates, sorted, in the lanes of warp 0.  Barriers on entry and inside.
-__device__ __forceinline__ u64 best_of(Scan &sh) {
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// The best 32 of the first n candidates, sorted, in the lanes of warp 0.
+__device__ __forceinline__ u64 best_of(Scan &sh, int n) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    constexpr int kWarps = kScanThreads / 32;
-    __syncthreads();
-    const int n = sh.count;
     u64 top = 0;
     for (int i = warp * 32; i < n; i += kScanThreads) {
         const u64 v = sort_desc(i + lane < n ? sh.buf[i + lane] : 0);
         top = i == warp * 32 ? v : merge_desc(top, v);
     }
-    for (int half = kWarps / 2; half > 0; half >>= 1) {  // warps [half, 2 half) hand over and are done
+    for (int half = kScanThreads / 64; half > 0; half >>= 1) {  // warps [half, 2 half) hand over and are done
+        if (n <= half * 32) continue;                           // they had none
         if (warp >= half && warp < 2 * half) sh.tops[warp][lane] = top;
         __syncthreads();
         if (warp < half) top = merge_desc(top, sh.tops[warp + half][lane]);
@@ -319,72 +331,193 @@ __device__ __forceinline__ u64 best_of(Scan &sh) {
 }
 
 template <bool BF16>
-__global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(const ScanArgs a) {
-    __shared__ Scan sh;
+__global__ void __launch_bounds__(kScanThreads, kScanCtas) beam_scan_kernel(const ScanArgs a) {
+    extern __shared__ __align__(16) unsigned char scan_smem[];
+    Scan &sh = *reinterpret_cast<Scan *>(scan_smem);
     const int row = blockIdx.x / a.shares, share = blockIdx.x - row * a.shares;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    constexpr int kWarps = kScanThreads / 32, kPer = Row<BF16>::kPer;
+    constexpr int kWarps = kScanThreads / 32, kPer = Row<BF16>::kPer, kMine = kWords * kPer;
     if (tid == 0) sh.count = 0;
     pdl_wait();
     pdl_trigger();
-    // a beam that is dead or has ended has nothing to read
-    if ((a.finished && a.finished[row]) || !(fabsf(a.scores[row]) <= FLT_MAX)) return;
     Row<BF16> r;
     r.init(a, row);
     const int tiles = (r.words() + kTileWords - 1) / kTileWords;
     const int t0 = static_cast<int>(static_cast<int64_t>(share) * tiles / a.shares);
     const int t1 = static_cast<int>(static_cast<int64_t>(share + 1) * tiles / a.shares);
     const int K = a.K;
-    float thr = -CUDART_INF_F;  // at least K logits of lower tokens are >= thr (or it is -inf): only larger ones count
-    float m = 0.f, limit = -FLT_MAX, hi = 0.f, lo = 0.f;
-    bool have_m = false;
-    int bound = 0;  // at least as many as sh.count
-    uint4 v[kWords], next[kWords];
-    if (t0 < t1) r.load(v, t0);
-    __syncthreads();
-    for (int t = t0; t < t1; ++t) {
-        if (t + 1 < t1) r.load(next, t + 1);
-        float top = tile_max<BF16>(v);
-        if (!(top <= FLT_MAX)) {  // +inf or nothing but NaN
-            mask_infinite<BF16>(v);
-            top = tile_max<BF16>(v);
-        }
-        int passing = __syncthreads_count(top > thr);
-        if (!have_m && passing) {  // (thr is -inf until then) the first finite logits: m is their maximum in the CTA
-            have_m = true;
-            const float w = warp_max(top);
-            if (lane == 0) sh.maxima[warp] = w;
-            __syncthreads();
-            m = sh.maxima[0];
+    // The ring: tile t is copied kStages - 1 tiles ahead, a thread's words by itself.
+    const int in0 = r.first_whole(), in1 = min(t1, r.end_whole());
+    const uint32_t ring = smem_addr(&sh.ring[0][0][tid]);
+    const char *ahead = r.base + (static_cast<int64_t>(t0) * kTileWords + tid) * 16;
+    auto slot_of = [&](int t) { return sh.ring[(t - t0) % kStages]; };
+    auto fetch_whole = [&](int t) {
+        const uint32_t to = ring + (t - t0) % kStages * (kTileWords * 16);
 #pragma unroll
-            for (int i = 1; i < kWarps; ++i) m = fmaxf(m, sh.maxima[i]);
-            limit = m + kRise;
+        for (int j = 0; j < kWords; ++j)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + j * kScanThreads * 16),
+                         "l"(ahead + j * kScanThreads * 16)
+                         : "memory");
+        ahead += kTileWords * 16;
+        cp_async_commit();
+    };
+    auto fetch = [&](int t) {
+        if (t >= in0 && t < in1) {
+            fetch_whole(t);
+        } else {
+            if (t < t1) r.copy(slot_of(t), t);
+            ahead += kTileWords * 16;
+            cp_async_commit();
         }
-        if (have_m) {
-            if (top > limit) {  // a thread's own m from here on
-                const float f = ex2((m - top) * 1.44269504f);
-                m = top;
-                limit = m + kRise;
-                hi *= f;
-                lo *= f;
-            }
-            float s = tile_sum<BF16>(v, m);
-            if (!(s <= FLT_MAX)) {  // a NaN beside finite logits
-                mask_infinite<BF16>(v);
-                s = tile_sum<BF16>(v, m);
-            }
-            two_sum(hi, lo, s);
+    };
+    for (int t = t0; t < t0 + kStages - 1; ++t) fetch(t);
+    // a beam that is dead or has ended has nothing more to read (the first tiles are under way while this is known)
+    if ((a.finished && a.finished[row]) || !(fabsf(a.scores[row]) <= FLT_MAX)) {
+        cp_async_wait<0>();
+        return;
+    }
+
+    float thr = -CUDART_INF_F;  // at least K logits of lower tokens are >= thr (or it is -inf): only larger ones count
+    Base base = {0.f, false};
+    float limit = -FLT_MAX, hi = 0.f, lo = 0.f;  // limit: the largest logit that base is good for
+    bool have_base = false;
+    int kept = 0;  // candidates in buf that are the best so far, sorted
+    bool brought = false;
+    // buf's best to its front; with K of them, only larger logits of later tokens count.  Barriers.
+    auto compact = [&]() {
+        const int n = min(sh.count, kCap);
+        const u64 best = best_of(sh, n);
+        __syncthreads();
+        kept = min(n, K);
+        if (warp == 0 && lane < kept) sh.buf[lane] = best;
+        if (tid == 0) sh.count = kept;
+        __syncthreads();
+        if (kept == K) thr = fmaxf(thr, candidate_logit(sh.buf[K - 1]));
+    };
+    // The candidates of a warp's threads `who`, thread by thread: a lane to each of that thread's logits.
+    auto bring = [&](unsigned who, const uint4(*slot)[kScanThreads], int t, float over, float tie, int last_tie) {
+        brought = true;
+        __syncwarp();  // the words that other lanes copied
+        do {
+            const int owner = warp * 32 + __ffs(who) - 1;
+            who &= who - 1;
+            const int token = r.token(t, lane / kPer, lane % kPer, owner);
+            float x = -CUDART_INF_F;
+            if (lane < kMine) x = r.staged(slot, owner, lane);
+            const bool some = (x > over || (x == tie && token <= last_tie)) && x <= FLT_MAX;
+            const unsigned which = __ballot_sync(0xffffffffu, some);
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&sh.count, __popc(which));
+            at = __shfl_sync(0xffffffffu, at, 0) + __popc(which & ((1u << lane) - 1));
+            if (some && at < kCap) sh.buf[at] = candidate(x, token);
+        } while (who);
+        __syncwarp();  // before the words are overwritten
+    };
+
+    // Tiles go by in groups of 1, 3, 12, 48 ...; within a group each warp goes by itself and brings what passes the
+    // threshold, and at its end the threshold rises to the K-th best.  The first tile, those after it while fewer than
+    // K logits were finite, and a group that brought too much (rising logits), once more, go tile by tile,
+    // carefully: the threshold rises before candidates are brought.
+    int from = t0, end = t0, group = 3, redo = -1;  // redo: where a group is gone through once more, its end
+    __syncthreads();  // sh.count
+    for (int t = t0; t < t1;) {
+        const bool careful = redo >= 0 || !have_base || thr == -CUDART_INF_F;
+        if (!careful && t == end) {
+            from = t;
+            end = min(t1, t + group);
+            group *= 4;
+            brought = false;
         }
-        if (passing) {
-            // Few enough threads bring candidates, or the threshold rises: to one that at least K of their maxima exceed
-            // and at most kFew, found by bisection over the numbers (each step a count), or, where too many are
-            // equal, over the tokens of equal logits.
+        uint4 v[kWords];
+        bool taken = false;  // the tile below has been waited for
+        if (!careful) {
+            // Usual tiles, of whole words and with an ordinary base: one question a tile about all that is not usual.
+            const int stop = __any_sync(0xffffffffu, base.wide) ? t : min(end, in1 - (kStages - 1));
+            const float usual = fminf(thr, limit);
+            for (; t < stop; ++t) {
+                fetch_whole(t + kStages - 1);  // over tile t - 1
+                cp_async_wait<kStages - 1>();
+                const uint4(*slot)[kScanThreads] = slot_of(t);
+#pragma unroll
+                for (int j = 0; j < kWords; ++j) v[j] = slot[j][tid];
+                const float top = tile_max<BF16>(v), s = tile_sum<BF16>(v, base.c);
+                if (__any_sync(0xffffffffu, !(top <= usual) || !(s <= FLT_MAX))) {
+                    taken = __any_sync(0xffffffffu, !(top <= limit) || !(s <= FLT_MAX));
+                    if (taken) break;
+                    bring(__ballot_sync(0xffffffffu, top > thr), slot, t, thr, CUDART_INF_F, -1);
+                }
+                two_sum(hi, lo, s);
+            }
+        }
+        if (careful || t < end) {  // any tile
+            uint4(*slot)[kScanThreads] = slot_of(redo >= 0 ? redo - 1 : t);
+            if (redo >= 0) {  // nothing is in flight in that slot
+                r.copy(slot, t);
+                cp_async_commit();
+                cp_async_wait<0>();
+            } else if (!taken) {
+                fetch(t + kStages - 1);
+                cp_async_wait<kStages - 1>();
+            }
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) v[j] = slot[j][tid];
+            float top = tile_max<BF16>(v);
+            if (!(top <= FLT_MAX)) {  // +inf or nothing but NaN: the largest finite one
+                top = -CUDART_INF_F;
+                for (int i = 0; i < kMine; ++i) {
+                    const float x = r.staged(slot, tid, i);
+                    if (x <= FLT_MAX) top = fmaxf(top, x);
+                }
+            }
+            const uint32_t mine = float_key(top + 0.f);
+            uint32_t most = 0, least = 0;  // keys of the largest and the least of the CTA's maxima
+            int passing = 0;
+            if (careful) {
+                const uint32_t w_most = __reduce_max_sync(0xffffffffu, mine), w_least = __reduce_min_sync(0xffffffffu, mine);
+                if (lane == 0) {
+                    sh.most[warp] = w_most;
+                    sh.least[warp] = w_least;
+                }
+                passing = __syncthreads_count(top > thr);
+                most = sh.most[0];
+                least = sh.least[0];
+#pragma unroll
+                for (int i = 1; i < kWarps; ++i) {
+                    most = max(most, sh.most[i]);
+                    least = min(least, sh.least[i]);
+                }
+                if (!have_base && passing) {  // (thr is -inf until then) the first finite logits
+                    have_base = true;
+                    base.set(key_float(most));
+                    limit = key_float(most) + kRise;
+                }
+            }
+            if (have_base && redo < 0) {
+                if (top > limit) {  // a thread's own base from here on
+                    const Base old = base;
+                    base.set(top);
+                    limit = top + kRise;
+                    const float f = rebase(old, base);
+                    hi *= f;
+                    lo *= f;
+                }
+                float s = tile_sum<BF16>(v, base.c);
+                if (!(s <= FLT_MAX) || base.wide) {  // a logit that is not finite, or a wide base: one by one
+                    s = 0.f;
+                    for (int i = 0; i < kMine; ++i) {
+                        const float x = r.staged(slot, tid, i);
+                        if (fabsf(x) <= FLT_MAX) s += ex2(base.wide ? (x - base.c) * kLog2e : fmaf(x, kLog2e, -base.c));
+                    }
+                }
+                two_sum(hi, lo, s);
+            }
             float over = thr, tie = CUDART_INF_F;
-            int last_tie = -1, brings = passing;
+            int last_tie = -1;
             if (passing > kFew) {
-                const uint32_t mine = float_key(top + 0.f);
-                uint32_t below = float_key(thr), above = 0xff800000u;  // the keys of thr and of +inf
-                int n_above = 0;
+                // Too many threads would bring candidates.  Find a threshold that at least K of their maxima exceed and at
+                // most kFew, by bisection over the numbers (each step a count), or, where too many are equal, over the
+                // tokens of equal logits.
+                uint32_t below = max(float_key(thr), least - 1), above = most;  // more than kFew are over below, none over above
                 bool found = false;
                 while (above - below > 1) {
                     const uint32_t mid = below + (above - below) / 2;
@@ -393,78 +526,70 @@ __global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(const ScanAr
                         below = mid;
                     } else if (n < K) {
                         above = mid;
-                        n_above = n;
                     } else {
                         over = key_float(mid == 0x7fffffffu ? mid - 1 : mid);  // never -0, which no maximum's key is
-                        brings = n;
                         found = true;
                         break;
                     }
                 }
-                if (!found) {  // n_above < K maxima are over the number of key `above`, and more than kFew over the one below
+                if (!found) {  // fewer than K maxima are over the number of key `above`, more than kFew over the one below
                     over = tie = key_float(above);
-                    int first = INT32_MAX;  // my first logit equal to it
-#pragma unroll
-                    for (int j = kWords - 1; j >= 0; --j)
-#pragma unroll
-                        for (int e = kPer - 1; e >= 0; --e)
-                            if (logit<BF16>(v[j], e) == tie) first = r.token(t, j, e);
-                    int from = r.token(t, 0, 0) - tid * kPer - 1, to = from + kTileWords * kPer;  // (from, to]: the tile's tokens
-                    for (;;) {  // the number with first <= from is below K, with first <= to at least K
-                        last_tie = from + (to - from + 1) / 2;
-                        const int n = __syncthreads_count(first <= last_tie);
-                        if (n < K) from = last_tie;
-                        else if (n > kFew) to = last_tie;
-                        else {
-                            brings = n_above + n;
-                            break;
-                        }
+                    int mine_at = INT32_MAX;  // my first logit equal to it
+                    for (int i = kMine - 1; i >= 0; --i)
+                        if (r.staged(slot, tid, i) == tie) mine_at = r.token(t, i / kPer, i % kPer, tid);
+                    int lo_t = r.token(t, 0, 0, 0) - 1, hi_t = lo_t + kTileWords * kPer;  // (lo_t, hi_t]: the tile's tokens
+                    for (;;) {  // the number with mine_at <= lo_t is below K, with mine_at <= hi_t at least K
+                        last_tie = lo_t + (hi_t - lo_t + 1) / 2;
+                        const int n = __syncthreads_count(mine_at <= last_tie);
+                        if (n < K) lo_t = last_tie;
+                        else if (n > kFew) hi_t = last_tie;
+                        else break;
                     }
                 }
             }
-            constexpr int kMine = kWords * kPer;
-            if (bound + brings * kMine > kCap) {  // keep the K best; K are then at least as large as the least of them
-                const u64 best = best_of(sh);
-                __syncthreads();
-                if (warp == 0 && lane < K) sh.buf[lane] = best;
-                if (tid == 0) sh.count = min(sh.count, K);
-                __syncthreads();
-                bound = K;
-                const u64 least = sh.count == K ? sh.buf[K - 1] : 0;
-                if (least) over = fmaxf(over, candidate_logit(least));
-                __syncthreads();
+            // In a careful tile at most K - 1 + kFew threads bring theirs: these and what compact() leaves have room in buf.
+            static_assert((LLA_MAX_BEAMS - 1 + kFew) * kMine + LLA_MAX_BEAMS <= kCap, "candidates of a tile");
+            const unsigned who = __ballot_sync(0xffffffffu, top > over || top >= tie);
+            if (who) bring(who, slot, t, over, tie, last_tie);
+            ++t;
+            if (careful) {
+                if (passing) {
+                    thr = fmaxf(thr, over);
+                    __syncthreads();
+                    compact();
+                }
+                if (t == redo) redo = -1;
+                if (redo < 0) end = t;
+                continue;
             }
-            bound += brings * kMine;
-            if (top > over || top >= tie) {
-#pragma unroll
-                for (int j = 0; j < kWords; ++j)
-#pragma unroll
-                    for (int e = 0; e < kPer; ++e) {
-                        const float x = logit<BF16>(v[j], e);
-                        const int token = r.token(t, j, e);
-                        if (x > over || (x == tie && token <= last_tie)) {
-                            const int at = atomicAdd(&sh.count, 1);
-                            if (at < kCap) sh.buf[at] = candidate(x, token);
-                        }
-                    }
-            }
-            if (over > thr) thr = over;
         }
-#pragma unroll
-        for (int j = 0; j < kWords; ++j) v[j] = next[j];
+        if (t < end || !__syncthreads_or(brought)) continue;  // the end of a group
+        if (sh.count <= kCap) {
+            compact();
+        } else {  // some were dropped: the group once more
+            __syncthreads();
+            if (tid == 0) sh.count = kept;
+            redo = end;
+            t = from;
+            __syncthreads();
+        }
     }
-    // the share's best, and its sum: threads' sums in units of the largest m
-    const u64 best = best_of(sh);
+    // the share's best, and its sum
     const int at = row * a.shares + share;
-    if (warp == 0 && lane < K) a.lists[static_cast<int64_t>(at) * K + lane] = best;
-    float M = warp_max(have_m ? m : -CUDART_INF_F);
+    if (tid < K) a.lists[static_cast<int64_t>(at) * K + tid] = tid < kept ? sh.buf[tid] : 0;
+    __syncthreads();
+    // threads' sums in units of the base of the one whose base is highest
+    float M = warp_max(have_base ? base.at() : -CUDART_INF_F);
     if (lane == 0) sh.maxima[warp] = M;
     __syncthreads();
     M = sh.maxima[0];
 #pragma unroll
     for (int i = 1; i < kWarps; ++i) M = fmaxf(M, sh.maxima[i]);
-    if (have_m && m != M) {
-        const float f = ex2((m - M) * 1.44269504f);
+    if (have_base && base.at() == M) sh.base = base;  // those of equal at() are the same
+    __syncthreads();
+    const Base common = sh.base;
+    if (have_base && base.at() != M) {
+        const float f = rebase(base, common);
         hi *= f;
         lo *= f;
     }
@@ -485,7 +610,7 @@ __global__ void __launch_bounds__(kScanThreads, 4) beam_scan_kernel(const ScanAr
             two_sum(hi, lo, sh.his[i]);
             lo += sh.los[i];
         }
-        a.sums[at] = Share{M, hi, lo, 0.f};
+        a.sums[at] = Share{have_base ? common.c : -CUDART_INF_F, hi, lo, have_base && common.wide ? 1.f : 0.f};
     }
 }
 
@@ -521,8 +646,8 @@ __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const Finis
     __shared__ uint32_t tags[LLA_MAX_BEAMS][kListLen];
     __shared__ double total[LLA_MAX_BEAMS][kListLen];
     __shared__ u64 part[kFinishWarps][kListLen];
-    __shared__ double mass[LLA_MAX_BEAMS], log_mass[LLA_MAX_BEAMS], scale[LLA_MAX_BEAMS];
-    __shared__ float offset[LLA_MAX_BEAMS], score[LLA_MAX_BEAMS];
+    __shared__ double mass[LLA_MAX_BEAMS], log_mass[LLA_MAX_BEAMS], scale[LLA_MAX_BEAMS], offset[LLA_MAX_BEAMS];
+    __shared__ float score[LLA_MAX_BEAMS];
     __shared__ int state[LLA_MAX_BEAMS], length[LLA_MAX_BEAMS];  // state 0: dead, 1: goes on, 2: ended
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int W = a.W, K = a.K, b = blockIdx.x;
@@ -559,17 +684,20 @@ __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const Finis
             }
             if (p == parts - 1) {  // and the sum over the shares
                 const Share sum = lane < a.shares ? a.sums[(b * W + w) * a.shares + lane] : Share{-CUDART_INF_F, 0.f, 0.f, 0.f};
-                const float M = warp_max(sum.m);
+                const Base base = {sum.c, sum.wide != 0.f};
+                const float M = warp_max(base.at());
+                const int top_lane = __ffs(__ballot_sync(0xffffffffu, base.at() == M)) - 1;
+                const Base common = {__shfl_sync(0xffffffffu, base.c, top_lane), __shfl_sync(0xffffffffu, base.wide, top_lane) != 0};
                 double S = 0.0;
-                if (sum.m > -CUDART_INF_F) {
-                    const float f = sum.m == M ? 1.f : expf(sum.m - M);
+                if (sum.c > -CUDART_INF_F) {
+                    const float f = base.at() == M ? 1.f : rebase(base, common);
                     S = (static_cast<double>(sum.hi) + static_cast<double>(sum.lo)) * static_cast<double>(f);
                 }
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
                 if (lane == 0) {
                     mass[w] = S;
-                    offset[w] = M;
+                    offset[w] = common.wide ? static_cast<double>(common.c) : static_cast<double>(common.c) / static_cast<double>(kLog2e);
                 }
             }
         }
@@ -600,7 +728,7 @@ __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const Finis
             some = c != 0;
             if (some)
                 s = static_cast<double>(score[w]) +
-                    ((static_cast<double>(candidate_logit(c)) - static_cast<double>(offset[w])) - log_mass[w]);
+                    ((static_cast<double>(candidate_logit(c)) - offset[w]) - log_mass[w]);
         }
         total[w][lane] = s;
         keys[w][lane] = some ? double_key(s * scale[w]) : 0;
@@ -650,7 +778,7 @@ lla_status launch_beam_select(const BeamSelectArgs &b, cudaStream_t stream) {
     int shares = 1;
     int64_t best = INT64_MAX;
     for (int s = 1; s <= kMaxShares && s <= tiles; ++s) {
-        const int64_t turns = (static_cast<int64_t>(rows) * s + sms * 4 - 1) / (sms * 4);
+        const int64_t turns = (static_cast<int64_t>(rows) * s + sms * kScanCtas - 1) / (sms * kScanCtas);
         const int64_t cost = turns * ((tiles + s - 1) / s + 4);
         if (cost < best) {
             best = cost;
@@ -663,8 +791,11 @@ lla_status launch_beam_select(const BeamSelectArgs &b, cudaStream_t stream) {
     a.V = b.V; a.K = b.K; a.shares = shares;
     a.sums = static_cast<Share *>(b.workspace);
     a.lists = reinterpret_cast<u64 *>(a.sums + static_cast<size_t>(rows) * shares);
-    lla_status st = b.bf16 ? launch_ex(beam_scan_kernel<true>, dim3(rows * shares), kScanThreads, 0, stream, a)
-                           : launch_ex(beam_scan_kernel<false>, dim3(rows * shares), kScanThreads, 0, stream, a);
+    static DeviceOnce once[2];
+    auto kern = b.bf16 ? beam_scan_kernel<true> : beam_scan_kernel<false>;
+    lla_status st = raise_smem_limit(kern, static_cast<int>(sizeof(Scan)), once[b.bf16 ? 1 : 0]);
+    if (st != LLA_OK) return st;
+    st = launch_ex(kern, dim3(rows * shares), kScanThreads, static_cast<int>(sizeof(Scan)), stream, a);
     if (st != LLA_OK) return st;
     FinishArgs f = {};
     f.W = b.W; f.K = b.K; f.shares = shares;
