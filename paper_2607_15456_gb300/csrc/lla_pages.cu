@@ -147,33 +147,37 @@ free_kernel(int32_t *ref, int nb, const int32_t *table, int max_blocks, int32_t 
 constexpr int kPlanThreads = 1024;  // a sequence each, too
 static_assert(kPlanThreads == LLA_MAX_BATCH, "thread s plans sequence s");
 
-// Exclusive prefix sum over a CTA's threads and the CTA's total.  `part` has 33 entries; a barrier on both sides.
-template <typename T>
-__device__ __forceinline__ T block_scan(T v, T *part, T &total) {
+// Exclusive prefix sums of two values over a CTA's threads, and the CTA's totals.  `part` has 33 entries.  Three barriers.
+struct Two {
+    unsigned long long a;
+    int b;
+};
+__device__ __forceinline__ Two block_scan(Two v, Two *part, Two &total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    T inc = v;
+    auto scan = [&](Two x) {  // inclusive, of a warp
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const T u = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += u;
-    }
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned long long ua = __shfl_up_sync(0xffffffffu, x.a, o);
+            const int ub = __shfl_up_sync(0xffffffffu, x.b, o);
+            if (lane >= o) {
+                x.a += ua;
+                x.b += ub;
+            }
+        }
+        return x;
+    };
+    const Two inc = scan(v);
     __syncthreads();  // part is free
     if (lane == 31) part[warp] = inc;
     __syncthreads();
     if (warp == 0) {
-        T w = part[lane];
-        T winc = w;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const T u = __shfl_up_sync(0xffffffffu, winc, o);
-            if (lane >= o) winc += u;
-        }
-        part[lane] = winc - w;
-        if (lane == 31) part[32] = winc;
+        const Two w = part[lane], all = scan(w);
+        part[lane] = Two{all.a - w.a, all.b - w.b};
+        if (lane == 31) part[32] = all;
     }
     __syncthreads();
     total = part[32];
-    return part[warp] + inc - v;
+    return Two{part[warp].a + inc.a - v.a, part[warp].b + inc.b - v.b};
 }
 
 // The ledger entries [begin, end) of a thread of the cluster: consecutive entries to consecutive threads, a
@@ -213,6 +217,10 @@ struct ClusterSums {
 __device__ __forceinline__ ClusterSums cluster_sums(int mine, int *totals /* shared, 16 */) {
     cg::cluster_group cl = cg::this_cluster();
     const int rank = static_cast<int>(cl.block_rank()), n = static_cast<int>(cl.num_blocks());
+    if (n == 1) {
+        __syncthreads();
+        return ClusterSums{0, mine};
+    }
     if (threadIdx.x < static_cast<unsigned>(n)) cl.map_shared_rank(totals, threadIdx.x)[rank] = mine;
     cl.sync();
     ClusterSums s = {0, 0};
@@ -255,13 +263,13 @@ struct ExtendArgs {
 // is less than passing them on), all threads count the free blocks of their part of the ledger, and after the
 // cluster's exchange of counts each free block whose rank is below the need knows its sequence by a binary search.
 // Everything that is read and later changed (lengths, counts, last pages) is read before that exchange.
-__global__ void __launch_bounds__(kPlanThreads) extend_plan_kernel(const ExtendArgs a) {
+__global__ void __launch_bounds__(kPlanThreads, 1) extend_plan_kernel(const ExtendArgs a) {
     constexpr int kSlots = 2 * LLA_MAX_BATCH;
     __shared__ int key[kSlots], growers[kSlots], lowest[kSlots];
     __shared__ int first[LLA_MAX_BATCH];  // blocks that sequences before s take
     __shared__ int old_pages[LLA_MAX_BATCH], copy_of[LLA_MAX_BATCH];
-    __shared__ unsigned long long part64[33];
-    __shared__ int part[33], totals[16];
+    __shared__ Two part[33];
+    __shared__ int totals[16];
     cg::cluster_group cl = cg::this_cluster();
     const int tid = threadIdx.x, rank = static_cast<int>(cl.block_rank()), ctas = static_cast<int>(cl.num_blocks());
     for (int i = tid; i < kSlots; i += kPlanThreads) {
@@ -269,9 +277,13 @@ __global__ void __launch_bounds__(kPlanThreads) extend_plan_kernel(const ExtendA
         growers[i] = 0;
         lowest[i] = kSlots;
     }
-    cl.sync();  // every CTA has started
+    if (ctas > 1) cl.sync();  // every CTA has started
     pdl_wait();
     pdl_trigger();
+    // free blocks of my part of the ledger: its loads are under way beside those of the sequences
+    const Segment seg = my_segment(a.nb, rank, ctas);
+    int mine = 0;
+    for_ledger(a.ref, seg, [&](int, int count) { mine += count == 0; });
     // sequence tid: its growth, and whether others hold its last page
     int len = 0, n = 0, tail = -1, holders = 0;
     unsigned bad = 0;
@@ -302,9 +314,9 @@ __global__ void __launch_bounds__(kPlanThreads) extend_plan_kernel(const ExtendA
         }
     }
     if (bad && rank == 0) atomicOr(a.err, bad);
-    __syncthreads();
     int slot = 0;
     const bool shared_tail = n > 0 && holders > 1;
+    const bool some_shared = __syncthreads_or(shared_tail);  // (and the table is clear)
     if (shared_tail) {  // the growing holders of a page meet in a hash table: their number and the lowest of them
         slot = (static_cast<unsigned>(tail) * 2654435769u) >> 21;  // golden-ratio hashing to 2048 slots
         for (;;) {
@@ -315,28 +327,23 @@ __global__ void __launch_bounds__(kPlanThreads) extend_plan_kernel(const ExtendA
         atomicAdd(&growers[slot], 1);
         atomicMin(&lowest[slot], tid);
     }
-    __syncthreads();
+    if (some_shared) __syncthreads();
     const int copy = shared_tail && !(growers[slot] >= holders && lowest[slot] == tid);
     const int rows = len % kBlockTokens;
-    unsigned long long need = 0, all = 0;
+    unsigned long long need = 0;
     if (n > 0) need = static_cast<unsigned long long>(pages_of(len + n) - pages_of(len) + copy);
     // copies in the high bits: at most 2^10, and at most 2^10 * 2^24 blocks in the low ones
-    const unsigned long long at = block_scan<unsigned long long>(need | static_cast<unsigned long long>(copy) << 40, part64, all);
+    Two total;
+    const Two at = block_scan(Two{need | static_cast<unsigned long long>(copy) << 40, mine}, part, total);
     const unsigned long long low40 = (1ull << 40) - 1;
-    const int64_t wanted = static_cast<int64_t>(all & low40);
+    const int64_t wanted = static_cast<int64_t>(total.a & low40);
     // a need beyond the ledger is not granted, so that what is used of `first` is below 2^24
-    const int copy_index = static_cast<int>(at >> 40);
-    first[tid] = static_cast<int>(min(static_cast<unsigned long long>(LLA_MAX_BLOCKS) * 2, at & low40));
+    const int copy_index = static_cast<int>(at.a >> 40);
+    first[tid] = static_cast<int>(min(static_cast<unsigned long long>(LLA_MAX_BLOCKS) * 2, at.a & low40));
     old_pages[tid] = n > 0 ? pages_of(len) : 0;
     copy_of[tid] = copy ? copy_index : -1;
-    // free blocks of my part of the ledger (none needed and none asked for: no need to look)
-    const Segment seg = my_segment(a.nb, rank, ctas);
-    int mine = 0, cta_free = 0;
-    if (wanted > 0 || a.free_blocks)
-        for_ledger(a.ref, seg, [&](int, int count) { mine += count == 0; });
-    const int before_me = block_scan<int>(mine, part, cta_free);
-    const ClusterSums free = cluster_sums(cta_free, totals);
-    const bool granted = wanted <= free.all || wanted == 0;
+    const ClusterSums free = cluster_sums(total.b, totals);
+    const bool granted = wanted <= free.all;
     if (rank == 0) {
         if (tid < a.S) {
             if (a.lens_before) a.lens_before[tid] = len;
@@ -351,14 +358,14 @@ __global__ void __launch_bounds__(kPlanThreads) extend_plan_kernel(const ExtendA
             }
         }
         if (tid == 0) {
-            a.plan->copies = granted ? static_cast<int>(all >> 40) : 0;
+            a.plan->copies = granted ? static_cast<int>(total.a >> 40) : 0;
             if (a.free_blocks) *a.free_blocks = free.all - (granted ? static_cast<int>(wanted) : 0);
             if (!granted) atomicOr(a.err, LLA_DEVERR_PAGES);
         }
     }
     if (!granted || wanted == 0) return;
     // the k-th free block: to sequence s = the last with first[s] <= k
-    int k = free.before + before_me;
+    int k = free.before + at.b;
     if (k >= wanted) return;
     for_ledger(a.ref, seg, [&](int id, int count) {
         if (count != 0) return;
@@ -379,82 +386,125 @@ __global__ void __launch_bounds__(kPlanThreads) extend_plan_kernel(const ExtendA
     });
 }
 
-// Up to LLA_MAX_POOLS pools; first[l] is the number of pages that a block has in the pools before l.
+constexpr int kCopyThreads = 256, kCopyWarps = kCopyThreads / 32;
+constexpr int kCopyCtas = 4;        // of an SM
+constexpr int kSliceBytes = 4096;   // of a full page's plane, moved by a warp at once
+
+// Up to LLA_MAX_POOLS pools.  A page of pool l has slices[l] slices (of its K-plane, then of its V-plane); a CTA takes
+// kCopyWarps of them at once, of one page or of several: first[l] is the number of such units that a block has in the
+// pools before l.
 struct PoolSet {
     lla_pool p[LLA_MAX_POOLS];
     int first[LLA_MAX_POOLS + 1];
+    uint16_t slices[LLA_MAX_POOLS];
     int L;
 };
+__host__ __device__ __forceinline__ int k_slices(const lla_pool &p) { return (kBlockTokens * p.k_row_bytes + kSliceBytes - 1) / kSliceBytes; }
+__host__ __device__ __forceinline__ int v_slices(const lla_pool &p) { return (kBlockTokens * p.v_row_bytes + kSliceBytes - 1) / kSliceBytes; }
 
-__device__ __forceinline__ int pool_of(const PoolSet &ps, int unit) {
-    int lo = 0, hi = ps.L - 1;
+__device__ __forceinline__ int pool_of(const int *first, int L, int unit) {
+    int lo = 0, hi = L - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (ps.first[mid] <= unit) lo = mid;
+        if (first[mid] <= unit) lo = mid;
         else hi = mid - 1;
     }
     return lo;
 }
 
-constexpr int kCopyThreads = 256;
+constexpr int kSliceWords = kSliceBytes / 512;  // of 16 bytes, a lane's
 
-// Words of T that a warp moves, kAhead loads in flight per lane: n words, word w at byte offset at(w) of both sides.
-template <typename T, int kAhead, typename F>
-__device__ __forceinline__ void warp_copy(char *dst, const char *src, int n, F at) {
-    const int lane = threadIdx.x & 31;
-    for (int w0 = lane; w0 < n; w0 += 32 * kAhead) {
-        T v[kAhead];
-        int off[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-            if (w0 + 32 * j < n) {
-                off[j] = at(w0 + 32 * j);
-                v[j] = *reinterpret_cast<const T *>(src + off[j]);
-            }
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-            if (w0 + 32 * j < n) *reinterpret_cast<T *>(dst + off[j]) = v[j];
-    }
+// One load or store where `on`.
+__device__ __forceinline__ uint4 load_if(const char *p, bool on) {
+    uint4 v;
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t@p ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p), "r"(static_cast<uint32_t>(on)));
+    return v;
+}
+__device__ __forceinline__ void store_if(char *p, const uint4 &v, bool on) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t@p st.global.v4.u32 [%4], {%0, %1, %2, %3};\n\t}" ::"r"(v.x),
+                 "r"(v.y), "r"(v.z), "r"(v.w), "l"(p), "r"(static_cast<uint32_t>(on))
+                 : "memory");
 }
 
-// Behind the plan: the rows of copied pages in every pool, a warp per (copy, page), and the slots of the new tokens.
-// Of a page only the rows that hold tokens are read and written: the first `rows` of each K granule, and a prefix of
-// the V-plane.
-__global__ void __launch_bounds__(kCopyThreads, 4)
+// Behind the plan: the rows of copied pages in every pool, and the slots of the new tokens.  Of a page only the rows
+// that hold tokens are read and written: the first `rows` of each K granule, and a prefix of the V-plane.  A warp moves
+// a slice, 16 bytes a lane (4 where granules are that small), eight words in flight.
+__global__ void __launch_bounds__(kCopyThreads, kCopyCtas)
 extend_finish_kernel(const ExtendArgs a, const __grid_constant__ PoolSet ps, int64_t *slots) {
     pdl_wait();
     pdl_trigger();
     const ExtendPlan *plan = a.plan;
-    const int per_copy = ps.first[ps.L];
-    const int64_t units = static_cast<int64_t>(plan->copies) * per_copy;
-    const int warps = gridDim.x * (kCopyThreads / 32);
-    for (int64_t u = blockIdx.x * (kCopyThreads / 32) + (threadIdx.x >> 5); u < units; u += warps) {
-        const int c = static_cast<int>(u / per_copy), in_copy = static_cast<int>(u - static_cast<int64_t>(c) * per_copy);
-        const int l = pool_of(ps, in_copy), page = in_copy - ps.first[l];
-        const int kb = ps.p[l].k_row_bytes, vb = ps.p[l].v_row_bytes, rows = plan->copy[c].rows;
-        const int64_t page_bytes = static_cast<int64_t>(kBlockTokens) * (kb + vb);
-        char *base = static_cast<char *>(ps.p[l].base) + page * page_bytes;
-        const char *src = base + plan->copy[c].src * (page_bytes * ps.p[l].pages);
-        char *dst = base + plan->copy[c].dst * (page_bytes * ps.p[l].pages);
-        // word w of the K-plane is row w % rows of granule w / rows: (w + 1/2) / rows is at least 1/126 away from a
-        // whole number and at most 2048, where two roundings of fp32 are off by less than 2^-11
-        const float inv = 1.f / static_cast<float>(rows);
-        if (kb % 16 == 0)
-            warp_copy<uint4, 8>(dst, src, kb / 16 * rows, [&](int w) {
-                const int g = static_cast<int>((static_cast<float>(w) + 0.5f) * inv);
-                return (g * kBlockTokens + (w - g * rows)) * 16;
-            });
-        else
-            warp_copy<uint32_t, 8>(dst, src, kb / 4 * rows, [&](int w) {
-                const int g = static_cast<int>((static_cast<float>(w) + 0.5f) * inv);
-                return (g * kBlockTokens + (w - g * rows)) * 4;
-            });
-        const int v0 = kBlockTokens * kb, words = vb * rows / 16, rest = vb * rows % 16 / 4;
-        warp_copy<uint4, 8>(dst, src, words, [&](int w) { return v0 + w * 16; });
-        warp_copy<uint32_t, 1>(dst, src, rest, [&](int w) { return v0 + words * 16 + w * 4; });
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int copies = plan->copies, per_copy = max(1, ps.first[ps.L]), stride = gridDim.x;
+    // units in the order of copies, then pools and pages; a CTA takes every stride-th
+    const int step_c = stride / per_copy, step_in = stride - step_c * per_copy;
+    int c = blockIdx.x / per_copy, in_copy = blockIdx.x - c * per_copy;
+    for (; ps.L > 0 && c < copies; c += step_c, in_copy += step_in) {
+        if (in_copy >= per_copy) {
+            in_copy -= per_copy;
+            if (++c >= copies) break;
+        }
+        const int l = pool_of(ps.first, ps.L, in_copy);
+        const lla_pool pool = ps.p[l];
+        const int slices = ps.slices[l], units = (slices + kCopyWarps - 1) / kCopyWarps, in_pool = in_copy - ps.first[l];
+        int page, slice;
+        if (slices < kCopyWarps) {  // several pages
+            const int at_once = kCopyWarps / slices, p = warp / slices;
+            page = in_pool * at_once + p;
+            slice = warp - p * slices;
+            if (p >= at_once) continue;
+        } else {
+            page = in_pool / units;
+            slice = (in_pool - page * units) * kCopyWarps + warp;
+        }
+        if (page >= pool.pages || slice >= slices) continue;
+        const ExtendCopy job = plan->copy[c];
+        const int kb = pool.k_row_bytes, vb = pool.v_row_bytes, rows = job.rows;
+        const int64_t page_bytes = static_cast<int64_t>(kBlockTokens) * (kb + vb), block = page_bytes * pool.pages;
+        const char *src = static_cast<const char *>(pool.base) + page * page_bytes + job.src * block;
+        char *dst = static_cast<char *>(pool.base) + page * page_bytes + job.dst * block;
+        // The lane's words j * 32 + lane of 16 bytes, where bit j of `mask` is set, and words of 4 bytes at off_a and off_b.
+        const int ks = k_slices(pool);
+        unsigned mask;
+        int off_a = -1, off_b = -1;
+        if (slice < ks) {
+            // The plane as words of 16 bytes in a row: with granules of 16 bytes word w is row w % 64, with granules of 4
+            // it is rows 4 (w % 16) to 4 (w % 16) + 3, of which the last rows % 4 go as words of 4 bytes.
+            src += slice * kSliceBytes;
+            dst += slice * kSliceBytes;
+            const int bytes = min(kSliceBytes, kBlockTokens * kb - slice * kSliceBytes);  // a multiple of 256
+            const unsigned all = (1u << (bytes - lane * 16 + 511) / 512) - 1;  // bytes > lane * 16 - 512
+            if (kb % 16 == 0) {
+                mask = all & ((lane < rows ? 0x5555u : 0u) | (lane + 32 < rows ? 0xaaaau : 0u));
+            } else {
+                mask = lane % 16 < rows / 4 ? all : 0u;
+                const int r = lane % 4, at = lane / 4 * 256 + rows / 4 * 16 + r * 4;
+                if (r < rows % 4 && at < bytes) off_a = at;
+                if (r < rows % 4 && at + 2048 < bytes) off_b = at + 2048;
+            }
+        } else {
+            const int words = vb * rows / 16, rest = vb * rows % 16 / 4;  // of 16 bytes, and of 4 behind them
+            const int share = (words + (slices - ks) - 1) / (slices - ks);
+            const int w0 = (slice - ks) * share, n = min(words - w0, share) - lane;
+            src += kBlockTokens * kb + w0 * 16;
+            dst += kBlockTokens * kb + w0 * 16;
+            mask = (1u << (max(0, n) + 31) / 32) - 1;
+            if (slice == slices - 1 && lane < rest) off_a = (words - w0) * 16 + lane * 4;
+        }
+        uint32_t rest_a = 0, rest_b = 0;
+        if (off_a >= 0) rest_a = *reinterpret_cast<const uint32_t *>(src + off_a);
+        if (off_b >= 0) rest_b = *reinterpret_cast<const uint32_t *>(src + off_b);
+        uint4 v[kSliceWords];
+#pragma unroll
+        for (int j = 0; j < kSliceWords; ++j) v[j] = load_if(src + lane * 16 + j * 512, mask >> j & 1);
+#pragma unroll
+        for (int j = 0; j < kSliceWords; ++j) store_if(dst + lane * 16 + j * 512, v[j], mask >> j & 1);
+        if (off_a >= 0) *reinterpret_cast<uint32_t *>(dst + off_a) = rest_a;
+        if (off_b >= 0) *reinterpret_cast<uint32_t *>(dst + off_b) = rest_b;
     }
-    const int threads = gridDim.x * kCopyThreads;
-    for (int i = blockIdx.x * kCopyThreads + threadIdx.x; i < a.N; i += threads) {
+    for (int i = blockIdx.x * kCopyThreads + threadIdx.x; i < a.N; i += stride * kCopyThreads) {
         int s, j;
         if (a.cu_new) {
             int lo = 0, hi = a.S - 1;
@@ -499,19 +549,25 @@ struct CompactArgs {
     unsigned *err;
 };
 
-__global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const CompactArgs a) {
-    __shared__ int part[33], totals[16];
+__global__ void __launch_bounds__(kPlanThreads, 1) compact_plan_kernel(const CompactArgs a) {
+    __shared__ Two part[33];
+    __shared__ int totals[16];
     cg::cluster_group cl = cg::this_cluster();
     const int tid = threadIdx.x, rank = static_cast<int>(cl.block_rank()), ctas = static_cast<int>(cl.num_blocks());
-    cl.sync();  // every CTA has started
+    auto sync_all = [&]() {
+        if (ctas > 1) cl.sync();
+        else __syncthreads();
+    };
+    if (ctas > 1) cl.sync();  // every CTA has started
     pdl_wait();
     pdl_trigger();
     const Segment seg = my_segment(a.nb, rank, ctas);
-    int mine = 0, cta_live = 0;
+    int mine = 0;
     for_ledger(a.ref, seg, [&](int, int count) { mine += count != 0; });
-    const int before_me = block_scan<int>(mine, part, cta_live);
-    const ClusterSums live = cluster_sums(cta_live, totals);
-    const int R = live.all, my_rank = live.before + before_me;
+    Two total;
+    const Two before_me = block_scan(Two{0, mine}, part, total);
+    const ClusterSums live = cluster_sums(total.b, totals);
+    const int R = live.all, my_rank = live.before + before_me.b;
     // blocks in use below R, known to the one thread whose entries hold R (nobody where all are in use)
     if (R == a.nb) {
         if (rank == 0 && tid == 0) a.plan->live_below = R;
@@ -520,7 +576,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const Compac
         for_ledger(a.ref, seg, [&](int id, int count) { lr += id < R && count != 0; });
         a.plan->live_below = lr;
     }
-    cl.sync();
+    sync_all();
     const int below = *static_cast<volatile int *>(&a.plan->live_below);
     int lr = my_rank;
     for_ledger(a.ref, seg, [&](int id, int count) {
@@ -533,7 +589,7 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(const Compac
             if (id < R) a.holes[id - lr] = id;
         }
     });
-    cl.sync();
+    sync_all();
     const int moves = R - below;
     for (int k = rank * kPlanThreads + tid; k < moves; k += ctas * kPlanThreads) {
         const int from = a.movers[k], to = a.holes[k];
@@ -581,12 +637,7 @@ __global__ void __launch_bounds__(kCopyThreads) compact_move_kernel(const Compac
     const int64_t units = static_cast<int64_t>(a.plan->moves) * per_block;
     for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
         const int k = static_cast<int>(u / per_block), in_block = static_cast<int>(u - static_cast<int64_t>(k) * per_block);
-        int lo = 0, hi = bs.L - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (bs.first[mid] <= in_block) lo = mid;
-            else hi = mid - 1;
-        }
+        const int lo = pool_of(bs.first, bs.L, in_block);
         const int64_t bytes = bs.bytes[lo], off = static_cast<int64_t>(in_block - bs.first[lo]) * kMoveBytes;
         const char *src = bs.base[lo] + a.movers[k] * bytes + off;
         char *dst = bs.base[lo] + a.holes[k] * bytes + off;
@@ -666,16 +717,20 @@ lla_status launch_pages_extend(const lla_pages &p, const lla_pool *pools, int L,
     PoolSet ps = {};
     ps.L = L;
     for (int l = 0; l < L; ++l) {
+        const int slices = k_slices(pools[l]) + v_slices(pools[l]);
         ps.p[l] = pools[l];
-        ps.first[l + 1] = ps.first[l] + pools[l].pages;
+        ps.slices[l] = static_cast<uint16_t>(slices);
+        const int at_once = slices < kCopyWarps ? kCopyWarps / slices : 1;
+        const int units = slices < kCopyWarps ? (pools[l].pages + at_once - 1) / at_once
+                                              : pools[l].pages * ((slices + kCopyWarps - 1) / kCopyWarps);
+        ps.first[l + 1] = ps.first[l] + units;
     }
     if ((st = launch_plan(extend_plan_kernel, plan_ctas(p.num_blocks), a, stream)) != LLA_OK) return st;
     const int sms = num_sms();
     if (sms <= 0) return LLA_ERR_CUDA;
     // every CTA resident at once; no more than there can be work for
-    const int64_t work = static_cast<int64_t>(p.S) * ps.first[L] * 32 + N;
-    const int64_t ctas = (work + kCopyThreads - 1) / kCopyThreads;
-    return launch_ex(extend_finish_kernel, dim3(static_cast<unsigned>(ctas < sms * 4 ? (ctas > 0 ? ctas : 1) : sms * 4)),
+    const int64_t work = static_cast<int64_t>(p.S) * ps.first[L] + (N + kCopyThreads - 1) / kCopyThreads;
+    return launch_ex(extend_finish_kernel, dim3(static_cast<unsigned>(work < sms * kCopyCtas ? (work > 0 ? work : 1) : sms * kCopyCtas)),
                      kCopyThreads, 0, stream, a, ps, slots);
 }
 
