@@ -85,17 +85,35 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const ForkArgs a) {
     }
     const int p = blockIdx.x - a.to_S;
     const int n = pages_of(max(0, checked_len(a.from_lens[p], a.from_max)));
-    if (static_cast<int>(blockIdx.y) * kForkSpan >= n) return;
-    int change = -1;
-    if (n <= a.to_max)
-        for (int i = 0; i < a.to_S; i += kForkThreads)
-            change += __syncthreads_count(i + tid < a.to_S && a.parents[i + tid] == p);
+    const int lo0 = blockIdx.y * kForkSpan;
+    if (lo0 >= n) return;
     const int32_t *row = a.from_table + static_cast<int64_t>(p) * a.from_max;
-    for (int lo = blockIdx.y * kForkSpan + tid; lo < n; lo += gridDim.y * kForkSpan) {
-        const int hi = min(n, lo - tid + kForkSpan);
-#pragma unroll 4
-        for (int i = lo; i < hi; i += kForkThreads) {
-            const int b = row[i];
+    constexpr int kEach = kForkSpan / kForkThreads;
+    int v[kEach];  // the first span's blocks, read while the children are counted
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) v[j] = lo0 + tid + j * kForkThreads < n ? row[lo0 + tid + j * kForkThreads] : 0;
+    int mine = 0;
+    if (n <= a.to_max) {
+#pragma unroll
+        for (int j = 0; j < LLA_MAX_BATCH / kForkThreads; ++j) {
+            const int i = tid + j * kForkThreads;
+            if (i < a.to_S) mine += a.parents[i] == p;
+        }
+    }
+    __shared__ int children[kForkThreads / 32];
+    mine = __reduce_add_sync(0xffffffffu, mine);
+    if (tid % 32 == 0) children[tid / 32] = mine;
+    __syncthreads();
+    int change = -1;
+#pragma unroll
+    for (int w = 0; w < kForkThreads / 32; ++w) change += children[w];
+    for (int lo = lo0; lo < n; lo += gridDim.y * kForkSpan) {
+        const int hi = min(n, lo + kForkSpan);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int i = lo + tid + j * kForkThreads;
+            if (i >= hi) break;
+            const int b = lo == lo0 ? v[j] : row[i];
             if (b < 0 || b >= a.nb)
                 bad = LLA_DEVERR_BLOCK_ID;
             else if (change)
@@ -180,32 +198,65 @@ __device__ __forceinline__ Two block_scan(Two v, Two *part, Two &total) {
     return Two{part[warp].a + inc.a - v.a, part[warp].b + inc.b - v.b};
 }
 
-// The ledger entries [begin, end) of a thread of the cluster: consecutive entries to consecutive threads, a
-// multiple of four each, so that they are read in 16-byte words.
+// The ledger entries [begin, end) of a warp of the cluster, 128 at a time: lane l has entries 4 l to 4 l + 3 of them.
 struct Segment {
     int begin, end;
 };
 __device__ __forceinline__ Segment my_segment(int nb, int rank, int ctas) {
-    const int threads = ctas * kPlanThreads;
-    const int per = ((nb + threads - 1) / threads + 3) & ~3;
-    const int64_t b = static_cast<int64_t>(rank * kPlanThreads + threadIdx.x) * per;
+    const int warps = ctas * (kPlanThreads / 32);
+    const int64_t per = (static_cast<int64_t>(nb) + warps * 128 - 1) / (warps * 128) * 128;
+    const int64_t b = (rank * (kPlanThreads / 32) + (threadIdx.x >> 5)) * per;
     Segment s;
     s.begin = static_cast<int>(b < nb ? b : nb);
     s.end = static_cast<int>(b + per < nb ? b + per : nb);
     return s;
 }
-// f(id, count) for the entries of a segment, in order.
-template <typename F>
-__device__ __forceinline__ void for_ledger(const int32_t *ref, Segment s, F f) {
-    int i = s.begin;
-    for (; i + 4 <= s.end; i += 4) {
-        const int4 v = *reinterpret_cast<const int4 *>(ref + i);
-        f(i, v.x);
-        f(i + 1, v.y);
-        f(i + 2, v.z);
-        f(i + 3, v.w);
+// The lane's four entries of those from i on; what lies behind the ledger is `none`.
+__device__ __forceinline__ int4 ledger_four(const int32_t *ref, int nb, int i, int none) {
+    i += (threadIdx.x & 31) * 4;
+    if (i + 4 <= nb) return *reinterpret_cast<const int4 *>(ref + i);
+    return make_int4(i < nb ? ref[i] : none, i + 1 < nb ? ref[i + 1] : none, i + 2 < nb ? ref[i + 2] : none, none);
+}
+// Bit k: the k-th of four entries is free, or (FREE false) in use.
+template <bool FREE>
+__device__ __forceinline__ unsigned four_flags(int4 v) {
+    return static_cast<unsigned>((v.x == 0) == FREE) | static_cast<unsigned>((v.y == 0) == FREE) << 1 |
+           static_cast<unsigned>((v.z == 0) == FREE) << 2 | static_cast<unsigned>((v.w == 0) == FREE) << 3;
+}
+// How many of the segment's entries (below `limit`) are free, or in use: a lane's part of it.
+template <bool FREE>
+__device__ __forceinline__ int count_ledger(const int32_t *ref, int nb, Segment s, int limit) {
+    int n = 0;
+#pragma unroll 4
+    for (int i = s.begin; i < s.end; i += 128) {
+        unsigned m = four_flags<FREE>(ledger_four(ref, nb, i, FREE ? 1 : 0));
+        const int left = limit - (i + static_cast<int>(threadIdx.x & 31) * 4);
+        if (left < 4) m &= left > 0 ? (1u << left) - 1 : 0u;
+        n += __popc(m);
     }
-    for (; i < s.end; ++i) f(i, ref[i]);
+    return n;
+}
+// f(id, counted, rank) for every entry of the segment, rank being the number of counted entries before it; `rank` is that
+// of the segment's first entry.  Ends early where no rank below `enough` is left.
+template <bool FREE, typename F>
+__device__ __forceinline__ void rank_ledger(const int32_t *ref, int nb, Segment s, int rank, int64_t enough, F f) {
+    const unsigned lane = threadIdx.x & 31, below = (1u << lane) - 1;
+    for (int i = s.begin; i < s.end && rank < enough; i += 128) {
+        const unsigned m = four_flags<FREE>(ledger_four(ref, nb, i, FREE ? 1 : 0));
+        int r = rank;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const unsigned b = __ballot_sync(0xffffffffu, m >> k & 1);
+            r += __popc(b & below);
+            rank += __popc(b);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int id = i + static_cast<int>(lane) * 4 + k;
+            if (id < nb) f(id, (m >> k & 1) != 0, r);
+            r += m >> k & 1;
+        }
+    }
 }
 
 // Sums `mine` over the CTAs of the cluster: what the CTAs before this one have, and all.  A cluster barrier lies in
@@ -282,8 +333,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) extend_plan_kernel(const Exte
     pdl_trigger();
     // free blocks of my part of the ledger: its loads are under way beside those of the sequences
     const Segment seg = my_segment(a.nb, rank, ctas);
-    int mine = 0;
-    for_ledger(a.ref, seg, [&](int, int count) { mine += count == 0; });
+    const int mine = count_ledger<true>(a.ref, a.nb, seg, a.nb);
     // sequence tid: its growth, and whether others hold its last page
     int len = 0, n = 0, tail = -1, holders = 0;
     unsigned bad = 0;
@@ -365,24 +415,20 @@ __global__ void __launch_bounds__(kPlanThreads, 1) extend_plan_kernel(const Exte
     }
     if (!granted || wanted == 0) return;
     // the k-th free block: to sequence s = the last with first[s] <= k
-    int k = free.before + at.b;
-    if (k >= wanted) return;
-    for_ledger(a.ref, seg, [&](int id, int count) {
-        if (count != 0) return;
-        if (k < wanted) {
-            int lo = 0, hi = a.S - 1;  // first[lo] <= k
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (first[mid] <= k) lo = mid;
-                else hi = mid - 1;
-            }
-            const int i = k - first[lo], c = copy_of[lo];
-            // the copied last page comes first, then the fresh ones
-            a.table[static_cast<int64_t>(lo) * a.max_blocks + old_pages[lo] + i - (c >= 0)] = id;
-            if (c >= 0 && i == 0) a.plan->copy[c].dst = id;
-            a.ref[id] = 1;
+    const int warp_first = free.before + __shfl_sync(0xffffffffu, at.b, 0);
+    rank_ledger<true>(a.ref, a.nb, seg, warp_first, wanted, [&](int id, bool is_free, int k) {
+        if (!is_free || k >= wanted) return;
+        int lo = 0, hi = a.S - 1;  // first[lo] <= k
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (first[mid] <= k) lo = mid;
+            else hi = mid - 1;
         }
-        ++k;
+        const int i = k - first[lo], c = copy_of[lo];
+        // the copied last page comes first, then the fresh ones
+        a.table[static_cast<int64_t>(lo) * a.max_blocks + old_pages[lo] + i - (c >= 0)] = id;
+        if (c >= 0 && i == 0) a.plan->copy[c].dst = id;
+        a.ref[id] = 1;
     });
 }
 
@@ -562,31 +608,27 @@ __global__ void __launch_bounds__(kPlanThreads, 1) compact_plan_kernel(const Com
     pdl_wait();
     pdl_trigger();
     const Segment seg = my_segment(a.nb, rank, ctas);
-    int mine = 0;
-    for_ledger(a.ref, seg, [&](int, int count) { mine += count != 0; });
+    const int mine = count_ledger<false>(a.ref, a.nb, seg, a.nb);
     Two total;
     const Two before_me = block_scan(Two{0, mine}, part, total);
     const ClusterSums live = cluster_sums(total.b, totals);
-    const int R = live.all, my_rank = live.before + before_me.b;
-    // blocks in use below R, known to the one thread whose entries hold R (nobody where all are in use)
+    const int R = live.all, my_rank = live.before + __shfl_sync(0xffffffffu, before_me.b, 0);
+    // blocks in use below R, known to the one warp whose entries hold R (nobody where all are in use)
     if (R == a.nb) {
         if (rank == 0 && tid == 0) a.plan->live_below = R;
     } else if (seg.begin <= R && R < seg.end) {
-        int lr = my_rank;
-        for_ledger(a.ref, seg, [&](int id, int count) { lr += id < R && count != 0; });
-        a.plan->live_below = lr;
+        const int below_r = __reduce_add_sync(0xffffffffu, count_ledger<false>(a.ref, a.nb, seg, R));
+        if (tid % 32 == 0) a.plan->live_below = my_rank + below_r;
     }
     sync_all();
     const int below = *static_cast<volatile int *>(&a.plan->live_below);
-    int lr = my_rank;
-    for_ledger(a.ref, seg, [&](int id, int count) {
-        if (count != 0) {
+    rank_ledger<false>(a.ref, a.nb, seg, my_rank, INT64_MAX, [&](int id, bool in_use, int r) {
+        if (in_use) {
             if (id < R) a.remap[id] = id;
-            else a.movers[lr - below] = id;
-            ++lr;
+            else a.movers[r - below] = id;
         } else {
             a.remap[id] = -1;
-            if (id < R) a.holes[id - lr] = id;
+            if (id < R) a.holes[id - r] = id;
         }
     });
     sync_all();
@@ -655,7 +697,7 @@ __global__ void __launch_bounds__(kCopyThreads) compact_move_kernel(const Compac
 // ------------------------------------------------------------------------------------------- launches
 
 // CTAs of a plan's cluster.
-int plan_ctas(int64_t num_blocks) { return num_blocks > 16384 ? 8 : 1; }
+int plan_ctas(int64_t num_blocks) { return num_blocks > 8192 ? 8 : 1; }
 
 template <typename A>
 lla_status launch_plan(void (*kern)(A), int ctas, const A &a, cudaStream_t stream) {
