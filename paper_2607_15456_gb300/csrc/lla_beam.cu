@@ -36,8 +36,8 @@ constexpr int kWords = 4;                             // 16-byte words of a thre
 constexpr int kTileWords = kScanThreads * kWords;     // 16 KB a tile
 constexpr int kStages = 2;                            // tiles in shared memory
 constexpr int kScanCtas = 4;                          // of an SM
-constexpr int kFew = 40;                              // threads of a tile that may bring candidates
-constexpr int kCap = 2304;                            // candidates that a CTA holds
+constexpr int kFew = 4;                               // threads over K that may bring candidates of a tile
+constexpr int kCap = 2176;                            // candidates that a CTA holds
 constexpr int kMaxShares = 32;                        // shares of a row: a warp merges them
 constexpr int kListLen = LLA_MAX_BEAMS;               // a list is a warp's lanes
 constexpr float kRise = 60.f;                         // a logit this far over m moves m (e^60 2^24 is finite)
@@ -313,6 +313,13 @@ __device__ __forceinline__ void cp_async_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+// One more of *count; its value before.
+__device__ __forceinline__ int claim(int *count) {
+    int old;
+    asm volatile("atom.shared.add.u32 %0, [%1], 1;" : "=r"(old) : "r"(smem_addr(count)) : "memory");
+    return old;
+}
+
 // The best 32 of the first n candidates, sorted, in the lanes of warp 0.
 __device__ __forceinline__ u64 best_of(Scan &sh, int n) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -345,7 +352,7 @@ __global__ void __launch_bounds__(kScanThreads, kScanCtas) beam_scan_kernel(cons
     const int tiles = (r.words() + kTileWords - 1) / kTileWords;
     const int t0 = static_cast<int>(static_cast<int64_t>(share) * tiles / a.shares);
     const int t1 = static_cast<int>(static_cast<int64_t>(share + 1) * tiles / a.shares);
-    const int K = a.K;
+    const int K = a.K, few = K + kFew;
     // The ring: tile t is copied kStages - 1 tiles ahead, a thread's words by itself.
     const int in0 = r.first_whole(), in1 = min(t1, r.end_whole());
     const uint32_t ring = smem_addr(&sh.ring[0][0][tid]);
@@ -383,49 +390,62 @@ __global__ void __launch_bounds__(kScanThreads, kScanCtas) beam_scan_kernel(cons
     bool have_base = false;
     int kept = 0;  // candidates in buf that are the best so far, sorted
     bool brought = false;
-    // buf's best to its front; with K of them, only larger logits of later tokens count.  Barriers.
+    // buf's best to its front, sorted; with K of them, only larger logits of later tokens count.  Up to a candidate a thread:
+    // its place is the number of better ones (no two are equal).  More of them are sorted.  Barriers, one behind the
+    // last candidate of all before.
     auto compact = [&]() {
         const int n = min(sh.count, kCap);
-        const u64 best = best_of(sh, n);
+        u64 mine = 0;
+        int place = tid;
+        if (n <= kScanThreads / 2) {
+            if (warp * 32 < n) {
+                mine = tid < n ? sh.buf[tid] : 0;
+                place = tid < n ? 0 : kScanThreads;
+#pragma unroll 8
+                for (int i = 0; i < n; ++i) place += sh.buf[i] > mine;
+            }
+        } else {
+            mine = best_of(sh, n);
+        }
         __syncthreads();
         kept = min(n, K);
-        if (warp == 0 && lane < kept) sh.buf[lane] = best;
+        if (place < kept) sh.buf[place] = mine;
         if (tid == 0) sh.count = kept;
         __syncthreads();
         if (kept == K) thr = fmaxf(thr, candidate_logit(sh.buf[K - 1]));
     };
-    // The candidates of a warp's threads `who`, thread by thread: a lane to each of that thread's logits.
-    auto bring = [&](unsigned who, const uint4(*slot)[kScanThreads], int t, float over, float tie, int last_tie) {
+    // The candidates of a warp's threads `who`, thread by thread: a lane to each of that thread's logits, where pass(x, token).
+    auto bring = [&](unsigned who, const uint4(*slot)[kScanThreads], int t, auto pass) {
         brought = true;
         __syncwarp();  // the words that other lanes copied
+        const int token0 = r.token(t, lane / kPer, lane % kPer, warp * 32);
         do {
-            const int owner = warp * 32 + __ffs(who) - 1;
+            const int owner = __ffs(who) - 1;
             who &= who - 1;
-            const int token = r.token(t, lane / kPer, lane % kPer, owner);
-            float x = -CUDART_INF_F;
-            if (lane < kMine) x = r.staged(slot, owner, lane);
-            const bool some = (x > over || (x == tie && token <= last_tie)) && x <= FLT_MAX;
-            const unsigned which = __ballot_sync(0xffffffffu, some);
-            int at = 0;
-            if (lane == 0) at = atomicAdd(&sh.count, __popc(which));
-            at = __shfl_sync(0xffffffffu, at, 0) + __popc(which & ((1u << lane) - 1));
-            if (some && at < kCap) sh.buf[at] = candidate(x, token);
+            if (lane < kMine) {
+                const float x = r.staged(slot, warp * 32 + owner, lane);
+                const int token = token0 + owner * kPer;
+                if (pass(x, token)) {
+                    const int at = claim(&sh.count);
+                    if (at < kCap) sh.buf[at] = candidate(x, token);
+                }
+            }
         } while (who);
         __syncwarp();  // before the words are overwritten
     };
 
-    // Tiles go by in groups of 1, 3, 12, 48 ...; within a group each warp goes by itself and brings what passes the
+    // Tiles go by in groups of 1, 2, 6, 18 ...; within a group each warp goes by itself and brings what passes the
     // threshold, and at its end the threshold rises to the K-th best.  The first tile, those after it while fewer than
     // K logits were finite, and a group that brought too much (rising logits), once more, go tile by tile,
     // carefully: the threshold rises before candidates are brought.
-    int from = t0, end = t0, group = 3, redo = -1;  // redo: where a group is gone through once more, its end
+    int from = t0, end = t0, group = 2, redo = -1;  // redo: where a group is gone through once more, its end
     __syncthreads();  // sh.count
     for (int t = t0; t < t1;) {
         const bool careful = redo >= 0 || !have_base || thr == -CUDART_INF_F;
         if (!careful && t == end) {
             from = t;
             end = min(t1, t + group);
-            group *= 4;
+            group *= 3;
             brought = false;
         }
         uint4 v[kWords];
@@ -444,7 +464,7 @@ __global__ void __launch_bounds__(kScanThreads, kScanCtas) beam_scan_kernel(cons
                 if (__any_sync(0xffffffffu, !(top <= usual) || !(s <= FLT_MAX))) {
                     taken = __any_sync(0xffffffffu, !(top <= limit) || !(s <= FLT_MAX));
                     if (taken) break;
-                    bring(__ballot_sync(0xffffffffu, top > thr), slot, t, thr, CUDART_INF_F, -1);
+                    bring(__ballot_sync(0xffffffffu, top > thr), slot, t, [&](float x, int) { return x > thr; });
                 }
                 two_sum(hi, lo, s);
             }
@@ -513,16 +533,16 @@ __global__ void __launch_bounds__(kScanThreads, kScanCtas) beam_scan_kernel(cons
             }
             float over = thr, tie = CUDART_INF_F;
             int last_tie = -1;
-            if (passing > kFew) {
+            if (passing > few) {
                 // Too many threads would bring candidates.  Find a threshold that at least K of their maxima exceed and at
-                // most kFew, by bisection over the numbers (each step a count), or, where too many are equal, over the
+                // most `few`, by bisection over the numbers (each step a count), or, where too many are equal, over the
                 // tokens of equal logits.
-                uint32_t below = max(float_key(thr), least - 1), above = most;  // more than kFew are over below, none over above
+                uint32_t below = max(float_key(thr), least - 1), above = most;  // more than `few` are over below, none over above
                 bool found = false;
                 while (above - below > 1) {
                     const uint32_t mid = below + (above - below) / 2;
                     const int n = __syncthreads_count(mine > mid);
-                    if (n > kFew) {
+                    if (n > few) {
                         below = mid;
                     } else if (n < K) {
                         above = mid;
@@ -532,25 +552,29 @@ __global__ void __launch_bounds__(kScanThreads, kScanCtas) beam_scan_kernel(cons
                         break;
                     }
                 }
-                if (!found) {  // fewer than K maxima are over the number of key `above`, more than kFew over the one below
+                if (!found) {  // fewer than K maxima are over the number of key `above`, more than `few` over the one below
                     over = tie = key_float(above);
                     int mine_at = INT32_MAX;  // my first logit equal to it
                     for (int i = kMine - 1; i >= 0; --i)
                         if (r.staged(slot, tid, i) == tie) mine_at = r.token(t, i / kPer, i % kPer, tid);
-                    int lo_t = r.token(t, 0, 0, 0) - 1, hi_t = lo_t + kTileWords * kPer;  // (lo_t, hi_t]: the tile's tokens
-                    for (;;) {  // the number with mine_at <= lo_t is below K, with mine_at <= hi_t at least K
+                    // Threads over the tie, or with a tie up to a token: fewer than K up to lo_t, more than few up to hi_t (the
+                    // whole tile), and one more at most from token to token, so that some token gives K to few of them.
+                    // Fewer than 20 halvings lead there.
+                    int lo_t = r.token(t, 0, 0, 0) - 1, hi_t = lo_t + kTileWords * kPer;
+                    for (int step = 0; step < 32; ++step) {
                         last_tie = lo_t + (hi_t - lo_t + 1) / 2;
-                        const int n = __syncthreads_count(mine_at <= last_tie);
+                        const int n = __syncthreads_count(mine > above || mine_at <= last_tie);
                         if (n < K) lo_t = last_tie;
-                        else if (n > kFew) hi_t = last_tie;
+                        else if (n > few) hi_t = last_tie;
                         else break;
                     }
                 }
             }
-            // In a careful tile at most K - 1 + kFew threads bring theirs: these and what compact() leaves have room in buf.
-            static_assert((LLA_MAX_BEAMS - 1 + kFew) * kMine + LLA_MAX_BEAMS <= kCap, "candidates of a tile");
+            // In a careful tile at most K + few threads bring theirs: these and what compact() leaves have room in buf.
+            static_assert((2 * LLA_MAX_BEAMS - 1 + kFew) * kMine + LLA_MAX_BEAMS <= kCap, "candidates of a tile");
             const unsigned who = __ballot_sync(0xffffffffu, top > over || top >= tie);
-            if (who) bring(who, slot, t, over, tie, last_tie);
+            if (who)
+                bring(who, slot, t, [&](float x, int token) { return x <= FLT_MAX && (x > over || (x == tie && token <= last_tie)); });
             ++t;
             if (careful) {
                 if (passing) {

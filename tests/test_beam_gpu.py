@@ -223,6 +223,18 @@ def rows_of_a_kind(lla, what, V, dtype, B, W):
     Select(lla, z, scores(V, B, W), K).check()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("K", [1, 2, 6, 21, 22, 31, 32])
+def test_ties_of_every_number(lla, K, dtype):
+    """Rounded logits: from row to row another number of logits share the K-th best value, a handful or thousands."""
+    B, W, V = 16, 4, 9000
+    g = torch.Generator(device=DEV).manual_seed(K)
+    step = 2.0 ** (torch.arange(B * W, device=DEV).view(B, W, 1) / 7 - 7)
+    z = (torch.round(torch.randn(B, W, V, generator=g, device=DEV) / step) * step).to(dtype)
+    z[0, :, 300:] = -math.inf  # few finite ones, equal in part
+    Select(lla, z, scores(K, B, W), K).check()
+
+
 def test_the_same_beam_twice(lla):
     """Equal beams tie everywhere: the lower beam first, then the lower token."""
     z = logits(4, 1, 1, 5000, BF16).expand(1, 4, 5000).contiguous()
