@@ -664,50 +664,92 @@ __device__ __forceinline__ u64 double_key(double x) {
     return u ^ ((u >> 63) ? ~0ull : 1ull << 63);
 }
 
+// log x of a normal positive x, off by less than 1e-12: x = 2^e m with m between sqrt(1/2) and sqrt(2), and
+// log m = 2 atanh t = 2 (t + t^3 / 3 + ... + t^13 / 13), t = (m - 1) / (m + 1), |t| <= 0.172.  An fp64 operation
+// is slow and this is on the way of every call: about 15 one after the other, a third of the library's.
+__device__ __forceinline__ double log_of(double x) {
+    long long u = __double_as_longlong(x);
+    const long long half = 0x3fe6a09e667f3bcdll;  // sqrt(1/2)
+    const int e = static_cast<int>((u - half) >> 52);
+    const double m = __longlong_as_double(u - (static_cast<long long>(e) << 52));
+    const double d = m + 1.0;
+    const double r0 = static_cast<double>(__frcp_rn(static_cast<float>(d)));
+    const double r = r0 * (2.0 - d * r0);  // one step of Newton: 2^-23 squared
+    const double t = (m - 1.0) * r, w = t * t;
+    double p = 1.0 / 13.0;
+    p = p * w + 1.0 / 11.0;
+    p = p * w + 1.0 / 9.0;
+    p = p * w + 1.0 / 7.0;
+    p = p * w + 1.0 / 5.0;
+    p = p * w + 1.0 / 3.0;
+    p = p * w + 1.0;
+    return static_cast<double>(e) * 0.693147180559945309 + 2.0 * t * p;
+}
+
+// exp x for |x| <= 400, off by less than 1e-13 of itself: x = k log 2 + r, |r| <= 0.347, and the series of exp r to r^13.
+__device__ __forceinline__ double exp_of(double x) {
+    const double k = rint(x * 1.4426950408889634);
+    const double r = fma(-k, 2.3190468138462996e-17, fma(-k, 0.6931471805599453, x));  // log 2 as a sum of two
+    double p = 1.0 / 6227020800.0;
+    p = p * r + 1.0 / 479001600.0;
+    p = p * r + 1.0 / 39916800.0;
+    p = p * r + 1.0 / 3628800.0;
+    p = p * r + 1.0 / 362880.0;
+    p = p * r + 1.0 / 40320.0;
+    p = p * r + 1.0 / 5040.0;
+    p = p * r + 1.0 / 720.0;
+    p = p * r + 1.0 / 120.0;
+    p = p * r + 1.0 / 24.0;
+    p = p * r + 1.0 / 6.0;
+    p = p * r + 0.5;
+    p = p * r + 1.0;
+    p = p * r + 1.0;
+    return p * __longlong_as_double((static_cast<long long>(k) + 1023) << 52);
+}
+
 __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const FinishArgs a) {
     __shared__ u64 cand[LLA_MAX_BEAMS][kListLen];    // each beam's best, sorted
     __shared__ u64 keys[LLA_MAX_BEAMS][kListLen];
     __shared__ uint32_t tags[LLA_MAX_BEAMS][kListLen];
     __shared__ double total[LLA_MAX_BEAMS][kListLen];
     __shared__ u64 part[kFinishWarps][kListLen];
-    __shared__ double mass[LLA_MAX_BEAMS], log_mass[LLA_MAX_BEAMS], scale[LLA_MAX_BEAMS], offset[LLA_MAX_BEAMS];
-    __shared__ float score[LLA_MAX_BEAMS];
-    __shared__ int state[LLA_MAX_BEAMS], length[LLA_MAX_BEAMS];  // state 0: dead, 1: goes on, 2: ended
+    __shared__ double mass[LLA_MAX_BEAMS], offset[LLA_MAX_BEAMS];  // S in units of exp(offset)
+    __shared__ double rest[LLA_MAX_BEAMS], scale[LLA_MAX_BEAMS];   // score - log S, n^-alpha
+    __shared__ int state[LLA_MAX_BEAMS], length[LLA_MAX_BEAMS];    // state 0: dead, 1: goes on, 2: ended
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int W = a.W, K = a.K, b = blockIdx.x;
+    const int W = a.W, K = a.K, row0 = blockIdx.x * W;
     pdl_wait();
     pdl_trigger();
-    if (tid < W) {
-        const int row = b * W + tid;
-        const float s = a.scores[row];
-        score[tid] = s;
-        const bool ended = a.finished && a.finished[row];
-        state[tid] = !(fabsf(s) <= FLT_MAX) ? 0 : ended ? 2 : 1;
-        const int64_t n = a.lengths ? static_cast<int64_t>(a.lengths[row]) + (ended ? 0 : 1) : 1;
-        length[tid] = static_cast<int>(n < INT32_MAX ? n : INT32_MAX);
-        mass[tid] = 0.0;
+    // the last warp keeps the beams' states, and n^-alpha while the others merge
+    float my_score = 0.f;
+    if (warp == kFinishWarps - 1 && lane < W) {
+        const float s = a.scores[row0 + lane];
+        const bool ended = a.finished && a.finished[row0 + lane];
+        const int64_t n = a.lengths ? static_cast<int64_t>(a.lengths[row0 + lane]) + (ended ? 0 : 1) : 1;
+        state[lane] = !(fabsf(s) <= FLT_MAX) ? 0 : ended ? 2 : 1;
+        length[lane] = static_cast<int>(n < INT32_MAX ? n : INT32_MAX);
+        scale[lane] = a.alpha == 0.0 ? 1.0 : exp_of(-a.alpha * log_of(static_cast<double>(n > 1 ? n : 1)));  // |x| <= 16 log 2^31
+        my_score = s;
     }
-    __syncthreads();
-    // n^-alpha of every beam by the last warp, while the others merge
-    if (warp == kFinishWarps - 1 && lane < W)
-        scale[lane] = a.alpha == 0.0 ? 1.0 : pow(static_cast<double>(max(1, length[lane])), -a.alpha);
-    // parts warps merge a beam's shares, then one of them the parts
+    // `parts` warps merge the lists of a beam's shares and one of them sums up its shares (of a beam that does not go on,
+    // whatever is there, which nobody looks at); then one of them merges the parts
     const int parts = max(1, min(4, min(a.shares, kFinishWarps / W)));
     const int at_once = kFinishWarps / parts;
     for (int w0 = 0; w0 < W; w0 += at_once) {
         const int w = w0 + warp / parts, p = warp % parts;
-        const bool mine = warp / parts < at_once && w < W && state[w < W ? w : 0] == 1;
+        const bool mine = warp / parts < at_once && w < W;
         u64 top = 0;
         if (mine) {
-            const u64 *list = a.lists + static_cast<int64_t>(b * W + w) * a.shares * K;
-            u64 ahead = p < a.shares && lane < K ? list[static_cast<int64_t>(p) * K + lane] : 0;
+            const u64 *list = a.lists + static_cast<int64_t>(row0 + w) * a.shares * K;
+            u64 ahead = lane < K ? list[static_cast<int64_t>(p) * K + lane] : 0;
+            Share sum = {-CUDART_INF_F, 0.f, 0.f, 0.f};
+            if (p == parts - 1 && lane < a.shares) sum = a.sums[(row0 + w) * a.shares + lane];
             for (int s = p; s < a.shares; s += parts) {
                 const u64 v = ahead;
                 ahead = s + parts < a.shares && lane < K ? list[static_cast<int64_t>(s + parts) * K + lane] : 0;
                 top = s == p ? v : merge_desc(top, v);
             }
-            if (p == parts - 1) {  // and the sum over the shares
-                const Share sum = lane < a.shares ? a.sums[(b * W + w) * a.shares + lane] : Share{-CUDART_INF_F, 0.f, 0.f, 0.f};
+            if (p == parts - 1) {
                 const Base base = {sum.c, sum.wide != 0.f};
                 const float M = warp_max(base.at());
                 const int top_lane = __ffs(__ballot_sync(0xffffffffu, base.at() == M)) - 1;
@@ -717,11 +759,10 @@ __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const Finis
                     const float f = base.at() == M ? 1.f : rebase(base, common);
                     S = (static_cast<double>(sum.hi) + static_cast<double>(sum.lo)) * static_cast<double>(f);
                 }
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
+                for (int o = 1; o < a.shares; o <<= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
                 if (lane == 0) {
                     mass[w] = S;
-                    offset[w] = common.wide ? static_cast<double>(common.c) : static_cast<double>(common.c) / static_cast<double>(kLog2e);
+                    offset[w] = common.wide ? static_cast<double>(common.c) : static_cast<double>(common.c) * (1.0 / static_cast<double>(kLog2e));
                 }
             }
         }
@@ -738,24 +779,22 @@ __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const Finis
         }
     }
     __syncthreads();
-    if (warp == 0 && lane < W) log_mass[lane] = mass[lane] > 0.0 ? log(mass[lane]) : 0.0;
+    if (warp == kFinishWarps - 1 && lane < W)
+        rest[lane] = state[lane] == 1 && mass[lane] > 0.0 ? static_cast<double>(my_score) - log_of(mass[lane]) : static_cast<double>(my_score);
     __syncthreads();
     for (int w = warp; w < W; w += kFinishWarps) {
-        double s = 0.0;
+        double s = rest[w];
         bool some = false;
         if (state[w] == 2) {
-            s = score[w];
             some = lane == 0;
             if (some) cand[w][0] = candidate(0.f, a.eos);
         } else if (state[w] == 1) {
             const u64 c = lane < K ? cand[w][lane] : 0;
             some = c != 0;
-            if (some)
-                s = static_cast<double>(score[w]) +
-                    ((static_cast<double>(candidate_logit(c)) - offset[w]) - log_mass[w]);
+            s += static_cast<double>(candidate_logit(c)) - offset[w];  // exact near the offset, and not lost beside a huge one
         }
         total[w][lane] = s;
-        keys[w][lane] = some ? double_key(s * scale[w]) : 0;
+        keys[w][lane] = some ? double_key(a.alpha == 0.0 ? s : s * scale[w]) : 0;
         tags[w][lane] = w * kListLen + lane;
     }
     __syncthreads();
@@ -769,11 +808,11 @@ __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const Finis
         __syncthreads();
     }
     if (tid < K) {
-        const int at = b * K + tid;
+        const int at = blockIdx.x * K + tid;
         const bool some = keys[0][tid] != 0;
         const int w = tags[0][tid] / kListLen, i = tags[0][tid] % kListLen;
         const int token = some ? candidate_token(cand[w][i]) : -1;
-        a.parents[at] = some ? b * W + w : -1;
+        a.parents[at] = some ? row0 + w : -1;
         a.tokens[at] = token;
         a.out_scores[at] = some ? static_cast<float>(total[w][i]) : -CUDART_INF_F;
         if (a.out_finished) a.out_finished[at] = !some || state[w] == 2 || token == a.eos;
