@@ -495,7 +495,8 @@ lla_status lla_dense_decode_attn(const lla_geometry *g, const lla_cache *cache,
  * The paper has no counterpart: its caches are fabricated (Sec. 7); this is what a serving program
  * (parallel samples, beam search, shared prompts) needs around the calls above.
  *
- * With every count and length zero (cudaMemset) all blocks are free and all sequences empty.
+ * With every count and length zero (cudaMemset) all blocks are free and all sequences empty.  Calls on one
+ * ledger, and calls that read its pages, must be ordered (one stream).
  */
 #define LLA_MAX_BLOCKS (1 << 24)
 #define LLA_MAX_POOLS 128
@@ -585,7 +586,7 @@ lla_status lla_pages_compact_workspace_size(int64_t num_blocks, size_t *bytes);
  * whole, in every pool), and the tables of `pages` and ref_count follow.
  *   pages  holds every table of the ledger; a table that it does not hold is renamed with `remap`
  *   remap  device [num_blocks] int32, written: the new number of every block, -1 for a free one
- *   live   device int32, written: R
+ *   live   device int32, written: R.  Neither may lie in ref_count or a table (LLA_ERR_INVALID_ARG)
  * Two kernels on the stream; the workspace as for lla_pages_extend.
  */
 lla_status lla_pages_compact(const lla_pages *pages, const lla_pool *pools, int32_t L, int32_t *remap,
@@ -620,7 +621,8 @@ lla_status lla_beam_select_workspace_size(int32_t B, int32_t W, int32_t V, int32
  *   out_scores    device [B][K] fp32, written: s, rounded once (-inf where parents is -1)
  *   out_finished  device [B][K] uint8 or NULL, written: 1 where the token is eos or parents is -1, else 0
  *   out_lengths   device [B][K] int32 or NULL, written (0 where parents is -1)
- * W, K <= LLA_MAX_BEAMS, B W <= LLA_MAX_BATCH, V <= LLA_MAX_VOCAB.  No output may overlap an input.  Two
+ * W, K <= LLA_MAX_BEAMS, B W <= LLA_MAX_BATCH, V <= LLA_MAX_VOCAB.  No output may overlap an input
+ * (LLA_ERR_INVALID_ARG among scores, flags and lengths).  Two
  * kernels on the stream; the workspace as for lla_pages_extend.
  */
 lla_status lla_beam_select(int32_t B, int32_t W, int32_t V, int32_t K, const void *logits,

@@ -616,6 +616,8 @@ bool overlap(const void *a, size_t na, const void *b, size_t nb) {
     return na > 0 && nb > 0 && x < y + nb && y < x + na;
 }
 
+size_t table_bytes(const lla_pages *p) { return static_cast<size_t>(p->S) * p->max_blocks_per_seq * 4; }
+
 lla_status pool_of_geometry(const lla_geometry *g, int max_rank, int pages, void *pool, lla_pool *out) {
     const lla_status st = check_geometry(g, max_rank);
     if (st != LLA_OK) return st;
@@ -625,6 +627,18 @@ lla_status pool_of_geometry(const lla_geometry *g, int max_rank, int pages, void
 }
 
 }  // namespace
+
+// Two page sets of one ledger whose arrays do not overlap (also what lla_beam_search asks of its two).
+extern "C++" lla_status lla::check_fork(const lla_pages *from, const lla_pages *to) {
+    lla_status st = check_pages(from);
+    if (st != LLA_OK) return st;
+    if ((st = check_pages(to)) != LLA_OK) return st;
+    if (from->ref_count != to->ref_count || from->num_blocks != to->num_blocks) return LLA_ERR_INVALID_ARG;
+    if (overlap(from->block_table, table_bytes(from), to->block_table, table_bytes(to)) ||
+        overlap(from->context_lens, static_cast<size_t>(from->S) * 4, to->context_lens, static_cast<size_t>(to->S) * 4))
+        return LLA_ERR_INVALID_ARG;
+    return LLA_OK;
+}
 
 lla_status lla_cache_pool(const lla_geometry *g, void *pool, lla_pool *out) {
     return pool_of_geometry(g, kMaxRank, g ? g->H : 0, pool, out);
@@ -644,15 +658,11 @@ lla_status lla_rope_pool(int32_t d_rope, void *rope_pool, lla_pool *out) {
 }
 
 lla_status lla_pages_fork(const lla_pages *from, const lla_pages *to, const int32_t *parents, void *stream) {
-    lla_status st = check_pages(from);
+    const lla_status st = check_fork(from, to);
     if (st != LLA_OK) return st;
-    if ((st = check_pages(to)) != LLA_OK) return st;
-    if (from->ref_count != to->ref_count || from->num_blocks != to->num_blocks) return LLA_ERR_INVALID_ARG;
     if (to->S > 0 && !parents) return LLA_ERR_INVALID_ARG;
-    const size_t ft = static_cast<size_t>(from->S) * from->max_blocks_per_seq * 4, fl = static_cast<size_t>(from->S) * 4;
-    const size_t tt = static_cast<size_t>(to->S) * to->max_blocks_per_seq * 4, tl = static_cast<size_t>(to->S) * 4;
-    if (overlap(from->block_table, ft, to->block_table, tt) || overlap(from->context_lens, fl, to->context_lens, tl) ||
-        overlap(parents, tl, to->block_table, tt) || overlap(parents, tl, to->context_lens, tl))
+    if (overlap(parents, static_cast<size_t>(to->S) * 4, to->block_table, table_bytes(to)) ||
+        overlap(parents, static_cast<size_t>(to->S) * 4, to->context_lens, static_cast<size_t>(to->S) * 4))
         return LLA_ERR_INVALID_ARG;
     if (from->S + to->S == 0) return LLA_OK;
     return launch_pages_fork(*from, *to, parents, static_cast<cudaStream_t>(stream));
@@ -705,6 +715,10 @@ lla_status lla_pages_compact(const lla_pages *pages, const lla_pool *pools, int3
     if (st != LLA_OK) return st;
     if ((st = check_pools(pools, L)) != LLA_OK) return st;
     if (!remap || !live || !workspace || !aligned(workspace, 16)) return LLA_ERR_INVALID_ARG;
+    const size_t ledger = static_cast<size_t>(pages->num_blocks) * 4;
+    if (overlap(remap, ledger, pages->ref_count, ledger) || overlap(remap, ledger, pages->block_table, table_bytes(pages)) ||
+        overlap(live, 4, pages->ref_count, ledger) || overlap(live, 4, remap, ledger))
+        return LLA_ERR_INVALID_ARG;
     if (workspace_bytes < pages_compact_workspace_bytes(pages->num_blocks)) return LLA_ERR_WORKSPACE;
     return launch_pages_compact(*pages, pools, L, remap, live, workspace, static_cast<cudaStream_t>(stream));
 }
@@ -741,6 +755,12 @@ lla_status lla_beam_select(int32_t B, int32_t W, int32_t V, int32_t K, const voi
     if (B == 0) return LLA_OK;
     if (!logits || !aligned(logits, elem_size(logits_dtype)) || !scores || !parents || !tokens || !out_scores)
         return LLA_ERR_INVALID_ARG;
+    const size_t in = static_cast<size_t>(B) * W * 4, out = static_cast<size_t>(B) * K * 4;
+    const void *const ins[] = {scores, lengths}, *const outs[] = {parents, tokens, out_scores, out_lengths};
+    for (const void *o : outs)
+        for (const void *i : ins)
+            if (o && i && overlap(o, out, i, in)) return LLA_ERR_INVALID_ARG;
+    if (finished && out_finished && overlap(finished, in / 4, out_finished, out / 4)) return LLA_ERR_INVALID_ARG;
     if (!workspace || !aligned(workspace, 16)) return LLA_ERR_INVALID_ARG;
     if (workspace_bytes < beam_select_workspace_bytes(B, W, V, K, logits_dtype == LLA_BF16)) return LLA_ERR_WORKSPACE;
     BeamSelectArgs a = {};

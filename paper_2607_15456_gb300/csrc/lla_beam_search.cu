@@ -48,6 +48,7 @@ extern "C" lla_status lla_beam_search(const lla_pages *pages_a, const lla_pages 
     if (st != LLA_OK) return st;
     const int64_t n = static_cast<int64_t>(B) * W;
     if (!pages_a || !pages_b || pages_a->S != n || pages_b->S != n || steps < 0) return LLA_ERR_INVALID_ARG;
+    if ((st = lla::check_fork(pages_a, pages_b)) != LLA_OK) return st;
     if (n == 0 || steps == 0) return LLA_OK;
     if (!step || !tokens || !scores || !finished || !lengths || !parents) return LLA_ERR_INVALID_ARG;
     if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return LLA_ERR_INVALID_ARG;

@@ -140,6 +140,7 @@ lla_status launch_rope_key_store(int d_rope, double base, int pairing, void *rop
                                  const void *k, int x_bf16, const int32_t *positions, const int64_t *slots,
                                  int N, cudaStream_t stream);
 
+lla_status check_fork(const lla_pages *from, const lla_pages *to);  // (lla_abi.cu)
 // Sequences that share pages (lla_pages.cu): launches behind the checks of lla_abi.cu (no empty batch).
 lla_status launch_pages_fork(const lla_pages &from, const lla_pages &to, const int32_t *parents, cudaStream_t stream);
 lla_status launch_pages_free(const lla_pages &p, const int32_t *seqs, int n, cudaStream_t stream);

@@ -78,6 +78,7 @@ def test_fork_checks(lla):
     assert fork(b=pages(lla, other, block_table=a.block_table + 4 * 8 * 4 - 4)) == INVALID  # the last entry
     assert fork(b=pages(lla, other, context_lens=a.context_lens - 12)) == INVALID
     assert fork(parents=other + 0x200000) == INVALID                        # the lengths it writes
+    assert fork(parents=other + 0x100000 + 16) == INVALID                   # the table it writes
     assert lla.library().lla_pages_fork(None, ctypes.byref(a), FAKE, None) == INVALID
     none = dict(S=0, block_table=None, context_lens=None)
     assert fork(a=pages(lla, **none), b=pages(lla, other, **none), parents=None) == OK
@@ -131,7 +132,7 @@ def test_free_and_compact_checks(lla):
     assert so.lla_pages_compact_workspace_size((1 << 24) + 1, ctypes.byref(n)) == UNSUPPORTED
     assert so.lla_pages_compact_workspace_size(100, None) == INVALID
 
-    def compact(p=None, pools=None, remap=FAKE, live=FAKE, ws=FAKE, ws_bytes=BIG):
+    def compact(p=None, pools=None, remap=FAKE + 0x800000, live=FAKE + 0x900000, ws=FAKE, ws_bytes=BIG):
         arr = (lla.lla_pool * 1)(pools or pool(lla))
         return so.lla_pages_compact(ctypes.byref(p or pages(lla)), arr, 1, remap, live, ws, ws_bytes, None)
 
@@ -140,6 +141,10 @@ def test_free_and_compact_checks(lla):
     for bad in BAD_POOLS:
         assert compact(pools=pool(lla, **bad)) == INVALID, bad
     assert compact(remap=None) == INVALID
+    assert compact(remap=FAKE + 4 * 99) == INVALID                          # the last count
+    assert compact(remap=FAKE + 0x100000 - 4) == INVALID                    # a table
+    assert compact(live=FAKE) == INVALID
+    assert compact(live=FAKE + 0x800000 + 4) == INVALID
     assert compact(live=None) == INVALID
     assert compact(ws=None) == INVALID
     assert compact(ws=FAKE + 4) == INVALID
@@ -155,16 +160,20 @@ def test_select_checks(lla):
                         (dict(W=33), UNSUPPORTED), (dict(K=33), UNSUPPORTED), (dict(V=(1 << 24) + 1), UNSUPPORTED), (dict(B=257), INVALID)):
         assert size(**bad) == status, bad
 
-    def select(B=2, W=4, V=100, K=8, z=FAKE, stride=100, dt=0, s=FAKE, n=FAKE, eos=-1, alpha=0.0, parents=FAKE, tokens=FAKE, scores=FAKE, lens=FAKE,
-               ws=FAKE, ws_bytes=BIG):
-        return so.lla_beam_select(B, W, V, K, z, stride, dt, s, None, n, eos, alpha, parents, tokens, scores, None, lens, ws, ws_bytes, None)
+    at = lambda i: FAKE + i * 0x1000
+
+    def select(B=2, W=4, V=100, K=8, z=FAKE, stride=100, dt=0, s=at(1), fin=at(2), n=at(3), eos=-1, alpha=0.0, parents=at(4), tokens=at(5),
+               scores=at(6), ended=at(7), lens=at(8), ws=at(9), ws_bytes=BIG):
+        return so.lla_beam_select(B, W, V, K, z, stride, dt, s, fin, n, eos, alpha, parents, tokens, scores, ended, lens, ws, ws_bytes, None)
 
     for bad, status in ((dict(B=-1), INVALID), (dict(W=0), INVALID), (dict(V=0), INVALID), (dict(K=0), INVALID), (dict(dt=2), INVALID), (dict(B=257), INVALID),
                         (dict(W=33), UNSUPPORTED), (dict(K=33), UNSUPPORTED), (dict(stride=99), INVALID), (dict(stride=1 << 41), INVALID),
                         (dict(z=None), INVALID), (dict(z=FAKE + 1), INVALID), (dict(z=FAKE + 2, dt=1), INVALID), (dict(s=None), INVALID),
                         (dict(eos=-2), INVALID), (dict(eos=100), INVALID), (dict(alpha=17.0), INVALID), (dict(alpha=float("nan")), INVALID),
                         (dict(n=None), INVALID), (dict(n=None, lens=None, alpha=1.0), INVALID), (dict(parents=None), INVALID), (dict(tokens=None), INVALID),
-                        (dict(scores=None), INVALID), (dict(ws=None), INVALID), (dict(ws=FAKE + 8), INVALID), (dict(ws_bytes=need - 1), WORKSPACE)):
+                        (dict(scores=None), INVALID), (dict(ws=None), INVALID), (dict(ws=FAKE + 8), INVALID), (dict(ws_bytes=need - 1), WORKSPACE),
+                        (dict(scores=at(1)), INVALID), (dict(scores=at(1) - 60), INVALID), (dict(lens=at(3)), INVALID), (dict(ended=at(2) + 7), INVALID),
+                        (dict(parents=at(3)), INVALID)):
         assert select(**bad) == status, bad
     assert select(B=0, z=None, s=None, parents=None, tokens=None, scores=None, ws=None) == OK
 
@@ -187,7 +196,7 @@ def test_search_checks(lla):
                         (dict(steps=-1), INVALID), (dict(V=0), INVALID), (dict(dt=3), INVALID), (dict(step=lla.STEP_FN(0)), INVALID), (dict(tokens=None), INVALID),
                         (dict(scores=None), INVALID), (dict(finished=None), INVALID), (dict(lengths=None), INVALID), (dict(parents=None), INVALID),
                         (dict(ws=None), INVALID), (dict(ws=FAKE + 4), INVALID), (dict(ws_bytes=need - 1), WORKSPACE),
-                        (dict(a=pages(lla, ref_count=None)), INVALID)):
+                        (dict(a=pages(lla, ref_count=None)), INVALID), (dict(b=pages(lla)), INVALID)):
         assert search(**bad) == status, bad
     assert search(steps=0) == OK
     assert not called
