@@ -112,7 +112,7 @@ __device__ __forceinline__ u64 sort_desc(u64 v) {
         for (int j = k >> 1; j > 0; j >>= 1) {
             const u64 o = shfl_xor64(v, j);
             const bool keep_max = ((lane & j) == 0) == ((lane & k) == 0);
-            v = keep_max ? (v > o ? v : o) : (v < o ? v : o);
+            v = (v > o) == keep_max ? v : o;  // one comparison and a select
         }
     return v;
 }
@@ -124,7 +124,7 @@ __device__ __forceinline__ u64 merge_desc(u64 a, u64 b) {
 #pragma unroll
     for (int j = 16; j > 0; j >>= 1) {
         const u64 o = shfl_xor64(v, j);
-        v = (lane & j) == 0 ? (v > o ? v : o) : (v < o ? v : o);
+        v = (v > o) == ((lane & j) == 0) ? v : o;
     }
     return v;
 }
@@ -134,7 +134,7 @@ struct Ranked {
     uint32_t tag;
 };
 __device__ __forceinline__ bool better(const Ranked &a, const Ranked &b) {
-    return a.key != b.key ? a.key > b.key : a.tag < b.tag;
+    return (a.key > b.key) | ((a.key == b.key) & (a.tag < b.tag));
 }
 __device__ __forceinline__ Ranked merge_ranked(Ranked a, Ranked b) {
     const int lane = threadIdx.x & 31;
@@ -660,13 +660,14 @@ struct FinishArgs {
 
 // Doubles in order as unsigned integers (no NaN); 0 is below all of them.
 __device__ __forceinline__ u64 double_key(double x) {
-    const u64 u = static_cast<u64>(__double_as_longlong(x + 0.0));
+    u64 u = static_cast<u64>(__double_as_longlong(x));
+    if (u << 1 == 0) u = 0;  // -0
     return u ^ ((u >> 63) ? ~0ull : 1ull << 63);
 }
 
-// log x of a normal positive x, off by less than 1e-12: x = 2^e m with m between sqrt(1/2) and sqrt(2), and
+// log x of a normal positive x (of another: some number), off by less than 1e-12: x = 2^e m with m between sqrt(1/2) and sqrt(2), and
 // log m = 2 atanh t = 2 (t + t^3 / 3 + ... + t^13 / 13), t = (m - 1) / (m + 1), |t| <= 0.172.  An fp64 operation
-// is slow and this is on the way of every call: about 15 one after the other, a third of the library's.
+// takes about 100 cycles here, and this is on the way of every call: about 15 one after the other.
 __device__ __forceinline__ double log_of(double x) {
     long long u = __double_as_longlong(x);
     const long long half = 0x3fe6a09e667f3bcdll;  // sqrt(1/2)
@@ -713,8 +714,10 @@ __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const Finis
     __shared__ uint32_t tags[LLA_MAX_BEAMS][kListLen];
     __shared__ double total[LLA_MAX_BEAMS][kListLen];
     __shared__ u64 part[kFinishWarps][kListLen];
-    __shared__ double mass[LLA_MAX_BEAMS], offset[LLA_MAX_BEAMS];  // S in units of exp(offset)
-    __shared__ double rest[LLA_MAX_BEAMS], scale[LLA_MAX_BEAMS];   // score - log S, n^-alpha
+    __shared__ double offset[LLA_MAX_BEAMS], rest[LLA_MAX_BEAMS];  // S is in units of exp(offset); score - log S
+    __shared__ double scale[LLA_MAX_BEAMS];                        // n^-alpha
+    __shared__ float2 mass[LLA_MAX_BEAMS];                         // S as a sum of two
+    __shared__ float score_of[LLA_MAX_BEAMS];
     __shared__ int state[LLA_MAX_BEAMS], length[LLA_MAX_BEAMS];    // state 0: dead, 1: goes on, 2: ended
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int W = a.W, K = a.K, row0 = blockIdx.x * W;
@@ -728,13 +731,16 @@ __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const Finis
         const int64_t n = a.lengths ? static_cast<int64_t>(a.lengths[row0 + lane]) + (ended ? 0 : 1) : 1;
         state[lane] = !(fabsf(s) <= FLT_MAX) ? 0 : ended ? 2 : 1;
         length[lane] = static_cast<int>(n < INT32_MAX ? n : INT32_MAX);
+        score_of[lane] = my_score = s;
         scale[lane] = a.alpha == 0.0 ? 1.0 : exp_of(-a.alpha * log_of(static_cast<double>(n > 1 ? n : 1)));  // |x| <= 16 log 2^31
-        my_score = s;
     }
     // `parts` warps merge the lists of a beam's shares and one of them sums up its shares (of a beam that does not go on,
     // whatever is there, which nobody looks at); then one of them merges the parts
     const int parts = max(1, min(4, min(a.shares, kFinishWarps / W)));
     const int at_once = kFinishWarps / parts;
+    // A warp's fp64 instruction holds the SM's one fp64 unit for about 20 cycles, whatever its lanes do: a few beams'
+    // logarithms are taken by their warps beside the merges, those of many by one warp behind them.
+    const bool logs_here = W <= 4;
     for (int w0 = 0; w0 < W; w0 += at_once) {
         const int w = w0 + warp / parts, p = warp % parts;
         const bool mine = warp / parts < at_once && w < W;
@@ -743,27 +749,31 @@ __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const Finis
             const u64 *list = a.lists + static_cast<int64_t>(row0 + w) * a.shares * K;
             u64 ahead = lane < K ? list[static_cast<int64_t>(p) * K + lane] : 0;
             Share sum = {-CUDART_INF_F, 0.f, 0.f, 0.f};
-            if (p == parts - 1 && lane < a.shares) sum = a.sums[(row0 + w) * a.shares + lane];
-            for (int s = p; s < a.shares; s += parts) {
-                const u64 v = ahead;
-                ahead = s + parts < a.shares && lane < K ? list[static_cast<int64_t>(s + parts) * K + lane] : 0;
-                top = s == p ? v : merge_desc(top, v);
-            }
+            float score = 0.f;
             if (p == parts - 1) {
+                if (lane < a.shares) sum = a.sums[(row0 + w) * a.shares + lane];
+                if (logs_here) score = a.scores[row0 + w];
                 const Base base = {sum.c, sum.wide != 0.f};
                 const float M = warp_max(base.at());
                 const int top_lane = __ffs(__ballot_sync(0xffffffffu, base.at() == M)) - 1;
                 const Base common = {__shfl_sync(0xffffffffu, base.c, top_lane), __shfl_sync(0xffffffffu, base.wide, top_lane) != 0};
-                double S = 0.0;
-                if (sum.c > -CUDART_INF_F) {
-                    const float f = base.at() == M ? 1.f : rebase(base, common);
-                    S = (static_cast<double>(sum.hi) + static_cast<double>(sum.lo)) * static_cast<double>(f);
+                const float f = sum.c > -CUDART_INF_F ? rebase(base, common) : 0.f;  // a power of two but for wide bases
+                float hi = sum.hi * f, lo = sum.lo * f;
+                for (int o = 1; o < a.shares; o <<= 1) {
+                    const float h = __shfl_xor_sync(0xffffffffu, hi, o), l = __shfl_xor_sync(0xffffffffu, lo, o);
+                    two_sum(hi, lo, h);
+                    lo += l;
                 }
-                for (int o = 1; o < a.shares; o <<= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
                 if (lane == 0) {
-                    mass[w] = S;
+                    mass[w] = make_float2(hi, lo);
+                    if (logs_here) rest[w] = static_cast<double>(score) - log_of(static_cast<double>(hi) + static_cast<double>(lo));
                     offset[w] = common.wide ? static_cast<double>(common.c) : static_cast<double>(common.c) * (1.0 / static_cast<double>(kLog2e));
                 }
+            }
+            for (int s = p; s < a.shares; s += parts) {
+                const u64 v = ahead;
+                ahead = s + parts < a.shares && lane < K ? list[static_cast<int64_t>(s + parts) * K + lane] : 0;
+                top = s == p ? v : merge_desc(top, v);
             }
         }
         if (parts > 1) {
@@ -779,22 +789,26 @@ __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const Finis
         }
     }
     __syncthreads();
-    if (warp == kFinishWarps - 1 && lane < W)
-        rest[lane] = state[lane] == 1 && mass[lane] > 0.0 ? static_cast<double>(my_score) - log_of(mass[lane]) : static_cast<double>(my_score);
-    __syncthreads();
+    if (!logs_here) {
+        if (warp == kFinishWarps - 1 && lane < W)
+            rest[lane] = static_cast<double>(my_score) - log_of(static_cast<double>(mass[lane].x) + static_cast<double>(mass[lane].y));
+        __syncthreads();
+    }
     for (int w = warp; w < W; w += kFinishWarps) {
-        double s = rest[w];
-        bool some = false;
+        u64 c = 0, key = 0;
         if (state[w] == 2) {
-            some = lane == 0;
-            if (some) cand[w][0] = candidate(0.f, a.eos);
-        } else if (state[w] == 1) {
-            const u64 c = lane < K ? cand[w][lane] : 0;
-            some = c != 0;
-            s += static_cast<double>(candidate_logit(c)) - offset[w];  // exact near the offset, and not lost beside a huge one
+            c = lane == 0 ? candidate(0.f, a.eos) : 0;
+            if (lane == 0) cand[w][0] = c;
+        } else if (state[w] == 1 && lane < K) {
+            c = cand[w][lane];
         }
-        total[w][lane] = s;
-        keys[w][lane] = some ? double_key(a.alpha == 0.0 ? s : s * scale[w]) : 0;
+        if (c) {
+            double s = score_of[w];
+            if (state[w] == 1) s = rest[w] + (static_cast<double>(candidate_logit(c)) - offset[w]);  // not lost beside a huge offset
+            total[w][lane] = s;
+            key = double_key(a.alpha == 0.0 ? s : s * scale[w]);
+        }
+        keys[w][lane] = key;
         tags[w][lane] = w * kListLen + lane;
     }
     __syncthreads();
