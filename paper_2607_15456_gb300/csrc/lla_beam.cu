@@ -42,7 +42,7 @@ constexpr int kTileWords = kScanThreads * kWords;     // 16 KB a tile
 constexpr int kStages = 2;                            // tiles in shared memory
 constexpr int kScanCtas = 4;                          // of an SM
 constexpr int kFew = 4;                               // threads over K that may bring candidates of a tile
-constexpr int kCap = 2176;                            // candidates that a CTA holds
+constexpr int kCap = (2 * LLA_MAX_BEAMS - 1 + kFew) * kWords * 8 + LLA_MAX_BEAMS;                            // candidates that a CTA holds
 constexpr int kMaxShares = 32;                        // shares of a row: a warp merges them
 constexpr int kListLen = LLA_MAX_BEAMS;               // a list is a warp's lanes
 constexpr float kRise = 60.f;                         // a logit this far over the base's moves it (e^60 2^24 is finite)
@@ -249,14 +249,21 @@ __device__ __forceinline__ float tile_max(const uint4 (&v)[kWords]) {
             const __nv_bfloat162 *p = reinterpret_cast<const __nv_bfloat162 *>(&v[j]);
             m[j] = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3]));
         }
-        const __nv_bfloat162 t = __hmax2(__hmax2(m[0], m[1]), __hmax2(m[2], m[3]));
-        return fmaxf(__low2float(t), __high2float(t));
+#pragma unroll
+        for (int n = kWords / 2; n > 0; n /= 2)
+#pragma unroll
+            for (int j = 0; j < n; ++j) m[j] = __hmax2(m[j], m[j + n]);
+        return fmaxf(__low2float(m[0]), __high2float(m[0]));
     } else {
         float m[kWords];
 #pragma unroll
         for (int j = 0; j < kWords; ++j)
             m[j] = fmaxf(fmaxf(logit<BF16>(v[j], 0), logit<BF16>(v[j], 1)), fmaxf(logit<BF16>(v[j], 2), logit<BF16>(v[j], 3)));
-        return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+        #pragma unroll
+        for (int n = kWords / 2; n > 0; n /= 2)
+#pragma unroll
+            for (int j = 0; j < n; ++j) m[j] = fmaxf(m[j], m[j + n]);
+        return m[0];
     }
 }
 

@@ -673,7 +673,8 @@ class Pool:
 
 
 class Pools:
-    """The pools that a page call copies in (every layer's, and its rotary planes), marshalled once."""
+    """The pools that a page call copies in (every layer's, and its rotary planes), marshalled once for all calls that
+    take it (a list of Pool is marshalled at each)."""
 
     def __init__(self, pools=()):
         self.pools = tuple(pools)
@@ -741,6 +742,7 @@ def lla_pages_extend(pages: Pages, pools: Pools, slot_mapping: torch.Tensor, wor
             pages, pools, slot_mapping, workspace, cu_new, skip, lens_before, free_blocks, _handle(stream))):
         return
     p = pages.c()
+    pools = pools if isinstance(pools, Pools) else Pools(pools)
     pools.check(pages)
     if skip is not None and skip.dtype == torch.bool:
         skip = skip.view(torch.uint8)
@@ -774,6 +776,7 @@ def lla_pages_compact(pages: Pages, pools: Pools, remap: torch.Tensor, live: tor
     if _done("lla_pages_compact", _native().pages_compact(pages, pools, remap, live, workspace, _handle(stream))):
         return
     p = pages.c()
+    pools = pools if isinstance(pools, Pools) else Pools(pools)
     pools.check(pages)
     _check("lla_pages_compact", library().lla_pages_compact(
         ctypes.byref(p), pools.address, pools.count, _typed(remap, torch.int32, "remap", (p.num_blocks,)),
@@ -848,6 +851,7 @@ def lla_beam_search(pages_a: Pages, pages_b: Pages, pools: Pools, V: int, step, 
     steps, B, W = parents.shape
     slabs = (steps + 1, B, W)
     a, b = pages_a.c(), pages_b.c()
+    pools = pools if isinstance(pools, Pools) else Pools(pools)
     pools.check(pages_a)
     pools.check(pages_b)
     base, nbytes = _scratch(workspace)

@@ -398,6 +398,8 @@ def test_bad_device_data_is_flagged_and_left_alone(lla):
 def test_wrong_tensors_are_refused(lla):
     x = Both(lla, shapes(lla, "heads"), 10, 2, 4)
     p, slots = x.sets[0], torch.zeros(4, dtype=torch.int64, device=DEV)
+    lla.lla_pages_extend(p, list(x.t_pools), slots, x.ws, skip=torch.ones(4, dtype=torch.bool, device=DEV))  # a list, a bool mask
+    assert slots.tolist() == [-1] * 4
     with pytest.raises(ValueError, match="int64"):
         lla.lla_pages_extend(p, x.pools, slots.to(I32), x.ws)
     with pytest.raises(ValueError, match="shape"):
