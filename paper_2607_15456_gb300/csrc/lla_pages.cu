@@ -448,7 +448,8 @@ struct PoolSet {
     lla_pool p[LLA_MAX_POOLS];
     int first[LLA_MAX_POOLS + 1];
     uint16_t slices[LLA_MAX_POOLS];
-    int L;
+    int L, alike;     // alike: every pool has first[1] units
+    FastDiv by_pool;  // a division by first[1]
 };
 __host__ __device__ __forceinline__ int k_slices(const lla_pool &p) { return (kBlockTokens * p.k_row_bytes + kSliceBytes - 1) / kSliceBytes; }
 __host__ __device__ __forceinline__ int v_slices(const lla_pool &p) { return (kBlockTokens * p.v_row_bytes + kSliceBytes - 1) / kSliceBytes; }
@@ -499,7 +500,7 @@ extend_finish_kernel(const ExtendArgs a, const __grid_constant__ PoolSet ps, int
             in_copy -= per_copy;
             if (++c >= copies) break;
         }
-        const int l = pool_of(ps.first, ps.L, in_copy);
+        const int l = ps.alike ? div_by(in_copy, ps.by_pool) : pool_of(ps.first, ps.L, in_copy);
         const lla_pool pool = ps.p[l];
         const int slices = ps.slices[l], units = (slices + kCopyWarps - 1) / kCopyWarps, in_pool = in_copy - ps.first[l];
         int page, slice;
@@ -776,6 +777,9 @@ lla_status launch_pages_extend(const lla_pages &p, const lla_pool *pools, int L,
                                               : pools[l].pages * ((slices + kCopyWarps - 1) / kCopyWarps);
         ps.first[l + 1] = ps.first[l] + units;
     }
+    ps.alike = 1;
+    for (int l = 1; l < L; ++l) ps.alike &= ps.first[l + 1] - ps.first[l] == ps.first[1];
+    ps.by_pool = fast_div(static_cast<uint32_t>(L > 0 ? ps.first[1] : 1));
     if ((st = launch_plan(extend_plan_kernel, plan_ctas(p.num_blocks), a, stream)) != LLA_OK) return st;
     const int sms = num_sms();
     if (sms <= 0) return LLA_ERR_CUDA;
