@@ -845,7 +845,7 @@ def lla_beam_search(pages_a: Pages, pages_b: Pages, pools: Pools, V: int, step, 
     """Beam search over parents.shape[0] steps: tokens, scores, finished, lengths [steps + 1][B][W] (slab 0 filled
     by the caller), parents [steps][B][W].  step(i, pages, lens_before, tokens, slots) runs the model for step i
     and returns its logits [B][W][V] of `dtype` (kept alive until the call returns): pages is pages_a or pages_b,
-    lens_before [B W] int32, tokens [B][W] int32, slots [B W] int64."""
+    lens_before [B W] int32, tokens [B][W] int32, slots [B W] int64.  It runs with `stream` as the current one."""
     if parents.dim() != 3:
         raise ValueError("parents are [steps][B][W]")
     steps, B, W = parents.shape
@@ -879,13 +879,15 @@ def lla_beam_search(pages_a: Pages, pages_b: Pages, pools: Pools, V: int, step, 
     if dtype not in (torch.bfloat16, torch.float32):
         raise ValueError(f"unsupported dtype {dtype}")
     cb = STEP_FN(_step)
-    st = library().lla_beam_search(
-        ctypes.byref(a), ctypes.byref(b), pools.address, pools.count, B, W, V,
-        LLA_BF16 if dtype == torch.bfloat16 else LLA_F32, steps, eos, length_penalty,
-        _typed(tokens, torch.int32, "tokens", slabs), _typed(scores, torch.float32, "scores", slabs),
-        _typed(finished, torch.uint8, "finished", slabs), _typed(lengths, torch.int32, "lengths", slabs),
-        _typed(parents, torch.int32, "parents"), cb, None, base,
-        nbytes, _stream(stream))
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream)
+    with torch.cuda.stream(stream):  # None: the current one
+        st = library().lla_beam_search(
+            ctypes.byref(a), ctypes.byref(b), pools.address, pools.count, B, W, V,
+            LLA_BF16 if dtype == torch.bfloat16 else LLA_F32, steps, eos, length_penalty,
+            _typed(tokens, torch.int32, "tokens", slabs), _typed(scores, torch.float32, "scores", slabs),
+            _typed(finished, torch.uint8, "finished", slabs), _typed(lengths, torch.int32, "lengths", slabs),
+            _typed(parents, torch.int32, "parents"), cb, None, base, nbytes, _stream(None))
     if errors:
         raise errors[0]
     _check("lla_beam_search", st)

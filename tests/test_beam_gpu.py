@@ -477,6 +477,37 @@ def history_before(prompts, tk, pr, fn, step, s, W):
     return prompts[s // W] + got[::-1]
 
 
+@pytest.mark.parametrize("which", ["stream", "handle"])
+def test_search_on_another_stream(lla, which):
+    """The callback runs with the search's stream as the current one: the same hypotheses as on the default stream."""
+    B, W, V, steps = 2, 3, 400, 12
+    table = torch.randn(V, V, generator=torch.Generator(device=DEV).manual_seed(3), device=DEV) * 3
+    results = []
+    for stream in (None, torch.cuda.Stream()):
+        ref = torch.zeros(40, dtype=I32, device=DEV)
+        pages = [lla.Pages(ref, torch.zeros(B * W, 4, dtype=I32, device=DEV), torch.zeros(B * W, dtype=I32, device=DEV)) for _ in range(2)]
+        tokens, lengths = (torch.zeros(steps + 1, B, W, dtype=I32, device=DEV) for _ in range(2))
+        finished, parents = torch.zeros(steps + 1, B, W, dtype=U8, device=DEV), torch.zeros(steps, B, W, dtype=I32, device=DEV)
+        score = torch.full((steps + 1, B, W), -math.inf, device=DEV)
+        score[0, :, 0] = 0
+        tokens[0, 1] = 7
+        ws = torch.empty(lla.lla_beam_search_workspace_size(B, W, V, F32), dtype=U8, device=DEV)
+        streams = []
+
+        def step(i, pages, before, toks, slots):
+            streams.append(torch.cuda.current_stream().cuda_stream)
+            return table[toks.long()]
+
+        torch.cuda.synchronize()
+        lla.lla_beam_search(*pages, lla.Pools(), V, step, tokens, score, finished, lengths, parents, ws, dtype=F32, eos=5, length_penalty=0.3,
+                            stream=stream.cuda_stream if stream is not None and which == "handle" else stream)
+        torch.cuda.synchronize()
+        assert set(streams) == {(stream or torch.cuda.current_stream()).cuda_stream}
+        results.append([t.clone() for t in (tokens, parents, score, finished, lengths, ref, pages[0].context_lens)])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    assert lla.lla_get_device_error() == 0
+
+
 def test_search_stops_with_the_callback(lla):
     m = Model(lla, 3, -1)
     pages = [lla.Pages(torch.zeros(8, dtype=I32, device=DEV), torch.zeros(2, 2, dtype=I32, device=DEV), torch.zeros(2, dtype=I32, device=DEV)) for _ in range(2)]
