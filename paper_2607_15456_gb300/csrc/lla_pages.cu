@@ -558,7 +558,9 @@ extend_finish_kernel(const ExtendArgs a, const __grid_constant__ PoolSet ps, int
         if (off_a >= 0) *reinterpret_cast<uint32_t *>(dst + off_a) = rest_a;
         if (off_b >= 0) *reinterpret_cast<uint32_t *>(dst + off_b) = rest_b;
     }
-    for (int i = blockIdx.x * kCopyThreads + threadIdx.x; i < a.N; i += stride * kCopyThreads) {
+    // (64 bits: the last step over N near 2^31 passes it by a grid of threads)
+    for (int64_t at = static_cast<int64_t>(blockIdx.x) * kCopyThreads + threadIdx.x; at < a.N; at += static_cast<int64_t>(stride) * kCopyThreads) {
+        const int i = static_cast<int>(at);
         int s, j;
         if (a.cu_new) {
             int lo = 0, hi = a.S - 1;
@@ -784,7 +786,7 @@ lla_status launch_pages_extend(const lla_pages &p, const lla_pool *pools, int L,
     const int sms = num_sms();
     if (sms <= 0) return LLA_ERR_CUDA;
     // every CTA resident at once; no more than there can be work for
-    const int64_t work = static_cast<int64_t>(p.S) * ps.first[L] + (N + kCopyThreads - 1) / kCopyThreads;
+    const int64_t work = static_cast<int64_t>(p.S) * ps.first[L] + (static_cast<int64_t>(N) + kCopyThreads - 1) / kCopyThreads;
     return launch_ex(extend_finish_kernel, dim3(static_cast<unsigned>(work < sms * kCopyCtas ? (work > 0 ? work : 1) : sms * kCopyCtas)),
                      kCopyThreads, 0, stream, a, ps, slots);
 }
