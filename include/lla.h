@@ -586,7 +586,9 @@ lla_status lla_pages_compact_workspace_size(int64_t num_blocks, size_t *bytes);
  * whole, in every pool), and the tables of `pages` and ref_count follow.
  *   pages  holds every table of the ledger; a table that it does not hold is renamed with `remap`
  *   remap  device [num_blocks] int32, written: the new number of every block, -1 for a free one
- *   live   device int32, written: R.  Neither may lie in ref_count or a table (LLA_ERR_INVALID_ARG)
+ *   live   device int32, written: R
+ * Neither of the two may lie in the other, nor in ref_count, the table or the lengths of `pages` or the workspace
+ * (LLA_ERR_INVALID_ARG).
  * Two kernels on the stream; the workspace as for lla_pages_extend.
  */
 lla_status lla_pages_compact(const lla_pages *pages, const lla_pool *pools, int32_t L, int32_t *remap,

@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <initializer_list>
 
 #include "lla_internal.h"
 
@@ -616,7 +617,26 @@ bool overlap(const void *a, size_t na, const void *b, size_t nb) {
     return na > 0 && nb > 0 && x < y + nb && y < x + na;
 }
 
+struct Span {
+    const void *p;
+    size_t bytes;
+};
+// Whether one of `written` overlaps another of them or one of `read` (absent arrays overlap nothing).
+bool any_overlap(std::initializer_list<Span> written, std::initializer_list<Span> read) {
+    for (const Span *o = written.begin(); o != written.end(); ++o) {
+        if (!o->p) continue;
+        for (const Span *i = o + 1; i != written.end(); ++i)
+            if (i->p && overlap(o->p, o->bytes, i->p, i->bytes)) return true;
+        for (const Span &i : read)
+            if (i.p && overlap(o->p, o->bytes, i.p, i.bytes)) return true;
+    }
+    return false;
+}
+
 size_t table_bytes(const lla_pages *p) { return static_cast<size_t>(p->S) * p->max_blocks_per_seq * 4; }
+Span ledger_of(const lla_pages *p) { return Span{p->ref_count, static_cast<size_t>(p->num_blocks) * 4}; }
+Span table_of(const lla_pages *p) { return Span{p->block_table, table_bytes(p)}; }
+Span lens_of(const lla_pages *p) { return Span{p->context_lens, static_cast<size_t>(p->S) * 4}; }
 
 lla_status pool_of_geometry(const lla_geometry *g, int max_rank, int pages, void *pool, lla_pool *out) {
     const lla_status st = check_geometry(g, max_rank);
@@ -715,11 +735,11 @@ lla_status lla_pages_compact(const lla_pages *pages, const lla_pool *pools, int3
     if (st != LLA_OK) return st;
     if ((st = check_pools(pools, L)) != LLA_OK) return st;
     if (!remap || !live || !workspace || !aligned(workspace, 16)) return LLA_ERR_INVALID_ARG;
-    const size_t ledger = static_cast<size_t>(pages->num_blocks) * 4;
-    if (overlap(remap, ledger, pages->ref_count, ledger) || overlap(remap, ledger, pages->block_table, table_bytes(pages)) ||
-        overlap(live, 4, pages->ref_count, ledger) || overlap(live, 4, remap, ledger))
-        return LLA_ERR_INVALID_ARG;
-    if (workspace_bytes < pages_compact_workspace_bytes(pages->num_blocks)) return LLA_ERR_WORKSPACE;
+    const size_t need = pages_compact_workspace_bytes(pages->num_blocks);
+    const Span ledger = ledger_of(pages), table = table_of(pages), lens = lens_of(pages);
+    if (any_overlap({{remap, ledger.bytes}, {live, 4}}, {ledger, table, lens})) return LLA_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return LLA_ERR_WORKSPACE;
+    if (any_overlap({{workspace, need}}, {{remap, ledger.bytes}, {live, 4}, ledger, table, lens})) return LLA_ERR_INVALID_ARG;
     return launch_pages_compact(*pages, pools, L, remap, live, workspace, static_cast<cudaStream_t>(stream));
 }
 
