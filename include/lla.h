@@ -496,7 +496,9 @@ lla_status lla_dense_decode_attn(const lla_geometry *g, const lla_cache *cache,
  * (parallel samples, beam search, shared prompts) needs around the calls above.
  *
  * With every count and length zero (cudaMemset) all blocks are free and all sequences empty.  Calls on one
- * ledger, and calls that read its pages, must be ordered (one stream).
+ * ledger, and calls that read its pages, must be ordered (one stream).  The arrays of a call must not overlap
+ * where one of them is written: the page sets' arrays, each other, the outputs, the workspace (as much of it as the
+ * call needs) and the inputs (LLA_ERR_INVALID_ARG; the pools are not compared).
  */
 #define LLA_MAX_BLOCKS (1 << 24)
 #define LLA_MAX_POOLS 128
@@ -533,7 +535,7 @@ lla_status lla_rope_pool(int32_t d_rope, void *rope_pool, lla_pool *out);
  * reordering of states after lla_beam_select, the parallel samples of a prompt, and the removal of
  * ended sequences from a batch, in one call.
  *   from, to   two views of the same ref_count and num_blocks, with different block_table and
- *              context_lens arrays (LLA_ERR_INVALID_ARG where they overlap); `from` holds nothing
+ *              context_lens arrays; `from` holds nothing
  *              after the call, although its arrays are left as they are: its next use is as a `to`
  *   parents    device [to->S] int32; one outside [-1, from->S) sets LLA_DEVERR_SEQUENCE and counts as -1
  * A parent of more pages than to->max_blocks_per_seq sets LLA_DEVERR_CONTEXT, and its children are empty.
@@ -587,8 +589,6 @@ lla_status lla_pages_compact_workspace_size(int64_t num_blocks, size_t *bytes);
  *   pages  holds every table of the ledger; a table that it does not hold is renamed with `remap`
  *   remap  device [num_blocks] int32, written: the new number of every block, -1 for a free one
  *   live   device int32, written: R
- * Neither of the two may lie in the other, nor in ref_count, the table or the lengths of `pages` or the workspace
- * (LLA_ERR_INVALID_ARG).
  * Two kernels on the stream; the workspace as for lla_pages_extend.
  */
 lla_status lla_pages_compact(const lla_pages *pages, const lla_pool *pools, int32_t L, int32_t *remap,

@@ -592,26 +592,6 @@ lla_status lla_prefill_attn_rope(const lla_geometry *g, const lla_codec *codec,
 
 namespace {
 
-lla_status check_pages(const lla_pages *p) {
-    if (!p || p->num_blocks < 1 || p->max_blocks_per_seq < 1 || p->S < 0 || p->S > LLA_MAX_BATCH) return LLA_ERR_INVALID_ARG;
-    if (p->num_blocks > LLA_MAX_BLOCKS || p->max_blocks_per_seq > LLA_MAX_BLOCKS) return LLA_ERR_UNSUPPORTED;
-    if (!p->ref_count || !aligned(p->ref_count, 16)) return LLA_ERR_INVALID_ARG;
-    if (p->S > 0 && (!p->block_table || !p->context_lens)) return LLA_ERR_INVALID_ARG;
-    return LLA_OK;
-}
-
-lla_status check_pools(const lla_pool *pools, int32_t L) {
-    if (L < 0 || (L > 0 && !pools)) return LLA_ERR_INVALID_ARG;
-    if (L > LLA_MAX_POOLS) return LLA_ERR_UNSUPPORTED;
-    for (int32_t l = 0; l < L; ++l) {
-        const lla_pool &p = pools[l];
-        if (!p.base || !aligned(p.base, 16) || p.pages < 1 || p.pages > 4096) return LLA_ERR_INVALID_ARG;
-        if (p.k_row_bytes < 4 || p.k_row_bytes > 8192 || p.k_row_bytes % 4 != 0) return LLA_ERR_INVALID_ARG;
-        if (p.v_row_bytes < 0 || p.v_row_bytes > 8192 || p.v_row_bytes % 4 != 0) return LLA_ERR_INVALID_ARG;
-    }
-    return LLA_OK;
-}
-
 bool overlap(const void *a, size_t na, const void *b, size_t nb) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return na > 0 && nb > 0 && x < y + nb && y < x + na;
@@ -638,6 +618,26 @@ Span ledger_of(const lla_pages *p) { return Span{p->ref_count, static_cast<size_
 Span table_of(const lla_pages *p) { return Span{p->block_table, table_bytes(p)}; }
 Span lens_of(const lla_pages *p) { return Span{p->context_lens, static_cast<size_t>(p->S) * 4}; }
 
+lla_status check_pages(const lla_pages *p) {
+    if (!p || p->num_blocks < 1 || p->max_blocks_per_seq < 1 || p->S < 0 || p->S > LLA_MAX_BATCH) return LLA_ERR_INVALID_ARG;
+    if (p->num_blocks > LLA_MAX_BLOCKS || p->max_blocks_per_seq > LLA_MAX_BLOCKS) return LLA_ERR_UNSUPPORTED;
+    if (!p->ref_count || !aligned(p->ref_count, 16)) return LLA_ERR_INVALID_ARG;
+    if (p->S > 0 && (!p->block_table || !p->context_lens)) return LLA_ERR_INVALID_ARG;
+    return any_overlap({ledger_of(p), table_of(p), lens_of(p)}, {}) ? LLA_ERR_INVALID_ARG : LLA_OK;
+}
+
+lla_status check_pools(const lla_pool *pools, int32_t L) {
+    if (L < 0 || (L > 0 && !pools)) return LLA_ERR_INVALID_ARG;
+    if (L > LLA_MAX_POOLS) return LLA_ERR_UNSUPPORTED;
+    for (int32_t l = 0; l < L; ++l) {
+        const lla_pool &p = pools[l];
+        if (!p.base || !aligned(p.base, 16) || p.pages < 1 || p.pages > 4096) return LLA_ERR_INVALID_ARG;
+        if (p.k_row_bytes < 4 || p.k_row_bytes > 8192 || p.k_row_bytes % 4 != 0) return LLA_ERR_INVALID_ARG;
+        if (p.v_row_bytes < 0 || p.v_row_bytes > 8192 || p.v_row_bytes % 4 != 0) return LLA_ERR_INVALID_ARG;
+    }
+    return LLA_OK;
+}
+
 lla_status pool_of_geometry(const lla_geometry *g, int max_rank, int pages, void *pool, lla_pool *out) {
     const lla_status st = check_geometry(g, max_rank);
     if (st != LLA_OK) return st;
@@ -654,9 +654,7 @@ extern "C++" lla_status lla::check_fork(const lla_pages *from, const lla_pages *
     if (st != LLA_OK) return st;
     if ((st = check_pages(to)) != LLA_OK) return st;
     if (from->ref_count != to->ref_count || from->num_blocks != to->num_blocks) return LLA_ERR_INVALID_ARG;
-    if (overlap(from->block_table, table_bytes(from), to->block_table, table_bytes(to)) ||
-        overlap(from->context_lens, static_cast<size_t>(from->S) * 4, to->context_lens, static_cast<size_t>(to->S) * 4))
-        return LLA_ERR_INVALID_ARG;
+    if (any_overlap({table_of(to), lens_of(to)}, {table_of(from), lens_of(from)})) return LLA_ERR_INVALID_ARG;
     return LLA_OK;
 }
 
@@ -681,9 +679,7 @@ lla_status lla_pages_fork(const lla_pages *from, const lla_pages *to, const int3
     const lla_status st = check_fork(from, to);
     if (st != LLA_OK) return st;
     if (to->S > 0 && !parents) return LLA_ERR_INVALID_ARG;
-    if (overlap(parents, static_cast<size_t>(to->S) * 4, to->block_table, table_bytes(to)) ||
-        overlap(parents, static_cast<size_t>(to->S) * 4, to->context_lens, static_cast<size_t>(to->S) * 4))
-        return LLA_ERR_INVALID_ARG;
+    if (any_overlap({ledger_of(to), table_of(to), lens_of(to)}, {{parents, static_cast<size_t>(to->S) * 4}})) return LLA_ERR_INVALID_ARG;
     if (from->S + to->S == 0) return LLA_OK;
     return launch_pages_fork(*from, *to, parents, static_cast<cudaStream_t>(stream));
 }
@@ -702,14 +698,21 @@ lla_status lla_pages_extend(const lla_pages *pages, const lla_pool *pools, int32
     if ((st = check_pools(pools, L)) != LLA_OK) return st;
     if (N < 0 || (N > 0 && !slot_mapping)) return LLA_ERR_INVALID_ARG;
     if (!cu_new && (pages->S == 0 ? N != 0 : N % pages->S != 0)) return LLA_ERR_INVALID_ARG;
-    // with no sequence there is no token, and cu_new is one zero: every slot of a padded mapping is a token to skip
-    if (pages->S == 0) {
-        if (N > 0 && cudaMemsetAsync(slot_mapping, 0xff, static_cast<size_t>(N) * 8, static_cast<cudaStream_t>(stream)) != cudaSuccess)
-            return LLA_ERR_CUDA;
-        if (!free_blocks) return LLA_OK;
+    const size_t need = pages_extend_workspace_bytes(), each = static_cast<size_t>(pages->S) * 4;
+    const bool launch = pages->S > 0 || free_blocks;
+    if (launch) {
+        if (!workspace || !aligned(workspace, 16)) return LLA_ERR_INVALID_ARG;
+        if (workspace_bytes < need) return LLA_ERR_WORKSPACE;
     }
-    if (!workspace || !aligned(workspace, 16)) return LLA_ERR_INVALID_ARG;
-    if (workspace_bytes < pages_extend_workspace_bytes()) return LLA_ERR_WORKSPACE;
+    if (any_overlap({{slot_mapping, static_cast<size_t>(N) * 8}, {lens_before, each}, {free_blocks, 4}, {launch ? workspace : nullptr, need},
+                     ledger_of(pages), table_of(pages), lens_of(pages)},
+                    {{cu_new, each + 4}, {skip, static_cast<size_t>(pages->S)}}))
+        return LLA_ERR_INVALID_ARG;
+    // with no sequence there is no token, and cu_new is one zero: every slot of a padded mapping is a token to skip
+    if (pages->S == 0 && N > 0 &&
+        cudaMemsetAsync(slot_mapping, 0xff, static_cast<size_t>(N) * 8, static_cast<cudaStream_t>(stream)) != cudaSuccess)
+        return LLA_ERR_CUDA;
+    if (!launch) return LLA_OK;
     return launch_pages_extend(*pages, pools, L, slot_mapping, pages->S == 0 ? 0 : N, cu_new, skip, lens_before, free_blocks,
                                workspace, static_cast<cudaStream_t>(stream));
 }
@@ -719,6 +722,7 @@ lla_status lla_pages_free(const lla_pages *pages, const int32_t *seqs, int32_t n
     if (st != LLA_OK) return st;
     if (n < 0 || n > LLA_MAX_BATCH || (n > 0 && !seqs)) return LLA_ERR_INVALID_ARG;
     if (n == 0) return LLA_OK;
+    if (any_overlap({ledger_of(pages), table_of(pages), lens_of(pages)}, {{seqs, static_cast<size_t>(n) * 4}})) return LLA_ERR_INVALID_ARG;
     return launch_pages_free(*pages, seqs, n, static_cast<cudaStream_t>(stream));
 }
 

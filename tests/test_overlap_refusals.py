@@ -58,3 +58,59 @@ def test_compact(lla):
             assert compact(ws=bad) == INVALID, hex(bad)
     for bad in over(remap, 400, 4):
         assert compact(live=bad) == INVALID
+
+
+def test_a_page_set_s_own_arrays(lla):
+    so, seqs = lla.library(), FAKE + 0x40000
+    free = lambda **kw: so.lla_pages_free(ctypes.byref(pages(lla, **kw)), seqs, 2, None)
+    for bad in over(TABLE, TABLE_BYTES, REF_BYTES, 16):
+        assert free(ref_count=bad) == INVALID, hex(bad)
+    for at, size in ARRAYS[:2]:
+        for bad in over(at, size, LENS_BYTES):
+            assert free(context_lens=bad) == INVALID, hex(bad)
+
+
+def test_free(lla):
+    so = lla.library()
+    for at, size in ARRAYS:
+        for bad in over(at, size, 8):
+            assert so.lla_pages_free(ctypes.byref(pages(lla)), bad, 2, None) == INVALID, hex(bad)
+
+
+def test_fork(lla):
+    so = lla.library()
+    table, lens, parents = FAKE + 0x40000, FAKE + 0x50000, FAKE + 0x60000
+
+    def fork(parents=parents, **kw):
+        to = pages(lla, **{**dict(block_table=table, context_lens=lens), **kw})
+        return so.lla_pages_fork(ctypes.byref(pages(lla)), ctypes.byref(to), parents, None)
+
+    for at, size in ARRAYS:  # what `from` and the ledger have
+        for bad in over(at, size, TABLE_BYTES):
+            assert fork(block_table=bad) == INVALID, hex(bad)
+        for bad in over(at, size, LENS_BYTES):
+            assert fork(context_lens=bad) == INVALID, hex(bad)
+    for at, size in ((REF, REF_BYTES), (table, TABLE_BYTES), (lens, LENS_BYTES)):  # what is written
+        for bad in over(at, size, 16):
+            assert fork(parents=bad) == INVALID, hex(bad)
+
+
+def test_extend(lla):
+    so, need = lla.library(), ctypes.c_size_t()
+    assert so.lla_pages_extend_workspace_size(4, ctypes.byref(need)) == OK
+    names = ["slots", "cu", "skip", "before", "free", "ws"]
+    place = {n: FAKE + 0x40000 + i * 0x10000 for i, n in enumerate(names)}
+    size = dict(slots=24 * 8, cu=5 * 4, skip=4, before=16, free=4, ws=need.value)
+    align = dict(slots=8, cu=4, skip=1, before=4, free=4, ws=16)
+
+    def extend(**kw):
+        a = {**place, **kw}
+        return so.lla_pages_extend(ctypes.byref(pages(lla)), None, 0, a["slots"], 24, a["cu"], a["skip"], a["before"], a["free"], a["ws"], need.value, None)
+
+    for n in names:
+        for at, bytes_ in ARRAYS + [(place[m], size[m]) for m in names if m != n and {n, m} != {"cu", "skip"}]:
+            for bad in over(at, bytes_, size[n], align[n]):
+                assert extend(**{n: bad}) == INVALID, (n, hex(bad))
+    for at, bytes_ in ARRAYS[:1] + [(place["cu"], 4)]:  # no sequence: the slots are still written
+        for bad in over(at, bytes_, size["slots"], 8):
+            assert so.lla_pages_extend(ctypes.byref(pages(lla, S=0)), None, 0, bad, 24, place["cu"], None, None, None, None, 0, None) == INVALID
