@@ -623,8 +623,8 @@ lla_status lla_beam_select_workspace_size(int32_t B, int32_t W, int32_t V, int32
  *   out_scores    device [B][K] fp32, written: s, rounded once (-inf where parents is -1)
  *   out_finished  device [B][K] uint8 or NULL, written: 1 where the token is eos or parents is -1, else 0
  *   out_lengths   device [B][K] int32 or NULL, written (0 where parents is -1)
- * W, K <= LLA_MAX_BEAMS, B W <= LLA_MAX_BATCH, V <= LLA_MAX_VOCAB.  No output may overlap an input
- * (LLA_ERR_INVALID_ARG among scores, flags and lengths).  Two
+ * W, K <= LLA_MAX_BEAMS, B W <= LLA_MAX_BATCH, V <= LLA_MAX_VOCAB.  Outputs and workspace may overlap neither each
+ * other nor an input (LLA_ERR_INVALID_ARG; the logits are not compared).  Two
  * kernels on the stream; the workspace as for lla_pages_extend.
  */
 lla_status lla_beam_select(int32_t B, int32_t W, int32_t V, int32_t K, const void *logits,

@@ -779,14 +779,14 @@ lla_status lla_beam_select(int32_t B, int32_t W, int32_t V, int32_t K, const voi
     if (B == 0) return LLA_OK;
     if (!logits || !aligned(logits, elem_size(logits_dtype)) || !scores || !parents || !tokens || !out_scores)
         return LLA_ERR_INVALID_ARG;
-    const size_t in = static_cast<size_t>(B) * W * 4, out = static_cast<size_t>(B) * K * 4;
-    const void *const ins[] = {scores, lengths}, *const outs[] = {parents, tokens, out_scores, out_lengths};
-    for (const void *o : outs)
-        for (const void *i : ins)
-            if (o && i && overlap(o, out, i, in)) return LLA_ERR_INVALID_ARG;
-    if (finished && out_finished && overlap(finished, in / 4, out_finished, out / 4)) return LLA_ERR_INVALID_ARG;
+    const size_t in = static_cast<size_t>(B) * W, out = static_cast<size_t>(B) * K;
+    const size_t need = beam_select_workspace_bytes(B, W, V, K, logits_dtype == LLA_BF16);
+    const Span r0 = {scores, in * 4}, r1 = {finished, in}, r2 = {lengths, in * 4};
+    const Span w0 = {parents, out * 4}, w1 = {tokens, out * 4}, w2 = {out_scores, out * 4}, w3 = {out_finished, out}, w4 = {out_lengths, out * 4};
+    if (any_overlap({w0, w1, w2, w3, w4}, {r0, r1, r2})) return LLA_ERR_INVALID_ARG;
     if (!workspace || !aligned(workspace, 16)) return LLA_ERR_INVALID_ARG;
-    if (workspace_bytes < beam_select_workspace_bytes(B, W, V, K, logits_dtype == LLA_BF16)) return LLA_ERR_WORKSPACE;
+    if (workspace_bytes < need) return LLA_ERR_WORKSPACE;
+    if (any_overlap({{workspace, need}}, {r0, r1, r2, w0, w1, w2, w3, w4})) return LLA_ERR_INVALID_ARG;
     BeamSelectArgs a = {};
     a.B = B; a.W = W; a.V = V; a.K = K; a.bf16 = logits_dtype == LLA_BF16;
     a.logits = logits; a.row_stride = row_stride;

@@ -114,3 +114,28 @@ def test_extend(lla):
     for at, bytes_ in ARRAYS[:1] + [(place["cu"], 4)]:  # no sequence: the slots are still written
         for bad in over(at, bytes_, size["slots"], 8):
             assert so.lla_pages_extend(ctypes.byref(pages(lla, S=0)), None, 0, bad, 24, place["cu"], None, None, None, None, 0, None) == INVALID
+
+
+def test_select(lla):
+    so, need = lla.library(), ctypes.c_size_t()
+    B, W, V, K = 2, 4, 100, 8
+    assert so.lla_beam_select_workspace_size(B, W, V, K, 0, ctypes.byref(need)) == OK
+    ins = dict(s=4 * B * W, fin=B * W, n=4 * B * W)
+    outs = dict(parents=4 * B * K, tokens=4 * B * K, scores=4 * B * K, ended=B * K, lens=4 * B * K, ws=need.value)
+    size = {**ins, **outs}
+    place = {n: FAKE + 0x40000 + i * 0x10000 for i, n in enumerate(size)}
+    align = {n: 1 if n in ("fin", "ended") else 16 if n == "ws" else 4 for n in size}
+
+    def select(ws_bytes=need.value, **kw):
+        a = {**place, **kw}
+        return so.lla_beam_select(B, W, V, K, FAKE, V, 0, a["s"], a["fin"], a["n"], -1, 0.0, a["parents"], a["tokens"], a["scores"], a["ended"], a["lens"],
+                                  a["ws"], ws_bytes, None)
+
+    for n in outs:
+        for m in size:
+            if m != n:
+                for bad in over(place[m], size[m], size[n], align[n]):
+                    assert select(**{n: bad}) == INVALID, (n, m, hex(bad))
+    # beside each other is no overlap: the next check is the workspace's size
+    beside = dict(parents=place["s"] + size["s"], tokens=place["s"] - size["tokens"], ended=place["fin"] + size["fin"], lens=place["n"] - size["lens"])
+    assert select(ws_bytes=need.value - 1, **beside) == WORKSPACE
