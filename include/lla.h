@@ -664,8 +664,9 @@ lla_status lla_beam_search_workspace_size(int32_t B, int32_t W, int32_t V, lla_d
  *   parents           device [steps][B][W] int32, written: the beam of slab i that each of slab i + 1
  *                     continues; a hypothesis is read by walking back from its beam in the last slab
  *   pools, L          as lla_pages_extend
- * The error behaviour of each step is that of its call; the first non-OK status is returned (the work
- * enqueued before it stays enqueued).  The workspace as for lla_pages_extend.
+ * What would be wrong in every step (page sets, pools, eos, length_penalty, arrays that overlap) is refused before the
+ * first.  Beyond that the error behaviour of each step is that of its call; the first non-OK status is returned (the
+ * work enqueued before it stays enqueued).  The workspace as for lla_pages_extend.
  */
 lla_status lla_beam_search(const lla_pages *pages_a, const lla_pages *pages_b, const lla_pool *pools,
                            int32_t L, int32_t B, int32_t W, int32_t V, lla_dtype logits_dtype,

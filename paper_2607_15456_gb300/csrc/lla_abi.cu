@@ -638,6 +638,16 @@ lla_status check_pools(const lla_pool *pools, int32_t L) {
     return LLA_OK;
 }
 
+// Two page sets of one ledger whose arrays do not overlap.
+lla_status check_fork(const lla_pages *from, const lla_pages *to) {
+    lla_status st = check_pages(from);
+    if (st != LLA_OK) return st;
+    if ((st = check_pages(to)) != LLA_OK) return st;
+    if (from->ref_count != to->ref_count || from->num_blocks != to->num_blocks) return LLA_ERR_INVALID_ARG;
+    if (any_overlap({table_of(to), lens_of(to)}, {table_of(from), lens_of(from)})) return LLA_ERR_INVALID_ARG;
+    return LLA_OK;
+}
+
 lla_status pool_of_geometry(const lla_geometry *g, int max_rank, int pages, void *pool, lla_pool *out) {
     const lla_status st = check_geometry(g, max_rank);
     if (st != LLA_OK) return st;
@@ -647,16 +657,6 @@ lla_status pool_of_geometry(const lla_geometry *g, int max_rank, int pages, void
 }
 
 }  // namespace
-
-// Two page sets of one ledger whose arrays do not overlap (also what lla_beam_search asks of its two).
-extern "C++" lla_status lla::check_fork(const lla_pages *from, const lla_pages *to) {
-    lla_status st = check_pages(from);
-    if (st != LLA_OK) return st;
-    if ((st = check_pages(to)) != LLA_OK) return st;
-    if (from->ref_count != to->ref_count || from->num_blocks != to->num_blocks) return LLA_ERR_INVALID_ARG;
-    if (any_overlap({table_of(to), lens_of(to)}, {table_of(from), lens_of(from)})) return LLA_ERR_INVALID_ARG;
-    return LLA_OK;
-}
 
 lla_status lla_cache_pool(const lla_geometry *g, void *pool, lla_pool *out) {
     return pool_of_geometry(g, kMaxRank, g ? g->H : 0, pool, out);
@@ -756,7 +756,28 @@ lla_status check_beams(int32_t B, int32_t W, int32_t V, int32_t K, lla_dtype dty
     return LLA_OK;
 }
 
+bool valid_ranking(int32_t V, int32_t eos, float length_penalty) {
+    return eos >= -1 && eos < V && length_penalty >= -16.f && length_penalty <= 16.f;
+}
+
 }  // namespace
+
+// What every step of lla_beam_search would refuse, before the first.
+extern "C++" lla_status lla::check_search(const lla_pages *a, const lla_pages *b, const lla_pool *pools, int32_t L, int32_t V, int32_t eos,
+                                          float length_penalty) {
+    lla_status st = check_fork(a, b);
+    if (st != LLA_OK) return st;
+    if ((st = check_pools(pools, L)) != LLA_OK) return st;
+    return valid_ranking(V, eos, length_penalty) ? LLA_OK : LLA_ERR_INVALID_ARG;
+}
+extern "C++" bool lla::search_arrays_overlap(const lla_pages *a, const lla_pages *b, size_t n, size_t steps, const int32_t *tokens,
+                                             const float *scores, const uint8_t *finished, const int32_t *lengths, const int32_t *parents,
+                                             const void *workspace, size_t workspace_bytes) {
+    const size_t slabs = (steps + 1) * n;
+    return any_overlap({{tokens, slabs * 4}, {scores, slabs * 4}, {finished, slabs}, {lengths, slabs * 4}, {parents, steps * n * 4},
+                        {workspace, workspace_bytes}},
+                       {ledger_of(a), table_of(a), lens_of(a), table_of(b), lens_of(b)});
+}
 
 lla_status lla_beam_select_workspace_size(int32_t B, int32_t W, int32_t V, int32_t K, lla_dtype logits_dtype, size_t *bytes) {
     const lla_status st = check_beams(B, W, V, K, logits_dtype);
@@ -773,8 +794,7 @@ lla_status lla_beam_select(int32_t B, int32_t W, int32_t V, int32_t K, const voi
                            void *stream) {
     const lla_status st = check_beams(B, W, V, K, logits_dtype);
     if (st != LLA_OK) return st;
-    if (row_stride < V || row_stride > (int64_t(1) << 40) || eos < -1 || eos >= V) return LLA_ERR_INVALID_ARG;
-    if (!(length_penalty >= -16.f && length_penalty <= 16.f)) return LLA_ERR_INVALID_ARG;
+    if (row_stride < V || row_stride > (int64_t(1) << 40) || !valid_ranking(V, eos, length_penalty)) return LLA_ERR_INVALID_ARG;
     if (!lengths && (length_penalty != 0.f || out_lengths)) return LLA_ERR_INVALID_ARG;
     if (B == 0) return LLA_OK;
     if (!logits || !aligned(logits, elem_size(logits_dtype)) || !scores || !parents || !tokens || !out_scores)

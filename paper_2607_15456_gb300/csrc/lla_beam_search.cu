@@ -48,11 +48,14 @@ extern "C" lla_status lla_beam_search(const lla_pages *pages_a, const lla_pages 
     if (st != LLA_OK) return st;
     const int64_t n = static_cast<int64_t>(B) * W;
     if (!pages_a || !pages_b || pages_a->S != n || pages_b->S != n || steps < 0) return LLA_ERR_INVALID_ARG;
-    if ((st = lla::check_fork(pages_a, pages_b)) != LLA_OK) return st;
+    if ((st = lla::check_search(pages_a, pages_b, pools, L, V, eos, length_penalty)) != LLA_OK) return st;
     if (n == 0 || steps == 0) return LLA_OK;
     if (!step || !tokens || !scores || !finished || !lengths || !parents) return LLA_ERR_INVALID_ARG;
     if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return LLA_ERR_INVALID_ARG;
     if (workspace_bytes < l.total) return LLA_ERR_WORKSPACE;
+    if (lla::search_arrays_overlap(pages_a, pages_b, static_cast<size_t>(n), static_cast<size_t>(steps), tokens, scores, finished, lengths,
+                                   parents, workspace, l.total))
+        return LLA_ERR_INVALID_ARG;
     char *ws = static_cast<char *>(workspace);
     int64_t *slots = reinterpret_cast<int64_t *>(ws + l.slots);
     int32_t *before = reinterpret_cast<int32_t *>(ws + l.before);

@@ -140,7 +140,12 @@ lla_status launch_rope_key_store(int d_rope, double base, int pairing, void *rop
                                  const void *k, int x_bf16, const int32_t *positions, const int64_t *slots,
                                  int N, cudaStream_t stream);
 
-lla_status check_fork(const lla_pages *from, const lla_pages *to);  // (lla_abi.cu)
+// The checks of lla_beam_search (lla_abi.cu): what holds for every step, and its arrays beside those of its page sets.
+lla_status check_search(const lla_pages *a, const lla_pages *b, const lla_pool *pools, int32_t L, int32_t V, int32_t eos,
+                        float length_penalty);
+bool search_arrays_overlap(const lla_pages *a, const lla_pages *b, size_t n, size_t steps, const int32_t *tokens, const float *scores,
+                           const uint8_t *finished, const int32_t *lengths, const int32_t *parents, const void *workspace,
+                           size_t workspace_bytes);
 // Sequences that share pages (lla_pages.cu): launches behind the checks of lla_abi.cu (no empty batch).
 lla_status launch_pages_fork(const lla_pages &from, const lla_pages &to, const int32_t *parents, cudaStream_t stream);
 lla_status launch_pages_free(const lla_pages &p, const int32_t *seqs, int n, cudaStream_t stream);
