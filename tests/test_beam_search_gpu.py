@@ -1,0 +1,118 @@
+"""lla_beam_search: what the model's callback is given and what becomes of the search where a beam dies or pages run out."""
+import gc
+import math
+import weakref
+
+import pytest
+import torch
+
+from helpers import ensure_library
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+I32, I64, U8, F32 = torch.int32, torch.int64, torch.uint8, torch.float32
+
+
+@pytest.fixture(scope="module")
+def lla():
+    ensure_library()
+    from paper_2607_15456_gb300 import lla as m
+    return m
+
+
+@pytest.fixture(autouse=True)
+def no_error_left(lla):
+    lla.lla_clear_device_error()
+    yield
+    assert lla.lla_get_device_error() == 0
+
+
+class Search:
+    """Page sets, slabs and workspace of a search without pools."""
+
+    def __init__(self, lla, B, W, V, steps, blocks=64, max_blocks=4):
+        self.lla, self.B, self.W, self.V, self.steps = lla, B, W, V, steps
+        S = B * W
+        self.ref = torch.zeros(blocks, dtype=I32, device=DEV)
+        self.pages = [lla.Pages(self.ref, torch.full((S, max_blocks), -1, dtype=I32, device=DEV), torch.zeros(S, dtype=I32, device=DEV)) for _ in range(2)]
+        self.tokens, self.lengths = (torch.zeros(steps + 1, B, W, dtype=I32, device=DEV) for _ in range(2))
+        self.finished = torch.zeros(steps + 1, B, W, dtype=U8, device=DEV)
+        self.parents = torch.zeros(steps, B, W, dtype=I32, device=DEV)
+        self.scores = torch.full((steps + 1, B, W), -math.inf, device=DEV)
+        self.scores[0, :, 0] = 0
+        self.ws = torch.full((lla.lla_beam_search_workspace_size(B, W, V, F32),), 0xA5, dtype=U8, device=DEV)
+
+    def run(self, step, pools=None, **kw):
+        self.lla.lla_beam_search(*self.pages, pools or self.lla.Pools(), self.V, step, self.tokens, self.scores, self.finished, self.lengths, self.parents,
+                                 self.ws, dtype=F32, **kw)
+        return self
+
+    def prompt(self, lens):
+        """Every sequence's prompt of lens[b] cached tokens, forked into its beams."""
+        first = self.lla.Pages(self.ref, torch.full((self.B, self.pages[0].block_table.shape[1]), -1, dtype=I32, device=DEV),
+                               torch.zeros(self.B, dtype=I32, device=DEV))
+        ws = torch.empty(self.lla.lla_pages_extend_workspace_size(self.B), dtype=U8, device=DEV)
+        cu = torch.tensor([0] + lens, dtype=I32, device=DEV).cumsum(0).to(I32)
+        self.lla.lla_pages_extend(first, self.lla.Pools(), torch.zeros(sum(lens), dtype=I64, device=DEV), ws, cu_new=cu)
+        self.lla.lla_pages_fork(first, self.pages[0], (torch.arange(self.B * self.W, device=DEV) // self.W).to(I32))
+        return self
+
+    def last(self):
+        return self.pages[self.steps % 2]
+
+    def check_ledger(self):
+        """Every block is held as often as the last set's tables hold it."""
+        count, last = [0] * len(self.ref), self.last()
+        table = last.block_table.tolist()
+        for s, n in enumerate(last.context_lens.tolist()):
+            for b in table[s][:-(-n // 64)]:
+                count[b] += 1
+        assert self.ref.tolist() == count
+
+
+def test_logits_of_earlier_steps_are_let_go(lla):
+    """Each step's logits are needed until its selection is enqueued: at most the last step's are alive in the callback, and
+    the memory that the search takes does not grow with its steps."""
+    s = Search(lla, 4, 8, 50000, 30)  # 6.4 MB a step
+    base = torch.randn(s.B, s.W, s.V, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV)
+    refs, alive = [], []
+
+    def step(i, *_):
+        gc.collect()
+        alive.append(sum(r() is not None for r in refs))
+        z = base + float(i)
+        refs.append(weakref.ref(z))
+        return z
+
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    s.run(step)
+    assert max(alive) <= 1
+    assert torch.cuda.max_memory_allocated() - before <= 4 * base.numel() * 4
+
+
+def test_logits_from_another_stream(lla):
+    """The memory of logits that were made on a stream of the model's own is not handed out again before the selection has read
+    it: the hypotheses are those of logits that are all kept."""
+    side = torch.cuda.Stream()
+    results = []
+    for keep in (True, False):
+        s, kept = Search(lla, 4, 8, 50000, 20), []
+        base = torch.randn(s.B, s.W, s.V, generator=torch.Generator(device=DEV).manual_seed(2), device=DEV)
+        torch.cuda.synchronize()
+
+        def step(i, *_):
+            here = torch.cuda.current_stream()
+            with torch.cuda.stream(side):
+                z = base.roll(i * 977, 2)
+                here.wait_stream(side)
+                if keep:
+                    kept.append(z)
+            return z
+
+        s.run(step)
+        torch.cuda.synchronize()
+        results.append((s.tokens, s.parents, s.scores))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
