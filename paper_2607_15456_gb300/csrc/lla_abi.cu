@@ -681,7 +681,7 @@ lla_status lla_pages_fork(const lla_pages *from, const lla_pages *to, const int3
     if (to->S > 0 && !parents) return LLA_ERR_INVALID_ARG;
     if (any_overlap({ledger_of(to), table_of(to), lens_of(to)}, {{parents, static_cast<size_t>(to->S) * 4}})) return LLA_ERR_INVALID_ARG;
     if (from->S + to->S == 0) return LLA_OK;
-    return launch_pages_fork(*from, *to, parents, static_cast<cudaStream_t>(stream));
+    return launch_pages_fork(*from, *to, parents, false, static_cast<cudaStream_t>(stream));
 }
 
 lla_status lla_pages_extend_workspace_size(int32_t S, size_t *bytes) {
@@ -787,6 +787,23 @@ lla_status lla_beam_select_workspace_size(int32_t B, int32_t W, int32_t V, int32
     return LLA_OK;
 }
 
+extern "C++" lla_status lla::beam_select(const BeamSelectArgs &a, size_t workspace_bytes, cudaStream_t stream) {
+    if (a.row_stride < a.V || a.row_stride > (int64_t(1) << 40) || !valid_ranking(a.V, a.eos, a.length_penalty)) return LLA_ERR_INVALID_ARG;
+    if (!a.lengths && (a.length_penalty != 0.f || a.out_lengths)) return LLA_ERR_INVALID_ARG;
+    if (a.B == 0) return LLA_OK;
+    if (!a.logits || !aligned(a.logits, a.bf16 ? 2 : 4) || !a.scores || !a.parents || !a.tokens || !a.out_scores) return LLA_ERR_INVALID_ARG;
+    const size_t in = static_cast<size_t>(a.B) * a.W, out = static_cast<size_t>(a.B) * a.K;
+    const size_t need = beam_select_workspace_bytes(a.B, a.W, a.V, a.K, a.bf16);
+    const Span r0 = {a.scores, in * 4}, r1 = {a.finished, in}, r2 = {a.lengths, in * 4};
+    const Span w0 = {a.parents, out * 4}, w1 = {a.tokens, out * 4}, w2 = {a.out_scores, out * 4}, w3 = {a.out_finished, out},
+               w4 = {a.out_lengths, out * 4};
+    if (any_overlap({w0, w1, w2, w3, w4}, {r0, r1, r2})) return LLA_ERR_INVALID_ARG;
+    if (!a.workspace || !aligned(a.workspace, 16)) return LLA_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return LLA_ERR_WORKSPACE;
+    if (any_overlap({{a.workspace, need}}, {r0, r1, r2, w0, w1, w2, w3, w4})) return LLA_ERR_INVALID_ARG;
+    return launch_beam_select(a, stream);
+}
+
 lla_status lla_beam_select(int32_t B, int32_t W, int32_t V, int32_t K, const void *logits, int64_t row_stride,
                            lla_dtype logits_dtype, const float *scores, const uint8_t *finished, const int32_t *lengths,
                            int32_t eos, float length_penalty, int32_t *parents, int32_t *tokens, float *out_scores,
@@ -794,19 +811,6 @@ lla_status lla_beam_select(int32_t B, int32_t W, int32_t V, int32_t K, const voi
                            void *stream) {
     const lla_status st = check_beams(B, W, V, K, logits_dtype);
     if (st != LLA_OK) return st;
-    if (row_stride < V || row_stride > (int64_t(1) << 40) || !valid_ranking(V, eos, length_penalty)) return LLA_ERR_INVALID_ARG;
-    if (!lengths && (length_penalty != 0.f || out_lengths)) return LLA_ERR_INVALID_ARG;
-    if (B == 0) return LLA_OK;
-    if (!logits || !aligned(logits, elem_size(logits_dtype)) || !scores || !parents || !tokens || !out_scores)
-        return LLA_ERR_INVALID_ARG;
-    const size_t in = static_cast<size_t>(B) * W, out = static_cast<size_t>(B) * K;
-    const size_t need = beam_select_workspace_bytes(B, W, V, K, logits_dtype == LLA_BF16);
-    const Span r0 = {scores, in * 4}, r1 = {finished, in}, r2 = {lengths, in * 4};
-    const Span w0 = {parents, out * 4}, w1 = {tokens, out * 4}, w2 = {out_scores, out * 4}, w3 = {out_finished, out}, w4 = {out_lengths, out * 4};
-    if (any_overlap({w0, w1, w2, w3, w4}, {r0, r1, r2})) return LLA_ERR_INVALID_ARG;
-    if (!workspace || !aligned(workspace, 16)) return LLA_ERR_INVALID_ARG;
-    if (workspace_bytes < need) return LLA_ERR_WORKSPACE;
-    if (any_overlap({{workspace, need}}, {r0, r1, r2, w0, w1, w2, w3, w4})) return LLA_ERR_INVALID_ARG;
     BeamSelectArgs a = {};
     a.B = B; a.W = W; a.V = V; a.K = K; a.bf16 = logits_dtype == LLA_BF16;
     a.logits = logits; a.row_stride = row_stride;
@@ -815,7 +819,7 @@ lla_status lla_beam_select(int32_t B, int32_t W, int32_t V, int32_t K, const voi
     a.parents = parents; a.tokens = tokens; a.out_scores = out_scores;
     a.out_finished = out_finished; a.out_lengths = out_lengths;
     a.workspace = workspace;
-    return launch_beam_select(a, static_cast<cudaStream_t>(stream));
+    return beam_select(a, workspace_bytes, static_cast<cudaStream_t>(stream));
 }
 
 lla_status lla_get_device_error(void *stream, uint32_t *word) {

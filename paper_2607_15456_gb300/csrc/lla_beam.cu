@@ -689,6 +689,7 @@ struct FinishArgs {
     float *out_scores;
     uint8_t *out_finished;
     int32_t *out_lengths;
+    int32_t *model_tokens;
 };
 
 // Doubles in order as unsigned integers (no NaN); 0 is below all of them.
@@ -866,6 +867,7 @@ __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const __gri
         a.out_scores[at] = some ? static_cast<float>(total[w][i]) : -CUDART_INF_F;
         if (a.out_finished) a.out_finished[at] = !some || state[w] == 2 || token == a.eos;
         if (a.out_lengths) a.out_lengths[at] = some ? length[w] : 0;
+        if (a.model_tokens) a.model_tokens[at] = max(token, 0);
     }
 }
 
@@ -916,7 +918,7 @@ lla_status launch_beam_select(const BeamSelectArgs &b, cudaStream_t stream) {
     f.scores = b.scores; f.finished = b.finished; f.lengths = b.lengths;
     f.eos = b.eos; f.alpha = static_cast<double>(b.length_penalty);
     f.parents = b.parents; f.tokens = b.tokens; f.out_scores = b.out_scores;
-    f.out_finished = b.out_finished; f.out_lengths = b.out_lengths;
+    f.out_finished = b.out_finished; f.out_lengths = b.out_lengths; f.model_tokens = b.model_tokens;
     return launch_ex(beam_finish_kernel, dim3(b.B), kFinishThreads, 0, stream, f);
 }
 

@@ -12,9 +12,10 @@ namespace {
 
 size_t up16(size_t n) { return (n + 15) & ~static_cast<size_t>(15); }
 
-// The workspace: slots, lengths before the step, then what the extend and the selection share in turn.
+// The workspace: slots, lengths before the step, the tokens that the model gets, then what the extend and the selection share
+// in turn.
 struct Layout {
-    size_t slots, before, calls, total;
+    size_t slots, before, tokens, calls, total;
 };
 lla_status layout(int32_t B, int32_t W, int32_t V, lla_dtype dtype, Layout *l) {
     size_t extend = 0, select = 0;
@@ -23,7 +24,8 @@ lla_status layout(int32_t B, int32_t W, int32_t V, lla_dtype dtype, Layout *l) {
     if ((st = lla_pages_extend_workspace_size(B * W, &extend)) != LLA_OK) return st;
     l->slots = 0;
     l->before = up16(static_cast<size_t>(B) * W * sizeof(int64_t));
-    l->calls = l->before + up16(static_cast<size_t>(B) * W * sizeof(int32_t));
+    l->tokens = l->before + up16(static_cast<size_t>(B) * W * sizeof(int32_t));
+    l->calls = l->tokens + up16(static_cast<size_t>(B) * W * sizeof(int32_t));
     l->total = l->calls + (extend > select ? extend : select);
     return LLA_OK;
 }
@@ -58,7 +60,7 @@ extern "C" lla_status lla_beam_search(const lla_pages *pages_a, const lla_pages 
         return LLA_ERR_INVALID_ARG;
     char *ws = static_cast<char *>(workspace);
     int64_t *slots = reinterpret_cast<int64_t *>(ws + l.slots);
-    int32_t *before = reinterpret_cast<int32_t *>(ws + l.before);
+    int32_t *before = reinterpret_cast<int32_t *>(ws + l.before), *model_tokens = reinterpret_cast<int32_t *>(ws + l.tokens);
     void *calls = ws + l.calls;
     for (int32_t i = 0; i < steps; ++i) {
         const lla_pages *now = i % 2 ? pages_b : pages_a, *next = i % 2 ? pages_a : pages_b;
@@ -66,15 +68,20 @@ extern "C" lla_status lla_beam_search(const lla_pages *pages_a, const lla_pages 
         st = lla_pages_extend(now, pools, L, slots, static_cast<int32_t>(n), nullptr, finished + in, before, nullptr, calls,
                               l.total - l.calls, stream);
         if (st != LLA_OK) return st;
-        const void *logits = nullptr;
-        int64_t row_stride = V;
-        st = step(i, now, before, tokens + in, slots, &logits, &row_stride, stream, user);
+        lla::BeamSelectArgs s = {};
+        s.row_stride = V;
+        // the selection before left the tokens without the -1 of dead beams, which no table has
+        st = step(i, now, before, i ? model_tokens : tokens, slots, &s.logits, &s.row_stride, stream, user);
         if (st != LLA_OK) return st;
-        st = lla_beam_select(B, W, V, W, logits, row_stride, logits_dtype, scores + in, finished + in, lengths + in, eos,
-                             length_penalty, parents + in, tokens + out, scores + out, finished + out, lengths + out, calls,
-                             l.total - l.calls, stream);
-        if (st != LLA_OK) return st;
-        st = lla_pages_fork(now, next, parents + in, stream);
+        s.B = B; s.W = W; s.V = V; s.K = W; s.bf16 = logits_dtype == LLA_BF16;
+        s.scores = scores + in; s.finished = finished + in; s.lengths = lengths + in;
+        s.eos = eos; s.length_penalty = length_penalty;
+        s.parents = parents + in; s.tokens = tokens + out; s.out_scores = scores + out;
+        s.out_finished = finished + out; s.out_lengths = lengths + out; s.model_tokens = model_tokens;
+        s.workspace = calls;
+        if ((st = lla::beam_select(s, l.total - l.calls, static_cast<cudaStream_t>(stream))) != LLA_OK) return st;
+        // a beam that died keeps its pages: the model gets no empty sequence
+        st = lla::launch_pages_fork(*now, *next, parents + in, true, static_cast<cudaStream_t>(stream));
         if (st != LLA_OK) return st;
     }
     return LLA_OK;

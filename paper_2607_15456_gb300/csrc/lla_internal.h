@@ -147,7 +147,8 @@ bool search_arrays_overlap(const lla_pages *a, const lla_pages *b, size_t n, siz
                            const uint8_t *finished, const int32_t *lengths, const int32_t *parents, const void *workspace,
                            size_t workspace_bytes);
 // Sequences that share pages (lla_pages.cu): launches behind the checks of lla_abi.cu (no empty batch).
-lla_status launch_pages_fork(const lla_pages &from, const lla_pages &to, const int32_t *parents, cudaStream_t stream);
+// keep: a parent of -1 stands for the sequence itself (as many in `to` as in `from`).
+lla_status launch_pages_fork(const lla_pages &from, const lla_pages &to, const int32_t *parents, bool keep, cudaStream_t stream);
 lla_status launch_pages_free(const lla_pages &p, const int32_t *seqs, int n, cudaStream_t stream);
 size_t pages_extend_workspace_bytes();
 lla_status launch_pages_extend(const lla_pages &p, const lla_pool *pools, int L, int64_t *slots, int N, const int32_t *cu_new,
@@ -170,9 +171,12 @@ struct BeamSelectArgs {
     float *out_scores;
     uint8_t *out_finished;
     int32_t *out_lengths;
+    int32_t *model_tokens;  // or NULL: the tokens once more, 0 where they are -1
     void *workspace;
 };
 size_t beam_select_workspace_bytes(int B, int W, int V, int K, bool bf16);
+// lla_beam_select behind the checks of its sizes and type (lla_abi.cu), and its launches behind all checks.
+lla_status beam_select(const BeamSelectArgs &a, size_t workspace_bytes, cudaStream_t stream);
 lla_status launch_beam_select(const BeamSelectArgs &a, cudaStream_t stream);
 
 int num_sms();  // SM count of the current device (cached), 0 on failure

@@ -44,8 +44,13 @@ struct ForkArgs {
     int32_t *to_table, *to_lens;
     int to_max, to_S;
     const int32_t *parents;
+    int keep;  // parent -1 stands for the sequence itself (from_S == to_S)
     unsigned *err;
 };
+__device__ __forceinline__ int parent_of(const ForkArgs &a, int s) {
+    const int p = a.parents[s];
+    return p == -1 && a.keep ? s : p;
+}
 
 // Rows 0 .. to_S-1 of the grid copy a child's table (a CTA per kForkSpan entries, so that one long parent of many
 // children spreads over the SMs); rows to_S .. to_S+from_S-1 change the counts of a parent's
@@ -57,7 +62,7 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const ForkArgs a) {
     unsigned bad = 0;
     if (static_cast<int>(blockIdx.x) < a.to_S) {
         const int s = blockIdx.x;
-        const int p = a.parents[s];
+        const int p = parent_of(a, s);
         int len = 0;
         if (p < -1 || p >= a.from_S) {
             bad = LLA_DEVERR_SEQUENCE;
@@ -101,7 +106,7 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const ForkArgs a) {
 #pragma unroll
         for (int j = 0; j < LLA_MAX_BATCH / kForkThreads; ++j) {
             const int i = tid + j * kForkThreads;
-            if (i < a.to_S) mine += a.parents[i] == p;
+            if (i < a.to_S) mine += parent_of(a, i) == p;
         }
     }
     __shared__ int children[kForkThreads / 32];
@@ -730,7 +735,7 @@ lla_status launch_plan(void (*kern)(A), int ctas, const A &a, cudaStream_t strea
 
 }  // namespace
 
-lla_status launch_pages_fork(const lla_pages &from, const lla_pages &to, const int32_t *parents, cudaStream_t stream) {
+lla_status launch_pages_fork(const lla_pages &from, const lla_pages &to, const int32_t *parents, bool keep, cudaStream_t stream) {
     lla_status st;
     ForkArgs a = {};
     a.ref = from.ref_count; a.nb = static_cast<int>(from.num_blocks);
@@ -739,6 +744,7 @@ lla_status launch_pages_fork(const lla_pages &from, const lla_pages &to, const i
     a.to_table = to.block_table; a.to_lens = to.context_lens;
     a.to_max = to.max_blocks_per_seq; a.to_S = to.S;
     a.parents = parents;
+    a.keep = keep;
     a.err = device_error_word(&st);
     if (!a.err) return st;
     const int most = from.max_blocks_per_seq;

@@ -845,7 +845,8 @@ def lla_beam_search(pages_a: Pages, pages_b: Pages, pools: Pools, V: int, step, 
     """Beam search over parents.shape[0] steps: tokens, scores, finished, lengths [steps + 1][B][W] (slab 0 filled
     by the caller), parents [steps][B][W].  step(i, pages, lens_before, tokens, slots) runs the model for step i
     and returns its logits [B][W][V] of `dtype` (kept alive until the next step): pages is pages_a or pages_b,
-    lens_before [B W] int32, tokens [B][W] int32, slots [B W] int64.  It runs with `stream` as the current one."""
+    lens_before [B W] int32, tokens [B][W] int32 (slab 0, then the selected ones with 0 for the -1 of dead beams), slots
+    [B W] int64 (-1: the beam does not grow).  It runs with `stream` as the current one."""
     if parents.dim() != 3:
         raise ValueError("parents are [steps][B][W]")
     steps, B, W = parents.shape
@@ -861,12 +862,12 @@ def lla_beam_search(pages_a: Pages, pages_b: Pages, pools: Pools, V: int, step, 
     def _view(address, dtype_, size):
         return flat[address - base:address - base + size].view(dtype_)
 
-    def _step(i, _pages, before, _tokens, slots, logits, row_stride, _stream_, _user):
+    def _step(i, _pages, before, model_tokens, slots, logits, row_stride, _stream_, _user):
         try:
             n = B * W
             held.clear()  # the selection that reads the last step's logits is on the stream
-            z = step(i, pages_b if i % 2 else pages_a, _view(before, torch.int32, 4 * n), tokens[i],
-                     _view(slots, torch.int64, 8 * n))
+            z = step(i, pages_b if i % 2 else pages_a, _view(before, torch.int32, 4 * n),
+                     _view(model_tokens, torch.int32, 4 * n).view(B, W) if i else tokens[0], _view(slots, torch.int64, 8 * n))
             if z.dtype != dtype or tuple(z.shape) != (B, W, V):
                 raise ValueError(f"step must return {dtype} logits of shape {(B, W, V)}, not {z.dtype} {tuple(z.shape)}")
             row_stride[0] = _logit_rows(z)

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from helpers import ensure_library
+from paper_2607_15456_gb300 import workloads
 
 pytestmark = pytest.mark.gpu
 
@@ -116,3 +117,76 @@ def test_logits_from_another_stream(lla):
         torch.cuda.synchronize()
         results.append((s.tokens, s.parents, s.scores))
     assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+def masked(s, step, open_tokens, seed=5):
+    """Logits with only the tokens open_tokens[b] finite."""
+    g = torch.Generator(device=DEV).manual_seed(seed * 1000 + step)
+    z = torch.full((s.B, s.W, s.V), -math.inf, device=DEV)
+    for b, ids in enumerate(open_tokens):
+        z[b][:, ids] = torch.randn(s.W, len(ids), generator=g, device=DEV)
+    return z
+
+
+def test_dead_beams(lla):
+    """Sequence 0 has two continuations a beam in the first two steps, so two of its four beams die in the first and come back
+    in the second; sequence 1 has none at step 2 and is dead from there on; sequence 2 is as usual.  The model is
+    given a token of the vocabulary and a sequence that is not empty for every beam, dead ones too, and its decode reports
+    nothing; a dead beam keeps the pages that it had and does not grow."""
+    B, W, V, steps = 3, 4, 50, 6
+    s = Search(lla, B, W, V, steps).prompt([5, 63, 128])
+    allowed = lambda i: [[3, 7] if i < 2 else list(range(V)), list(range(V)) if i != 2 else [], list(range(V))]
+    geom = lla.Geometry(1, 1, 128, 96, 160)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    rnd = lambda *n: torch.randn(*n, generator=g, device=DEV)
+    codec = lla.Codec(**workloads.codec_tensors(1, 1, 128, 96, 160, 3, 0, device=DEV))
+    pool = torch.zeros(len(s.ref) * lla.lla_cache_block_bytes(geom), dtype=U8, device=DEV)
+    dws = torch.zeros(lla.lla_decode_workspace_size(geom, B * W), dtype=U8, device=DEV)
+    seen = []
+
+    def step(i, pages, before, toks, slots):
+        seen.append([t.clone() for t in (toks, before, pages.context_lens, slots)])
+        out = torch.empty(B * W, 1, 128, dtype=F32, device=DEV)
+        cache = lla.Cache(pool, len(s.ref), pages.block_table, 4)
+        lla.lla_decode_attn(geom, codec, cache, pages.context_lens, 256, 0, rnd(B * W, 1, 128), None, None, out, dws)  # pass 2
+        assert torch.isfinite(out).all()
+        return masked(s, i, allowed(i))
+
+    s.run(step, pools=[lla.lla_cache_pool(geom, pool)])
+    assert lla.lla_get_device_error() == 0
+    tokens, parents, finished, lengths = (t.tolist() for t in (s.tokens, s.parents, s.finished, s.lengths))
+    # dead where there is no continuation: two in sequence 0 at the first step; all of sequence 1 from step 2 on
+    dead = [[[p < 0 for p in row] for row in slab] for slab in parents]
+    assert [sum(d) for d in dead[0]] == [2, 0, 0] and [sum(d) for d in dead[1]] == [0, 0, 0]
+    assert [[sum(d) for d in slab] for slab in dead[2:]] == [[0, 4, 0]] * (steps - 2)
+    for i in range(steps):
+        toks, before, lens, slots = (t.view(B, W).tolist() for t in seen[i])
+        for b in range(B):
+            for w in range(W):
+                was_dead = i > 0 and dead[i - 1][b][w]
+                if was_dead:  # the slabs say so; the model gets a token that it can look up
+                    assert tokens[i][b][w] == -1 and finished[i][b][w] == 1 and lengths[i][b][w] == 0 and s.scores[i, b, w] == -math.inf
+                    # the pages of its last step, as they are
+                    assert toks[b][w] == 0 and slots[b][w] == -1 and lens[b][w] == before[b][w] == seen[i - 1][2].view(B, W)[b, w]
+                else:
+                    assert toks[b][w] == tokens[i][b][w] and slots[b][w] >= 0 and lens[b][w] == before[b][w] + 1
+                assert lens[b][w] > 0
+    s.check_ledger()
+    lla.lla_pages_free(s.last(), torch.arange(B * W, dtype=I32, device=DEV))
+    assert not s.ref.any()
+
+
+def test_ended_beams_without_an_ending_token(lla):
+    """With eos = -1 a beam that the caller marks as ended has token -1 in the slabs; the model is given one that it can look up."""
+    s = Search(lla, 1, 3, 40, 3).prompt([10])
+    s.finished[0, 0, 1] = 1
+    s.scores[0, 0, 1] = 1.0
+    seen = []
+
+    def step(i, pages, before, toks, slots):
+        seen.append(toks.clone())
+        return masked(s, i, [list(range(s.V))])
+
+    s.run(step)
+    assert (s.tokens[1:, 0, 0] == -1).all() and (s.parents[1:, 0, 0] == 0).all()
+    assert all((t >= 0).all() and (t < s.V).all() for t in seen)
