@@ -656,6 +656,8 @@ lla_status lla_beam_search_workspace_size(int32_t B, int32_t W, int32_t V, lla_d
  * kernels on `stream`.  Step i is lla_pages_extend by one token (finished beams do not grow), the caller's
  * model, lla_beam_select with K = W, lla_pages_fork by its parents.  Where a sequence has fewer than W continuations
  * (masked logits), the beams behind them are dead: parent and token -1, score -inf, finished, length 0 in the slabs.  A
+ * beam whose token finds no room (LLA_DEVERR_PAGES, _CONTEXT or _BLOCK_ID of lla_pages_extend) has no continuation, so no
+ * hypothesis goes on with a hole; the ended ones stay, and the parents of that step hold -1 for the others.  A
  * dead beam keeps the pages that the same beam had before the selection, so that the model meets no empty sequence, and is
  * replaced as soon as its sequence has enough continuations again.
  *   pages_a, pages_b  two page sets as lla_pages_fork takes them, S = B W; sequence b W + w is beam w of
@@ -669,6 +671,11 @@ lla_status lla_beam_search_workspace_size(int32_t B, int32_t W, int32_t V, lla_d
  *   parents           device [steps][B][W] int32, written: the beam of slab i that each of slab i + 1
  *                     continues; a hypothesis is read by walking back from its beam in the last slab
  *   pools, L          as lla_pages_extend
+ * Pages: the beams of a sequence whose P cached tokens they share hold P / 64 + W (ceil((P + steps) / 64) - P / 64) blocks
+ * at most (divisions rounded down), so a search with that many for each sequence never runs out.  Nothing is read back, so
+ * a search does not stop when every beam has ended: a caller who wants that runs it in pieces (an even number of steps
+ * leaves the beams in pages_a; the last slab of a piece is slab 0 of the next, with any token in place of a -1) and
+ * looks between them.
  * What would be wrong in every step (page sets, pools, eos, length_penalty, arrays that overlap) is refused before the
  * first.  Beyond that the error behaviour of each step is that of its call; the first non-OK status is returned (the
  * work enqueued before it stays enqueued).  The workspace as for lla_pages_extend.

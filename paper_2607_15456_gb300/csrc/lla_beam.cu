@@ -683,6 +683,7 @@ struct FinishArgs {
     const float *scores;
     const uint8_t *finished;
     const int32_t *lengths;
+    const int64_t *slots;
     int eos;
     double alpha;
     int32_t *parents, *tokens;
@@ -764,7 +765,8 @@ __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const __gri
         const float s = a.scores[row0 + lane];
         const bool ended = a.finished && a.finished[row0 + lane];
         const int64_t n = a.lengths ? static_cast<int64_t>(a.lengths[row0 + lane]) + (ended ? 0 : 1) : 1;
-        state[lane] = !(fabsf(s) <= FLT_MAX) ? 0 : ended ? 2 : 1;
+        const bool hole = a.slots && a.slots[row0 + lane] < 0;  // its last token is not cached
+        state[lane] = !(fabsf(s) <= FLT_MAX) ? 0 : ended ? 2 : hole ? 0 : 1;
         length[lane] = static_cast<int>(n < INT32_MAX ? n : INT32_MAX);
         score_of[lane] = my_score = s;
         scale[lane] = a.alpha == 0.0 ? 1.0 : exp_of(-a.alpha * log_of(static_cast<double>(n > 1 ? n : 1)));  // |x| <= 16 log 2^31
@@ -915,7 +917,7 @@ lla_status launch_beam_select(const BeamSelectArgs &b, cudaStream_t stream) {
     f.logs = log_table();
     f.W = b.W; f.K = b.K; f.shares = shares;
     f.lists = a.lists; f.sums = a.sums;
-    f.scores = b.scores; f.finished = b.finished; f.lengths = b.lengths;
+    f.scores = b.scores; f.finished = b.finished; f.lengths = b.lengths; f.slots = b.slots;
     f.eos = b.eos; f.alpha = static_cast<double>(b.length_penalty);
     f.parents = b.parents; f.tokens = b.tokens; f.out_scores = b.out_scores;
     f.out_finished = b.out_finished; f.out_lengths = b.out_lengths; f.model_tokens = b.model_tokens;

@@ -74,7 +74,7 @@ extern "C" lla_status lla_beam_search(const lla_pages *pages_a, const lla_pages 
         st = step(i, now, before, i ? model_tokens : tokens, slots, &s.logits, &s.row_stride, stream, user);
         if (st != LLA_OK) return st;
         s.B = B; s.W = W; s.V = V; s.K = W; s.bf16 = logits_dtype == LLA_BF16;
-        s.scores = scores + in; s.finished = finished + in; s.lengths = lengths + in;
+        s.scores = scores + in; s.finished = finished + in; s.lengths = lengths + in; s.slots = slots;
         s.eos = eos; s.length_penalty = length_penalty;
         s.parents = parents + in; s.tokens = tokens + out; s.out_scores = scores + out;
         s.out_finished = finished + out; s.out_lengths = lengths + out; s.model_tokens = model_tokens;

@@ -165,6 +165,7 @@ struct BeamSelectArgs {
     const float *scores;
     const uint8_t *finished;
     const int32_t *lengths;
+    const int64_t *slots;  // [B][W] or NULL: a beam that has not ended and whose slot is -1 has no continuation
     int eos;
     float length_penalty;
     int32_t *parents, *tokens;

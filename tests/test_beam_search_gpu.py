@@ -190,3 +190,76 @@ def test_ended_beams_without_an_ending_token(lla):
     s.run(step)
     assert (s.tokens[1:, 0, 0] == -1).all() and (s.parents[1:, 0, 0] == 0).all()
     assert all((t >= 0).all() and (t < s.V).all() for t in seen)
+
+
+@pytest.mark.parametrize("why", ["pages", "context"])
+def test_growth_that_fails(lla, why):
+    """A beam whose token finds no room has no continuation, so that no hypothesis with a hole goes on: from the step that fails
+    only the beam that has ended is left, and the first slab of parents with -1 says which step that was."""
+    B, W, V, steps, eos = 1, 3, 30, 5, 4
+    if why == "pages":  # 64 cached tokens: each beam takes a block in step 0, the other two of the four are free in step 1, until one is taken
+        s, error = Search(lla, B, W, V, steps, blocks=4).prompt([64]), lla.LLA_DEVERR_PAGES
+    else:               # a row of one page: step 0 fills it
+        s, error = Search(lla, B, W, V, steps, blocks=8, max_blocks=1).prompt([63]), lla.LLA_DEVERR_CONTEXT
+    seen = []
+
+    def step(i, pages, before, toks, slots):
+        seen.append([t.clone() for t in (slots, pages.context_lens, toks)])
+        z = masked(s, i, [list(range(V))])
+        if i == 0:
+            z[:, :, eos] = 9.0  # the best continuation ends
+            if why == "pages":
+                s.ref[3] += 1   # another user of the pool
+        return z
+
+    s.run(step, eos=eos)
+    assert lla.lla_get_device_error() == error
+    lla.lla_clear_device_error()
+    assert s.parents[0].tolist() == [[0, 0, 0]] and s.finished[1].tolist() == [[1, 0, 0]]
+    for i in range(1, steps):
+        assert s.parents[i].tolist() == [[0, -1, -1]], i
+        assert s.tokens[i + 1].tolist() == [[eos, -1, -1]] and s.finished[i + 1].tolist() == [[1, 1, 1]]
+        assert s.scores[i + 1].tolist() == [[s.scores[1, 0, 0].item(), -math.inf, -math.inf]]
+        assert seen[i][0].tolist() == [-1] * 3
+        assert seen[i][1].tolist() == seen[1][1].tolist()
+        assert (seen[i][2] >= 0).all()
+    if why == "pages":
+        s.ref[3] -= 1
+    s.check_ledger()
+    lla.lla_pages_free(s.last(), torch.arange(B * W, dtype=I32, device=DEV))
+    assert not s.ref.any()
+
+
+def test_in_pieces(lla):
+    """Two steps and then four give what six give; and no more blocks are held at any step than the documented number."""
+    B, W, V, prompts = 2, 4, 50, [130, 62]
+    allowed = [[3, 7], list(range(V))]  # sequence 0 has dead beams at first
+    bound = sum(P // 64 + W * (-(-(P + 6) // 64) - P // 64) for P in prompts)
+
+    def run(steps, start=None, first=0):
+        s = Search(lla, B, W, V, steps, blocks=bound)
+        if start is None:
+            s.prompt(prompts)
+        else:
+            s.ref, s.pages = start.ref, start.pages
+            for name in ("tokens", "scores", "finished", "lengths"):
+                getattr(s, name)[0] = getattr(start, name)[-1]
+            s.tokens[0].clamp_(min=0)
+
+        def step(i, pages, before, toks, slots):
+            z = masked(s, i + first, allowed if i + first < 2 else [allowed[1]] * 2)
+            z[:, :, 9] += 1.5
+            return z + toks[:, :, None] / 100
+
+        return s.run(step, eos=9, length_penalty=0.4)
+
+    whole, one = run(6), run(2)
+    assert lla.lla_get_device_error() == 0
+    two = run(4, one, 2)
+    for name in ("tokens", "scores", "finished", "lengths"):
+        a, b = getattr(whole, name), getattr(two, name)
+        assert torch.equal(a[3:], b[1:]) and torch.equal(a[:3], getattr(one, name)), name
+    assert torch.equal(whole.parents, torch.cat([one.parents, two.parents]))
+    assert torch.equal(whole.ref, two.ref) and torch.equal(whole.last().context_lens, two.last().context_lens)
+    two.check_ledger()
+    assert whole.finished.any()
