@@ -539,6 +539,7 @@ lla_status lla_rope_pool(int32_t d_rope, void *rope_pool, lla_pool *out);
  *              after the call, although its arrays are left as they are: its next use is as a `to`
  *   parents    device [to->S] int32; one outside [-1, from->S) sets LLA_DEVERR_SEQUENCE and counts as -1
  * A parent of more pages than to->max_blocks_per_seq sets LLA_DEVERR_CONTEXT, and its children are empty.
+ * So does a sequence of `from` whose length is out of range, child or not: its pages stay counted.
  */
 lla_status lla_pages_fork(const lla_pages *from, const lla_pages *to, const int32_t *parents,
                           void *stream);

@@ -93,8 +93,9 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const ForkArgs a) {
         return;
     }
     const int p = blockIdx.x - a.to_S;
-    const int n = pages_of(max(0, checked_len(a.from_lens[p], a.from_max)));
+    const int len = checked_len(a.from_lens[p], a.from_max), n = pages_of(max(0, len));
     const int lo0 = blockIdx.y * kForkSpan;
+    if (len < 0 && blockIdx.y == 0 && tid == 0) atomicOr(a.err, LLA_DEVERR_CONTEXT);  // its pages stay counted
     if (lo0 >= n) return;
     const int32_t *row = a.from_table + static_cast<int64_t>(p) * a.from_max;
     constexpr int kEach = kForkSpan / kForkThreads;

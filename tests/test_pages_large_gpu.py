@@ -44,3 +44,17 @@ def test_the_longest_slot_mapping(lla):
     assert one.context_lens.tolist() == [3]
     assert lla.lla_get_device_error() == lla.LLA_DEVERR_CONTEXT
     lla.lla_clear_device_error()
+
+
+@pytest.mark.parametrize("length", [-1, 257, -2 ** 31, 2 ** 31 - 1])
+def test_fork_reports_a_length_out_of_range_that_no_child_has(lla, length):
+    """Its pages cannot be given back, so the call says so, as lla_pages_free does; the others' are."""
+    i = lambda *v: torch.tensor(v, dtype=I32, device=DEV)
+    ref = i(1, 2, 1, 1)
+    a = lla.Pages(ref, torch.tensor([[0, 1, -7, -7], [1, 2, 3, -7]], dtype=I32, device=DEV), i(100, length))
+    b = lla.Pages(ref, torch.full((3, 4), -7, dtype=I32, device=DEV), i(9, 9, 9))
+    lla.lla_pages_fork(a, b, i(0, -1, 0))
+    assert lla.lla_get_device_error() == lla.LLA_DEVERR_CONTEXT
+    lla.lla_clear_device_error()
+    assert b.context_lens.tolist() == [100, 0, 100] and b.block_table.tolist() == [[0, 1, -7, -7], [-7] * 4, [0, 1, -7, -7]]
+    assert ref.tolist() == [2, 3, 1, 1]
