@@ -30,8 +30,7 @@
 #include <math_constants.h>
 #include <stdint.h>
 
-#include <cmath>
-
+#include "lla_beam_math.cuh"
 #include "lla_device.cuh"
 #include "lla_internal.h"
 #include "lla_units.cuh"
@@ -658,23 +657,6 @@ __global__ void __launch_bounds__(kScanThreads, kScanCtas) beam_scan_kernel(cons
 constexpr int kFinishThreads = 512;
 constexpr int kFinishWarps = kFinishThreads / 32;
 
-// For a number in the i-th of 32 parts of [1, 2): a float r near its reciprocal, and -log r.
-struct LogTable {
-    float r[32];
-    double minus_log[32];
-};
-const LogTable &log_table() {
-    static const LogTable t = [] {
-        LogTable x;
-        for (int i = 0; i < 32; ++i) {
-            x.r[i] = static_cast<float>(1.0 / (1.0 + (i + 0.5) / 32));
-            x.minus_log[i] = -std::log(static_cast<double>(x.r[i]));
-        }
-        return x;
-    }();
-    return t;
-}
-
 struct FinishArgs {
     LogTable logs;
     int W, K, shares;
@@ -698,50 +680,6 @@ __device__ __forceinline__ u64 double_key(double x) {
     u64 u = static_cast<u64>(__double_as_longlong(x));
     if (u << 1 == 0) u = 0;  // -0
     return u ^ ((u >> 63) ? ~0ull : 1ull << 63);
-}
-
-// An fp64 operation takes about 100 cycles here, and what follows is on the way of every call: few of them, one after
-// the other.
-
-// log (hi + lo) of a normal positive hi, |lo| far below it (of another: some number), off by less than 4e-9: with hi = 2^e m,
-// m r = 1 + u, |u| <= 1/64, it is e log 2 - log r + log (1 + u), the last a short series in fp32.
-__device__ __forceinline__ double log_sum(float hi, float lo, const LogTable &t) {
-    const uint32_t b = __float_as_uint(hi);
-    const int e = static_cast<int>(b >> 23 & 255) - 127, i = b >> 18 & 31;
-    const float m = __uint_as_float((b & 0x7fffffu) | 0x3f800000u), r = t.r[i];
-    const float u = lo / hi + fmaf(m, r, -1.f);
-    const float p = u * fmaf(u, fmaf(u, fmaf(u, fmaf(u, 0.2f, -0.25f), 1.f / 3.f), -0.5f), 1.f);
-    return static_cast<double>(e) * 0.693147180559945309 + (t.minus_log[i] + static_cast<double>(p));
-}
-
-// log n of n >= 1, off by less than 1e-12: n = 2^e m with m between sqrt(1/2) and sqrt(2), and log m = 2 atanh t =
-// 2 (t + t^3 / 3 + ... + t^13 / 13), t = (m - 1) / (m + 1), |t| <= 0.172, the series in pairs (Estrin).
-__device__ __forceinline__ double log_of(double x) {
-    const long long u = __double_as_longlong(x);
-    const long long half = 0x3fe6a09e667f3bcdll;  // sqrt(1/2)
-    const int e = static_cast<int>((u - half) >> 52);
-    const double m = __longlong_as_double(u - (static_cast<long long>(e) << 52));
-    const double d = m + 1.0;
-    const double r0 = static_cast<double>(__frcp_rn(static_cast<float>(d)));
-    const double r = r0 * fma(-d, r0, 2.0);  // one step of Newton: 2^-23 squared
-    const double t = (m - 1.0) * r, w = t * t, w2 = w * w;
-    const double a = fma(w, 1.0 / 3.0, 1.0), b = fma(w, 1.0 / 7.0, 1.0 / 5.0), c = fma(w, 1.0 / 11.0, 1.0 / 9.0);
-    const double p = fma(w2, fma(w2, fma(w2, 1.0 / 13.0, c), b), a);
-    return fma(static_cast<double>(e), 0.693147180559945309, 2.0 * t * p);
-}
-
-// exp x for |x| <= 400, off by less than 1e-13 of itself: x = k log 2 + r, |r| <= 0.347, and the series of exp r to
-// r^13, in pairs.
-__device__ __forceinline__ double exp_of(double x) {
-    const double k = rint(x * 1.4426950408889634);
-    const double r = fma(-k, 2.3190468138462996e-17, fma(-k, 0.6931471805599453, x));  // log 2 as a sum of two
-    const double r2 = r * r, r4 = r2 * r2, r8 = r4 * r4;
-    const double p01 = 1.0 + r, p23 = fma(r, 1.0 / 6.0, 0.5), p45 = fma(r, 1.0 / 120.0, 1.0 / 24.0);
-    const double p67 = fma(r, 1.0 / 5040.0, 1.0 / 720.0), p89 = fma(r, 1.0 / 362880.0, 1.0 / 40320.0);
-    const double pab = fma(r, 1.0 / 39916800.0, 1.0 / 3628800.0), pcd = fma(r, 1.0 / 6227020800.0, 1.0 / 479001600.0);
-    const double p03 = fma(r2, p23, p01), p47 = fma(r2, p67, p45), p8b = fma(r2, pab, p89);
-    const double p = fma(r8, fma(r4, pcd, p8b), fma(r4, p47, p03));
-    return p * __longlong_as_double((static_cast<long long>(k) + 1023) << 52);
 }
 
 __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const __grid_constant__ FinishArgs a) {
