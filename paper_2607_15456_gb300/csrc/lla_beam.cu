@@ -20,10 +20,18 @@
 // bound by the chain of the two launches: 4 beams of 32000 logits take 8.4 us, of which the host call is 4.
 //
 // Precision.  Ranks are compared in 64 bits, so what matters is log S, which the candidates of a beam share: it
-// decides between beams.  A term 2^(z log2 e - c) takes one rounding of its exponent, small where the term counts; c is a
-// whole number, so that sums of threads and shares go to a common one exactly; a tile's 16 or 32 terms are summed as a
-// tree, and the sums of tiles, threads and shares carry their rounding errors along (Knuth's two-sum).  So log S is
-// off by the 2^-22 of ex2.approx on single terms, and not by the length of the row.
+// decides between beams.  A term 2^(z K - c), K the fp32 number next to log2 e, takes one rounding of its exponent: 2^-24 |z - b|
+// in log S, b = c / K.  K is off by less than 2^-26 of itself, and since sums are put together as powers of 2^K, with b formed from
+// the same K, that counts with |z - b| as well, not with |z|.  b is a largest logit seen (to within 0.35, as c is whole), and a thread
+// moves it once a logit is kRise = 5 above, so |z - b| <= max(5, top - z) + 0.35, of which the mean under the softmax, d, counts.
+// ex2.approx adds 2^-22; a tile's 16 or 32 terms are summed as a tree of five roundings of 2^-24 (logit by logit, where some are not
+// finite, ten); the sums of tiles, threads and shares carry their rounding errors along (Knuth's two-sum) and go to a common base
+// exactly; the logarithm adds 4e-9:
+//   |error of log S| <= 2^-22 + (5 or 10) 2^-24 + 1.25 2^-24 d + 4e-9 < (6 or 9)e-7 + 7.5e-8 d,
+// whatever the length of the row.  (d is 5 to 7 for most rows; below one large logit, flat rows have ln V.)  How a row is cut into
+// shares decides which b a term meets, so the same beam's score may differ by as much from batch to batch.  With kRise = 60 single
+// logits far above the first tile were off by 1.4e-6 in a test and by up to 3.4e-6 on paper.  A move sends its warp past the usual tiles'
+// loop: kRise = 60, 5, 4 and 2 took 55.9, 56.5, 57.0 and 58.0 us on the largest batch.
 #include <cuda_runtime.h>
 #include <float.h>
 #include <math.h>
@@ -47,7 +55,7 @@ constexpr int kFew = 4;                               // threads over K that may
 constexpr int kCap = (2 * LLA_MAX_BEAMS - 1 + kFew) * kWords * 8 + LLA_MAX_BEAMS;                            // candidates that a CTA holds
 constexpr int kMaxShares = 32;                        // shares of a row: a warp merges them
 constexpr int kListLen = LLA_MAX_BEAMS;               // a list is a warp's lanes
-constexpr float kRise = 60.f;                         // a logit this far over the base's moves it (e^60 2^24 is finite)
+constexpr float kRise = 5.f;                          // a logit this far over the base's moves it: exponents of terms stay below 8
 
 typedef unsigned long long u64;
 
@@ -282,9 +290,12 @@ struct Base {
     }
     __device__ __forceinline__ float at() const { return wide ? c : c * (1.f / kLog2e); }  // as a logit, nearly
 };
-// The factor of a sum that goes from one base to another.
+// The factor of a sum that goes from one base to another: exact, where neither is wide (and 0 below 2^-126).
 __device__ __forceinline__ float rebase(const Base &from, const Base &to) {
-    if (!from.wide && !to.wide) return ex2(from.c - to.c);
+    if (!from.wide && !to.wide) {
+        const float n = fminf(from.c - to.c, 127.f);
+        return n < -126.f ? 0.f : __int_as_float((static_cast<int>(n) + 127) << 23);
+    }
     return ex2((from.at() - to.at()) * kLog2e);
 }
 
@@ -536,11 +547,15 @@ __global__ void __launch_bounds__(kScanThreads, kScanCtas) beam_scan_kernel(cons
                     lo *= f;
                 }
                 float s = tile_sum<BF16>(v, base.c);
-                if (!(s <= FLT_MAX) || base.wide) {  // a logit that is not finite, or a wide base: one by one
+                if (!(s <= FLT_MAX) || base.wide) {  // a logit that is not finite, or a wide base: one by one, word by word
                     s = 0.f;
-                    for (int i = 0; i < kMine; ++i) {
-                        const float x = r.staged(slot, tid, i);
-                        if (fabsf(x) <= FLT_MAX) s += ex2(base.wide ? (x - base.c) * kLog2e : fmaf(x, kLog2e, -base.c));
+                    for (int j = 0; j < kWords; ++j) {
+                        float word = 0.f;
+                        for (int i = j * kPer; i < (j + 1) * kPer; ++i) {
+                            const float x = r.staged(slot, tid, i);
+                            if (fabsf(x) <= FLT_MAX) word += ex2(base.wide ? (x - base.c) * kLog2e : fmaf(x, kLog2e, -base.c));
+                        }
+                        s += word;
                     }
                 }
                 two_sum(hi, lo, s);
