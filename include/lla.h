@@ -608,8 +608,9 @@ lla_status lla_beam_select_workspace_size(int32_t B, int32_t W, int32_t V, int32
  *   s = s_w + z_v - log sum_u exp z_u
  * over the beam's finite logits z (a logit that is infinite or NaN masks its token).  Continuations are
  * ranked by s n^-length_penalty, n the hypothesis' tokens after the step; s and the ranking are formed in 64 bits from
- * log sum exp, which is off by less than 1e-6 + 1e-7 d, d the mean under the softmax of max(5, the largest logit - z): beams whose
- * continuations rank closer together than that may change places.  Within a beam the order is that of the logits; ties
+ * log sum exp, which is off by less than 1e-6 + 1e-7 d, d the mean under the softmax of max(5, the largest logit - z) (three
+ * times as much where the largest logit is beyond +-65536): beams whose continuations rank closer together than that
+ * may change places.  Within a beam the order is that of the logits; ties
  * go to the lower beam, within a beam to the lower token.  A beam whose score is not finite has no
  * continuation; a finished one has one: itself, with token eos, at its score and length.
  *   logits        device [B][W] rows of V, row_stride elements apart (>= V), logits_dtype; element-aligned

@@ -28,7 +28,8 @@
 // finite, ten); the sums of tiles, threads and shares carry their rounding errors along (Knuth's two-sum) and go to a common base
 // exactly; the logarithm adds 4e-9:
 //   |error of log S| <= 2^-22 + (5 or 10) 2^-24 + 1.25 2^-24 d + 4e-9 < (6 or 9)e-7 + 7.5e-8 d,
-// whatever the length of the row.  (d is 5 to 7 for most rows; below one large logit, flat rows have ln V.)  How a row is cut into
+// whatever the length of the row.  Rows with logits beyond +-65536 (Base::wide) pay 2^-22 + 2^-23 + 2^-23 d more for each move of a sum
+// to another base, of which there are three, as a rule, and six that count at most.  (d is 5 to 7 for most rows; below one large logit, flat rows have ln V.)  How a row is cut into
 // shares decides which b a term meets, so the same beam's score may differ by as much from batch to batch.  With kRise = 60 single
 // logits far above the first tile were off by 1.4e-6 in a test and by up to 3.4e-6 on paper.  A move sends its warp past the usual tiles'
 // loop: kRise = 60, 5, 4 and 2 took 55.9, 56.5, 57.0 and 58.0 us on the largest batch.
@@ -290,13 +291,33 @@ struct Base {
     }
     __device__ __forceinline__ float at() const { return wide ? c : c * (1.f / kLog2e); }  // as a logit, nearly
 };
-// The factor of a sum that goes from one base to another: exact, where neither is wide (and 0 below 2^-126).
+__device__ __forceinline__ bool same(const Base &a, const Base &b) { return a.c == b.c && a.wide == b.wide; }
+
+// A base as a logit in 64 bits: what its sums are in units of the exponential of.
+__device__ __forceinline__ double logit_of(const Base &b) {
+    return static_cast<double>(b.c) * (b.wide ? 1.0 : 1.0 / static_cast<double>(kLog2e));
+}
+
+// The factor of a sum that goes from one base to another, 2^(from - to) with bases in units of 1 / K: a power of two, and exact, where
+// neither is wide (0 below 2^-126).  A wide base's c K is taken as a sum of two: near +-65536 its fp32 number is 2^-8 off (1.1e-4 of
+// log S in rows on both sides, when this went through fp32 logits).  Beyond 2^20 a wide and another base are too far apart for any sum.
+// (In fp64 the same cost small calls 1.2 us, even where no base is wide.)
 __device__ __forceinline__ float rebase(const Base &from, const Base &to) {
-    if (!from.wide && !to.wide) {
-        const float n = fminf(from.c - to.c, 127.f);
-        return n < -126.f ? 0.f : __int_as_float((static_cast<int>(n) + 127) << 23);
+    float n = from.c - to.c, rest = 0.f;
+    if (from.wide || to.wide) {
+        float d = n * kLog2e, low = 0.f;
+        if (from.wide != to.wide) {
+            const float w = fminf(fmaxf(from.wide ? from.c : to.c, -1048576.f), 1048576.f), wk = w * kLog2e, wl = fmaf(w, kLog2e, -wk);
+            d = from.wide ? wk - to.c : from.c - wk;
+            low = from.wide ? wl : -wl;
+        }
+        d = fmaxf(d, -1000.f);
+        n = rintf(d);
+        rest = (d - n) + low;
     }
-    return ex2((from.at() - to.at()) * kLog2e);
+    n = fminf(n, 127.f);
+    const float f = n < -126.f ? 0.f : __int_as_float((static_cast<int>(n) + 127) << 23);
+    return f * ex2(rest);
 }
 
 // The sum of a thread's terms of a tile, not wide: a tree of pairs.
@@ -638,10 +659,12 @@ __global__ void __launch_bounds__(kScanThreads, kScanCtas) beam_scan_kernel(cons
     M = sh.maxima[0];
 #pragma unroll
     for (int i = 1; i < kWarps; ++i) M = fmaxf(M, sh.maxima[i]);
-    if (have_base && base.at() == M) sh.base = base;  // those of equal at() are the same
+    // those of equal at() are the same, but that one may be wide and another not
+    const bool wide = __syncthreads_or(have_base && base.at() == M && base.wide);
+    if (have_base && base.at() == M && base.wide == wide) sh.base = base;
     __syncthreads();
     const Base common = sh.base;
-    if (have_base && base.at() != M) {
+    if (have_base && !same(base, common)) {
         const float f = rebase(base, common);
         hi *= f;
         lo *= f;
@@ -746,9 +769,10 @@ __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const __gri
                 if (logs_here) score = a.scores[row0 + w];
                 const Base base = {sum.c, sum.wide != 0.f};
                 const float M = warp_max(base.at());
-                const int top_lane = __ffs(__ballot_sync(0xffffffffu, base.at() == M)) - 1;
+                const unsigned tops = __ballot_sync(0xffffffffu, base.at() == M), wide_tops = __ballot_sync(0xffffffffu, base.wide) & tops;
+                const int top_lane = __ffs(wide_tops ? wide_tops : tops) - 1;
                 const Base common = {__shfl_sync(0xffffffffu, base.c, top_lane), __shfl_sync(0xffffffffu, base.wide, top_lane) != 0};
-                const float f = sum.c > -CUDART_INF_F ? rebase(base, common) : 0.f;  // a power of two but for wide bases
+                const float f = sum.c > -CUDART_INF_F ? rebase(base, common) : 0.f;  // 1 where they are the same
                 float hi = sum.hi * f, lo = sum.lo * f;
                 for (int o = 1; o < a.shares; o <<= 1) {
                     const float h = __shfl_xor_sync(0xffffffffu, hi, o), l = __shfl_xor_sync(0xffffffffu, lo, o);
@@ -758,7 +782,7 @@ __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const __gri
                 if (lane == 0) {
                     mass[w] = make_float2(hi, lo);
                     if (logs_here) rest[w] = static_cast<double>(score) - log_sum(hi, lo, a.logs);
-                    offset[w] = common.wide ? static_cast<double>(common.c) : static_cast<double>(common.c) * (1.0 / static_cast<double>(kLog2e));
+                    offset[w] = logit_of(common);
                 }
             }
             for (int s = p; s < a.shares; s += parts) {

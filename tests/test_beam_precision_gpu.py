@@ -5,7 +5,9 @@ log S, b = c / K; K is off by less than 2^-26 of itself, which counts with |z - 
 the largest logit that the thread or its CTA had seen when it was set, to within 0.35 (c is whole), and a thread sets it anew
 where a logit is 5 above that: so -0.35 - (largest - z) <= z - b <= 5.35.  A tile's terms are summed as a tree of five levels at
 most, 2^-24 each, or logit by logit with ten roundings where some are not finite; what comes behind carries its errors along; the
-logarithm is off by 4e-9.  Moving a sum to another b is exact.  Weights are those of the softmax.
+logarithm is off by 4e-9.  Moving a sum to another b is exact,
+or beyond +-65536, where terms are 2^((z - b) K) with a logit b (and are summed one by one), costs 2^-22 for another ex2, 2^-23 for its
+factor, and 2^-24 of the distance moved, which is at most 2 d in all: the thread's own move, to its CTA's b, to the row's.  Weights are those of the softmax.
 
 Scores are given so that results are near zero, where an fp32 output has no rounding of its own to speak of."""
 import math
@@ -32,13 +34,13 @@ def lla():
     return m
 
 
-def log_sum(x, tree=TREE):
+def log_sum(x, tree=TREE, moves=0):
     """log sum exp of finite logits in 64 bits, and how far the kernel's may be off."""
     top = x.max()
     p = np.exp(x - top)
     S = math.fsum(p)
     d = float((p / S * np.maximum(5.0, top - x)).sum()) + 0.35
-    return top + math.log(S), EX2 + tree + 1.25 * 2.0 ** -24 * d + 4e-9
+    return top + math.log(S), (1 + 1.5 * moves) * EX2 + tree + (1.25 + (2 if moves else 0)) * 2.0 ** -24 * d + 4e-9
 
 
 def best_score(lla, z, score):
@@ -52,11 +54,11 @@ def best_score(lla, z, score):
     return f64(out)[:, 0], tokens.view(-1).tolist()
 
 
-def check(lla, z, tree=TREE):
+def check(lla, z, *how):
     """Every row of z [B][1][V], with the beam's score set to what brings the result near zero."""
     x = f64(z)[:, 0]
     fin = [r[np.isfinite(r)] for r in x]
-    want = [log_sum(r, tree) for r in fin]
+    want = [log_sum(r, *how) for r in fin]
     lift = np.array([np.float32(L - r.max()) for (L, _), r in zip(want, fin)], dtype=np.float32)
     got, _ = best_score(lla, z, torch.from_numpy(lift).to(DEV))
     for b, ((L, bound), r) in enumerate(zip(want, fin)):
@@ -77,10 +79,10 @@ def test_noise(lla, dtype, B, V, scale):
     check(lla, z) if B <= 40 else check_some(lla, z)
 
 
-def check_some(lla, z, tree=TREE):
+def check_some(lla, z, *how):
     """All rows at once (so that a CTA has a whole one), 40 of them compared."""
     x = f64(z[::16])[:, 0]
-    want = [log_sum(r[np.isfinite(r)], tree) for r in x]
+    want = [log_sum(r[np.isfinite(r)], *how) for r in x]
     tops = [r[np.isfinite(r)].max() for r in x]
     lift = torch.zeros(len(z), device=DEV)
     lift[::16] = torch.tensor([L - t for (L, _), t in zip(want, tops)], dtype=torch.float64).float().to(DEV)
@@ -135,6 +137,25 @@ def test_long_rows_of_equal_logits(lla, value):
     exact = float(f64(lift)[0]) - math.log(V)
     bound = EX2 + 1.25 * 2.0 ** -24 * 0.35 + 4e-9
     assert np.abs(got - exact).max() <= bound + abs(exact) * 2.0 ** -24, (got[0], exact, bound)
+
+
+@pytest.mark.parametrize("shares", ["one", "many"])
+@pytest.mark.parametrize("at", [65536.0, -65536.0])
+def test_logits_on_both_sides_of_the_wide_base(lla, at, shares):
+    """fp32 logits around +-65536, where terms change their form: tiles of a row, and threads of a tile, on either side."""
+    B, V = (640, 40000) if shares == "one" else (12, 90000)
+    g = torch.Generator(device=DEV).manual_seed(13)
+    step = 2.0 ** -7
+    z = at + torch.round(torch.randn(B, 1, V, generator=g, device=DEV) * 0.7 / step) * step
+    # rows by kind: as they are; the first half 3 below; the second half 3 below; one logit far over; one side only
+    z[1::5, :, :V // 2] -= 3
+    z[2::5, :, V // 2:] -= 3
+    z[3::5, :, V - 7] = at + 9
+    z[4::5] = torch.where(z[4::5] > at, at - (z[4::5] - at), z[4::5])
+    if shares == "one":
+        check_some(lla, z, ONE_BY_ONE, 3)
+    else:
+        check(lla, z, ONE_BY_ONE, 3)
 
 
 def test_a_beam_s_score_whatever_the_batch(lla):
