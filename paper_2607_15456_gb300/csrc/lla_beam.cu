@@ -752,9 +752,10 @@ __global__ void __launch_bounds__(kFinishThreads) beam_finish_kernel(const __gri
     const int parts = max(1, min(4, min(a.shares, kFinishWarps / W)));
     const int at_once = kFinishWarps / parts;
     // A warp's fp64 instruction holds the SM's one fp64 unit for about 20 cycles, whatever its lanes do: a few beams'
-    // logarithms are taken by their warps beside the merges (0.2 us less with 4 beams), those of many by one warp behind
-    // them (3.4 us less with 16).
-    const bool logs_here = W <= 4;
+    // logarithms are taken by their warps beside the merges, those of many by one warp behind them.  One sequence of 32000
+    // tokens, K = W, beside and behind: W = 2 7.06 and 7.17 us, 4 8.1 and 8.3, 8 8.9 and 9.1, 10 alike, 12 10.2 and 10.1, 16 11.2 and
+    // 11.0, 32 16.4 and 15.3 (eight sequences: the same order, 20.8 and 19.8 with 32).
+    const bool logs_here = W < 10;
     for (int w0 = 0; w0 < W; w0 += at_once) {
         const int w = w0 + warp / parts, p = warp % parts;
         const bool mine = warp / parts < at_once && w < W;
