@@ -642,9 +642,9 @@ lla_status lla_beam_select(int32_t B, int32_t W, int32_t V, int32_t K, const voi
  * `stream` and sets *logits (and *row_stride, preset to V) to the B W rows of its logits.  The beams' new
  * tokens are `tokens`; pass 1 of the decode attends to lens_before[s] cached tokens of pages->block_table,
  * the encode takes `slots`, and after it pages->context_lens[s] tokens are cached.  A beam that is finished or dead
- * (below) has slot -1 and as many tokens as before; its logits are not looked at.  Behind step 0 (whose tokens are slab
- * 0) every token is one of the vocabulary: 0 where the slab holds -1.  Returns LLA_OK, or
- * another status to stop the search (lla_beam_search then returns it).
+ * (below) has slot -1 and as many tokens as before; its logits are not used.  Behind step 0 (whose tokens are slab 0)
+ * every token is one of the vocabulary: 0 where the slab holds -1.  Returns LLA_OK, or another status to stop the
+ * search (lla_beam_search then returns it).
  */
 typedef lla_status (*lla_step_fn)(int32_t step, const lla_pages *pages, const int32_t *lens_before,
                                   const int32_t *tokens, const int64_t *slots, const void **logits,
@@ -658,11 +658,12 @@ lla_status lla_beam_search_workspace_size(int32_t B, int32_t W, int32_t V, lla_d
  * Beam search of B sequences with W beams each over `steps` steps: host orchestration of this library's
  * kernels on `stream`.  Step i is lla_pages_extend by one token (finished beams do not grow), the caller's
  * model, lla_beam_select with K = W, lla_pages_fork by its parents.  Where a sequence has fewer than W continuations
- * (masked logits), the beams behind them are dead: parent and token -1, score -inf, finished, length 0 in the slabs.  A
- * beam whose token finds no room (LLA_DEVERR_PAGES, _CONTEXT or _BLOCK_ID of lla_pages_extend) has no continuation, so no
- * hypothesis goes on with a hole; the ended ones stay, and the parents of that step hold -1 for the others.  A
- * dead beam keeps the pages that the same beam had before the selection, so that the model meets no empty sequence, and is
- * replaced as soon as its sequence has enough continuations again.
+ * (masked logits), the beams behind them are dead: parent and token -1, score -inf, finished, length 0 in the slabs.
+ * A dead beam keeps the pages that the same beam had before the selection, so that the model meets no empty sequence,
+ * and is replaced as soon as its sequence has enough continuations again.  A beam whose token finds no room
+ * (LLA_DEVERR_CONTEXT or _BLOCK_ID of lla_pages_extend; after LLA_DEVERR_PAGES that is every beam that has not ended) has
+ * no continuation, so no hypothesis goes on with a hole; the ended ones stay, and the parents of that step hold -1 for
+ * the others.
  *   pages_a, pages_b  two page sets as lla_pages_fork takes them, S = B W; sequence b W + w is beam w of
  *                     sequence b.  Step i runs on pages_a where i is even, on pages_b where it is odd;
  *                     before the call pages_a holds the prompts without their last token (a fork of every

@@ -12,12 +12,13 @@
 //   beam_finish_kernel a CTA per sequence: merges the shares of each beam, takes the logarithm, forms the keys in 64
 //                      bits, and merges the W sorted lists.
 //
-// Bound by HBM for large batches: 64 x 16 beams of 131072 bf16 logits (268 MB, 39.6 us at the copy rate) take 56 us.
-// A second 268 MB on top takes 36.5 us, so tiles go by at the rate of HBM; the rest is the start of the two waves of rows (a
-// first tile, its threshold: about 3 us each, 5 % of a wave for each look at the candidates) and the second kernel (4 us).
+// Bound by HBM for large batches: 64 x 16 beams of 131072 bf16 logits (268 MB, 39.6 us at the copy rate) take 56.5 us.
+// A second 268 MB on top takes 36.7 us, so tiles go by at the rate of HBM; the rest is the start of the two waves of rows (a
+// first tile, its threshold: about 3 us each, 5 % of a wave for each look at the candidates), of which the second fills 416 of
+// the 608 CTA slots, and the second kernel (4 us).
 // Rows cut evenly over resident CTAs took 77 us against 66 then: every piece of a row pays a start.  Three stages and
 // three CTAs an SM, four more registers, or candidates found in registers (spills) lost 2 to 20 %.  Small batches are
-// bound by the chain of the two launches: 4 beams of 32000 logits take 8.4 us, of which the host call is 4.
+// bound by the chain of the two launches: 4 beams of 32000 logits take 8.7 us, of which the host call is 4.
 //
 // Precision.  Ranks are compared in 64 bits, so what matters is log S, which the candidates of a beam share: it
 // decides between beams.  A term 2^(z K - c), K the fp32 number next to log2 e, takes one rounding of its exponent: 2^-24 |z - b|
