@@ -263,3 +263,60 @@ def test_in_pieces(lla):
     assert torch.equal(whole.ref, two.ref) and torch.equal(whole.last().context_lens, two.last().context_lens)
     two.check_ledger()
     assert whole.finished.any()
+
+
+def test_captured_and_replayed(lla):
+    """A whole search with dead beams in a CUDA graph, replayed on other prompts and scores: what the same calls give outside."""
+    B, W, V, steps = 2, 4, 60, 8
+    table = torch.randn(V, V, generator=torch.Generator(device=DEV).manual_seed(8), device=DEV)
+    table[:, 5:50][table[:, 5:50] < 1.2] = -math.inf  # few continuations a token
+
+    def step(i, pages, before, toks, slots):
+        return table[toks.long()].masked_fill(torch.arange(V, device=DEV) > (2 if i < 1 else V), -math.inf)
+
+    def fresh():
+        return Search(lla, B, W, V, steps, blocks=40).prompt([70, 3])
+
+    def start(s, like, first):
+        for a, b in zip([s.ref, s.pages[0].block_table, s.pages[0].context_lens], [like.ref, like.pages[0].block_table, like.pages[0].context_lens]):
+            a.copy_(b)
+        s.tokens[0] = first
+
+    begin, s, plain = fresh(), fresh(), fresh()
+    s.run(step, eos=9)  # once outside
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        s.run(step, eos=9, stream=side)
+    for first in (0, 17, 44):
+        start(s, begin, first)
+        graph.replay()
+        start(plain, begin, first)
+        plain.run(step, eos=9)
+        torch.cuda.synchronize()
+        for name in ("tokens", "parents", "scores", "finished", "lengths", "ref"):
+            assert torch.equal(getattr(s, name), getattr(plain, name)), (first, name)
+        assert torch.equal(s.last().block_table, plain.last().block_table) and torch.equal(s.last().context_lens, plain.last().context_lens)
+        s.check_ledger()
+    assert (s.parents < 0).any() and lla.lla_get_device_error() == 0
+
+
+def test_the_largest_batch(lla):
+    """32 sequences of 32 beams, all but a few dead at first."""
+    B, W, V, steps = 32, 32, 300, 4
+    s = Search(lla, B, W, V, steps, blocks=4096).prompt([40 + 3 * b for b in range(B)])
+    allowed = lambda i: [list(range(1 + b % 7)) if i < 2 else list(range(V)) for b in range(B)]
+    seen = []
+
+    def step(i, pages, before, toks, slots):
+        seen.append((toks.clone(), pages.context_lens.clone()))
+        return masked(s, i, allowed(i))
+
+    s.run(step)
+    alive = [(s.parents[i] >= 0).sum(1).tolist() for i in range(steps)]
+    assert alive[0] == [min(W, 1 + b % 7) for b in range(B)]
+    assert alive[1] == [min(W, (1 + b % 7) ** 2) for b in range(B)]
+    assert alive[2] == alive[3] == [W] * B
+    assert all((t >= 0).all() and (t < V).all() and (n > 0).all() for t, n in seen)
+    s.check_ledger()
