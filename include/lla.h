@@ -28,6 +28,13 @@
  *                        sequences that share pages of any of these caches: forked and reordered,
  *                        grown (copying a shared last page before it is written), freed, moved
  *                        to the front of the pools
+ *   lla_pages_admit      requests that start on a kept part of another sequence: their rows, lengths,
+ *                        copied rows and slots
+ *   lla_prefix_plan, lla_decode_attn_prefix, lla_decode_attn_prefix_decoupled
+ *                        which sequences share which pages, and decodes that read a shared page once
+ *                        for up to 64 of them
+ *   lla_encode_rope_keys_axes, lla_decode_attn_decoupled_axes
+ *                        the rotary branch with positions on up to three axes (images, video)
  *   lla_beam_select, lla_beam_search
  *                        the best continuations of the beams over the vocabulary, and the beam
  *                        search loop over the calls above
@@ -392,6 +399,44 @@ lla_status lla_decode_attn_decoupled(const lla_geometry *g, const lla_codec *cod
                                      size_t workspace_bytes, void *stream);
 
 /*
+ * Rotary positions on up to three axes (time, height and width of images and video): every token has a
+ * position on each axis, and pair j of the rotary branch is turned by
+ *   positions[axis(j)] * base^(-2j/d_rope).
+ * A text token has one position on all axes.  pairs[a] >= 0 is the number of pairs of axis a; their sum must be
+ * d_rope / 2.
+ */
+#define LLA_ROPE_AXES 3
+
+typedef enum {
+    LLA_AXES_BLOCKS = 0,      /* the first pairs[0] pairs turn with axis 0, the next pairs[1] with axis 1, the rest with axis 2 */
+    LLA_AXES_INTERLEAVED = 1  /* axis(j) = j % 3 where j / 3 < pairs[j % 3], else 0 */
+} lla_axes_order;
+
+typedef struct {
+    double base;              /* rotation base, > 1 */
+    lla_rope_pairing pairing; /* which two of the d_rope values are pair j */
+    int32_t pairs[LLA_ROPE_AXES];
+    lla_axes_order order;
+} lla_rope_axes;
+
+/* lla_encode_rope_keys with positions device [3][N] int32, one row per axis (a token with a negative one sets
+ * LLA_DEVERR_CONTEXT and is skipped). */
+lla_status lla_encode_rope_keys_axes(int32_t d_rope, const lla_rope_axes *rope, void *rope_pool, int64_t num_blocks,
+                                     const void *k_rope, lla_dtype x_dtype, const int32_t *positions,
+                                     const int64_t *slot_mapping, int32_t N, void *stream);
+
+/* lla_decode_attn_decoupled with rotary keys written by lla_encode_rope_keys_axes: the rotary query of sequence b, and in
+ * pass 1 its current rotary key, stand at positions device [3][B] int32 instead of at the context length (a negative
+ * one sets LLA_DEVERR_CONTEXT and counts as 0).  The same workspace. */
+lla_status lla_decode_attn_decoupled_axes(const lla_geometry *g, const lla_codec *codec, const lla_cache *cache,
+                                          const void *rope_pool, int32_t d_rope, const lla_rope_axes *rope,
+                                          const int32_t *positions, const int32_t *context_lens, int32_t B,
+                                          int32_t max_ctx, int32_t loop, const void *q, const void *q_rope,
+                                          const void *cur_k, const void *cur_v, const void *cur_k_rope,
+                                          lla_dtype io_dtype, void *out, void *workspace, size_t workspace_bytes,
+                                          void *stream);
+
+/*
  * lla_decode_attn for callers that cannot allocate device memory (for example a plug-in inside a
  * host application that owns all device memory and offers it no allocator, or a latency-critical
  * loop that cannot afford cudaMalloc's device-wide synchronisation).  Same arguments and result
@@ -594,6 +639,102 @@ lla_status lla_pages_compact_workspace_size(int64_t num_blocks, size_t *bytes);
  */
 lla_status lla_pages_compact(const lla_pages *pages, const lla_pool *pools, int32_t L, int32_t *remap,
                              int32_t *live, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Requests that start from a part of another sequence (a common system prompt, the next turn of a conversation, samples
+ * of a prompt that goes on serving): request i becomes sequence rows[i], which must be empty, of length new_lens[i].  Its
+ * first keep[i] tokens are those of sequence parents[i] (-1: of none, then keep[i] is 0), which keeps them: the
+ * keep / 64 full pages are shared, the keep % 64 rows of the next one are copied in every pool into a block of its own,
+ * and the rest are fresh blocks, all of them the free ones of the lowest numbers in the order of the requests.
+ * The block tables, lengths and slots that the encodes and prefills of the new tokens take come out on the device, so
+ * that admission needs no round trip to the host.
+ *   rows, parents, keep, new_lens
+ *                 device [n] int32; 0 <= keep[i] <= context_lens[parents[i]], keep[i] <= new_lens[i]
+ *   slot_mapping  device [N] int64, written: the slots of the requests' new tokens, packed; -1 behind cu_new[n]
+ *   cu_new        device [n + 1] int32, written: prefix sums of the new tokens (new_lens[i] - keep[i], or 0 where request i
+ *                 is not admitted)
+ *   admitted      device [n] uint8, written: 1 where the request got its row
+ *   free_blocks   device int32 or NULL, written: the free blocks that remain
+ *   pools, L      as lla_pages_extend
+ * Requests are admitted in order as long as the free blocks and the N slots suffice: the first that finds no room and all
+ * behind it are not, and their rows stay empty (no error).  A request whose row or parent is outside the batch, or whose
+ * row an earlier request names, sets LLA_DEVERR_SEQUENCE; one whose row is not empty, or whose lengths are out of
+ * range, LLA_DEVERR_CONTEXT; one whose page to copy is no block, LLA_DEVERR_BLOCK_ID: it is not admitted and takes nothing.
+ * A request's row may be another's parent only in so far as it is empty.  0 <= n <= LLA_MAX_BATCH.
+ * Two kernels on the stream; the workspace as for lla_pages_extend.
+ */
+lla_status lla_pages_admit_workspace_size(int32_t n, size_t *bytes);
+lla_status lla_pages_admit(const lla_pages *pages, const lla_pool *pools, int32_t L, const int32_t *rows,
+                           const int32_t *parents, const int32_t *keep, const int32_t *new_lens, int32_t n,
+                           int64_t *slot_mapping, int32_t N, int32_t *cu_new, uint8_t *admitted, int32_t *free_blocks,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Which sequences share which pages.  A level is a partition of the batch: at first all sequences are one set.  The
+ * sequences of a set that have the same block in the set's next full page form a set of their own, whose pages go on as
+ * long as all of them have them full and agree (the set's leader is its lowest sequence).  One of two sequences and
+ * min_pages pages at least becomes groups of at most LLA_PREFIX_MEMBERS members, evenly; the others end there.  Three
+ * levels hold a system prompt, a document and a conversation's branches; what lies behind is a sequence's own.
+ * Groups are in the order of levels, within a level of leaders, members in the order of sequence numbers: a function of the
+ * tables alone.
+ */
+#define LLA_PREFIX_LEVELS 3
+#define LLA_PREFIX_MEMBERS 64
+
+typedef struct {
+    int32_t *num_groups; /* device int32 */
+    int32_t *groups;     /* device [3 max(1, B / 2)][4], 16-byte aligned: first page, page behind the last, first member's
+                            index in `members`, members; zeros behind the last group */
+    int32_t *members;    /* device [3 B]: sequence numbers, group by group; -1 behind the last */
+    int32_t *column;     /* device [3][B]: group * LLA_PREFIX_MEMBERS + rank of each sequence at each level, or -1 */
+    int32_t *own_page;   /* device [B]: first page that a sequence reads alone */
+} lla_prefix;
+
+/*
+ * Fills `plan` for B sequences of `cache` (its block table and num_blocks; the pool is not read and may be NULL).  A plan
+ * holds as long as the pages it names stay in the rows it was made from: tokens may be appended, so it has to be made again
+ * only when sequences come, go or move (and should be when many pages more could be shared).
+ *   min_pages  pages that a set must share to become a group, >= 1
+ * A length out of range sets LLA_DEVERR_CONTEXT, a shared page that is no block LLA_DEVERR_BLOCK_ID: such a sequence
+ * shares nothing (from that page on).  One kernel on the stream.
+ */
+lla_status lla_prefix_plan(const lla_cache *cache, const int32_t *context_lens, int32_t B, int32_t max_ctx,
+                           int32_t min_pages, const lla_prefix *plan, void *stream);
+
+/* Workspace bytes of lla_decode_attn_prefix (d_rope = 0) and lla_decode_attn_prefix_decoupled for B sequences on the
+ * current device (LLA_ERR_UNSUPPORTED for a shape with no kernel). */
+lla_status lla_decode_prefix_workspace_size(const lla_geometry *g, int32_t d_rope, int32_t B, size_t *bytes);
+
+/*
+ * lla_decode_attn for a batch whose sequences share pages: a page of a group is read once for all of its members, whose
+ * queries meet it on the tensor cores, and the softmax states of a sequence's groups and of its own pages are joined,
+ *   o = sum_j 2^(m_j - M) o_j / sum_j 2^(m_j - M) l_j,  M = max_j m_j.
+ *   plan       of lla_prefix_plan for these rows.  What a plan names outside the tables sets LLA_DEVERR_SEQUENCE or
+ *              LLA_DEVERR_CONTEXT and is not read
+ *   workspace  >= lla_decode_prefix_workspace_size bytes, 16-byte aligned; needs no initialisation; calls that share it must
+ *              be ordered
+ * Other arguments and the error behaviour are those of lla_decode_attn.  Storage LLA_BF16, d = 128, (r_k, r_v) one of
+ * (96, 160), (128, 128), (72, 120); LLA_ERR_UNSUPPORTED otherwise.  q~ enters the products as the sum of three bf16 numbers,
+ * the softmax weights as two: 24 and 16 bits.  Three kernels on the stream.
+ */
+lla_status lla_decode_attn_prefix(const lla_geometry *g, const lla_codec *codec, const lla_cache *cache,
+                                  const lla_prefix *plan, const int32_t *context_lens, int32_t B, int32_t max_ctx,
+                                  int32_t loop, const void *q, const void *cur_k, const void *cur_v, lla_dtype io_dtype,
+                                  void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The same for a cache with a rotary branch (lla_decode_attn_decoupled).
+ *   positions  device [3][B] int32 as lla_decode_attn_decoupled_axes, or NULL: the current token stands on every axis at its
+ *              index in the sequence, as in lla_decode_attn_decoupled
+ * (r_k, r_v) = (96, 160), d_rope 32, 64 or 96.
+ */
+lla_status lla_decode_attn_prefix_decoupled(const lla_geometry *g, const lla_codec *codec, const lla_cache *cache,
+                                            const lla_prefix *plan, const void *rope_pool, int32_t d_rope,
+                                            const lla_rope_axes *rope, const int32_t *positions,
+                                            const int32_t *context_lens, int32_t B, int32_t max_ctx, int32_t loop,
+                                            const void *q, const void *q_rope, const void *cur_k, const void *cur_v,
+                                            const void *cur_k_rope, lla_dtype io_dtype, void *out, void *workspace,
+                                            size_t workspace_bytes, void *stream);
 
 #define LLA_MAX_BEAMS 32
 #define LLA_MAX_VOCAB (1 << 24)

@@ -406,22 +406,94 @@ lla_status lla_rope_plane_bytes(int32_t d_rope, size_t *bytes) {
 }
 
 namespace {
+bool overlap(const void *a, size_t na, const void *b, size_t nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return na > 0 && nb > 0 && x < y + nb && y < x + na;
+}
+
+struct Span {
+    const void *p;
+    size_t bytes;
+};
+// Whether one of `written` overlaps another of them or one of `read` (absent arrays overlap nothing).
+bool any_overlap(std::initializer_list<Span> written, std::initializer_list<Span> read) {
+    for (const Span *o = written.begin(); o != written.end(); ++o) {
+        if (!o->p) continue;
+        for (const Span *i = o + 1; i != written.end(); ++i)
+            if (i->p && overlap(o->p, o->bytes, i->p, i->bytes)) return true;
+        for (const Span &i : read)
+            if (i.p && overlap(o->p, o->bytes, i.p, i.bytes)) return true;
+    }
+    return false;
+}
+
 bool valid_rope(const lla_rope *rope) {
     return rope && rope->base > 1.0 && rope->base < 1e300 &&
            (rope->pairing == LLA_ROPE_HALF || rope->pairing == LLA_ROPE_ADJACENT);
 }
+
+// The rotation of one position per token.
+RotaryAxes one_axis(const lla_rope &r) {
+    RotaryAxes o = {};
+    o.base = r.base;
+    o.pairing = r.pairing == LLA_ROPE_ADJACENT ? 1 : 0;
+    o.axes = 1;
+    return o;
+}
+
+// The rotation of three positions per token; false where it is no rotation of d_rope (a valid d_rope) values.
+bool rotary_axes(const lla_rope_axes *r, int d_rope, RotaryAxes *o) {
+    if (!r || !(r->base > 1.0) || !(r->base < 1e300)) return false;
+    if (r->pairing != LLA_ROPE_HALF && r->pairing != LLA_ROPE_ADJACENT) return false;
+    if (r->order != LLA_AXES_BLOCKS && r->order != LLA_AXES_INTERLEAVED) return false;
+    int64_t sum = 0;
+    for (int a = 0; a < LLA_ROPE_AXES; ++a) {
+        if (r->pairs[a] < 0) return false;
+        sum += r->pairs[a];
+    }
+    if (sum != d_rope / 2) return false;
+    *o = RotaryAxes{};
+    o->base = r->base;
+    o->pairing = r->pairing == LLA_ROPE_ADJACENT ? 1 : 0;
+    o->axes = LLA_ROPE_AXES;
+    for (int j = 0; j < d_rope / 2; ++j) {
+        int a;
+        if (r->order == LLA_AXES_BLOCKS) a = j < r->pairs[0] ? 0 : j < r->pairs[0] + r->pairs[1] ? 1 : 2;
+        else a = j / 3 < r->pairs[j % 3] ? j % 3 : 0;
+        o->axis[j] = static_cast<uint8_t>(a);
+    }
+    return true;
+}
+
+bool valid_d_rope(int d_rope) { return d_rope >= 16 && d_rope <= 96 && d_rope % 16 == 0; }
+}  // namespace
+
+namespace {
+
+lla_status store_rope_keys(int32_t d_rope, const RotaryAxes &rope, void *rope_pool, int64_t num_blocks, const void *k_rope,
+                           lla_dtype x_dtype, const int32_t *positions, const int64_t *slot_mapping, int32_t N, void *stream) {
+    if (!rope_pool || num_blocks < 1 || !aligned(rope_pool, 16) || !valid_dtype(x_dtype) || N < 0)
+        return LLA_ERR_INVALID_ARG;
+    if (N > 0 && (!k_rope || !positions || !slot_mapping)) return LLA_ERR_INVALID_ARG;
+    return launch_rope_key_store(d_rope, rope, rope_pool, num_blocks, k_rope, x_dtype == LLA_BF16, positions, slot_mapping, N,
+                                 static_cast<cudaStream_t>(stream));
+}
+
 }  // namespace
 
 lla_status lla_encode_rope_keys(int32_t d_rope, const lla_rope *rope, void *rope_pool, int64_t num_blocks,
                                 const void *k_rope, lla_dtype x_dtype, const int32_t *positions,
                                 const int64_t *slot_mapping, int32_t N, void *stream) {
-    if (d_rope < 16 || d_rope > 96 || d_rope % 16 != 0 || !valid_rope(rope)) return LLA_ERR_INVALID_ARG;
-    if (!rope_pool || num_blocks < 1 || !aligned(rope_pool, 16) || !valid_dtype(x_dtype) || N < 0)
-        return LLA_ERR_INVALID_ARG;
-    if (N > 0 && (!k_rope || !positions || !slot_mapping)) return LLA_ERR_INVALID_ARG;
-    return launch_rope_key_store(d_rope, rope->base, rope->pairing == LLA_ROPE_ADJACENT ? 1 : 0, rope_pool,
-                                 num_blocks, k_rope, x_dtype == LLA_BF16, positions, slot_mapping, N,
-                                 static_cast<cudaStream_t>(stream));
+    if (!valid_d_rope(d_rope) || !valid_rope(rope)) return LLA_ERR_INVALID_ARG;
+    return store_rope_keys(d_rope, one_axis(*rope), rope_pool, num_blocks, k_rope, x_dtype, positions, slot_mapping, N, stream);
+}
+
+lla_status lla_encode_rope_keys_axes(int32_t d_rope, const lla_rope_axes *rope, void *rope_pool, int64_t num_blocks,
+                                     const void *k_rope, lla_dtype x_dtype, const int32_t *positions,
+                                     const int64_t *slot_mapping, int32_t N, void *stream) {
+    RotaryAxes axes;
+    if (!valid_d_rope(d_rope) || !rotary_axes(rope, d_rope, &axes)) return LLA_ERR_INVALID_ARG;
+    return store_rope_keys(d_rope, axes, rope_pool, num_blocks, k_rope, x_dtype, positions, slot_mapping, N, stream);
 }
 
 lla_status lla_decode_decoupled_workspace_size(const lla_geometry *g, int32_t d_rope, int32_t B,
@@ -437,30 +509,35 @@ lla_status lla_decode_decoupled_workspace_size(const lla_geometry *g, int32_t d_
     return LLA_OK;
 }
 
-lla_status lla_decode_attn_decoupled(const lla_geometry *g, const lla_codec *codec, const lla_cache *cache,
-                                     const void *rope_pool, int32_t d_rope, const lla_rope *rope,
-                                     const int32_t *context_lens, int32_t B, int32_t max_ctx, int32_t loop,
-                                     const void *q, const void *q_rope, const void *cur_k, const void *cur_v,
-                                     const void *cur_k_rope, lla_dtype io_dtype, void *out, void *workspace,
-                                     size_t workspace_bytes, void *stream) {
+namespace {
+
+// The decodes of an absorbed per-head cache with or without a rotary branch: `rope_pool` NULL without one, `plan` where
+// sequences share pages.
+lla_status decode_branch(const lla_geometry *g, const lla_codec *codec, const lla_cache *cache, const lla_prefix *plan,
+                         const void *rope_pool, int32_t d_rope, const RotaryAxes &rope, const int32_t *positions,
+                         const int32_t *context_lens, int32_t B, int32_t max_ctx, int32_t loop, const void *q,
+                         const void *q_rope, const void *cur_k, const void *cur_v, const void *cur_k_rope,
+                         lla_dtype io_dtype, void *out, void *workspace, size_t workspace_bytes, void *stream) {
     lla_status st = check_geometry(g);
     if (st != LLA_OK) return st;
     if ((st = check_cache(cache, true)) != LLA_OK) return st;
     if (!codec || !codec->w_up_k || !codec->w_up_v) return LLA_ERR_INVALID_ARG;
     if (!aligned(codec->w_up_k, 16) || !aligned(codec->w_up_v, 16)) return LLA_ERR_INVALID_ARG;
     if (loop < 0 || loop >= g->T) return LLA_ERR_INVALID_ARG;
-    if (!valid_rope(rope) || !rope_pool || !aligned(rope_pool, 16)) return LLA_ERR_INVALID_ARG;
+    if (d_rope > 0 && (!rope_pool || !aligned(rope_pool, 16))) return LLA_ERR_INVALID_ARG;
     if (B < 0 || B > LLA_MAX_BATCH || !valid_dtype(io_dtype)) return LLA_ERR_INVALID_ARG;
     if (max_ctx < 0 || static_cast<int64_t>(max_ctx) >
                            static_cast<int64_t>(cache->max_blocks_per_seq) * LLA_BLOCK_TOKENS)
         return LLA_ERR_INVALID_ARG;
-    if ((cur_k == nullptr) != (cur_v == nullptr) || (cur_k == nullptr) != (cur_k_rope == nullptr))
-        return LLA_ERR_INVALID_ARG;
-    if (B > 0 && (!context_lens || !q || !q_rope || !out)) return LLA_ERR_INVALID_ARG;
-    if (!decode_decoupled_supported(elem_size(g->storage), g->d, g->H, g->r_k, g->r_v, d_rope))
+    if ((cur_k == nullptr) != (cur_v == nullptr)) return LLA_ERR_INVALID_ARG;
+    if (d_rope > 0 && (cur_k == nullptr) != (cur_k_rope == nullptr)) return LLA_ERR_INVALID_ARG;
+    if (B > 0 && (!context_lens || !q || (d_rope > 0 && !q_rope) || !out)) return LLA_ERR_INVALID_ARG;
+    if (plan ? !decode_prefix_supported(elem_size(g->storage), g->d, g->r_k, g->r_v, d_rope)
+             : !decode_decoupled_supported(elem_size(g->storage), g->d, g->H, g->r_k, g->r_v, d_rope))
         return LLA_ERR_UNSUPPORTED;
-    // the pages of every (sequence, head) are counted in 32 bits inside the kernels
-    if (static_cast<int64_t>(B) * g->H *
+    // the pages of every (sequence, head) are counted in 32 bits inside the kernels, those of a plan's groups (at most as
+    // many again on each level) too
+    if (static_cast<int64_t>(B) * g->H * (plan ? 1 + LLA_PREFIX_LEVELS : 1) *
             ((static_cast<int64_t>(max_ctx) + LLA_BLOCK_TOKENS - 1) / LLA_BLOCK_TOKENS) >= (int64_t(1) << 31))
         return LLA_ERR_UNSUPPORTED;
     if (B == 0) return LLA_OK;
@@ -479,8 +556,99 @@ lla_status lla_decode_attn_decoupled(const lla_geometry *g, const lla_codec *cod
     a.context_lens = context_lens; a.B = B; a.max_ctx = max_ctx;
     a.q = q; a.cur_k = cur_k; a.cur_v = cur_v; a.out = out;
     a.workspace = workspace; a.workspace_bytes = workspace_bytes;
-    return launch_decode_decoupled(a, rope_pool, d_rope, rope->base, rope->pairing == LLA_ROPE_ADJACENT ? 1 : 0,
-                                   q_rope, cur_k_rope, static_cast<cudaStream_t>(stream));
+    const cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    if (plan) return launch_decode_prefix(a, *plan, rope_pool, d_rope, rope, positions, q_rope, cur_k_rope, cs);
+    return launch_decode_decoupled(a, rope_pool, d_rope, rope, positions, q_rope, cur_k_rope, cs);
+}
+
+// The arrays of a plan are there (the members' and the sequences' where there is a batch).
+bool valid_prefix(const lla_prefix *p, int32_t B) {
+    if (!p || !p->num_groups || !p->groups || !aligned(p->groups, 16)) return false;
+    return B <= 0 || (p->members && p->column && p->own_page);
+}
+
+}  // namespace
+
+lla_status lla_decode_attn_decoupled(const lla_geometry *g, const lla_codec *codec, const lla_cache *cache,
+                                     const void *rope_pool, int32_t d_rope, const lla_rope *rope,
+                                     const int32_t *context_lens, int32_t B, int32_t max_ctx, int32_t loop,
+                                     const void *q, const void *q_rope, const void *cur_k, const void *cur_v,
+                                     const void *cur_k_rope, lla_dtype io_dtype, void *out, void *workspace,
+                                     size_t workspace_bytes, void *stream) {
+    const lla_status st = check_geometry(g);
+    if (st != LLA_OK) return st;
+    if (!valid_rope(rope) || !rope_pool) return LLA_ERR_INVALID_ARG;
+    return decode_branch(g, codec, cache, nullptr, rope_pool, d_rope, one_axis(*rope), nullptr, context_lens, B, max_ctx, loop, q,
+                         q_rope, cur_k, cur_v, cur_k_rope, io_dtype, out, workspace, workspace_bytes, stream);
+}
+
+lla_status lla_decode_attn_decoupled_axes(const lla_geometry *g, const lla_codec *codec, const lla_cache *cache,
+                                          const void *rope_pool, int32_t d_rope, const lla_rope_axes *rope,
+                                          const int32_t *positions, const int32_t *context_lens, int32_t B,
+                                          int32_t max_ctx, int32_t loop, const void *q, const void *q_rope,
+                                          const void *cur_k, const void *cur_v, const void *cur_k_rope,
+                                          lla_dtype io_dtype, void *out, void *workspace, size_t workspace_bytes,
+                                          void *stream) {
+    const lla_status st = check_geometry(g);
+    if (st != LLA_OK) return st;
+    RotaryAxes axes;
+    if (!valid_d_rope(d_rope) || !rotary_axes(rope, d_rope, &axes) || !rope_pool || (B > 0 && !positions))
+        return LLA_ERR_INVALID_ARG;
+    return decode_branch(g, codec, cache, nullptr, rope_pool, d_rope, axes, positions, context_lens, B, max_ctx, loop, q, q_rope,
+                         cur_k, cur_v, cur_k_rope, io_dtype, out, workspace, workspace_bytes, stream);
+}
+
+lla_status lla_prefix_plan(const lla_cache *cache, const int32_t *context_lens, int32_t B, int32_t max_ctx,
+                           int32_t min_pages, const lla_prefix *plan, void *stream) {
+    if (!cache || cache->num_blocks < 1 || !cache->block_table || cache->max_blocks_per_seq < 1) return LLA_ERR_INVALID_ARG;
+    if (cache->num_blocks > LLA_MAX_BLOCKS || cache->max_blocks_per_seq > LLA_MAX_BLOCKS) return LLA_ERR_UNSUPPORTED;
+    if (B < 0 || B > LLA_MAX_BATCH || min_pages < 1 || !valid_prefix(plan, B)) return LLA_ERR_INVALID_ARG;
+    if (max_ctx < 0 || static_cast<int64_t>(max_ctx) >
+                           static_cast<int64_t>(cache->max_blocks_per_seq) * LLA_BLOCK_TOKENS)
+        return LLA_ERR_INVALID_ARG;
+    if (B > 0 && !context_lens) return LLA_ERR_INVALID_ARG;
+    const size_t each = static_cast<size_t>(B) * 4;
+    const size_t rows = LLA_PREFIX_LEVELS * static_cast<size_t>(B / 2 > 1 ? B / 2 : 1);
+    if (any_overlap({{plan->num_groups, 4}, {plan->groups, rows * 16}, {plan->members, LLA_PREFIX_LEVELS * each},
+                     {plan->column, LLA_PREFIX_LEVELS * each}, {plan->own_page, each}},
+                    {{cache->block_table, each * cache->max_blocks_per_seq}, {context_lens, each}}))
+        return LLA_ERR_INVALID_ARG;
+    return launch_prefix_plan(cache->block_table, cache->num_blocks, cache->max_blocks_per_seq, context_lens, B, max_ctx, min_pages,
+                              *plan, static_cast<cudaStream_t>(stream));
+}
+
+lla_status lla_decode_prefix_workspace_size(const lla_geometry *g, int32_t d_rope, int32_t B, size_t *bytes) {
+    const lla_status st = check_geometry(g);
+    if (st != LLA_OK) return st;
+    if (!bytes || B < 0 || B > LLA_MAX_BATCH) return LLA_ERR_INVALID_ARG;
+    if (!decode_prefix_supported(elem_size(g->storage), g->d, g->r_k, g->r_v, d_rope)) return LLA_ERR_UNSUPPORTED;
+    const size_t n = decode_prefix_workspace_bytes(g->r_k, g->r_v, d_rope, B, g->H);
+    if (n == 0) return LLA_ERR_CUDA;
+    *bytes = n;
+    return LLA_OK;
+}
+
+lla_status lla_decode_attn_prefix(const lla_geometry *g, const lla_codec *codec, const lla_cache *cache,
+                                  const lla_prefix *plan, const int32_t *context_lens, int32_t B, int32_t max_ctx,
+                                  int32_t loop, const void *q, const void *cur_k, const void *cur_v, lla_dtype io_dtype,
+                                  void *out, void *workspace, size_t workspace_bytes, void *stream) {
+    if (!valid_prefix(plan, B) || (workspace && !aligned(workspace, 16))) return LLA_ERR_INVALID_ARG;
+    return decode_branch(g, codec, cache, plan, nullptr, 0, RotaryAxes{}, nullptr, context_lens, B, max_ctx, loop, q, nullptr, cur_k,
+                         cur_v, nullptr, io_dtype, out, workspace, workspace_bytes, stream);
+}
+
+lla_status lla_decode_attn_prefix_decoupled(const lla_geometry *g, const lla_codec *codec, const lla_cache *cache,
+                                            const lla_prefix *plan, const void *rope_pool, int32_t d_rope,
+                                            const lla_rope_axes *rope, const int32_t *positions,
+                                            const int32_t *context_lens, int32_t B, int32_t max_ctx, int32_t loop,
+                                            const void *q, const void *q_rope, const void *cur_k, const void *cur_v,
+                                            const void *cur_k_rope, lla_dtype io_dtype, void *out, void *workspace,
+                                            size_t workspace_bytes, void *stream) {
+    RotaryAxes axes;
+    if (!valid_prefix(plan, B) || (workspace && !aligned(workspace, 16))) return LLA_ERR_INVALID_ARG;
+    if (!valid_d_rope(d_rope) || !rotary_axes(rope, d_rope, &axes)) return LLA_ERR_INVALID_ARG;
+    return decode_branch(g, codec, cache, plan, rope_pool, d_rope, axes, positions, context_lens, B, max_ctx, loop, q, q_rope, cur_k,
+                         cur_v, cur_k_rope, io_dtype, out, workspace, workspace_bytes, stream);
 }
 
 lla_status lla_dense_decode_attn(const lla_geometry *g, const lla_cache *cache,
@@ -592,27 +760,6 @@ lla_status lla_prefill_attn_rope(const lla_geometry *g, const lla_codec *codec,
 
 namespace {
 
-bool overlap(const void *a, size_t na, const void *b, size_t nb) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return na > 0 && nb > 0 && x < y + nb && y < x + na;
-}
-
-struct Span {
-    const void *p;
-    size_t bytes;
-};
-// Whether one of `written` overlaps another of them or one of `read` (absent arrays overlap nothing).
-bool any_overlap(std::initializer_list<Span> written, std::initializer_list<Span> read) {
-    for (const Span *o = written.begin(); o != written.end(); ++o) {
-        if (!o->p) continue;
-        for (const Span *i = o + 1; i != written.end(); ++i)
-            if (i->p && overlap(o->p, o->bytes, i->p, i->bytes)) return true;
-        for (const Span &i : read)
-            if (i.p && overlap(o->p, o->bytes, i.p, i.bytes)) return true;
-    }
-    return false;
-}
-
 size_t table_bytes(const lla_pages *p) { return static_cast<size_t>(p->S) * p->max_blocks_per_seq * 4; }
 Span ledger_of(const lla_pages *p) { return Span{p->ref_count, static_cast<size_t>(p->num_blocks) * 4}; }
 Span table_of(const lla_pages *p) { return Span{p->block_table, table_bytes(p)}; }
@@ -715,6 +862,32 @@ lla_status lla_pages_extend(const lla_pages *pages, const lla_pool *pools, int32
     if (!launch) return LLA_OK;
     return launch_pages_extend(*pages, pools, L, slot_mapping, pages->S == 0 ? 0 : N, cu_new, skip, lens_before, free_blocks,
                                workspace, static_cast<cudaStream_t>(stream));
+}
+
+lla_status lla_pages_admit_workspace_size(int32_t n, size_t *bytes) {
+    if (!bytes || n < 0 || n > LLA_MAX_BATCH) return LLA_ERR_INVALID_ARG;
+    *bytes = pages_admit_workspace_bytes();
+    return LLA_OK;
+}
+
+lla_status lla_pages_admit(const lla_pages *pages, const lla_pool *pools, int32_t L, const int32_t *rows,
+                           const int32_t *parents, const int32_t *keep, const int32_t *new_lens, int32_t n,
+                           int64_t *slot_mapping, int32_t N, int32_t *cu_new, uint8_t *admitted, int32_t *free_blocks,
+                           void *workspace, size_t workspace_bytes, void *stream) {
+    lla_status st = check_pages(pages);
+    if (st != LLA_OK) return st;
+    if ((st = check_pools(pools, L)) != LLA_OK) return st;
+    if (n < 0 || n > LLA_MAX_BATCH || N < 0 || (N > 0 && !slot_mapping) || !cu_new) return LLA_ERR_INVALID_ARG;
+    if (n > 0 && (!rows || !parents || !keep || !new_lens || !admitted)) return LLA_ERR_INVALID_ARG;
+    const size_t need = pages_admit_workspace_bytes(), each = static_cast<size_t>(n) * 4;
+    if (!workspace || !aligned(workspace, 16)) return LLA_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return LLA_ERR_WORKSPACE;
+    if (any_overlap({{slot_mapping, static_cast<size_t>(N) * 8}, {cu_new, each + 4}, {admitted, static_cast<size_t>(n)},
+                     {free_blocks, 4}, {workspace, need}, ledger_of(pages), table_of(pages), lens_of(pages)},
+                    {{rows, each}, {parents, each}, {keep, each}, {new_lens, each}}))
+        return LLA_ERR_INVALID_ARG;
+    return launch_pages_admit(*pages, pools, L, AdmitRequests{rows, parents, keep, new_lens, n}, slot_mapping, N, cu_new, admitted,
+                              free_blocks, workspace, static_cast<cudaStream_t>(stream));
 }
 
 lla_status lla_pages_free(const lla_pages *pages, const int32_t *seqs, int32_t n, void *stream) {

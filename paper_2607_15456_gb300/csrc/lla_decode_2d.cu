@@ -351,17 +351,6 @@ __device__ Share find_share(const T2Params &p, int G, int c) {
     return r;
 }
 
-// named_bar_sync that also tells every thread whether any of them passed true.
-__device__ __forceinline__ bool named_bar_or(int id, int nthreads, bool mine) {
-    int any;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %3, 0;\n\tbarrier.cta.red.or.pred q, %1, %2, p;\n\t"
-                 "selp.b32 %0, 1, 0, q;\n\t}"
-                 : "=r"(any)
-                 : "r"(id), "r"(nthreads), "r"(mine ? 1 : 0)
-                 : "memory");
-    return any != 0;
-}
-
 // Products issued by a converged warp (WARP) or by one thread.
 template <bool WARP>
 struct Issue {
@@ -388,17 +377,6 @@ __device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, float (&v)[N]) {
     static_assert(N == 16 || N == 32, "score columns");
     if constexpr (N == 16) tmem_ld16(taddr, v);
     else tmem_ld32(taddr, v);
-}
-
-// The K bf16 parts of v: part 0 = bf16(v), part k = bf16 of what parts 0 .. k-1 leave (each
-// difference is exact in fp32).
-template <int K>
-__device__ __forceinline__ void bf16_parts(float v, float (&part)[K]) {
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        part[k] = __bfloat162float(__float2bfloat16_rn(v));
-        v -= part[k];
-    }
 }
 
 template <int RK, int RV, int NQ>
@@ -1577,14 +1555,16 @@ struct RKParams {
     char *pool;
     int64_t num_blocks;
     const void *k;  // [N][d_rope]
-    const int32_t *positions;
+    const int32_t *positions;  // [axes][N]
     const int64_t *slots;
-    unsigned long long phi[48];
+    int axes;  // 1 or 3
+    uint8_t axis[kMaxRopePairs];
+    unsigned long long phi[kMaxRopePairs];
     unsigned *err;
 };
 
-// One thread per (token, pair): k^R of token n turned at positions[n] (pair j by
-// positions[n] theta_j), written as bf16 at row slot % 64 of block slot / 64 in the granule
+// One thread per (token, pair): k^R of token n turned at its position (pair j by
+// positions[axis(j)][n] theta_j), written as bf16 at row slot % 64 of block slot / 64 in the granule
 // layout of a K-plane (granule g of row i at g*1024 + i*16).
 __global__ void __launch_bounds__(256) rope_key_store_kernel(const RKParams p) {
     const int hp = p.d_rope / 2;
@@ -1593,13 +1573,14 @@ __global__ void __launch_bounds__(256) rope_key_store_kernel(const RKParams p) {
     if (i < static_cast<int64_t>(p.N) * hp) {
         const int n = static_cast<int>(i / hp), j = static_cast<int>(i - static_cast<int64_t>(n) * hp);
         const int64_t slot = p.slots[n];
-        const int pos = p.positions[n];
+        const int pos = p.positions[static_cast<int64_t>(p.axis[j]) * p.N + n];
         if (slot >= 0) {
             const int64_t blk = slot / kPT;
             const int row = static_cast<int>(slot - blk * kPT);
             if (blk >= p.num_blocks) {
                 atomicOr(p.err, LLA_DEVERR_SLOT);
-            } else if (pos < 0) {
+            } else if (p.positions[n] < 0 || (p.axes == 3 && (p.positions[static_cast<int64_t>(p.N) + n] < 0 ||
+                                                              p.positions[2 * static_cast<int64_t>(p.N) + n] < 0))) {
                 atomicOr(p.err, LLA_DEVERR_CONTEXT);
             } else {
                 float sn, cs;
@@ -1639,7 +1620,7 @@ size_t decode_2d_workspace_bytes(int r_k, int r_v, int B) {
     return ws2_layout(r_k, r_v, kNQ, B, grid).total;
 }
 
-lla_status launch_rope_key_store(int d_rope, double base, int pairing, void *rope_pool, int64_t num_blocks,
+lla_status launch_rope_key_store(int d_rope, const RotaryAxes &rope, void *rope_pool, int64_t num_blocks,
                                  const void *k, int x_bf16, const int32_t *positions, const int64_t *slots,
                                  int N, cudaStream_t stream) {
     if (N == 0) return LLA_OK;
@@ -1647,10 +1628,12 @@ lla_status launch_rope_key_store(int d_rope, double base, int pairing, void *rop
     unsigned *err = device_error_word(&st);
     if (st != LLA_OK) return st;
     RKParams rp = {};
-    rp.N = N; rp.d_rope = d_rope; rp.pairing = pairing; rp.x_bf16 = x_bf16;
+    rp.N = N; rp.d_rope = d_rope; rp.pairing = rope.pairing; rp.x_bf16 = x_bf16;
+    rp.axes = rope.axes;
+    for (int j = 0; j < d_rope / 2; ++j) rp.axis[j] = rope.axis[j];
     rp.pool = static_cast<char *>(rope_pool); rp.num_blocks = num_blocks;
     rp.k = k; rp.positions = positions; rp.slots = slots; rp.err = err;
-    rotary_phases(d_rope, base, rp.phi);
+    rotary_phases(d_rope, rope.base, rp.phi);
     const int64_t total = static_cast<int64_t>(N) * (d_rope / 2);
     if ((total + 255) / 256 > 0x7fffffff) return LLA_ERR_UNSUPPORTED;
     return launch_ex(rope_key_store_kernel, dim3(static_cast<unsigned>((total + 255) / 256)), 256, 0, stream, rp);

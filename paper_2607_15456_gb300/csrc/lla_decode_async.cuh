@@ -11,17 +11,18 @@
 namespace lla {
 namespace {
 
-constexpr int kMaxRopePairs = 48;  // d_rope <= 96
-
 // Launch parameters of the rotary branch: the decode parameters, the rotary planes (one per
 // block, [64 x d_rope] bf16 in the K-plane's granule layout), the rotary query q^R [B][H][d_rope]
-// and, in pass 1, the current token's rotary key [B][d_rope], and theta_j of every pair in 64-bit
-// fixed-point turns (theta_j / 2 pi * 2^64).
+// and, in pass 1, the current token's rotary key [B][d_rope], theta_j of every pair in 64-bit
+// fixed-point turns (theta_j / 2 pi * 2^64), and, where tokens have a position on each of three axes, the
+// current tokens' positions [3][B] and the axis of every pair.
 struct DecParams {
     Params p;
     const char *rope_pool;
     const void *q_rope, *cur_k_rope;
     int pairing;  // 0: pair j = (j, j + d_rope/2); 1: (2j, 2j + 1)
+    const int32_t *positions;  // or NULL: P from the context length
+    uint8_t axis[kMaxRopePairs];
     unsigned long long phi[kMaxRopePairs];
 };
 
@@ -43,7 +44,7 @@ __host__ __device__ inline int rotary_query_offset(int stages, int stage_bytes, 
 }
 
 // Management warps, after m_setup of a run: rot(q^R, P) into the run's rotary query slot, with P
-// the current token's position (its context length in pass 1, one less in pass 2), and in pass 1
+// the current token's position (given, or its context length in pass 1, one less in pass 2), and in pass 1
 // q^R . k^R_cur added to the partial of q . k_cur (both sit at P, so the rotation cancels).
 template <int DR>
 __device__ void m_rotary(const DecParams &d, const ASmem &a, int b, int h, int slot, int mt, float *rq) {
@@ -55,7 +56,15 @@ __device__ void m_rotary(const DecParams &d, const ASmem &a, int b, int h, int s
     float *dst = rq + slot * DR;
     for (int j = mt; j < DR / 2; j += kMThreads) {
         float sn, cs;
-        turn_sincos(P, d.phi[j], &sn, &cs);
+        long long at = P;
+        if (d.positions) {
+            at = d.positions[static_cast<int64_t>(d.axis[j]) * p.B + b];
+            if (at < 0) {
+                atomicOr(p.err, LLA_DEVERR_CONTEXT);
+                at = 0;
+            }
+        }
+        turn_sincos(at, d.phi[j], &sn, &cs);
         const int ia = d.pairing ? 2 * j : j, ic = d.pairing ? 2 * j + 1 : j + DR / 2;
         const float x = load_elem(d.q_rope, src + ia, p.io_bf16);
         const float y = load_elem(d.q_rope, src + ic, p.io_bf16);

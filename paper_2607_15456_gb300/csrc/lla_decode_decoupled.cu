@@ -41,8 +41,8 @@ size_t decode_decoupled_workspace_bytes(int r_k, int r_v, int d_rope, int B, int
     return decode_workspace_bytes(r_v, B, H, grid);
 }
 
-lla_status launch_decode_decoupled(const DecodeArgs &a, const void *rope_pool, int d_rope, double base,
-                                   int pairing, const void *q_rope, const void *cur_k_rope,
+lla_status launch_decode_decoupled(const DecodeArgs &a, const void *rope_pool, int d_rope, const RotaryAxes &rope,
+                                   const int32_t *positions, const void *q_rope, const void *cur_k_rope,
                                    cudaStream_t stream) {
     if (!decode_decoupled_supported(a.storage_bf16 ? 2 : 4, a.d, a.H, a.r_k, a.r_v, d_rope))
         return LLA_ERR_UNSUPPORTED;
@@ -85,8 +85,10 @@ lla_status launch_decode_decoupled(const DecodeArgs &a, const void *rope_pool, i
     dp.rope_pool = static_cast<const char *>(rope_pool);
     dp.q_rope = q_rope;
     dp.cur_k_rope = cur_k_rope;
-    dp.pairing = pairing;
-    rotary_phases(d_rope, base, dp.phi);
+    dp.pairing = rope.pairing;
+    dp.positions = positions;
+    for (int j = 0; j < d_rope / 2; ++j) dp.axis[j] = rope.axis[j];
+    rotary_phases(d_rope, rope.base, dp.phi);
     return go(dp, grid, smem, stream);
 }
 

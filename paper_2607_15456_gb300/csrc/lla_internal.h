@@ -133,12 +133,29 @@ void rotary_phases(int d_rope, double base, unsigned long long *phi);
 // q_rope [B][H][d_rope], cur_k_rope [B][d_rope] in pass 1); and the rotary-key store.
 bool decode_decoupled_supported(int es, int d, int H, int r_k, int r_v, int d_rope);
 size_t decode_decoupled_workspace_bytes(int r_k, int r_v, int d_rope, int B, int H);
-lla_status launch_decode_decoupled(const DecodeArgs &a, const void *rope_pool, int d_rope, double base,
-                                   int pairing, const void *q_rope, const void *cur_k_rope,
+// Rotation of the branch: `axes` rows of positions (1: one position per token, 3: lla_rope_axes), the axis of each pair.
+constexpr int kMaxRopePairs = 48;  // d_rope <= 96
+struct RotaryAxes {
+    double base;
+    int pairing;  // 0: pair j = (j, j + d_rope/2); 1: (2j, 2j + 1)
+    int axes;
+    uint8_t axis[kMaxRopePairs];
+};
+// positions [3][B] of the current tokens, or NULL: their index in the sequence
+lla_status launch_decode_decoupled(const DecodeArgs &a, const void *rope_pool, int d_rope, const RotaryAxes &rope,
+                                   const int32_t *positions, const void *q_rope, const void *cur_k_rope,
                                    cudaStream_t stream);
-lla_status launch_rope_key_store(int d_rope, double base, int pairing, void *rope_pool, int64_t num_blocks,
+lla_status launch_rope_key_store(int d_rope, const RotaryAxes &rope, void *rope_pool, int64_t num_blocks,
                                  const void *k, int x_bf16, const int32_t *positions, const int64_t *slots,
                                  int N, cudaStream_t stream);
+// Decode of sequences that share pages (lla_decode_prefix.cu), and the plan of what they share (lla_prefix_plan.cu).
+bool decode_prefix_supported(int es, int d, int r_k, int r_v, int d_rope);
+size_t decode_prefix_workspace_bytes(int r_k, int r_v, int d_rope, int B, int H);
+lla_status launch_decode_prefix(const DecodeArgs &a, const lla_prefix &plan, const void *rope_pool, int d_rope,
+                                const RotaryAxes &rope, const int32_t *positions, const void *q_rope,
+                                const void *cur_k_rope, cudaStream_t stream);
+lla_status launch_prefix_plan(const int32_t *block_table, int64_t num_blocks, int max_blocks, const int32_t *context_lens, int B,
+                              int max_ctx, int min_pages, const lla_prefix &plan, cudaStream_t stream);
 
 // The checks of lla_beam_search (lla_abi.cu): what holds for every step, and its arrays beside those of its page sets.
 lla_status check_search(const lla_pages *a, const lla_pages *b, const lla_pool *pools, int32_t L, int32_t V, int32_t eos,
@@ -154,6 +171,13 @@ size_t pages_extend_workspace_bytes();
 lla_status launch_pages_extend(const lla_pages &p, const lla_pool *pools, int L, int64_t *slots, int N, const int32_t *cu_new,
                                const uint8_t *skip, int32_t *lens_before, int32_t *free_blocks, void *workspace,
                                cudaStream_t stream);
+struct AdmitRequests {
+    const int32_t *rows, *parents, *keep, *new_lens;
+    int n;
+};
+size_t pages_admit_workspace_bytes();
+lla_status launch_pages_admit(const lla_pages &p, const lla_pool *pools, int L, const AdmitRequests &r, int64_t *slots, int N,
+                              int32_t *cu_new, uint8_t *admitted, int32_t *free_blocks, void *workspace, cudaStream_t stream);
 size_t pages_compact_workspace_bytes(int64_t num_blocks);
 lla_status launch_pages_compact(const lla_pages &p, const lla_pool *pools, int L, int32_t *remap, int32_t *live, void *workspace,
                                 cudaStream_t stream);

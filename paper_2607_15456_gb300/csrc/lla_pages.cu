@@ -15,6 +15,7 @@
 
 #include "lla_device.cuh"
 #include "lla_internal.h"
+#include "lla_plan.cuh"
 #include "lla_units.cuh"
 
 namespace lla {
@@ -172,42 +173,6 @@ free_kernel(int32_t *ref, int nb, const int32_t *table, int max_blocks, int32_t 
 }
 
 // ------------------------------------------------------------------------------- prefix sums of a cluster
-
-constexpr int kPlanThreads = 1024;  // a sequence each, too
-static_assert(kPlanThreads == LLA_MAX_BATCH, "thread s plans sequence s");
-
-// Exclusive prefix sums of two values over a CTA's threads, and the CTA's totals.  `part` has 33 entries.  Three barriers.
-struct Two {
-    unsigned long long a;
-    int b;
-};
-__device__ __forceinline__ Two block_scan(Two v, Two *part, Two &total) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    auto scan = [&](Two x) {  // inclusive, of a warp
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const unsigned long long ua = __shfl_up_sync(0xffffffffu, x.a, o);
-            const int ub = __shfl_up_sync(0xffffffffu, x.b, o);
-            if (lane >= o) {
-                x.a += ua;
-                x.b += ub;
-            }
-        }
-        return x;
-    };
-    const Two inc = scan(v);
-    __syncthreads();  // part is free
-    if (lane == 31) part[warp] = inc;
-    __syncthreads();
-    if (warp == 0) {
-        const Two w = part[lane], all = scan(w);
-        part[lane] = Two{all.a - w.a, all.b - w.b};
-        if (lane == 31) part[32] = all;
-    }
-    __syncthreads();
-    total = part[32];
-    return Two{part[warp].a + inc.a - v.a, part[warp].b + inc.b - v.b};
-}
 
 // The ledger entries [begin, end) of a warp of the cluster, 128 at a time: lane l has entries 4 l to 4 l + 3 of them.
 struct Segment {
@@ -487,18 +452,14 @@ __device__ __forceinline__ void store_if(char *p, const uint4 &v, bool on) {
                  : "memory");
 }
 
-// Behind the plan: the rows of copied pages in every pool, and the slots of the new tokens.  Of a page only the rows
+// The rows of copied pages in every pool.  Of a page only the rows
 // that hold tokens are read and written: the first `rows` of each K granule, and a prefix of the V-plane.  A warp moves
 // a slice, eight words of 16 bytes in flight a lane, and each CTA takes every stride-th unit, so that long and short copies
 // mix on every SM.  Slices of 4 KB with four CTAs an SM measured 20.4 us (16-byte granules) and 30 us (4-byte ones); 4 KB and
 // five CTAs 23 and 34, 2 KB and six 27 and 45, two slices a warp in flight 3 us more than one.
-__global__ void __launch_bounds__(kCopyThreads, kCopyCtas)
-extend_finish_kernel(const ExtendArgs a, const __grid_constant__ PoolSet ps, int64_t *slots) {
-    pdl_wait();
-    pdl_trigger();
-    const ExtendPlan *plan = a.plan;
+__device__ __forceinline__ void copy_pages(const ExtendCopy *copy, int copies, const PoolSet &ps) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int copies = plan->copies, per_copy = max(1, ps.first[ps.L]), stride = gridDim.x;
+    const int per_copy = max(1, ps.first[ps.L]), stride = gridDim.x;
     // units in the order of copies, then pools and pages; a CTA takes every stride-th
     const int step_c = stride / per_copy, step_in = stride - step_c * per_copy;
     int c = blockIdx.x / per_copy, in_copy = blockIdx.x - c * per_copy;
@@ -521,7 +482,7 @@ extend_finish_kernel(const ExtendArgs a, const __grid_constant__ PoolSet ps, int
             slice = (in_pool - page * units) * kCopyWarps + warp;
         }
         if (page >= pool.pages || slice >= slices) continue;
-        const ExtendCopy job = plan->copy[c];
+        const ExtendCopy job = copy[c];
         const int kb = pool.k_row_bytes, vb = pool.v_row_bytes, rows = job.rows;
         const int64_t page_bytes = static_cast<int64_t>(kBlockTokens) * (kb + vb), block = page_bytes * pool.pages;
         const char *src = static_cast<const char *>(pool.base) + page * page_bytes + job.src * block;
@@ -565,6 +526,16 @@ extend_finish_kernel(const ExtendArgs a, const __grid_constant__ PoolSet ps, int
         if (off_a >= 0) *reinterpret_cast<uint32_t *>(dst + off_a) = rest_a;
         if (off_b >= 0) *reinterpret_cast<uint32_t *>(dst + off_b) = rest_b;
     }
+}
+
+// Behind the plan: the rows of copied pages, and the slots of the new tokens.
+__global__ void __launch_bounds__(kCopyThreads, kCopyCtas)
+extend_finish_kernel(const ExtendArgs a, const __grid_constant__ PoolSet ps, int64_t *slots) {
+    pdl_wait();
+    pdl_trigger();
+    const ExtendPlan *plan = a.plan;
+    copy_pages(plan->copy, plan->copies, ps);
+    const int stride = gridDim.x;
     // (64 bits: the last step over N near 2^31 passes it by a grid of threads)
     for (int64_t at = static_cast<int64_t>(blockIdx.x) * kCopyThreads + threadIdx.x; at < a.N; at += static_cast<int64_t>(stride) * kCopyThreads) {
         const int i = static_cast<int>(at);
@@ -589,6 +560,175 @@ extend_finish_kernel(const ExtendArgs a, const __grid_constant__ PoolSet ps, int
             slot = static_cast<int64_t>(b) * kBlockTokens + pos % kBlockTokens;
         }
         slots[i] = slot;
+    }
+}
+
+// ----------------------------------------------------------------------------------------------- admit
+
+// The workspace: what the plan tells the kernel behind it.
+struct AdmitPlan {
+    int copies, unused[3];
+    ExtendCopy copy[LLA_MAX_BATCH];
+};
+
+struct AdmitArgs {
+    int32_t *ref;
+    int nb;
+    int32_t *table;
+    int max_blocks;
+    int32_t *lens;
+    int S;
+    AdmitRequests r;
+    int N;
+    int32_t *cu_new;
+    uint8_t *admitted;
+    int32_t *free_blocks;
+    AdmitPlan *plan;
+    unsigned *err;
+};
+
+// The plan of an admission, by one cluster, as a growth is planned: thread i of every CTA works out request i, all threads
+// count the free blocks of their part of the ledger, and behind the cluster's exchange of counts the requests whose sums of
+// blocks and tokens (with all before them) find room are admitted, and each free block whose rank is below their need knows
+// its request by a binary search.  Both sums grow with the request, so that those admitted are the first ones.
+__global__ void __launch_bounds__(kPlanThreads, 1) admit_plan_kernel(const AdmitArgs a) {
+    __shared__ int owner[LLA_MAX_BATCH];  // lowest request of each row
+    __shared__ int first[LLA_MAX_BATCH];  // blocks that requests before i take
+    __shared__ int row_of[LLA_MAX_BATCH], shared_of[LLA_MAX_BATCH], copy_of[LLA_MAX_BATCH];
+    __shared__ Two part[33];
+    __shared__ int totals[16];
+    __shared__ unsigned long long most_blocks, most_tokens;  // of the admitted
+    cg::cluster_group cl = cg::this_cluster();
+    const int tid = threadIdx.x, rank = static_cast<int>(cl.block_rank()), ctas = static_cast<int>(cl.num_blocks());
+    owner[tid] = LLA_MAX_BATCH;
+    if (tid == 0) most_blocks = most_tokens = 0;
+    if (ctas > 1) cl.sync();  // every CTA has started
+    else __syncthreads();
+    pdl_wait();
+    pdl_trigger();
+    const Segment seg = my_segment(a.nb, rank, ctas);
+    const int mine = count_ledger<true>(a.ref, a.nb, seg, a.nb);
+    int row = 0, parent = -1, keep = 0, len = 0, tail = -1;
+    unsigned bad = 0;
+    if (tid < a.r.n) {
+        row = a.r.rows[tid];
+        parent = a.r.parents[tid];
+        keep = a.r.keep[tid];
+        len = a.r.new_lens[tid];
+        if (row < 0 || row >= a.S || parent < -1 || parent >= a.S) bad = LLA_DEVERR_SEQUENCE;
+        if (row >= 0 && row < a.S) atomicMin(&owner[row], tid);
+    }
+    __syncthreads();
+    if (tid < a.r.n && !bad) {
+        const int held = parent >= 0 ? checked_len(a.lens[parent], a.max_blocks) : 0;
+        if (owner[row] != tid)
+            bad = LLA_DEVERR_SEQUENCE;
+        else if (a.lens[row] != 0 || held < 0 || keep < 0 || keep > held || len < keep || checked_len(len, a.max_blocks) < 0)
+            bad = LLA_DEVERR_CONTEXT;
+        else if (keep % kBlockTokens) {
+            tail = a.table[static_cast<int64_t>(parent) * a.max_blocks + keep / kBlockTokens];
+            if (tail < 0 || tail >= a.nb) bad = LLA_DEVERR_BLOCK_ID;
+        }
+    }
+    if (bad && rank == 0) atomicOr(a.err, bad);
+    const bool valid = tid < a.r.n && !bad;
+    const int shared = keep / kBlockTokens, copy = valid && keep % kBlockTokens != 0;
+    // copies in the high bits: at most 2^10, and at most 2^10 * 2^24 blocks in the low ones
+    const unsigned long long need = valid ? static_cast<unsigned long long>(pages_of(len) - shared) : 0, tokens = valid ? len - keep : 0;
+    Two total, unused;
+    const Two at = block_scan(Two{need | static_cast<unsigned long long>(copy) << 40, mine}, part, total);
+    const Two at_token = block_scan(Two{tokens, 0}, part, unused);
+    const unsigned long long low40 = (1ull << 40) - 1;
+    const unsigned long long before = at.a & low40;
+    const int copy_index = static_cast<int>(at.a >> 40);
+    first[tid] = static_cast<int>(min(static_cast<unsigned long long>(LLA_MAX_BLOCKS) * 2, before));
+    row_of[tid] = row;
+    shared_of[tid] = shared;
+    copy_of[tid] = copy ? copy_index : -1;
+    const ClusterSums free = cluster_sums(total.b, totals);
+    const bool ok = valid && before + need <= static_cast<unsigned long long>(free.all) &&
+                    at_token.a + tokens <= static_cast<unsigned long long>(a.N);
+    if (ok) {
+        atomicMax(&most_blocks, at.a + (need | static_cast<unsigned long long>(copy) << 40));
+        atomicMax(&most_tokens, at_token.a + tokens);
+    }
+    __syncthreads();
+    const int64_t wanted = static_cast<int64_t>(most_blocks & low40);
+    if (rank == 0) {
+        if (tid < a.r.n) {
+            a.admitted[tid] = ok;
+            a.cu_new[tid] = static_cast<int32_t>(min(at_token.a, most_tokens));
+            if (ok) a.lens[row] = len;
+            if (ok && copy) {
+                a.plan->copy[copy_index].src = tail;
+                a.plan->copy[copy_index].rows = keep % kBlockTokens;
+            }
+        }
+        if (tid == 0) {
+            a.cu_new[a.r.n] = static_cast<int32_t>(most_tokens);
+            a.plan->copies = static_cast<int>(most_blocks >> 40);
+            if (a.free_blocks) *a.free_blocks = free.all - static_cast<int>(wanted);
+        }
+    }
+    if (wanted == 0) return;
+    // the k-th free block: to request i = the last with first[i] <= k
+    const int warp_first = free.before + __shfl_sync(0xffffffffu, at.b, 0);
+    rank_ledger<true>(a.ref, a.nb, seg, warp_first, wanted, [&](int id, bool is_free, int k) {
+        if (!is_free || k >= wanted) return;
+        int lo = 0, hi = a.r.n - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (first[mid] <= k) lo = mid;
+            else hi = mid - 1;
+        }
+        const int i = k - first[lo], c = copy_of[lo];  // the copied page comes first, then the fresh ones
+        a.table[static_cast<int64_t>(row_of[lo]) * a.max_blocks + shared_of[lo] + i] = id;
+        if (c >= 0 && i == 0) a.plan->copy[c].dst = id;
+        a.ref[id] = 1;
+    });
+}
+
+// Behind the plan: the rows of copied pages, the shared pages' table entries and references (kCopyThreads of a request at a
+// time), and the slots of the new tokens, whose pages are all the requests' own.
+__global__ void __launch_bounds__(kCopyThreads, kCopyCtas)
+admit_finish_kernel(const AdmitArgs a, const __grid_constant__ PoolSet ps, int64_t *slots, int spans) {
+    __shared__ int cu[LLA_MAX_BATCH + 1];
+    pdl_wait();
+    pdl_trigger();
+    for (int i = threadIdx.x; i <= a.r.n; i += kCopyThreads) cu[i] = a.cu_new[i];
+    copy_pages(a.plan->copy, a.plan->copies, ps);
+    const int stride = gridDim.x;
+    bool bad = false;
+    for (int u = blockIdx.x; u < a.r.n * spans; u += stride) {
+        const int i = u / spans, span = u - i * spans;
+        if (!a.admitted[i]) continue;
+        const int shared = a.r.keep[i] / kBlockTokens;
+        const int32_t *src = a.table + static_cast<int64_t>(max(0, a.r.parents[i])) * a.max_blocks;
+        int32_t *dst = a.table + static_cast<int64_t>(a.r.rows[i]) * a.max_blocks;
+        for (int64_t e = static_cast<int64_t>(span) * kCopyThreads + threadIdx.x; e < shared; e += static_cast<int64_t>(spans) * kCopyThreads) {
+            const int b = src[e];
+            dst[e] = b;
+            if (b < 0 || b >= a.nb) bad = true;
+            else atomicAdd(a.ref + b, 1);
+        }
+    }
+    if (bad) atomicOr(a.err, LLA_DEVERR_BLOCK_ID);
+    __syncthreads();  // cu
+    for (int64_t at = static_cast<int64_t>(blockIdx.x) * kCopyThreads + threadIdx.x; at < a.N; at += static_cast<int64_t>(stride) * kCopyThreads) {
+        const int t = static_cast<int>(at);
+        int64_t slot = -1;
+        if (t < cu[a.r.n]) {
+            int lo = 0, hi = a.r.n - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (cu[mid] <= t) lo = mid;
+                else hi = mid - 1;
+            }
+            const int pos = a.r.keep[lo] + t - cu[lo];
+            const int b = a.table[static_cast<int64_t>(a.r.rows[lo]) * a.max_blocks + pos / kBlockTokens];
+            slot = static_cast<int64_t>(b) * kBlockTokens + pos % kBlockTokens;
+        }
+        slots[at] = slot;
     }
 }
 
@@ -718,21 +858,23 @@ __global__ void __launch_bounds__(kCopyThreads) compact_move_kernel(const Compac
 // eight take 5.0 and 8.4, and 5.2 and 8.4.
 int plan_ctas(int64_t num_blocks) { return num_blocks > 8192 ? 8 : 1; }
 
-template <typename A>
-lla_status launch_plan(void (*kern)(A), int ctas, const A &a, cudaStream_t stream) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(ctas);
-    cfg.blockDim = dim3(kPlanThreads);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = ctas;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kern, a) == cudaSuccess ? LLA_OK : LLA_ERR_CUDA;
+// The pools of a copy, and how many units of work a block has in them.
+void fill_pools(PoolSet *out, const lla_pool *pools, int L) {
+    PoolSet &ps = *out;
+    ps = PoolSet{};
+    ps.L = L;
+    for (int l = 0; l < L; ++l) {
+        const int slices = k_slices(pools[l]) + v_slices(pools[l]);
+        ps.p[l] = pools[l];
+        ps.slices[l] = static_cast<uint16_t>(slices);
+        const int at_once = slices < kCopyWarps ? kCopyWarps / slices : 1;
+        const int units = slices < kCopyWarps ? (pools[l].pages + at_once - 1) / at_once
+                                              : pools[l].pages * ((slices + kCopyWarps - 1) / kCopyWarps);
+        ps.first[l + 1] = ps.first[l] + units;
+    }
+    ps.alike = 1;
+    for (int l = 1; l < L; ++l) ps.alike &= ps.first[l + 1] - ps.first[l] == ps.first[1];
+    ps.by_pool = fast_div(static_cast<uint32_t>(L > 0 ? ps.first[1] : 1));
 }
 
 }  // namespace
@@ -776,20 +918,8 @@ lla_status launch_pages_extend(const lla_pages &p, const lla_pool *pools, int L,
     a.plan = static_cast<ExtendPlan *>(workspace);
     a.err = device_error_word(&st);
     if (!a.err) return st;
-    PoolSet ps = {};
-    ps.L = L;
-    for (int l = 0; l < L; ++l) {
-        const int slices = k_slices(pools[l]) + v_slices(pools[l]);
-        ps.p[l] = pools[l];
-        ps.slices[l] = static_cast<uint16_t>(slices);
-        const int at_once = slices < kCopyWarps ? kCopyWarps / slices : 1;
-        const int units = slices < kCopyWarps ? (pools[l].pages + at_once - 1) / at_once
-                                              : pools[l].pages * ((slices + kCopyWarps - 1) / kCopyWarps);
-        ps.first[l + 1] = ps.first[l] + units;
-    }
-    ps.alike = 1;
-    for (int l = 1; l < L; ++l) ps.alike &= ps.first[l + 1] - ps.first[l] == ps.first[1];
-    ps.by_pool = fast_div(static_cast<uint32_t>(L > 0 ? ps.first[1] : 1));
+    PoolSet ps;
+    fill_pools(&ps, pools, L);
     if ((st = launch_plan(extend_plan_kernel, plan_ctas(p.num_blocks), a, stream)) != LLA_OK) return st;
     const int sms = num_sms();
     if (sms <= 0) return LLA_ERR_CUDA;
@@ -797,6 +927,30 @@ lla_status launch_pages_extend(const lla_pages &p, const lla_pool *pools, int L,
     const int64_t work = static_cast<int64_t>(p.S) * ps.first[L] + (static_cast<int64_t>(N) + kCopyThreads - 1) / kCopyThreads;
     return launch_ex(extend_finish_kernel, dim3(static_cast<unsigned>(work < sms * kCopyCtas ? (work > 0 ? work : 1) : sms * kCopyCtas)),
                      kCopyThreads, 0, stream, a, ps, slots);
+}
+
+size_t pages_admit_workspace_bytes() { return sizeof(AdmitPlan); }
+
+lla_status launch_pages_admit(const lla_pages &p, const lla_pool *pools, int L, const AdmitRequests &r, int64_t *slots, int N,
+                              int32_t *cu_new, uint8_t *admitted, int32_t *free_blocks, void *workspace, cudaStream_t stream) {
+    lla_status st;
+    AdmitArgs a = {};
+    a.ref = p.ref_count; a.nb = static_cast<int>(p.num_blocks);
+    a.table = p.block_table; a.max_blocks = p.max_blocks_per_seq; a.lens = p.context_lens; a.S = p.S;
+    a.r = r; a.N = N;
+    a.cu_new = cu_new; a.admitted = admitted; a.free_blocks = free_blocks;
+    a.plan = static_cast<AdmitPlan *>(workspace);
+    a.err = device_error_word(&st);
+    if (!a.err) return st;
+    PoolSet ps;
+    fill_pools(&ps, pools, L);
+    const int sms = num_sms();
+    if (sms <= 0) return LLA_ERR_CUDA;
+    if ((st = launch_plan(admit_plan_kernel, plan_ctas(p.num_blocks), a, stream)) != LLA_OK) return st;
+    const int most = (p.max_blocks_per_seq + kCopyThreads - 1) / kCopyThreads, spans = most < 8 ? most : 8;
+    const int64_t work = static_cast<int64_t>(r.n) * (ps.first[L] + spans) + (static_cast<int64_t>(N) + kCopyThreads - 1) / kCopyThreads;
+    return launch_ex(admit_finish_kernel, dim3(static_cast<unsigned>(work < sms * kCopyCtas ? (work > 0 ? work : 1) : sms * kCopyCtas)),
+                     kCopyThreads, 0, stream, a, ps, slots, spans);
 }
 
 size_t pages_compact_workspace_bytes(int64_t num_blocks) {

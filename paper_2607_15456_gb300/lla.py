@@ -34,6 +34,9 @@ LLA_DEVERR_SLOT = 0x10
 LLA_DEVERR_SEQUENCE = 0x20
 LLA_DEVERR_PAGES = 0x40
 LLA_MAX_BEAMS = 32
+LLA_ROPE_AXES = 3
+LLA_AXES_BLOCKS, LLA_AXES_INTERLEAVED = 0, 1
+LLA_PREFIX_LEVELS, LLA_PREFIX_MEMBERS = 3, 64
 
 _STATUS = {0: "LLA_OK", 1: "LLA_ERR_INVALID_ARG", 2: "LLA_ERR_UNSUPPORTED", 3: "LLA_ERR_CUDA",
            4: "LLA_ERR_TIMEOUT", 5: "LLA_ERR_DEVICE_CHECK", 6: "LLA_ERR_WORKSPACE"}
@@ -58,6 +61,15 @@ class lla_codec(ctypes.Structure):
 
 class lla_rope(ctypes.Structure):
     _fields_ = [("base", ctypes.c_double), ("pairing", ctypes.c_int32)]
+
+
+class lla_rope_axes(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_double), ("pairing", ctypes.c_int32), ("pairs", ctypes.c_int32 * 3),
+                ("order", ctypes.c_int32)]
+
+
+class lla_prefix(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("num_groups", "groups", "members", "column", "own_page")]
 
 
 class lla_cache(ctypes.Structure):
@@ -153,6 +165,16 @@ def library() -> ctypes.CDLL:
             "lla_decode_decoupled_workspace_size": (I32, [P, I32, I32, P]),
             "lla_decode_attn_decoupled": (I32, [P, P, P, P, I32, P, P, I32, I32, I32, P, P, P, P, P, I32,
                                                 P, P, SZ, P]),
+            "lla_encode_rope_keys_axes": (I32, [I32, P, P, I64, P, I32, P, P, I32, P]),
+            "lla_decode_attn_decoupled_axes": (I32, [P, P, P, P, I32, P, P, P, I32, I32, I32, P, P, P, P, P, I32,
+                                                     P, P, SZ, P]),
+            "lla_prefix_plan": (I32, [P, P, I32, I32, I32, P, P]),
+            "lla_decode_prefix_workspace_size": (I32, [P, I32, I32, P]),
+            "lla_decode_attn_prefix": (I32, [P, P, P, P, P, I32, I32, I32, P, P, P, I32, P, P, SZ, P]),
+            "lla_decode_attn_prefix_decoupled": (I32, [P, P, P, P, P, I32, P, P, P, I32, I32, I32, P, P, P, P, P,
+                                                       I32, P, P, SZ, P]),
+            "lla_pages_admit_workspace_size": (I32, [I32, P]),
+            "lla_pages_admit": (I32, [P, P, I32, P, P, P, P, I32, P, I32, P, P, P, P, SZ, P]),
             "lla_get_device_error": (I32, [P, P]),
             "lla_clear_device_error": (I32, [P]),
             "lla_prefill_two_pass": (I32, [P, I32, P, P, I32, P, I32, P, I32, I32, I32, P, CAPTURE_FN,
@@ -600,6 +622,51 @@ def lla_decode_attn_decoupled(geom: Geometry, codec: Codec, cache: Cache, rope_p
         workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
+@dataclass
+class RopeAxes:
+    """Rotation of a rotary branch with a position on each of three axes: pair j turns with the axis that `order` gives it
+    (LLA_AXES_BLOCKS: pairs[0] pairs of axis 0, then pairs[1] of axis 1, ...; LLA_AXES_INTERLEAVED: the axes in turn)."""
+    base: float
+    pairing: int
+    pairs: tuple
+    order: int = LLA_AXES_BLOCKS
+
+    def c(self) -> lla_rope_axes:
+        if len(self.pairs) != LLA_ROPE_AXES:
+            raise ValueError(f"pairs of {LLA_ROPE_AXES} axes, not of {len(self.pairs)}")
+        return lla_rope_axes(float(self.base), int(self.pairing), (ctypes.c_int32 * 3)(*self.pairs), int(self.order))
+
+
+def lla_encode_rope_keys_axes(d_rope: int, rope: RopeAxes, rope_pool: torch.Tensor, num_blocks: int,
+                              k_rope: torch.Tensor, positions: torch.Tensor, slot_mapping: torch.Tensor,
+                              stream=None) -> None:
+    """Rotary keys k_rope [N][d_rope], turned at positions [3][N] int32, into the rotary planes."""
+    rp = rope.c()
+    N = k_rope.shape[0] if k_rope.dim() == 2 else 0
+    if k_rope.dim() == 2 and k_rope.shape[1] != d_rope:
+        raise ValueError(f"k_rope is [N][{d_rope}], not {tuple(k_rope.shape)}")
+    _check("lla_encode_rope_keys_axes", library().lla_encode_rope_keys_axes(
+        d_rope, ctypes.byref(rp), _ptr(rope_pool), num_blocks, _ptr(k_rope), _dtype_code(k_rope),
+        _typed(positions, torch.int32, "positions", (3, N)), _typed(slot_mapping, torch.int64, "slot_mapping", (N,)), N,
+        _stream(stream)))
+
+
+def lla_decode_attn_decoupled_axes(geom: Geometry, codec: Codec, cache: Cache, rope_pool: torch.Tensor,
+                                   d_rope: int, rope: RopeAxes, positions: torch.Tensor,
+                                   context_lens: torch.Tensor, max_ctx: int, loop: int, q: torch.Tensor,
+                                   q_rope: torch.Tensor, cur_k: Optional[torch.Tensor],
+                                   cur_v: Optional[torch.Tensor], cur_k_rope: Optional[torch.Tensor],
+                                   out: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """lla_decode_attn_decoupled with the current tokens at positions [3][B] int32."""
+    g, cd, ch, rp = geom.c(), codec.c(), cache.c(), rope.c()
+    B = q.shape[0]
+    _check("lla_decode_attn_decoupled_axes", library().lla_decode_attn_decoupled_axes(
+        ctypes.byref(g), ctypes.byref(cd), ctypes.byref(ch), _ptr(rope_pool), d_rope, ctypes.byref(rp),
+        _typed(positions, torch.int32, "positions", (3, B)), _ptr(context_lens), B, max_ctx, loop, _ptr(q), _ptr(q_rope),
+        _ptr(cur_k), _ptr(cur_v), _ptr(cur_k_rope), _dtype_code(q), _ptr(out), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
 def lla_dense_store(geom: Geometry, cache: Cache, k: torch.Tensor, v: torch.Tensor,
                     slot_mapping: torch.Tensor, stream=None) -> None:
     """k, v [N][H][d]: plain loop-t keys and values for the uncompressed comparator."""
@@ -781,6 +848,124 @@ def lla_pages_compact(pages: Pages, pools: Pools, remap: torch.Tensor, live: tor
     _check("lla_pages_compact", library().lla_pages_compact(
         ctypes.byref(p), pools.address, pools.count, _typed(remap, torch.int32, "remap", (p.num_blocks,)),
         _typed(live, torch.int32, "live", (1,)), *_scratch(workspace), _stream(stream)))
+
+
+def lla_pages_admit_workspace_size(n: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check("lla_pages_admit_workspace_size",
+           library().lla_pages_admit_workspace_size(n, ctypes.byref(out)))
+    return out.value
+
+
+def lla_pages_admit(pages: Pages, pools: Pools, rows: torch.Tensor, parents: torch.Tensor, keep: torch.Tensor,
+                    new_lens: torch.Tensor, slot_mapping: torch.Tensor, cu_new: torch.Tensor,
+                    admitted: torch.Tensor, workspace: torch.Tensor, free_blocks: Optional[torch.Tensor] = None,
+                    stream=None) -> None:
+    """Request i becomes the empty sequence rows[i], of new_lens[i] tokens, the first keep[i] of them those of sequence
+    parents[i] (-1: none): all [n] int32.  slot_mapping [N] int64, cu_new [n + 1] int32, admitted [n] uint8 and free_blocks
+    [1] int32 are written."""
+    p = pages.c()
+    pools = pools if isinstance(pools, Pools) else Pools(pools)
+    pools.check(pages)
+    n = rows.numel()
+    requests = [_typed(t, torch.int32, name, (n,)) for t, name in
+                ((rows, "rows"), (parents, "parents"), (keep, "keep"), (new_lens, "new_lens"))]
+    _check("lla_pages_admit", library().lla_pages_admit(
+        ctypes.byref(p), pools.address, pools.count, *requests, n, _typed(slot_mapping, torch.int64, "slot_mapping"),
+        slot_mapping.numel(), _typed(cu_new, torch.int32, "cu_new", (n + 1,)),
+        _typed(admitted, torch.uint8, "admitted", (n,)), _typed(free_blocks, torch.int32, "free_blocks", (1,)),
+        *_scratch(workspace), _stream(stream)))
+
+
+@dataclass
+class Prefix:
+    """Which sequences share which pages, as lla_prefix_plan writes it: num_groups [1], groups [3 max(1, B // 2)][4], members
+    [3 B], column [3][B], own_page [B], all int32."""
+    num_groups: torch.Tensor
+    groups: torch.Tensor
+    members: torch.Tensor
+    column: torch.Tensor
+    own_page: torch.Tensor
+
+    @classmethod
+    def empty(cls, B: int, device="cuda") -> "Prefix":
+        """The arrays of a plan for B sequences."""
+        def new(*shape):
+            return torch.zeros(shape, dtype=torch.int32, device=device)
+        L = LLA_PREFIX_LEVELS
+        return cls(new(1), new(L * max(1, B // 2), 4), new(L * B), new(L, B), new(B))
+
+    def c(self, B: int) -> lla_prefix:
+        L = LLA_PREFIX_LEVELS
+        shapes = dict(num_groups=(1,), groups=(L * max(1, B // 2), 4), members=(L * B,), column=(L, B), own_page=(B,))
+        return lla_prefix(*(_typed(getattr(self, n), torch.int32, n, s) for n, s in shapes.items()))
+
+
+def _table_rows(cache: Cache, B: int) -> None:
+    """Refuses a block table that has no rows of max_blocks_per_seq entries for B sequences (it may have more)."""
+    t = cache.block_table
+    _typed(t, torch.int32, "block_table")
+    if t.dim() != 2 or t.shape[0] < B or t.shape[1] != cache.max_blocks_per_seq:
+        raise ValueError(f"block_table must have shape {(B, cache.max_blocks_per_seq)}, not {tuple(t.shape)}")
+
+
+def lla_prefix_plan(cache: Cache, context_lens: torch.Tensor, max_ctx: int, plan: Prefix, min_pages: int = 1,
+                    stream=None) -> None:
+    """Works out what the sequences of cache.block_table share (the pool is not read and may be None); writes `plan`."""
+    B = context_lens.numel()
+    _table_rows(cache, B)
+    ch, pl = cache.c(), plan.c(B)
+    _check("lla_prefix_plan", library().lla_prefix_plan(
+        ctypes.byref(ch), _typed(context_lens, torch.int32, "context_lens", (B,)), B, max_ctx, min_pages, ctypes.byref(pl),
+        _stream(stream)))
+
+
+def lla_decode_prefix_workspace_size(geom: Geometry, B: int, d_rope: int = 0) -> int:
+    out = ctypes.c_size_t(0)
+    g = geom.c()
+    _check("lla_decode_prefix_workspace_size", library().lla_decode_prefix_workspace_size(
+        ctypes.byref(g), d_rope, B, ctypes.byref(out)))
+    return out.value
+
+
+def _decode_prefix_check(geom: Geometry, cache: Cache, context_lens, q, q_rope, cur_k, cur_v, cur_k_rope, out, d_rope):
+    """The shapes and types of a prefix decode's arrays (its callers give the addresses)."""
+    B, shape = q.shape[0], (q.shape[0], geom.H, geom.d)
+    for t, name in ((q, "q"), (cur_k, "cur_k"), (cur_v, "cur_v"), (out, "out")):
+        _typed(t, q.dtype, name, shape)
+    _typed(q_rope, q.dtype, "q_rope", (B, geom.H, d_rope))
+    _typed(cur_k_rope, q.dtype, "cur_k_rope", (B, d_rope))
+    _typed(context_lens, torch.int32, "context_lens", (B,))
+    _table_rows(cache, B)
+
+
+def lla_decode_attn_prefix(geom: Geometry, codec: Codec, cache: Cache, plan: Prefix, context_lens: torch.Tensor,
+                           max_ctx: int, loop: int, q: torch.Tensor, cur_k: Optional[torch.Tensor],
+                           cur_v: Optional[torch.Tensor], out: torch.Tensor, workspace: torch.Tensor,
+                           stream=None) -> None:
+    """lla_decode_attn with the pages that `plan` (lla_prefix_plan) names read once for all sequences of a group."""
+    _decode_prefix_check(geom, cache, context_lens, q, None, cur_k, cur_v, None, out, 0)
+    B = q.shape[0]
+    g, cd, ch, pl = geom.c(), codec.c(), cache.c(), plan.c(B)
+    _check("lla_decode_attn_prefix", library().lla_decode_attn_prefix(
+        ctypes.byref(g), ctypes.byref(cd), ctypes.byref(ch), ctypes.byref(pl), _ptr(context_lens), B, max_ctx, loop, _ptr(q),
+        _ptr(cur_k), _ptr(cur_v), _dtype_code(q), _ptr(out), *_scratch(workspace), _stream(stream)))
+
+
+def lla_decode_attn_prefix_decoupled(geom: Geometry, codec: Codec, cache: Cache, plan: Prefix, rope_pool: torch.Tensor,
+                                     d_rope: int, rope: RopeAxes, positions: Optional[torch.Tensor],
+                                     context_lens: torch.Tensor, max_ctx: int, loop: int, q: torch.Tensor,
+                                     q_rope: torch.Tensor, cur_k: Optional[torch.Tensor],
+                                     cur_v: Optional[torch.Tensor], cur_k_rope: Optional[torch.Tensor],
+                                     out: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """The same with a rotary branch; positions [3][B] int32 of the current tokens, or None: their index on every axis."""
+    _decode_prefix_check(geom, cache, context_lens, q, q_rope, cur_k, cur_v, cur_k_rope, out, d_rope)
+    B = q.shape[0]
+    g, cd, ch, pl, rp = geom.c(), codec.c(), cache.c(), plan.c(B), rope.c()
+    _check("lla_decode_attn_prefix_decoupled", library().lla_decode_attn_prefix_decoupled(
+        ctypes.byref(g), ctypes.byref(cd), ctypes.byref(ch), ctypes.byref(pl), _ptr(rope_pool), d_rope, ctypes.byref(rp),
+        _typed(positions, torch.int32, "positions", (3, B)), _ptr(context_lens), B, max_ctx, loop, _ptr(q), _ptr(q_rope),
+        _ptr(cur_k), _ptr(cur_v), _ptr(cur_k_rope), _dtype_code(q), _ptr(out), *_scratch(workspace), _stream(stream)))
 
 
 def lla_beam_select_workspace_size(B: int, W: int, V: int, K: int, dtype=torch.bfloat16) -> int:
