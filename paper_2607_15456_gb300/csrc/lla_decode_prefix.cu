@@ -11,22 +11,29 @@
 // current token:
 //   o = (W_up,t^V sum_j w_j o~_j + (sum_j w_j l_j) mu^V_t + w_cur v_cur) / (sum_j w_j l_j + w_cur),  w_j = e^(m_j - M).
 //
-// Three launches on the caller's stream, chained by programmatic dependent launch:
+// Four launches on the caller's stream, chained by programmatic dependent launch:
 //   absorb_kernel  q~ (fp32, scaled into the exp2 domain) and beta of every (sequence, head); the prefix sums of the nodes'
 //                  pages and the checks of lengths and plan
-//   trunk_kernel   one CTA per SM.  The units' pages, in the order of the nodes, are split evenly over the CTAs; a CTA takes
-//                  its pages as runs (its part of one unit).  A page is two products on the tensor cores,
-//                    S^T [64 tokens x 3 NQ]  = [C_k | K^R] [Q~_0; Q~_1; Q~_2]^T   (q~ as three bf16 parts)
-//                    O^T [r_v x 2 NQ]       += C_v^T [P_0; P_1]^T                 (p as two)
-//                  for 8 or 32 queries; a group of 33 to 64 members is two halves of 32, which take turns on each page
-//                  while it is in shared memory.
-//                    warp 0        producer: the K-plane (and rotary plane) by bulk copies, the V-plane by TMA boxes
-//                    warp 1        issuer of S^T, and owner of TMEM
-//                    warp 2        q~ of the next run as an operand, beta
-//                    warp 3        issuer of O^T
-//                    warps 4-7     softmax: p as an operand, lazy rescale of O^T
-//                    warps 8-11    epilogue: O^T, maxima and sums of a finished run to the workspace
-//                  S^T, P, q~ and O^T have two buffers each, so that every role works ahead of the next.
+//   trunk_kernel   nodes of more than kLeaf queries, one CTA per SM.  Their pages, unit by unit in the order of the nodes, are
+//                  split evenly over the CTAs; a CTA takes its pages as runs (its part of one unit).  A page is two products on the tensor cores, with 128 rows for
+//                  the 64 queries of a run, each of them twice:
+//                    S [128 x 64 tokens] = sum_i Q~_i [C_k | K^R]^T      i = 0, 1, 2: q~ as three bf16 parts, in TMEM
+//                    O [128 x r_v]      += P C_v                         P in TMEM
+//                  Rows q and 64 + q have the same scores; the thread of the first gives its weights p as bf16(p), that of
+//                  the second as bf16(p - bf16(p)), so that the two rows of O add up to a sum with p in two parts, for the
+//                  tensor cores' price of one, and each thread has the scores of its query in its own registers.
+//                    warp 0        producer of K-planes (and rotary planes): bulk copies
+//                    warp 2        producer of V-planes: TMA boxes of 64 columns with 128-byte swizzle
+//                    warp 1        issuer of S, and owner of TMEM
+//                    warp 3        issuer of O
+//                    warps 4-11    softmax: two groups that take the pages in turn (as in the prefill, a page's step from scores
+//                                  to weights takes longer than its products); the running maximum goes from page to page
+//                                  through shared memory and a named barrier per pair of warps; lazy rescale of O
+//                    warps 12-15   q~ of the next run into TMEM as soon as the last S of the run before is done; then that
+//                                  run's O, maxima and sums to the workspace
+//   leaf_kernel    nodes of up to kLeaf queries, which are short (a sequence's own pages): one page at a time in each of as
+//                  many warps as pages fit in an SM's shared memory, every warp on its own with an even share of the pages.
+//                  It starts on each SM as the trunk kernel leaves it
 //   join_kernel    per head and up to 8 sequences: joins the runs of each sequence's nodes and the current token, and applies
 //                  W_up,t^V once for all of them
 //
@@ -48,13 +55,13 @@ namespace {
 
 constexpr int kPT = 64;          // tokens per page
 constexpr int kD = 128;          // head width
-constexpr int kHalf = 32;        // queries of an operand
-constexpr int kFew = 8;          // of the small one
+constexpr int kRows = 128;       // rows of the products: every query twice
 constexpr int kLevels = LLA_PREFIX_LEVELS;
 constexpr int kMembers = LLA_PREFIX_MEMBERS;
 constexpr int kMaxNodes = kLevels * (LLA_MAX_BATCH / 2) + LLA_MAX_BATCH;
-constexpr int kTrunkThreads = 384;
-constexpr int kQueryWarp = 2, kValueWarp = 3, kSoftmaxWarp = 4, kEpilogueWarp = 8;
+constexpr int kTrunkThreads = 512;
+constexpr int kSoftmaxWarp = 4, kAuxWarp = 12;
+constexpr int kLeaf = 2;         // most queries of a node that the leaf kernel takes
 constexpr int kMaxGrid = 256;
 constexpr int kJoinSeqs = 8;
 constexpr int kSmemCap = 227 * 1024;
@@ -72,10 +79,11 @@ struct TrunkParams {
     const char *rope_pool;
     const int32_t *block_table, *context_lens;
     PlanView plan;
-    float *qt;    // [B][H][RKT]: q~ * scale * log2 e, zero past r_k, then the rotary part
-    float *beta;  // [B][H]
-    float *part;  // run records, see record_of
-    int *pstart;  // [groups + B + 1]: pages of the nodes before each
+    uint16_t *qt;  // [B][H][3][RKT]: q~ * scale * log2 e as three bf16 parts, zero past r_k, then the rotary part
+    float *beta;   // [B][H]: q . mu^K * scale * log2 e
+    float *part;   // run records, see record_of
+    int *pstart;   // [groups + B]: pages of the nodes of the same kind before each; then the pages of either kind
+    int64_t leaf;  // first record of the leaf kernel
     unsigned *err;
 };
 
@@ -94,7 +102,7 @@ struct AbsorbParams {
 
 struct JoinParams {
     TrunkParams t;
-    int T, loop, io_bf16, grid, spb, d_rope;
+    int T, loop, io_bf16, grid, workers, spb, d_rope;
     float scale_log2;
     const void *w_up_v;  // [H][T][d][r_v]
     const float *mu_v;
@@ -139,10 +147,14 @@ __device__ __forceinline__ Node node_at(const TrunkParams &p, int groups, int i)
     return d;
 }
 
-// Record of query r of node d at head h, from CTA c: r_v latent values, the maximum, the sum.  The runs of a unit lie
-// kMembers records apart, and so no two of them meet: units and CTAs grow together.
+__device__ __forceinline__ bool is_leaf(const Node &d) { return d.n <= kLeaf; }
+
+// Record of the first query of node d at head h, from CTA (or leaf warp) c: r_v latent values, the maximum, the sum.  The
+// records of a unit's runs lie as far apart as a node of its kind can have queries, so that no two of them meet: units and
+// CTAs grow together.
 __device__ __forceinline__ int64_t record_of(const TrunkParams &p, const Node &d, int h, int c) {
-    return static_cast<int64_t>(p.H) * d.member + static_cast<int64_t>(h) * d.n + static_cast<int64_t>(kMembers) * c;
+    const int64_t at = static_cast<int64_t>(p.H) * d.member + static_cast<int64_t>(h) * d.n;
+    return is_leaf(d) ? p.leaf + at + static_cast<int64_t>(kLeaf) * c : at + static_cast<int64_t>(kMembers) * c;
 }
 __host__ __device__ constexpr int record_floats(int rv) { return rv + 4; }
 
@@ -150,7 +162,6 @@ __host__ __device__ constexpr int record_floats(int rv) { return rv + 4; }
 
 // One CTA: the prefix sums of the nodes' pages, and the flags of what node_at leaves out.
 __device__ void node_prefix(const TrunkParams &p) {
-    __shared__ int wsum[8];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int groups = count_groups(p), nodes = groups + p.B;
     const int cap = static_cast<int>(min(static_cast<int64_t>(p.max_ctx), static_cast<int64_t>(p.max_blocks) * kPT));
@@ -173,23 +184,50 @@ __device__ void node_prefix(const TrunkParams &p) {
         if (node_at(p, groups, g).pages == 0) bad |= LLA_DEVERR_SEQUENCE;
     if (bad) atomicOr(p.err, bad);
     const int per = (nodes + 255) / 256;
-    int tot = 0;
-    for (int i = tid * per; i < min(nodes, (tid + 1) * per); ++i) tot += node_at(p, groups, i).pages;
-    int x = tot;  // inclusive scan over the warp
+    int tot[2] = {0, 0};  // pages of the trunk's nodes, of the leaves
+    for (int i = tid * per; i < min(nodes, (tid + 1) * per); ++i) {
+        const Node d = node_at(p, groups, i);
+        if (is_leaf(d)) tot[1] += d.pages;
+        else tot[0] += d.pages;
+    }
+    __shared__ int wsum[2][8];
+    int x[2] = {tot[0], tot[1]};  // inclusive scans over the warp
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
+        const int y0 = __shfl_up_sync(0xffffffffu, x[0], o), y1 = __shfl_up_sync(0xffffffffu, x[1], o);
+        if (lane >= o) {
+            x[0] += y0;
+            x[1] += y1;
+        }
     }
-    if (lane == 31) wsum[warp] = x;
+    if (lane == 31) {
+        wsum[0][warp] = x[0];
+        wsum[1][warp] = x[1];
+    }
     __syncthreads();
-    int ex = x - tot;
-    for (int w = 0; w < warp; ++w) ex += wsum[w];
-    for (int i = tid * per; i < min(nodes, (tid + 1) * per); ++i) {
-        p.pstart[i] = ex;
-        ex += node_at(p, groups, i).pages;
+    int ex[2] = {x[0] - tot[0], x[1] - tot[1]};
+    for (int w = 0; w < warp; ++w) {
+        ex[0] += wsum[0][w];
+        ex[1] += wsum[1][w];
     }
-    if (tid == 255) p.pstart[nodes] = ex;
+    for (int i = tid * per; i < min(nodes, (tid + 1) * per); ++i) {
+        const Node d = node_at(p, groups, i);
+        int &e = is_leaf(d) ? ex[1] : ex[0];
+        p.pstart[i] = e;
+        e += d.pages;
+    }
+    if (tid == 255) {
+        p.pstart[nodes] = ex[0];
+        p.pstart[nodes + 1] = ex[1];
+    }
+}
+
+// v as three bf16 parts, `stride` apart.
+__device__ __forceinline__ void store_parts(uint16_t *dst, int stride, float v) {
+    float part[3];
+    bf16_parts(v, part);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) dst[k * stride] = __bfloat16_as_ushort(__float2bfloat16_rn(part[k]));
 }
 
 // Grid (H, RKX / 32 [+ 1 with a rotary branch], ceil(B / 16)), 256 threads = 32 columns x 8 slices of 16 rows: q~ of 32
@@ -223,9 +261,9 @@ __global__ void __launch_bounds__(256) absorb_kernel(const __grid_constant__ Abs
                 const int ia = a.pairing ? 2 * j : j, ic = a.pairing ? 2 * j + 1 : j + DR / 2;
                 const int64_t src = (static_cast<int64_t>(b) * p.H + h) * DR;
                 const float x = load_elem(a.q_rope, src + ia, a.io_bf16), y = load_elem(a.q_rope, src + ic, a.io_bf16);
-                float *dst = p.qt + (static_cast<int64_t>(b) * p.H + h) * RKT + RKX;
-                dst[ia] = (x * cs - y * sn) * a.scale_log2;
-                dst[ic] = (x * sn + y * cs) * a.scale_log2;
+                uint16_t *dst = p.qt + (static_cast<int64_t>(b) * p.H + h) * 3 * RKT + RKX;
+                store_parts(dst + ia, RKT, (x * cs - y * sn) * a.scale_log2);
+                store_parts(dst + ic, RKT, (x * sn + y * cs) * a.scale_log2);
             }
             return;
         }
@@ -256,7 +294,7 @@ __global__ void __launch_bounds__(256) absorb_kernel(const __grid_constant__ Abs
 #pragma unroll
         for (int sl = 0; sl < 8; ++sl) s += red[sl][bi][c];
         if (bi < nb && j0 + c < RKX)
-            p.qt[(static_cast<int64_t>(b0 + bi) * p.H + h) * RKT + j0 + c] = j0 + c < RK ? s * a.scale_log2 : 0.f;
+            store_parts(p.qt + (static_cast<int64_t>(b0 + bi) * p.H + h) * 3 * RKT + j0 + c, RKT, j0 + c < RK ? s * a.scale_log2 : 0.f);
     }
     if (blockIdx.y == 0) {
         for (int bi = warp; bi < nb; bi += 8) {
@@ -276,61 +314,71 @@ template <int RK, int RV, int DR>
 struct Z {
     static constexpr int RKX = (RK + 15) / 16 * 16;   // content contraction, zero-padded
     static constexpr int RKT = RKX + DR;              // with the rotary one
-    static constexpr int NCH = (RV + 127) / 128;      // chunks of O^T rows: 128, the last 64 if that holds it
-    static constexpr bool LAST64 = RV % 128 != 0 && RV % 128 <= 64;
+    static constexpr int RVX = (RV + 15) / 16 * 16;   // columns of O (a box reads zeros past r_v)
     static constexpr int NBOX = (RV + 63) / 64;       // TMA boxes of a V-plane
     static constexpr int BOX = kPT * 128;             // one: 64 rows x 128 bytes
     static constexpr int KPLANE = kPT * RK * 2, KPAD = kPT * RKX * 2, RPLANE = kPT * DR * 2;
     static constexpr int KPAGE = KPAD + RPLANE;
-    static constexpr int VPAGE = (LAST64 ? 2 * NCH - 1 : 2 * NCH) * BOX;
-    static constexpr int QB = 3 * kHalf * RKT * 2;    // q~ operand (one of two)
-    static constexpr int PB = kPT * 2 * kHalf * 2;    // P operand (one of two)
+    static constexpr int VPAGE = NBOX * BOX;
+    // TMEM columns: the parts of q~ (the third in shared memory where it does not fit), O, S of either group, P of either
+    // group (in the columns of its S where it does not fit: then S of its next page waits for O of this one)
+    static constexpr int PART = RKT / 2;
+    static constexpr int QT = 3 * PART + RVX + 4 * kPT / 2 + 2 * kPT / 2 <= 512 ? 3 : 2;
+    static constexpr bool ALIAS = QT * PART + RVX + 2 * kPT + kPT > 512;
+    static constexpr uint32_t TM_Q = 0, TM_O = QT * PART, TM_S = TM_O + RVX, TM_P = ALIAS ? TM_S : TM_S + 2 * kPT;
+    static constexpr uint32_t P_STEP = ALIAS ? kPT : kPT / 2;  // from one group's P to the other's
+    static constexpr uint32_t TM_COLS = 512;
+    static constexpr int QB = QT < 3 ? kRows * RKT * 2 : 0;  // the third part as an operand in shared memory
+    static constexpr int QROW = 3 * RKT * 2;                // bytes of a query's parts
+    static constexpr int XCOLS = RVX / 2, XROW = XCOLS + 4;  // columns of O exchanged at once, floats of their row
     static constexpr int NBAR = 40;
-    // floats: maxima [2][4][32], factors [32], sums [2][4][32], beta [4][32], states [2 slots][2][32]
-    static constexpr int RED = (256 + 32 + 256 + 128 + 128) * 4;
-    static constexpr int FIXED = 2 * QB + 2 * PB + RED + NBAR * 8 + kMaxNodes * 2 + 1024;
-    static constexpr int ST0 = (kSmemCap - 1024 - FIXED) / (KPAGE + VPAGE);
-    static constexpr int ST = ST0 > 4 ? 4 : ST0;
+    static constexpr int EXCH = 64 * XROW * 4;
+    static constexpr int RED = (kRows + 2 * 2 * 64 * 2) * 4;  // running maxima; maxima and sums of two runs and groups
+    static constexpr int FIXED = QB + EXCH + RED + NBAR * 8 + kMaxNodes * 2;
+    static constexpr int ST0 = (kSmemCap - 2048 - FIXED) / (KPAGE + VPAGE);
+    static constexpr int ST = ST0 > 5 ? 5 : ST0;
     static constexpr int oV = 0;
     static constexpr int oK = oV + ST * VPAGE;
     static constexpr int oQ = oK + ST * KPAGE;
-    static constexpr int oP = oQ + 2 * QB;
-    static constexpr int oRed = oP + 2 * PB;
+    static constexpr int oExch = oQ + QB;
+    static constexpr int oRed = oExch + EXCH;
     static constexpr int oBar = oRed + RED;
     static constexpr int oList = oBar + NBAR * 8;
     // (at least half of an SM's: one CTA per SM, which holds all of TMEM)
     static constexpr int SMEM0 = 1024 + oList + kMaxNodes * 2, SMEM = SMEM0 > 116 * 1024 ? SMEM0 : 116 * 1024;
-    static constexpr uint32_t TM_S = 3 * kHalf;             // columns of one S^T buffer
-    static constexpr uint32_t TM_O0 = 2 * TM_S, TM_O = NCH * 2 * kHalf, TM_COLS = 512;
-    static_assert(RKT % 16 == 0 && RV % 8 == 0 && NCH <= 2, "ranks");
-    static_assert(VPAGE == NBOX * BOX, "every box of a V stage is loaded");
+    static constexpr uint32_t IDESC_S = umma_idesc_bf16(kRows, kPT, 0, 0);
+    static constexpr uint32_t IDESC_O = umma_idesc_bf16(kRows, RVX, 0, 1);
+    static_assert(RKT % 16 == 0 && RV % 8 == 0 && RVX % 32 == 0, "ranks");
+    static_assert(TM_P + 2 * P_STEP <= TM_COLS && TM_S + 2 * kPT <= TM_COLS, "TMEM columns");
     static_assert(ST >= 2 && SMEM + 1024 <= kSmemCap, "shared memory");
-    static_assert(TM_O0 + 2 * TM_O <= TM_COLS, "TMEM columns");
 };
 
 // barrier indices
 enum {
-    bKfull = 0 /* [4] */, bKempty = 4, bVfull = 8, bVempty = 12, bSfull = 16 /* [2] */, bSfree = 18, bPfull = 20, bPfree = 22,
-    bQfull = 24, bQfree = 26, bOdone = 28, bOfree = 30, bMfull = 32, bAbort = 34, bTslot = 35, bBfull = 36 /* [4] */
+    bKfull = 0 /* [5] */, bKempty = 5, bVfull = 10, bVempty = 15, bSfull = 20 /* [2] */, bSfree = 22, bPfull = 24, bPfree = 26,
+    bQfull = 28, bQfree = 29, bOdone = 30, bOfree = 31 /* [2] */, bMfull = 33 /* [2] */, bAbort = 35, bTslot = 36
 };
 
-// A CTA's part of a unit.  Its queries are `subs` operands of up to 32, which take turns on every page.
+// A CTA's part of a unit.
 struct TrunkRun {
     Node d;
-    int h, page, pages, subs;  // page: the first in the table row
+    int h, page, pages;  // page: the first in the table row
 };
 
 struct Share {
-    int g0, g1;      // global pages of this CTA
-    int nodes, s;    // nodes in `list`, first global page of the first
+    int g0, g1;      // pages of this CTA, among all of the kind
+    int nodes, s;    // nodes in `list`, first page of the first
+    int np, we;      // all pages, and the workers that have some
 };
 
-// This CTA's share of the units' pages, and the nodes that it lies in: worked out from the inputs of the call by all threads,
-// so that the producer can start on the pages while the absorb kernel still runs.
-__device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list) {
-    __shared__ int wsum[kTrunkThreads / 32], wcnt[kTrunkThreads / 32], first;
+// This CTA's share of the pages of the leaves (LEAF) or of the other nodes, and the nodes that it lies in: worked out from the
+// inputs of the call by all threads, so that copies can start while the absorb kernel still runs.  The share is that of
+// workers w0 .. w0 + ws - 1 of `workers`.
+template <bool LEAF, int THREADS>
+__device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list, int w0, int ws, int workers) {
+    __shared__ int wsum[THREADS / 32], wcnt[THREADS / 32], first;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int nodes = groups + p.B, per = (nodes + kTrunkThreads - 1) / kTrunkThreads;
+    const int nodes = groups + p.B, per = (nodes + THREADS - 1) / THREADS;
     auto scan = [&](int v) {
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -339,25 +387,30 @@ __device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list) {
         }
         return v;
     };
+    auto pages = [&](int i) {
+        const Node d = node_at(p, groups, i);
+        return is_leaf(d) == LEAF ? d.pages * p.H : 0;
+    };
     int tot = 0;
-    for (int i = tid * per; i < min(nodes, (tid + 1) * per); ++i) tot += node_at(p, groups, i).pages * p.H;
+    for (int i = tid * per; i < min(nodes, (tid + 1) * per); ++i) tot += pages(i);
     const int x = scan(tot);
     if (lane == 31) wsum[warp] = x;
     __syncthreads();
     int ex0 = x - tot, np = 0;
-#pragma unroll
-    for (int w = 0; w < kTrunkThreads / 32; ++w) {
+    for (int w = 0; w < THREADS / 32; ++w) {
         if (w < warp) ex0 += wsum[w];
         np += wsum[w];
     }
-    // with fewer pages than CTAs the first np CTAs take one each
-    const int c = blockIdx.x, Ge = min(static_cast<int>(gridDim.x), np);
+    // with fewer pages than workers the first np take one each
+    const int we = min(workers, np);
     Share r;
-    r.g0 = c < Ge ? page_lo(c, np, Ge) : 0;
-    r.g1 = c < Ge ? page_lo(c + 1, np, Ge) : 0;
+    r.np = np;
+    r.we = we;
+    r.g0 = w0 < we ? page_lo(w0, np, we) : 0;
+    r.g1 = w0 < we ? page_lo(min(w0 + ws, we), np, we) : 0;
     int mine = 0, ex = ex0;
     for (int i = tid * per; i < min(nodes, (tid + 1) * per); ++i) {
-        const int n = node_at(p, groups, i).pages * p.H;
+        const int n = pages(i);
         mine += n > 0 && ex < r.g1 && ex + n > r.g0;
         ex += n;
     }
@@ -366,14 +419,13 @@ __device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list) {
     __syncthreads();
     int at = y - mine;
     r.nodes = 0;
-#pragma unroll
-    for (int w = 0; w < kTrunkThreads / 32; ++w) {
+    for (int w = 0; w < THREADS / 32; ++w) {
         if (w < warp) at += wcnt[w];
         r.nodes += wcnt[w];
     }
     ex = ex0;
     for (int i = tid * per; mine > 0 && i < min(nodes, (tid + 1) * per); ++i) {
-        const int n = node_at(p, groups, i).pages * p.H;
+        const int n = pages(i);
         if (n > 0 && ex < r.g1 && ex + n > r.g0) {
             if (at == 0) first = ex;
             list[at++] = static_cast<uint16_t>(i);
@@ -385,204 +437,71 @@ __device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list) {
     return r;
 }
 
-// f(run) for every run of the share, in order, until it says false.
-template <typename F>
-__device__ __forceinline__ void for_runs(const TrunkParams &p, int groups, const Share &sh, const uint16_t *list, F f) {
-    int s = sh.s;
-    for (int i = 0; i < sh.nodes; ++i) {
-        TrunkRun r;
-        r.d = node_at(p, groups, list[i]);
-        r.subs = r.d.n > kHalf ? 2 : 1;
-        const int end = s + r.d.pages * p.H;
-        int u = max(sh.g0, s) - s;  // page of the node, head by head
-        const int stop = min(sh.g1, end) - s;
-        r.h = u / r.d.pages;
-        int in = u - r.h * r.d.pages;
-        for (; u < stop; ++r.h) {
-            r.pages = min(stop - u, r.d.pages - in);
-            r.page = r.d.first + in;
-            if (!f(r)) return;
-            u += r.pages;
-            in = 0;
-        }
-        s = end;
+// The runs of a share, in order.
+struct RunWalk {
+    const TrunkParams &p;
+    const uint16_t *list;
+    int groups, g0, g1, nodes, i, s, u, stop, in;  // node i of the list starts at page s; u: page of the node, head by head
+    TrunkRun r;
+    __device__ __forceinline__ RunWalk(const TrunkParams &pp, int gr, const Share &sh, const uint16_t *l)
+        : p(pp), list(l), groups(gr), g0(sh.g0), g1(sh.g1), nodes(sh.nodes), i(-1), s(sh.s), u(0), stop(0), in(0) {
+        r.pages = 0;
+        r.d.pages = 0;
     }
+    // The next run, or false behind the last.
+    __device__ __forceinline__ bool next() {
+        u += r.pages;
+        if (u < stop) {
+            ++r.h;
+            in = 0;
+        } else {
+            do {
+                if (i >= 0) s += r.d.pages * p.H;
+                if (++i >= nodes || s >= g1) {
+                    r.pages = 0;
+                    r.d.pages = 0;
+                    i = nodes;
+                    u = stop = 0;
+                    return false;
+                }
+                r.d = node_at(p, groups, list[i]);
+            } while (s + r.d.pages * p.H <= g0);  // (a warp's part of a CTA's share may start behind its first nodes)
+            u = max(g0, s) - s;
+            stop = min(g1, s + r.d.pages * p.H) - s;
+            r.h = u / r.d.pages;
+            in = u - r.h * r.d.pages;
+        }
+        r.pages = min(stop - u, r.d.pages - in);
+        r.page = r.d.first + in;
+        return true;
+    }
+};
+
+// The parts of query i of a run, or NULL where it has none.
+template <int QROW>
+__device__ __forceinline__ const char *query_parts(const TrunkParams &p, const TrunkRun &r, int i) {
+    if (i >= r.d.n) return nullptr;
+    int b = r.d.row;
+    if (r.d.member < kLevels * p.B) b = p.plan.members[r.d.member + i];
+    if (b < 0 || b >= p.B) return nullptr;
+    return reinterpret_cast<const char *>(p.qt) + (static_cast<int64_t>(b) * p.H + r.h) * QROW;
 }
 
 // A value that every lane has, for a warp that issues products (their descriptors are in uniform registers then).
 __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
-
-struct TrunkCtx {
-    char *sm;
-    uint64_t *bar;
-    volatile int *abort_flag;
-    float *red, *factor, *lsum, *beta, *state;
-    unsigned *err;
-};
-
-// The softmax warps' part of one run with NQ query slots in each of SUBS operands.  Lane l of warp w holds the scores of
-// tokens 16 w + l / 4 (+ 8) for the queries 8 k + 2 (l % 4) (+ 1) of every operand.
-template <typename ZZ, int NQ, int SUBS>
-__device__ __forceinline__ void softmax_run(const TrunkCtx &x, const TrunkRun &r, int &it, int &pgs, int sr) {
-    constexpr int NV = NQ / 4, NP = 2 * NQ;  // values of a token in a thread, rows of P
-    const int tid = threadIdx.x - 32 * kSoftmaxWarp, w = tid >> 5, lane = tid & 31, l4 = lane >> 2, c2 = 2 * (lane & 3);
-    const uint32_t tl = static_cast<uint32_t>(32 * w) << 16;
-    auto query = [&](int v) { return 8 * (v >> 1) + c2 + (v & 1); };
-    float beta[SUBS][NV], m[SUBS][NV], acc[SUBS][NV];
-#pragma unroll
-    for (int j = 0; j < SUBS; ++j) {
-        mbar_wait(&x.bar[bBfull + ((sr + j) & 3)], ((sr + j) >> 2) & 1, x.abort_flag, x.err);
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            beta[j][v] = x.beta[((sr + j) & 3) * kHalf + query(v)];
-            m[j][v] = -INFINITY;
-            acc[j][v] = 0.f;
-        }
-    }
-    for (int k = 0; k < r.pages; ++k, ++pgs) {
-        const int left = r.d.len - (r.page + k) * kPT;  // tokens of the page that are there (more than a page: all)
-#pragma unroll
-        for (int j = 0; j < SUBS; ++j, ++it) {
-            const int s = it & 1;
-            mbar_wait(&x.bar[bSfull + s], (it >> 1) & 1, x.abort_flag, x.err);
-            tc_fence_after();
-            float raw[3][2 * NV];
-            const uint32_t ts = tl + s * ZZ::TM_S;
-            tmem_ld16x256_three(ts, ts + NQ, ts + 2 * NQ, raw);
-            tc_fence_before();
-            mbar_arrive(&x.bar[bSfree + s]);
-            float sc[2][NV];
-            bool mine = false;
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const bool valid = 16 * w + l4 + 8 * t < left;
-#pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    const int i = 4 * (v >> 1) + 2 * t + (v & 1);
-                    sc[t][v] = valid ? (raw[0][i] + raw[1][i]) + (raw[2][i] + beta[j][v]) : -INFINITY;
-                    mine = mine || sc[t][v] > m[j][v] + kRescaleLog2;
-                }
-            }
-            // most pages raise no query's maximum by 2^8: one barrier that also votes tells all four warps so
-            if (named_bar_or(1, 128, mine)) {
-                float *rp = x.red + s * 128;
-#pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    float mx = fmaxf(sc[0][v], sc[1][v]);
-#pragma unroll
-                    for (int o = 4; o <= 16; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-                    if (l4 == 0) rp[w * kHalf + query(v)] = mx;
-                }
-                named_bar_sync(1, 128);
-#pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    float mx = m[j][v];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, rp[i * kHalf + query(v)]);
-                    const bool grows = mx > m[j][v] + kRescaleLog2;  // also the first page
-                    const float f = grows ? ex2_approx(m[j][v] - mx) : 1.f;
-                    if (grows) {
-                        acc[j][v] *= f;
-                        m[j][v] = mx;
-                    }
-                    if (w == 0 && l4 == 0) x.factor[query(v)] = f;
-                }
-                named_bar_sync(1, 128);
-                if (k > 0) {
-                    // O^T holds pages up to the one before of this run (the last product issued has released its P buffer;
-                    // the one before it had released the other before this warp wrote the last P): scale its columns
-                    mbar_wait(&x.bar[bPfree + ((it - 1) & 1)], ((it - 1) >> 1) & 1, x.abort_flag, x.err);
-                    tc_fence_after();
-#pragma unroll
-                    for (int i = 0; i < ZZ::NCH * NP / 16; ++i) {
-                        const uint32_t col = ZZ::TM_O0 + ((sr + j) & 1) * ZZ::TM_O + (i / (NP / 16)) * (2 * kHalf) + (i % (NP / 16)) * 16;
-                        float o[16];
-                        tmem_ld16(tl + col, o);
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] *= x.factor[((i % (NP / 16)) * 16 + e) % NQ];
-                        tmem_st16(tl + col, o);
-                    }
-                }
-            }
-            if (it >= 2) mbar_wait(&x.bar[bPfree + s], ((it - 2) >> 1) & 1, x.abort_flag, x.err);
-            // P as a K-major operand: row part NQ + query, tokens 8 g .. 8 g + 7 at g NP 16 + row 16
-            char *pp = x.sm + ZZ::oP + s * ZZ::PB + l4 * 2;
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    const float pv = ex2_approx(sc[t][v] - m[j][v]);
-                    acc[j][v] += pv;
-                    float part[2];
-                    bf16_parts(pv, part);
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        *reinterpret_cast<uint16_t *>(pp + (2 * w + t) * (NP * 16) + (i * NQ + query(v)) * 16) =
-                            __bfloat16_as_ushort(__float2bfloat16_rn(part[i]));
-                }
-            if (SUBS == 1 && left < kPT) {
-                // V rows past the sequence hold no latents: zero them (0 * NaN would poison O^T)
-                const int st = pgs % ZZ::ST;
-                mbar_wait(&x.bar[bVfull + st], (pgs / ZZ::ST) & 1, x.abort_flag, x.err);
-                char *vs = x.sm + ZZ::oV + st * ZZ::VPAGE;
-                for (int i = tid; i < (kPT - left) * ZZ::NBOX * 8; i += 128) {
-                    const int chunk = i & 7, box = (i >> 3) % ZZ::NBOX, row = left + (i >> 3) / ZZ::NBOX;
-                    *reinterpret_cast<uint4 *>(vs + box * ZZ::BOX + row * 128 + chunk * 16) = make_uint4(0, 0, 0, 0);
-                }
-            }
-            fence_proxy_async_smem();
-            tc_fence_before();
-            mbar_arrive(&x.bar[bPfull + s]);
-        }
-    }
-    // the run's maxima and sums, for the epilogue
-#pragma unroll
-    for (int j = 0; j < SUBS; ++j) {
-        const int slot = (sr + j) & 1;
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            float a = acc[j][v];
-#pragma unroll
-            for (int o = 4; o <= 16; o <<= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
-            if (l4 == 0) x.lsum[(j * 4 + w) * kHalf + query(v)] = a;
-        }
-        if (sr + j >= 2) mbar_wait(&x.bar[bOfree + slot], ((sr + j - 2) >> 1) & 1, x.abort_flag, x.err);
-        if (w == 0 && l4 == 0) {
-#pragma unroll
-            for (int v = 0; v < NV; ++v) x.state[slot * 2 * kHalf + query(v)] = m[j][v];
-        }
-    }
-    named_bar_sync(1, 128);
-#pragma unroll
-    for (int j = 0; j < SUBS; ++j) {
-        const int slot = (sr + j) & 1;
-        if (tid < NQ) {
-            const float *ls = x.lsum + j * 4 * kHalf + tid;
-            x.state[slot * 2 * kHalf + kHalf + tid] = (ls[0] + ls[kHalf]) + (ls[2 * kHalf] + ls[3 * kHalf]);
-        }
-        mbar_arrive(&x.bar[bMfull + slot]);
-    }
-}
 
 template <int RK, int RV, int DR>
 __global__ void __launch_bounds__(kTrunkThreads, 1)
     trunk_kernel(const __grid_constant__ CUtensorMap tv, const __grid_constant__ TrunkParams p) {
     using ZZ = Z<RK, RV, DR>;
     extern __shared__ __align__(1024) char sm_raw[];
-    TrunkCtx x;
-    x.sm = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(sm_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    x.bar = reinterpret_cast<uint64_t *>(x.sm + ZZ::oBar);
-    x.abort_flag = reinterpret_cast<volatile int *>(x.bar + bAbort);
-    x.red = reinterpret_cast<float *>(x.sm + ZZ::oRed);
-    x.factor = x.red + 256;
-    x.lsum = x.factor + 32;
-    x.beta = x.lsum + 256;
-    x.state = x.beta + 128;
-    x.err = p.err;
-    uint32_t *tslot = reinterpret_cast<uint32_t *>(x.bar + bTslot);
-    uint16_t *list = reinterpret_cast<uint16_t *>(x.sm + ZZ::oList);
-    char *sm = x.sm;
-    uint64_t *bar = x.bar;
+    char *sm = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(sm_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    uint64_t *bar = reinterpret_cast<uint64_t *>(sm + ZZ::oBar);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(bar + bAbort);
+    uint32_t *tslot = reinterpret_cast<uint32_t *>(bar + bTslot);
+    float *running = reinterpret_cast<float *>(sm + ZZ::oRed);          // [128] maxima
+    float2 *states = reinterpret_cast<float2 *>(running + kRows);       // [2 runs][2 groups][64] maxima and sums
+    uint16_t *list = reinterpret_cast<uint16_t *>(sm + ZZ::oList);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
     if (tid == 0) {
@@ -597,14 +516,13 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
             mbar_init(&bar[bSfree + s], 128);
             mbar_init(&bar[bPfull + s], 128);
             mbar_init(&bar[bPfree + s], 1);
-            mbar_init(&bar[bQfull + s], 32);
-            mbar_init(&bar[bQfree + s], 1);
-            mbar_init(&bar[bOdone + s], 1);
             mbar_init(&bar[bOfree + s], 128);
-            mbar_init(&bar[bMfull + s], 128);
+            mbar_init(&bar[bMfull + s], 256);
         }
-        for (int s = 0; s < 4; ++s) mbar_init(&bar[bBfull + s], 32);
-        *x.abort_flag = 0;
+        mbar_init(&bar[bQfull], 128);
+        mbar_init(&bar[bQfree], 1);
+        mbar_init(&bar[bOdone], 1);
+        *abort_flag = 0;
         fence_mbar_init();
     }
     if (warp == 1) tmem_alloc(tslot, ZZ::TM_COLS);
@@ -619,236 +537,344 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
     tc_fence_after();
     constexpr uint32_t tmem = 0;  // the whole of TMEM is allocated (one CTA per SM)
     const int groups = count_groups(p);
-    const Share sh = find_share(p, groups, list);
+    const Share sh = find_share<false, kTrunkThreads>(p, groups, list, blockIdx.x, 1, gridDim.x);
     // q~ and beta come from the absorb kernel, and the workspace is free once it has waited for the kernel before it; the
-    // producer reads only inputs of the call, which that kernel's wait ordered before this launch, and waits at its end
-    if (warp != 0) pdl_wait();
+    // producers read only inputs of the call, which that kernel's wait ordered before this launch, and wait at their end
+    if (warp != 0 && warp != 2) {
+        pdl_wait();
+        pdl_trigger();  // the leaf kernel may take this SM as soon as this CTA has left it
+    }
+    RunWalk w(p, groups, sh, list);
 
-    if (warp == 0) {
-        // ------------------------------------------------------------------------------- producer
+    if (warp == 0 || warp == 2) {
+        // ------------------------------------------------------------------------------ producers
         if (lane == 0) {
             // after a failed wait (or once the abort flag is up) no further copy is issued, so no full barrier receives a
             // second arrival in one phase; the last ST rounds issued are awaited below
+            const int full = warp == 0 ? bKfull : bVfull, empty = warp == 0 ? bKempty : bVempty;
             const uint64_t pol = policy_evict_first();
-            int itk = 0, itv = 0;
-            for_runs(p, groups, sh, list, [&](const TrunkRun &r) {
-                const int32_t *bt = p.block_table + static_cast<int64_t>(r.d.row) * p.max_blocks + r.page;
-                for (int k = 0; k < r.pages; ++k) {
-                    const int st = itk % ZZ::ST;
-                    const uint32_t ph = (itk / ZZ::ST) & 1;
+            int it = 0;
+            bool stop = false;
+            while (!stop && w.next()) {
+                const int32_t *bt = p.block_table + static_cast<int64_t>(w.r.d.row) * p.max_blocks + w.r.page;
+                for (int k = 0; k < w.r.pages; ++k, ++it) {
+                    const int st = it % ZZ::ST;
                     int32_t blk = bt[k];
                     if (blk < 0 || blk >= p.num_blocks) {
                         atomicOr(p.err, LLA_DEVERR_BLOCK_ID);
                         blk = 0;
                     }
-                    const int64_t page = static_cast<int64_t>(blk) * p.H + r.h;
-                    if (!mbar_wait(&bar[bKempty + st], ph ^ 1u, x.abort_flag, p.err) || *x.abort_flag) return false;
-                    mbar_arrive_expect_tx(&bar[bKfull + st], ZZ::KPLANE + ZZ::RPLANE);
-                    char *ks = sm + ZZ::oK + st * ZZ::KPAGE;
-                    bulk_g2s(ks, p.pool + page * p.page_bytes, ZZ::KPLANE, &bar[bKfull + st], pol);
-                    if constexpr (DR > 0)
-                        bulk_g2s(ks + ZZ::KPAD, p.rope_pool + static_cast<int64_t>(blk) * ZZ::RPLANE, ZZ::RPLANE, &bar[bKfull + st], pol);
-                    ++itk;
-                    if (!mbar_wait(&bar[bVempty + st], ph ^ 1u, x.abort_flag, p.err) || *x.abort_flag) return false;
-                    mbar_arrive_expect_tx(&bar[bVfull + st], ZZ::VPAGE);
-                    char *vs = sm + ZZ::oV + st * ZZ::VPAGE;
+                    const int64_t page = static_cast<int64_t>(blk) * p.H + w.r.h;
+                    if (!mbar_wait(&bar[empty + st], ((it / ZZ::ST) & 1) ^ 1u, abort_flag, p.err) || *abort_flag) {
+                        stop = true;
+                        break;
+                    }
+                    if (warp == 0) {
+                        mbar_arrive_expect_tx(&bar[bKfull + st], ZZ::KPLANE + ZZ::RPLANE);
+                        char *ks = sm + ZZ::oK + st * ZZ::KPAGE;
+                        bulk_g2s(ks, p.pool + page * p.page_bytes, ZZ::KPLANE, &bar[bKfull + st], pol);
+                        if constexpr (DR > 0)
+                            bulk_g2s(ks + ZZ::KPAD, p.rope_pool + static_cast<int64_t>(blk) * ZZ::RPLANE, ZZ::RPLANE, &bar[bKfull + st], pol);
+                    } else {
+                        mbar_arrive_expect_tx(&bar[bVfull + st], ZZ::VPAGE);
+                        char *vs = sm + ZZ::oV + st * ZZ::VPAGE;
 #pragma unroll
-                    for (int a = 0; a < ZZ::NBOX; ++a)
-                        tma_load_3d(vs + a * ZZ::BOX, &tv, a * 64, 0, static_cast<int>(page), &bar[bVfull + st]);
-                    ++itv;
+                        for (int a = 0; a < ZZ::NBOX; ++a)
+                            tma_load_3d(vs + a * ZZ::BOX, &tv, a * 64, 0, static_cast<int>(page), &bar[bVfull + st]);
+                    }
                 }
-                return true;
-            });
+            }
             // every copy has landed before the CTA can exit, even after an abort
             volatile int never = 0;
-            for (int j = max(0, itk - ZZ::ST); j < itk; ++j) mbar_wait(&bar[bKfull + j % ZZ::ST], (j / ZZ::ST) & 1, &never, p.err);
-            for (int j = max(0, itv - ZZ::ST); j < itv; ++j) mbar_wait(&bar[bVfull + j % ZZ::ST], (j / ZZ::ST) & 1, &never, p.err);
+            for (int j = max(0, it - ZZ::ST); j < it; ++j) mbar_wait(&bar[full + j % ZZ::ST], (j / ZZ::ST) & 1, &never, p.err);
         }
         __syncwarp();
         pdl_wait();
     } else if (warp == 1) {
-        // ----------------------------------------------------------------------------- S^T issuer
+        // ------------------------------------------------------------------------------- S issuer
         const uint32_t base = smem_addr(sm);
         const uint64_t dk0 = umma_desc(base + ZZ::oK, kPT * 16, 128);
-        int it = 0, pgs = 0, sr = 0;
-        auto run = [&](int pages, int subs, int nq) {
-            const uint32_t idesc = umma_idesc_bf16(64, 3 * nq, 0, 0);
-            for (int k = 0; k < pages; ++k, ++pgs) {
-                const int st = pgs % ZZ::ST;
+        [[maybe_unused]] const uint64_t dq = umma_desc(base + ZZ::oQ, kRows * 16, 128);
+        int it = 0;
+        for (int run = 0; uniform(w.next()); ++run) {
+            const int pages = uniform(w.r.pages);
+            mbar_wait_warp(&bar[bQfull], run & 1, abort_flag, p.err);
+            for (int k = 0; k < pages; ++k, ++it) {
+                const int g = it & 1, st = it % ZZ::ST;
+                mbar_wait_warp(&bar[bKfull + st], (it / ZZ::ST) & 1, abort_flag, p.err);
+                if (it >= 2) mbar_wait_warp(&bar[(ZZ::ALIAS ? bPfree : bSfree) + g], ((it >> 1) - 1) & 1, abort_flag, p.err);
+                tc_fence_after();
                 const uint64_t dk = dk0 + static_cast<uint64_t>((st * ZZ::KPAGE) >> 4);
-                for (int j = 0; j < subs; ++j, ++it) {
-                    const int s = it & 1, slot = (sr + j) & 1;
-                    if (k == 0) mbar_wait_warp(&bar[bQfull + slot], ((sr + j) >> 1) & 1, x.abort_flag, p.err);
-                    if (j == 0) mbar_wait_warp(&bar[bKfull + st], (pgs / ZZ::ST) & 1, x.abort_flag, p.err);
-                    if (it >= 2) mbar_wait_warp(&bar[bSfree + s], ((it - 2) >> 1) & 1, x.abort_flag, p.err);
-                    tc_fence_after();
-                    const uint64_t dq = umma_desc(base + ZZ::oQ + slot * ZZ::QB, 3 * nq * 16, 128);
+                const uint32_t ts = tmem + ZZ::TM_S + g * kPT;
 #pragma unroll
-                    for (int ks = 0; ks < ZZ::RKT / 16; ++ks)
-                        umma_bf16_warp(tmem + s * ZZ::TM_S, dk + ks * ((2 * kPT * 16) >> 4), dq + ks * ((2 * 3 * nq * 16) >> 4), idesc, ks > 0);
-                    if (k == pages - 1) umma_commit_warp(&bar[bQfree + slot]);
-                    if (j == subs - 1) umma_commit_warp(&bar[bKempty + st]);
-                    umma_commit_warp(&bar[bSfull + s]);
-                }
+                for (int part = 0; part < 3; ++part)
+#pragma unroll
+                    for (int ks = 0; ks < ZZ::RKT / 16; ++ks) {
+                        if (part < ZZ::QT)
+                            umma_bf16_ts_warp(ts, tmem + ZZ::TM_Q + part * ZZ::PART + ks * 8, dk + ks * ((2 * kPT * 16) >> 4), ZZ::IDESC_S,
+                                              part > 0 || ks > 0);
+                        else
+                            umma_bf16_warp(ts, dq + ks * ((2 * kRows * 16) >> 4), dk + ks * ((2 * kPT * 16) >> 4), ZZ::IDESC_S, true);
+                    }
+                if (k == pages - 1) umma_commit_warp(&bar[bQfree]);
+                umma_commit_warp(&bar[bKempty + st]);
+                umma_commit_warp(&bar[bSfull + g]);
             }
-            sr += subs;
-        };
-        for_runs(p, groups, sh, list, [&](const TrunkRun &r) {
-            run(uniform(r.pages), uniform(r.subs), uniform(r.d.n) <= kFew ? kFew : kHalf);
-            return true;
-        });
+        }
         // every product has completed before TMEM is released, even after an abort: the last commit on each buffer
         volatile int never = 0;
         for (int j = max(0, it - 2); j < it; ++j) mbar_wait_warp(&bar[bSfull + (j & 1)], (j >> 1) & 1, &never, p.err);
         __syncwarp();
-    } else if (warp == kValueWarp) {
-        // ----------------------------------------------------------------------------- O^T issuer
+    } else if (warp == 3) {
+        // ------------------------------------------------------------------------------- O issuer
         const uint32_t base = smem_addr(sm);
         const uint64_t dv0 = umma_desc_sw128_mn(base + ZZ::oV, ZZ::BOX);
-        int it = 0, pgs = 0, sr = 0;
-        for_runs(p, groups, sh, list, [&](const TrunkRun &r) {
-            const int pages = uniform(r.pages), subs = uniform(r.subs), np = 2 * (uniform(r.d.n) <= kFew ? kFew : kHalf);
-            const uint32_t idesc = umma_idesc_bf16(128, np, 1, 0), idesc64 = umma_idesc_bf16(64, np, 1, 0);
-            for (int k = 0; k < pages; ++k, ++pgs) {
-                const int st = pgs % ZZ::ST;
-                const uint64_t dv = dv0 + static_cast<uint64_t>((st * ZZ::VPAGE) >> 4);
-                for (int j = 0; j < subs; ++j, ++it) {
-                    const int s = it & 1, slot = (sr + j) & 1;
-                    mbar_wait_warp(&bar[bPfull + s], (it >> 1) & 1, x.abort_flag, p.err);
-                    if (j == 0) mbar_wait_warp(&bar[bVfull + st], (pgs / ZZ::ST) & 1, x.abort_flag, p.err);
-                    // the first page of a run starts O^T anew, once the epilogue has read the run before the last
-                    if (k == 0 && sr + j >= 2) mbar_wait_warp(&bar[bOfree + slot], ((sr + j - 2) >> 1) & 1, x.abort_flag, p.err);
-                    tc_fence_after();
-                    const uint64_t dp = umma_desc(base + ZZ::oP + s * ZZ::PB, np * 16, 128);
-#pragma unroll
-                    for (int ch = 0; ch < ZZ::NCH; ++ch)
-#pragma unroll
-                        for (int ks = 0; ks < kPT / 16; ++ks)
-                            umma_bf16_warp(tmem + ZZ::TM_O0 + slot * ZZ::TM_O + ch * (2 * kHalf), dv + ((ch * 2 * ZZ::BOX + ks * 2048) >> 4),
-                                           dp + ks * ((2 * np * 16) >> 4), ZZ::LAST64 && ch == ZZ::NCH - 1 ? idesc64 : idesc, k > 0 || ks > 0);
-                    if (j == subs - 1) umma_commit_warp(&bar[bVempty + st]);
-                    if (k == pages - 1) umma_commit_warp(&bar[bOdone + slot]);
-                    umma_commit_warp(&bar[bPfree + s]);  // also: O^T holds pages up to it
-                }
-            }
-            sr += subs;
-            return true;
-        });
-        if (it > 0) {  // every product has completed before TMEM is released, even after an abort
-            volatile int never = 0;
-            mbar_wait_warp(&bar[bPfree + ((it - 1) & 1)], ((it - 1) >> 1) & 1, &never, p.err);
-        }
-        __syncwarp();
-    } else if (warp == kQueryWarp) {
-        // ---------------------------------------------------------------------------- q~ operands
-        int sr = 0;
-        for_runs(p, groups, sh, list, [&](const TrunkRun &r) {
-            const int nq = r.d.n <= kFew ? kFew : kHalf;
-            for (int j = 0; j < r.subs; ++j, ++sr) {
-                const int slot = sr & 1;
-                if (sr >= 2) mbar_wait(&bar[bQfree + slot], ((sr - 2) >> 1) & 1, x.abort_flag, p.err);
-                auto seq = [&](int n) {  // the sequence of query n of this operand, or none
-                    const int i = j * kHalf + n;
-                    if (i >= r.d.n) return -1;
-                    if (r.d.member >= kLevels * p.B) return r.d.row;
-                    const int b = p.plan.members[r.d.member + i];
-                    return b < 0 || b >= p.B ? -1 : b;
-                };
-                // row part nq + n is bf16 part `part` of q~_n; its granule g lies at g (3 nq 16) + row 16
-                for (int i = lane; i < nq * (ZZ::RKT / 8); i += 32) {
-                    const int n = i / (ZZ::RKT / 8), g = i - n * (ZZ::RKT / 8), b = seq(n);
-                    float part[3][8];
-#pragma unroll
-                    for (int k = 0; k < 3; ++k)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) part[k][e] = 0.f;
-                    if (b >= 0) {
-                        const float4 *src = reinterpret_cast<const float4 *>(p.qt + (static_cast<int64_t>(b) * p.H + r.h) * ZZ::RKT) + 2 * g;
-                        const float4 u0 = src[0], u1 = src[1];
-                        const float v[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w};
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            float pe[3];
-                            bf16_parts(v[e], pe);
-#pragma unroll
-                            for (int k = 0; k < 3; ++k) part[k][e] = pe[k];
-                        }
-                    }
-                    char *dq = sm + ZZ::oQ + slot * ZZ::QB + g * (3 * nq * 16);
-#pragma unroll
-                    for (int k = 0; k < 3; ++k)
-                        *reinterpret_cast<uint4 *>(dq + (k * nq + n) * 16) =
-                            make_uint4(pack_bf16x2(part[k][0], part[k][1]), pack_bf16x2(part[k][2], part[k][3]),
-                                       pack_bf16x2(part[k][4], part[k][5]), pack_bf16x2(part[k][6], part[k][7]));
-                }
-                // Four slots of beta, each with its barrier: while S^T of a run of one page is issued the softmax warps may still
-                // be a run behind.  They have read the slot that is written: S^T of operand sr - 2, which has been waited for,
-                // needed the buffer of the page two before it, and so one of operand sr - 4 or behind.
-                if (lane < nq) {
-                    const int b = seq(lane);
-                    x.beta[(sr & 3) * kHalf + lane] = b >= 0 ? p.beta[static_cast<int64_t>(b) * p.H + r.h] : 0.f;
-                }
-                mbar_arrive(&bar[bBfull + (sr & 3)]);
-                fence_proxy_async_smem();
-                mbar_arrive(&bar[bQfull + slot]);
-            }
-            return true;
-        });
-    } else if (warp < kEpilogueWarp) {
-        // ------------------------------------------------------------------------ softmax, warps 4-7
-        int it = 0, pgs = 0, sr = 0;
-        for_runs(p, groups, sh, list, [&](const TrunkRun &r) {
-            if (r.d.n <= kFew) softmax_run<ZZ, kFew, 1>(x, r, it, pgs, sr);
-            else if (r.subs == 1) softmax_run<ZZ, kHalf, 1>(x, r, it, pgs, sr);
-            else softmax_run<ZZ, kHalf, 2>(x, r, it, pgs, sr);
-            sr += r.subs;
-            return true;
-        });
-    } else {
-        // ----------------------------------------------------------------------- epilogue, warps 8-11
-        constexpr int RS = record_floats(RV);
-        const int w = warp & 3, et = tid - 32 * kEpilogueWarp;
-        const uint32_t tl = static_cast<uint32_t>(32 * w) << 16;
-        int sr = 0;
-        for_runs(p, groups, sh, list, [&](const TrunkRun &r) {
-            for (int j = 0; j < r.subs; ++j, ++sr) {
-                const int slot = sr & 1, n = min(kHalf, r.d.n - j * kHalf);
-                mbar_wait(&bar[bOdone + slot], (sr >> 1) & 1, x.abort_flag, p.err);
-                mbar_wait(&bar[bMfull + slot], (sr >> 1) & 1, x.abort_flag, p.err);
+        int it = 0;
+        for (int run = 0; uniform(w.next()); ++run) {
+            const int pages = uniform(w.r.pages);
+            for (int k = 0; k < pages; ++k, ++it) {
+                const int g = it & 1, st = it % ZZ::ST;
+                mbar_wait_warp(&bar[bVfull + st], (it / ZZ::ST) & 1, abort_flag, p.err);
+                mbar_wait_warp(&bar[bPfull + g], (it >> 1) & 1, abort_flag, p.err);
+                // the first page of a run starts O anew, once the run before has been read
+                if (k == 0 && run > 0) mbar_wait_warp(&bar[bOfree + ((run - 1) & 1)], ((run - 1) >> 1) & 1, abort_flag, p.err);
                 tc_fence_after();
-                float *dst = p.part + (record_of(p, r.d, r.h, blockIdx.x) + j * kHalf) * RS;
+                const uint64_t dv = dv0 + static_cast<uint64_t>((st * ZZ::VPAGE) >> 4);
 #pragma unroll
-                for (int ch = 0; ch < ZZ::NCH; ++ch) {
-                    const bool half = ZZ::LAST64 && ch == ZZ::NCH - 1;  // 16 rows in each quarter of the lanes
-                    const int row = ch * 128 + (half ? 16 : 32) * w + lane;
-                    const bool mine = row < RV && (!half || lane < 16);
-                    const uint32_t to = tl + ZZ::TM_O0 + slot * ZZ::TM_O + ch * (2 * kHalf);
-                    if (r.d.n <= kFew) {
-                        float o[16];
-                        tmem_ld16(to, o);
+                for (int ks = 0; ks < kPT / 16; ++ks)
+                    umma_bf16_ts_warp(tmem + ZZ::TM_O, tmem + ZZ::TM_P + g * ZZ::P_STEP + ks * 8, dv + ks * (2048 >> 4), ZZ::IDESC_O, k > 0 || ks > 0);
+                umma_commit_warp(&bar[bVempty + st]);
+                if (k == pages - 1) umma_commit_warp(&bar[bOdone]);
+                umma_commit_warp(&bar[bPfree + g]);  // also: O holds pages up to it
+            }
+        }
+        // every product has completed before TMEM is released, even after an abort
+        volatile int never = 0;
+        for (int j = max(0, it - 2); j < it; ++j) mbar_wait_warp(&bar[bPfree + (j & 1)], (j >> 1) & 1, &never, p.err);
+        __syncwarp();
+    } else if (warp < kAuxWarp) {
+        // ------------------------------------------------------------------- softmax, warps 4-7 and 8-11
+        const int g = (warp - kSoftmaxWarp) >> 2, quarter = warp & 3, row = 32 * quarter + lane;
+        const bool second = quarter >= 2;  // rows 64 + q: the second part of p
+        const uint32_t tl = tmem + (static_cast<uint32_t>(32 * quarter) << 16);
+        const uint32_t ts = tl + ZZ::TM_S + g * kPT, tp = tl + ZZ::TM_P + g * ZZ::P_STEP;
+        const int total = sh.g1 - sh.g0;
+        int it = 0;
+        for (int run = 0; w.next(); ++run) {
+            // warps whose queries the run does not have only keep step
+            const bool active = (quarter & 1) == 0 || w.r.d.n > 32;
+            float m = -INFINITY, l = 0.f;
+            const int end = it + w.r.pages;
+            for (int j = it + ((it ^ g) & 1); j < end; j += 2) {
+                const int jj = j >> 1, k = j - it;
+                const int left = w.r.d.len - (w.r.page + k) * kPT;  // tokens of the page that are there (more than a page: all)
+                mbar_wait(&bar[bSfull + g], jj & 1, abort_flag, p.err);
+                tc_fence_after();
+                float x[kPT];
+                float mx = -INFINITY;
+                if (active) {
+                    uint32_t a[32], b[32];
+                    tmem_ld32_nowait(ts, a);
+                    tmem_ld32_nowait(ts + 32, b);
+                    tmem_wait_ld(a);
+                    tmem_wait_ld(b);
 #pragma unroll
-                        for (int q = 0; q < kFew; ++q)
-                            if (mine && q < n) dst[q * RS + row] = o[q] + o[kFew + q];
-                    } else {
-                        float o0[32], o1[32];
-                        tmem_ld32(to, o0);
-                        tmem_ld32(to + kHalf, o1);
-#pragma unroll
-                        for (int q = 0; q < kHalf; ++q)
-                            if (mine && q < n) dst[q * RS + row] = o0[q] + o1[q];
+                    for (int c = 0; c < 32; ++c) {
+                        x[c] = __uint_as_float(a[c]);
+                        x[32 + c] = __uint_as_float(b[c]);
                     }
-                }
-                if (et < n) {
-                    dst[et * RS + RV] = x.state[slot * 2 * kHalf + et];
-                    dst[et * RS + RV + 1] = x.state[slot * 2 * kHalf + kHalf + et];
                 }
                 tc_fence_before();
-                mbar_arrive(&bar[bOfree + slot]);
+                mbar_arrive(&bar[bSfree + g]);
+                if (active) {
+                    if (left < kPT) {
+#pragma unroll
+                        for (int c = 0; c < kPT; ++c) x[c] = c < left ? x[c] : -INFINITY;
+                    }
+                    float t[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) t[c] = x[c];
+#pragma unroll
+                    for (int c = 4; c < kPT; c += 8)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) t[e] = c + 4 + e < kPT ? fmaxf(fmaxf(t[e], x[c + e]), x[c + 4 + e]) : fmaxf(t[e], x[c + e]);
+                    mx = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+                }
+                // The running maximum after the page before, from the other group's thread of this row; each page's weights are
+                // relative to the running maximum that its own step leaves.  Also between runs, where nothing is handed over:
+                // what the other group reads here is not written again before it has.
+                if (j > 0) {
+                    named_bar_sync(1 + quarter * 2 + ((j - 1) & 1), 64);
+                    const float mp = k > 0 ? running[row] : m;
+                    if (mp != m) {
+                        l *= ex2_approx(m - mp);  // (m = -inf: no page yet, l = 0)
+                        m = mp;
+                    }
+                }
+                const float m_new = fmaxf(m, mx);
+                const bool need = m_new > m + kRescaleLog2;  // also the first page
+                const float factor = need ? ex2_approx(m - m_new) : 1.f;
+                if (need) {
+                    l *= factor;
+                    m = m_new;
+                }
+                if (j + 1 < total) {
+                    running[row] = m;
+                    named_bar_arrive(1 + quarter * 2 + (j & 1), 64);
+                }
+                const bool any = __any_sync(0xffffffffu, need && k > 0);
+                // this group's page before has been read by its product (and O holds it)
+                if (jj > 0) mbar_wait(&bar[bPfree + g], (jj - 1) & 1, abort_flag, p.err);
+                if (any) {
+                    // O holds the run's pages before this one: wait for the last of them, which is the other group's (products
+                    // complete in order, so that its barrier is at most one phase behind), and rescale
+                    mbar_wait(&bar[bPfree + (g ^ 1)], ((j - 1) >> 1) & 1, abort_flag, p.err);
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c0 = 0; c0 < ZZ::RVX; c0 += 16) {
+                        float v[16];
+                        tmem_ld16(tl + ZZ::TM_O + c0, v);
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) v[c] *= factor;
+                        tmem_st16(tl + ZZ::TM_O + c0, v);
+                    }
+                }
+                if (active) {
+                    const float2 mm = make_float2(-m, -m);
+                    uint32_t pw[kPT / 2];
+                    float2 s4[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s4[e] = make_float2(0.f, 0.f);
+#pragma unroll
+                    for (int c = 0; c < kPT; c += 2) {
+                        float2 y = __fadd2_rn(make_float2(x[c], x[c + 1]), mm);
+                        y.x = ex2_approx(y.x);
+                        y.y = ex2_approx(y.y);
+                        s4[(c >> 1) & 3] = __fadd2_rn(s4[(c >> 1) & 3], y);
+                        pw[c / 2] = pack_bf16x2(y.x, y.y);
+                        if (second) {
+                            const float2 f = bf2_to_f2(pw[c / 2]);
+                            pw[c / 2] = pack_bf16x2(y.x - f.x, y.y - f.y);
+                        }
+                    }
+                    const float2 sa = __fadd2_rn(s4[0], s4[1]), sb = __fadd2_rn(s4[2], s4[3]);
+                    l += (sa.x + sa.y) + (sb.x + sb.y);
+                    tc_fence_after();
+                    tmem_st32u_nowait(tp, pw);
+                }
+                if (left < kPT) {
+                    // V rows past the sequence hold no latents: zero them (0 * NaN would poison O)
+                    const int st = j % ZZ::ST;
+                    mbar_wait(&bar[bVfull + st], (j / ZZ::ST) & 1, abort_flag, p.err);
+                    char *vs = sm + ZZ::oV + st * ZZ::VPAGE;
+                    for (int i = row; i < (kPT - left) * ZZ::NBOX * 8; i += 128) {
+                        const int chunk = i & 7, box = (i >> 3) % ZZ::NBOX, tr = left + (i >> 3) / ZZ::NBOX;
+                        *reinterpret_cast<uint4 *>(vs + box * ZZ::BOX + tr * 128 + chunk * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_proxy_async_smem();
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(&bar[bPfull + g]);
             }
-            return true;
-        });
+            it = end;
+            // this group's maximum and sum of the run, once the run before the last has been read from there
+            if (run >= 2) mbar_wait(&bar[bOfree + (run & 1)], ((run - 2) >> 1) & 1, abort_flag, p.err);
+            if (!second) states[((run & 1) * 2 + g) * 64 + row] = make_float2(m, l);
+            mbar_arrive(&bar[bMfull + (run & 1)]);
+        }
+    } else {
+        // --------------------------------------------------------- q~ and epilogue, warps 12-15
+        constexpr int RS = record_floats(RV);
+        const int quarter = warp & 3, row = 32 * quarter + lane, q = row & 63;
+        const uint32_t tl = tmem + (static_cast<uint32_t>(32 * quarter) << 16);
+        // the parts of a run's queries into TMEM: row by row, words of two columns
+        constexpr int kAtOnce = ZZ::RKT % 96 == 0 ? 6 : ZZ::RKT % 80 == 0 ? 5 : 4;  // pairs of 16-byte words
+        static_assert(ZZ::RKT % (16 * kAtOnce) == 0, "words of two");
+        auto load_queries = [&](const TrunkRun &r) {
+            if ((quarter & 1) == 0 || r.d.n > 32) {
+                const char *src = query_parts<ZZ::QROW>(p, r, q);
+#pragma unroll 1
+                for (int part = 0; part < 3; ++part)
+#pragma unroll 1
+                    for (int c0 = 0; c0 < ZZ::RKT / 8; c0 += 2 * kAtOnce) {
+                        uint4 v[2 * kAtOnce];
+#pragma unroll
+                        for (int c = 0; c < 2 * kAtOnce; ++c)
+                            v[c] = src ? *reinterpret_cast<const uint4 *>(src + (part * (ZZ::RKT / 8) + c0 + c) * 16) : make_uint4(0, 0, 0, 0);
+                        if (part < ZZ::QT) {
+#pragma unroll
+                            for (int c = 0; c < 2 * kAtOnce; c += 2) {
+                                const uint32_t u[8] = {v[c].x, v[c].y, v[c].z, v[c].w, v[c + 1].x, v[c + 1].y, v[c + 1].z, v[c + 1].w};
+                                tmem_st8u(tl + ZZ::TM_Q + part * ZZ::PART + (c0 + c) * 4, u);
+                            }
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < 2 * kAtOnce; ++c)
+                                *reinterpret_cast<uint4 *>(sm + ZZ::oQ + (c0 + c) * (kRows * 16) + row * 16) = v[c];
+                        }
+                    }
+                if (ZZ::QT < 3) fence_proxy_async_smem();
+                tmem_wait_st();
+            }
+            tc_fence_before();
+            mbar_arrive(&bar[bQfull]);
+        };
+        RunWalk ahead(p, groups, sh, list);
+        if (ahead.next()) load_queries(ahead.r);
+        for (int run = 0; w.next(); ++run) {
+            if (ahead.next()) {  // the next run's q~, as soon as S of this one's pages is done
+                mbar_wait(&bar[bQfree], run & 1, abort_flag, p.err);
+                tc_fence_after();
+                load_queries(ahead.r);
+            }
+            mbar_wait(&bar[bOdone], run & 1, abort_flag, p.err);
+            mbar_wait(&bar[bMfull + (run & 1)], (run >> 1) & 1, abort_flag, p.err);
+            tc_fence_after();
+            const int n = w.r.d.n;
+            float *dst = p.part + (record_of(p, w.r.d, w.r.h, blockIdx.x) + q) * RS;
+            {
+                // rows q and 64 + q: the second parts through shared memory
+                float *xr = reinterpret_cast<float *>(sm + ZZ::oExch) + q * ZZ::XROW;
+                const bool mine = q < n;
+#pragma unroll 1
+                for (int c0 = 0; c0 < ZZ::RVX; c0 += ZZ::XCOLS) {
+                    if (c0 > 0) named_bar_sync(9, 128);
+                    if (quarter >= 2 && (quarter == 2 || n > 32)) {
+#pragma unroll 1
+                        for (int c = 0; c < ZZ::XCOLS; c += 16) {
+                            float o[16];
+                            tmem_ld16(tl + ZZ::TM_O + c0 + c, o);
+#pragma unroll
+                            for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4 *>(xr + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                        }
+                    }
+                    named_bar_sync(9, 128);
+                    if (quarter < 2 && (quarter == 0 || n > 32)) {
+#pragma unroll 1
+                        for (int c = 0; c < ZZ::XCOLS; c += 16) {
+                            float o[16];
+                            tmem_ld16(tl + ZZ::TM_O + c0 + c, o);
+#pragma unroll
+                            for (int e = 0; e < 16; e += 4) {
+                                const float4 v = *reinterpret_cast<const float4 *>(xr + c + e);
+                                if (mine && c0 + c + e < RV)
+                                    *reinterpret_cast<float4 *>(dst + c0 + c + e) = make_float4(o[e] + v.x, o[e + 1] + v.y, o[e + 2] + v.z, o[e + 3] + v.w);
+                            }
+                        }
+                    }
+                }
+            }
+            if (quarter < 2 && q < n) {
+                const float2 s0 = states[((run & 1) * 2) * 64 + q], s1 = states[((run & 1) * 2 + 1) * 64 + q];
+                const float mf = fmaxf(s0.x, s1.x);
+                dst[RV] = mf;
+                dst[RV + 1] = (s0.x == mf ? s0.y : s0.y * ex2_approx(s0.x - mf)) + (s1.x == mf ? s1.y : s1.y * ex2_approx(s1.x - mf));
+            }
+            tc_fence_before();
+            mbar_arrive(&bar[bOfree + (run & 1)]);
+        }
     }
-    pdl_trigger();
     tc_fence_before();
     __syncthreads();
     if (warp == 1) {
@@ -857,16 +883,251 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
     }
 }
 
+// -------------------------------------------------------------------------------------------- leaf kernel
+
+// Shared memory of the leaf kernel: a slot for one page, the queries and the weights of each warp.
+constexpr int kMaxWarps = 9;
+template <int RK, int RV, int DR>
+struct L {
+    static constexpr int RKX = (RK + 15) / 16 * 16, RKT = RKX + DR;
+    static constexpr int KPLANE = kPT * RK * 2, RPLANE = kPT * DR * 2, VPLANE = kPT * RV * 2;
+    static constexpr int SLOT = KPLANE + RPLANE + VPLANE;
+    static constexpr int SCRATCH = kLeaf * (RKT + kPT) * 4 + 16;  // q~, p, two barriers
+    static constexpr int W0 = (kSmemCap - 2048 - kMaxNodes * 2 - 64) / (SLOT + SCRATCH);
+    static constexpr int WARPS = W0 > kMaxWarps ? kMaxWarps : W0;
+    static constexpr int oScratch = WARPS * SLOT;
+    static constexpr int oList = oScratch + WARPS * SCRATCH;
+    static constexpr int SMEM = 128 + oList + kMaxNodes * 2 + 16;
+    static constexpr int QROW = 3 * RKT * 2;
+    static constexpr bool TAIL = RV > 128;  // 4 columns in each lane, and one more behind the 128th
+    static_assert(RV <= 160 && (RV <= 128 || RV == 160) && SCRATCH % 16 == 0, "columns of a warp");
+};
+
+// Where a warp's next page comes from.
+struct PageWalk {
+    RunWalk w;
+    int k;
+    bool ok;
+    __device__ __forceinline__ PageWalk(const RunWalk &ww) : w(ww), k(-1), ok(true) { step(); }
+    __device__ __forceinline__ void step() {
+        if (++k >= w.r.pages) {
+            ok = w.next();
+            k = 0;
+        }
+    }
+    __device__ __forceinline__ int block(const TrunkParams &p) const {
+        return ok ? p.block_table[static_cast<int64_t>(w.r.d.row) * p.max_blocks + w.r.page + k] : 0;
+    }
+};
+
+// One page of NQ queries, by a warp: scores of tokens lane and lane + 32 from the K-plane (and the rotary plane), the online
+// softmax of each query, and 4 or 5 columns of its value sum in each lane.  `k_read` is called when the K-plane has been read.
+template <typename LL, int NQ, typename F>
+__device__ __forceinline__ void leaf_page(const char *slot, const float *qs, float *ps, int left, float (&m)[kLeaf], float (&l)[kLeaf],
+                                          float (&acc)[kLeaf][5], F k_read) {
+    constexpr int RV = LL::VPLANE / (kPT * 2);
+    const int lane = threadIdx.x & 31;
+    float s[NQ][2];
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) s[q][0] = s[q][1] = 0.f;
+    auto dot = [&](const char *plane, const float *qq, int granules) {
+#pragma unroll 2
+        for (int g = 0; g < granules; ++g) {
+            const uint4 a = *reinterpret_cast<const uint4 *>(plane + g * (kPT * 16) + lane * 16);
+            const uint4 b = *reinterpret_cast<const uint4 *>(plane + g * (kPT * 16) + (lane + 32) * 16);
+            const float2 a0 = bf2_to_f2(a.x), a1 = bf2_to_f2(a.y), a2 = bf2_to_f2(a.z), a3 = bf2_to_f2(a.w);
+            const float2 b0 = bf2_to_f2(b.x), b1 = bf2_to_f2(b.y), b2 = bf2_to_f2(b.z), b3 = bf2_to_f2(b.w);
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) {
+                const float4 u = *reinterpret_cast<const float4 *>(qq + q * LL::RKT + g * 8), v = *reinterpret_cast<const float4 *>(qq + q * LL::RKT + g * 8 + 4);
+                s[q][0] = fmaf(a3.y, v.w, fmaf(a3.x, v.z, fmaf(a2.y, v.y, fmaf(a2.x, v.x, fmaf(a1.y, u.w, fmaf(a1.x, u.z, fmaf(a0.y, u.y, fmaf(a0.x, u.x, s[q][0]))))))));
+                s[q][1] = fmaf(b3.y, v.w, fmaf(b3.x, v.z, fmaf(b2.y, v.y, fmaf(b2.x, v.x, fmaf(b1.y, u.w, fmaf(b1.x, u.z, fmaf(b0.y, u.y, fmaf(b0.x, u.x, s[q][1]))))))));
+            }
+        }
+    };
+    dot(slot, qs, LL::KPLANE / (kPT * 16));
+    if constexpr (LL::RPLANE > 0) dot(slot + LL::KPLANE, qs + LL::RKX, LL::RPLANE / (kPT * 16));
+    k_read();
+#pragma unroll
+    for (int q = 0; q < NQ; ++q) {
+        const float x0 = lane < left ? s[q][0] : -INFINITY, x1 = lane + 32 < left ? s[q][1] : -INFINITY;
+        const float mn = fmaxf(m[q], warp_max(fmaxf(x0, x1)));
+        const float f = m[q] == -INFINITY ? 0.f : ex2_approx(m[q] - mn);
+        const float p0 = ex2_approx(x0 - mn), p1 = ex2_approx(x1 - mn);
+        m[q] = mn;
+        l[q] = fmaf(l[q], f, p0 + p1);
+        ps[q * kPT + lane] = p0;
+        ps[q * kPT + 32 + lane] = p1;
+#pragma unroll
+        for (int e = 0; e < 5; ++e) acc[q][e] *= f;
+    }
+    __syncwarp();
+    const char *vp = slot + LL::KPLANE + LL::RPLANE;
+    const int c4 = lane * 4 < RV ? lane * 8 : 0;
+    auto token = [&](int t, const float (&pv)[NQ]) {
+        const uint2 a = *reinterpret_cast<const uint2 *>(vp + t * (RV * 2) + c4);
+        const float2 a0 = bf2_to_f2(a.x), a1 = bf2_to_f2(a.y);
+        float a4 = 0.f;
+        if constexpr (LL::TAIL) a4 = bf_to_f(*reinterpret_cast<const uint16_t *>(vp + t * (RV * 2) + 256 + lane * 2));
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            acc[q][0] = fmaf(pv[q], a0.x, acc[q][0]);
+            acc[q][1] = fmaf(pv[q], a0.y, acc[q][1]);
+            acc[q][2] = fmaf(pv[q], a1.x, acc[q][2]);
+            acc[q][3] = fmaf(pv[q], a1.y, acc[q][3]);
+            if constexpr (LL::TAIL) acc[q][4] = fmaf(pv[q], a4, acc[q][4]);
+        }
+    };
+    const int nt = min(left, kPT);  // rows behind the sequence hold no latents
+#pragma unroll 2
+    for (int t = 0; t + 4 <= nt; t += 4) {
+        float4 p4[NQ];
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) p4[q] = *reinterpret_cast<const float4 *>(ps + q * kPT + t);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float pv[NQ];
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) pv[q] = i == 0 ? p4[q].x : i == 1 ? p4[q].y : i == 2 ? p4[q].z : p4[q].w;
+            token(t + i, pv);
+        }
+    }
+    for (int t = nt & ~3; t < nt; ++t) {
+        float pv[NQ];
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) pv[q] = ps[q * kPT + t];
+        token(t, pv);
+    }
+}
+
+// Every warp streams its own pages through a slot of its own: while it works on the values of a page the K-plane of the next
+// one lands, and while it works on that one's scores its V-plane does.  The other warps' copies fill the rest of HBM's time, so
+// that a warp's run boundaries (the queries of the next run, the record of this one) cost nothing until the warps of an SM
+// together cannot keep up.
+template <int RK, int RV, int DR>
+__global__ void __launch_bounds__(L<RK, RV, DR>::WARPS * 32, 1) leaf_kernel(const __grid_constant__ TrunkParams p) {
+    using LL = L<RK, RV, DR>;
+    constexpr int RS = record_floats(RV);
+    extern __shared__ __align__(128) char sm[];
+    __shared__ int abort_word;
+    volatile int *abort_flag = &abort_word;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+    char *slot = sm + warp * LL::SLOT;
+    uint64_t *bar = reinterpret_cast<uint64_t *>(sm + LL::oScratch + warp * LL::SCRATCH);  // K, V
+    float *qs = reinterpret_cast<float *>(bar + 2), *ps = qs + kLeaf * LL::RKT;
+    uint16_t *list = reinterpret_cast<uint16_t *>(sm + LL::oList);
+    if (lane == 0) {
+        mbar_init(&bar[0], 1);
+        mbar_init(&bar[1], 1);
+        fence_mbar_init();
+    }
+    if (tid == 0) abort_word = 0;
+    // The trunk kernel lets this one start when all of its CTAs have waited for the absorb kernel, so that q~ and beta are
+    // there and the workspace is free.  Its own records are not read here; the wait for it is at the end.
+    const int groups = count_groups(p), workers = gridDim.x * LL::WARPS;
+    Share sh = find_share<true, LL::WARPS * 32>(p, groups, list, blockIdx.x * LL::WARPS, LL::WARPS, workers);
+    const int me = blockIdx.x * LL::WARPS + warp;
+    sh.g0 = me < sh.we ? page_lo(me, sh.np, sh.we) : 0;
+    sh.g1 = me < sh.we ? page_lo(me + 1, sh.np, sh.we) : 0;
+    if (sh.g0 < sh.g1) {
+        RunWalk w(p, groups, sh, list);
+        PageWalk ahead(w);
+        const uint64_t pol = policy_evict_first();
+        auto checked = [&](int blk) {
+            if (blk >= 0 && blk < p.num_blocks) return blk;
+            if (lane == 0) atomicOr(p.err, LLA_DEVERR_BLOCK_ID);
+            return 0;
+        };
+        auto issue_k = [&](int blk, int h) {
+            if (lane == 0) {
+                mbar_arrive_expect_tx(&bar[0], LL::KPLANE + LL::RPLANE);
+                bulk_g2s(slot, p.pool + (static_cast<int64_t>(blk) * p.H + h) * p.page_bytes, LL::KPLANE, &bar[0], pol);
+                if constexpr (DR > 0)
+                    bulk_g2s(slot + LL::KPLANE, p.rope_pool + static_cast<int64_t>(blk) * LL::RPLANE, LL::RPLANE, &bar[0], pol);
+            }
+        };
+        auto issue_v = [&](int blk, int h) {
+            if (lane == 0) {
+                mbar_arrive_expect_tx(&bar[1], LL::VPLANE);
+                bulk_g2s(slot + LL::KPLANE + LL::RPLANE, p.pool + (static_cast<int64_t>(blk) * p.H + h) * p.page_bytes + LL::KPLANE, LL::VPLANE,
+                         &bar[1], pol);
+            }
+        };
+        int blk = checked(ahead.block(p));
+        issue_k(blk, ahead.w.r.h);
+        issue_v(blk, ahead.w.r.h);
+        int it = 0, issued_k = 1, issued_v = 1;
+        bool ok = true;
+        while (ok && w.next()) {
+            // the queries, each the sum of its three parts (which is exact)
+            const int n = w.r.d.n;
+            for (int q = 0; q < n; ++q) {
+                const uint16_t *src = reinterpret_cast<const uint16_t *>(query_parts<LL::QROW>(p, w.r, q));
+                for (int i = lane; i < LL::RKT; i += 32)
+                    qs[q * LL::RKT + i] = src ? bf_to_f(__ldcg(src + i)) + (bf_to_f(__ldcg(src + LL::RKT + i)) + bf_to_f(__ldcg(src + 2 * LL::RKT + i))) : 0.f;
+            }
+            __syncwarp();
+            float m[kLeaf], l[kLeaf], acc[kLeaf][5];
+#pragma unroll
+            for (int q = 0; q < kLeaf; ++q) {
+                m[q] = -INFINITY;
+                l[q] = 0.f;
+#pragma unroll
+                for (int e = 0; e < 5; ++e) acc[q][e] = 0.f;
+            }
+            for (int k = 0; ok && k < w.r.pages; ++k, ++it) {
+                const int left = w.r.d.len - (w.r.page + k) * kPT;
+                ahead.step();
+                const int next = ahead.block(p);  // (in flight while the scores are worked out)
+                ok = mbar_wait(&bar[0], it & 1, abort_flag, p.err);
+                auto k_read = [&] {
+                    __syncwarp();
+                    blk = checked(next);
+                    if (ok && ahead.ok) {
+                        issue_k(blk, ahead.w.r.h);
+                        ++issued_k;
+                    }
+                    ok = mbar_wait(&bar[1], it & 1, abort_flag, p.err) && ok;
+                };
+                if (n == 1) leaf_page<LL, 1>(slot, qs, ps, left, m, l, acc, k_read);
+                else leaf_page<LL, kLeaf>(slot, qs, ps, left, m, l, acc, k_read);
+                __syncwarp();
+                if (ok && ahead.ok) {
+                    issue_v(blk, ahead.w.r.h);
+                    ++issued_v;
+                }
+            }
+            float *dst = p.part + record_of(p, w.r.d, w.r.h, me) * RS;
+#pragma unroll
+            for (int q = 0; q < kLeaf; ++q) {
+                const float sum = warp_sum(l[q]);
+                if (q >= n) continue;
+                if (lane * 4 < RV)
+                    *reinterpret_cast<float4 *>(dst + q * RS + lane * 4) = make_float4(acc[q][0], acc[q][1], acc[q][2], acc[q][3]);
+                if constexpr (LL::TAIL) dst[q * RS + 128 + lane] = acc[q][4];
+                if (lane == 0) {
+                    dst[q * RS + RV] = m[q];
+                    dst[q * RS + RV + 1] = sum;
+                }
+            }
+            __syncwarp();  // the queries are free
+        }
+        if (!ok) {  // a wait ran out: what is in flight lands before the CTA can exit
+            volatile int never = 0;
+            mbar_wait(&bar[0], (issued_k - 1) & 1, &never, p.err);
+            mbar_wait(&bar[1], (issued_v - 1) & 1, &never, p.err);
+        }
+    }
+    pdl_wait();  // behind this kernel the trunk kernel is complete, too
+}
+
 // ------------------------------------------------------------------------------------------- join kernel
 
 // Grid (H, ceil(B / spb)), 128 threads; SPB: the sequences that the projection is unrolled for.
 template <int RV, int SPB>
 __global__ void __launch_bounds__(128, 1) join_kernel(const __grid_constant__ JoinParams a) {
     constexpr int RS = record_floats(RV), NW = RV / 8, NJ = (RV + 31) / 32;
-    constexpr int kMaxRuns = kMaxGrid + kLevels + 1;  // a CTA holds pages of several of a sequence's nodes at their ends only
     __shared__ __align__(16) float ob[SPB][RV];
-    __shared__ float wts[4][kMaxRuns];
-    __shared__ int recs[4][kMaxRuns];
     __shared__ float coef[SPB][3], scs[SPB];
     const TrunkParams &p = a.t;
     const int h = blockIdx.x, b0 = blockIdx.y * a.spb, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -899,71 +1160,73 @@ __global__ void __launch_bounds__(128, 1) join_kernel(const __grid_constant__ Jo
     __syncthreads();
     pdl_wait();
     const int groups = count_groups(p), nodes = groups + p.B;
-    const int NP = p.pstart[nodes] * p.H, Ge = min(a.grid, NP);  // the split of find_share
+    // the split of find_share
+    const int np[2] = {p.pstart[nodes] * p.H, p.pstart[nodes + 1] * p.H};
+    const int we[2] = {min(a.grid, np[0]), min(a.workers, np[1])};
     // G warps per sequence: warp `sub` of them takes the columns lane + 32 (sub + G q)
     const int G = nb == 1 ? 4 : nb == 2 ? 2 : 1;
     const int grp = warp / G, sub = warp - grp * G;
-    float *wt = wts[warp];
-    int *rec = recs[warp];
     for (int bi = grp; bi < SPB; bi += 4 / G) {
         if (bi >= nb) {
             for (int j = lane + 32 * sub; j < RV; j += 32 * G) ob[bi][j] = 0.f;
             continue;
         }
         const int b = b0 + bi;
-        // the runs of the sequence's nodes
-        int nr = 0;
-        for (int l = 0; l <= kLevels; ++l) {
+        // the states of the runs of the sequence's nodes, up to 32 at a time
+        float M = -INFINITY, l = 0.f;
+        float acc[NJ];
+#pragma unroll
+        for (int q = 0; q < NJ; ++q) acc[q] = 0.f;
+#pragma unroll 1
+        for (int level = 0; level <= kLevels; ++level) {
             int i = groups + b, q = 0;
-            if (l < kLevels) {
-                const int col = p.plan.column[static_cast<int64_t>(l) * p.B + b];
+            if (level < kLevels) {
+                const int col = p.plan.column[static_cast<int64_t>(level) * p.B + b];
                 if (col < 0 || col / kMembers >= groups) continue;
                 i = col / kMembers;
                 q = col % kMembers;
             }
             const Node d = node_at(p, groups, i);
             if (d.pages == 0 || q >= d.n) continue;
-            const int s0 = p.pstart[i] * p.H + h * d.pages, c0 = cta_of(s0, NP, Ge), c1 = cta_of(s0 + d.pages - 1, NP, Ge);
-            const int64_t r0 = record_of(p, d, h, c0) + q;
-            for (int c = lane; c <= c1 - c0 && nr + c < kMaxRuns; c += 32) rec[nr + c] = static_cast<int>(r0 + static_cast<int64_t>(kMembers) * c);
-            nr = min(kMaxRuns, nr + c1 - c0 + 1);
-        }
-        __syncwarp();
-        float M = -INFINITY, ls = 0.f;
-        for (int i = lane; i < nr; i += 32) M = fmaxf(M, wt[i] = p.part[static_cast<int64_t>(rec[i]) * RS + RV]);
-        M = warp_max(M);
-        for (int i = lane; i < nr; i += 32) {
-            const float w8 = wt[i] == -INFINITY ? 0.f : ex2_approx(wt[i] - M);
-            ls = fmaf(w8, p.part[static_cast<int64_t>(rec[i]) * RS + RV + 1], ls);
-            wt[i] = w8;
-        }
-        const float l = warp_sum(ls);
-        __syncwarp();
-        float acc[NJ];
+            const int kind = is_leaf(d), s0 = p.pstart[i] * p.H + h * d.pages;
+            const int c0 = cta_of(s0, np[kind], we[kind]), c1 = cta_of(s0 + d.pages - 1, np[kind], we[kind]);
+            const int64_t step = static_cast<int64_t>(kind ? kLeaf : kMembers) * RS;
+            const float *first = p.part + (record_of(p, d, h, c0) + q) * RS;
+#pragma unroll 1
+            for (int c = c0; c <= c1; c += 32) {
+                const int nr = min(32, c1 - c + 1);
+                const float *mine = first + (c - c0 + min(lane, nr - 1)) * step;
+                const float mi = lane < nr ? mine[RV] : -INFINITY, li = mine[RV + 1];
+                const float Mn = fmaxf(M, warp_max(mi)), f = M == -INFINITY ? 0.f : ex2_approx(M - Mn);
+                const float wi = mi == -INFINITY ? 0.f : ex2_approx(mi - Mn);
+                M = Mn;
+                l = fmaf(l, f, warp_sum(lane < nr ? wi * li : 0.f));
 #pragma unroll
-        for (int q = 0; q < NJ; ++q) acc[q] = 0.f;
-        constexpr int KR = 4;  // runs whose loads are in flight together
-        for (int i0 = 0; i0 < nr; i0 += KR) {
-            float v[KR][NJ];
+                for (int j = 0; j < NJ; ++j) acc[j] *= f;
+                constexpr int KR = 4;  // runs whose loads are in flight together
+#pragma unroll 1
+                for (int k0 = 0; k0 < nr; k0 += KR) {
+                    float v[KR][NJ];
 #pragma unroll
-            for (int k = 0; k < KR; ++k) {
-                const float *pr = p.part + static_cast<int64_t>(rec[min(i0 + k, nr - 1)]) * RS;
+                    for (int k = 0; k < KR; ++k) {
+                        const float *pr = first + (c - c0 + min(k0 + k, nr - 1)) * step;
 #pragma unroll
-                for (int q = 0; q < NJ; ++q) {
-                    const int j = lane + 32 * (sub + G * q);
-                    v[k][q] = j < RV ? pr[j] : 0.f;
+                        for (int j = 0; j < NJ; ++j) {
+                            const int e = lane + 32 * (sub + G * j);
+                            v[k][j] = e < RV ? pr[e] : 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < KR; ++k) {
+                        const float wk = __shfl_sync(0xffffffffu, wi, k0 + k);  // (0 behind the last)
+                        if (wk != 0.f && k0 + k < nr) {  // warp-uniform (a NaN state stays one)
+#pragma unroll
+                            for (int j = 0; j < NJ; ++j) acc[j] = fmaf(wk, v[k][j], acc[j]);
+                        }
+                    }
                 }
             }
-#pragma unroll
-            for (int k = 0; k < KR; ++k) {
-                const float w8 = i0 + k < nr ? wt[i0 + k] : 0.f;
-                if (w8 != 0.f) {  // warp-uniform (a NaN state stays one)
-#pragma unroll
-                    for (int q = 0; q < NJ; ++q) acc[q] = fmaf(w8, v[k][q], acc[q]);
-                }
-            }
         }
-        __syncwarp();  // wt and rec are free for the warp's next sequence
 #pragma unroll
         for (int q = 0; q < NJ; ++q) {
             const int j = lane + 32 * (sub + G * q);
@@ -971,6 +1234,7 @@ __global__ void __launch_bounds__(128, 1) join_kernel(const __grid_constant__ Jo
         }
         if (sub == 0 && lane == 0) {
             const float sc = a.cur_k ? scs[bi] : -INFINITY;
+            M += p.beta[iorow(b)];  // the same for all of a query's cached tokens
             const float Mx = fmaxf(M, sc);
             const float al = M == -INFINITY ? 0.f : ex2_approx(M - Mx);
             const float pc = a.cur_k ? ex2_approx(sc - Mx) : 0.f;
@@ -1014,18 +1278,20 @@ __global__ void __launch_bounds__(128, 1) join_kernel(const __grid_constant__ Jo
 
 struct PrefixWorkspace {
     size_t part, qt, beta, pstart, total;
+    size_t leaf;  // first record of the leaf kernel
 };
 
 inline size_t al256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 PrefixWorkspace prefix_workspace(int rkt, int r_v, int B, int H, int grid) {
     PrefixWorkspace w;
-    const size_t records = static_cast<size_t>(H) * (kLevels + 1) * B + static_cast<size_t>(kMembers) * grid;
+    w.leaf = static_cast<size_t>(H) * kLevels * B + static_cast<size_t>(kMembers) * grid;
+    const size_t records = w.leaf + static_cast<size_t>(H) * (kLevels + 1) * B + static_cast<size_t>(kLeaf) * kMaxWarps * grid;
     w.part = 0;
     w.qt = al256(records * record_floats(r_v) * sizeof(float));
-    w.beta = w.qt + al256(static_cast<size_t>(B) * H * rkt * sizeof(float));
+    w.beta = w.qt + al256(static_cast<size_t>(B) * H * 3 * rkt * sizeof(uint16_t));
     w.pstart = w.beta + al256(static_cast<size_t>(B) * H * sizeof(float));
-    w.total = w.pstart + al256((kMaxNodes + 1) * sizeof(int));
+    w.total = w.pstart + al256((kMaxNodes + 2) * sizeof(int));
     return w;
 }
 
@@ -1043,7 +1309,9 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     const PrefixWorkspace w = prefix_workspace(ZZ::RKT, RV, a.B, a.H, grid);
     if (a.workspace_bytes < w.total) return LLA_ERR_WORKSPACE;
     char *ws = static_cast<char *>(a.workspace);
-    static DeviceOnce configured;
+    using LL = L<RK, RV, DR>;
+    static DeviceOnce configured, configured_leaf;
+    if (raise_smem_limit(leaf_kernel<RK, RV, DR>, LL::SMEM, configured_leaf) != LLA_OK) return LLA_ERR_CUDA;
     if (raise_smem_limit(trunk_kernel<RK, RV, DR>, ZZ::SMEM, configured) != LLA_OK) return LLA_ERR_CUDA;
     const int64_t page_bytes = static_cast<int64_t>(head_page_bytes(RK, RV, 2));
     // the V-planes of every page: [num_blocks * H][64 tokens][r_v] bf16
@@ -1060,10 +1328,11 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     tp.rope_pool = static_cast<const char *>(rope_pool);
     tp.block_table = a.block_table; tp.context_lens = a.context_lens;
     tp.plan = PlanView{plan.num_groups, plan.groups, plan.members, plan.column, plan.own_page};
-    tp.qt = reinterpret_cast<float *>(ws + w.qt);
+    tp.qt = reinterpret_cast<uint16_t *>(ws + w.qt);
     tp.beta = reinterpret_cast<float *>(ws + w.beta);
     tp.part = reinterpret_cast<float *>(ws + w.part);
     tp.pstart = reinterpret_cast<int *>(ws + w.pstart);
+    tp.leaf = static_cast<int64_t>(w.leaf);
     tp.err = err;
 
     AbsorbParams ap = {};
@@ -1079,10 +1348,11 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     if ((st = launch_ex(absorb_kernel<RK, DR>, dim3(a.H, (ZZ::RKX + 31) / 32 + (DR > 0), (a.B + 15) / 16), 256, 0, stream, ap)) != LLA_OK)
         return st;
     if ((st = launch_ex(trunk_kernel<RK, RV, DR>, dim3(grid), kTrunkThreads, ZZ::SMEM, stream, tv, tp)) != LLA_OK) return st;
+    if ((st = launch_ex(leaf_kernel<RK, RV, DR>, dim3(grid), LL::WARPS * 32, LL::SMEM, stream, tp)) != LLA_OK) return st;
 
     JoinParams jp = {};
     jp.t = tp;
-    jp.T = a.T; jp.loop = a.loop; jp.io_bf16 = a.io_bf16; jp.grid = grid; jp.d_rope = DR;
+    jp.T = a.T; jp.loop = a.loop; jp.io_bf16 = a.io_bf16; jp.grid = grid; jp.workers = grid * LL::WARPS; jp.d_rope = DR;
     jp.scale_log2 = ap.scale_log2;
     jp.w_up_v = a.w_up_v; jp.mu_v = a.mu_v;
     jp.q = a.q; jp.q_rope = q_rope; jp.cur_k = a.cur_k; jp.cur_v = a.cur_v; jp.cur_k_rope = cur_k_rope;
