@@ -43,6 +43,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "lla_device.cuh"
 #include "lla_internal.h"
@@ -162,16 +163,25 @@ __host__ __device__ constexpr int record_floats(int rv) { return rv + 4; }
 
 // One CTA: the prefix sums of the nodes' pages, and the flags of what node_at leaves out.
 __device__ void node_prefix(const TrunkParams &p) {
+    __shared__ int pages[kMaxNodes];  // a leaf's as -1 - pages
+    __shared__ int wsum[2][8];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int groups = count_groups(p), nodes = groups + p.B;
     const int cap = static_cast<int>(min(static_cast<int64_t>(p.max_ctx), static_cast<int64_t>(p.max_blocks) * kPT));
     unsigned bad = 0;
     if (*p.plan.num_groups != groups) bad |= LLA_DEVERR_SEQUENCE;
+    for (int i = tid; i < nodes; i += 256) {
+        const Node d = node_at(p, groups, i);
+        pages[i] = is_leaf(d) ? -1 - d.pages : d.pages;
+        if (i < groups && d.pages == 0) bad |= LLA_DEVERR_SEQUENCE;
+        if (i >= groups) {
+            if (d.len < 0 || d.len > cap || d.first < 0 || d.first > d.len / kPT) bad |= LLA_DEVERR_CONTEXT;
+            if (d.len == 0 && !p.pass1) bad |= LLA_DEVERR_EMPTY_PASS2;
+        }
+    }
     for (int b = tid; b < p.B; b += 256) {
         const int len = p.context_lens[b];
-        if (len < 0 || len > cap) bad |= LLA_DEVERR_CONTEXT;
-        else if (p.plan.own_page[b] < 0 || p.plan.own_page[b] > len / kPT) bad |= LLA_DEVERR_CONTEXT;
-        if (len == 0 && !p.pass1) bad |= LLA_DEVERR_EMPTY_PASS2;
+#pragma unroll
         for (int l = 0; l < kLevels; ++l) {
             const int col = p.plan.column[static_cast<int64_t>(l) * p.B + b];
             if (col < 0) continue;
@@ -180,17 +190,14 @@ __device__ void node_prefix(const TrunkParams &p) {
             else if (d.first + d.pages > len / kPT) bad |= LLA_DEVERR_CONTEXT;
         }
     }
-    for (int g = tid; g < groups; g += 256)
-        if (node_at(p, groups, g).pages == 0) bad |= LLA_DEVERR_SEQUENCE;
     if (bad) atomicOr(p.err, bad);
+    __syncthreads();
     const int per = (nodes + 255) / 256;
     int tot[2] = {0, 0};  // pages of the trunk's nodes, of the leaves
     for (int i = tid * per; i < min(nodes, (tid + 1) * per); ++i) {
-        const Node d = node_at(p, groups, i);
-        if (is_leaf(d)) tot[1] += d.pages;
-        else tot[0] += d.pages;
+        tot[0] += max(0, pages[i]);
+        tot[1] += max(0, -1 - pages[i]);
     }
-    __shared__ int wsum[2][8];
     int x[2] = {tot[0], tot[1]};  // inclusive scans over the warp
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -211,10 +218,10 @@ __device__ void node_prefix(const TrunkParams &p) {
         ex[1] += wsum[1][w];
     }
     for (int i = tid * per; i < min(nodes, (tid + 1) * per); ++i) {
-        const Node d = node_at(p, groups, i);
-        int &e = is_leaf(d) ? ex[1] : ex[0];
-        p.pstart[i] = e;
-        e += d.pages;
+        const int v = pages[i];
+        p.pstart[i] = v < 0 ? ex[1] : ex[0];
+        if (v < 0) ex[1] += -1 - v;
+        else ex[0] += v;
     }
     if (tid == 255) {
         p.pstart[nodes] = ex[0];
@@ -230,9 +237,10 @@ __device__ __forceinline__ void store_parts(uint16_t *dst, int stride, float v) 
     for (int k = 0; k < 3; ++k) dst[k * stride] = __bfloat16_as_ushort(__float2bfloat16_rn(part[k]));
 }
 
-// Grid (H, RKX / 32 [+ 1 with a rotary branch], ceil(B / 16)), 256 threads = 32 columns x 8 slices of 16 rows: q~ of 32
+// Grid (H, RKX / 32 [+ 1 with a rotary branch] + 1, ceil(B / 16)), 256 threads = 32 columns x 8 slices of 16 rows: q~ of 32
 // columns of one head for 16 sequences, every weight load of a thread in flight at once; beta by the CTAs of the first
-// column chunk; the rotary queries, turned at the current tokens' positions, by those of the last.
+// column chunk; the rotary queries, turned at the current tokens' positions, by those behind the columns; the nodes' prefix
+// sums by one CTA of the last row.
 template <int RK, int DR>
 __global__ void __launch_bounds__(256) absorb_kernel(const __grid_constant__ AbsorbParams a) {
     constexpr int RKX = (RK + 15) / 16 * 16, RKT = RKX + DR, CHUNKS = (RKX + 31) / 32;
@@ -247,6 +255,10 @@ __global__ void __launch_bounds__(256) absorb_kernel(const __grid_constant__ Abs
     // The trunk kernel may start: once every CTA is here the caller's previous kernel is complete, so its producers may read
     // any input of the call, and q~, beta and the workspace only after their own wait.
     pdl_trigger();
+    if (blockIdx.y == gridDim.y - 1) {
+        if (blockIdx.x == 0 && blockIdx.z == 0) node_prefix(p);
+        return;
+    }
     if constexpr (DR > 0) {
         if (blockIdx.y == CHUNKS) {
             for (int i = tid; i < nb * (DR / 2); i += 256) {
@@ -274,7 +286,6 @@ __global__ void __launch_bounds__(256) absorb_kernel(const __grid_constant__ Abs
     float wv[16];
 #pragma unroll
     for (int u = 0; u < 16; ++u) wv[u] = col < RK ? bf_to_f(W[(warp * 16 + u) * RK]) : 0.f;
-    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) node_prefix(p);
     for (int i = tid; i < 16 * kD; i += 256) {
         const int bi = i >> 7, e = i & (kD - 1);
         qs[bi][e] = bi < nb ? load_elem(a.q, (static_cast<int64_t>(b0 + bi) * p.H + h) * kD + e, a.io_bf16) : 0.f;
@@ -1123,121 +1134,135 @@ __global__ void __launch_bounds__(L<RK, RV, DR>::WARPS * 32, 1) leaf_kernel(cons
 
 // ------------------------------------------------------------------------------------------- join kernel
 
-// Grid (H, ceil(B / spb)), 128 threads; SPB: the sequences that the projection is unrolled for.
+// Grid (H, ceil(B / spb)), 256 threads; SPB: the sequences that the projection is unrolled for.  W_up,t^V of the head waits in
+// shared memory, and what a sequence's nodes are in registers, when the records are there.
+constexpr int kJoinThreads = 256;
+template <int RV>
+struct J {
+    static constexpr int WROW = RV * 2 + 16;  // bytes of a row of W_up^V, padded: rows 16 bytes apart in the banks
+    static constexpr int SMEM = kD * WROW;
+};
 template <int RV, int SPB>
-__global__ void __launch_bounds__(128, 1) join_kernel(const __grid_constant__ JoinParams a) {
-    constexpr int RS = record_floats(RV), NW = RV / 8, NJ = (RV + 31) / 32;
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ JoinParams a) {
+    constexpr int RS = record_floats(RV), NJ = (RV + 31) / 32, HALF = (RV / 8 + 1) / 2;  // 16-byte words of half a row
+    extern __shared__ __align__(16) char jw[];
     __shared__ __align__(16) float ob[SPB][RV];
-    __shared__ float coef[SPB][3], scs[SPB];
+    __shared__ float coef[SPB][3], halves[SPB][kD];
     const TrunkParams &p = a.t;
     const int h = blockIdx.x, b0 = blockIdx.y * a.spb, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int nb = min(a.spb, p.B - b0);
     const int64_t th = static_cast<int64_t>(h) * a.T + a.loop;
     auto iorow = [&](int b) { return static_cast<int64_t>(b) * p.H + h; };
-    // this thread's row of W_up^V and mu^V, the current tokens' scores and values: inputs of the call, before the wait
-    const uint4 *W = reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.w_up_v) + (th * kD + tid) * RV);
-    uint4 wr[NW];
-#pragma unroll
-    for (int j = 0; j < NW; ++j) wr[j] = W[j];
-    const float muv = a.mu_v ? a.mu_v[th * kD + tid] : 0.f;
-    float cv[SPB];
-#pragma unroll
-    for (int bi = 0; bi < SPB; ++bi) cv[bi] = a.cur_v && bi < nb ? load_elem(a.cur_v, iorow(b0 + bi) * kD + tid, a.io_bf16) : 0.f;
+    const char *W = static_cast<const char *>(a.w_up_v) + th * kD * RV * 2;
+    for (int i = tid; i < kD * (RV / 8); i += kJoinThreads) {
+        const int e = i / (RV / 8), c = i - e * (RV / 8);
+        cp_async16(jw + e * J<RV>::WROW + c * 16, W + i * 16);
+    }
+    cp_async_commit();
+    const int e = tid & (kD - 1), half = tid >> 7;  // this thread's output row, and half of its sum
+    const float muv = a.mu_v && half == 0 ? a.mu_v[th * kD + e] : 0.f;
+    // G warps per sequence: warp `sub` of them takes the columns lane + 32 (sub + G j)
+    int G = 1;
+    while (2 * G * nb <= kJoinThreads / 32) G *= 2;
+    const int bi = warp / G, sub = warp - bi * G, b = b0 + min(bi, nb - 1);
+    // (inputs of the call, before the wait:) the current token's score; lane l < 4 knows level l's node of the sequence, lane 3
+    // its own pages
+    float qk = -INFINITY;
     if (a.cur_k) {
-        for (int bi = warp; bi < nb; bi += 4) {
-            const int64_t row = iorow(b0 + bi);
-            float qk = 0.f;
+        const int64_t row = iorow(b);
+        qk = 0.f;
 #pragma unroll
-            for (int i = 0; i < kD / 32; ++i)
-                qk = fmaf(load_elem(a.q, row * kD + lane + 32 * i, a.io_bf16), load_elem(a.cur_k, row * kD + lane + 32 * i, a.io_bf16), qk);
-            for (int i = lane; i < a.d_rope; i += 32)  // both stand at one position: the rotation cancels
-                qk = fmaf(load_elem(a.q_rope, row * a.d_rope + i, a.io_bf16),
-                          load_elem(a.cur_k_rope, static_cast<int64_t>(b0 + bi) * a.d_rope + i, a.io_bf16), qk);
-            qk = warp_sum(qk);
-            if (lane == 0) scs[bi] = qk * a.scale_log2;
+        for (int i = 0; i < kD / 32; ++i)
+            qk = fmaf(load_elem(a.q, row * kD + lane + 32 * i, a.io_bf16), load_elem(a.cur_k, row * kD + lane + 32 * i, a.io_bf16), qk);
+        for (int i = lane; i < a.d_rope; i += 32)  // both stand at one position: the rotation cancels
+            qk = fmaf(load_elem(a.q_rope, row * a.d_rope + i, a.io_bf16), load_elem(a.cur_k_rope, static_cast<int64_t>(b) * a.d_rope + i, a.io_bf16), qk);
+        qk = warp_sum(qk) * a.scale_log2;
+    }
+    const int groups = count_groups(p), nodes = groups + p.B;
+    int node = groups + b, rank = 0;
+    bool there = lane == kLevels;
+    if (lane < kLevels) {
+        const int col = p.plan.column[static_cast<int64_t>(lane) * p.B + b];
+        there = col >= 0 && col / kMembers < groups;
+        if (there) {
+            node = col / kMembers;
+            rank = col % kMembers;
         }
     }
-    __syncthreads();
+    Node d = {0, 0, 0, 0, 0, 0};
+    if (there) d = node_at(p, groups, node);
+    there = d.pages > 0 && rank < d.n;
     pdl_wait();
-    const int groups = count_groups(p), nodes = groups + p.B;
-    // the split of find_share
-    const int np[2] = {p.pstart[nodes] * p.H, p.pstart[nodes + 1] * p.H};
-    const int we[2] = {min(a.grid, np[0]), min(a.workers, np[1])};
-    // G warps per sequence: warp `sub` of them takes the columns lane + 32 (sub + G q)
-    const int G = nb == 1 ? 4 : nb == 2 ? 2 : 1;
-    const int grp = warp / G, sub = warp - grp * G;
-    for (int bi = grp; bi < SPB; bi += 4 / G) {
-        if (bi >= nb) {
-            for (int j = lane + 32 * sub; j < RV; j += 32 * G) ob[bi][j] = 0.f;
-            continue;
-        }
-        const int b = b0 + bi;
-        // the states of the runs of the sequence's nodes, up to 32 at a time
-        float M = -INFINITY, l = 0.f;
-        float acc[NJ];
+    // the runs of the nodes: records first + step i of run i
+    int runs = 0, first = 0, step = 0;
+    if (there) {
+        const int kind = is_leaf(d), np = p.pstart[nodes + kind] * p.H, we = min(kind ? a.workers : a.grid, np);  // the split of find_share
+        const int s0 = p.pstart[node] * p.H + h * d.pages, c0 = cta_of(s0, np, we);
+        runs = cta_of(s0 + d.pages - 1, np, we) - c0 + 1;
+        first = static_cast<int>(record_of(p, d, h, c0)) + rank;
+        step = kind ? kLeaf : kMembers;
+    }
+    int upto[kLevels + 1];  // runs of the nodes up to each
 #pragma unroll
-        for (int q = 0; q < NJ; ++q) acc[q] = 0.f;
+    for (int l = 0; l <= kLevels; ++l) upto[l] = (l ? upto[l - 1] : 0) + __shfl_sync(0xffffffffu, runs, l);
+    const float beta = p.beta[iorow(b)];
+    float M = -INFINITY, l = 0.f;
+    float acc[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[j] = 0.f;
+    if (bi < nb) {
 #pragma unroll 1
-        for (int level = 0; level <= kLevels; ++level) {
-            int i = groups + b, q = 0;
-            if (level < kLevels) {
-                const int col = p.plan.column[static_cast<int64_t>(level) * p.B + b];
-                if (col < 0 || col / kMembers >= groups) continue;
-                i = col / kMembers;
-                q = col % kMembers;
-            }
-            const Node d = node_at(p, groups, i);
-            if (d.pages == 0 || q >= d.n) continue;
-            const int kind = is_leaf(d), s0 = p.pstart[i] * p.H + h * d.pages;
-            const int c0 = cta_of(s0, np[kind], we[kind]), c1 = cta_of(s0 + d.pages - 1, np[kind], we[kind]);
-            const int64_t step = static_cast<int64_t>(kind ? kLeaf : kMembers) * RS;
-            const float *first = p.part + (record_of(p, d, h, c0) + q) * RS;
+        for (int r0 = 0; r0 < upto[kLevels]; r0 += 32) {
+            const int nr = min(32, upto[kLevels] - r0), r = r0 + min(lane, nr - 1);
+            int level = 0, in = r;
+#pragma unroll
+            for (int k = 0; k < kLevels; ++k)
+                if (r >= upto[k]) {
+                    level = k + 1;
+                    in = r - upto[k];
+                }
+            const int rec = __shfl_sync(0xffffffffu, first, level) + in * __shfl_sync(0xffffffffu, step, level);
+            const float2 ml = *reinterpret_cast<const float2 *>(p.part + static_cast<int64_t>(rec) * RS + RV);
+            const float mi = lane < nr ? ml.x : -INFINITY;
+            const float Mn = fmaxf(M, warp_max(mi)), f = M == -INFINITY ? 0.f : ex2_approx(M - Mn);
+            const float wi = mi == -INFINITY ? 0.f : ex2_approx(mi - Mn);
+            M = Mn;
+            l = fmaf(l, f, warp_sum(lane < nr ? wi * ml.y : 0.f));
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) acc[j] *= f;
+            constexpr int KR = 4;  // runs whose loads are in flight together
 #pragma unroll 1
-            for (int c = c0; c <= c1; c += 32) {
-                const int nr = min(32, c1 - c + 1);
-                const float *mine = first + (c - c0 + min(lane, nr - 1)) * step;
-                const float mi = lane < nr ? mine[RV] : -INFINITY, li = mine[RV + 1];
-                const float Mn = fmaxf(M, warp_max(mi)), f = M == -INFINITY ? 0.f : ex2_approx(M - Mn);
-                const float wi = mi == -INFINITY ? 0.f : ex2_approx(mi - Mn);
-                M = Mn;
-                l = fmaf(l, f, warp_sum(lane < nr ? wi * li : 0.f));
+            for (int k0 = 0; k0 < nr; k0 += KR) {
+                float v[KR][NJ];
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) acc[j] *= f;
-                constexpr int KR = 4;  // runs whose loads are in flight together
-#pragma unroll 1
-                for (int k0 = 0; k0 < nr; k0 += KR) {
-                    float v[KR][NJ];
+                for (int k = 0; k < KR; ++k) {
+                    const float *pr = p.part + static_cast<int64_t>(__shfl_sync(0xffffffffu, rec, min(k0 + k, nr - 1))) * RS;
 #pragma unroll
-                    for (int k = 0; k < KR; ++k) {
-                        const float *pr = first + (c - c0 + min(k0 + k, nr - 1)) * step;
-#pragma unroll
-                        for (int j = 0; j < NJ; ++j) {
-                            const int e = lane + 32 * (sub + G * j);
-                            v[k][j] = e < RV ? pr[e] : 0.f;
-                        }
+                    for (int j = 0; j < NJ; ++j) {
+                        const int c = lane + 32 * (sub + G * j);
+                        v[k][j] = c < RV ? pr[c] : 0.f;
                     }
+                }
 #pragma unroll
-                    for (int k = 0; k < KR; ++k) {
-                        const float wk = __shfl_sync(0xffffffffu, wi, k0 + k);  // (0 behind the last)
-                        if (wk != 0.f && k0 + k < nr) {  // warp-uniform (a NaN state stays one)
+                for (int k = 0; k < KR; ++k) {
+                    const float wk = __shfl_sync(0xffffffffu, wi, k0 + k);  // (0 behind the last)
+                    if (wk != 0.f && k0 + k < nr) {  // warp-uniform (a NaN state stays one)
 #pragma unroll
-                            for (int j = 0; j < NJ; ++j) acc[j] = fmaf(wk, v[k][j], acc[j]);
-                        }
+                        for (int j = 0; j < NJ; ++j) acc[j] = fmaf(wk, v[k][j], acc[j]);
                     }
                 }
             }
         }
 #pragma unroll
-        for (int q = 0; q < NJ; ++q) {
-            const int j = lane + 32 * (sub + G * q);
-            if (j < RV) ob[bi][j] = acc[q];
+        for (int j = 0; j < NJ; ++j) {
+            const int c = lane + 32 * (sub + G * j);
+            if (c < RV) ob[bi][c] = acc[j];
         }
         if (sub == 0 && lane == 0) {
-            const float sc = a.cur_k ? scs[bi] : -INFINITY;
-            M += p.beta[iorow(b)];  // the same for all of a query's cached tokens
-            const float Mx = fmaxf(M, sc);
+            M += beta;  // the same for all of a query's cached tokens
+            const float Mx = fmaxf(M, qk);
             const float al = M == -INFINITY ? 0.f : ex2_approx(M - Mx);
-            const float pc = a.cur_k ? ex2_approx(sc - Mx) : 0.f;
+            const float pc = a.cur_k ? ex2_approx(qk - Mx) : 0.f;
             const float den = al * l + pc;
             const float inv = den == 0.f ? 0.f : 1.f / den;
             coef[bi][0] = al * inv;
@@ -1245,33 +1270,43 @@ __global__ void __launch_bounds__(128, 1) join_kernel(const __grid_constant__ Jo
             coef[bi][2] = pc * inv;
         }
     }
-    __syncthreads();
-    // out_b[e] = coef0 (W_up^V o~_b)[e] + coef1 mu^V[e] + coef2 v_cur,b[e]
-    float acc[SPB];
-#pragma unroll
-    for (int bi = 0; bi < SPB; ++bi) acc[bi] = 0.f;
-#pragma unroll
-    for (int j = 0; j < NW; ++j) {
-        const float2 w0 = bf2_to_f2(wr[j].x), w1 = bf2_to_f2(wr[j].y), w2 = bf2_to_f2(wr[j].z), w3 = bf2_to_f2(wr[j].w);
-#pragma unroll
-        for (int bi = 0; bi < SPB; ++bi) {
-            const float4 o0 = *reinterpret_cast<const float4 *>(&ob[bi][j * 8]);
-            const float4 o1 = *reinterpret_cast<const float4 *>(&ob[bi][j * 8 + 4]);
-            float s = acc[bi];
-            s = fmaf(w0.x, o0.x, s); s = fmaf(w0.y, o0.y, s); s = fmaf(w1.x, o0.z, s); s = fmaf(w1.y, o0.w, s);
-            s = fmaf(w2.x, o1.x, s); s = fmaf(w2.y, o1.y, s); s = fmaf(w3.x, o1.z, s); s = fmaf(w3.y, o1.w, s);
-            acc[bi] = s;
-        }
-    }
-#pragma unroll
-    for (int bi = 0; bi < SPB; ++bi) {
-        if (bi >= nb) break;
-        float v = acc[bi] * coef[bi][0] + coef[bi][1] * muv;
-        if (a.cur_v) v = fmaf(coef[bi][2], cv[bi], v);
-        store_elem(a.out, iorow(b0 + bi) * kD + tid, v, a.io_bf16);
-    }
+    for (int i = tid; i < (SPB - nb) * RV; i += kJoinThreads) ob[nb + i / RV][i % RV] = 0.f;
+    cp_async_wait_all();
     __syncthreads();
     pdl_trigger();
+    // out_b[e] = coef0 (W_up^V o~_b)[e] + coef1 mu^V[e] + coef2 v_cur,b[e], the sum of a row in two halves
+    float sum[SPB];
+#pragma unroll
+    for (int i = 0; i < SPB; ++i) sum[i] = 0.f;
+    const char *wrow = jw + e * J<RV>::WROW;
+#pragma unroll 2
+    for (int j = half * HALF; j < (half ? RV / 8 : HALF); ++j) {
+        const uint4 w4 = *reinterpret_cast<const uint4 *>(wrow + j * 16);
+        const float2 w0 = bf2_to_f2(w4.x), w1 = bf2_to_f2(w4.y), w2 = bf2_to_f2(w4.z), w3 = bf2_to_f2(w4.w);
+#pragma unroll
+        for (int i = 0; i < SPB; ++i) {
+            const float4 o0 = *reinterpret_cast<const float4 *>(&ob[i][j * 8]);
+            const float4 o1 = *reinterpret_cast<const float4 *>(&ob[i][j * 8 + 4]);
+            float s = sum[i];
+            s = fmaf(w0.x, o0.x, s); s = fmaf(w0.y, o0.y, s); s = fmaf(w1.x, o0.z, s); s = fmaf(w1.y, o0.w, s);
+            s = fmaf(w2.x, o1.x, s); s = fmaf(w2.y, o1.y, s); s = fmaf(w3.x, o1.z, s); s = fmaf(w3.y, o1.w, s);
+            sum[i] = s;
+        }
+    }
+    if (half == 1) {
+#pragma unroll
+        for (int i = 0; i < SPB; ++i) halves[i][e] = sum[i];
+    }
+    __syncthreads();
+    if (half == 0) {
+#pragma unroll
+        for (int i = 0; i < SPB; ++i) {
+            if (i >= nb) break;
+            float v = (sum[i] + halves[i][e]) * coef[i][0] + coef[i][1] * muv;
+            if (a.cur_v) v = fmaf(coef[i][2], load_elem(a.cur_v, iorow(b0 + i) * kD + e, a.io_bf16), v);
+            store_elem(a.out, iorow(b0 + i) * kD + e, v, a.io_bf16);
+        }
+    }
 }
 
 // ----------------------------------------------------------------------------------------------- host side
@@ -1345,7 +1380,7 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
         for (int j = 0; j < DR / 2; ++j) ap.axis[j] = rope.axis[j];
         rotary_phases(DR, rope.base, ap.phi);
     }
-    if ((st = launch_ex(absorb_kernel<RK, DR>, dim3(a.H, (ZZ::RKX + 31) / 32 + (DR > 0), (a.B + 15) / 16), 256, 0, stream, ap)) != LLA_OK)
+    if ((st = launch_ex(absorb_kernel<RK, DR>, dim3(a.H, (ZZ::RKX + 31) / 32 + (DR > 0) + 1, (a.B + 15) / 16), 256, 0, stream, ap)) != LLA_OK)
         return st;
     if ((st = launch_ex(trunk_kernel<RK, RV, DR>, dim3(grid), kTrunkThreads, ZZ::SMEM, stream, tv, tp)) != LLA_OK) return st;
     if ((st = launch_ex(leaf_kernel<RK, RV, DR>, dim3(grid), LL::WARPS * 32, LL::SMEM, stream, tp)) != LLA_OK) return st;
@@ -1361,9 +1396,15 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     const int64_t units = static_cast<int64_t>(a.B) * a.H;
     jp.spb = static_cast<int>(std::min<int64_t>(kJoinSeqs, std::max<int64_t>(1, (units + 2 * grid - 1) / (2 * grid))));
     const dim3 jg(a.H, (a.B + jp.spb - 1) / jp.spb);
-    if (jp.spb <= 2) return launch_ex(join_kernel<RV, 2>, jg, 128, 0, stream, jp);
-    if (jp.spb <= 4) return launch_ex(join_kernel<RV, 4>, jg, 128, 0, stream, jp);
-    return launch_ex(join_kernel<RV, 8>, jg, 128, 0, stream, jp);
+    auto join = [&](auto spb) {
+        constexpr int SPB = decltype(spb)::value;
+        static DeviceOnce configured_join;
+        if (raise_smem_limit(join_kernel<RV, SPB>, J<RV>::SMEM, configured_join) != LLA_OK) return LLA_ERR_CUDA;
+        return launch_ex(join_kernel<RV, SPB>, jg, kJoinThreads, J<RV>::SMEM, stream, jp);
+    };
+    if (jp.spb <= 2) return join(std::integral_constant<int, 2>());
+    if (jp.spb <= 4) return join(std::integral_constant<int, 4>());
+    return join(std::integral_constant<int, 8>());
 }
 
 }  // namespace
