@@ -159,6 +159,18 @@ __device__ __forceinline__ int64_t record_of(const TrunkParams &p, const Node &d
 }
 __host__ __device__ constexpr int record_floats(int rv) { return rv + 4; }
 
+// np pages over w workers (0 < w <= np): the first np % w of them take a page more than the others.  32-bit arithmetic: a
+// 64-bit division is a called subroutine.
+struct Split {
+    int each, more;  // pages of a worker, and workers that take one more
+    __device__ __forceinline__ Split(int np, int w) : each(np / max(w, 1)), more(np - each * w) {}
+    __device__ __forceinline__ int begin(int c) const { return c * each + min(c, more); }
+    __device__ __forceinline__ int worker(int page) const {
+        const int wide = more * (each + 1);
+        return page < wide ? page / (each + 1) : more + (page - wide) / each;
+    }
+};
+
 // ----------------------------------------------------------------------------------------- absorb kernel
 
 // One CTA: the prefix sums of the nodes' pages, and the flags of what node_at leaves out.
@@ -291,7 +303,7 @@ __global__ void __launch_bounds__(256) absorb_kernel(const __grid_constant__ Abs
         qs[bi][e] = bi < nb ? load_elem(a.q, (static_cast<int64_t>(b0 + bi) * p.H + h) * kD + e, a.io_bf16) : 0.f;
     }
     __syncthreads();
-#pragma unroll
+#pragma unroll 4
     for (int bi = 0; bi < 16; ++bi) {
         float s = 0.f;
 #pragma unroll
@@ -343,8 +355,9 @@ struct Z {
     static constexpr int QROW = 3 * RKT * 2;                // bytes of a query's parts
     static constexpr int XCOLS = RVX / 2, XROW = XCOLS + 4;  // columns of O exchanged at once, floats of their row
     static constexpr int NBAR = 40;
-    static constexpr int EXCH = 64 * XROW * 4;
-    static constexpr int RED = (kRows + 2 * 2 * 64 * 2) * 4;  // running maxima; maxima and sums of two runs and groups
+    static constexpr int EXCH = 96 * XROW * 4;
+    // running maxima; maxima and sums of two runs and groups; a page's maxima of either group
+    static constexpr int RED = (kRows + 2 * 2 * 64 * 2 + 2 * 64) * 4;
     static constexpr int FIXED = QB + EXCH + RED + NBAR * 8 + kMaxNodes * 2;
     static constexpr int ST0 = (kSmemCap - 2048 - FIXED) / (KPAGE + VPAGE);
     static constexpr int ST = ST0 > 5 ? 5 : ST0;
@@ -417,8 +430,9 @@ __device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list, in
     Share r;
     r.np = np;
     r.we = we;
-    r.g0 = w0 < we ? page_lo(w0, np, we) : 0;
-    r.g1 = w0 < we ? page_lo(min(w0 + ws, we), np, we) : 0;
+    const Split split(np, we);
+    r.g0 = w0 < we ? split.begin(w0) : 0;
+    r.g1 = w0 < we ? split.begin(min(w0 + ws, we)) : 0;
     int mine = 0, ex = ex0;
     for (int i = tid * per; i < min(nodes, (tid + 1) * per); ++i) {
         const int n = pages(i);
@@ -501,6 +515,150 @@ __device__ __forceinline__ const char *query_parts(const TrunkParams &p, const T
 // A value that every lane has, for a warp that issues products (their descriptors are in uniform registers then).
 __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 
+// The 128 rows hold R queries 128 / R times: replica i = row / R has part i % 2 of their weights p for the tokens
+// R (i / 2) to R (i / 2) + R - 1 of each page, and zeros for the others, so that a thread works on R tokens and the sum of a
+// query's rows of O is the sum over all tokens of both parts.  (With R = 64 for all, two of the four schedulers did the
+// work of up to 32 queries.)
+__device__ __forceinline__ int replica_rows(int n) { return n > 32 ? 64 : n > 16 ? 32 : 16; }
+struct SoftmaxCtx {
+    uint64_t *bar;
+    volatile int *abort_flag;
+    unsigned *err;
+    float *running, *page_max;
+    float2 *states;
+    int total, g;  // pages of the CTA, this group
+};
+
+template <int N>
+__device__ __forceinline__ void tmem_ld_n(uint32_t taddr, float (&v)[N]) {
+    static_assert(N == 16 || N == 32 || N == 64, "columns");
+    if constexpr (N == 16) {
+        tmem_ld16(taddr, v);
+    } else {
+        uint32_t a[32], b[32];
+        tmem_ld32_nowait(taddr, a);
+        if constexpr (N == 64) tmem_ld32_nowait(taddr + 32, b);
+        tmem_wait_ld(a);
+        if constexpr (N == 64) tmem_wait_ld(b);
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+            v[c] = __uint_as_float(a[c]);
+            if constexpr (N == 64) v[32 + c] = __uint_as_float(b[c]);
+        }
+    }
+}
+
+template <typename ZZ, int R>
+__device__ __forceinline__ void softmax_run(const SoftmaxCtx &x, int run, int it, int pages) {
+    const int g = x.g, quarter = (threadIdx.x >> 5) & 3, lane = threadIdx.x & 31, row = 32 * quarter + lane;
+    const int replica = row / R, slice = replica >> 1, q = row % R;
+    const bool second = replica & 1;
+    const uint32_t tl = static_cast<uint32_t>(32 * quarter) << 16;
+    const int col0 = R == 64 ? 0 : R == 32 ? 32 * (quarter >> 1) : 16 * quarter;  // the slice's tokens (of a whole warp)
+    const uint32_t ts = tl + ZZ::TM_S + g * kPT + col0, tp = tl + ZZ::TM_P + g * ZZ::P_STEP;
+    float m = -INFINITY, l = 0.f;
+    const int first = it + ((it ^ g) & 1), end = it + pages;
+    for (int j = first; j < end; j += 2) {
+        const int jj = j >> 1, k = j - it;
+        mbar_wait(&x.bar[bSfull + g], jj & 1, x.abort_flag, x.err);
+        tc_fence_after();
+        float s[R];
+        tmem_ld_n<R>(ts, s);
+        tc_fence_before();
+        mbar_arrive(&x.bar[bSfree + g]);
+        float t[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) t[c] = s[c];
+#pragma unroll
+        for (int c = 4; c < R; c += 8)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] = c + 4 + e < R ? fmaxf(fmaxf(t[e], s[c + e]), s[c + 4 + e]) : fmaxf(t[e], s[c + e]);
+        float mx = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+        // The running maximum after the page before, from the other group's thread of this row; each page's weights are
+        // relative to the running maximum that its own step leaves.  Also between runs, where nothing is handed over:
+        // what the other group reads here is not written again before it has.
+        if (j > 0) {
+            named_bar_sync(1 + quarter * 2 + ((j - 1) & 1), 64);
+            const float mp = k > 0 ? x.running[row] : m;
+            if (mp != m) {
+                l *= ex2_approx(m - mp);  // (m = -inf: no page yet, l = 0)
+                m = mp;
+            }
+        }
+        // the page's maximum over the slices, where one of them raises it
+        if (R < 64 && named_bar_or(10 + g, 128, mx > m + kRescaleLog2)) {
+            if (!second) x.page_max[g * 64 + slice * R + q] = mx;
+            named_bar_sync(10 + g, 128);
+#pragma unroll
+            for (int i = 0; i < 64 / R; ++i) mx = fmaxf(mx, x.page_max[g * 64 + i * R + q]);
+        }
+        const float m_new = fmaxf(m, mx);
+        const bool need = m_new > m + kRescaleLog2;  // also the first page
+        const float factor = need ? ex2_approx(m - m_new) : 1.f;
+        if (need) {
+            l *= factor;
+            m = m_new;
+        }
+        if (j + 1 < x.total) {
+            x.running[row] = m;
+            named_bar_arrive(1 + quarter * 2 + (j & 1), 64);
+        }
+        const bool any = __any_sync(0xffffffffu, need && k > 0);
+        // this group's page before has been read by its product (and O holds it)
+        if (jj > 0) mbar_wait(&x.bar[bPfree + g], (jj - 1) & 1, x.abort_flag, x.err);
+        if (any) {
+            // O holds the run's pages before this one: wait for the last of them, which is the other group's (products
+            // complete in order, so that its barrier is at most one phase behind), and rescale
+            mbar_wait(&x.bar[bPfree + (g ^ 1)], ((j - 1) >> 1) & 1, x.abort_flag, x.err);
+            tc_fence_after();
+#pragma unroll 1
+            for (int c0 = 0; c0 < ZZ::RVX; c0 += 16) {
+                float v[16];
+                tmem_ld16(tl + ZZ::TM_O + c0, v);
+#pragma unroll
+                for (int c = 0; c < 16; ++c) v[c] *= factor;
+                tmem_st16(tl + ZZ::TM_O + c0, v);
+            }
+        }
+        tc_fence_after();
+        if (R < 64 && (ZZ::ALIAS || j == first)) {  // the other slices' tokens
+            uint32_t zero[16];
+#pragma unroll
+            for (int c = 0; c < 16; ++c) zero[c] = 0;
+            tmem_st16u(tp, zero);
+            tmem_st16u(tp + 16, zero);
+            tmem_wait_st();
+        }
+        const float2 mm = make_float2(-m, -m);
+        uint32_t pw[R / 2];
+        float2 s4[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s4[e] = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int c = 0; c < R; c += 2) {
+            float2 y = __fadd2_rn(make_float2(s[c], s[c + 1]), mm);
+            y.x = ex2_approx(y.x);
+            y.y = ex2_approx(y.y);
+            s4[(c >> 1) & 3] = __fadd2_rn(s4[(c >> 1) & 3], y);
+            pw[c / 2] = pack_bf16x2(y.x, y.y);
+            const float2 f = bf2_to_f2(pw[c / 2]);
+            if (second) pw[c / 2] = pack_bf16x2(y.x - f.x, y.y - f.y);
+        }
+        const float2 sa = __fadd2_rn(s4[0], s4[1]), sb = __fadd2_rn(s4[2], s4[3]);
+        l += (sa.x + sa.y) + (sb.x + sb.y);
+        if constexpr (R == 64) tmem_st32u_nowait(tp, pw);
+        else if constexpr (R == 32) tmem_st16u(tp + col0 / 2, pw);
+        else tmem_st8u(tp + col0 / 2, pw);
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(&x.bar[bPfull + g]);
+    }
+    // this group's maxima and sums of the run, once the run before the last has been read from there
+    if (run >= 2) mbar_wait(&x.bar[bOfree + (run & 1)], ((run - 2) >> 1) & 1, x.abort_flag, x.err);
+    if (!second) x.states[((run & 1) * 2 + g) * 64 + slice * R + q] = make_float2(m, l);
+    mbar_arrive(&x.bar[bMfull + (run & 1)]);
+}
+
 template <int RK, int RV, int DR>
 __global__ void __launch_bounds__(kTrunkThreads, 1)
     trunk_kernel(const __grid_constant__ CUtensorMap tv, const __grid_constant__ TrunkParams p) {
@@ -512,6 +670,7 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
     uint32_t *tslot = reinterpret_cast<uint32_t *>(bar + bTslot);
     float *running = reinterpret_cast<float *>(sm + ZZ::oRed);          // [128] maxima
     float2 *states = reinterpret_cast<float2 *>(running + kRows);       // [2 runs][2 groups][64] maxima and sums
+    float *page_max = reinterpret_cast<float *>(states + 2 * 2 * 64);    // [2 groups][64]
     uint16_t *list = reinterpret_cast<uint16_t *>(sm + ZZ::oList);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
@@ -665,146 +824,25 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
         __syncwarp();
     } else if (warp < kAuxWarp) {
         // ------------------------------------------------------------------- softmax, warps 4-7 and 8-11
-        const int g = (warp - kSoftmaxWarp) >> 2, quarter = warp & 3, row = 32 * quarter + lane;
-        const bool second = quarter >= 2;  // rows 64 + q: the second part of p
-        const uint32_t tl = tmem + (static_cast<uint32_t>(32 * quarter) << 16);
-        const uint32_t ts = tl + ZZ::TM_S + g * kPT, tp = tl + ZZ::TM_P + g * ZZ::P_STEP;
-        const int total = sh.g1 - sh.g0;
+        SoftmaxCtx x = {bar, abort_flag, p.err, running, page_max, states, sh.g1 - sh.g0, (warp - kSoftmaxWarp) >> 2};
         int it = 0;
         for (int run = 0; w.next(); ++run) {
-            // warps whose queries the run does not have only keep step
-            const bool active = (quarter & 1) == 0 || w.r.d.n > 32;
-            float m = -INFINITY, l = 0.f;
-            const int end = it + w.r.pages;
-            for (int j = it + ((it ^ g) & 1); j < end; j += 2) {
-                const int jj = j >> 1, k = j - it;
-                const int left = w.r.d.len - (w.r.page + k) * kPT;  // tokens of the page that are there (more than a page: all)
-                mbar_wait(&bar[bSfull + g], jj & 1, abort_flag, p.err);
-                tc_fence_after();
-                float x[kPT];
-                float mx = -INFINITY;
-                if (active) {
-                    uint32_t a[32], b[32];
-                    tmem_ld32_nowait(ts, a);
-                    tmem_ld32_nowait(ts + 32, b);
-                    tmem_wait_ld(a);
-                    tmem_wait_ld(b);
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) {
-                        x[c] = __uint_as_float(a[c]);
-                        x[32 + c] = __uint_as_float(b[c]);
-                    }
-                }
-                tc_fence_before();
-                mbar_arrive(&bar[bSfree + g]);
-                if (active) {
-                    if (left < kPT) {
-#pragma unroll
-                        for (int c = 0; c < kPT; ++c) x[c] = c < left ? x[c] : -INFINITY;
-                    }
-                    float t[4];
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) t[c] = x[c];
-#pragma unroll
-                    for (int c = 4; c < kPT; c += 8)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) t[e] = c + 4 + e < kPT ? fmaxf(fmaxf(t[e], x[c + e]), x[c + 4 + e]) : fmaxf(t[e], x[c + e]);
-                    mx = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-                }
-                // The running maximum after the page before, from the other group's thread of this row; each page's weights are
-                // relative to the running maximum that its own step leaves.  Also between runs, where nothing is handed over:
-                // what the other group reads here is not written again before it has.
-                if (j > 0) {
-                    named_bar_sync(1 + quarter * 2 + ((j - 1) & 1), 64);
-                    const float mp = k > 0 ? running[row] : m;
-                    if (mp != m) {
-                        l *= ex2_approx(m - mp);  // (m = -inf: no page yet, l = 0)
-                        m = mp;
-                    }
-                }
-                const float m_new = fmaxf(m, mx);
-                const bool need = m_new > m + kRescaleLog2;  // also the first page
-                const float factor = need ? ex2_approx(m - m_new) : 1.f;
-                if (need) {
-                    l *= factor;
-                    m = m_new;
-                }
-                if (j + 1 < total) {
-                    running[row] = m;
-                    named_bar_arrive(1 + quarter * 2 + (j & 1), 64);
-                }
-                const bool any = __any_sync(0xffffffffu, need && k > 0);
-                // this group's page before has been read by its product (and O holds it)
-                if (jj > 0) mbar_wait(&bar[bPfree + g], (jj - 1) & 1, abort_flag, p.err);
-                if (any) {
-                    // O holds the run's pages before this one: wait for the last of them, which is the other group's (products
-                    // complete in order, so that its barrier is at most one phase behind), and rescale
-                    mbar_wait(&bar[bPfree + (g ^ 1)], ((j - 1) >> 1) & 1, abort_flag, p.err);
-                    tc_fence_after();
-#pragma unroll 1
-                    for (int c0 = 0; c0 < ZZ::RVX; c0 += 16) {
-                        float v[16];
-                        tmem_ld16(tl + ZZ::TM_O + c0, v);
-#pragma unroll
-                        for (int c = 0; c < 16; ++c) v[c] *= factor;
-                        tmem_st16(tl + ZZ::TM_O + c0, v);
-                    }
-                }
-                if (active) {
-                    const float2 mm = make_float2(-m, -m);
-                    uint32_t pw[kPT / 2];
-                    float2 s4[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s4[e] = make_float2(0.f, 0.f);
-#pragma unroll
-                    for (int c = 0; c < kPT; c += 2) {
-                        float2 y = __fadd2_rn(make_float2(x[c], x[c + 1]), mm);
-                        y.x = ex2_approx(y.x);
-                        y.y = ex2_approx(y.y);
-                        s4[(c >> 1) & 3] = __fadd2_rn(s4[(c >> 1) & 3], y);
-                        pw[c / 2] = pack_bf16x2(y.x, y.y);
-                        if (second) {
-                            const float2 f = bf2_to_f2(pw[c / 2]);
-                            pw[c / 2] = pack_bf16x2(y.x - f.x, y.y - f.y);
-                        }
-                    }
-                    const float2 sa = __fadd2_rn(s4[0], s4[1]), sb = __fadd2_rn(s4[2], s4[3]);
-                    l += (sa.x + sa.y) + (sb.x + sb.y);
-                    tc_fence_after();
-                    tmem_st32u_nowait(tp, pw);
-                }
-                if (left < kPT) {
-                    // V rows past the sequence hold no latents: zero them (0 * NaN would poison O)
-                    const int st = j % ZZ::ST;
-                    mbar_wait(&bar[bVfull + st], (j / ZZ::ST) & 1, abort_flag, p.err);
-                    char *vs = sm + ZZ::oV + st * ZZ::VPAGE;
-                    for (int i = row; i < (kPT - left) * ZZ::NBOX * 8; i += 128) {
-                        const int chunk = i & 7, box = (i >> 3) % ZZ::NBOX, tr = left + (i >> 3) / ZZ::NBOX;
-                        *reinterpret_cast<uint4 *>(vs + box * ZZ::BOX + tr * 128 + chunk * 16) = make_uint4(0, 0, 0, 0);
-                    }
-                    fence_proxy_async_smem();
-                }
-                tmem_wait_st();
-                tc_fence_before();
-                mbar_arrive(&bar[bPfull + g]);
-            }
-            it = end;
-            // this group's maximum and sum of the run, once the run before the last has been read from there
-            if (run >= 2) mbar_wait(&bar[bOfree + (run & 1)], ((run - 2) >> 1) & 1, abort_flag, p.err);
-            if (!second) states[((run & 1) * 2 + g) * 64 + row] = make_float2(m, l);
-            mbar_arrive(&bar[bMfull + (run & 1)]);
+            if (w.r.d.n > 32) softmax_run<ZZ, 64>(x, run, it, w.r.pages);
+            else if (w.r.d.n > 16) softmax_run<ZZ, 32>(x, run, it, w.r.pages);
+            else softmax_run<ZZ, 16>(x, run, it, w.r.pages);
+            it += w.r.pages;
         }
     } else {
         // --------------------------------------------------------- q~ and epilogue, warps 12-15
         constexpr int RS = record_floats(RV);
-        const int quarter = warp & 3, row = 32 * quarter + lane, q = row & 63;
+        const int quarter = warp & 3, row = 32 * quarter + lane;
         const uint32_t tl = tmem + (static_cast<uint32_t>(32 * quarter) << 16);
         // the parts of a run's queries into TMEM: row by row, words of two columns
         constexpr int kAtOnce = ZZ::RKT % 96 == 0 ? 6 : ZZ::RKT % 80 == 0 ? 5 : 4;  // pairs of 16-byte words
         static_assert(ZZ::RKT % (16 * kAtOnce) == 0, "words of two");
         auto load_queries = [&](const TrunkRun &r) {
-            if ((quarter & 1) == 0 || r.d.n > 32) {
-                const char *src = query_parts<ZZ::QROW>(p, r, q);
+            {
+                const char *src = query_parts<ZZ::QROW>(p, r, row & (replica_rows(r.d.n) - 1));
 #pragma unroll 1
                 for (int part = 0; part < 3; ++part)
 #pragma unroll 1
@@ -842,45 +880,71 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
             mbar_wait(&bar[bOdone], run & 1, abort_flag, p.err);
             mbar_wait(&bar[bMfull + (run & 1)], (run >> 1) & 1, abort_flag, p.err);
             tc_fence_after();
-            const int n = w.r.d.n;
+            // the rows of a query: those of 16 queries first within their warp, then the warps' through shared memory
+            const int n = w.r.d.n, R = replica_rows(n), q = row & (R - 1);
+            const bool sums = R == 64 ? quarter < 2 : quarter == 0, mine = sums && (R > 16 || lane < 16) && q < n;
             float *dst = p.part + (record_of(p, w.r.d, w.r.h, blockIdx.x) + q) * RS;
-            {
-                // rows q and 64 + q: the second parts through shared memory
-                float *xr = reinterpret_cast<float *>(sm + ZZ::oExch) + q * ZZ::XROW;
-                const bool mine = q < n;
+            float *exch = reinterpret_cast<float *>(sm + ZZ::oExch);
+            float *xr = exch + (R == 64 ? row - 64 : (quarter - 1) * R + q) * ZZ::XROW;  // of a warp that does not sum
 #pragma unroll 1
-                for (int c0 = 0; c0 < ZZ::RVX; c0 += ZZ::XCOLS) {
-                    if (c0 > 0) named_bar_sync(9, 128);
-                    if (quarter >= 2 && (quarter == 2 || n > 32)) {
+            for (int c0 = 0; c0 < ZZ::RVX; c0 += ZZ::XCOLS) {
+                if (c0 > 0) named_bar_sync(9, 128);
+                if (!sums) {
 #pragma unroll 1
-                        for (int c = 0; c < ZZ::XCOLS; c += 16) {
-                            float o[16];
-                            tmem_ld16(tl + ZZ::TM_O + c0 + c, o);
+                    for (int c = 0; c < ZZ::XCOLS; c += 16) {
+                        float o[16];
+                        tmem_ld16(tl + ZZ::TM_O + c0 + c, o);
+                        if (R == 16) {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] += __shfl_xor_sync(0xffffffffu, o[e], 16);
+                        }
+                        if (R > 16 || lane < 16) {
 #pragma unroll
                             for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4 *>(xr + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                         }
                     }
-                    named_bar_sync(9, 128);
-                    if (quarter < 2 && (quarter == 0 || n > 32)) {
+                }
+                named_bar_sync(9, 128);
+                if (sums) {
 #pragma unroll 1
-                        for (int c = 0; c < ZZ::XCOLS; c += 16) {
-                            float o[16];
-                            tmem_ld16(tl + ZZ::TM_O + c0 + c, o);
+                    for (int c = 0; c < ZZ::XCOLS; c += 16) {
+                        float o[16];
+                        tmem_ld16(tl + ZZ::TM_O + c0 + c, o);
+                        if (R == 16) {
 #pragma unroll
-                            for (int e = 0; e < 16; e += 4) {
-                                const float4 v = *reinterpret_cast<const float4 *>(xr + c + e);
-                                if (mine && c0 + c + e < RV)
-                                    *reinterpret_cast<float4 *>(dst + c0 + c + e) = make_float4(o[e] + v.x, o[e + 1] + v.y, o[e + 2] + v.z, o[e + 3] + v.w);
+                            for (int e = 0; e < 16; ++e) o[e] += __shfl_xor_sync(0xffffffffu, o[e], 16);
+                        }
+                        if (mine) {
+                            const float *xo = exch + q * ZZ::XROW + c;
+#pragma unroll 1
+                            for (int i = 0; i < (R == 64 ? 1 : 3); ++i, xo += R * ZZ::XROW) {
+#pragma unroll
+                                for (int e = 0; e < 16; e += 4) {
+                                    const float4 v = *reinterpret_cast<const float4 *>(xo + e);
+                                    o[e] += v.x;
+                                    o[e + 1] += v.y;
+                                    o[e + 2] += v.z;
+                                    o[e + 3] += v.w;
+                                }
                             }
+#pragma unroll
+                            for (int e = 0; e < 16; e += 4)
+                                if (c0 + c + e < RV) *reinterpret_cast<float4 *>(dst + c0 + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                         }
                     }
                 }
             }
-            if (quarter < 2 && q < n) {
-                const float2 s0 = states[((run & 1) * 2) * 64 + q], s1 = states[((run & 1) * 2 + 1) * 64 + q];
-                const float mf = fmaxf(s0.x, s1.x);
+            if (mine) {
+                // (a group's slices have one maximum)
+                const float2 *st = states + (run & 1) * 2 * 64;
+                const float m0 = st[q].x, m1 = st[64 + q].x, mf = fmaxf(m0, m1);
+                float l0 = 0.f, l1 = 0.f;
+                for (int i = q; i < 64; i += R) {
+                    l0 += st[i].y;
+                    l1 += st[64 + i].y;
+                }
                 dst[RV] = mf;
-                dst[RV + 1] = (s0.x == mf ? s0.y : s0.y * ex2_approx(s0.x - mf)) + (s1.x == mf ? s1.y : s1.y * ex2_approx(s1.x - mf));
+                dst[RV + 1] = (m0 == mf ? l0 : l0 * ex2_approx(m0 - mf)) + (m1 == mf ? l1 : l1 * ex2_approx(m1 - mf));
             }
             tc_fence_before();
             mbar_arrive(&bar[bOfree + (run & 1)]);
@@ -1016,7 +1080,7 @@ __device__ __forceinline__ void leaf_page(const char *slot, const float *qs, flo
 // that a warp's run boundaries (the queries of the next run, the record of this one) cost nothing until the warps of an SM
 // together cannot keep up.
 template <int RK, int RV, int DR>
-__global__ void __launch_bounds__(L<RK, RV, DR>::WARPS * 32, 1) leaf_kernel(const __grid_constant__ TrunkParams p) {
+__global__ void __launch_bounds__(L<RK, RV, DR>::WARPS * 32, 1) leaf_kernel(const __grid_constant__ TrunkParams p, int alone) {
     using LL = L<RK, RV, DR>;
     constexpr int RS = record_floats(RV);
     extern __shared__ __align__(128) char sm[];
@@ -1035,11 +1099,14 @@ __global__ void __launch_bounds__(L<RK, RV, DR>::WARPS * 32, 1) leaf_kernel(cons
     if (tid == 0) abort_word = 0;
     // The trunk kernel lets this one start when all of its CTAs have waited for the absorb kernel, so that q~ and beta are
     // there and the workspace is free.  Its own records are not read here; the wait for it is at the end.
+    if (alone) pdl_wait();  // there is no trunk kernel between the absorb kernel and this one
+    pdl_trigger();          // the join may take this SM as soon as this CTA has left it
     const int groups = count_groups(p), workers = gridDim.x * LL::WARPS;
     Share sh = find_share<true, LL::WARPS * 32>(p, groups, list, blockIdx.x * LL::WARPS, LL::WARPS, workers);
     const int me = blockIdx.x * LL::WARPS + warp;
-    sh.g0 = me < sh.we ? page_lo(me, sh.np, sh.we) : 0;
-    sh.g1 = me < sh.we ? page_lo(me + 1, sh.np, sh.we) : 0;
+    const Split split(sh.np, sh.we);
+    sh.g0 = me < sh.we ? split.begin(me) : 0;
+    sh.g1 = me < sh.we ? split.begin(me + 1) : 0;
     if (sh.g0 < sh.g1) {
         RunWalk w(p, groups, sh, list);
         PageWalk ahead(w);
@@ -1101,7 +1168,7 @@ __global__ void __launch_bounds__(L<RK, RV, DR>::WARPS * 32, 1) leaf_kernel(cons
                     ok = mbar_wait(&bar[1], it & 1, abort_flag, p.err) && ok;
                 };
                 if (n == 1) leaf_page<LL, 1>(slot, qs, ps, left, m, l, acc, k_read);
-                else leaf_page<LL, kLeaf>(slot, qs, ps, left, m, l, acc, k_read);
+                else leaf_page<LL, 2>(slot, qs, ps, left, m, l, acc, k_read);
                 __syncwarp();
                 if (ok && ahead.ok) {
                     issue_v(blk, ahead.w.r.h);
@@ -1140,14 +1207,16 @@ constexpr int kJoinThreads = 256;
 template <int RV>
 struct J {
     static constexpr int WROW = RV * 2 + 16;  // bytes of a row of W_up^V, padded: rows 16 bytes apart in the banks
-    static constexpr int SMEM = kD * WROW;
+    // (two CTAs an SM: a third waits for an SM that the leaf kernel has not left yet)
+    static constexpr int SMEM = kD * WROW > 84 * 1024 ? kD * WROW : 84 * 1024;
 };
 template <int RV, int SPB>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ JoinParams a) {
-    constexpr int RS = record_floats(RV), NJ = (RV + 31) / 32, HALF = (RV / 8 + 1) / 2;  // 16-byte words of half a row
+    constexpr int RS = record_floats(RV), NJ = (RV + 31) / 32, QUARTER = (RV / 8 + 3) / 4;  // 16-byte words of a quarter row
     extern __shared__ __align__(16) char jw[];
     __shared__ __align__(16) float ob[SPB][RV];
-    __shared__ float coef[SPB][3], halves[SPB][kD];
+    __shared__ float coef[SPB][3];
+    __shared__ float quarters[3][SPB][kD];
     const TrunkParams &p = a.t;
     const int h = blockIdx.x, b0 = blockIdx.y * a.spb, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int nb = min(a.spb, p.B - b0);
@@ -1159,8 +1228,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
         cp_async16(jw + e * J<RV>::WROW + c * 16, W + i * 16);
     }
     cp_async_commit();
-    const int e = tid & (kD - 1), half = tid >> 7;  // this thread's output row, and half of its sum
-    const float muv = a.mu_v && half == 0 ? a.mu_v[th * kD + e] : 0.f;
+    const int e = tid & 63, part = tid >> 6;  // this thread's output rows e and 64 + e, and quarter of their sums
     // G warps per sequence: warp `sub` of them takes the columns lane + 32 (sub + G j)
     int G = 1;
     while (2 * G * nb <= kJoinThreads / 32) G *= 2;
@@ -1192,20 +1260,28 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     Node d = {0, 0, 0, 0, 0, 0};
     if (there) d = node_at(p, groups, node);
     there = d.pages > 0 && rank < d.n;
-    pdl_wait();
+    // Twice: first without a run, while the kernels before still run, so that the instructions are there when the records are
+    // (fetched behind the wait they took longer than the join).
+#pragma unroll 1
+    for (int dry = 1; dry >= 0; --dry) {
+    if (dry == 0) {
+        pdl_wait();
+        pdl_trigger();
+    }
     // the runs of the nodes: records first + step i of run i
     int runs = 0, first = 0, step = 0;
-    if (there) {
+    if (there && dry == 0) {
         const int kind = is_leaf(d), np = p.pstart[nodes + kind] * p.H, we = min(kind ? a.workers : a.grid, np);  // the split of find_share
-        const int s0 = p.pstart[node] * p.H + h * d.pages, c0 = cta_of(s0, np, we);
-        runs = cta_of(s0 + d.pages - 1, np, we) - c0 + 1;
+        const Split split(np, we);
+        const int s0 = p.pstart[node] * p.H + h * d.pages, c0 = split.worker(s0);
+        runs = split.worker(s0 + d.pages - 1) - c0 + 1;
         first = static_cast<int>(record_of(p, d, h, c0)) + rank;
         step = kind ? kLeaf : kMembers;
     }
     int upto[kLevels + 1];  // runs of the nodes up to each
 #pragma unroll
     for (int l = 0; l <= kLevels; ++l) upto[l] = (l ? upto[l - 1] : 0) + __shfl_sync(0xffffffffu, runs, l);
-    const float beta = p.beta[iorow(b)];
+    const float beta = dry ? 0.f : p.beta[iorow(b)];
     float M = -INFINITY, l = 0.f;
     float acc[NJ];
 #pragma unroll
@@ -1273,39 +1349,50 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
     for (int i = tid; i < (SPB - nb) * RV; i += kJoinThreads) ob[nb + i / RV][i % RV] = 0.f;
     cp_async_wait_all();
     __syncthreads();
-    pdl_trigger();
-    // out_b[e] = coef0 (W_up^V o~_b)[e] + coef1 mu^V[e] + coef2 v_cur,b[e], the sum of a row in two halves
-    float sum[SPB];
+    // out_b[e] = coef0 (W_up^V o~_b)[e] + coef1 mu^V[e] + coef2 v_cur,b[e], the sum of a row in four quarters
+    float sum[2][SPB];
 #pragma unroll
-    for (int i = 0; i < SPB; ++i) sum[i] = 0.f;
+    for (int i = 0; i < SPB; ++i) sum[0][i] = sum[1][i] = 0.f;
     const char *wrow = jw + e * J<RV>::WROW;
-#pragma unroll 2
-    for (int j = half * HALF; j < (half ? RV / 8 : HALF); ++j) {
-        const uint4 w4 = *reinterpret_cast<const uint4 *>(wrow + j * 16);
-        const float2 w0 = bf2_to_f2(w4.x), w1 = bf2_to_f2(w4.y), w2 = bf2_to_f2(w4.z), w3 = bf2_to_f2(w4.w);
+#pragma unroll 1
+    for (int j = part * QUARTER; j < min((part + 1) * QUARTER, RV / 8); ++j) {
+        const uint4 wa = *reinterpret_cast<const uint4 *>(wrow + j * 16), wb = *reinterpret_cast<const uint4 *>(wrow + 64 * J<RV>::WROW + j * 16);
+        const float2 a0 = bf2_to_f2(wa.x), a1 = bf2_to_f2(wa.y), a2 = bf2_to_f2(wa.z), a3 = bf2_to_f2(wa.w);
+        const float2 c0 = bf2_to_f2(wb.x), c1 = bf2_to_f2(wb.y), c2 = bf2_to_f2(wb.z), c3 = bf2_to_f2(wb.w);
 #pragma unroll
         for (int i = 0; i < SPB; ++i) {
             const float4 o0 = *reinterpret_cast<const float4 *>(&ob[i][j * 8]);
             const float4 o1 = *reinterpret_cast<const float4 *>(&ob[i][j * 8 + 4]);
-            float s = sum[i];
-            s = fmaf(w0.x, o0.x, s); s = fmaf(w0.y, o0.y, s); s = fmaf(w1.x, o0.z, s); s = fmaf(w1.y, o0.w, s);
-            s = fmaf(w2.x, o1.x, s); s = fmaf(w2.y, o1.y, s); s = fmaf(w3.x, o1.z, s); s = fmaf(w3.y, o1.w, s);
-            sum[i] = s;
+            sum[0][i] = fmaf(a3.y, o1.w, fmaf(a3.x, o1.z, fmaf(a2.y, o1.y, fmaf(a2.x, o1.x, fmaf(a1.y, o0.w, fmaf(a1.x, o0.z, fmaf(a0.y, o0.y, fmaf(a0.x, o0.x, sum[0][i]))))))));
+            sum[1][i] = fmaf(c3.y, o1.w, fmaf(c3.x, o1.z, fmaf(c2.y, o1.y, fmaf(c2.x, o1.x, fmaf(c1.y, o0.w, fmaf(c1.x, o0.z, fmaf(c0.y, o0.y, fmaf(c0.x, o0.x, sum[1][i]))))))));
         }
     }
-    if (half == 1) {
-#pragma unroll
-        for (int i = 0; i < SPB; ++i) halves[i][e] = sum[i];
-    }
-    __syncthreads();
-    if (half == 0) {
+    if (part > 0) {
 #pragma unroll
         for (int i = 0; i < SPB; ++i) {
-            if (i >= nb) break;
-            float v = (sum[i] + halves[i][e]) * coef[i][0] + coef[i][1] * muv;
-            if (a.cur_v) v = fmaf(coef[i][2], load_elem(a.cur_v, iorow(b0 + i) * kD + e, a.io_bf16), v);
-            store_elem(a.out, iorow(b0 + i) * kD + e, v, a.io_bf16);
+            quarters[part - 1][i][e] = sum[0][i];
+            quarters[part - 1][i][64 + e] = sum[1][i];
         }
+    }
+    __syncthreads();
+    if (part == 0 && dry == 0) {
+#pragma unroll
+        for (int i = 0; i < SPB; ++i) {
+            quarters[0][i][e] = (sum[0][i] + quarters[0][i][e]) + (quarters[1][i][e] + quarters[2][i][e]);
+            quarters[0][i][64 + e] = (sum[1][i] + quarters[0][i][64 + e]) + (quarters[1][i][64 + e] + quarters[2][i][64 + e]);
+        }
+    }
+    __syncthreads();
+    if (dry == 0) {
+        for (int o = tid; o < nb * kD; o += kJoinThreads) {
+            const int i = o / kD, r = o % kD;
+            const int64_t at = iorow(b0 + i) * kD + r;
+            float v = quarters[0][i][r] * coef[i][0];
+            if (a.mu_v) v = fmaf(coef[i][1], a.mu_v[th * kD + r], v);
+            if (a.cur_v) v = fmaf(coef[i][2], load_elem(a.cur_v, at, a.io_bf16), v);
+            store_elem(a.out, at, v, a.io_bf16);
+        }
+    }
     }
 }
 
@@ -1382,8 +1469,9 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     }
     if ((st = launch_ex(absorb_kernel<RK, DR>, dim3(a.H, (ZZ::RKX + 31) / 32 + (DR > 0) + 1, (a.B + 15) / 16), 256, 0, stream, ap)) != LLA_OK)
         return st;
-    if ((st = launch_ex(trunk_kernel<RK, RV, DR>, dim3(grid), kTrunkThreads, ZZ::SMEM, stream, tv, tp)) != LLA_OK) return st;
-    if ((st = launch_ex(leaf_kernel<RK, RV, DR>, dim3(grid), LL::WARPS * 32, LL::SMEM, stream, tp)) != LLA_OK) return st;
+    const bool alone = a.B <= kLeaf;  // no group can have more members
+    if (!alone && (st = launch_ex(trunk_kernel<RK, RV, DR>, dim3(grid), kTrunkThreads, ZZ::SMEM, stream, tv, tp)) != LLA_OK) return st;
+    if ((st = launch_ex(leaf_kernel<RK, RV, DR>, dim3(grid), LL::WARPS * 32, LL::SMEM, stream, tp, static_cast<int>(alone))) != LLA_OK) return st;
 
     JoinParams jp = {};
     jp.t = tp;
