@@ -353,11 +353,12 @@ struct Z {
     static constexpr uint32_t TM_COLS = 512;
     static constexpr int QB = QT < 3 ? kRows * RKT * 2 : 0;  // the third part as an operand in shared memory
     static constexpr int QROW = 3 * RKT * 2;                // bytes of a query's parts
-    static constexpr int XCOLS = RVX / 2, XROW = XCOLS + 4;  // columns of O exchanged at once, floats of their row
+    // O on its way to the records: all of its columns at once, or half of them where the rotary plane needs the room
+    static constexpr int XCOLS = DR > 0 ? RVX / 2 : RVX, XROW = XCOLS + 4;  // columns, floats of a row
     static constexpr int NBAR = 40;
-    static constexpr int EXCH = 96 * XROW * 4;
-    // running maxima; maxima and sums of two runs and groups; a page's maxima of either group
-    static constexpr int RED = (kRows + 2 * 2 * 64 * 2 + 2 * 64) * 4;
+    static constexpr int EXCH = kRows * XROW * 4;
+    // running maxima; maxima and sums of three runs and two groups; a page's maxima of either group
+    static constexpr int RED = (kRows + 3 * 2 * 64 * 2 + 2 * 64) * 4;
     static constexpr int FIXED = QB + EXCH + RED + NBAR * 8 + kMaxNodes * 2;
     static constexpr int ST0 = (kSmemCap - 2048 - FIXED) / (KPAGE + VPAGE);
     static constexpr int ST = ST0 > 5 ? 5 : ST0;
@@ -653,9 +654,9 @@ __device__ __forceinline__ void softmax_run(const SoftmaxCtx &x, int run, int it
         tc_fence_before();
         mbar_arrive(&x.bar[bPfull + g]);
     }
-    // this group's maxima and sums of the run, once the run before the last has been read from there
+    // this group's maxima and sums of the run.  Three slots: when O of run - 2 is free the states of run - 3 have been read.
     if (run >= 2) mbar_wait(&x.bar[bOfree + (run & 1)], ((run - 2) >> 1) & 1, x.abort_flag, x.err);
-    if (!second) x.states[((run & 1) * 2 + g) * 64 + slice * R + q] = make_float2(m, l);
+    if (!second) x.states[((run % 3) * 2 + g) * 64 + slice * R + q] = make_float2(m, l);
     mbar_arrive(&x.bar[bMfull + (run & 1)]);
 }
 
@@ -669,11 +670,16 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
     volatile int *abort_flag = reinterpret_cast<volatile int *>(bar + bAbort);
     uint32_t *tslot = reinterpret_cast<uint32_t *>(bar + bTslot);
     float *running = reinterpret_cast<float *>(sm + ZZ::oRed);          // [128] maxima
-    float2 *states = reinterpret_cast<float2 *>(running + kRows);       // [2 runs][2 groups][64] maxima and sums
-    float *page_max = reinterpret_cast<float *>(states + 2 * 2 * 64);    // [2 groups][64]
+    float2 *states = reinterpret_cast<float2 *>(running + kRows);       // [3 runs][2 groups][64] maxima and sums
+    float *page_max = reinterpret_cast<float *>(states + 3 * 2 * 64);    // [2 groups][64]
     uint16_t *list = reinterpret_cast<uint16_t *>(sm + ZZ::oList);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
+    const int groups = count_groups(p);
+    if (groups == 0) {  // nothing is shared
+        pdl_wait();
+        return;
+    }
     if (tid == 0) {
         for (int s = 0; s < ZZ::ST; ++s) {
             mbar_init(&bar[bKfull + s], 1);
@@ -706,7 +712,6 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
     __syncthreads();
     tc_fence_after();
     constexpr uint32_t tmem = 0;  // the whole of TMEM is allocated (one CTA per SM)
-    const int groups = count_groups(p);
     const Share sh = find_share<false, kTrunkThreads>(p, groups, list, blockIdx.x, 1, gridDim.x);
     // q~ and beta come from the absorb kernel, and the workspace is free once it has waited for the kernel before it; the
     // producers read only inputs of the call, which that kernel's wait ordered before this launch, and wait at their end
@@ -837,117 +842,104 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
         constexpr int RS = record_floats(RV);
         const int quarter = warp & 3, row = 32 * quarter + lane;
         const uint32_t tl = tmem + (static_cast<uint32_t>(32 * quarter) << 16);
-        // the parts of a run's queries into TMEM: row by row, words of two columns
-        constexpr int kAtOnce = ZZ::RKT % 96 == 0 ? 6 : ZZ::RKT % 80 == 0 ? 5 : 4;  // pairs of 16-byte words
-        static_assert(ZZ::RKT % (16 * kAtOnce) == 0, "words of two");
-        auto load_queries = [&](const TrunkRun &r) {
-            {
-                const char *src = query_parts<ZZ::QROW>(p, r, row & (replica_rows(r.d.n) - 1));
-#pragma unroll 1
-                for (int part = 0; part < 3; ++part)
-#pragma unroll 1
-                    for (int c0 = 0; c0 < ZZ::RKT / 8; c0 += 2 * kAtOnce) {
-                        uint4 v[2 * kAtOnce];
+        // the parts of a run's queries into TMEM, row by row, a fetch ahead of what is stored
+        constexpr int WORDS = ZZ::RKT / 8, AT_ONCE = WORDS <= 12 ? WORDS : WORDS / 2, CHUNKS = 3 * WORDS / AT_ONCE;  // of 16 bytes
+        static_assert(AT_ONCE % 2 == 0 && AT_ONCE <= 12, "words of two");
+        uint4 v[2][AT_ONCE];
+        const char *src = nullptr;
+        auto fetch = [&](int c) {
 #pragma unroll
-                        for (int c = 0; c < 2 * kAtOnce; ++c)
-                            v[c] = src ? *reinterpret_cast<const uint4 *>(src + (part * (ZZ::RKT / 8) + c0 + c) * 16) : make_uint4(0, 0, 0, 0);
-                        if (part < ZZ::QT) {
+            for (int i = 0; i < AT_ONCE; ++i)
+                v[c & 1][i] = src ? *reinterpret_cast<const uint4 *>(src + (c * AT_ONCE + i) * 16) : make_uint4(0, 0, 0, 0);
+        };
+        // the first words of a run's queries, before their place is free
+        auto fetch_queries = [&](const TrunkRun &r) {
+            src = query_parts<ZZ::QROW>(p, r, row & (replica_rows(r.d.n) - 1));
+            fetch(0);
+        };
+        auto store_queries = [&] {
 #pragma unroll
-                            for (int c = 0; c < 2 * kAtOnce; c += 2) {
-                                const uint32_t u[8] = {v[c].x, v[c].y, v[c].z, v[c].w, v[c + 1].x, v[c + 1].y, v[c + 1].z, v[c + 1].w};
-                                tmem_st8u(tl + ZZ::TM_Q + part * ZZ::PART + (c0 + c) * 4, u);
-                            }
-                        } else {
+            for (int c = 0; c < CHUNKS; ++c) {
+                if (c + 1 < CHUNKS) fetch(c + 1);
+                const int part = c * AT_ONCE / WORDS, w0 = c * AT_ONCE - part * WORDS;
+                if (part < ZZ::QT) {
 #pragma unroll
-                            for (int c = 0; c < 2 * kAtOnce; ++c)
-                                *reinterpret_cast<uint4 *>(sm + ZZ::oQ + (c0 + c) * (kRows * 16) + row * 16) = v[c];
-                        }
+                    for (int i = 0; i < AT_ONCE; i += 2) {
+                        const uint4 a = v[c & 1][i], b = v[c & 1][i + 1];
+                        const uint32_t u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                        tmem_st8u(tl + ZZ::TM_Q + part * ZZ::PART + (w0 + i) * 4, u);
                     }
-                if (ZZ::QT < 3) fence_proxy_async_smem();
-                tmem_wait_st();
+                } else {
+#pragma unroll
+                    for (int i = 0; i < AT_ONCE; ++i) *reinterpret_cast<uint4 *>(sm + ZZ::oQ + (w0 + i) * (kRows * 16) + row * 16) = v[c & 1][i];
+                }
             }
+            if (ZZ::QT < 3) fence_proxy_async_smem();
+            tmem_wait_st();
             tc_fence_before();
             mbar_arrive(&bar[bQfull]);
         };
         RunWalk ahead(p, groups, sh, list);
-        if (ahead.next()) load_queries(ahead.r);
+        if (ahead.next()) {
+            fetch_queries(ahead.r);
+            store_queries();
+        }
         for (int run = 0; w.next(); ++run) {
             if (ahead.next()) {  // the next run's q~, as soon as S of this one's pages is done
+                fetch_queries(ahead.r);
                 mbar_wait(&bar[bQfree], run & 1, abort_flag, p.err);
                 tc_fence_after();
-                load_queries(ahead.r);
+                store_queries();
             }
             mbar_wait(&bar[bOdone], run & 1, abort_flag, p.err);
             mbar_wait(&bar[bMfull + (run & 1)], (run >> 1) & 1, abort_flag, p.err);
             tc_fence_after();
-            // the rows of a query: those of 16 queries first within their warp, then the warps' through shared memory
-            const int n = w.r.d.n, R = replica_rows(n), q = row & (R - 1);
-            const bool sums = R == 64 ? quarter < 2 : quarter == 0, mine = sums && (R > 16 || lane < 16) && q < n;
-            float *dst = p.part + (record_of(p, w.r.d, w.r.h, blockIdx.x) + q) * RS;
+            // every row of O into shared memory, which frees it, and from there the sums of the queries' rows
+            const int n = w.r.d.n, R = replica_rows(n);
+            float *rec = p.part + record_of(p, w.r.d, w.r.h, blockIdx.x) * RS;
             float *exch = reinterpret_cast<float *>(sm + ZZ::oExch);
-            float *xr = exch + (R == 64 ? row - 64 : (quarter - 1) * R + q) * ZZ::XROW;  // of a warp that does not sum
 #pragma unroll 1
             for (int c0 = 0; c0 < ZZ::RVX; c0 += ZZ::XCOLS) {
                 if (c0 > 0) named_bar_sync(9, 128);
-                if (!sums) {
 #pragma unroll 1
-                    for (int c = 0; c < ZZ::XCOLS; c += 16) {
-                        float o[16];
-                        tmem_ld16(tl + ZZ::TM_O + c0 + c, o);
-                        if (R == 16) {
+                for (int c = 0; c < ZZ::XCOLS; c += 16) {
+                    float o[16];
+                    tmem_ld16(tl + ZZ::TM_O + c0 + c, o);
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] += __shfl_xor_sync(0xffffffffu, o[e], 16);
-                        }
-                        if (R > 16 || lane < 16) {
-#pragma unroll
-                            for (int e = 0; e < 16; e += 4) *reinterpret_cast<float4 *>(xr + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-                        }
-                    }
+                    for (int e = 0; e < 16; e += 4)
+                        *reinterpret_cast<float4 *>(exch + row * ZZ::XROW + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                }
+                if (c0 + ZZ::XCOLS >= ZZ::RVX) {
+                    tc_fence_before();
+                    mbar_arrive(&bar[bOfree + (run & 1)]);
                 }
                 named_bar_sync(9, 128);
-                if (sums) {
-#pragma unroll 1
-                    for (int c = 0; c < ZZ::XCOLS; c += 16) {
-                        float o[16];
-                        tmem_ld16(tl + ZZ::TM_O + c0 + c, o);
-                        if (R == 16) {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) o[e] += __shfl_xor_sync(0xffffffffu, o[e], 16);
-                        }
-                        if (mine) {
-                            const float *xo = exch + q * ZZ::XROW + c;
-#pragma unroll 1
-                            for (int i = 0; i < (R == 64 ? 1 : 3); ++i, xo += R * ZZ::XROW) {
-#pragma unroll
-                                for (int e = 0; e < 16; e += 4) {
-                                    const float4 v = *reinterpret_cast<const float4 *>(xo + e);
-                                    o[e] += v.x;
-                                    o[e + 1] += v.y;
-                                    o[e + 2] += v.z;
-                                    o[e + 3] += v.w;
-                                }
-                            }
-#pragma unroll
-                            for (int e = 0; e < 16; e += 4)
-                                if (c0 + c + e < RV) *reinterpret_cast<float4 *>(dst + c0 + c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-                        }
+                const int words = min(ZZ::XCOLS, RV - c0) / 4;
+#pragma unroll 2
+                for (int i = row; i < n * words; i += 128) {
+                    const int q = i / words, c = 4 * (i - q * words);
+                    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int k = q; k < kRows; k += R) {
+                        const float4 b = *reinterpret_cast<const float4 *>(exch + k * ZZ::XROW + c);
+                        a = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
                     }
+                    *reinterpret_cast<float4 *>(rec + static_cast<int64_t>(q) * RS + c0 + c) = a;
                 }
             }
-            if (mine) {
+            if (row < n) {
                 // (a group's slices have one maximum)
-                const float2 *st = states + (run & 1) * 2 * 64;
+                const int q = row;
+                const float2 *st = states + (run % 3) * 2 * 64;
                 const float m0 = st[q].x, m1 = st[64 + q].x, mf = fmaxf(m0, m1);
                 float l0 = 0.f, l1 = 0.f;
                 for (int i = q; i < 64; i += R) {
                     l0 += st[i].y;
                     l1 += st[64 + i].y;
                 }
-                dst[RV] = mf;
-                dst[RV + 1] = (m0 == mf ? l0 : l0 * ex2_approx(m0 - mf)) + (m1 == mf ? l1 : l1 * ex2_approx(m1 - mf));
+                rec[q * RS + RV] = mf;
+                rec[q * RS + RV + 1] = (m0 == mf ? l0 : l0 * ex2_approx(m0 - mf)) + (m1 == mf ? l1 : l1 * ex2_approx(m1 - mf));
             }
-            tc_fence_before();
-            mbar_arrive(&bar[bOfree + (run & 1)]);
+            named_bar_sync(9, 128);  // the shared memory is free
         }
     }
     tc_fence_before();
@@ -1203,15 +1195,14 @@ __global__ void __launch_bounds__(L<RK, RV, DR>::WARPS * 32, 1) leaf_kernel(cons
 
 // Grid (H, ceil(B / spb)), 256 threads; SPB: the sequences that the projection is unrolled for.  W_up,t^V of the head waits in
 // shared memory, and what a sequence's nodes are in registers, when the records are there.
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 256, kJoinCtas = 4;  // of an SM
 template <int RV>
 struct J {
     static constexpr int WROW = RV * 2 + 16;  // bytes of a row of W_up^V, padded: rows 16 bytes apart in the banks
-    // (two CTAs an SM: a third waits for an SM that the leaf kernel has not left yet)
-    static constexpr int SMEM = kD * WROW > 84 * 1024 ? kD * WROW : 84 * 1024;
+    static constexpr int SMEM = kD * WROW;
 };
 template <int RV, int SPB>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ JoinParams a) {
+__global__ void __launch_bounds__(kJoinThreads, kJoinCtas) join_kernel(const __grid_constant__ JoinParams a) {
     constexpr int RS = record_floats(RV), NJ = (RV + 31) / 32, QUARTER = (RV / 8 + 3) / 4;  // 16-byte words of a quarter row
     extern __shared__ __align__(16) char jw[];
     __shared__ __align__(16) float ob[SPB][RV];
@@ -1480,9 +1471,9 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     jp.w_up_v = a.w_up_v; jp.mu_v = a.mu_v;
     jp.q = a.q; jp.q_rope = q_rope; jp.cur_k = a.cur_k; jp.cur_v = a.cur_v; jp.cur_k_rope = cur_k_rope;
     jp.out = a.out;
-    // about two CTAs per SM: fewer sequences per CTA for small batches
+    // all of its CTAs at once on the SMs: fewer sequences per CTA for small batches
     const int64_t units = static_cast<int64_t>(a.B) * a.H;
-    jp.spb = static_cast<int>(std::min<int64_t>(kJoinSeqs, std::max<int64_t>(1, (units + 2 * grid - 1) / (2 * grid))));
+    jp.spb = static_cast<int>(std::min<int64_t>(kJoinSeqs, std::max<int64_t>(1, (units + kJoinCtas * grid - 1) / (kJoinCtas * grid))));
     const dim3 jg(a.H, (a.B + jp.spb - 1) / jp.spb);
     auto join = [&](auto spb) {
         constexpr int SPB = decltype(spb)::value;
