@@ -32,6 +32,7 @@ struct Names {
     PyObject *codec[6];
     PyObject *pool, *num_blocks, *block_table, *max_blocks;
     PyObject *ref_count, *context_lens, *address, *count, *blocks, *device;
+    PyObject *base, *pairing, *pairs, *order, *prefix[5];
 } names;
 
 struct Unusual {};  // thrown to leave for the Python path
@@ -374,6 +375,166 @@ PoolArray pools(PyObject *o, const lla_pages &p) {  // lla.Pools, whose array li
     return a;
 }
 
+lla_rope_axes rope_axes(PyObject *o) {
+    const Ref base(PyObject_GetAttr(o, names.base)), pairs(PyObject_GetAttr(o, names.pairs));
+    lla_rope_axes r;
+    r.base = real(base.o);
+    r.pairing = static_cast<lla_rope_pairing>(attr32(o, names.pairing));
+    r.order = static_cast<lla_axes_order>(attr32(o, names.order));
+    if (!PyTuple_CheckExact(pairs.o) || PyTuple_GET_SIZE(pairs.o) != LLA_ROPE_AXES) throw Unusual();
+    for (int i = 0; i < LLA_ROPE_AXES; ++i) r.pairs[i] = integer32(PyTuple_GET_ITEM(pairs.o, i));
+    return r;
+}
+lla_prefix prefix(PyObject *o, int64_t B) {
+    const int64_t rows = LLA_PREFIX_LEVELS * (B / 2 > 1 ? B / 2 : 1);
+    const Ref a(PyObject_GetAttr(o, names.prefix[0])), b(PyObject_GetAttr(o, names.prefix[1])), c(PyObject_GetAttr(o, names.prefix[2])),
+        d(PyObject_GetAttr(o, names.prefix[3])), e(PyObject_GetAttr(o, names.prefix[4]));
+    return lla_prefix{typed_ptr<int32_t>(a.o, at::kInt, 1), typed_ptr<int32_t>(b.o, at::kInt, rows, 4),
+                      typed_ptr<int32_t>(c.o, at::kInt, LLA_PREFIX_LEVELS * B), typed_ptr<int32_t>(d.o, at::kInt, LLA_PREFIX_LEVELS, B),
+                      typed_ptr<int32_t>(e.o, at::kInt, B)};
+}
+// A cache whose block table has rows for B sequences.
+lla_cache cache_of(PyObject *o, int64_t B) {
+    const Ref bt(PyObject_GetAttr(o, names.block_table));
+    const at::Tensor &t = typed(bt.o, at::kInt);
+    const lla_cache c = cache(o);
+    if (t.dim() != 2 || t.size(0) < B || t.size(1) != c.max_blocks_per_seq) throw Unusual();
+    return c;
+}
+// Data of type `type`, n0 x n1 [x n2] values on the current device, or None.
+void *values(PyObject *o, at::ScalarType type, int64_t n0, int64_t n1, int64_t n2 = -1) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = typed(o, type);
+    if (t.dim() != (n2 < 0 ? 2 : 3) || t.size(0) != n0 || t.size(1) != n1 || (n2 >= 0 && t.size(2) != n2)) throw Unusual();
+    return t.data_ptr();
+}
+
+PyObject *encode_rope_keys_axes(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 8, [&] {
+        const int32_t dr = integer32(a[0]);
+        const lla_rope_axes rp = rope_axes(a[1]);
+        void *pool = address(a[2]);
+        const int64_t nb = integer(a[3]);
+        const at::Tensor &k = tensor(a[4]);
+        if (k.dim() != 2 || k.size(1) != dr) throw Unusual();
+        const int32_t N = size32(k.size(0));
+        const lla_dtype xd = dtype(k);
+        void *kp = k.data_ptr();
+        const auto *pos = typed_ptr<int32_t>(a[5], at::kInt, LLA_ROPE_AXES, N);
+        const auto *slots = typed_ptr<int64_t>(a[6], at::kLong, N);
+        void *st = stream_of(a[7]);
+        NoGil nogil;
+        return lla_encode_rope_keys_axes(dr, &rp, pool, nb, kp, xd, pos, slots, N, st);
+    });
+}
+
+PyObject *decode_attn_decoupled_axes(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 18, [&] {
+        const lla_geometry g = geometry(a[0]);
+        const lla_codec cd = codec(a[1]);
+        const lla_cache ch = cache(a[2]);
+        void *pool = address(a[3]);
+        const int32_t dr = integer32(a[4]);
+        const lla_rope_axes rp = rope_axes(a[5]);
+        const at::Tensor &q = tensor(a[10]), &ws = tensor(a[16]);
+        if (q.dim() < 1) throw Unusual();
+        const int32_t B = size32(q.size(0));
+        const auto *pos = typed_ptr<int32_t>(a[6], at::kInt, LLA_ROPE_AXES, B), *ctx = static_cast<const int32_t *>(address(a[7]));
+        const int32_t max_ctx = integer32(a[8]), loop = integer32(a[9]);
+        void *qr = address(a[11]), *ck = address(a[12]), *cv = address(a[13]), *ckr = address(a[14]), *out = address(a[15]);
+        void *w = ws.data_ptr(), *qp = q.data_ptr();
+        const lla_dtype io = dtype(q);
+        const size_t wb = nbytes(ws);
+        void *st = stream_of(a[17]);
+        NoGil nogil;
+        return lla_decode_attn_decoupled_axes(&g, &cd, &ch, pool, dr, &rp, pos, ctx, B, max_ctx, loop, qp, qr, ck, cv, ckr, io, out, w, wb,
+                                              st);
+    });
+}
+
+PyObject *prefix_plan(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 6, [&] {
+        const at::Tensor &lens = typed(a[1], at::kInt);
+        if (lens.dim() != 1) throw Unusual();
+        const int32_t B = size32(lens.size(0));
+        const lla_cache ch = cache_of(a[0], B);
+        const int32_t max_ctx = integer32(a[2]), min_pages = integer32(a[4]);
+        const lla_prefix pl = prefix(a[3], B);
+        const auto *lp = static_cast<const int32_t *>(lens.data_ptr());
+        void *st = stream_of(a[5]);
+        NoGil nogil;
+        return lla_prefix_plan(&ch, lp, B, max_ctx, min_pages, &pl, st);
+    });
+}
+
+PyObject *decode_attn_prefix(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 13, [&] {
+        const lla_geometry g = geometry(a[0]);
+        const lla_codec cd = codec(a[1]);
+        const at::Tensor &q = typed(a[7], tensor(a[7]).scalar_type()), &ws = scratch(a[11]);
+        if (q.dim() != 3 || q.size(1) != g.H || q.size(2) != g.d) throw Unusual();
+        const int32_t B = size32(q.size(0));
+        const lla_cache ch = cache_of(a[2], B);
+        const lla_prefix pl = prefix(a[3], B);
+        const auto *ctx = typed_ptr<int32_t>(a[4], at::kInt, B);
+        const int32_t max_ctx = integer32(a[5]), loop = integer32(a[6]);
+        const at::ScalarType t = q.scalar_type();
+        void *ck = values(a[8], t, B, g.H, g.d), *cv = values(a[9], t, B, g.H, g.d), *out = values(a[10], t, B, g.H, g.d);
+        void *w = ws.data_ptr(), *qp = q.data_ptr();
+        const lla_dtype io = dtype(q);
+        const size_t wb = nbytes(ws);
+        void *st = stream_of(a[12]);
+        NoGil nogil;
+        return lla_decode_attn_prefix(&g, &cd, &ch, &pl, ctx, B, max_ctx, loop, qp, ck, cv, io, out, w, wb, st);
+    });
+}
+
+PyObject *decode_attn_prefix_decoupled(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 19, [&] {
+        const lla_geometry g = geometry(a[0]);
+        const lla_codec cd = codec(a[1]);
+        void *pool = address(a[4]);
+        const int32_t dr = integer32(a[5]);
+        const lla_rope_axes rp = rope_axes(a[6]);
+        const at::Tensor &q = typed(a[11], tensor(a[11]).scalar_type()), &ws = scratch(a[17]);
+        if (q.dim() != 3 || q.size(1) != g.H || q.size(2) != g.d) throw Unusual();
+        const int32_t B = size32(q.size(0));
+        const lla_cache ch = cache_of(a[2], B);
+        const lla_prefix pl = prefix(a[3], B);
+        const auto *pos = typed_ptr<int32_t>(a[7], at::kInt, LLA_ROPE_AXES, B), *ctx = typed_ptr<int32_t>(a[8], at::kInt, B);
+        const int32_t max_ctx = integer32(a[9]), loop = integer32(a[10]);
+        const at::ScalarType t = q.scalar_type();
+        void *qr = values(a[12], t, B, g.H, dr), *ck = values(a[13], t, B, g.H, g.d), *cv = values(a[14], t, B, g.H, g.d);
+        void *ckr = values(a[15], t, B, dr), *out = values(a[16], t, B, g.H, g.d);
+        void *w = ws.data_ptr(), *qp = q.data_ptr();
+        const lla_dtype io = dtype(q);
+        const size_t wb = nbytes(ws);
+        void *st = stream_of(a[18]);
+        NoGil nogil;
+        return lla_decode_attn_prefix_decoupled(&g, &cd, &ch, &pl, pool, dr, &rp, pos, ctx, B, max_ctx, loop, qp, qr, ck, cv, ckr, io, out, w,
+                                                wb, st);
+    });
+}
+
+PyObject *pages_admit(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return guarded(n, 12, [&] {
+        const lla_pages p = pages(a[0]);
+        const PoolArray ps = pools(a[1], p);
+        const at::Tensor &rows = typed(a[2], at::kInt), &slots = typed(a[6], at::kLong), &ws = scratch(a[9]);
+        const int32_t count = size32(rows.numel()), N = size32(slots.numel());
+        const auto *r = typed_ptr<int32_t>(a[2], at::kInt, count), *par = typed_ptr<int32_t>(a[3], at::kInt, count),
+                   *keep = typed_ptr<int32_t>(a[4], at::kInt, count), *fresh = typed_ptr<int32_t>(a[5], at::kInt, count);
+        auto *sp = static_cast<int64_t *>(slots.data_ptr());
+        auto *cu = typed_ptr<int32_t>(a[7], at::kInt, static_cast<int64_t>(count) + 1), *free_blocks = typed_ptr<int32_t>(a[10], at::kInt, 1);
+        auto *ok = typed_ptr<uint8_t>(a[8], at::kByte, count);
+        void *w = ws.data_ptr();
+        const size_t wb = nbytes(ws);
+        void *st = stream_of(a[11]);
+        NoGil nogil;
+        return lla_pages_admit(&p, ps.p, ps.L, r, par, keep, fresh, count, sp, N, cu, ok, free_blocks, w, wb, st);
+    });
+}
+
 PyObject *pages_fork(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return guarded(n, 4, [&] {
         const lla_pages from = pages(a[0]), to = pages(a[1]);
@@ -464,7 +625,9 @@ PyMethodDef methods[] = {
     LLA_METHOD(decode_attn), LLA_METHOD(decode_attn_2d), LLA_METHOD(decode_attn_loops), LLA_METHOD(decode_attn_rope),
     LLA_METHOD(decode_attn_decoupled), LLA_METHOD(encode), LLA_METHOD(encode_2d), LLA_METHOD(encode_layers),
     LLA_METHOD(prefill_attn), LLA_METHOD(prefill_attn_rope), LLA_METHOD(pages_fork), LLA_METHOD(pages_extend),
-    LLA_METHOD(pages_free), LLA_METHOD(pages_compact), LLA_METHOD(beam_select), {nullptr, nullptr, 0, nullptr}};
+    LLA_METHOD(pages_free), LLA_METHOD(pages_compact), LLA_METHOD(beam_select), LLA_METHOD(encode_rope_keys_axes),
+    LLA_METHOD(decode_attn_decoupled_axes), LLA_METHOD(prefix_plan), LLA_METHOD(decode_attn_prefix),
+    LLA_METHOD(decode_attn_prefix_decoupled), LLA_METHOD(pages_admit), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lla_native", "Native marshalling of the calls of lla.py.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
@@ -476,6 +639,8 @@ PyMODINIT_FUNC PyInit__lla_native() {
     names = Names{s("T"), s("H"), s("d"), s("r_k"), s("r_v"), s("storage"), s("scale"),
                   {s("w_down_k"), s("w_down_v"), s("w_up_k"), s("w_up_v"), s("mu_k"), s("mu_v")},
                   s("pool"), s("num_blocks"), s("block_table"), s("max_blocks_per_seq"),
-                  s("ref_count"), s("context_lens"), s("address"), s("count"), s("blocks"), s("device")};
+                  s("ref_count"), s("context_lens"), s("address"), s("count"), s("blocks"), s("device"),
+                  s("base"), s("pairing"), s("pairs"), s("order"),
+                  {s("num_groups"), s("groups"), s("members"), s("column"), s("own_page")}};
     return PyModule_Create(&module);
 }

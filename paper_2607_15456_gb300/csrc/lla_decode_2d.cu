@@ -1551,7 +1551,7 @@ lla_status launch_units(const DecodeArgs &a, bool loops, cudaStream_t stream) {
 // ------------------------------------------------------------------------- rotary keys
 
 struct RKParams {
-    int N, d_rope, pairing, x_bf16;
+    int N, d_rope, pairing;
     char *pool;
     int64_t num_blocks;
     const void *k;  // [N][d_rope]
@@ -1563,40 +1563,96 @@ struct RKParams {
     unsigned *err;
 };
 
-// One thread per (token, pair): k^R of token n turned at its position (pair j by
-// positions[axis(j)][n] theta_j), written as bf16 at row slot % 64 of block slot / 64 in the granule
-// layout of a K-plane (granule g of row i at g*1024 + i*16).
-__global__ void __launch_bounds__(256) rope_key_store_kernel(const RKParams p) {
-    const int hp = p.d_rope / 2;
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    pdl_wait();
-    if (i < static_cast<int64_t>(p.N) * hp) {
-        const int n = static_cast<int>(i / hp), j = static_cast<int>(i - static_cast<int64_t>(n) * hp);
-        const int64_t slot = p.slots[n];
-        const int pos = p.positions[static_cast<int64_t>(p.axis[j]) * p.N + n];
-        if (slot >= 0) {
-            const int64_t blk = slot / kPT;
-            const int row = static_cast<int>(slot - blk * kPT);
-            if (blk >= p.num_blocks) {
-                atomicOr(p.err, LLA_DEVERR_SLOT);
-            } else if (p.positions[n] < 0 || (p.axes == 3 && (p.positions[static_cast<int64_t>(p.N) + n] < 0 ||
-                                                              p.positions[2 * static_cast<int64_t>(p.N) + n] < 0))) {
-                atomicOr(p.err, LLA_DEVERR_CONTEXT);
-            } else {
-                float sn, cs;
-                turn_sincos(pos, p.phi[j], &sn, &cs);
-                const int a = p.pairing ? 2 * j : j, c = p.pairing ? 2 * j + 1 : j + hp;
-                const float x = load_elem(p.k, static_cast<int64_t>(n) * p.d_rope + a, p.x_bf16);
-                const float y = load_elem(p.k, static_cast<int64_t>(n) * p.d_rope + c, p.x_bf16);
-                char *plane = p.pool + blk * (static_cast<int64_t>(kPT) * p.d_rope * 2);
-                *reinterpret_cast<__nv_bfloat16 *>(plane + (a >> 3) * (kPT * 16) + row * 16 + (a & 7) * 2) =
-                    __float2bfloat16_rn(x * cs - y * sn);
-                *reinterpret_cast<__nv_bfloat16 *>(plane + (c >> 3) * (kPT * 16) + row * 16 + (c & 7) * 2) =
-                    __float2bfloat16_rn(x * sn + y * cs);
-            }
+// One thread per token and eight pairs: k^R of token n turned at its position (pair j by positions[axis(j)][n] theta_j),
+// written as bf16 at row slot % 64 of block slot / 64 in the granule layout of a K-plane (granule g of row i at
+// g*1024 + i*16): two granules of 16 bytes, and consecutive lanes are consecutive tokens, whose rows lie side by side.
+// The pairs of the two granules are (j, j + d_rope/2) with eight j of one granule each, or the 16 values of adjacent pairs.
+// Bound by HBM where there are many tokens: 32768 of 96 fp32 values 26 -> NEW us from a thread per pair that stored two bytes.
+template <bool BF16>
+__device__ __forceinline__ void load8(const void *base, int64_t i, float (&v)[8]) {
+    if constexpr (BF16) {
+        const uint16_t *src = static_cast<const uint16_t *>(base) + i;
+        if (reinterpret_cast<uintptr_t>(src) % 16 == 0) {
+            const uint4 u = *reinterpret_cast<const uint4 *>(src);
+            const float2 a = bf2_to_f2(u.x), b = bf2_to_f2(u.y), c = bf2_to_f2(u.z), d = bf2_to_f2(u.w);
+            v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y; v[4] = c.x; v[5] = c.y; v[6] = d.x; v[7] = d.y;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = bf_to_f(src[e]);
+        }
+    } else {
+        const float *src = static_cast<const float *>(base) + i;
+        if (reinterpret_cast<uintptr_t>(src) % 16 == 0) {
+            const float4 a = *reinterpret_cast<const float4 *>(src), b = *reinterpret_cast<const float4 *>(src + 4);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = src[e];
         }
     }
+}
+
+constexpr int kRKThreads = 128;
+template <bool BF16>
+__global__ void __launch_bounds__(kRKThreads) rope_key_store_kernel(const __grid_constant__ RKParams p) {
+    const int oct = blockIdx.y, hp = p.d_rope / 2;  // pairs 8 oct .. 8 oct + 7
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kRKThreads + threadIdx.x;
+    pdl_wait();
     pdl_trigger();
+    if (i >= p.N) return;
+    const int n = static_cast<int>(i);
+    const int64_t slot = p.slots[n];
+    int pos[3];
+    pos[0] = pos[1] = pos[2] = p.positions[n];
+    if (p.axes == 3) {
+        pos[1] = p.positions[static_cast<int64_t>(p.N) + n];
+        pos[2] = p.positions[2 * static_cast<int64_t>(p.N) + n];
+    }
+    float x[8], y[8];
+    const int64_t row0 = static_cast<int64_t>(n) * p.d_rope;
+    load8<BF16>(p.k, row0 + (p.pairing ? 16 * oct : 8 * oct), x);
+    load8<BF16>(p.k, row0 + (p.pairing ? 16 * oct + 8 : hp + 8 * oct), y);
+    if (slot < 0) return;
+    const int64_t blk = slot / kPT;
+    const int row = static_cast<int>(slot - blk * kPT);
+    if (blk >= p.num_blocks) {
+        atomicOr(p.err, LLA_DEVERR_SLOT);
+        return;
+    }
+    if (pos[0] < 0 || pos[1] < 0 || pos[2] < 0) {
+        atomicOr(p.err, LLA_DEVERR_CONTEXT);
+        return;
+    }
+    uint32_t u[4], w[4];
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        float sn[2], cs[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int j = 8 * oct + e + k, a = p.axis[j];
+            turn_sincos(a == 0 ? pos[0] : a == 1 ? pos[1] : pos[2], p.phi[j], &sn[k], &cs[k]);
+        }
+        if (p.pairing) {  // x then y are pairs (v[0], v[1]), (v[2], v[3]), ...
+            const float a0 = e < 4 ? x[(2 * e) & 7] : y[(2 * e) & 7], b0 = e < 4 ? x[(2 * e + 1) & 7] : y[(2 * e + 1) & 7];
+            const float a1 = e < 4 ? x[(2 * e + 2) & 7] : y[(2 * e + 2) & 7], b1 = e < 4 ? x[(2 * e + 3) & 7] : y[(2 * e + 3) & 7];
+            const uint32_t first = pack_bf16x2(a0 * cs[0] - b0 * sn[0], a0 * sn[0] + b0 * cs[0]);
+            const uint32_t next = pack_bf16x2(a1 * cs[1] - b1 * sn[1], a1 * sn[1] + b1 * cs[1]);
+            if (e < 4) {
+                u[e] = first;
+                u[e + 1] = next;
+            } else {
+                w[e - 4] = first;
+                w[e - 3] = next;
+            }
+        } else {
+            u[e / 2] = pack_bf16x2(x[e] * cs[0] - y[e] * sn[0], x[e + 1] * cs[1] - y[e + 1] * sn[1]);
+            w[e / 2] = pack_bf16x2(x[e] * sn[0] + y[e] * cs[0], x[e + 1] * sn[1] + y[e + 1] * cs[1]);
+        }
+    }
+    char *plane = p.pool + blk * (static_cast<int64_t>(kPT) * p.d_rope * 2) + row * 16;
+    const int g0 = p.pairing ? 2 * oct : oct, g1 = p.pairing ? 2 * oct + 1 : hp / 8 + oct;
+    *reinterpret_cast<uint4 *>(plane + g0 * (kPT * 16)) = make_uint4(u[0], u[1], u[2], u[3]);
+    *reinterpret_cast<uint4 *>(plane + g1 * (kPT * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 }  // namespace
@@ -1628,15 +1684,15 @@ lla_status launch_rope_key_store(int d_rope, const RotaryAxes &rope, void *rope_
     unsigned *err = device_error_word(&st);
     if (st != LLA_OK) return st;
     RKParams rp = {};
-    rp.N = N; rp.d_rope = d_rope; rp.pairing = rope.pairing; rp.x_bf16 = x_bf16;
+    rp.N = N; rp.d_rope = d_rope; rp.pairing = rope.pairing;
     rp.axes = rope.axes;
     for (int j = 0; j < d_rope / 2; ++j) rp.axis[j] = rope.axis[j];
     rp.pool = static_cast<char *>(rope_pool); rp.num_blocks = num_blocks;
     rp.k = k; rp.positions = positions; rp.slots = slots; rp.err = err;
     rotary_phases(d_rope, rope.base, rp.phi);
-    const int64_t total = static_cast<int64_t>(N) * (d_rope / 2);
-    if ((total + 255) / 256 > 0x7fffffff) return LLA_ERR_UNSUPPORTED;
-    return launch_ex(rope_key_store_kernel, dim3(static_cast<unsigned>((total + 255) / 256)), 256, 0, stream, rp);
+    const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(N) + kRKThreads - 1) / kRKThreads), d_rope / 16);
+    if (x_bf16) return launch_ex(rope_key_store_kernel<true>, grid, kRKThreads, 0, stream, rp);
+    return launch_ex(rope_key_store_kernel<false>, grid, kRKThreads, 0, stream, rp);
 }
 
 namespace {

@@ -641,6 +641,9 @@ def lla_encode_rope_keys_axes(d_rope: int, rope: RopeAxes, rope_pool: torch.Tens
                               k_rope: torch.Tensor, positions: torch.Tensor, slot_mapping: torch.Tensor,
                               stream=None) -> None:
     """Rotary keys k_rope [N][d_rope], turned at positions [3][N] int32, into the rotary planes."""
+    if _done("lla_encode_rope_keys_axes", _native().encode_rope_keys_axes(
+            d_rope, rope, rope_pool, num_blocks, k_rope, positions, slot_mapping, _handle(stream))):
+        return
     rp = rope.c()
     N = k_rope.shape[0] if k_rope.dim() == 2 else 0
     if k_rope.dim() == 2 and k_rope.shape[1] != d_rope:
@@ -658,6 +661,10 @@ def lla_decode_attn_decoupled_axes(geom: Geometry, codec: Codec, cache: Cache, r
                                    cur_v: Optional[torch.Tensor], cur_k_rope: Optional[torch.Tensor],
                                    out: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """lla_decode_attn_decoupled with the current tokens at positions [3][B] int32."""
+    if _done("lla_decode_attn_decoupled_axes", _native().decode_attn_decoupled_axes(
+            geom, codec, cache, rope_pool, d_rope, rope, positions, context_lens, max_ctx, loop, q, q_rope, cur_k, cur_v,
+            cur_k_rope, out, workspace, _handle(stream))):
+        return
     g, cd, ch, rp = geom.c(), codec.c(), cache.c(), rope.c()
     B = q.shape[0]
     _check("lla_decode_attn_decoupled_axes", library().lla_decode_attn_decoupled_axes(
@@ -864,6 +871,9 @@ def lla_pages_admit(pages: Pages, pools: Pools, rows: torch.Tensor, parents: tor
     """Request i becomes the empty sequence rows[i], of new_lens[i] tokens, the first keep[i] of them those of sequence
     parents[i] (-1: none): all [n] int32.  slot_mapping [N] int64, cu_new [n + 1] int32, admitted [n] uint8 and free_blocks
     [1] int32 are written."""
+    if _done("lla_pages_admit", _native().pages_admit(
+            pages, pools, rows, parents, keep, new_lens, slot_mapping, cu_new, admitted, workspace, free_blocks, _handle(stream))):
+        return
     p = pages.c()
     pools = pools if isinstance(pools, Pools) else Pools(pools)
     pools.check(pages)
@@ -912,6 +922,8 @@ def _table_rows(cache: Cache, B: int) -> None:
 def lla_prefix_plan(cache: Cache, context_lens: torch.Tensor, max_ctx: int, plan: Prefix, min_pages: int = 1,
                     stream=None) -> None:
     """Works out what the sequences of cache.block_table share (the pool is not read and may be None); writes `plan`."""
+    if _done("lla_prefix_plan", _native().prefix_plan(cache, context_lens, max_ctx, plan, min_pages, _handle(stream))):
+        return
     B = context_lens.numel()
     _table_rows(cache, B)
     ch, pl = cache.c(), plan.c(B)
@@ -944,6 +956,9 @@ def lla_decode_attn_prefix(geom: Geometry, codec: Codec, cache: Cache, plan: Pre
                            cur_v: Optional[torch.Tensor], out: torch.Tensor, workspace: torch.Tensor,
                            stream=None) -> None:
     """lla_decode_attn with the pages that `plan` (lla_prefix_plan) names read once for all sequences of a group."""
+    if _done("lla_decode_attn_prefix", _native().decode_attn_prefix(
+            geom, codec, cache, plan, context_lens, max_ctx, loop, q, cur_k, cur_v, out, workspace, _handle(stream))):
+        return
     _decode_prefix_check(geom, cache, context_lens, q, None, cur_k, cur_v, None, out, 0)
     B = q.shape[0]
     g, cd, ch, pl = geom.c(), codec.c(), cache.c(), plan.c(B)
@@ -959,6 +974,10 @@ def lla_decode_attn_prefix_decoupled(geom: Geometry, codec: Codec, cache: Cache,
                                      cur_v: Optional[torch.Tensor], cur_k_rope: Optional[torch.Tensor],
                                      out: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """The same with a rotary branch; positions [3][B] int32 of the current tokens, or None: their index on every axis."""
+    if _done("lla_decode_attn_prefix_decoupled", _native().decode_attn_prefix_decoupled(
+            geom, codec, cache, plan, rope_pool, d_rope, rope, positions, context_lens, max_ctx, loop, q, q_rope, cur_k, cur_v,
+            cur_k_rope, out, workspace, _handle(stream))):
+        return
     _decode_prefix_check(geom, cache, context_lens, q, q_rope, cur_k, cur_v, cur_k_rope, out, d_rope)
     B = q.shape[0]
     g, cd, ch, pl, rp = geom.c(), codec.c(), cache.c(), plan.c(B), rope.c()

@@ -191,3 +191,14 @@ def test_python_refuses_wrong_arrays(lla):
         lla.RopeAxes(1e4, 0, (16, 16)).c()
     with pytest.raises(ValueError, match="k_rope"):
         lla.lla_encode_rope_keys_axes(64, rope, w, 1, torch.zeros(2, 32), i(3, 2), torch.zeros(2, dtype=torch.int64))
+
+
+@pytest.mark.parametrize("name, count", [("encode_rope_keys_axes", 8), ("decode_attn_decoupled_axes", 18), ("prefix_plan", 6),
+                                         ("decode_attn_prefix", 13), ("decode_attn_prefix_decoupled", 19), ("pages_admit", 12)])
+def test_unusual_arguments_are_left_to_python(lla, name, count):
+    native = getattr(lla._native(), name)
+    t = torch.zeros(2, 2, dtype=torch.int32)
+    for x in (t, FAKE, "x", None, lla.Pages(t[0], t, t[0]), lla.RopeAxes(1e4, 0, (1, 2)), lla.Prefix.empty(2, "cpu")):
+        assert native(*[x] * count) is None
+    with pytest.raises(TypeError):
+        native(None)
