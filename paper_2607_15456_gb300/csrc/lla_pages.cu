@@ -648,7 +648,10 @@ __global__ void __launch_bounds__(kPlanThreads, 1) admit_plan_kernel(const Admit
     const ClusterSums free = cluster_sums(total.b, totals);
     const bool ok = valid && before + need <= static_cast<unsigned long long>(free.all) &&
                     at_token.a + tokens <= static_cast<unsigned long long>(a.N);
-    if (ok) {
+    // the sums grow with the request: a warp's largest are those of its last admitted one (an atomic of every thread on one
+    // word took 5 us)
+    const unsigned admitted = __ballot_sync(0xffffffffu, ok);
+    if (admitted && tid % 32 == 31 - __clz(admitted)) {
         atomicMax(&most_blocks, at.a + (need | static_cast<unsigned long long>(copy) << 40));
         atomicMax(&most_tokens, at_token.a + tokens);
     }

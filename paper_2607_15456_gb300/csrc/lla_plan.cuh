@@ -46,6 +46,18 @@ __device__ __forceinline__ Two block_scan(Two v, Two *part, Two &total) {
     return Two{part[warp].a + inc.a - v.a, part[warp].b + inc.b - v.b};
 }
 
+// Clusters of more than 8 CTAs are an opt-in of the kernel, once per device.
+template <typename K>
+lla_status allow_clusters_of_16(K kern, DeviceOnce &once) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return LLA_ERR_CUDA;
+    const bool cached = dev >= 0 && dev < 64;
+    if (cached && once.done[dev].load(std::memory_order_acquire)) return LLA_OK;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return LLA_ERR_CUDA;
+    if (cached) once.done[dev].store(true, std::memory_order_release);
+    return LLA_OK;
+}
+
 // A cluster of `ctas` CTAs of kPlanThreads.
 template <typename A>
 lla_status launch_plan(void (*kern)(A), int ctas, const A &a, cudaStream_t stream, int smem = 0) {

@@ -42,21 +42,21 @@ struct PrefixShared {
     Two part[33];
 };
 
-constexpr int kScan = 8;  // table entries of a lane in flight, of either row
-
-// The first page of [from, limit) where two rows differ, or limit: by a warp.
+// The first page of [from, limit) where two rows differ, or limit: by a warp, with LOADS loads of either row in flight in a
+// lane.  (Four int4 where both rows start on 16 bytes took as long; twelve entries 4 us more for 1024 long rows.)
+constexpr int kLoads = 8;
 __device__ __forceinline__ int first_difference(const int32_t *a, const int32_t *b, int from, int limit) {
     const int lane = threadIdx.x & 31;
-    for (int p = from; p < limit; p += 32 * kScan) {
-        int va[kScan], vb[kScan];
+    for (int p = from; p < limit; p += 32 * kLoads) {
+        int va[kLoads], vb[kLoads];
 #pragma unroll
-        for (int j = 0; j < kScan; ++j) {
+        for (int j = 0; j < kLoads; ++j) {
             const int i = p + 32 * j + lane;
             va[j] = i < limit ? a[i] : 0;
             vb[j] = i < limit ? b[i] : 0;
         }
 #pragma unroll
-        for (int j = 0; j < kScan; ++j) {
+        for (int j = 0; j < kLoads; ++j) {
             const unsigned m = __ballot_sync(0xffffffffu, va[j] != vb[j]);
             if (m) return p + 32 * j + __ffs(m) - 1;
         }
@@ -86,6 +86,11 @@ __global__ void __launch_bounds__(kPlanThreads, 1) prefix_plan_kernel(const Pref
         } else {
             full = len / kBlockTokens;
         }
+    }
+    // the rows on their way to L2 while the first blocks are sorted (each CTA fetches its part of them)
+    if (full > 1) {
+        const char *row = reinterpret_cast<const char *>(a.table + static_cast<int64_t>(tid) * a.max_blocks);
+        for (int i = rank * 128; i < full * 4; i += ctas * 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + i));
     }
     sh.full[tid] = full;
 #pragma unroll
@@ -118,9 +123,13 @@ __global__ void __launch_bounds__(kPlanThreads, 1) prefix_plan_kernel(const Pref
             }
         }
         __syncthreads();
+        // The sequences of a warp with one key send their lowest, for all of them: a thousand atomics on one word took longer than
+        // the rest of a level.
         int slot = 0;
-        if (alive) {
-            const unsigned long long key = static_cast<unsigned long long>(lead) << 32 | static_cast<unsigned>(block);
+        const unsigned long long key = alive ? static_cast<unsigned long long>(lead) << 32 | static_cast<unsigned>(block) : kNoKey;
+        const unsigned same = __match_any_sync(0xffffffffu, key);
+        const int sender = __ffs(same) - 1;
+        if (alive && tid % 32 == sender) {
             slot = (static_cast<unsigned>(block) * 2654435769u + static_cast<unsigned>(lead) * 40503u) >> 21;  // golden-ratio hashing
             for (;;) {
                 const unsigned long long was = atomicCAS(&sh.key[slot], kNoKey, key);
@@ -128,8 +137,9 @@ __global__ void __launch_bounds__(kPlanThreads, 1) prefix_plan_kernel(const Pref
                 slot = (slot + 1) % kSlots;
             }
             atomicMin(&sh.lowest[slot], tid);
-            atomicAdd(&sh.count[slot], 1);
+            atomicAdd(&sh.count[slot], __popc(same));
         }
+        slot = __shfl_sync(0xffffffffu, slot, sender);
         __syncthreads();
         const int n = alive ? sh.count[slot] : 0;
         const int lead_new = alive ? sh.lowest[slot] : tid;
@@ -216,11 +226,12 @@ lla_status launch_prefix_plan(const int32_t *block_table, int64_t num_blocks, in
     a.plan = plan;
     a.err = device_error_word(&st);
     if (!a.err) return st;
-    static DeviceOnce configured;
+    static DeviceOnce configured, configured_cluster;
     constexpr int smem = static_cast<int>(sizeof(PrefixShared));
     if ((st = raise_smem_limit(prefix_plan_kernel, smem, configured)) != LLA_OK) return st;
+    if ((st = allow_clusters_of_16(prefix_plan_kernel, configured_cluster)) != LLA_OK) return st;
     const int64_t entries = static_cast<int64_t>(B) * (max_ctx / kBlockTokens);
-    return launch_plan(prefix_plan_kernel, entries > 8192 ? 8 : 1, a, stream, smem);
+    return launch_plan(prefix_plan_kernel, entries > 32768 ? 16 : entries > 8192 ? 8 : 1, a, stream, smem);
 }
 
 }  // namespace lla
