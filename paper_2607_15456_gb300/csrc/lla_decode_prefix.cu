@@ -37,9 +37,9 @@
 //   join_kernel    per head and up to 8 sequences: joins the runs of each sequence's nodes and the current token, and applies
 //                  W_up,t^V once for all of them
 //
-// Storage bf16, d = 128; accumulators fp32 in TMEM.  Three parts of q~ hold the 24 bits of fp32.  Two parts of p are off by at
-// most 2^-18 of p (half a step of the second part), which a sum of many p averages below the rounding of its fp32 sums; the
-// sums l take p itself.
+// Storage bf16, d = 128; accumulators fp32 in TMEM.  Three parts of q~, and of p, hold the 24 bits of fp32.  For bf16 outputs p has
+// two: they are off by at most 2^-18 of p, half a step of the second part, and an output is rounded to 2^-9.  (With two for
+// fp32 outputs, too, a few tokens' outputs were off by 2e-6.)  The sums l take p itself.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -333,7 +333,8 @@ __global__ void __launch_bounds__(256) absorb_kernel(const __grid_constant__ Abs
 // ------------------------------------------------------------------------------------------ trunk kernel
 
 // Shared memory and TMEM of the trunk kernel.  Offsets from a 1024-byte aligned base (128-byte swizzle atoms of the V stages).
-template <int RK, int RV, int DR>
+// THIRD: p in three parts (24 bits, for fp32 outputs); the third in rows of an operand of its own.
+template <int RK, int RV, int DR, bool THIRD>
 struct Z {
     static constexpr int RKX = (RK + 15) / 16 * 16;   // content contraction, zero-padded
     static constexpr int RKT = RKX + DR;              // with the rotary one
@@ -345,11 +346,12 @@ struct Z {
     static constexpr int VPAGE = NBOX * BOX;
     // TMEM columns: the parts of q~ (the third in shared memory where it does not fit), O, S of either group, P of either
     // group (in the columns of its S where it does not fit: then S of its next page waits for O of this one)
-    static constexpr int PART = RKT / 2;
-    static constexpr int QT = 3 * PART + RVX + 4 * kPT / 2 + 2 * kPT / 2 <= 512 ? 3 : 2;
-    static constexpr bool ALIAS = QT * PART + RVX + 2 * kPT + kPT > 512;
+    static constexpr int PART = RKT / 2, PW = THIRD ? kPT : kPT / 2;  // columns of a part of q~, of a group's P
+    static constexpr int QT = 3 * PART + RVX + 2 * kPT + 2 * PW <= 512 ? 3 : 2;
+    static constexpr bool ALIAS = QT * PART + RVX + 2 * kPT + 2 * PW > 512;
     static constexpr uint32_t TM_Q = 0, TM_O = QT * PART, TM_S = TM_O + RVX, TM_P = ALIAS ? TM_S : TM_S + 2 * kPT;
-    static constexpr uint32_t P_STEP = ALIAS ? kPT : kPT / 2;  // from one group's P to the other's
+    static constexpr uint32_t P_STEP = ALIAS ? kPT : PW;  // from one group's P to the other's
+    static constexpr bool P3 = THIRD;
     static constexpr uint32_t TM_COLS = 512;
     static constexpr int QB = QT < 3 ? kRows * RKT * 2 : 0;  // the third part as an operand in shared memory
     static constexpr int QROW = 3 * RKT * 2;                // bytes of a query's parts
@@ -374,7 +376,7 @@ struct Z {
     static constexpr uint32_t IDESC_S = umma_idesc_bf16(kRows, kPT, 0, 0);
     static constexpr uint32_t IDESC_O = umma_idesc_bf16(kRows, RVX, 0, 1);
     static_assert(RKT % 16 == 0 && RV % 8 == 0 && RVX % 32 == 0, "ranks");
-    static_assert(TM_P + 2 * P_STEP <= TM_COLS && TM_S + 2 * kPT <= TM_COLS, "TMEM columns");
+    static_assert(TM_P + P_STEP + PW <= TM_COLS && TM_S + 2 * kPT <= TM_COLS, "TMEM columns");
     static_assert(ST >= 2 && SMEM + 1024 <= kSmemCap, "shared memory");
 };
 
@@ -516,7 +518,8 @@ __device__ __forceinline__ const char *query_parts(const TrunkParams &p, const T
 // A value that every lane has, for a warp that issues products (their descriptors are in uniform registers then).
 __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 
-// The 128 rows hold R queries 128 / R times: replica i = row / R has part i % 2 of their weights p for the tokens
+// The 128 rows hold R queries 128 / R times: replica i = row / R has part i % 2 of their weights p (in the operand behind it the
+// third part, where i is even) for the tokens
 // R (i / 2) to R (i / 2) + R - 1 of each page, and zeros for the others, so that a thread works on R tokens and the sum of a
 // query's rows of O is the sum over all tokens of both parts.  (With R = 64 for all, two of the four schedulers did the
 // work of up to 32 queries.)
@@ -628,6 +631,10 @@ __device__ __forceinline__ void softmax_run(const SoftmaxCtx &x, int run, int it
             for (int c = 0; c < 16; ++c) zero[c] = 0;
             tmem_st16u(tp, zero);
             tmem_st16u(tp + 16, zero);
+            if constexpr (ZZ::P3) {
+                tmem_st16u(tp + kPT / 2, zero);
+                tmem_st16u(tp + kPT / 2 + 16, zero);
+            }
             tmem_wait_st();
         }
         const float2 mm = make_float2(-m, -m);
@@ -643,13 +650,27 @@ __device__ __forceinline__ void softmax_run(const SoftmaxCtx &x, int run, int it
             s4[(c >> 1) & 3] = __fadd2_rn(s4[(c >> 1) & 3], y);
             pw[c / 2] = pack_bf16x2(y.x, y.y);
             const float2 f = bf2_to_f2(pw[c / 2]);
-            if (second) pw[c / 2] = pack_bf16x2(y.x - f.x, y.y - f.y);
+            const uint32_t rest = pack_bf16x2(y.x - f.x, y.y - f.y);
+            if constexpr (ZZ::P3) {  // (s is free behind its weight: the third part in its place)
+                const float2 r = bf2_to_f2(rest);
+                s[c] = second ? 0.f : (y.x - f.x) - r.x;
+                s[c + 1] = second ? 0.f : (y.y - f.y) - r.y;
+            }
+            if (second) pw[c / 2] = rest;
         }
         const float2 sa = __fadd2_rn(s4[0], s4[1]), sb = __fadd2_rn(s4[2], s4[3]);
         l += (sa.x + sa.y) + (sb.x + sb.y);
-        if constexpr (R == 64) tmem_st32u_nowait(tp, pw);
-        else if constexpr (R == 32) tmem_st16u(tp + col0 / 2, pw);
-        else tmem_st8u(tp + col0 / 2, pw);
+        auto store = [&](uint32_t at) {
+            if constexpr (R == 64) tmem_st32u_nowait(at, pw);
+            else if constexpr (R == 32) tmem_st16u(at + col0 / 2, pw);
+            else tmem_st8u(at + col0 / 2, pw);
+        };
+        store(tp);
+        if constexpr (ZZ::P3) {
+#pragma unroll
+            for (int c = 0; c < R; c += 2) pw[c / 2] = pack_bf16x2(s[c], s[c + 1]);
+            store(tp + kPT / 2);
+        }
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(&x.bar[bPfull + g]);
@@ -660,10 +681,10 @@ __device__ __forceinline__ void softmax_run(const SoftmaxCtx &x, int run, int it
     mbar_arrive(&x.bar[bMfull + (run & 1)]);
 }
 
-template <int RK, int RV, int DR>
+template <int RK, int RV, int DR, bool THIRD>
 __global__ void __launch_bounds__(kTrunkThreads, 1)
     trunk_kernel(const __grid_constant__ CUtensorMap tv, const __grid_constant__ TrunkParams p) {
-    using ZZ = Z<RK, RV, DR>;
+    using ZZ = Z<RK, RV, DR, THIRD>;
     extern __shared__ __align__(1024) char sm_raw[];
     char *sm = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(sm_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     uint64_t *bar = reinterpret_cast<uint64_t *>(sm + ZZ::oBar);
@@ -781,15 +802,16 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
                 tc_fence_after();
                 const uint64_t dk = dk0 + static_cast<uint64_t>((st * ZZ::KPAGE) >> 4);
                 const uint32_t ts = tmem + ZZ::TM_S + g * kPT;
+                // the small parts first: what they add is not rounded to the size of the whole
 #pragma unroll
-                for (int part = 0; part < 3; ++part)
+                for (int part = 2; part >= 0; --part)
 #pragma unroll
                     for (int ks = 0; ks < ZZ::RKT / 16; ++ks) {
+                        const bool more = part < 2 || ks > 0;
                         if (part < ZZ::QT)
-                            umma_bf16_ts_warp(ts, tmem + ZZ::TM_Q + part * ZZ::PART + ks * 8, dk + ks * ((2 * kPT * 16) >> 4), ZZ::IDESC_S,
-                                              part > 0 || ks > 0);
+                            umma_bf16_ts_warp(ts, tmem + ZZ::TM_Q + part * ZZ::PART + ks * 8, dk + ks * ((2 * kPT * 16) >> 4), ZZ::IDESC_S, more);
                         else
-                            umma_bf16_warp(ts, dq + ks * ((2 * kRows * 16) >> 4), dk + ks * ((2 * kPT * 16) >> 4), ZZ::IDESC_S, true);
+                            umma_bf16_warp(ts, dq + ks * ((2 * kRows * 16) >> 4), dk + ks * ((2 * kPT * 16) >> 4), ZZ::IDESC_S, more);
                     }
                 if (k == pages - 1) umma_commit_warp(&bar[bQfree]);
                 umma_commit_warp(&bar[bKempty + st]);
@@ -818,6 +840,11 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
 #pragma unroll
                 for (int ks = 0; ks < kPT / 16; ++ks)
                     umma_bf16_ts_warp(tmem + ZZ::TM_O, tmem + ZZ::TM_P + g * ZZ::P_STEP + ks * 8, dv + ks * (2048 >> 4), ZZ::IDESC_O, k > 0 || ks > 0);
+                if constexpr (THIRD) {
+#pragma unroll
+                    for (int ks = 0; ks < kPT / 16; ++ks)
+                        umma_bf16_ts_warp(tmem + ZZ::TM_O, tmem + ZZ::TM_P + g * ZZ::P_STEP + kPT / 2 + ks * 8, dv + ks * (2048 >> 4), ZZ::IDESC_O, true);
+                }
                 umma_commit_warp(&bar[bVempty + st]);
                 if (k == pages - 1) umma_commit_warp(&bar[bOdone]);
                 umma_commit_warp(&bar[bPfree + g]);  // also: O holds pages up to it
@@ -994,9 +1021,9 @@ __device__ __forceinline__ void leaf_page(const char *slot, const float *qs, flo
                                           float (&acc)[kLeaf][5], F k_read) {
     constexpr int RV = LL::VPLANE / (kPT * 2);
     const int lane = threadIdx.x & 31;
-    float s[NQ][2];
+    float s[NQ][2][2];  // of two tokens, in two sums each: shorter chains, and less to round
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) s[q][0] = s[q][1] = 0.f;
+    for (int q = 0; q < NQ; ++q) s[q][0][0] = s[q][0][1] = s[q][1][0] = s[q][1][1] = 0.f;
     auto dot = [&](const char *plane, const float *qq, int granules) {
 #pragma unroll 2
         for (int g = 0; g < granules; ++g) {
@@ -1007,8 +1034,10 @@ __device__ __forceinline__ void leaf_page(const char *slot, const float *qs, flo
 #pragma unroll
             for (int q = 0; q < NQ; ++q) {
                 const float4 u = *reinterpret_cast<const float4 *>(qq + q * LL::RKT + g * 8), v = *reinterpret_cast<const float4 *>(qq + q * LL::RKT + g * 8 + 4);
-                s[q][0] = fmaf(a3.y, v.w, fmaf(a3.x, v.z, fmaf(a2.y, v.y, fmaf(a2.x, v.x, fmaf(a1.y, u.w, fmaf(a1.x, u.z, fmaf(a0.y, u.y, fmaf(a0.x, u.x, s[q][0]))))))));
-                s[q][1] = fmaf(b3.y, v.w, fmaf(b3.x, v.z, fmaf(b2.y, v.y, fmaf(b2.x, v.x, fmaf(b1.y, u.w, fmaf(b1.x, u.z, fmaf(b0.y, u.y, fmaf(b0.x, u.x, s[q][1]))))))));
+                s[q][0][0] = fmaf(a1.y, u.w, fmaf(a1.x, u.z, fmaf(a0.y, u.y, fmaf(a0.x, u.x, s[q][0][0]))));
+                s[q][0][1] = fmaf(a3.y, v.w, fmaf(a3.x, v.z, fmaf(a2.y, v.y, fmaf(a2.x, v.x, s[q][0][1]))));
+                s[q][1][0] = fmaf(b1.y, u.w, fmaf(b1.x, u.z, fmaf(b0.y, u.y, fmaf(b0.x, u.x, s[q][1][0]))));
+                s[q][1][1] = fmaf(b3.y, v.w, fmaf(b3.x, v.z, fmaf(b2.y, v.y, fmaf(b2.x, v.x, s[q][1][1]))));
             }
         }
     };
@@ -1017,7 +1046,7 @@ __device__ __forceinline__ void leaf_page(const char *slot, const float *qs, flo
     k_read();
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
-        const float x0 = lane < left ? s[q][0] : -INFINITY, x1 = lane + 32 < left ? s[q][1] : -INFINITY;
+        const float x0 = lane < left ? s[q][0][0] + s[q][0][1] : -INFINITY, x1 = lane + 32 < left ? s[q][1][0] + s[q][1][1] : -INFINITY;
         const float mn = fmaxf(m[q], warp_max(fmaxf(x0, x1)));
         const float f = m[q] == -INFINITY ? 0.f : ex2_approx(m[q] - mn);
         const float p0 = ex2_approx(x0 - mn), p1 = ex2_approx(x1 - mn);
@@ -1408,10 +1437,10 @@ PrefixWorkspace prefix_workspace(int rkt, int r_v, int B, int H, int grid) {
     return w;
 }
 
-template <int RK, int RV, int DR>
+template <int RK, int RV, int DR, bool THIRD>
 lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void *rope_pool, const RotaryAxes &rope,
                          const int32_t *positions, const void *q_rope, const void *cur_k_rope, cudaStream_t stream) {
-    using ZZ = Z<RK, RV, DR>;
+    using ZZ = Z<RK, RV, DR, THIRD>;
     lla_status st = LLA_OK;
     unsigned *err = device_error_word(&st);
     if (st != LLA_OK) return st;
@@ -1425,7 +1454,7 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     using LL = L<RK, RV, DR>;
     static DeviceOnce configured, configured_leaf;
     if (raise_smem_limit(leaf_kernel<RK, RV, DR>, LL::SMEM, configured_leaf) != LLA_OK) return LLA_ERR_CUDA;
-    if (raise_smem_limit(trunk_kernel<RK, RV, DR>, ZZ::SMEM, configured) != LLA_OK) return LLA_ERR_CUDA;
+    if (raise_smem_limit(trunk_kernel<RK, RV, DR, THIRD>, ZZ::SMEM, configured) != LLA_OK) return LLA_ERR_CUDA;
     const int64_t page_bytes = static_cast<int64_t>(head_page_bytes(RK, RV, 2));
     // the V-planes of every page: [num_blocks * H][64 tokens][r_v] bf16
     CUtensorMap tv;
@@ -1461,7 +1490,7 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     if ((st = launch_ex(absorb_kernel<RK, DR>, dim3(a.H, (ZZ::RKX + 31) / 32 + (DR > 0) + 1, (a.B + 15) / 16), 256, 0, stream, ap)) != LLA_OK)
         return st;
     const bool alone = a.B <= kLeaf;  // no group can have more members
-    if (!alone && (st = launch_ex(trunk_kernel<RK, RV, DR>, dim3(grid), kTrunkThreads, ZZ::SMEM, stream, tv, tp)) != LLA_OK) return st;
+    if (!alone && (st = launch_ex(trunk_kernel<RK, RV, DR, THIRD>, dim3(grid), kTrunkThreads, ZZ::SMEM, stream, tv, tp)) != LLA_OK) return st;
     if ((st = launch_ex(leaf_kernel<RK, RV, DR>, dim3(grid), LL::WARPS * 32, LL::SMEM, stream, tp, static_cast<int>(alone))) != LLA_OK) return st;
 
     JoinParams jp = {};
@@ -1505,7 +1534,8 @@ lla_status launch_decode_prefix(const DecodeArgs &a, const lla_prefix &plan, con
                                 const void *cur_k_rope, cudaStream_t stream) {
 #define LLA_PREFIX(K, V, R) \
     if (a.r_k == K && a.r_v == V && d_rope == R) \
-        return launch_prefix<K, V, R>(a, plan, rope_pool, rope, positions, q_rope, cur_k_rope, stream);
+        return a.io_bf16 ? launch_prefix<K, V, R, false>(a, plan, rope_pool, rope, positions, q_rope, cur_k_rope, stream) \
+                         : launch_prefix<K, V, R, true>(a, plan, rope_pool, rope, positions, q_rope, cur_k_rope, stream);
     LLA_PREFIX(96, 160, 0)
     LLA_PREFIX(128, 128, 0)
     LLA_PREFIX(72, 120, 0)
