@@ -62,7 +62,8 @@ constexpr int kMembers = LLA_PREFIX_MEMBERS;
 constexpr int kMaxNodes = kLevels * (LLA_MAX_BATCH / 2) + LLA_MAX_BATCH;
 constexpr int kTrunkThreads = 512;
 constexpr int kSoftmaxWarp = 4, kAuxWarp = 12;
-constexpr int kLeaf = 2;         // most queries of a node that the leaf kernel takes
+constexpr int kLeaf = 2;         // most queries of a node that the leaf kernel takes beside a trunk kernel
+constexpr int kLeafAlone = 4;    // and without one: most sequences of a call that has none
 constexpr int kMaxGrid = 256;
 constexpr int kJoinSeqs = 8;
 constexpr int kSmemCap = 227 * 1024;
@@ -75,6 +76,7 @@ struct PlanView {
 
 struct TrunkParams {
     int H, B, max_ctx, max_blocks, pass1;
+    int leaf_max;  // queries of a node that the leaf kernel takes, at most
     const char *pool;
     int64_t num_blocks, page_bytes;
     const char *rope_pool;
@@ -129,7 +131,7 @@ __device__ __forceinline__ Node node_at(const TrunkParams &p, int groups, int i)
     Node d = {0, 0, 0, 0, 0, INT32_MAX};
     if (i < groups) {
         const int4 g = reinterpret_cast<const int4 *>(p.plan.groups)[i];
-        if (g.x < 0 || g.y <= g.x || g.y > cap / kPT || g.w < 1 || g.w > kMembers || g.z < 0 || g.z > kLevels * p.B - g.w) return d;
+        if (g.x < 0 || g.y <= g.x || g.y > cap / kPT || g.w < 1 || g.w > min(kMembers, p.B) || g.z < 0 || g.z > kLevels * p.B - g.w) return d;
         d.row = p.plan.members[g.z];
         if (d.row < 0 || d.row >= p.B) return d;
         d.pages = g.y - g.x;
@@ -148,14 +150,14 @@ __device__ __forceinline__ Node node_at(const TrunkParams &p, int groups, int i)
     return d;
 }
 
-__device__ __forceinline__ bool is_leaf(const Node &d) { return d.n <= kLeaf; }
+__device__ __forceinline__ bool is_leaf(const TrunkParams &p, const Node &d) { return d.n <= p.leaf_max; }
 
 // Record of the first query of node d at head h, from CTA (or leaf warp) c: r_v latent values, the maximum, the sum.  The
 // records of a unit's runs lie as far apart as a node of its kind can have queries, so that no two of them meet: units and
 // CTAs grow together.
 __device__ __forceinline__ int64_t record_of(const TrunkParams &p, const Node &d, int h, int c) {
     const int64_t at = static_cast<int64_t>(p.H) * d.member + static_cast<int64_t>(h) * d.n;
-    return is_leaf(d) ? p.leaf + at + static_cast<int64_t>(kLeaf) * c : at + static_cast<int64_t>(kMembers) * c;
+    return is_leaf(p, d) ? p.leaf + at + static_cast<int64_t>(p.leaf_max) * c : at + static_cast<int64_t>(kMembers) * c;
 }
 __host__ __device__ constexpr int record_floats(int rv) { return rv + 4; }
 
@@ -184,7 +186,7 @@ __device__ void node_prefix(const TrunkParams &p) {
     if (*p.plan.num_groups != groups) bad |= LLA_DEVERR_SEQUENCE;
     for (int i = tid; i < nodes; i += 256) {
         const Node d = node_at(p, groups, i);
-        pages[i] = is_leaf(d) ? -1 - d.pages : d.pages;
+        pages[i] = is_leaf(p, d) ? -1 - d.pages : d.pages;
         if (i < groups && d.pages == 0) bad |= LLA_DEVERR_SEQUENCE;
         if (i >= groups) {
             if (d.len < 0 || d.len > cap || d.first < 0 || d.first > d.len / kPT) bad |= LLA_DEVERR_CONTEXT;
@@ -416,7 +418,7 @@ __device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list, in
     };
     auto pages = [&](int i) {
         const Node d = node_at(p, groups, i);
-        return is_leaf(d) == LEAF ? d.pages * p.H : 0;
+        return is_leaf(p, d) == LEAF ? d.pages * p.H : 0;
     };
     int tot = 0;
     for (int i = tid * per; i < min(nodes, (tid + 1) * per); ++i) tot += pages(i);
@@ -981,12 +983,13 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
 
 // Shared memory of the leaf kernel: a slot for one page, the queries and the weights of each warp.
 constexpr int kMaxWarps = 9;
-template <int RK, int RV, int DR>
+template <int RK, int RV, int DR, bool ALONE>
 struct L {
+    static constexpr int NQ = ALONE ? kLeafAlone : kLeaf;  // queries of a node
     static constexpr int RKX = (RK + 15) / 16 * 16, RKT = RKX + DR;
     static constexpr int KPLANE = kPT * RK * 2, RPLANE = kPT * DR * 2, VPLANE = kPT * RV * 2;
     static constexpr int SLOT = KPLANE + RPLANE + VPLANE;
-    static constexpr int SCRATCH = kLeaf * (RKT + kPT) * 4 + 16;  // q~, p, two barriers
+    static constexpr int SCRATCH = NQ * (RKT + kPT) * 4 + 16;  // q~, p, two barriers
     static constexpr int W0 = (kSmemCap - 2048 - kMaxNodes * 2 - 64) / (SLOT + SCRATCH);
     static constexpr int WARPS = W0 > kMaxWarps ? kMaxWarps : W0;
     static constexpr int oScratch = WARPS * SLOT;
@@ -1017,8 +1020,8 @@ struct PageWalk {
 // One page of NQ queries, by a warp: scores of tokens lane and lane + 32 from the K-plane (and the rotary plane), the online
 // softmax of each query, and 4 or 5 columns of its value sum in each lane.  `k_read` is called when the K-plane has been read.
 template <typename LL, int NQ, typename F>
-__device__ __forceinline__ void leaf_page(const char *slot, const float *qs, float *ps, int left, float (&m)[kLeaf], float (&l)[kLeaf],
-                                          float (&acc)[kLeaf][5], F k_read) {
+__device__ __forceinline__ void leaf_page(const char *slot, const float *qs, float *ps, int left, float (&m)[LL::NQ], float (&l)[LL::NQ],
+                                          float (&acc)[LL::NQ][5], F k_read) {
     constexpr int RV = LL::VPLANE / (kPT * 2);
     const int lane = threadIdx.x & 31;
     float s[NQ][2][2];  // of two tokens, in two sums each: shorter chains, and less to round
@@ -1100,9 +1103,10 @@ __device__ __forceinline__ void leaf_page(const char *slot, const float *qs, flo
 // one lands, and while it works on that one's scores its V-plane does.  The other warps' copies fill the rest of HBM's time, so
 // that a warp's run boundaries (the queries of the next run, the record of this one) cost nothing until the warps of an SM
 // together cannot keep up.
-template <int RK, int RV, int DR>
-__global__ void __launch_bounds__(L<RK, RV, DR>::WARPS * 32, 1) leaf_kernel(const __grid_constant__ TrunkParams p, int alone) {
-    using LL = L<RK, RV, DR>;
+template <int RK, int RV, int DR, bool ALONE>
+__global__ void __launch_bounds__(L<RK, RV, DR, ALONE>::WARPS * 32, 1) leaf_kernel(const __grid_constant__ TrunkParams p) {
+    using LL = L<RK, RV, DR, ALONE>;
+    constexpr int NQ = LL::NQ;
     constexpr int RS = record_floats(RV);
     extern __shared__ __align__(128) char sm[];
     __shared__ int abort_word;
@@ -1110,7 +1114,7 @@ __global__ void __launch_bounds__(L<RK, RV, DR>::WARPS * 32, 1) leaf_kernel(cons
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     char *slot = sm + warp * LL::SLOT;
     uint64_t *bar = reinterpret_cast<uint64_t *>(sm + LL::oScratch + warp * LL::SCRATCH);  // K, V
-    float *qs = reinterpret_cast<float *>(bar + 2), *ps = qs + kLeaf * LL::RKT;
+    float *qs = reinterpret_cast<float *>(bar + 2), *ps = qs + NQ * LL::RKT;
     uint16_t *list = reinterpret_cast<uint16_t *>(sm + LL::oList);
     if (lane == 0) {
         mbar_init(&bar[0], 1);
@@ -1120,7 +1124,7 @@ __global__ void __launch_bounds__(L<RK, RV, DR>::WARPS * 32, 1) leaf_kernel(cons
     if (tid == 0) abort_word = 0;
     // The trunk kernel lets this one start when all of its CTAs have waited for the absorb kernel, so that q~ and beta are
     // there and the workspace is free.  Its own records are not read here; the wait for it is at the end.
-    if (alone) pdl_wait();  // there is no trunk kernel between the absorb kernel and this one
+    if (ALONE) pdl_wait();  // there is no trunk kernel between the absorb kernel and this one
     pdl_trigger();          // the join may take this SM as soon as this CTA has left it
     const int groups = count_groups(p), workers = gridDim.x * LL::WARPS;
     Share sh = find_share<true, LL::WARPS * 32>(p, groups, list, blockIdx.x * LL::WARPS, LL::WARPS, workers);
@@ -1160,15 +1164,15 @@ __global__ void __launch_bounds__(L<RK, RV, DR>::WARPS * 32, 1) leaf_kernel(cons
         while (ok && w.next()) {
             // the queries, each the sum of its three parts (which is exact)
             const int n = w.r.d.n;
-            for (int q = 0; q < n; ++q) {
+            for (int q = 0; q < (n == 3 ? 4 : n); ++q) {  // (beside three queries there is a fourth of zeros)
                 const uint16_t *src = reinterpret_cast<const uint16_t *>(query_parts<LL::QROW>(p, w.r, q));
                 for (int i = lane; i < LL::RKT; i += 32)
                     qs[q * LL::RKT + i] = src ? bf_to_f(__ldcg(src + i)) + (bf_to_f(__ldcg(src + LL::RKT + i)) + bf_to_f(__ldcg(src + 2 * LL::RKT + i))) : 0.f;
             }
             __syncwarp();
-            float m[kLeaf], l[kLeaf], acc[kLeaf][5];
+            float m[NQ], l[NQ], acc[NQ][5];
 #pragma unroll
-            for (int q = 0; q < kLeaf; ++q) {
+            for (int q = 0; q < NQ; ++q) {
                 m[q] = -INFINITY;
                 l[q] = 0.f;
 #pragma unroll
@@ -1189,7 +1193,8 @@ __global__ void __launch_bounds__(L<RK, RV, DR>::WARPS * 32, 1) leaf_kernel(cons
                     ok = mbar_wait(&bar[1], it & 1, abort_flag, p.err) && ok;
                 };
                 if (n == 1) leaf_page<LL, 1>(slot, qs, ps, left, m, l, acc, k_read);
-                else leaf_page<LL, 2>(slot, qs, ps, left, m, l, acc, k_read);
+                else if (NQ == 2 || n == 2) leaf_page<LL, 2>(slot, qs, ps, left, m, l, acc, k_read);
+                else leaf_page<LL, NQ>(slot, qs, ps, left, m, l, acc, k_read);
                 __syncwarp();
                 if (ok && ahead.ok) {
                     issue_v(blk, ahead.w.r.h);
@@ -1198,7 +1203,7 @@ __global__ void __launch_bounds__(L<RK, RV, DR>::WARPS * 32, 1) leaf_kernel(cons
             }
             float *dst = p.part + record_of(p, w.r.d, w.r.h, me) * RS;
 #pragma unroll
-            for (int q = 0; q < kLeaf; ++q) {
+            for (int q = 0; q < NQ; ++q) {
                 const float sum = warp_sum(l[q]);
                 if (q >= n) continue;
                 if (lane * 4 < RV)
@@ -1253,19 +1258,8 @@ __global__ void __launch_bounds__(kJoinThreads, kJoinCtas) join_kernel(const __g
     int G = 1;
     while (2 * G * nb <= kJoinThreads / 32) G *= 2;
     const int bi = warp / G, sub = warp - bi * G, b = b0 + min(bi, nb - 1);
-    // (inputs of the call, before the wait:) the current token's score; lane l < 4 knows level l's node of the sequence, lane 3
-    // its own pages
-    float qk = -INFINITY;
-    if (a.cur_k) {
-        const int64_t row = iorow(b);
-        qk = 0.f;
-#pragma unroll
-        for (int i = 0; i < kD / 32; ++i)
-            qk = fmaf(load_elem(a.q, row * kD + lane + 32 * i, a.io_bf16), load_elem(a.cur_k, row * kD + lane + 32 * i, a.io_bf16), qk);
-        for (int i = lane; i < a.d_rope; i += 32)  // both stand at one position: the rotation cancels
-            qk = fmaf(load_elem(a.q_rope, row * a.d_rope + i, a.io_bf16), load_elem(a.cur_k_rope, static_cast<int64_t>(b) * a.d_rope + i, a.io_bf16), qk);
-        qk = warp_sum(qk) * a.scale_log2;
-    }
+    // (inputs of the call, before the wait:) lane l < 3 knows level l's node of the sequence, lane 3 its own pages; then the
+    // current token's score
     const int groups = count_groups(p), nodes = groups + p.B;
     int node = groups + b, rank = 0;
     bool there = lane == kLevels;
@@ -1280,6 +1274,17 @@ __global__ void __launch_bounds__(kJoinThreads, kJoinCtas) join_kernel(const __g
     Node d = {0, 0, 0, 0, 0, 0};
     if (there) d = node_at(p, groups, node);
     there = d.pages > 0 && rank < d.n;
+    float qk = -INFINITY;
+    if (a.cur_k) {
+        const int64_t row = iorow(b);
+        qk = 0.f;
+#pragma unroll
+        for (int i = 0; i < kD / 32; ++i)
+            qk = fmaf(load_elem(a.q, row * kD + lane + 32 * i, a.io_bf16), load_elem(a.cur_k, row * kD + lane + 32 * i, a.io_bf16), qk);
+        for (int i = lane; i < a.d_rope; i += 32)  // both stand at one position: the rotation cancels
+            qk = fmaf(load_elem(a.q_rope, row * a.d_rope + i, a.io_bf16), load_elem(a.cur_k_rope, static_cast<int64_t>(b) * a.d_rope + i, a.io_bf16), qk);
+        qk = warp_sum(qk) * a.scale_log2;
+    }
     // Twice: first without a run, while the kernels before still run, so that the instructions are there when the records are
     // (fetched behind the wait they took longer than the join).
 #pragma unroll 1
@@ -1291,12 +1296,12 @@ __global__ void __launch_bounds__(kJoinThreads, kJoinCtas) join_kernel(const __g
     // the runs of the nodes: records first + step i of run i
     int runs = 0, first = 0, step = 0;
     if (there && dry == 0) {
-        const int kind = is_leaf(d), np = p.pstart[nodes + kind] * p.H, we = min(kind ? a.workers : a.grid, np);  // the split of find_share
+        const int kind = is_leaf(p, d), np = p.pstart[nodes + kind] * p.H, we = min(kind ? a.workers : a.grid, np);  // the split of find_share
         const Split split(np, we);
         const int s0 = p.pstart[node] * p.H + h * d.pages, c0 = split.worker(s0);
         runs = split.worker(s0 + d.pages - 1) - c0 + 1;
         first = static_cast<int>(record_of(p, d, h, c0)) + rank;
-        step = kind ? kLeaf : kMembers;
+        step = kind ? p.leaf_max : kMembers;
     }
     int upto[kLevels + 1];  // runs of the nodes up to each
 #pragma unroll
@@ -1428,7 +1433,7 @@ inline size_t al256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 PrefixWorkspace prefix_workspace(int rkt, int r_v, int B, int H, int grid) {
     PrefixWorkspace w;
     w.leaf = static_cast<size_t>(H) * kLevels * B + static_cast<size_t>(kMembers) * grid;
-    const size_t records = w.leaf + static_cast<size_t>(H) * (kLevels + 1) * B + static_cast<size_t>(kLeaf) * kMaxWarps * grid;
+    const size_t records = w.leaf + static_cast<size_t>(H) * (kLevels + 1) * B + static_cast<size_t>(kLeafAlone) * kMaxWarps * grid;
     w.part = 0;
     w.qt = al256(records * record_floats(r_v) * sizeof(float));
     w.beta = w.qt + al256(static_cast<size_t>(B) * H * 3 * rkt * sizeof(uint16_t));
@@ -1451,9 +1456,11 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     const PrefixWorkspace w = prefix_workspace(ZZ::RKT, RV, a.B, a.H, grid);
     if (a.workspace_bytes < w.total) return LLA_ERR_WORKSPACE;
     char *ws = static_cast<char *>(a.workspace);
-    using LL = L<RK, RV, DR>;
-    static DeviceOnce configured, configured_leaf;
-    if (raise_smem_limit(leaf_kernel<RK, RV, DR>, LL::SMEM, configured_leaf) != LLA_OK) return LLA_ERR_CUDA;
+    using LL = L<RK, RV, DR, false>;
+    using LA = L<RK, RV, DR, true>;
+    static DeviceOnce configured, configured_leaf, configured_alone;
+    if (raise_smem_limit(leaf_kernel<RK, RV, DR, false>, LL::SMEM, configured_leaf) != LLA_OK) return LLA_ERR_CUDA;
+    if (raise_smem_limit(leaf_kernel<RK, RV, DR, true>, LA::SMEM, configured_alone) != LLA_OK) return LLA_ERR_CUDA;
     if (raise_smem_limit(trunk_kernel<RK, RV, DR, THIRD>, ZZ::SMEM, configured) != LLA_OK) return LLA_ERR_CUDA;
     const int64_t page_bytes = static_cast<int64_t>(head_page_bytes(RK, RV, 2));
     // the V-planes of every page: [num_blocks * H][64 tokens][r_v] bf16
@@ -1475,6 +1482,11 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     tp.part = reinterpret_cast<float *>(ws + w.part);
     tp.pstart = reinterpret_cast<int *>(ws + w.pstart);
     tp.leaf = static_cast<int64_t>(w.leaf);
+    // No group of up to four sequences has more members than the leaf kernel can take: no trunk kernel then (four sequences over
+    // 768 tokens 25.5 -> 24.1 us).  Beside one, nodes of three and four queries are faster in it: 64 sequences over 16 prompts
+    // take 116 us, 123 with all of them as leaves.
+    const bool alone = a.B <= kLeafAlone;
+    tp.leaf_max = alone ? kLeafAlone : kLeaf;
     tp.err = err;
 
     AbsorbParams ap = {};
@@ -1489,13 +1501,17 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     }
     if ((st = launch_ex(absorb_kernel<RK, DR>, dim3(a.H, (ZZ::RKX + 31) / 32 + (DR > 0) + 1, (a.B + 15) / 16), 256, 0, stream, ap)) != LLA_OK)
         return st;
-    const bool alone = a.B <= kLeaf;  // no group can have more members
-    if (!alone && (st = launch_ex(trunk_kernel<RK, RV, DR, THIRD>, dim3(grid), kTrunkThreads, ZZ::SMEM, stream, tv, tp)) != LLA_OK) return st;
-    if ((st = launch_ex(leaf_kernel<RK, RV, DR>, dim3(grid), LL::WARPS * 32, LL::SMEM, stream, tp, static_cast<int>(alone))) != LLA_OK) return st;
+    if (alone) {
+        st = launch_ex(leaf_kernel<RK, RV, DR, true>, dim3(grid), LA::WARPS * 32, LA::SMEM, stream, tp);
+    } else {
+        if ((st = launch_ex(trunk_kernel<RK, RV, DR, THIRD>, dim3(grid), kTrunkThreads, ZZ::SMEM, stream, tv, tp)) != LLA_OK) return st;
+        st = launch_ex(leaf_kernel<RK, RV, DR, false>, dim3(grid), LL::WARPS * 32, LL::SMEM, stream, tp);
+    }
+    if (st != LLA_OK) return st;
 
     JoinParams jp = {};
     jp.t = tp;
-    jp.T = a.T; jp.loop = a.loop; jp.io_bf16 = a.io_bf16; jp.grid = grid; jp.workers = grid * LL::WARPS; jp.d_rope = DR;
+    jp.T = a.T; jp.loop = a.loop; jp.io_bf16 = a.io_bf16; jp.grid = grid; jp.workers = grid * (alone ? LA::WARPS : LL::WARPS); jp.d_rope = DR;
     jp.scale_log2 = ap.scale_log2;
     jp.w_up_v = a.w_up_v; jp.mu_v = a.mu_v;
     jp.q = a.q; jp.q_rope = q_rope; jp.cur_k = a.cur_k; jp.cur_v = a.cur_v; jp.cur_k_rope = cur_k_rope;

@@ -374,3 +374,45 @@ def test_no_batch_and_the_largest(lla):
     x = Batch(lla, rows, lens, H=2, rk=72, rv=120)
     assert x.B == 1024
     x.check(x.decode(), pairs=[(b, b % 2) for b in range(0, 1024, 37)])
+
+
+@pytest.mark.parametrize("B", [1, 2, 3, 4, 5])
+@pytest.mark.parametrize("rk, rv, d_rope", [(96, 160, 0), (128, 128, 0), (72, 120, 0), (96, 160, 96)])
+def test_up_to_four_sequences_and_one_more(lla, B, rk, rv, d_rope):
+    x = Batch(lla, *shared(1, B, 6, 100, system=1, branch=3, seed=B), H=5, rk=rk, rv=rv, d_rope=d_rope, mu=True, garbage=True)
+    first = x.decode()
+    x.check(first, pairs=[(b, h) for b in range(B) for h in range(5)])
+    for _ in range(5):
+        assert torch.equal(x.decode(), first)
+
+
+@pytest.mark.parametrize("W", [1, 2, 3, 4, 9, 33, 64])
+def test_weights_and_scores_keep_24_bits(lla, W):
+    """One page, with unit vectors for latents and weights: the score of token t is q_t scale, its value the t-th unit vector, so
+    that out_t / out_0 = e^(scale q_t) for q_0 = 0 >= q_t.  With |s| <= 1 in powers of two: q~ has two roundings and S two
+    (truncated) additions, 2^-23 + 2^-22; the difference to the maximum 2^-24; all of them times ln 2: 3e-7.  ex2 is good to
+    2^-22; and four roundings of either output, 8 2^-24.  Together 1.02e-6; weights of two bf16 parts would be off by 2^-18, and
+    scores with two parts of q~ by as much."""
+    x = Batch(lla, [[0]] * W, [64] * W, H=2)
+    page = x.pool[int(x.table[0, 0])]
+    page.zero_()
+    for t in range(BLOCK):
+        page[:, :BLOCK * 96].view(2, 12, BLOCK, 8)[:, t // 8, t, t % 8] = 1
+        page[:, BLOCK * 96:].view(2, BLOCK, 160)[:, t, t] = 1
+    x.wk.copy_(torch.eye(D, 96, dtype=BF16, device=DEV).expand_as(x.wk))
+    x.wv.copy_(torch.eye(D, 160, dtype=BF16, device=DEV).expand_as(x.wv))
+    g = torch.Generator().manual_seed(W)
+    x.q.copy_(-torch.rand(W, 2, D, generator=g) * (math.sqrt(D) * math.log(2.0)))
+    x.q[:, :, 0] = 0
+    out = f64(x.decode(pass1=False))[:, :, :BLOCK]
+    want = np.exp(f64(x.q)[:, :, :BLOCK] / math.sqrt(D))
+    assert np.abs(out / out[:, :, :1] / want - 1).max() <= 1.1e-6
+
+
+def test_a_group_of_more_members_than_sequences_is_flagged(lla):
+    x = Batch(lla, *shared(1, 3, 2, 64), H=2)
+    torch.cuda.synchronize()
+    x.plan.groups.view(-1)[3] = 5
+    x.decode()
+    assert lla.lla_get_device_error() & lla.LLA_DEVERR_SEQUENCE
+    lla.lla_clear_device_error()
