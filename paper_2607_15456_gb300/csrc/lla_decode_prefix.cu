@@ -83,6 +83,7 @@ struct TrunkParams {
     const int32_t *block_table, *context_lens;
     PlanView plan;
     uint16_t *qt;  // [B][H][3][RKT]: q~ * scale * log2 e as three bf16 parts, zero past r_k, then the rotary part
+    float *qf;     // [B][H][RKT]: the same in fp32, for the leaves
     float *beta;   // [B][H]: q . mu^K * scale * log2 e
     float *part;   // run records, see record_of
     int *pstart;   // [groups + B]: pages of the nodes of the same kind before each; then the pages of either kind
@@ -288,8 +289,12 @@ __global__ void __launch_bounds__(256) absorb_kernel(const __grid_constant__ Abs
                 const int64_t src = (static_cast<int64_t>(b) * p.H + h) * DR;
                 const float x = load_elem(a.q_rope, src + ia, a.io_bf16), y = load_elem(a.q_rope, src + ic, a.io_bf16);
                 uint16_t *dst = p.qt + (static_cast<int64_t>(b) * p.H + h) * 3 * RKT + RKX;
-                store_parts(dst + ia, RKT, (x * cs - y * sn) * a.scale_log2);
-                store_parts(dst + ic, RKT, (x * sn + y * cs) * a.scale_log2);
+                const float u = (x * cs - y * sn) * a.scale_log2, v = (x * sn + y * cs) * a.scale_log2;
+                store_parts(dst + ia, RKT, u);
+                store_parts(dst + ic, RKT, v);
+                float *qf = p.qf + (static_cast<int64_t>(b) * p.H + h) * RKT + RKX;
+                qf[ia] = u;
+                qf[ic] = v;
             }
             return;
         }
@@ -318,8 +323,12 @@ __global__ void __launch_bounds__(256) absorb_kernel(const __grid_constant__ Abs
         float s = 0.f;
 #pragma unroll
         for (int sl = 0; sl < 8; ++sl) s += red[sl][bi][c];
-        if (bi < nb && j0 + c < RKX)
-            store_parts(p.qt + (static_cast<int64_t>(b0 + bi) * p.H + h) * 3 * RKT + j0 + c, RKT, j0 + c < RK ? s * a.scale_log2 : 0.f);
+        if (bi < nb && j0 + c < RKX) {
+            const int64_t row = static_cast<int64_t>(b0 + bi) * p.H + h;
+            s = j0 + c < RK ? s * a.scale_log2 : 0.f;
+            store_parts(p.qt + row * 3 * RKT + j0 + c, RKT, s);
+            p.qf[row * RKT + j0 + c] = s;
+        }
     }
     if (blockIdx.y == 0) {
         for (int bi = warp; bi < nb; bi += 8) {
@@ -507,14 +516,13 @@ struct RunWalk {
     }
 };
 
-// The parts of query i of a run, or NULL where it has none.
-template <int QROW>
-__device__ __forceinline__ const char *query_parts(const TrunkParams &p, const TrunkRun &r, int i) {
-    if (i >= r.d.n) return nullptr;
+// Sequence * H + head of query i of a run, or -1 where it has none.
+__device__ __forceinline__ int64_t query_row(const TrunkParams &p, const TrunkRun &r, int i) {
+    if (i >= r.d.n) return -1;
     int b = r.d.row;
     if (r.d.member < kLevels * p.B) b = p.plan.members[r.d.member + i];
-    if (b < 0 || b >= p.B) return nullptr;
-    return reinterpret_cast<const char *>(p.qt) + (static_cast<int64_t>(b) * p.H + r.h) * QROW;
+    if (b < 0 || b >= p.B) return -1;
+    return static_cast<int64_t>(b) * p.H + r.h;
 }
 
 // A value that every lane has, for a warp that issues products (their descriptors are in uniform registers then).
@@ -883,7 +891,8 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
         };
         // the first words of a run's queries, before their place is free
         auto fetch_queries = [&](const TrunkRun &r) {
-            src = query_parts<ZZ::QROW>(p, r, row & (replica_rows(r.d.n) - 1));
+            const int64_t q = query_row(p, r, row & (replica_rows(r.d.n) - 1));
+            src = q < 0 ? nullptr : reinterpret_cast<const char *>(p.qt) + q * ZZ::QROW;
             fetch(0);
         };
         auto store_queries = [&] {
@@ -989,13 +998,12 @@ struct L {
     static constexpr int RKX = (RK + 15) / 16 * 16, RKT = RKX + DR;
     static constexpr int KPLANE = kPT * RK * 2, RPLANE = kPT * DR * 2, VPLANE = kPT * RV * 2;
     static constexpr int SLOT = KPLANE + RPLANE + VPLANE;
-    static constexpr int SCRATCH = NQ * (RKT + kPT) * 4 + 16;  // q~, p, two barriers
+    static constexpr int SCRATCH = NQ * (2 * RKT + kPT) * 4 + 16;  // q~ of two runs, p, two barriers
     static constexpr int W0 = (kSmemCap - 2048 - kMaxNodes * 2 - 64) / (SLOT + SCRATCH);
     static constexpr int WARPS = W0 > kMaxWarps ? kMaxWarps : W0;
     static constexpr int oScratch = WARPS * SLOT;
     static constexpr int oList = oScratch + WARPS * SCRATCH;
     static constexpr int SMEM = 128 + oList + kMaxNodes * 2 + 16;
-    static constexpr int QROW = 3 * RKT * 2;
     static constexpr bool TAIL = RV > 128;  // 4 columns in each lane, and one more behind the 128th
     static_assert(RV <= 160 && (RV <= 128 || RV == 160) && SCRATCH % 16 == 0, "columns of a warp");
 };
@@ -1114,7 +1122,7 @@ __global__ void __launch_bounds__(L<RK, RV, DR, ALONE>::WARPS * 32, 1) leaf_kern
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     char *slot = sm + warp * LL::SLOT;
     uint64_t *bar = reinterpret_cast<uint64_t *>(sm + LL::oScratch + warp * LL::SCRATCH);  // K, V
-    float *qs = reinterpret_cast<float *>(bar + 2), *ps = qs + NQ * LL::RKT;
+    float *qbuf = reinterpret_cast<float *>(bar + 2), *ps = qbuf + 2 * NQ * LL::RKT;
     uint16_t *list = reinterpret_cast<uint16_t *>(sm + LL::oList);
     if (lane == 0) {
         mbar_init(&bar[0], 1);
@@ -1156,19 +1164,28 @@ __global__ void __launch_bounds__(L<RK, RV, DR, ALONE>::WARPS * 32, 1) leaf_kern
                          &bar[1], pol);
             }
         };
+        // the queries of a run, as soon as its first page is asked for (loaded at its start, they took 2.6 us a run)
+        auto fetch_queries = [&](const TrunkRun &r, int run) {
+            for (int q = 0; q < (r.d.n == 3 ? 4 : r.d.n); ++q) {  // (beside three queries there is a fourth of zeros)
+                const int64_t row = query_row(p, r, q);
+                float *dst = qbuf + ((run & 1) * NQ + q) * LL::RKT;
+                for (int i = lane * 4; i < LL::RKT; i += 128) {
+                    if (row >= 0) cp_async16(dst + i, p.qf + row * LL::RKT + i);
+                    else *reinterpret_cast<float4 *>(dst + i) = make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+            }
+            cp_async_commit();
+        };
         int blk = checked(ahead.block(p));
         issue_k(blk, ahead.w.r.h);
         issue_v(blk, ahead.w.r.h);
-        int it = 0, issued_k = 1, issued_v = 1;
+        fetch_queries(ahead.w.r, 0);
+        int it = 0, run = 0, issued_k = 1, issued_v = 1;
         bool ok = true;
-        while (ok && w.next()) {
-            // the queries, each the sum of its three parts (which is exact)
+        for (; ok && w.next(); ++run) {
             const int n = w.r.d.n;
-            for (int q = 0; q < (n == 3 ? 4 : n); ++q) {  // (beside three queries there is a fourth of zeros)
-                const uint16_t *src = reinterpret_cast<const uint16_t *>(query_parts<LL::QROW>(p, w.r, q));
-                for (int i = lane; i < LL::RKT; i += 32)
-                    qs[q * LL::RKT + i] = src ? bf_to_f(__ldcg(src + i)) + (bf_to_f(__ldcg(src + LL::RKT + i)) + bf_to_f(__ldcg(src + 2 * LL::RKT + i))) : 0.f;
-            }
+            const float *qs = qbuf + (run & 1) * NQ * LL::RKT;
+            cp_async_wait_all();
             __syncwarp();
             float m[NQ], l[NQ], acc[NQ][5];
 #pragma unroll
@@ -1182,6 +1199,7 @@ __global__ void __launch_bounds__(L<RK, RV, DR, ALONE>::WARPS * 32, 1) leaf_kern
                 const int left = w.r.d.len - (w.r.page + k) * kPT;
                 ahead.step();
                 const int next = ahead.block(p);  // (in flight while the scores are worked out)
+                if (ahead.ok && ahead.k == 0) fetch_queries(ahead.w.r, run + 1);
                 ok = mbar_wait(&bar[0], it & 1, abort_flag, p.err);
                 auto k_read = [&] {
                     __syncwarp();
@@ -1214,8 +1232,8 @@ __global__ void __launch_bounds__(L<RK, RV, DR, ALONE>::WARPS * 32, 1) leaf_kern
                     dst[q * RS + RV + 1] = sum;
                 }
             }
-            __syncwarp();  // the queries are free
         }
+        cp_async_wait_all();
         if (!ok) {  // a wait ran out: what is in flight lands before the CTA can exit
             volatile int never = 0;
             mbar_wait(&bar[0], (issued_k - 1) & 1, &never, p.err);
@@ -1424,7 +1442,7 @@ __global__ void __launch_bounds__(kJoinThreads, kJoinCtas) join_kernel(const __g
 // ----------------------------------------------------------------------------------------------- host side
 
 struct PrefixWorkspace {
-    size_t part, qt, beta, pstart, total;
+    size_t part, qt, qf, beta, pstart, total;
     size_t leaf;  // first record of the leaf kernel
 };
 
@@ -1436,7 +1454,8 @@ PrefixWorkspace prefix_workspace(int rkt, int r_v, int B, int H, int grid) {
     const size_t records = w.leaf + static_cast<size_t>(H) * (kLevels + 1) * B + static_cast<size_t>(kLeafAlone) * kMaxWarps * grid;
     w.part = 0;
     w.qt = al256(records * record_floats(r_v) * sizeof(float));
-    w.beta = w.qt + al256(static_cast<size_t>(B) * H * 3 * rkt * sizeof(uint16_t));
+    w.qf = w.qt + al256(static_cast<size_t>(B) * H * 3 * rkt * sizeof(uint16_t));
+    w.beta = w.qf + al256(static_cast<size_t>(B) * H * rkt * sizeof(float));
     w.pstart = w.beta + al256(static_cast<size_t>(B) * H * sizeof(float));
     w.total = w.pstart + al256((kMaxNodes + 2) * sizeof(int));
     return w;
@@ -1478,6 +1497,7 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     tp.block_table = a.block_table; tp.context_lens = a.context_lens;
     tp.plan = PlanView{plan.num_groups, plan.groups, plan.members, plan.column, plan.own_page};
     tp.qt = reinterpret_cast<uint16_t *>(ws + w.qt);
+    tp.qf = reinterpret_cast<float *>(ws + w.qf);
     tp.beta = reinterpret_cast<float *>(ws + w.beta);
     tp.part = reinterpret_cast<float *>(ws + w.part);
     tp.pstart = reinterpret_cast<int *>(ws + w.pstart);
