@@ -11,17 +11,17 @@
 // current token:
 //   o = (W_up,t^V sum_j w_j o~_j + (sum_j w_j l_j) mu^V_t + w_cur v_cur) / (sum_j w_j l_j + w_cur),  w_j = e^(m_j - M).
 //
-// Four launches on the caller's stream, chained by programmatic dependent launch:
-//   absorb_kernel  q~ (fp32, scaled into the exp2 domain) and beta of every (sequence, head); the prefix sums of the nodes'
-//                  pages and the checks of lengths and plan
+// Four launches on the caller's stream, chained by programmatic dependent launch (three for up to four sequences):
+//   absorb_kernel  q~ (scaled into the exp2 domain) and beta of every (sequence, head); the prefix sums of the nodes' pages and
+//                  the checks of lengths and plan
 //   trunk_kernel   nodes of more than kLeaf queries, one CTA per SM.  Their pages, unit by unit in the order of the nodes, are
-//                  split evenly over the CTAs; a CTA takes its pages as runs (its part of one unit).  A page is two products on the tensor cores, with 128 rows for
-//                  the 64 queries of a run, each of them twice:
-//                    S [128 x 64 tokens] = sum_i Q~_i [C_k | K^R]^T      i = 0, 1, 2: q~ as three bf16 parts, in TMEM
+//                  split evenly over the CTAs; a CTA takes its pages as runs (its part of one unit).  A page is two products on
+//                  the tensor cores, with 128 rows for the up to 64 queries of a run, each of them 2, 4 or 8 times:
+//                    S [128 x 64 tokens] = sum_i Q~_i [C_k | K^R]^T      i = 2, 1, 0: q~ as three bf16 parts, in TMEM
 //                    O [128 x r_v]      += P C_v                         P in TMEM
-//                  Rows q and 64 + q have the same scores; the thread of the first gives its weights p as bf16(p), that of
-//                  the second as bf16(p - bf16(p)), so that the two rows of O add up to a sum with p in two parts, for the
-//                  tensor cores' price of one, and each thread has the scores of its query in its own registers.
+//                  All rows of a query have its scores; each thread works out the weights p of some of its tokens and gives them
+//                  as bf16(p) or as bf16(p - bf16(p)), so that the query's rows of O add up to a sum with p in two parts, for
+//                  the tensor cores' price of one.
 //                    warp 0        producer of K-planes (and rotary planes): bulk copies
 //                    warp 2        producer of V-planes: TMA boxes of 64 columns with 128-byte swizzle
 //                    warp 1        issuer of S, and owner of TMEM
@@ -30,12 +30,17 @@
 //                                  to weights takes longer than its products); the running maximum goes from page to page
 //                                  through shared memory and a named barrier per pair of warps; lazy rescale of O
 //                    warps 12-15   q~ of the next run into TMEM as soon as the last S of the run before is done; then that
-//                                  run's O, maxima and sums to the workspace
+//                                  run's O through shared memory, its maxima and its sums to the workspace
+//                  Bound by HBM and, at run ends, by latency: 393 MB of pages that 4 sequences each share take 74 us (5.3 TB/s),
+//                  287 MB that 64 share 73 us, with the tensor pipe busy for 55 % and the step from S to P for the rest
 //   leaf_kernel    nodes of up to kLeaf queries, which are short (a sequence's own pages): one page at a time in each of as
-//                  many warps as pages fit in an SM's shared memory, every warp on its own with an even share of the pages.
-//                  It starts on each SM as the trunk kernel leaves it
-//   join_kernel    per head and up to 8 sequences: joins the runs of each sequence's nodes and the current token, and applies
-//                  W_up,t^V once for all of them
+//                  many warps as pages fit in an SM's shared memory beside a CTA of the join, on the CUDA cores.  It starts on
+//                  each SM as the trunk kernel leaves it.  Bound by HBM while all warps run (6 TB/s)
+//   join_kernel    per head and up to 16 sequences: joins the runs of each sequence's nodes and the current token, and applies
+//                  W_up,t^V once for all of them.  One CTA per SM, beside the leaf kernel's, so that the weights and the
+//                  instructions are there when the records are: 13 us behind the leaves of 128 sequences in 16 heads (22 us where
+//                  it started when they had left, with the projection on the CUDA cores).  Bound by latency
+// 64 sequences over 16 prompts of 2048 to 4096 tokens, 16 heads, r 96 + 160: 110 us, of 83 us that HBM takes for the bytes.
 //
 // Storage bf16, d = 128; accumulators fp32 in TMEM.  Three parts of q~, and of p, hold the 24 bits of fp32.  For bf16 outputs p has
 // two: they are off by at most 2^-18 of p, half a step of the second part, and an output is rounded to 2^-9.  (With two for
@@ -65,7 +70,7 @@ constexpr int kSoftmaxWarp = 4, kAuxWarp = 12;
 constexpr int kLeaf = 2;         // most queries of a node that the leaf kernel takes beside a trunk kernel
 constexpr int kLeafAlone = 4;    // and without one: most sequences of a call that has none
 constexpr int kMaxGrid = 256;
-constexpr int kJoinSeqs = 8;
+constexpr int kJoinSeqs = 16;    // most sequences of a head that the join works on together
 constexpr int kSmemCap = 227 * 1024;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kRescaleLog2 = 8.f;  // rescale O^T only when a query's maximum grows by more
@@ -86,7 +91,8 @@ struct TrunkParams {
     float *qf;     // [B][H][RKT]: the same in fp32, for the leaves
     float *beta;   // [B][H]: q . mu^K * scale * log2 e
     float *part;   // run records, see record_of
-    int *pstart;   // [groups + B]: pages of the nodes of the same kind before each; then the pages of either kind
+    int *pstart;   // [2][kMaxNodes + 1]: pages of the trunk's nodes, and of the leaves, before each node; then all of them
+    int *next;     // share of the leaves that is taken next
     int64_t leaf;  // first record of the leaf kernel
     unsigned *err;
 };
@@ -174,6 +180,23 @@ struct Split {
     }
 };
 
+// The shares that the pages of the leaves are split into, for `workers` warps: one each of kLeafFirst / 8 of the pages, and the
+// rest in up to kLeafRest as many small ones, which the warps take as they get there.  A share's record does not depend on the
+// warp that took it, and so neither do the results.  (With one share of each warp the leaf kernel ended when the SM that the trunk
+// kernel left last had done its part: 102 us after the start for 128 sequences over 8 documents, 91 so.  Between 3/8 and 6/8, and
+// with 2 or 4, it is the same to 2 %; more shares are more records to join.)
+constexpr int kLeafFirst = 5, kLeafRest = 2;
+struct LeafShares {
+    int np, n1, w1, w2;  // pages; pages of the first shares, their number, the number of the small ones
+    Split first, rest;
+    __device__ __forceinline__ LeafShares(int pages, int workers)
+        : np(pages), n1(min(pages, max(workers, pages / 8 * kLeafFirst))), w1(min(workers, pages)), w2(min(kLeafRest * workers, pages - n1)),
+          first(n1, w1), rest(pages - n1, w2) {}
+    __device__ __forceinline__ int count() const { return w1 + w2; }
+    __device__ __forceinline__ int begin(int c) const { return c < w1 ? first.begin(c) : n1 + rest.begin(c - w1); }
+    __device__ __forceinline__ int share(int page) const { return page < n1 ? first.worker(page) : w1 + rest.worker(page - n1); }
+};
+
 // ----------------------------------------------------------------------------------------- absorb kernel
 
 // One CTA: the prefix sums of the nodes' pages, and the flags of what node_at leaves out.
@@ -234,13 +257,15 @@ __device__ void node_prefix(const TrunkParams &p) {
     }
     for (int i = tid * per; i < min(nodes, (tid + 1) * per); ++i) {
         const int v = pages[i];
-        p.pstart[i] = v < 0 ? ex[1] : ex[0];
+        p.pstart[i] = ex[0];
+        p.pstart[kMaxNodes + 1 + i] = ex[1];
         if (v < 0) ex[1] += -1 - v;
         else ex[0] += v;
     }
     if (tid == 255) {
         p.pstart[nodes] = ex[0];
-        p.pstart[nodes + 1] = ex[1];
+        p.pstart[kMaxNodes + 1 + nodes] = ex[1];
+        *p.next = 0;
     }
 }
 
@@ -406,14 +431,12 @@ struct TrunkRun {
 struct Share {
     int g0, g1;      // pages of this CTA, among all of the kind
     int nodes, s;    // nodes in `list`, first page of the first
-    int np, we;      // all pages, and the workers that have some
 };
 
-// This CTA's share of the pages of the leaves (LEAF) or of the other nodes, and the nodes that it lies in: worked out from the
-// inputs of the call by all threads, so that copies can start while the absorb kernel still runs.  The share is that of
-// workers w0 .. w0 + ws - 1 of `workers`.
-template <bool LEAF, int THREADS>
-__device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list, int w0, int ws, int workers) {
+// This CTA's share of the pages of the nodes with more queries than a leaf, and the nodes that it lies in: worked out from the
+// inputs of the call by all threads, so that copies can start while the absorb kernel still runs.
+template <int THREADS>
+__device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list) {
     __shared__ int wsum[THREADS / 32], wcnt[THREADS / 32], first;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int nodes = groups + p.B, per = (nodes + THREADS - 1) / THREADS;
@@ -427,7 +450,7 @@ __device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list, in
     };
     auto pages = [&](int i) {
         const Node d = node_at(p, groups, i);
-        return is_leaf(p, d) == LEAF ? d.pages * p.H : 0;
+        return is_leaf(p, d) ? 0 : d.pages * p.H;
     };
     int tot = 0;
     for (int i = tid * per; i < min(nodes, (tid + 1) * per); ++i) tot += pages(i);
@@ -439,14 +462,12 @@ __device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list, in
         if (w < warp) ex0 += wsum[w];
         np += wsum[w];
     }
-    // with fewer pages than workers the first np take one each
-    const int we = min(workers, np);
-    Share r;
-    r.np = np;
-    r.we = we;
+    // with fewer pages than CTAs the first np take one each
+    const int c = blockIdx.x, we = min(static_cast<int>(gridDim.x), np);
     const Split split(np, we);
-    r.g0 = w0 < we ? split.begin(w0) : 0;
-    r.g1 = w0 < we ? split.begin(min(w0 + ws, we)) : 0;
+    Share r;
+    r.g0 = c < we ? split.begin(c) : 0;
+    r.g1 = c < we ? split.begin(c + 1) : 0;
     int mine = 0, ex = ex0;
     for (int i = tid * per; i < min(nodes, (tid + 1) * per); ++i) {
         const int n = pages(i);
@@ -494,17 +515,15 @@ struct RunWalk {
             ++r.h;
             in = 0;
         } else {
-            do {
-                if (i >= 0) s += r.d.pages * p.H;
-                if (++i >= nodes || s >= g1) {
-                    r.pages = 0;
-                    r.d.pages = 0;
-                    i = nodes;
-                    u = stop = 0;
-                    return false;
-                }
-                r.d = node_at(p, groups, list[i]);
-            } while (s + r.d.pages * p.H <= g0);  // (a warp's part of a CTA's share may start behind its first nodes)
+            if (i >= 0) s += r.d.pages * p.H;
+            if (++i >= nodes) {
+                r.pages = 0;
+                r.d.pages = 0;
+                i = nodes;
+                u = stop = 0;
+                return false;
+            }
+            r.d = node_at(p, groups, list[i]);
             u = max(g0, s) - s;
             stop = min(g1, s + r.d.pages * p.H) - s;
             r.h = u / r.d.pages;
@@ -743,7 +762,7 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
     __syncthreads();
     tc_fence_after();
     constexpr uint32_t tmem = 0;  // the whole of TMEM is allocated (one CTA per SM)
-    const Share sh = find_share<false, kTrunkThreads>(p, groups, list, blockIdx.x, 1, gridDim.x);
+    const Share sh = find_share<kTrunkThreads>(p, groups, list);
     // q~ and beta come from the absorb kernel, and the workspace is free once it has waited for the kernel before it; the
     // producers read only inputs of the call, which that kernel's wait ordered before this launch, and wait at their end
     if (warp != 0 && warp != 2) {
@@ -990,6 +1009,18 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
 
 // -------------------------------------------------------------------------------------------- leaf kernel
 
+// Shared memory of the join kernel.
+constexpr int kJoinThreads = 512, kJoinWarps = kJoinThreads / 32;
+template <int RV>
+struct J {
+    static constexpr int RVX = (RV + 15) / 16 * 16;     // columns of the projection, zeros past r_v
+    static constexpr int WROW = (RVX / 8 | 1) * 16;     // bytes of a row of W_up^V: an odd number of 16-byte words
+    static constexpr int OROW = RVX + 8;                // floats of a row of o~
+    static constexpr int oO = kD * WROW, oCoef = oO + kJoinWarps * OROW * 4;
+    static constexpr int SMEM = oCoef + kJoinSeqs * 16;  // weights, a row of o~ of each warp, coefficients
+    static_assert(OROW % 32 == 8, "rows of o~ in other banks");
+};
+
 // Shared memory of the leaf kernel: a slot for one page, the queries and the weights of each warp.
 constexpr int kMaxWarps = 9;
 template <int RK, int RV, int DR, bool ALONE>
@@ -999,29 +1030,75 @@ struct L {
     static constexpr int KPLANE = kPT * RK * 2, RPLANE = kPT * DR * 2, VPLANE = kPT * RV * 2;
     static constexpr int SLOT = KPLANE + RPLANE + VPLANE;
     static constexpr int SCRATCH = NQ * (2 * RKT + kPT) * 4 + 16;  // q~ of two runs, p, two barriers
-    static constexpr int W0 = (kSmemCap - 2048 - kMaxNodes * 2 - 64) / (SLOT + SCRATCH);
+    // a CTA of the join kernel has room beside this one (1 KB of each is the system's)
+    static constexpr int W0 = (kSmemCap + 1024 - 2 * 1024 - 256 - J<RV>::SMEM) / (SLOT + SCRATCH);
     static constexpr int WARPS = W0 > kMaxWarps ? kMaxWarps : W0;
     static constexpr int oScratch = WARPS * SLOT;
-    static constexpr int oList = oScratch + WARPS * SCRATCH;
-    static constexpr int SMEM = 128 + oList + kMaxNodes * 2 + 16;
+    static constexpr int oAbort = oScratch + WARPS * SCRATCH, SMEM = 128 + oAbort + 16;
     static constexpr bool TAIL = RV > 128;  // 4 columns in each lane, and one more behind the 128th
     static_assert(RV <= 160 && (RV <= 128 || RV == 160) && SCRATCH % 16 == 0, "columns of a warp");
 };
 
-// Where a warp's next page comes from.
-struct PageWalk {
-    RunWalk w;
-    int k;
+// A warp's pages in order: of its first share, and of those that it takes then.
+struct LeafWalk {
+    const TrunkParams &p;
+    const LeafShares &sh;
+    const int *before;  // pages of the leaves before each node
+    int groups, nodes, share, u, end;  // pages u to end of the share are left
+    int i, s;                          // the node, and the page that it starts at
+    TrunkRun r;                        // the run
+    int k;                             // page of the run
     bool ok;
-    __device__ __forceinline__ PageWalk(const RunWalk &ww) : w(ww), k(-1), ok(true) { step(); }
-    __device__ __forceinline__ void step() {
-        if (++k >= w.r.pages) {
-            ok = w.next();
-            k = 0;
+    __device__ __forceinline__ LeafWalk(const TrunkParams &pp, const LeafShares &ss, int gr, int first)
+        : p(pp), sh(ss), before(pp.pstart + kMaxNodes + 1), groups(gr), nodes(gr + pp.B), share(first), u(0), end(0), i(-1), s(0), k(0) {
+        r.d.pages = 0;
+        ok = share < sh.w1;
+        if (ok) {
+            u = sh.begin(share);
+            end = sh.begin(share + 1);
+            next_run();
         }
     }
-    __device__ __forceinline__ int block(const TrunkParams &p) const {
-        return ok ? p.block_table[static_cast<int64_t>(w.r.d.row) * p.max_blocks + w.r.page + k] : 0;
+    // The last node with at most u pages of leaves before it: the one that page u lies in.  32 nodes behind node i are looked at
+    // first, then 32 parts of what is left.
+    __device__ __forceinline__ void find_node() {
+        const int page = u / p.H, lane = threadIdx.x & 31;
+        int lo = max(i, 0), n = nodes - lo;
+        for (int step = 1;; step = (n + 31) / 32) {
+            const int at = lo + lane * step;
+            const int c = __popc(__ballot_sync(0xffffffffu, lane * step < n && __ldcg(before + at) <= page));  // (at least one)
+            lo += (c - 1) * step;
+            n -= (c - 1) * step;
+            if (c < 32) n = min(n, step);
+            if (n == 1 || (step == 1 && c < 32)) break;
+        }
+        i = lo;
+        s = __ldcg(before + i) * p.H;
+        r.d = node_at(p, groups, i);
+    }
+    __device__ __forceinline__ void next_run() {
+        if (u >= s + r.d.pages * p.H) find_node();
+        r.h = (u - s) / r.d.pages;
+        const int in = u - s - r.h * r.d.pages;
+        r.page = r.d.first + in;
+        r.pages = min(end - u, r.d.pages - in);
+        u += r.pages;
+        k = 0;
+    }
+    __device__ __forceinline__ void step() {
+        if (++k < r.pages || !ok) return;
+        if (u >= end) {
+            if ((threadIdx.x & 31) == 0) share = sh.w1 + atomicAdd(p.next, 1);
+            share = __shfl_sync(0xffffffffu, share, 0);
+            ok = share < sh.count();
+            if (!ok) return;
+            u = sh.begin(share);
+            end = sh.begin(share + 1);
+        }
+        next_run();
+    }
+    __device__ __forceinline__ int block() const {
+        return ok ? p.block_table[static_cast<int64_t>(r.d.row) * p.max_blocks + r.page + k] : 0;
     }
 };
 
@@ -1112,37 +1189,31 @@ __device__ __forceinline__ void leaf_page(const char *slot, const float *qs, flo
 // that a warp's run boundaries (the queries of the next run, the record of this one) cost nothing until the warps of an SM
 // together cannot keep up.
 template <int RK, int RV, int DR, bool ALONE>
-__global__ void __launch_bounds__(L<RK, RV, DR, ALONE>::WARPS * 32, 1) leaf_kernel(const __grid_constant__ TrunkParams p) {
+__global__ void __maxnreg__(ALONE ? 160 : 120) leaf_kernel(const __grid_constant__ TrunkParams p) {
     using LL = L<RK, RV, DR, ALONE>;
     constexpr int NQ = LL::NQ;
     constexpr int RS = record_floats(RV);
     extern __shared__ __align__(128) char sm[];
-    __shared__ int abort_word;
-    volatile int *abort_flag = &abort_word;
+    volatile int *abort_flag = reinterpret_cast<int *>(sm + LL::oAbort);
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     char *slot = sm + warp * LL::SLOT;
     uint64_t *bar = reinterpret_cast<uint64_t *>(sm + LL::oScratch + warp * LL::SCRATCH);  // K, V
     float *qbuf = reinterpret_cast<float *>(bar + 2), *ps = qbuf + 2 * NQ * LL::RKT;
-    uint16_t *list = reinterpret_cast<uint16_t *>(sm + LL::oList);
     if (lane == 0) {
         mbar_init(&bar[0], 1);
         mbar_init(&bar[1], 1);
         fence_mbar_init();
     }
-    if (tid == 0) abort_word = 0;
+    if (tid == 0) *abort_flag = 0;
+    __syncthreads();
     // The trunk kernel lets this one start when all of its CTAs have waited for the absorb kernel, so that q~ and beta are
     // there and the workspace is free.  Its own records are not read here; the wait for it is at the end.
     if (ALONE) pdl_wait();  // there is no trunk kernel between the absorb kernel and this one
     pdl_trigger();          // the join may take this SM as soon as this CTA has left it
-    const int groups = count_groups(p), workers = gridDim.x * LL::WARPS;
-    Share sh = find_share<true, LL::WARPS * 32>(p, groups, list, blockIdx.x * LL::WARPS, LL::WARPS, workers);
-    const int me = blockIdx.x * LL::WARPS + warp;
-    const Split split(sh.np, sh.we);
-    sh.g0 = me < sh.we ? split.begin(me) : 0;
-    sh.g1 = me < sh.we ? split.begin(me + 1) : 0;
-    if (sh.g0 < sh.g1) {
-        RunWalk w(p, groups, sh, list);
-        PageWalk ahead(w);
+    const int groups = count_groups(p);
+    const LeafShares shares(__ldcg(p.pstart + kMaxNodes + 1 + groups + p.B) * p.H, gridDim.x * LL::WARPS);
+    LeafWalk ahead(p, shares, groups, blockIdx.x * LL::WARPS + warp);
+    if (ahead.ok) {
         const uint64_t pol = policy_evict_first();
         auto checked = [&](int blk) {
             if (blk >= 0 && blk < p.num_blocks) return blk;
@@ -1176,14 +1247,15 @@ __global__ void __launch_bounds__(L<RK, RV, DR, ALONE>::WARPS * 32, 1) leaf_kern
             }
             cp_async_commit();
         };
-        int blk = checked(ahead.block(p));
-        issue_k(blk, ahead.w.r.h);
-        issue_v(blk, ahead.w.r.h);
-        fetch_queries(ahead.w.r, 0);
+        int blk = checked(ahead.block());
+        issue_k(blk, ahead.r.h);
+        issue_v(blk, ahead.r.h);
+        fetch_queries(ahead.r, 0);
         int it = 0, run = 0, issued_k = 1, issued_v = 1;
         bool ok = true;
-        for (; ok && w.next(); ++run) {
-            const int n = w.r.d.n;
+        for (; ok && ahead.ok; ++run) {
+            const TrunkRun r = ahead.r;
+            const int n = r.d.n, share = ahead.share;
             const float *qs = qbuf + (run & 1) * NQ * LL::RKT;
             cp_async_wait_all();
             __syncwarp();
@@ -1195,17 +1267,17 @@ __global__ void __launch_bounds__(L<RK, RV, DR, ALONE>::WARPS * 32, 1) leaf_kern
 #pragma unroll
                 for (int e = 0; e < 5; ++e) acc[q][e] = 0.f;
             }
-            for (int k = 0; ok && k < w.r.pages; ++k, ++it) {
-                const int left = w.r.d.len - (w.r.page + k) * kPT;
+            for (int k = 0; ok && k < r.pages; ++k, ++it) {
+                const int left = r.d.len - (r.page + k) * kPT;
                 ahead.step();
-                const int next = ahead.block(p);  // (in flight while the scores are worked out)
-                if (ahead.ok && ahead.k == 0) fetch_queries(ahead.w.r, run + 1);
+                const int next = ahead.block();  // (in flight while the scores are worked out)
+                if (ahead.ok && ahead.k == 0) fetch_queries(ahead.r, run + 1);
                 ok = mbar_wait(&bar[0], it & 1, abort_flag, p.err);
                 auto k_read = [&] {
                     __syncwarp();
                     blk = checked(next);
                     if (ok && ahead.ok) {
-                        issue_k(blk, ahead.w.r.h);
+                        issue_k(blk, ahead.r.h);
                         ++issued_k;
                     }
                     ok = mbar_wait(&bar[1], it & 1, abort_flag, p.err) && ok;
@@ -1215,11 +1287,11 @@ __global__ void __launch_bounds__(L<RK, RV, DR, ALONE>::WARPS * 32, 1) leaf_kern
                 else leaf_page<LL, NQ>(slot, qs, ps, left, m, l, acc, k_read);
                 __syncwarp();
                 if (ok && ahead.ok) {
-                    issue_v(blk, ahead.w.r.h);
+                    issue_v(blk, ahead.r.h);
                     ++issued_v;
                 }
             }
-            float *dst = p.part + record_of(p, w.r.d, w.r.h, me) * RS;
+            float *dst = p.part + record_of(p, r.d, r.h, share) * RS;
 #pragma unroll
             for (int q = 0; q < NQ; ++q) {
                 const float sum = warp_sum(l[q]);
@@ -1247,38 +1319,64 @@ __global__ void __launch_bounds__(L<RK, RV, DR, ALONE>::WARPS * 32, 1) leaf_kern
 
 // Grid (H, ceil(B / spb)), 256 threads; SPB: the sequences that the projection is unrolled for.  W_up,t^V of the head waits in
 // shared memory, and what a sequence's nodes are in registers, when the records are there.
-constexpr int kJoinThreads = 256, kJoinCtas = 4;  // of an SM
-template <int RV>
-struct J {
-    static constexpr int WROW = RV * 2 + 16;  // bytes of a row of W_up^V, padded: rows 16 bytes apart in the banks
-    static constexpr int SMEM = kD * WROW;
-};
+__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr)
+                 : "memory");
+}
+__device__ __forceinline__ void mma_bf16_16816(float (&d)[4], const uint32_t (&a)[4], const uint32_t (&b)[2]) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
+}
+
 template <int RV, int SPB>
-__global__ void __launch_bounds__(kJoinThreads, kJoinCtas) join_kernel(const __grid_constant__ JoinParams a) {
-    constexpr int RS = record_floats(RV), NJ = (RV + 31) / 32, QUARTER = (RV / 8 + 3) / 4;  // 16-byte words of a quarter row
+__global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(const __grid_constant__ JoinParams a) {
+    using JJ = J<RV>;
+    constexpr int RS = record_floats(RV);
     extern __shared__ __align__(16) char jw[];
-    __shared__ __align__(16) float ob[SPB][RV];
-    __shared__ float coef[SPB][3];
-    __shared__ float quarters[3][SPB][kD];
+    float *rows = reinterpret_cast<float *>(jw + JJ::oO), *coef = reinterpret_cast<float *>(jw + JJ::oCoef);
     const TrunkParams &p = a.t;
-    const int h = blockIdx.x, b0 = blockIdx.y * a.spb, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    // the projection: this warp's rows 16 tile .. + 15 of the outputs of sequences 8 half .. + 7; this thread's two of either
+    const int tile = warp & 7, half = warp >> 3, e = 16 * tile + (lane >> 2), n = 8 * half + 2 * (lane & 3);
+    const bool projects = 8 * half < SPB;
+    for (int i = tid; i < kD * (JJ::RVX - RV) / 8; i += kJoinThreads) *reinterpret_cast<uint4 *>(jw + i * JJ::WROW + RV * 2) = make_uint4(0, 0, 0, 0);
+    for (int i = lane; i < JJ::OROW; i += 32) rows[warp * JJ::OROW + i] = 0.f;
+    const int groups = count_groups(p), nodes = groups + p.B;
+    const int per_head = (p.B + a.spb - 1) / a.spb, items = per_head * p.H;
+    const Split split_items(items, gridDim.x);
+    const int i0 = split_items.begin(blockIdx.x), i1 = split_items.begin(blockIdx.x + 1);
+    int head = -1;
+#pragma unroll 1
+    for (int item = i0; item < i1; ++item) {
+    const int h = item / per_head, b0 = (item - h * per_head) * a.spb;
     const int nb = min(a.spb, p.B - b0);
     const int64_t th = static_cast<int64_t>(h) * a.T + a.loop;
     auto iorow = [&](int b) { return static_cast<int64_t>(b) * p.H + h; };
-    const char *W = static_cast<const char *>(a.w_up_v) + th * kD * RV * 2;
-    for (int i = tid; i < kD * (RV / 8); i += kJoinThreads) {
-        const int e = i / (RV / 8), c = i - e * (RV / 8);
-        cp_async16(jw + e * J<RV>::WROW + c * 16, W + i * 16);
+    if (h != head) {
+        const char *W = static_cast<const char *>(a.w_up_v) + th * kD * RV * 2;
+        for (int i = tid; i < kD * (RV / 8); i += kJoinThreads) {
+            const int r = i / (RV / 8), c = i - r * (RV / 8);
+            cp_async16(jw + r * JJ::WROW + c * 16, W + i * 16);
+        }
+        cp_async_commit();
+        head = h;
     }
-    cp_async_commit();
-    const int e = tid & 63, part = tid >> 6;  // this thread's output rows e and 64 + e, and quarter of their sums
-    // G warps per sequence: warp `sub` of them takes the columns lane + 32 (sub + G j)
+    // (inputs of the call, before the wait:) what goes into this thread's outputs
+    float mu[2], cv[2][2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        mu[x] = a.mu_v ? a.mu_v[th * kD + e + 8 * x] : 0.f;
+#pragma unroll
+        for (int y = 0; y < 2; ++y) cv[x][y] = a.cur_v && n + y < nb ? load_elem(a.cur_v, iorow(b0 + n + y) * kD + e + 8 * x, a.io_bf16) : 0.f;
+    }
+    // G warps per sequence: warp `sub` of them takes the runs sub + G k
     int G = 1;
-    while (2 * G * nb <= kJoinThreads / 32) G *= 2;
+    while (2 * G * nb <= kJoinWarps) G *= 2;
     const int bi = warp / G, sub = warp - bi * G, b = b0 + min(bi, nb - 1);
-    // (inputs of the call, before the wait:) lane l < 3 knows level l's node of the sequence, lane 3 its own pages; then the
-    // current token's score
-    const int groups = count_groups(p), nodes = groups + p.B;
+    // lane l < 3 knows level l's node of the sequence, lane 3 its own pages; then the current token's score
     int node = groups + b, rank = 0;
     bool there = lane == kLevels;
     if (lane < kLevels) {
@@ -1303,32 +1401,43 @@ __global__ void __launch_bounds__(kJoinThreads, kJoinCtas) join_kernel(const __g
             qk = fmaf(load_elem(a.q_rope, row * a.d_rope + i, a.io_bf16), load_elem(a.cur_k_rope, static_cast<int64_t>(b) * a.d_rope + i, a.io_bf16), qk);
         qk = warp_sum(qk) * a.scale_log2;
     }
-    // Twice: first without a run, while the kernels before still run, so that the instructions are there when the records are
-    // (fetched behind the wait they took longer than the join).
+    // The first item twice: at first with a run of anything, and without an output, while the kernels before still run, so that the
+    // instructions are there when the records are (fetched behind the wait they took longer than the join).
 #pragma unroll 1
-    for (int dry = 1; dry >= 0; --dry) {
-    if (dry == 0) {
+    for (int dry = item == i0; dry >= 0; --dry) {
+    if (item == i0 && dry == 0) {
         pdl_wait();
         pdl_trigger();
     }
     // the runs of the nodes: records first + step i of run i
     int runs = 0, first = 0, step = 0;
-    if (there && dry == 0) {
-        const int kind = is_leaf(p, d), np = p.pstart[nodes + kind] * p.H, we = min(kind ? a.workers : a.grid, np);  // the split of find_share
-        const Split split(np, we);
-        const int s0 = p.pstart[node] * p.H + h * d.pages, c0 = split.worker(s0);
-        runs = split.worker(s0 + d.pages - 1) - c0 + 1;
+    if (there) {
+        const int *before = p.pstart + (is_leaf(p, d) ? kMaxNodes + 1 : 0);
+        const int np = before[nodes] * p.H, s0 = before[node] * p.H + h * d.pages, s1 = s0 + d.pages - 1;
+        int c0;
+        if (is_leaf(p, d)) {
+            const LeafShares shares(np, a.workers);
+            c0 = shares.share(s0);
+            runs = shares.share(s1) - c0 + 1;
+        } else {
+            const Split split(np, min(a.grid, np));  // as find_share
+            c0 = split.worker(s0);
+            runs = split.worker(s1) - c0 + 1;
+        }
         first = static_cast<int>(record_of(p, d, h, c0)) + rank;
-        step = kind ? p.leaf_max : kMembers;
+        step = is_leaf(p, d) ? p.leaf_max : kMembers;
+    }
+    if (dry) {  // (one run, the first record: whatever it holds)
+        runs = lane == kLevels;
+        first = step = 0;
     }
     int upto[kLevels + 1];  // runs of the nodes up to each
 #pragma unroll
     for (int l = 0; l <= kLevels; ++l) upto[l] = (l ? upto[l - 1] : 0) + __shfl_sync(0xffffffffu, runs, l);
     const float beta = dry ? 0.f : p.beta[iorow(b)];
-    float M = -INFINITY, l = 0.f;
-    float acc[NJ];
+    float M = -INFINITY, l = 0.f, acc[5];  // of columns 4 lane .. + 3, and 128 + lane
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) acc[j] = 0.f;
+    for (int c = 0; c < 5; ++c) acc[c] = 0.f;
     if (bi < nb) {
 #pragma unroll 1
         for (int r0 = 0; r0 < upto[kLevels]; r0 += 32) {
@@ -1342,41 +1451,45 @@ __global__ void __launch_bounds__(kJoinThreads, kJoinCtas) join_kernel(const __g
                 }
             const int rec = __shfl_sync(0xffffffffu, first, level) + in * __shfl_sync(0xffffffffu, step, level);
             const float2 ml = *reinterpret_cast<const float2 *>(p.part + static_cast<int64_t>(rec) * RS + RV);
+            constexpr int KR = 6;  // runs whose loads are in flight together, the first of them beside their maxima and sums
+            float4 v[KR];
+            float t[KR];
+            auto load = [&](int k0) {
+#pragma unroll
+                for (int k = 0; k < KR; ++k) {
+                    const float *pr = p.part + static_cast<int64_t>(__shfl_sync(0xffffffffu, rec, min(k0 + k * G, nr - 1))) * RS;
+                    v[k] = lane * 4 < RV ? *reinterpret_cast<const float4 *>(pr + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    t[k] = RV > 128 ? pr[128 + lane] : 0.f;
+                }
+            };
+            load(sub);
             const float mi = lane < nr ? ml.x : -INFINITY;
             const float Mn = fmaxf(M, warp_max(mi)), f = M == -INFINITY ? 0.f : ex2_approx(M - Mn);
             const float wi = mi == -INFINITY ? 0.f : ex2_approx(mi - Mn);
             M = Mn;
             l = fmaf(l, f, warp_sum(lane < nr ? wi * ml.y : 0.f));
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) acc[j] *= f;
-            constexpr int KR = 4;  // runs whose loads are in flight together
+            for (int c = 0; c < 5; ++c) acc[c] *= f;
 #pragma unroll 1
-            for (int k0 = 0; k0 < nr; k0 += KR) {
-                float v[KR][NJ];
+            for (int k0 = sub;;) {
 #pragma unroll
                 for (int k = 0; k < KR; ++k) {
-                    const float *pr = p.part + static_cast<int64_t>(__shfl_sync(0xffffffffu, rec, min(k0 + k, nr - 1))) * RS;
-#pragma unroll
-                    for (int j = 0; j < NJ; ++j) {
-                        const int c = lane + 32 * (sub + G * j);
-                        v[k][j] = c < RV ? pr[c] : 0.f;
+                    const float wk = __shfl_sync(0xffffffffu, wi, min(k0 + k * G, 31));
+                    if (wk != 0.f && k0 + k * G < nr) {  // warp-uniform (a NaN state stays one)
+                        acc[0] = fmaf(wk, v[k].x, acc[0]);
+                        acc[1] = fmaf(wk, v[k].y, acc[1]);
+                        acc[2] = fmaf(wk, v[k].z, acc[2]);
+                        acc[3] = fmaf(wk, v[k].w, acc[3]);
+                        if constexpr (RV > 128) acc[4] = fmaf(wk, t[k], acc[4]);
                     }
                 }
-#pragma unroll
-                for (int k = 0; k < KR; ++k) {
-                    const float wk = __shfl_sync(0xffffffffu, wi, k0 + k);  // (0 behind the last)
-                    if (wk != 0.f && k0 + k < nr) {  // warp-uniform (a NaN state stays one)
-#pragma unroll
-                        for (int j = 0; j < NJ; ++j) acc[j] = fmaf(wk, v[k][j], acc[j]);
-                    }
-                }
+                if ((k0 += KR * G) >= nr) break;
+                load(k0);
             }
         }
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const int c = lane + 32 * (sub + G * j);
-            if (c < RV) ob[bi][c] = acc[j];
-        }
+        float *row = rows + warp * JJ::OROW;  // (that of sequence bi and warp `sub` of its)
+        if (lane * 4 < RV) *reinterpret_cast<float4 *>(row + lane * 4) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+        if constexpr (RV > 128) row[128 + lane] = acc[4];
         if (sub == 0 && lane == 0) {
             M += beta;  // the same for all of a query's cached tokens
             const float Mx = fmaxf(M, qk);
@@ -1384,57 +1497,56 @@ __global__ void __launch_bounds__(kJoinThreads, kJoinCtas) join_kernel(const __g
             const float pc = a.cur_k ? ex2_approx(qk - Mx) : 0.f;
             const float den = al * l + pc;
             const float inv = den == 0.f ? 0.f : 1.f / den;
-            coef[bi][0] = al * inv;
-            coef[bi][1] = al * l * inv;
-            coef[bi][2] = pc * inv;
+            coef[bi * 4] = al * inv;
+            coef[bi * 4 + 1] = al * l * inv;
+            coef[bi * 4 + 2] = pc * inv;
         }
     }
-    for (int i = tid; i < (SPB - nb) * RV; i += kJoinThreads) ob[nb + i / RV][i % RV] = 0.f;
     cp_async_wait_all();
     __syncthreads();
-    // out_b[e] = coef0 (W_up^V o~_b)[e] + coef1 mu^V[e] + coef2 v_cur,b[e], the sum of a row in four quarters
-    float sum[2][SPB];
-#pragma unroll
-    for (int i = 0; i < SPB; ++i) sum[0][i] = sum[1][i] = 0.f;
-    const char *wrow = jw + e * J<RV>::WROW;
-#pragma unroll 1
-    for (int j = part * QUARTER; j < min((part + 1) * QUARTER, RV / 8); ++j) {
-        const uint4 wa = *reinterpret_cast<const uint4 *>(wrow + j * 16), wb = *reinterpret_cast<const uint4 *>(wrow + 64 * J<RV>::WROW + j * 16);
-        const float2 a0 = bf2_to_f2(wa.x), a1 = bf2_to_f2(wa.y), a2 = bf2_to_f2(wa.z), a3 = bf2_to_f2(wa.w);
-        const float2 c0 = bf2_to_f2(wb.x), c1 = bf2_to_f2(wb.y), c2 = bf2_to_f2(wb.z), c3 = bf2_to_f2(wb.w);
-#pragma unroll
-        for (int i = 0; i < SPB; ++i) {
-            const float4 o0 = *reinterpret_cast<const float4 *>(&ob[i][j * 8]);
-            const float4 o1 = *reinterpret_cast<const float4 *>(&ob[i][j * 8 + 4]);
-            sum[0][i] = fmaf(a3.y, o1.w, fmaf(a3.x, o1.z, fmaf(a2.y, o1.y, fmaf(a2.x, o1.x, fmaf(a1.y, o0.w, fmaf(a1.x, o0.z, fmaf(a0.y, o0.y, fmaf(a0.x, o0.x, sum[0][i]))))))));
-            sum[1][i] = fmaf(c3.y, o1.w, fmaf(c3.x, o1.z, fmaf(c2.y, o1.y, fmaf(c2.x, o1.x, fmaf(c1.y, o0.w, fmaf(c1.x, o0.z, fmaf(c0.y, o0.y, fmaf(c0.x, o0.x, sum[1][i]))))))));
+    if (G > 1) {
+        for (int i = tid; i < nb * RV; i += kJoinThreads) {
+            const int q = i / RV, c = i - q * RV;
+            float o = rows[q * G * JJ::OROW + c];
+            for (int k = 1; k < G; ++k) o += rows[(q * G + k) * JJ::OROW + c];
+            rows[q * G * JJ::OROW + c] = o;
         }
+        __syncthreads();
     }
-    if (part > 0) {
+    // out_b[e] = coef0 (W_up^V o~_b)[e] + coef1 mu^V[e] + coef2 v_cur,b[e]; the product with o~ as three bf16 parts (24 bits), the
+    // small ones in sums of their own.  (On CUDA cores it was bound by the reads of o~ from shared memory: 6 us for 16 sequences.)
+    if (projects) {
+        float big[4] = {0.f, 0.f, 0.f, 0.f}, small[4] = {0.f, 0.f, 0.f, 0.f};
+        const uint32_t wa = smem_addr(jw) + (16 * tile + (lane & 15)) * JJ::WROW + (lane >> 4) * 16;
+        const float *o = rows + min(8 * half + (lane >> 2), nb - 1) * G * JJ::OROW + 2 * (lane & 3);
+#pragma unroll 2
+        for (int ks = 0; ks < JJ::RVX / 16; ++ks) {
+            uint32_t w[4], q[3][2];
+            ldmatrix_x4(w, wa + ks * 32);
 #pragma unroll
-        for (int i = 0; i < SPB; ++i) {
-            quarters[part - 1][i][e] = sum[0][i];
-            quarters[part - 1][i][64 + e] = sum[1][i];
+            for (int x = 0; x < 2; ++x) {
+                const float2 u = *reinterpret_cast<const float2 *>(o + ks * 16 + 8 * x);
+                q[0][x] = pack_bf16x2(u.x, u.y);
+                const float2 f = bf2_to_f2(q[0][x]);
+                q[1][x] = pack_bf16x2(u.x - f.x, u.y - f.y);
+                const float2 g = bf2_to_f2(q[1][x]);
+                q[2][x] = pack_bf16x2(u.x - f.x - g.x, u.y - f.y - g.y);
+            }
+            mma_bf16_16816(small, w, q[2]);
+            mma_bf16_16816(small, w, q[1]);
+            mma_bf16_16816(big, w, q[0]);
         }
-    }
-    __syncthreads();
-    if (part == 0 && dry == 0) {
 #pragma unroll
-        for (int i = 0; i < SPB; ++i) {
-            quarters[0][i][e] = (sum[0][i] + quarters[0][i][e]) + (quarters[1][i][e] + quarters[2][i][e]);
-            quarters[0][i][64 + e] = (sum[1][i] + quarters[0][i][64 + e]) + (quarters[1][i][64 + e] + quarters[2][i][64 + e]);
-        }
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                if (dry || n + y >= nb) continue;
+                const float *cf = coef + (n + y) * 4;
+                const float v = fmaf(cf[2], cv[x][y], fmaf(cf[1], mu[x], (big[2 * x + y] + small[2 * x + y]) * cf[0]));
+                store_elem(a.out, iorow(b0 + n + y) * kD + e + 8 * x, v, a.io_bf16);
+            }
     }
-    __syncthreads();
-    if (dry == 0) {
-        for (int o = tid; o < nb * kD; o += kJoinThreads) {
-            const int i = o / kD, r = o % kD;
-            const int64_t at = iorow(b0 + i) * kD + r;
-            float v = quarters[0][i][r] * coef[i][0];
-            if (a.mu_v) v = fmaf(coef[i][1], a.mu_v[th * kD + r], v);
-            if (a.cur_v) v = fmaf(coef[i][2], load_elem(a.cur_v, at, a.io_bf16), v);
-            store_elem(a.out, at, v, a.io_bf16);
-        }
+    __syncthreads();  // o~, the coefficients and the weights are free
     }
     }
 }
@@ -1451,13 +1563,13 @@ inline size_t al256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 PrefixWorkspace prefix_workspace(int rkt, int r_v, int B, int H, int grid) {
     PrefixWorkspace w;
     w.leaf = static_cast<size_t>(H) * kLevels * B + static_cast<size_t>(kMembers) * grid;
-    const size_t records = w.leaf + static_cast<size_t>(H) * (kLevels + 1) * B + static_cast<size_t>(kLeafAlone) * kMaxWarps * grid;
+    const size_t records = w.leaf + static_cast<size_t>(H) * (kLevels + 1) * B + static_cast<size_t>(kLeafAlone) * (1 + kLeafRest) * kMaxWarps * grid;
     w.part = 0;
     w.qt = al256(records * record_floats(r_v) * sizeof(float));
     w.qf = w.qt + al256(static_cast<size_t>(B) * H * 3 * rkt * sizeof(uint16_t));
     w.beta = w.qf + al256(static_cast<size_t>(B) * H * rkt * sizeof(float));
     w.pstart = w.beta + al256(static_cast<size_t>(B) * H * sizeof(float));
-    w.total = w.pstart + al256((kMaxNodes + 2) * sizeof(int));
+    w.total = w.pstart + al256((2 * (kMaxNodes + 1) + 1) * sizeof(int));
     return w;
 }
 
@@ -1478,8 +1590,8 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     using LL = L<RK, RV, DR, false>;
     using LA = L<RK, RV, DR, true>;
     static DeviceOnce configured, configured_leaf, configured_alone;
-    if (raise_smem_limit(leaf_kernel<RK, RV, DR, false>, LL::SMEM, configured_leaf) != LLA_OK) return LLA_ERR_CUDA;
-    if (raise_smem_limit(leaf_kernel<RK, RV, DR, true>, LA::SMEM, configured_alone) != LLA_OK) return LLA_ERR_CUDA;
+    if (raise_smem_limit(leaf_kernel<RK, RV, DR, false>, LL::SMEM, configured_leaf, true) != LLA_OK) return LLA_ERR_CUDA;
+    if (raise_smem_limit(leaf_kernel<RK, RV, DR, true>, LA::SMEM, configured_alone, true) != LLA_OK) return LLA_ERR_CUDA;
     if (raise_smem_limit(trunk_kernel<RK, RV, DR, THIRD>, ZZ::SMEM, configured) != LLA_OK) return LLA_ERR_CUDA;
     const int64_t page_bytes = static_cast<int64_t>(head_page_bytes(RK, RV, 2));
     // the V-planes of every page: [num_blocks * H][64 tokens][r_v] bf16
@@ -1501,6 +1613,7 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     tp.beta = reinterpret_cast<float *>(ws + w.beta);
     tp.part = reinterpret_cast<float *>(ws + w.part);
     tp.pstart = reinterpret_cast<int *>(ws + w.pstart);
+    tp.next = tp.pstart + 2 * (kMaxNodes + 1);
     tp.leaf = static_cast<int64_t>(w.leaf);
     // No group of up to four sequences has more members than the leaf kernel can take: no trunk kernel then (four sequences over
     // 768 tokens 25.5 -> 24.1 us).  Beside one, nodes of three and four queries are faster in it: 64 sequences over 16 prompts
@@ -1536,19 +1649,19 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     jp.w_up_v = a.w_up_v; jp.mu_v = a.mu_v;
     jp.q = a.q; jp.q_rope = q_rope; jp.cur_k = a.cur_k; jp.cur_v = a.cur_v; jp.cur_k_rope = cur_k_rope;
     jp.out = a.out;
-    // all of its CTAs at once on the SMs: fewer sequences per CTA for small batches
-    const int64_t units = static_cast<int64_t>(a.B) * a.H;
-    jp.spb = static_cast<int>(std::min<int64_t>(kJoinSeqs, std::max<int64_t>(1, (units + kJoinCtas * grid - 1) / (kJoinCtas * grid))));
-    const dim3 jg(a.H, (a.B + jp.spb - 1) / jp.spb);
+    // one CTA per SM: as many sequences together as leave no CTA two items, where that can be
+    const auto items = [&](int spb) { return static_cast<int64_t>(a.H) * ((a.B + spb - 1) / spb); };
+    jp.spb = 1;
+    while (jp.spb < kJoinSeqs && items(jp.spb) > grid) ++jp.spb;
+    const dim3 jg(static_cast<unsigned>(std::min<int64_t>(grid, items(jp.spb))));
     auto join = [&](auto spb) {
         constexpr int SPB = decltype(spb)::value;
         static DeviceOnce configured_join;
-        if (raise_smem_limit(join_kernel<RV, SPB>, J<RV>::SMEM, configured_join) != LLA_OK) return LLA_ERR_CUDA;
+        if (raise_smem_limit(join_kernel<RV, SPB>, J<RV>::SMEM, configured_join, true) != LLA_OK) return LLA_ERR_CUDA;
         return launch_ex(join_kernel<RV, SPB>, jg, kJoinThreads, J<RV>::SMEM, stream, jp);
     };
-    if (jp.spb <= 2) return join(std::integral_constant<int, 2>());
-    if (jp.spb <= 4) return join(std::integral_constant<int, 4>());
-    return join(std::integral_constant<int, 8>());
+    if (jp.spb <= 8) return join(std::integral_constant<int, 8>());
+    return join(std::integral_constant<int, 16>());
 }
 
 }  // namespace

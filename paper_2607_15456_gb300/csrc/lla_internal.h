@@ -215,12 +215,14 @@ struct DeviceOnce {
 // Raises the dynamic shared-memory limit of `kern` to `bytes` on the current device, once per
 // device (a flag in `once`).
 template <typename K>
-inline lla_status raise_smem_limit(K kern, int bytes, DeviceOnce &once) {
+inline lla_status raise_smem_limit(K kern, int bytes, DeviceOnce &once, bool share_sm = false) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return LLA_ERR_CUDA;
     const bool cached = dev >= 0 && dev < 64;
     if (cached && once.done[dev].load(std::memory_order_acquire)) return LLA_OK;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess)
+        return LLA_ERR_CUDA;
+    if (share_sm && cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) != cudaSuccess)
         return LLA_ERR_CUDA;
     if (cached) once.done[dev].store(true, std::memory_order_release);
     return LLA_OK;
