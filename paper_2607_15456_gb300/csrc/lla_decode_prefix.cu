@@ -48,7 +48,6 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "lla_device.cuh"
 #include "lla_internal.h"
@@ -1317,8 +1316,6 @@ __global__ void __maxnreg__(ALONE ? 160 : 120) leaf_kernel(const __grid_constant
 
 // ------------------------------------------------------------------------------------------- join kernel
 
-// Grid (H, ceil(B / spb)), 256 threads; SPB: the sequences that the projection is unrolled for.  W_up,t^V of the head waits in
-// shared memory, and what a sequence's nodes are in registers, when the records are there.
 __device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
@@ -1331,7 +1328,10 @@ __device__ __forceinline__ void mma_bf16_16816(float (&d)[4], const uint32_t (&a
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
 
-template <int RV, int SPB>
+// An item is a head with up to spb sequences, of which a CTA (one per SM) has an even share; with one item or more each, spb is as
+// small as that leaves it.  W_up,t^V of the head waits in shared memory, and what a sequence's nodes are in registers, when the
+// records are there.  64 registers: as many as leave room beside the leaf kernel.
+template <int RV>
 __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(const __grid_constant__ JoinParams a) {
     using JJ = J<RV>;
     constexpr int RS = record_floats(RV);
@@ -1341,7 +1341,6 @@ __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(const __grid_cons
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     // the projection: this warp's rows 16 tile .. + 15 of the outputs of sequences 8 half .. + 7; this thread's two of either
     const int tile = warp & 7, half = warp >> 3, e = 16 * tile + (lane >> 2), n = 8 * half + 2 * (lane & 3);
-    const bool projects = 8 * half < SPB;
     for (int i = tid; i < kD * (JJ::RVX - RV) / 8; i += kJoinThreads) *reinterpret_cast<uint4 *>(jw + i * JJ::WROW + RV * 2) = make_uint4(0, 0, 0, 0);
     for (int i = lane; i < JJ::OROW; i += 32) rows[warp * JJ::OROW + i] = 0.f;
     const int groups = count_groups(p), nodes = groups + p.B;
@@ -1351,203 +1350,203 @@ __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(const __grid_cons
     int head = -1;
 #pragma unroll 1
     for (int item = i0; item < i1; ++item) {
-    const int h = item / per_head, b0 = (item - h * per_head) * a.spb;
-    const int nb = min(a.spb, p.B - b0);
-    const int64_t th = static_cast<int64_t>(h) * a.T + a.loop;
-    auto iorow = [&](int b) { return static_cast<int64_t>(b) * p.H + h; };
-    if (h != head) {
-        const char *W = static_cast<const char *>(a.w_up_v) + th * kD * RV * 2;
-        for (int i = tid; i < kD * (RV / 8); i += kJoinThreads) {
-            const int r = i / (RV / 8), c = i - r * (RV / 8);
-            cp_async16(jw + r * JJ::WROW + c * 16, W + i * 16);
+        const int h = item / per_head, b0 = (item - h * per_head) * a.spb;
+        const int nb = min(a.spb, p.B - b0);
+        const int64_t th = static_cast<int64_t>(h) * a.T + a.loop;
+        auto iorow = [&](int b) { return static_cast<int64_t>(b) * p.H + h; };
+        if (h != head) {
+            const char *W = static_cast<const char *>(a.w_up_v) + th * kD * RV * 2;
+            for (int i = tid; i < kD * (RV / 8); i += kJoinThreads) {
+                const int r = i / (RV / 8), c = i - r * (RV / 8);
+                cp_async16(jw + r * JJ::WROW + c * 16, W + i * 16);
+            }
+            cp_async_commit();
+            head = h;
         }
-        cp_async_commit();
-        head = h;
-    }
-    // (inputs of the call, before the wait:) what goes into this thread's outputs
-    float mu[2], cv[2][2];
+        // (inputs of the call, before the wait:) what goes into this thread's outputs
+        float mu[2], cv[2][2];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        mu[x] = a.mu_v ? a.mu_v[th * kD + e + 8 * x] : 0.f;
+        for (int x = 0; x < 2; ++x) {
+            mu[x] = a.mu_v ? a.mu_v[th * kD + e + 8 * x] : 0.f;
 #pragma unroll
-        for (int y = 0; y < 2; ++y) cv[x][y] = a.cur_v && n + y < nb ? load_elem(a.cur_v, iorow(b0 + n + y) * kD + e + 8 * x, a.io_bf16) : 0.f;
-    }
-    // G warps per sequence: warp `sub` of them takes the runs sub + G k
-    int G = 1;
-    while (2 * G * nb <= kJoinWarps) G *= 2;
-    const int bi = warp / G, sub = warp - bi * G, b = b0 + min(bi, nb - 1);
-    // lane l < 3 knows level l's node of the sequence, lane 3 its own pages; then the current token's score
-    int node = groups + b, rank = 0;
-    bool there = lane == kLevels;
-    if (lane < kLevels) {
-        const int col = p.plan.column[static_cast<int64_t>(lane) * p.B + b];
-        there = col >= 0 && col / kMembers < groups;
-        if (there) {
-            node = col / kMembers;
-            rank = col % kMembers;
+            for (int y = 0; y < 2; ++y) cv[x][y] = a.cur_v && n + y < nb ? load_elem(a.cur_v, iorow(b0 + n + y) * kD + e + 8 * x, a.io_bf16) : 0.f;
         }
-    }
-    Node d = {0, 0, 0, 0, 0, 0};
-    if (there) d = node_at(p, groups, node);
-    there = d.pages > 0 && rank < d.n;
-    float qk = -INFINITY;
-    if (a.cur_k) {
-        const int64_t row = iorow(b);
-        qk = 0.f;
+        // G warps per sequence: warp `sub` of them takes the runs sub + G k
+        int G = 1;
+        while (2 * G * nb <= kJoinWarps) G *= 2;
+        const int bi = warp / G, sub = warp - bi * G, b = b0 + min(bi, nb - 1);
+        // lane l < 3 knows level l's node of the sequence, lane 3 its own pages; then the current token's score
+        int node = groups + b, rank = 0;
+        bool there = lane == kLevels;
+        if (lane < kLevels) {
+            const int col = p.plan.column[static_cast<int64_t>(lane) * p.B + b];
+            there = col >= 0 && col / kMembers < groups;
+            if (there) {
+                node = col / kMembers;
+                rank = col % kMembers;
+            }
+        }
+        Node d = {0, 0, 0, 0, 0, 0};
+        if (there) d = node_at(p, groups, node);
+        there = d.pages > 0 && rank < d.n;
+        float qk = -INFINITY;
+        if (a.cur_k) {
+            const int64_t row = iorow(b);
+            qk = 0.f;
 #pragma unroll
-        for (int i = 0; i < kD / 32; ++i)
-            qk = fmaf(load_elem(a.q, row * kD + lane + 32 * i, a.io_bf16), load_elem(a.cur_k, row * kD + lane + 32 * i, a.io_bf16), qk);
-        for (int i = lane; i < a.d_rope; i += 32)  // both stand at one position: the rotation cancels
-            qk = fmaf(load_elem(a.q_rope, row * a.d_rope + i, a.io_bf16), load_elem(a.cur_k_rope, static_cast<int64_t>(b) * a.d_rope + i, a.io_bf16), qk);
-        qk = warp_sum(qk) * a.scale_log2;
-    }
-    // The first item twice: at first with a run of anything, and without an output, while the kernels before still run, so that the
-    // instructions are there when the records are (fetched behind the wait they took longer than the join).
+            for (int i = 0; i < kD / 32; ++i)
+                qk = fmaf(load_elem(a.q, row * kD + lane + 32 * i, a.io_bf16), load_elem(a.cur_k, row * kD + lane + 32 * i, a.io_bf16), qk);
+            for (int i = lane; i < a.d_rope; i += 32)  // both stand at one position: the rotation cancels
+                qk = fmaf(load_elem(a.q_rope, row * a.d_rope + i, a.io_bf16), load_elem(a.cur_k_rope, static_cast<int64_t>(b) * a.d_rope + i, a.io_bf16), qk);
+            qk = warp_sum(qk) * a.scale_log2;
+        }
+        // The first item twice: at first with a run of anything, and without an output, while the kernels before still run, so that the
+        // instructions are there when the records are (fetched behind the wait they took longer than the join).
 #pragma unroll 1
-    for (int dry = item == i0; dry >= 0; --dry) {
-    if (item == i0 && dry == 0) {
-        pdl_wait();
-        pdl_trigger();
-    }
-    // the runs of the nodes: records first + step i of run i
-    int runs = 0, first = 0, step = 0;
-    if (there) {
-        const int *before = p.pstart + (is_leaf(p, d) ? kMaxNodes + 1 : 0);
-        const int np = before[nodes] * p.H, s0 = before[node] * p.H + h * d.pages, s1 = s0 + d.pages - 1;
-        int c0;
-        if (is_leaf(p, d)) {
-            const LeafShares shares(np, a.workers);
-            c0 = shares.share(s0);
-            runs = shares.share(s1) - c0 + 1;
-        } else {
-            const Split split(np, min(a.grid, np));  // as find_share
-            c0 = split.worker(s0);
-            runs = split.worker(s1) - c0 + 1;
-        }
-        first = static_cast<int>(record_of(p, d, h, c0)) + rank;
-        step = is_leaf(p, d) ? p.leaf_max : kMembers;
-    }
-    if (dry) {  // (one run, the first record: whatever it holds)
-        runs = lane == kLevels;
-        first = step = 0;
-    }
-    int upto[kLevels + 1];  // runs of the nodes up to each
-#pragma unroll
-    for (int l = 0; l <= kLevels; ++l) upto[l] = (l ? upto[l - 1] : 0) + __shfl_sync(0xffffffffu, runs, l);
-    const float beta = dry ? 0.f : p.beta[iorow(b)];
-    float M = -INFINITY, l = 0.f, acc[5];  // of columns 4 lane .. + 3, and 128 + lane
-#pragma unroll
-    for (int c = 0; c < 5; ++c) acc[c] = 0.f;
-    if (bi < nb) {
-#pragma unroll 1
-        for (int r0 = 0; r0 < upto[kLevels]; r0 += 32) {
-            const int nr = min(32, upto[kLevels] - r0), r = r0 + min(lane, nr - 1);
-            int level = 0, in = r;
-#pragma unroll
-            for (int k = 0; k < kLevels; ++k)
-                if (r >= upto[k]) {
-                    level = k + 1;
-                    in = r - upto[k];
+        for (int dry = item == i0; dry >= 0; --dry) {
+            if (item == i0 && dry == 0) {
+                pdl_wait();
+                pdl_trigger();
+            }
+            // the runs of the nodes: records first + step i of run i
+            int runs = 0, first = 0, step = 0;
+            if (there) {
+                const int *before = p.pstart + (is_leaf(p, d) ? kMaxNodes + 1 : 0);
+                const int np = before[nodes] * p.H, s0 = before[node] * p.H + h * d.pages, s1 = s0 + d.pages - 1;
+                int c0;
+                if (is_leaf(p, d)) {
+                    const LeafShares shares(np, a.workers);
+                    c0 = shares.share(s0);
+                    runs = shares.share(s1) - c0 + 1;
+                } else {
+                    const Split split(np, min(a.grid, np));  // as find_share
+                    c0 = split.worker(s0);
+                    runs = split.worker(s1) - c0 + 1;
                 }
-            const int rec = __shfl_sync(0xffffffffu, first, level) + in * __shfl_sync(0xffffffffu, step, level);
-            const float2 ml = *reinterpret_cast<const float2 *>(p.part + static_cast<int64_t>(rec) * RS + RV);
-            constexpr int KR = 6;  // runs whose loads are in flight together, the first of them beside their maxima and sums
-            float4 v[KR];
-            float t[KR];
-            auto load = [&](int k0) {
+                first = static_cast<int>(record_of(p, d, h, c0)) + rank;
+                step = is_leaf(p, d) ? p.leaf_max : kMembers;
+            }
+            if (dry) {  // (one run, the first record: whatever it holds)
+                runs = lane == kLevels;
+                first = step = 0;
+            }
+            int upto[kLevels + 1];  // runs of the nodes up to each
 #pragma unroll
-                for (int k = 0; k < KR; ++k) {
-                    const float *pr = p.part + static_cast<int64_t>(__shfl_sync(0xffffffffu, rec, min(k0 + k * G, nr - 1))) * RS;
-                    v[k] = lane * 4 < RV ? *reinterpret_cast<const float4 *>(pr + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
-                    t[k] = RV > 128 ? pr[128 + lane] : 0.f;
-                }
-            };
-            load(sub);
-            const float mi = lane < nr ? ml.x : -INFINITY;
-            const float Mn = fmaxf(M, warp_max(mi)), f = M == -INFINITY ? 0.f : ex2_approx(M - Mn);
-            const float wi = mi == -INFINITY ? 0.f : ex2_approx(mi - Mn);
-            M = Mn;
-            l = fmaf(l, f, warp_sum(lane < nr ? wi * ml.y : 0.f));
+            for (int l = 0; l <= kLevels; ++l) upto[l] = (l ? upto[l - 1] : 0) + __shfl_sync(0xffffffffu, runs, l);
+            const float beta = dry ? 0.f : p.beta[iorow(b)];
+            float M = -INFINITY, l = 0.f, acc[5];  // of columns 4 lane .. + 3, and 128 + lane
 #pragma unroll
-            for (int c = 0; c < 5; ++c) acc[c] *= f;
+            for (int c = 0; c < 5; ++c) acc[c] = 0.f;
+            if (bi < nb) {
 #pragma unroll 1
-            for (int k0 = sub;;) {
+                for (int r0 = 0; r0 < upto[kLevels]; r0 += 32) {
+                    const int nr = min(32, upto[kLevels] - r0), r = r0 + min(lane, nr - 1);
+                    int level = 0, in = r;
 #pragma unroll
-                for (int k = 0; k < KR; ++k) {
-                    const float wk = __shfl_sync(0xffffffffu, wi, min(k0 + k * G, 31));
-                    if (wk != 0.f && k0 + k * G < nr) {  // warp-uniform (a NaN state stays one)
-                        acc[0] = fmaf(wk, v[k].x, acc[0]);
-                        acc[1] = fmaf(wk, v[k].y, acc[1]);
-                        acc[2] = fmaf(wk, v[k].z, acc[2]);
-                        acc[3] = fmaf(wk, v[k].w, acc[3]);
-                        if constexpr (RV > 128) acc[4] = fmaf(wk, t[k], acc[4]);
+                    for (int k = 0; k < kLevels; ++k)
+                        if (r >= upto[k]) {
+                            level = k + 1;
+                            in = r - upto[k];
+                        }
+                    const int rec = __shfl_sync(0xffffffffu, first, level) + in * __shfl_sync(0xffffffffu, step, level);
+                    const float2 ml = *reinterpret_cast<const float2 *>(p.part + static_cast<int64_t>(rec) * RS + RV);
+                    constexpr int KR = 6;  // runs whose loads are in flight together, the first of them beside their maxima and sums
+                    float4 v[KR];
+                    float t[KR];
+                    auto load = [&](int k0) {
+#pragma unroll
+                        for (int k = 0; k < KR; ++k) {
+                            const float *pr = p.part + static_cast<int64_t>(__shfl_sync(0xffffffffu, rec, min(k0 + k * G, nr - 1))) * RS;
+                            v[k] = lane * 4 < RV ? *reinterpret_cast<const float4 *>(pr + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+                            t[k] = RV > 128 ? pr[128 + lane] : 0.f;
+                        }
+                    };
+                    load(sub);
+                    const float mi = lane < nr ? ml.x : -INFINITY;
+                    const float Mn = fmaxf(M, warp_max(mi)), f = M == -INFINITY ? 0.f : ex2_approx(M - Mn);
+                    const float wi = mi == -INFINITY ? 0.f : ex2_approx(mi - Mn);
+                    M = Mn;
+                    l = fmaf(l, f, warp_sum(lane < nr ? wi * ml.y : 0.f));
+#pragma unroll
+                    for (int c = 0; c < 5; ++c) acc[c] *= f;
+#pragma unroll 1
+                    for (int k0 = sub;;) {
+#pragma unroll
+                        for (int k = 0; k < KR; ++k) {
+                            const float wk = __shfl_sync(0xffffffffu, wi, min(k0 + k * G, 31));
+                            if (wk != 0.f && k0 + k * G < nr) {  // warp-uniform (a NaN state stays one)
+                                acc[0] = fmaf(wk, v[k].x, acc[0]);
+                                acc[1] = fmaf(wk, v[k].y, acc[1]);
+                                acc[2] = fmaf(wk, v[k].z, acc[2]);
+                                acc[3] = fmaf(wk, v[k].w, acc[3]);
+                                if constexpr (RV > 128) acc[4] = fmaf(wk, t[k], acc[4]);
+                            }
+                        }
+                        if ((k0 += KR * G) >= nr) break;
+                        load(k0);
                     }
                 }
-                if ((k0 += KR * G) >= nr) break;
-                load(k0);
+                float *row = rows + warp * JJ::OROW;  // (that of sequence bi and warp `sub` of its)
+                if (lane * 4 < RV) *reinterpret_cast<float4 *>(row + lane * 4) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+                if constexpr (RV > 128) row[128 + lane] = acc[4];
+                if (sub == 0 && lane == 0) {
+                    M += beta;  // the same for all of a query's cached tokens
+                    const float Mx = fmaxf(M, qk);
+                    const float al = M == -INFINITY ? 0.f : ex2_approx(M - Mx);
+                    const float pc = a.cur_k ? ex2_approx(qk - Mx) : 0.f;
+                    const float den = al * l + pc;
+                    const float inv = den == 0.f ? 0.f : 1.f / den;
+                    coef[bi * 4] = al * inv;
+                    coef[bi * 4 + 1] = al * l * inv;
+                    coef[bi * 4 + 2] = pc * inv;
+                }
             }
-        }
-        float *row = rows + warp * JJ::OROW;  // (that of sequence bi and warp `sub` of its)
-        if (lane * 4 < RV) *reinterpret_cast<float4 *>(row + lane * 4) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-        if constexpr (RV > 128) row[128 + lane] = acc[4];
-        if (sub == 0 && lane == 0) {
-            M += beta;  // the same for all of a query's cached tokens
-            const float Mx = fmaxf(M, qk);
-            const float al = M == -INFINITY ? 0.f : ex2_approx(M - Mx);
-            const float pc = a.cur_k ? ex2_approx(qk - Mx) : 0.f;
-            const float den = al * l + pc;
-            const float inv = den == 0.f ? 0.f : 1.f / den;
-            coef[bi * 4] = al * inv;
-            coef[bi * 4 + 1] = al * l * inv;
-            coef[bi * 4 + 2] = pc * inv;
-        }
-    }
-    cp_async_wait_all();
-    __syncthreads();
-    if (G > 1) {
-        for (int i = tid; i < nb * RV; i += kJoinThreads) {
-            const int q = i / RV, c = i - q * RV;
-            float o = rows[q * G * JJ::OROW + c];
-            for (int k = 1; k < G; ++k) o += rows[(q * G + k) * JJ::OROW + c];
-            rows[q * G * JJ::OROW + c] = o;
-        }
-        __syncthreads();
-    }
-    // out_b[e] = coef0 (W_up^V o~_b)[e] + coef1 mu^V[e] + coef2 v_cur,b[e]; the product with o~ as three bf16 parts (24 bits), the
-    // small ones in sums of their own.  (On CUDA cores it was bound by the reads of o~ from shared memory: 6 us for 16 sequences.)
-    if (projects) {
-        float big[4] = {0.f, 0.f, 0.f, 0.f}, small[4] = {0.f, 0.f, 0.f, 0.f};
-        const uint32_t wa = smem_addr(jw) + (16 * tile + (lane & 15)) * JJ::WROW + (lane >> 4) * 16;
-        const float *o = rows + min(8 * half + (lane >> 2), nb - 1) * G * JJ::OROW + 2 * (lane & 3);
+            cp_async_wait_all();
+            __syncthreads();
+            if (G > 1) {
+                for (int i = tid; i < nb * RV; i += kJoinThreads) {
+                    const int q = i / RV, c = i - q * RV;
+                    float o = rows[q * G * JJ::OROW + c];
+                    for (int k = 1; k < G; ++k) o += rows[(q * G + k) * JJ::OROW + c];
+                    rows[q * G * JJ::OROW + c] = o;
+                }
+                __syncthreads();
+            }
+            // out_b[e] = coef0 (W_up^V o~_b)[e] + coef1 mu^V[e] + coef2 v_cur,b[e]; the product with o~ as three bf16 parts (24 bits), the
+            // small ones in sums of their own.  (On CUDA cores it was bound by the reads of o~ from shared memory: 6 us for 16 sequences.)
+            if (8 * half < nb) {
+                float big[4] = {0.f, 0.f, 0.f, 0.f}, small[4] = {0.f, 0.f, 0.f, 0.f};
+                const uint32_t wa = smem_addr(jw) + (16 * tile + (lane & 15)) * JJ::WROW + (lane >> 4) * 16;
+                const float *o = rows + min(8 * half + (lane >> 2), nb - 1) * G * JJ::OROW + 2 * (lane & 3);
 #pragma unroll 2
-        for (int ks = 0; ks < JJ::RVX / 16; ++ks) {
-            uint32_t w[4], q[3][2];
-            ldmatrix_x4(w, wa + ks * 32);
+                for (int ks = 0; ks < JJ::RVX / 16; ++ks) {
+                    uint32_t w[4], q[3][2];
+                    ldmatrix_x4(w, wa + ks * 32);
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const float2 u = *reinterpret_cast<const float2 *>(o + ks * 16 + 8 * x);
-                q[0][x] = pack_bf16x2(u.x, u.y);
-                const float2 f = bf2_to_f2(q[0][x]);
-                q[1][x] = pack_bf16x2(u.x - f.x, u.y - f.y);
-                const float2 g = bf2_to_f2(q[1][x]);
-                q[2][x] = pack_bf16x2(u.x - f.x - g.x, u.y - f.y - g.y);
+                    for (int x = 0; x < 2; ++x) {
+                        const float2 u = *reinterpret_cast<const float2 *>(o + ks * 16 + 8 * x);
+                        q[0][x] = pack_bf16x2(u.x, u.y);
+                        const float2 f = bf2_to_f2(q[0][x]);
+                        q[1][x] = pack_bf16x2(u.x - f.x, u.y - f.y);
+                        const float2 g = bf2_to_f2(q[1][x]);
+                        q[2][x] = pack_bf16x2(u.x - f.x - g.x, u.y - f.y - g.y);
+                    }
+                    mma_bf16_16816(small, w, q[2]);
+                    mma_bf16_16816(small, w, q[1]);
+                    mma_bf16_16816(big, w, q[0]);
+                }
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        if (dry || n + y >= nb) continue;
+                        const float *cf = coef + (n + y) * 4;
+                        const float v = fmaf(cf[2], cv[x][y], fmaf(cf[1], mu[x], (big[2 * x + y] + small[2 * x + y]) * cf[0]));
+                        store_elem(a.out, iorow(b0 + n + y) * kD + e + 8 * x, v, a.io_bf16);
+                    }
             }
-            mma_bf16_16816(small, w, q[2]);
-            mma_bf16_16816(small, w, q[1]);
-            mma_bf16_16816(big, w, q[0]);
+            __syncthreads();  // o~, the coefficients and the weights are free
         }
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int y = 0; y < 2; ++y) {
-                if (dry || n + y >= nb) continue;
-                const float *cf = coef + (n + y) * 4;
-                const float v = fmaf(cf[2], cv[x][y], fmaf(cf[1], mu[x], (big[2 * x + y] + small[2 * x + y]) * cf[0]));
-                store_elem(a.out, iorow(b0 + n + y) * kD + e + 8 * x, v, a.io_bf16);
-            }
-    }
-    __syncthreads();  // o~, the coefficients and the weights are free
-    }
     }
 }
 
@@ -1654,14 +1653,9 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     jp.spb = 1;
     while (jp.spb < kJoinSeqs && items(jp.spb) > grid) ++jp.spb;
     const dim3 jg(static_cast<unsigned>(std::min<int64_t>(grid, items(jp.spb))));
-    auto join = [&](auto spb) {
-        constexpr int SPB = decltype(spb)::value;
-        static DeviceOnce configured_join;
-        if (raise_smem_limit(join_kernel<RV, SPB>, J<RV>::SMEM, configured_join, true) != LLA_OK) return LLA_ERR_CUDA;
-        return launch_ex(join_kernel<RV, SPB>, jg, kJoinThreads, J<RV>::SMEM, stream, jp);
-    };
-    if (jp.spb <= 8) return join(std::integral_constant<int, 8>());
-    return join(std::integral_constant<int, 16>());
+    static DeviceOnce configured_join;
+    if (raise_smem_limit(join_kernel<RV>, J<RV>::SMEM, configured_join, true) != LLA_OK) return LLA_ERR_CUDA;
+    return launch_ex(join_kernel<RV>, jg, kJoinThreads, J<RV>::SMEM, stream, jp);
 }
 
 }  // namespace

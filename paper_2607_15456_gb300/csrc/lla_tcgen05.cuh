@@ -316,37 +316,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return a | (b << 16);
 }
 
-// 16 lanes x 8 columns at each of three addresses, and 16 lanes x 32 columns, from the lanes at `t*` (warp-collective) in
-// the 16x256b fragment layout, waited for: r[p][4k], r[p][4k+1] = lane t/4, columns 8k + 2(t%4) and 8k + 2(t%4) + 1 of
-// address p, r[p][4k+2], r[p][4k+3] = the same columns of lane t/4 + 8.
-__device__ __forceinline__ void tmem_ld16x256_three(uint32_t t0, uint32_t t1, uint32_t t2, float (&v)[3][4]) {
-    uint32_t r[12];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%0,%1,%2,%3}, [%12];\n\t"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%4,%5,%6,%7}, [%13];\n\t"
-        "tcgen05.ld.sync.aligned.16x256b.x1.b32 {%8,%9,%10,%11}, [%14];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=&r"(r[0]), "=&r"(r[1]), "=&r"(r[2]), "=&r"(r[3]), "=&r"(r[4]), "=&r"(r[5]), "=&r"(r[6]),
-          "=&r"(r[7]), "=&r"(r[8]), "=&r"(r[9]), "=&r"(r[10]), "=&r"(r[11])
-        : "r"(t0), "r"(t1), "r"(t2)
-        : "memory");
-#pragma unroll
-    for (int i = 0; i < 12; ++i) v[i / 4][i % 4] = __uint_as_float(r[i]);
-}
-__device__ __forceinline__ void tmem_ld16x256_three(uint32_t t0, uint32_t t1, uint32_t t2, float (&v)[3][16]) {
-    uint32_t r[48];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%48];\n\t"
-        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%49];\n\t"
-        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47}, [%50];\n\t"
-        "tcgen05.wait::ld.sync.aligned;"
-        : "=&r"(r[0]), "=&r"(r[1]), "=&r"(r[2]), "=&r"(r[3]), "=&r"(r[4]), "=&r"(r[5]), "=&r"(r[6]), "=&r"(r[7]), "=&r"(r[8]), "=&r"(r[9]), "=&r"(r[10]), "=&r"(r[11]), "=&r"(r[12]), "=&r"(r[13]), "=&r"(r[14]), "=&r"(r[15]), "=&r"(r[16]), "=&r"(r[17]), "=&r"(r[18]), "=&r"(r[19]), "=&r"(r[20]), "=&r"(r[21]), "=&r"(r[22]), "=&r"(r[23]), "=&r"(r[24]), "=&r"(r[25]), "=&r"(r[26]), "=&r"(r[27]), "=&r"(r[28]), "=&r"(r[29]), "=&r"(r[30]), "=&r"(r[31]), "=&r"(r[32]), "=&r"(r[33]), "=&r"(r[34]), "=&r"(r[35]), "=&r"(r[36]), "=&r"(r[37]), "=&r"(r[38]), "=&r"(r[39]), "=&r"(r[40]), "=&r"(r[41]), "=&r"(r[42]), "=&r"(r[43]), "=&r"(r[44]), "=&r"(r[45]), "=&r"(r[46]), "=&r"(r[47])
-        : "r"(t0), "r"(t1), "r"(t2)
-        : "memory");
-#pragma unroll
-    for (int i = 0; i < 48; ++i) v[i / 16][i % 16] = __uint_as_float(r[i]);
-}
-
 // The K bf16 parts of v: part 0 = bf16(v), part k = bf16 of what parts 0 .. k-1 leave (each
 // difference is exact in fp32).
 template <int K>
