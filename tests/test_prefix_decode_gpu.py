@@ -416,3 +416,30 @@ def test_a_group_of_more_members_than_sequences_is_flagged(lla):
     x.decode()
     assert lla.lla_get_device_error() & lla.LLA_DEVERR_SEQUENCE
     lla.lla_clear_device_error()
+
+
+@pytest.mark.parametrize("seed", range(16))
+def test_random_batches_as_without_a_plan(lla, seed):
+    """Batches of any size, from one page a sequence to many hundred, with whatever they share: as the decode that reads every
+    page for itself, each within the tolerance of the 64-bit definition."""
+    r = random.Random(seed)
+    P, W = r.randint(1, 6), r.choice([1, 2, 3, 4, 5, 17, 40])
+    prompt, own = r.choice([0, 1, 4, 30, 200]), r.choice([1, 64, 300, 3000, 20000])
+    if P * W * own > 400000:
+        own = 300
+    d_rope = r.choice([0, 0, 32, 64, 96])
+    rk, rv = (96, 160) if d_rope else r.choice([(96, 160), (128, 128), (72, 120)])
+    rows, lens = shared(P, W, prompt, own, system=r.choice([0, 2]), branch=r.choice([0, 1, 3]), seed=seed)
+    x = Batch(lla, rows, lens, H=r.choice([1, 2, 7]), rk=rk, rv=rv, d_rope=d_rope, mu=not d_rope, seed=seed, garbage=True)
+    out, want = x.decode(pos=False), torch.empty(x.B, x.H, D, device=DEV)
+    if d_rope:
+        rope = lla.RopeAxes(10000.0, lla.LLA_ROPE_HALF, (d_rope // 2, 0, 0), lla.LLA_AXES_BLOCKS)
+        at = x.lens_t.repeat(3, 1).contiguous()
+        ws = torch.zeros(lla.lla_decode_decoupled_workspace_size(x.geom, d_rope, x.B), dtype=torch.uint8, device=DEV)
+        lla.lla_decode_attn_decoupled_axes(x.geom, x.codec, x.cache, x.planes, d_rope, rope, at, x.lens_t, x.max_ctx, 1, x.q, x.qr, x.ck, x.cv,
+                                           x.ckr, want, ws)
+    else:
+        ws = torch.zeros(lla.lla_decode_workspace_size(x.geom, x.B), dtype=torch.uint8, device=DEV)
+        lla.lla_decode_attn(x.geom, x.codec, x.cache, x.lens_t, x.max_ctx, 1, x.q, x.ck, x.cv, want, ws)
+    assert ((out - want).norm(dim=2) <= 4e-4 * want.norm(dim=2)).all()
+    assert torch.equal(x.decode(pos=False), out)
