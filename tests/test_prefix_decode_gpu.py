@@ -443,3 +443,19 @@ def test_random_batches_as_without_a_plan(lla, seed):
         lla.lla_decode_attn(x.geom, x.codec, x.cache, x.lens_t, x.max_ctx, 1, x.q, x.ck, x.cv, want, ws)
     assert ((out - want).norm(dim=2) <= 4e-4 * want.norm(dim=2)).all()
     assert torch.equal(x.decode(pos=False), out)
+
+
+def test_two_streams_at_once(lla):
+    """Calls on two streams, each with its own workspace, in any overlap of their kernels."""
+    a, b = Batch(lla, *shared(4, 12, 30, 2000, seed=1), H=8), Batch(lla, *shared(1, 3, 40, 900, seed=2), H=8, d_rope=64)
+    want = [a.decode(), b.decode()]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    outs = []
+    for _ in range(20):
+        for x, s in zip((a, b), streams):
+            with torch.cuda.stream(s):
+                outs.append(x.decode())
+    torch.cuda.synchronize()
+    for i, out in enumerate(outs):
+        assert torch.equal(out, want[i % 2])
