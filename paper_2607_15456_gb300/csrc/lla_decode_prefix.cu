@@ -1616,8 +1616,9 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     tp.next = tp.pstart + 2 * (kMaxNodes + 1);
     tp.leaf = static_cast<int64_t>(w.leaf);
     // No group of up to four sequences has more members than the leaf kernel can take: no trunk kernel then (four sequences over
-    // 768 tokens 25.5 -> 24.1 us).  Beside one, nodes of three and four queries are faster in it: 64 sequences over 16 prompts
-    // take 116 us, 123 with all of them as leaves.
+    // 768 tokens 16.1 us, 25.0 with it in the chain).  Beside one, leaves of up to four queries need registers that the join's CTA
+    // holds: 64 sequences over 16 prompts, all of them leaves then, take 107 us instead of 109, but 128 samples of 8 documents 105
+    // instead of 97, and of two videos 149 instead of 140.
     const bool alone = a.B <= kLeafAlone;
     tp.leaf_max = alone ? kLeafAlone : kLeaf;
     tp.err = err;
