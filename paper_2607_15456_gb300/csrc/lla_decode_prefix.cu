@@ -547,7 +547,7 @@ __device__ __forceinline__ int64_t query_row(const TrunkParams &p, const TrunkRu
 __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xffffffffu, v, 0); }
 
 // The 128 rows hold R queries 128 / R times: replica i = row / R has part i % 2 of their weights p (in the operand behind it the
-// third part, where i is even) for the tokens
+// third part, where i is odd: those rows' sums are small, and what is added to them is not rounded to the size of the whole) for the tokens
 // R (i / 2) to R (i / 2) + R - 1 of each page, and zeros for the others, so that a thread works on R tokens and the sum of a
 // query's rows of O is the sum over all tokens of both parts.  (With R = 64 for all, two of the four schedulers did the
 // work of up to 32 queries.)
@@ -681,8 +681,8 @@ __device__ __forceinline__ void softmax_run(const SoftmaxCtx &x, int run, int it
             const uint32_t rest = pack_bf16x2(y.x - f.x, y.y - f.y);
             if constexpr (ZZ::P3) {  // (s is free behind its weight: the third part in its place)
                 const float2 r = bf2_to_f2(rest);
-                s[c] = second ? 0.f : (y.x - f.x) - r.x;
-                s[c + 1] = second ? 0.f : (y.y - f.y) - r.y;
+                s[c] = second ? (y.x - f.x) - r.x : 0.f;
+                s[c + 1] = second ? (y.y - f.y) - r.y : 0.f;
             }
             if (second) pw[c / 2] = rest;
         }
