@@ -40,7 +40,7 @@
 //                  W_up,t^V once for all of them.  One CTA per SM, beside the leaf kernel's, so that the weights and the
 //                  instructions are there when the records are: 13 us behind the leaves of 128 sequences in 16 heads (22 us where
 //                  it started when they had left, with the projection on the CUDA cores).  Bound by latency
-// 64 sequences over 16 prompts of 2048 to 4096 tokens, 16 heads, r 96 + 160: 110 us, of 83 us that HBM takes for the bytes.
+// 64 sequences over 16 prompts of 2048 to 4096 tokens, 16 heads, r 96 + 160: 108 us, of 83 us that HBM takes for the bytes.
 //
 // Storage bf16, d = 128; accumulators fp32 in TMEM.  Three parts of q~, and of p, hold the 24 bits of fp32.  For bf16 outputs p has
 // two: they are off by at most 2^-18 of p, half a step of the second part, and an output is rounded to 2^-9.  (With two for
@@ -178,6 +178,15 @@ struct Split {
         return page < wide ? page / (each + 1) : more + (page - wide) / each;
     }
 };
+
+// The shares that the trunk's pages are split into: one per CTA, or for fp32 outputs (`third`) up to kTrunkCuts of kTrunkPages pages
+// each that a CTA takes one after the other, a run each.  Tensor cores cut off what an addition leaves behind 24 bits, and all to
+// one side: 4 additions a page of 64 queries, so that over 50 pages the outputs were off by 3.7e-6, and are by 1.5e-6 so (an fp32
+// evaluation by 1.2e-6).  128 samples of 8 documents take 97.7 us with it, 96.4 without, 100 with 16 pages.
+constexpr int kTrunkPages = 24, kTrunkCuts = 8;
+__device__ __forceinline__ int trunk_cuts(int np, int ctas, bool third) {
+    return third ? max(1, min(kTrunkCuts, (np / ctas + kTrunkPages - 1) / kTrunkPages)) : 1;
+}
 
 // The shares that the pages of the leaves are split into, for `workers` warps: one each of kLeafFirst / 8 of the pages, and the
 // rest in up to kLeafRest as many small ones, which the warps take as they get there.  A share's record does not depend on the
@@ -429,13 +438,14 @@ struct TrunkRun {
 
 struct Share {
     int g0, g1;      // pages of this CTA, among all of the kind
+    int c0, np, we;  // its first share; all pages and all shares
     int nodes, s;    // nodes in `list`, first page of the first
 };
 
 // This CTA's share of the pages of the nodes with more queries than a leaf, and the nodes that it lies in: worked out from the
 // inputs of the call by all threads, so that copies can start while the absorb kernel still runs.
 template <int THREADS>
-__device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list) {
+__device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list, bool third) {
     __shared__ int wsum[THREADS / 32], wcnt[THREADS / 32], first;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int nodes = groups + p.B, per = (nodes + THREADS - 1) / THREADS;
@@ -462,11 +472,14 @@ __device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list) {
         np += wsum[w];
     }
     // with fewer pages than CTAs the first np take one each
-    const int c = blockIdx.x, we = min(static_cast<int>(gridDim.x), np);
+    const int cuts = trunk_cuts(np, gridDim.x, third), c = blockIdx.x * cuts, we = min(static_cast<int>(gridDim.x) * cuts, np);
     const Split split(np, we);
     Share r;
     r.g0 = c < we ? split.begin(c) : 0;
-    r.g1 = c < we ? split.begin(c + 1) : 0;
+    r.g1 = c < we ? split.begin(min(c + cuts, we)) : 0;
+    r.c0 = c;
+    r.np = np;
+    r.we = we;
     int mine = 0, ex = ex0;
     for (int i = tid * per; i < min(nodes, (tid + 1) * per); ++i) {
         const int n = pages(i);
@@ -501,9 +514,12 @@ struct RunWalk {
     const TrunkParams &p;
     const uint16_t *list;
     int groups, g0, g1, nodes, i, s, u, stop, in;  // node i of the list starts at page s; u: page of the node, head by head
+    Split split;
+    int share, cut;  // the run's share, and its end
     TrunkRun r;
     __device__ __forceinline__ RunWalk(const TrunkParams &pp, int gr, const Share &sh, const uint16_t *l)
-        : p(pp), list(l), groups(gr), g0(sh.g0), g1(sh.g1), nodes(sh.nodes), i(-1), s(sh.s), u(0), stop(0), in(0) {
+        : p(pp), list(l), groups(gr), g0(sh.g0), g1(sh.g1), nodes(sh.nodes), i(-1), s(sh.s), u(0), stop(0), in(0),
+          split(sh.np, sh.we), share(sh.c0), cut(split.begin(sh.c0 + 1)) {
         r.pages = 0;
         r.d.pages = 0;
     }
@@ -511,8 +527,11 @@ struct RunWalk {
     __device__ __forceinline__ bool next() {
         u += r.pages;
         if (u < stop) {
-            ++r.h;
-            in = 0;
+            in += r.pages;
+            if (in == r.d.pages) {
+                ++r.h;
+                in = 0;
+            }
         } else {
             if (i >= 0) s += r.d.pages * p.H;
             if (++i >= nodes) {
@@ -528,7 +547,8 @@ struct RunWalk {
             r.h = u / r.d.pages;
             in = u - r.h * r.d.pages;
         }
-        r.pages = min(stop - u, r.d.pages - in);
+        if (s + u >= cut) cut = split.begin(++share + 1);
+        r.pages = min(min(stop - u, r.d.pages - in), cut - s - u);
         r.page = r.d.first + in;
         return true;
     }
@@ -761,7 +781,7 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
     __syncthreads();
     tc_fence_after();
     constexpr uint32_t tmem = 0;  // the whole of TMEM is allocated (one CTA per SM)
-    const Share sh = find_share<kTrunkThreads>(p, groups, list);
+    const Share sh = find_share<kTrunkThreads>(p, groups, list, THIRD);
     // q~ and beta come from the absorb kernel, and the workspace is free once it has waited for the kernel before it; the
     // producers read only inputs of the call, which that kernel's wait ordered before this launch, and wait at their end
     if (warp != 0 && warp != 2) {
@@ -952,7 +972,7 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
             tc_fence_after();
             // every row of O into shared memory, which frees it, and from there the sums of the queries' rows
             const int n = w.r.d.n, R = replica_rows(n);
-            float *rec = p.part + record_of(p, w.r.d, w.r.h, blockIdx.x) * RS;
+            float *rec = p.part + record_of(p, w.r.d, w.r.h, w.share) * RS;
             float *exch = reinterpret_cast<float *>(sm + ZZ::oExch);
 #pragma unroll 1
             for (int c0 = 0; c0 < ZZ::RVX; c0 += ZZ::XCOLS) {
@@ -1419,7 +1439,7 @@ __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(const __grid_cons
                     c0 = shares.share(s0);
                     runs = shares.share(s1) - c0 + 1;
                 } else {
-                    const Split split(np, min(a.grid, np));  // as find_share
+                    const Split split(np, min(a.grid * trunk_cuts(np, a.grid, !a.io_bf16), np));  // as find_share
                     c0 = split.worker(s0);
                     runs = split.worker(s1) - c0 + 1;
                 }
@@ -1562,7 +1582,7 @@ inline size_t al256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 PrefixWorkspace prefix_workspace(int rkt, int r_v, int B, int H, int grid) {
     PrefixWorkspace w;
-    w.leaf = static_cast<size_t>(H) * kLevels * B + static_cast<size_t>(kMembers) * grid;
+    w.leaf = static_cast<size_t>(H) * kLevels * B + static_cast<size_t>(kMembers) * kTrunkCuts * grid;
     const size_t records = w.leaf + static_cast<size_t>(H) * (kLevels + 1) * B + static_cast<size_t>(kLeafAlone) * (1 + kLeafRest) * kMaxWarps * grid;
     w.part = 0;
     w.qt = al256(records * record_floats(r_v) * sizeof(float));
