@@ -29,8 +29,9 @@
 //                    warps 4-11    softmax: two groups that take the pages in turn (as in the prefill, a page's step from scores
 //                                  to weights takes longer than its products); the running maximum goes from page to page
 //                                  through shared memory and a named barrier per pair of warps; lazy rescale of O
-//                    warps 12-15   q~ of the next run into TMEM as soon as the last S of the run before is done; then that
-//                                  run's O through shared memory, its maxima and its sums to the workspace
+//                    warps 12-15   q~ of the next unit into TMEM as soon as the last S of the one before is done; a run's O through
+//                                  shared memory, its maxima and its sums to the workspace, joined with what the unit's
+//                                  runs before it have left there
 //                  Bound by HBM and, at run ends, by latency: 393 MB of pages that 4 sequences each share take 74 us (5.3 TB/s),
 //                  287 MB that 64 share 73 us, with the tensor pipe busy for 55 % and the step from S to P for the rest
 //   leaf_kernel    nodes of up to kLeaf queries, which are short (a sequence's own pages): one page at a time in each of as
@@ -42,9 +43,10 @@
 //                  it started when they had left, with the projection on the CUDA cores).  Bound by latency
 // 64 sequences over 16 prompts of 2048 to 4096 tokens, 16 heads, r 96 + 160: 108 us, of 83 us that HBM takes for the bytes.
 //
-// Storage bf16, d = 128; accumulators fp32 in TMEM.  Three parts of q~, and of p, hold the 24 bits of fp32.  For bf16 outputs p has
-// two: they are off by at most 2^-18 of p, half a step of the second part, and an output is rounded to 2^-9.  (With two for
-// fp32 outputs, too, a few tokens' outputs were off by 2e-6.)  The sums l take p itself.
+// Storage bf16, d = 128; accumulators fp32 in TMEM, for at most kRunPages pages.  Three parts of q~, and of p, hold the 24 bits of fp32.
+// For bf16 outputs p has two, for the price of one (see replica_rows): they are off by at most 2^-18 of p, half a step of the second
+// part and to both sides, where an output is rounded by up to 2^-8.  (With two for fp32 outputs, too, a few tokens' outputs were
+// off by 2e-6.)  The sums l take p itself.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -179,14 +181,14 @@ struct Split {
     }
 };
 
-// The shares that the trunk's pages are split into: one per CTA, or for fp32 outputs (`third`) up to kTrunkCuts of kTrunkPages pages
-// each that a CTA takes one after the other, a run each.  Tensor cores cut off what an addition leaves behind 24 bits, and all to
-// one side: 4 additions a page of 64 queries, so that over 50 pages the outputs were off by 3.7e-6, and are by 1.5e-6 so (an fp32
-// evaluation by 1.2e-6).  128 samples of 8 documents take 97.7 us with it, 96.4 without, 100 with 16 pages.
-constexpr int kTrunkPages = 24, kTrunkCuts = 8;
-__device__ __forceinline__ int trunk_cuts(int np, int ctas, bool third) {
-    return third ? max(1, min(kTrunkCuts, (np / ctas + kTrunkPages - 1) / kTrunkPages)) : 1;
-}
+// Most pages of a run: a CTA's pages are cut into even pieces of at most as many, a run is a piece's part of a unit, and the epilogue
+// joins the runs of a unit in fp32, in the CTA's record of it.  The tensor cores cut off what an addition leaves behind the last bits of
+// O, all to one side, so that a sum loses the more the larger it gets.  Measured on sums of one sign, mean over the outputs of 64
+// queries: 1.6e-6 of themselves with 24 pages, 9.9e-6 with 64, 2.9e-5 with 128 (of 20 queries, whose rows hold fewer tokens, 0.5, 2.9 and
+// 9.5e-6).  fp32 outputs: 24; 64 samples of two videos, d_rope 64, take 173 us so, 178 with 16, 169 with 40.  bf16 outputs: 64,
+// where the loss is 1/400 of their rounding; with 24 the same call takes 149 us instead of 138.
+template <bool FP32>
+constexpr int kRunPages = FP32 ? 24 : 64;
 
 // The shares that the pages of the leaves are split into, for `workers` warps: one each of kLeafFirst / 8 of the pages, and the
 // rest in up to kLeafRest as many small ones, which the warps take as they get there.  A share's record does not depend on the
@@ -430,22 +432,22 @@ enum {
     bQfull = 28, bQfree = 29, bOdone = 30, bOfree = 31 /* [2] */, bMfull = 33 /* [2] */, bAbort = 35, bTslot = 36
 };
 
-// A CTA's part of a unit.
+// Pages of a unit that go through O together.
 struct TrunkRun {
     Node d;
     int h, page, pages;  // page: the first in the table row
+    bool first, last;    // of the CTA's runs of the unit
 };
 
 struct Share {
-    int g0, g1;      // pages of this CTA, among all of the kind
-    int c0, np, we;  // its first share; all pages and all shares
-    int nodes, s;    // nodes in `list`, first page of the first
+    int g0, g1;    // pages of this CTA, among all of the kind
+    int nodes, s;  // nodes in `list`, first page of the first
 };
 
 // This CTA's share of the pages of the nodes with more queries than a leaf, and the nodes that it lies in: worked out from the
 // inputs of the call by all threads, so that copies can start while the absorb kernel still runs.
 template <int THREADS>
-__device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list, bool third) {
+__device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list) {
     __shared__ int wsum[THREADS / 32], wcnt[THREADS / 32], first;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int nodes = groups + p.B, per = (nodes + THREADS - 1) / THREADS;
@@ -472,14 +474,11 @@ __device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list, bo
         np += wsum[w];
     }
     // with fewer pages than CTAs the first np take one each
-    const int cuts = trunk_cuts(np, gridDim.x, third), c = blockIdx.x * cuts, we = min(static_cast<int>(gridDim.x) * cuts, np);
+    const int c = blockIdx.x, we = min(static_cast<int>(gridDim.x), np);
     const Split split(np, we);
     Share r;
     r.g0 = c < we ? split.begin(c) : 0;
-    r.g1 = c < we ? split.begin(min(c + cuts, we)) : 0;
-    r.c0 = c;
-    r.np = np;
-    r.we = we;
+    r.g1 = c < we ? split.begin(c + 1) : 0;
     int mine = 0, ex = ex0;
     for (int i = tid * per; i < min(nodes, (tid + 1) * per); ++i) {
         const int n = pages(i);
@@ -509,23 +508,26 @@ __device__ Share find_share(const TrunkParams &p, int groups, uint16_t *list, bo
     return r;
 }
 
-// The runs of a share, in order.
+// The runs of a share, in order, of at most MOST pages.
+template <int MOST>
 struct RunWalk {
     const TrunkParams &p;
     const uint16_t *list;
     int groups, g0, g1, nodes, i, s, u, stop, in;  // node i of the list starts at page s; u: page of the node, head by head
     Split split;
-    int share, cut;  // the run's share, and its end
+    int piece, cut;  // the run's piece of the share, and its end
     TrunkRun r;
     __device__ __forceinline__ RunWalk(const TrunkParams &pp, int gr, const Share &sh, const uint16_t *l)
         : p(pp), list(l), groups(gr), g0(sh.g0), g1(sh.g1), nodes(sh.nodes), i(-1), s(sh.s), u(0), stop(0), in(0),
-          split(sh.np, sh.we), share(sh.c0), cut(split.begin(sh.c0 + 1)) {
+          split(sh.g1 - sh.g0, (sh.g1 - sh.g0 + MOST - 1) / MOST), piece(0), cut(sh.g0 + split.begin(1)) {
         r.pages = 0;
         r.d.pages = 0;
+        r.last = true;
     }
     // The next run, or false behind the last.
     __device__ __forceinline__ bool next() {
         u += r.pages;
+        r.first = r.last;
         if (u < stop) {
             in += r.pages;
             if (in == r.d.pages) {
@@ -547,8 +549,10 @@ struct RunWalk {
             r.h = u / r.d.pages;
             in = u - r.h * r.d.pages;
         }
-        if (s + u >= cut) cut = split.begin(++share + 1);
-        r.pages = min(min(stop - u, r.d.pages - in), cut - s - u);
+        if (s + u >= cut) cut = g0 + split.begin(++piece + 1);
+        const int left = min(stop - u, r.d.pages - in);
+        r.pages = min(left, cut - s - u);
+        r.last = r.pages == left;
         r.page = r.d.first + in;
         return true;
     }
@@ -781,14 +785,14 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
     __syncthreads();
     tc_fence_after();
     constexpr uint32_t tmem = 0;  // the whole of TMEM is allocated (one CTA per SM)
-    const Share sh = find_share<kTrunkThreads>(p, groups, list, THIRD);
+    const Share sh = find_share<kTrunkThreads>(p, groups, list);
     // q~ and beta come from the absorb kernel, and the workspace is free once it has waited for the kernel before it; the
     // producers read only inputs of the call, which that kernel's wait ordered before this launch, and wait at their end
     if (warp != 0 && warp != 2) {
         pdl_wait();
         pdl_trigger();  // the leaf kernel may take this SM as soon as this CTA has left it
     }
-    RunWalk w(p, groups, sh, list);
+    RunWalk<kRunPages<THIRD>> w(p, groups, sh, list);
 
     if (warp == 0 || warp == 2) {
         // ------------------------------------------------------------------------------ producers
@@ -839,10 +843,10 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
         const uint32_t base = smem_addr(sm);
         const uint64_t dk0 = umma_desc(base + ZZ::oK, kPT * 16, 128);
         [[maybe_unused]] const uint64_t dq = umma_desc(base + ZZ::oQ, kRows * 16, 128);
-        int it = 0;
-        for (int run = 0; uniform(w.next()); ++run) {
-            const int pages = uniform(w.r.pages);
-            mbar_wait_warp(&bar[bQfull], run & 1, abort_flag, p.err);
+        int it = 0, parts = 0;
+        while (uniform(w.next())) {
+            const int pages = uniform(w.r.pages), last = uniform(w.r.last);
+            if (uniform(w.r.first)) mbar_wait_warp(&bar[bQfull], parts++ & 1, abort_flag, p.err);
             for (int k = 0; k < pages; ++k, ++it) {
                 const int g = it & 1, st = it % ZZ::ST;
                 mbar_wait_warp(&bar[bKfull + st], (it / ZZ::ST) & 1, abort_flag, p.err);
@@ -861,7 +865,7 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
                         else
                             umma_bf16_warp(ts, dq + ks * ((2 * kRows * 16) >> 4), dk + ks * ((2 * kPT * 16) >> 4), ZZ::IDESC_S, more);
                     }
-                if (k == pages - 1) umma_commit_warp(&bar[bQfree]);
+                if (last && k == pages - 1) umma_commit_warp(&bar[bQfree]);
                 umma_commit_warp(&bar[bKempty + st]);
                 umma_commit_warp(&bar[bSfull + g]);
             }
@@ -955,25 +959,38 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
             tc_fence_before();
             mbar_arrive(&bar[bQfull]);
         };
-        RunWalk ahead(p, groups, sh, list);
+        RunWalk<kRunPages<THIRD>> ahead(p, groups, sh, list);
         if (ahead.next()) {
             fetch_queries(ahead.r);
             store_queries();
         }
-        for (int run = 0; w.next(); ++run) {
-            if (ahead.next()) {  // the next run's q~, as soon as S of this one's pages is done
+        for (int run = 0, parts = 0; w.next(); ++run) {
+            if (ahead.next() && ahead.r.first) {  // the next unit's q~, as soon as S of this one's pages is done
                 fetch_queries(ahead.r);
-                mbar_wait(&bar[bQfree], run & 1, abort_flag, p.err);
+                mbar_wait(&bar[bQfree], parts++ & 1, abort_flag, p.err);
                 tc_fence_after();
                 store_queries();
             }
+            const int n = w.r.d.n, R = replica_rows(n);
+            const bool joins = !w.r.first;  // the record holds the part's runs before this one
+            float *rec = p.part + record_of(p, w.r.d, w.r.h, blockIdx.x) * RS;
+            float *exch = reinterpret_cast<float *>(sm + ZZ::oExch);
+            float2 *state = reinterpret_cast<float2 *>(rec + row * RS + RV);  // of query `row`: maximum and sum
+            const float2 was_state = joins && row < n ? *state : make_float2(0.f, 0.f);
             mbar_wait(&bar[bOdone], run & 1, abort_flag, p.err);
             mbar_wait(&bar[bMfull + (run & 1)], (run >> 1) & 1, abort_flag, p.err);
             tc_fence_after();
+            auto run_state = [&] {  // of query `row`: maximum and sum of both groups (whose slices have one maximum)
+                const float2 *st = states + (run % 3) * 2 * 64;
+                const float m0 = st[row].x, m1 = st[64 + row].x, m = fmaxf(m0, m1);
+                float l0 = 0.f, l1 = 0.f;
+                for (int i = row; i < 64; i += R) {
+                    l0 += st[i].y;
+                    l1 += st[64 + i].y;
+                }
+                return make_float2(m, (m0 == m ? l0 : l0 * ex2_approx(m0 - m)) + (m1 == m ? l1 : l1 * ex2_approx(m1 - m)));
+            };
             // every row of O into shared memory, which frees it, and from there the sums of the queries' rows
-            const int n = w.r.d.n, R = replica_rows(n);
-            float *rec = p.part + record_of(p, w.r.d, w.r.h, w.share) * RS;
-            float *exch = reinterpret_cast<float *>(sm + ZZ::oExch);
 #pragma unroll 1
             for (int c0 = 0; c0 < ZZ::RVX; c0 += ZZ::XCOLS) {
                 if (c0 > 0) named_bar_sync(9, 128);
@@ -989,32 +1006,41 @@ __global__ void __launch_bounds__(kTrunkThreads, 1)
                     tc_fence_before();
                     mbar_arrive(&bar[bOfree + (run & 1)]);
                 }
+                if (joins && c0 == 0 && row < n) {
+                    const float2 now = run_state(), was = was_state;
+                    const float m = fmaxf(was.x, now.x);
+                    const float2 f = make_float2(ex2_approx(was.x - m), ex2_approx(now.x - m));
+                    *reinterpret_cast<float2 *>(exch + row * ZZ::XROW + ZZ::XCOLS) = f;  // (behind the columns of a row)
+                    *state = make_float2(m, fmaf(was.y, f.x, now.y * f.y));
+                }
                 named_bar_sync(9, 128);
                 const int words = min(ZZ::XCOLS, RV - c0) / 4;
-#pragma unroll 2
-                for (int i = row; i < n * words; i += 128) {
-                    const int q = i / words, c = 4 * (i - q * words);
+                auto sum = [&](int q, int c) {
                     float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
                     for (int k = q; k < kRows; k += R) {
                         const float4 b = *reinterpret_cast<const float4 *>(exch + k * ZZ::XROW + c);
                         a = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
                     }
-                    *reinterpret_cast<float4 *>(rec + static_cast<int64_t>(q) * RS + c0 + c) = a;
+                    return a;
+                };
+                auto at = [&](int q, int c) { return reinterpret_cast<float4 *>(rec + static_cast<int64_t>(q) * RS + c0 + c); };
+                if (joins) {  // (a thread has the same words of every run of a part)
+#pragma unroll 2
+                    for (int i = row; i < n * words; i += 128) {
+                        const int q = i / words, c = 4 * (i - q * words);
+                        const float4 was = *at(q, c), a = sum(q, c);
+                        const float2 f = *reinterpret_cast<const float2 *>(exch + q * ZZ::XROW + ZZ::XCOLS);
+                        *at(q, c) = make_float4(fmaf(was.x, f.x, a.x * f.y), fmaf(was.y, f.x, a.y * f.y), fmaf(was.z, f.x, a.z * f.y), fmaf(was.w, f.x, a.w * f.y));
+                    }
+                } else {
+#pragma unroll 2
+                    for (int i = row; i < n * words; i += 128) {
+                        const int q = i / words, c = 4 * (i - q * words);
+                        *at(q, c) = sum(q, c);
+                    }
                 }
             }
-            if (row < n) {
-                // (a group's slices have one maximum)
-                const int q = row;
-                const float2 *st = states + (run % 3) * 2 * 64;
-                const float m0 = st[q].x, m1 = st[64 + q].x, mf = fmaxf(m0, m1);
-                float l0 = 0.f, l1 = 0.f;
-                for (int i = q; i < 64; i += R) {
-                    l0 += st[i].y;
-                    l1 += st[64 + i].y;
-                }
-                rec[q * RS + RV] = mf;
-                rec[q * RS + RV + 1] = (m0 == mf ? l0 : l0 * ex2_approx(m0 - mf)) + (m1 == mf ? l1 : l1 * ex2_approx(m1 - mf));
-            }
+            if (!joins && row < n) *state = run_state();
             named_bar_sync(9, 128);  // the shared memory is free
         }
     }
@@ -1439,7 +1465,7 @@ __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(const __grid_cons
                     c0 = shares.share(s0);
                     runs = shares.share(s1) - c0 + 1;
                 } else {
-                    const Split split(np, min(a.grid * trunk_cuts(np, a.grid, !a.io_bf16), np));  // as find_share
+                    const Split split(np, min(a.grid, np));  // as find_share
                     c0 = split.worker(s0);
                     runs = split.worker(s1) - c0 + 1;
                 }
@@ -1582,7 +1608,7 @@ inline size_t al256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
 PrefixWorkspace prefix_workspace(int rkt, int r_v, int B, int H, int grid) {
     PrefixWorkspace w;
-    w.leaf = static_cast<size_t>(H) * kLevels * B + static_cast<size_t>(kMembers) * kTrunkCuts * grid;
+    w.leaf = static_cast<size_t>(H) * kLevels * B + static_cast<size_t>(kMembers) * grid;
     const size_t records = w.leaf + static_cast<size_t>(H) * (kLevels + 1) * B + static_cast<size_t>(kLeafAlone) * (1 + kLeafRest) * kMaxWarps * grid;
     w.part = 0;
     w.qt = al256(records * record_floats(r_v) * sizeof(float));
