@@ -83,6 +83,7 @@ struct PlanView {
 struct TrunkParams {
     int H, B, max_ctx, max_blocks, pass1;
     int leaf_max;  // queries of a node that the leaf kernel takes, at most
+    int trunk_max; // queries of a node that the trunk kernel takes, at most; 0 without one
     const char *pool;
     int64_t num_blocks, page_bytes;
     const char *rope_pool;
@@ -165,7 +166,7 @@ __device__ __forceinline__ bool is_leaf(const TrunkParams &p, const Node &d) { r
 // CTAs grow together.
 __device__ __forceinline__ int64_t record_of(const TrunkParams &p, const Node &d, int h, int c) {
     const int64_t at = static_cast<int64_t>(p.H) * d.member + static_cast<int64_t>(h) * d.n;
-    return is_leaf(p, d) ? p.leaf + at + static_cast<int64_t>(p.leaf_max) * c : at + static_cast<int64_t>(kMembers) * c;
+    return is_leaf(p, d) ? p.leaf + at + static_cast<int64_t>(p.leaf_max) * c : at + static_cast<int64_t>(p.trunk_max) * c;
 }
 __host__ __device__ constexpr int record_floats(int rv) { return rv + 4; }
 
@@ -1470,7 +1471,7 @@ __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(const __grid_cons
                     runs = split.worker(s1) - c0 + 1;
                 }
                 first = static_cast<int>(record_of(p, d, h, c0)) + rank;
-                step = is_leaf(p, d) ? p.leaf_max : kMembers;
+                step = is_leaf(p, d) ? p.leaf_max : p.trunk_max;
             }
             if (dry) {  // (one run, the first record: whatever it holds)
                 runs = lane == kLevels;
@@ -1606,10 +1607,18 @@ struct PrefixWorkspace {
 
 inline size_t al256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
-PrefixWorkspace prefix_workspace(int rkt, int r_v, int B, int H, int grid) {
+// Queries of a node of either kind, at most, for B sequences.  No group of up to kLeafAlone sequences has more members than the leaf
+// kernel can take: no trunk kernel then.
+struct NodeSizes {
+    int leaf_max, trunk_max;
+    explicit NodeSizes(int B) : leaf_max(B <= kLeafAlone ? std::max(B, 1) : kLeaf), trunk_max(B <= kLeafAlone ? 0 : std::min(B, kMembers)) {}
+};
+
+PrefixWorkspace prefix_workspace(int rkt, int r_v, int B, int H, int grid, int leaf_warps) {
     PrefixWorkspace w;
-    w.leaf = static_cast<size_t>(H) * kLevels * B + static_cast<size_t>(kMembers) * grid;
-    const size_t records = w.leaf + static_cast<size_t>(H) * (kLevels + 1) * B + static_cast<size_t>(kLeafAlone) * (1 + kLeafRest) * kMaxWarps * grid;
+    const NodeSizes n(B);
+    w.leaf = n.trunk_max > 0 ? static_cast<size_t>(H) * kLevels * B + static_cast<size_t>(n.trunk_max) * grid : 0;
+    const size_t records = w.leaf + static_cast<size_t>(H) * (kLevels + 1) * B + static_cast<size_t>(n.leaf_max) * (1 + kLeafRest) * leaf_warps * grid;
     w.part = 0;
     w.qt = al256(records * record_floats(r_v) * sizeof(float));
     w.qf = w.qt + al256(static_cast<size_t>(B) * H * 3 * rkt * sizeof(uint16_t));
@@ -1630,11 +1639,13 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     if (grid <= 0) return LLA_ERR_CUDA;
     if (grid > kMaxGrid) return LLA_ERR_UNSUPPORTED;
     if (a.num_blocks * a.H >= (int64_t(1) << 31)) return LLA_ERR_UNSUPPORTED;  // TMA coordinate
-    const PrefixWorkspace w = prefix_workspace(ZZ::RKT, RV, a.B, a.H, grid);
-    if (a.workspace_bytes < w.total) return LLA_ERR_WORKSPACE;
-    char *ws = static_cast<char *>(a.workspace);
     using LL = L<RK, RV, DR, false>;
     using LA = L<RK, RV, DR, true>;
+    const NodeSizes sizes(a.B);
+    const bool alone = sizes.trunk_max == 0;
+    const PrefixWorkspace w = prefix_workspace(ZZ::RKT, RV, a.B, a.H, grid, alone ? LA::WARPS : LL::WARPS);
+    if (a.workspace_bytes < w.total) return LLA_ERR_WORKSPACE;
+    char *ws = static_cast<char *>(a.workspace);
     static DeviceOnce configured, configured_leaf, configured_alone;
     if (raise_smem_limit(leaf_kernel<RK, RV, DR, false>, LL::SMEM, configured_leaf, true) != LLA_OK) return LLA_ERR_CUDA;
     if (raise_smem_limit(leaf_kernel<RK, RV, DR, true>, LA::SMEM, configured_alone, true) != LLA_OK) return LLA_ERR_CUDA;
@@ -1661,12 +1672,11 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     tp.pstart = reinterpret_cast<int *>(ws + w.pstart);
     tp.next = tp.pstart + 2 * (kMaxNodes + 1);
     tp.leaf = static_cast<int64_t>(w.leaf);
-    // No group of up to four sequences has more members than the leaf kernel can take: no trunk kernel then (four sequences over
-    // 768 tokens 16.1 us, 25.0 with it in the chain).  Beside one, leaves of up to four queries need registers that the join's CTA
+    // Four sequences over 768 tokens take 16.1 us without a trunk kernel, 25.0 with it in the chain.  Beside one, leaves of up to four queries need registers that the join's CTA
     // holds: 64 sequences over 16 prompts, all of them leaves then, take 107 us instead of 109, but 128 samples of 8 documents 105
     // instead of 97, and of two videos 149 instead of 140.
-    const bool alone = a.B <= kLeafAlone;
-    tp.leaf_max = alone ? kLeafAlone : kLeaf;
+    tp.leaf_max = sizes.leaf_max;
+    tp.trunk_max = sizes.trunk_max;
     tp.err = err;
 
     AbsorbParams ap = {};
@@ -1714,10 +1724,19 @@ bool decode_prefix_supported(int es, int d, int r_k, int r_v, int d_rope) {
     return r_k == 96 && r_v == 160 && (d_rope == 32 || d_rope == 64 || d_rope == 96);
 }
 
+#define LLA_PREFIX_SHAPES(X) \
+    X(96, 160, 0) X(128, 128, 0) X(72, 120, 0) X(96, 160, 32) X(96, 160, 64) X(96, 160, 96)
+
 size_t decode_prefix_workspace_bytes(int r_k, int r_v, int d_rope, int B, int H) {
     const int grid = num_sms();
     if (grid <= 0) return 0;
-    return prefix_workspace((r_k + 15) / 16 * 16 + d_rope, r_v, B, H, grid).total;
+#define LLA_PREFIX(K, V, R) \
+    if (r_k == K && r_v == V && d_rope == R) \
+        return prefix_workspace(Z<K, V, R, false>::RKT, V, B, H, grid, \
+                                NodeSizes(B).trunk_max == 0 ? L<K, V, R, true>::WARPS : L<K, V, R, false>::WARPS).total;
+    LLA_PREFIX_SHAPES(LLA_PREFIX)
+#undef LLA_PREFIX
+    return 0;
 }
 
 lla_status launch_decode_prefix(const DecodeArgs &a, const lla_prefix &plan, const void *rope_pool, int d_rope,
@@ -1727,12 +1746,7 @@ lla_status launch_decode_prefix(const DecodeArgs &a, const lla_prefix &plan, con
     if (a.r_k == K && a.r_v == V && d_rope == R) \
         return a.io_bf16 ? launch_prefix<K, V, R, false>(a, plan, rope_pool, rope, positions, q_rope, cur_k_rope, stream) \
                          : launch_prefix<K, V, R, true>(a, plan, rope_pool, rope, positions, q_rope, cur_k_rope, stream);
-    LLA_PREFIX(96, 160, 0)
-    LLA_PREFIX(128, 128, 0)
-    LLA_PREFIX(72, 120, 0)
-    LLA_PREFIX(96, 160, 32)
-    LLA_PREFIX(96, 160, 64)
-    LLA_PREFIX(96, 160, 96)
+    LLA_PREFIX_SHAPES(LLA_PREFIX)
 #undef LLA_PREFIX
     return LLA_ERR_UNSUPPORTED;
 }
