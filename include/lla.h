@@ -695,8 +695,9 @@ typedef struct {
  * holds as long as the pages it names stay in the rows it was made from: tokens may be appended, so it has to be made again
  * only when sequences come, go or move (and should be when many pages more could be shared).
  *   min_pages  pages that a set must share to become a group, >= 1
- * A length out of range sets LLA_DEVERR_CONTEXT, a shared page that is no block LLA_DEVERR_BLOCK_ID: such a sequence
- * shares nothing (from that page on).  One kernel on the stream.
+ * A length out of range sets LLA_DEVERR_CONTEXT: such a sequence shares nothing.  A set's pages end before an entry that is no
+ * block; LLA_DEVERR_BLOCK_ID is set where that is the first full page of a sequence, or the one behind the pages of a group that it is in.
+ * One kernel on the stream.
  */
 lla_status lla_prefix_plan(const lla_cache *cache, const int32_t *context_lens, int32_t B, int32_t max_ctx,
                            int32_t min_pages, const lla_prefix *plan, void *stream);

@@ -3,7 +3,7 @@
 //
 // A level refines the sets of the level before it (at first the whole batch): sequences of a set with the same block in
 // the set's next full page form a set of their own.  Its pages go on from there to
-//   end = min over its members s of min(full_s, full_leader, first page where the rows of s and of the leader differ),
+//   end = min over its members s of min(full_s, full_leader, first page where the rows of s and of the leader differ or hold no block),
 // and with two members and min_pages pages it becomes ceil(n / 64) groups, member of rank r in part ((r + 1) k - 1) / n.
 //
 // Bound by latency: three levels one after the other, each a hash table in shared memory, a comparison of rows, prefix sums and the
@@ -46,10 +46,11 @@ struct PrefixShared {
     Two part[33];
 };
 
-// The first page of [from, limit) where two rows differ, or limit: by a warp, with LOADS loads of either row in flight in a
-// lane.  (Four int4 where both rows start on 16 bytes took as long; twelve entries 4 us more for 1024 long rows.)
+// The first page of [from, limit) where two rows differ or hold no block (one of `nb`), or limit: by a warp, with kLoads loads of either
+// row in flight in a lane.  (Four int4 where both rows start on 16 bytes took as long; twelve entries 4 us more for 1024 long rows, and a
+// flag set in here for entries that are no blocks 6 us.)
 constexpr int kLoads = 8;
-__device__ __forceinline__ int first_difference(const int32_t *a, const int32_t *b, int from, int limit) {
+__device__ __forceinline__ int first_difference(const int32_t *a, const int32_t *b, int from, int limit, int nb) {
     const int lane = threadIdx.x & 31;
     for (int p = from; p < limit; p += 32 * kLoads) {
         int va[kLoads], vb[kLoads];
@@ -61,7 +62,7 @@ __device__ __forceinline__ int first_difference(const int32_t *a, const int32_t 
         }
 #pragma unroll
         for (int j = 0; j < kLoads; ++j) {
-            const unsigned m = __ballot_sync(0xffffffffu, va[j] != vb[j]);
+            const unsigned m = __ballot_sync(0xffffffffu, va[j] != vb[j] || static_cast<unsigned>(va[j]) >= static_cast<unsigned>(nb));
             if (m) return p + 32 * j + __ffs(m) - 1;
         }
     }
@@ -156,7 +157,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) prefix_plan_kernel(const Pref
             if (j < 0 || j == i) continue;
             const int limit = min(sh.full[i], sh.full[j]);
             const int e = first_difference(a.table + static_cast<int64_t>(i) * a.max_blocks, a.table + static_cast<int64_t>(j) * a.max_blocks,
-                                           sh.page[i] + 1, limit);
+                                           sh.page[i] + 1, limit, a.nb);
             if (tid % 32 == 0) atomicMin(ends + level * LLA_MAX_BATCH + j, e);
         }
         sync_all();
@@ -205,6 +206,11 @@ __global__ void __launch_bounds__(kPlanThreads, 1) prefix_plan_kernel(const Pref
             lead = lead_new;
         }
         __syncthreads();
+    }
+    // the page behind the last level's pages (a level looks at those behind the ones of the level before it)
+    if (alive && full > page && rank == 0) {
+        const int block = a.table[static_cast<int64_t>(tid) * a.max_blocks + page];
+        if (block < 0 || block >= a.nb) atomicOr(a.err, LLA_DEVERR_BLOCK_ID);
     }
     // what no group holds
     const int at = rank * kPlanThreads + tid, step = ctas * kPlanThreads;
