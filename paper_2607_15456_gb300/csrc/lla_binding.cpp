@@ -432,16 +432,18 @@ PyObject *decode_attn_decoupled_axes(PyObject *, PyObject *const *a, Py_ssize_t 
     return guarded(n, 18, [&] {
         const lla_geometry g = geometry(a[0]);
         const lla_codec cd = codec(a[1]);
-        const lla_cache ch = cache(a[2]);
         void *pool = address(a[3]);
         const int32_t dr = integer32(a[4]);
         const lla_rope_axes rp = rope_axes(a[5]);
-        const at::Tensor &q = tensor(a[10]), &ws = tensor(a[16]);
-        if (q.dim() < 1) throw Unusual();
+        const at::Tensor &q = typed(a[10], tensor(a[10]).scalar_type()), &ws = scratch(a[16]);
+        if (q.dim() != 3 || q.size(1) != g.H || q.size(2) != g.d) throw Unusual();
         const int32_t B = size32(q.size(0));
-        const auto *pos = typed_ptr<int32_t>(a[6], at::kInt, LLA_ROPE_AXES, B), *ctx = static_cast<const int32_t *>(address(a[7]));
+        const lla_cache ch = cache_of(a[2], B);
+        const auto *pos = typed_ptr<int32_t>(a[6], at::kInt, LLA_ROPE_AXES, B), *ctx = typed_ptr<int32_t>(a[7], at::kInt, B);
         const int32_t max_ctx = integer32(a[8]), loop = integer32(a[9]);
-        void *qr = address(a[11]), *ck = address(a[12]), *cv = address(a[13]), *ckr = address(a[14]), *out = address(a[15]);
+        const at::ScalarType t = q.scalar_type();
+        void *qr = values(a[11], t, B, g.H, dr), *ck = values(a[12], t, B, g.H, g.d), *cv = values(a[13], t, B, g.H, g.d);
+        void *ckr = values(a[14], t, B, dr), *out = values(a[15], t, B, g.H, g.d);
         void *w = ws.data_ptr(), *qp = q.data_ptr();
         const lla_dtype io = dtype(q);
         const size_t wb = nbytes(ws);

@@ -665,13 +665,13 @@ def lla_decode_attn_decoupled_axes(geom: Geometry, codec: Codec, cache: Cache, r
             geom, codec, cache, rope_pool, d_rope, rope, positions, context_lens, max_ctx, loop, q, q_rope, cur_k, cur_v,
             cur_k_rope, out, workspace, _handle(stream))):
         return
+    _decode_check(geom, cache, context_lens, q, q_rope, cur_k, cur_v, cur_k_rope, out, d_rope)
     g, cd, ch, rp = geom.c(), codec.c(), cache.c(), rope.c()
     B = q.shape[0]
     _check("lla_decode_attn_decoupled_axes", library().lla_decode_attn_decoupled_axes(
         ctypes.byref(g), ctypes.byref(cd), ctypes.byref(ch), _ptr(rope_pool), d_rope, ctypes.byref(rp),
         _typed(positions, torch.int32, "positions", (3, B)), _ptr(context_lens), B, max_ctx, loop, _ptr(q), _ptr(q_rope),
-        _ptr(cur_k), _ptr(cur_v), _ptr(cur_k_rope), _dtype_code(q), _ptr(out), _ptr(workspace),
-        workspace.numel() * workspace.element_size(), _stream(stream)))
+        _ptr(cur_k), _ptr(cur_v), _ptr(cur_k_rope), _dtype_code(q), _ptr(out), *_scratch(workspace), _stream(stream)))
 
 
 def lla_dense_store(geom: Geometry, cache: Cache, k: torch.Tensor, v: torch.Tensor,
@@ -940,8 +940,8 @@ def lla_decode_prefix_workspace_size(geom: Geometry, B: int, d_rope: int = 0) ->
     return out.value
 
 
-def _decode_prefix_check(geom: Geometry, cache: Cache, context_lens, q, q_rope, cur_k, cur_v, cur_k_rope, out, d_rope):
-    """The shapes and types of a prefix decode's arrays (its callers give the addresses)."""
+def _decode_check(geom: Geometry, cache: Cache, context_lens, q, q_rope, cur_k, cur_v, cur_k_rope, out, d_rope):
+    """The shapes and types of a decode's arrays (its callers give the addresses)."""
     B, shape = q.shape[0], (q.shape[0], geom.H, geom.d)
     for t, name in ((q, "q"), (cur_k, "cur_k"), (cur_v, "cur_v"), (out, "out")):
         _typed(t, q.dtype, name, shape)
@@ -959,7 +959,7 @@ def lla_decode_attn_prefix(geom: Geometry, codec: Codec, cache: Cache, plan: Pre
     if _done("lla_decode_attn_prefix", _native().decode_attn_prefix(
             geom, codec, cache, plan, context_lens, max_ctx, loop, q, cur_k, cur_v, out, workspace, _handle(stream))):
         return
-    _decode_prefix_check(geom, cache, context_lens, q, None, cur_k, cur_v, None, out, 0)
+    _decode_check(geom, cache, context_lens, q, None, cur_k, cur_v, None, out, 0)
     B = q.shape[0]
     g, cd, ch, pl = geom.c(), codec.c(), cache.c(), plan.c(B)
     _check("lla_decode_attn_prefix", library().lla_decode_attn_prefix(
@@ -978,7 +978,7 @@ def lla_decode_attn_prefix_decoupled(geom: Geometry, codec: Codec, cache: Cache,
             geom, codec, cache, plan, rope_pool, d_rope, rope, positions, context_lens, max_ctx, loop, q, q_rope, cur_k, cur_v,
             cur_k_rope, out, workspace, _handle(stream))):
         return
-    _decode_prefix_check(geom, cache, context_lens, q, q_rope, cur_k, cur_v, cur_k_rope, out, d_rope)
+    _decode_check(geom, cache, context_lens, q, q_rope, cur_k, cur_v, cur_k_rope, out, d_rope)
     B = q.shape[0]
     g, cd, ch, pl, rp = geom.c(), codec.c(), cache.c(), plan.c(B), rope.c()
     _check("lla_decode_attn_prefix_decoupled", library().lla_decode_attn_prefix_decoupled(
