@@ -1447,8 +1447,8 @@ __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(const __grid_cons
                 qk = fmaf(load_elem(a.q_rope, row * a.d_rope + i, a.io_bf16), load_elem(a.cur_k_rope, static_cast<int64_t>(b) * a.d_rope + i, a.io_bf16), qk);
             qk = warp_sum(qk) * a.scale_log2;
         }
-        // The first item twice: at first with a run of anything, and without an output, while the kernels before still run, so that the
-        // instructions are there when the records are (fetched behind the wait they took longer than the join).
+        // The first item twice: at first with weights in the place of a record, and without an output, while the kernels before still
+        // write theirs, so that the instructions are there when the records are (fetched behind the wait they took longer than the join).
 #pragma unroll 1
         for (int dry = item == i0; dry >= 0; --dry) {
             if (item == i0 && dry == 0) {
@@ -1473,9 +1473,11 @@ __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(const __grid_cons
                 first = static_cast<int>(record_of(p, d, h, c0)) + rank;
                 step = is_leaf(p, d) ? p.leaf_max : p.trunk_max;
             }
-            if (dry) {  // (one run, the first record: whatever it holds)
+            const float *part = p.part;
+            if (dry) {  // (one run; a head's weights are many records long)
                 runs = lane == kLevels;
                 first = step = 0;
+                part = static_cast<const float *>(a.w_up_v);
             }
             int upto[kLevels + 1];  // runs of the nodes up to each
 #pragma unroll
@@ -1496,14 +1498,14 @@ __global__ void __launch_bounds__(kJoinThreads, 2) join_kernel(const __grid_cons
                             in = r - upto[k];
                         }
                     const int rec = __shfl_sync(0xffffffffu, first, level) + in * __shfl_sync(0xffffffffu, step, level);
-                    const float2 ml = *reinterpret_cast<const float2 *>(p.part + static_cast<int64_t>(rec) * RS + RV);
+                    const float2 ml = *reinterpret_cast<const float2 *>(part + static_cast<int64_t>(rec) * RS + RV);
                     constexpr int KR = 6;  // runs whose loads are in flight together, the first of them beside their maxima and sums
                     float4 v[KR];
                     float t[KR];
                     auto load = [&](int k0) {
 #pragma unroll
                         for (int k = 0; k < KR; ++k) {
-                            const float *pr = p.part + static_cast<int64_t>(__shfl_sync(0xffffffffu, rec, min(k0 + k * G, nr - 1))) * RS;
+                            const float *pr = part + static_cast<int64_t>(__shfl_sync(0xffffffffu, rec, min(k0 + k * G, nr - 1))) * RS;
                             v[k] = lane * 4 < RV ? *reinterpret_cast<const float4 *>(pr + lane * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
                             t[k] = RV > 128 ? pr[128 + lane] : 0.f;
                         }
