@@ -11,7 +11,7 @@
 // current token:
 //   o = (W_up,t^V sum_j w_j o~_j + (sum_j w_j l_j) mu^V_t + w_cur v_cur) / (sum_j w_j l_j + w_cur),  w_j = e^(m_j - M).
 //
-// Four launches on the caller's stream, chained by programmatic dependent launch (three for up to four sequences):
+// Four launches on the caller's stream, chained by programmatic dependent launch (three for few sequences, see leaf_alone):
 //   absorb_kernel  q~ (scaled into the exp2 domain) and beta of every (sequence, head); the prefix sums of the nodes' pages and
 //                  the checks of lengths and plan
 //   trunk_kernel   nodes of more than kLeaf queries, one CTA per SM.  Their pages, unit by unit in the order of the nodes, are
@@ -69,7 +69,7 @@ constexpr int kMaxNodes = kLevels * (LLA_MAX_BATCH / 2) + LLA_MAX_BATCH;
 constexpr int kTrunkThreads = 512;
 constexpr int kSoftmaxWarp = 4, kAuxWarp = 12;
 constexpr int kLeaf = 2;         // most queries of a node that the leaf kernel takes beside a trunk kernel
-constexpr int kLeafAlone = 4;    // and without one: most sequences of a call that has none
+constexpr int kLeafAlone = 4;    // and without one: most sequences of a call that has none (see leaf_alone)
 constexpr int kMaxGrid = 256;
 constexpr int kJoinSeqs = 16;    // most sequences of a head that the join works on together
 constexpr int kSmemCap = 227 * 1024;
@@ -1609,18 +1609,25 @@ struct PrefixWorkspace {
 
 inline size_t al256(size_t x) { return (x + 255) & ~static_cast<size_t>(255); }
 
-// Queries of a node of either kind, at most, for B sequences.  No group of up to kLeafAlone sequences has more members than the leaf
-// kernel can take: no trunk kernel then.
-struct NodeSizes {
-    int leaf_max, trunk_max;
-    explicit NodeSizes(int B) : leaf_max(B <= kLeafAlone ? std::max(B, 1) : kLeaf), trunk_max(B <= kLeafAlone ? 0 : std::min(B, kMembers)) {}
-};
+// Whether a call goes without a trunk kernel: no group of up to kLeafAlone sequences has more members than the leaf kernel can take,
+// and one of two never more than it takes beside a trunk.  For three and four the leaf kernel alone is faster over short contexts (us, four
+// sequences over one prompt of 768 / 4096 / 16384 / 65536 / 262144 tokens, alone and with a trunk kernel):
+//   16 heads               16.5  24.9  47.5  102  332     26.2  31.1  45.5  104  328
+//   2 heads                14.6  17.6  27.2   61  107     21.4  24.6  27.5   38   67
+//   16 heads, d_rope 64    17.4  29.1  59.9  148  512     26.3  34.1  52.7  127  414
+constexpr int kAloneTokens = 16384;
+bool leaf_alone(int B, int max_ctx) { return B <= kLeaf || (B <= kLeafAlone && max_ctx <= kAloneTokens); }
 
-PrefixWorkspace prefix_workspace(int rkt, int r_v, int B, int H, int grid, int leaf_warps) {
+// Queries of a node of either kind, at most, of B sequences.
+int leaf_queries(int B, bool alone) { return alone ? std::max(B, 1) : kLeaf; }
+int trunk_queries(int B) { return B <= kLeaf ? 0 : std::min(B, kMembers); }
+
+// For B sequences on either path: `warps` and `warps_alone` are the leaf kernel's on an SM.
+PrefixWorkspace prefix_workspace(int rkt, int r_v, int B, int H, int grid, int warps, int warps_alone) {
     PrefixWorkspace w;
-    const NodeSizes n(B);
-    w.leaf = n.trunk_max > 0 ? static_cast<size_t>(H) * kLevels * B + static_cast<size_t>(n.trunk_max) * grid : 0;
-    const size_t records = w.leaf + static_cast<size_t>(H) * (kLevels + 1) * B + static_cast<size_t>(n.leaf_max) * (1 + kLeafRest) * leaf_warps * grid;
+    w.leaf = trunk_queries(B) > 0 ? static_cast<size_t>(H) * kLevels * B + static_cast<size_t>(trunk_queries(B)) * grid : 0;
+    const int of_shares = std::max(trunk_queries(B) > 0 ? leaf_queries(B, false) * warps : 0, leaf_alone(B, 0) ? leaf_queries(B, true) * warps_alone : 0);
+    const size_t records = w.leaf + static_cast<size_t>(H) * (kLevels + 1) * B + static_cast<size_t>(of_shares) * (1 + kLeafRest) * grid;
     w.part = 0;
     w.qt = al256(records * record_floats(r_v) * sizeof(float));
     w.qf = w.qt + al256(static_cast<size_t>(B) * H * 3 * rkt * sizeof(uint16_t));
@@ -1643,9 +1650,7 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     if (a.num_blocks * a.H >= (int64_t(1) << 31)) return LLA_ERR_UNSUPPORTED;  // TMA coordinate
     using LL = L<RK, RV, DR, false>;
     using LA = L<RK, RV, DR, true>;
-    const NodeSizes sizes(a.B);
-    const bool alone = sizes.trunk_max == 0;
-    const PrefixWorkspace w = prefix_workspace(ZZ::RKT, RV, a.B, a.H, grid, alone ? LA::WARPS : LL::WARPS);
+    const PrefixWorkspace w = prefix_workspace(ZZ::RKT, RV, a.B, a.H, grid, LL::WARPS, LA::WARPS);
     if (a.workspace_bytes < w.total) return LLA_ERR_WORKSPACE;
     char *ws = static_cast<char *>(a.workspace);
     static DeviceOnce configured, configured_leaf, configured_alone;
@@ -1674,11 +1679,11 @@ lla_status launch_prefix(const DecodeArgs &a, const lla_prefix &plan, const void
     tp.pstart = reinterpret_cast<int *>(ws + w.pstart);
     tp.next = tp.pstart + 2 * (kMaxNodes + 1);
     tp.leaf = static_cast<int64_t>(w.leaf);
-    // Four sequences over 768 tokens take 16.1 us without a trunk kernel, 25.0 with it in the chain.  Beside one, leaves of up to four queries need registers that the join's CTA
-    // holds: 64 sequences over 16 prompts, all of them leaves then, take 107 us instead of 109, but 128 samples of 8 documents 105
-    // instead of 97, and of two videos 149 instead of 140.
-    tp.leaf_max = sizes.leaf_max;
-    tp.trunk_max = sizes.trunk_max;
+    // Beside a trunk kernel, leaves of up to four queries need registers that the join's CTA holds: 64 sequences over 16 prompts, all of
+    // them leaves then, take 107 us instead of 109, but 128 samples of 8 documents 105 instead of 97, and of two videos 149 instead of 140.
+    const bool alone = leaf_alone(a.B, a.max_ctx);
+    tp.leaf_max = leaf_queries(a.B, alone);
+    tp.trunk_max = trunk_queries(a.B);
     tp.err = err;
 
     AbsorbParams ap = {};
@@ -1735,7 +1740,7 @@ size_t decode_prefix_workspace_bytes(int r_k, int r_v, int d_rope, int B, int H)
 #define LLA_PREFIX(K, V, R) \
     if (r_k == K && r_v == V && d_rope == R) \
         return prefix_workspace(Z<K, V, R, false>::RKT, V, B, H, grid, \
-                                NodeSizes(B).trunk_max == 0 ? L<K, V, R, true>::WARPS : L<K, V, R, false>::WARPS).total;
+                                L<K, V, R, false>::WARPS, L<K, V, R, true>::WARPS).total;
     LLA_PREFIX_SHAPES(LLA_PREFIX)
 #undef LLA_PREFIX
     return 0;
