@@ -717,8 +717,8 @@ lla_status lla_decode_prefix_workspace_size(const lla_geometry *g, int32_t d_rop
  * Other arguments and the error behaviour are those of lla_decode_attn.  Storage LLA_BF16, d = 128, (r_k, r_v) one of
  * (96, 160), (128, 128), (72, 120); LLA_ERR_UNSUPPORTED otherwise.  q~ enters the products as the sum of three bf16 numbers,
  * the softmax weights as three for fp32 outputs, as two for bf16: 24 and 16 bits.  The tensor cores' additions are cut off, not
- * rounded: a sum of one sign may come out smaller by 4e-6 of itself for fp32 outputs and by 1.6e-5 before the rounding of bf16
- * ones, at any length.  Three or four kernels on the stream.
+ * rounded: a sum of one sign may come out smaller by 4e-6 of itself for fp32 outputs and by 4e-5 before the rounding of bf16 ones,
+ * at any length.  Three or four kernels on the stream.
  */
 lla_status lla_decode_attn_prefix(const lla_geometry *g, const lla_codec *codec, const lla_cache *cache,
                                   const lla_prefix *plan, const int32_t *context_lens, int32_t B, int32_t max_ctx,

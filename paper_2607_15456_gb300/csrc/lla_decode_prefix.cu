@@ -15,7 +15,7 @@
 //   absorb_kernel  q~ (scaled into the exp2 domain) and beta of every (sequence, head); the prefix sums of the nodes' pages and
 //                  the checks of lengths and plan
 //   trunk_kernel   nodes of more than kLeaf queries, one CTA per SM.  Their pages, unit by unit in the order of the nodes, are
-//                  split evenly over the CTAs; a CTA takes its pages as runs (its part of one unit).  A page is two products on
+//                  split evenly over the CTAs; a CTA takes its pages as runs (parts of one unit).  A page is two products on
 //                  the tensor cores, with 128 rows for the up to 64 queries of a run, each of them 2, 4 or 8 times:
 //                    S [128 x 64 tokens] = sum_i Q~_i [C_k | K^R]^T      i = 2, 1, 0: q~ as three bf16 parts, in TMEM
 //                    O [128 x r_v]      += P C_v                         P in TMEM
@@ -34,8 +34,8 @@
 //                                  runs before it have left there
 //                  Bound by HBM and, at run ends, by latency: 393 MB of pages that 4 sequences each share take 74 us (5.3 TB/s),
 //                  287 MB that 64 share 73 us, with the tensor pipe busy for 55 % and the step from S to P for the rest
-//   leaf_kernel    nodes of up to kLeaf queries, which are short (a sequence's own pages): one page at a time in each of as
-//                  many warps as pages fit in an SM's shared memory beside a CTA of the join, on the CUDA cores.  It starts on
+//   leaf_kernel    nodes of up to kLeaf queries (a sequence's own pages; all nodes where there is no trunk kernel): one page at a time in
+//                  each of as many warps as pages fit in an SM's shared memory beside a CTA of the join, on the CUDA cores.  It starts on
 //                  each SM as the trunk kernel leaves it.  Bound by HBM while all warps run (6 TB/s)
 //   join_kernel    per head and up to 16 sequences: joins the runs of each sequence's nodes and the current token, and applies
 //                  W_up,t^V once for all of them.  One CTA per SM, beside the leaf kernel's, so that the weights and the
@@ -62,7 +62,7 @@ namespace {
 
 constexpr int kPT = 64;          // tokens per page
 constexpr int kD = 128;          // head width
-constexpr int kRows = 128;       // rows of the products: every query twice
+constexpr int kRows = 128;       // rows of the products: every query 2, 4 or 8 times
 constexpr int kLevels = LLA_PREFIX_LEVELS;
 constexpr int kMembers = LLA_PREFIX_MEMBERS;
 constexpr int kMaxNodes = kLevels * (LLA_MAX_BATCH / 2) + LLA_MAX_BATCH;
@@ -186,10 +186,11 @@ struct Split {
 // joins the runs of a unit in fp32, in the CTA's record of it.  The tensor cores cut off what an addition leaves behind the last bits of
 // O, all to one side, so that a sum loses the more the larger it gets.  Measured on sums of one sign, mean over the outputs of 64
 // queries: 1.6e-6 of themselves with 24 pages, 9.9e-6 with 64, 2.9e-5 with 128 (of 20 queries, whose rows hold fewer tokens, 0.5, 2.9 and
-// 9.5e-6).  fp32 outputs: 24; 64 samples of two videos, d_rope 64, take 173 us so, 178 with 16, 169 with 40.  bf16 outputs: 64,
-// where the loss is 1/400 of their rounding; with 24 the same call takes 149 us instead of 138.
+// 9.5e-6).  fp32 outputs: 24; 64 samples of two videos, d_rope 64, take 174 us so, 178 with 16, 169 with 40.  bf16 outputs: 128, where
+// the loss is 1/130 of their half steps of up to 2^-8; 64 samples of 65536 tokens take 116 us so, and 125 with 64.  (A run that
+// ends a CTA's share waits for the record that it is joined with, 7 us for 64 queries.)
 template <bool FP32>
-constexpr int kRunPages = FP32 ? 24 : 64;
+constexpr int kRunPages = FP32 ? 24 : 128;
 
 // The shares that the pages of the leaves are split into, for `workers` warps: one each of kLeafFirst / 8 of the pages, and the
 // rest in up to kLeafRest as many small ones, which the warps take as they get there.  A share's record does not depend on the
