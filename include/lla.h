@@ -402,8 +402,10 @@ lla_status lla_decode_attn_decoupled(const lla_geometry *g, const lla_codec *cod
  * Rotary positions on up to three axes (time, height and width of images and video): every token has a
  * position on each axis, and pair j of the rotary branch is turned by
  *   positions[axis(j)] * base^(-2j/d_rope).
- * A text token has one position on all axes.  pairs[a] >= 0 is the number of pairs of axis a; their sum must be
- * d_rope / 2.
+ * A text token has one position on all axes.  pairs[a] >= 0, with the sum d_rope / 2: in blocks the number of pairs of axis a.
+ * Interleaved, axes 1 and 2 have at most pairs[1] and pairs[2], and axis 0 what is left: every third pair is an axis's own,
+ * so that a count above d_rope / 6 cannot be reached (d_rope 32 and (0, 8, 8) give 6, 5 and 5 pairs, d_rope 96 and (16, 16, 16) as
+ * many of each).
  */
 #define LLA_ROPE_AXES 3
 
@@ -646,8 +648,9 @@ lla_status lla_pages_compact(const lla_pages *pages, const lla_pool *pools, int3
  * first keep[i] tokens are those of sequence parents[i] (-1: of none, then keep[i] is 0), which keeps them: the
  * keep / 64 full pages are shared, the keep % 64 rows of the next one are copied in every pool into a block of its own,
  * and the rest are fresh blocks, all of them the free ones of the lowest numbers in the order of the requests.
- * The block tables, lengths and slots that the encodes and prefills of the new tokens take come out on the device, so
- * that admission needs no round trip to the host.
+ * The block tables, lengths and slots that the encodes of the new tokens take come out on the device, so that admission
+ * needs no round trip to the host.  (The prefill calls attend from position 0 of a prompt: they fit requests that keep
+ * nothing.  New tokens behind a kept part are attended to by the decode calls, token by token.)
  *   rows, parents, keep, new_lens
  *                 device [n] int32; 0 <= keep[i] <= context_lens[parents[i]], keep[i] <= new_lens[i]
  *   slot_mapping  device [N] int64, written: the slots of the requests' new tokens, packed; -1 behind cu_new[n]
@@ -694,7 +697,10 @@ typedef struct {
  * Fills `plan` for B sequences of `cache` (its block table and num_blocks; the pool is not read and may be NULL).  A plan
  * holds as long as the pages it names stay in the rows it was made from: tokens may be appended, so it has to be made again
  * only when sequences come, go or move (and should be when many pages more could be shared).
- *   min_pages  pages that a set must share to become a group, >= 1
+ *   min_pages  pages that a set must share to become a group, >= 1.  A set whose members part early ends there for all of them, and
+ *              a level is used up.  Groups of one page cost more than they save (512 sequences in groups of three over one page:
+ *              152 us a decode, 111 without them); two pages pay for themselves in batches of hundreds (129 against 131 in
+ *              groups of eight, 103 against 122 in groups of 64), four in batches of 64 (33 against 36)
  * A length out of range sets LLA_DEVERR_CONTEXT: such a sequence shares nothing.  A set's pages end before an entry that is no
  * block; LLA_DEVERR_BLOCK_ID is set where that is the first full page of a sequence, or the one behind the pages of a group that it is in.
  * One kernel on the stream.
@@ -714,6 +720,15 @@ lla_status lla_decode_prefix_workspace_size(const lla_geometry *g, int32_t d_rop
  *              LLA_DEVERR_CONTEXT and is not read
  *   workspace  >= lla_decode_prefix_workspace_size bytes, 16-byte aligned; needs no initialisation; calls that share it must
  *              be ordered
+ * It pays where several sequences share thousands of tokens, or many share hundreds; lla_decode_attn is the faster call for few
+ * sequences over short prompts and where nothing is shared (us, 16 heads, r 96 + 160, bf16, this call / lla_decode_attn):
+ *                                    4 sequences    8            16           64           128
+ *   one prompt of    256 tokens      15.8 / 15.9   23.3 / 15.5  25.8 / 18.8  32.3 / 45.8  40.7 / 88.8
+ *                    768             16.5 / 16.2   25.6 / 17.3  28.3 / 23.4  37.1 / 69.3  44.6 / 135
+ *                   2048             18.6 / 19.4   29.2 / 26.4  34.5 / 42.2  40.6 / 144   48.8 / 283
+ *                   4096             24.9 / 26.1   33.5 / 40.9  37.3 / 71.8  42.7 / 263   52.6 / 521
+ *                  16384             45.3 / 70.7   48.5 / 130   52.0 / 251   57.5 / 979   79.3 / 1950
+ *   4096 tokens each, none shared    33.5 / 29.1   -            90.9 / 85.9  321 / 312    -
  * Other arguments and the error behaviour are those of lla_decode_attn.  Storage LLA_BF16, d = 128, (r_k, r_v) one of
  * (96, 160), (128, 128), (72, 120); LLA_ERR_UNSUPPORTED otherwise.  q~ enters the products as the sum of three bf16 numbers,
  * the softmax weights as three for fp32 outputs, as two for bf16: 24 and 16 bits.  The tensor cores' additions are cut off, not

@@ -33,7 +33,7 @@
 //                                  shared memory, its maxima and its sums to the workspace, joined with what the unit's
 //                                  runs before it have left there
 //                  Bound by HBM and, at run ends, by latency: 393 MB of pages that 4 sequences each share take 74 us (5.3 TB/s),
-//                  287 MB that 64 share 73 us, with the tensor pipe busy for 55 % and the step from S to P for the rest
+//                  287 MB that 64 share 70 us, with the tensor pipe busy for 58 % and the step from S to P for the rest
 //   leaf_kernel    nodes of up to kLeaf queries (a sequence's own pages; all nodes where there is no trunk kernel): one page at a time in
 //                  each of as many warps as pages fit in an SM's shared memory beside a CTA of the join, on the CUDA cores.  It starts on
 //                  each SM as the trunk kernel leaves it.  Bound by HBM while all warps run (6 TB/s)

@@ -6,8 +6,8 @@
 //   end = min over its members s of min(full_s, full_leader, first page where the rows of s and of the leader differ or hold no block),
 // and with two members and min_pages pages it becomes ceil(n / 64) groups, member of rank r in part ((r + 1) k - 1) / n.
 //
-// Bound by latency: three levels one after the other, each a hash table in shared memory, a comparison of rows, prefix sums and the
-// cluster's barriers.  12 us for 64 sequences; 26 for 1024 with up to 512 pages (39 with eight CTAs, atomics of every thread on its
+// Bound by latency: three levels one after the other, each a hash table in shared memory (of a size for the largest batch), a comparison
+// of rows, prefix sums, and the barriers of a CTA's 32 warps, or for many long rows a cluster's.  12.6 us for 64 sequences, by one CTA; 26 for 1024 with up to 512 pages (39 with eight CTAs, atomics of every thread on its
 // set's words, and rows compared one load at a time), of which reading 1.6 MB of table rows takes 0.3.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
